@@ -186,7 +186,7 @@ def prepare(case, seed):
         s["K"], s["V"] = (_rows(g, (count, kv, n, D), dt, ch) for ch in (True, False))
         b = _budgets(c, seed, count * kv)
         s["offsets"] = np.concatenate([[0], np.cumsum(b, dtype=np.int64)])
-        rows = int(s["offsets"][-1])
+        s["rows_at"], rows = torch.from_numpy(s["offsets"]).cuda(), int(s["offsets"][-1])
         # kept tokens of every head, ascending: those whose score is among the head's `budget` largest
         order = torch.rand((count * kv, n), generator=g, device="cuda").argsort(1).argsort(1)
         s["indices"] = (order < torch.from_numpy(b).cuda()[:, None]).nonzero()[:, 1].to(torch.int32)
@@ -231,9 +231,10 @@ def run(s):
                    n_sink=c["sinks"], lse=s["lse"])
         return {"out": s["out"], "lse": s["lse"]}
     if c["op"] == "pack":
-        ctx.compact_mx(s["K"], s["V"], c["n"], s["indices"], s["offsets"], s["K_codes"], s["K_scales"], s["V_codes"], s["V_scales"])
+        rows = s["K_out"].shape[0]
+        ctx.compact_mx(s["K"], s["V"], c["n"], s["indices"], s["rows_at"], rows, s["K_codes"], s["K_scales"], s["V_codes"], s["V_scales"])
         for t in "KV":
-            ctx.expand_mx(s[t + "_codes"], s[t + "_scales"], s["K_out"].shape[0], s[t + "_out"])
+            ctx.expand_mx(s[t + "_codes"], s[t + "_scales"], rows, s[t + "_out"])
         return {"K": s["K_out"], "V": s["V_out"]}
     since = dict(K_tail=s["K_tail"], V_tail=s["V_tail"], tail_n=c["tail"], tail_stride=c["tail"], tail_lengths=s["lengths"], lse=s["lse"])
     if c["mx"]:

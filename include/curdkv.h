@@ -56,6 +56,8 @@ extern "C" {
 #define CURDKV_ERR_OOM         -4   /* device or host allocation failed */
 #define CURDKV_ERR_TOO_LARGE   -5   /* more (layer, group) pairs than a non-allocating call's fixed workspace holds */
 
+#define CURDKV_ATTEND_SCRATCH_BYTES 34078720   /* most scratch that an attention call uses (65536 rows of 520 bytes) */
+
 #define CURDKV_DTYPE_F32  0
 #define CURDKV_DTYPE_BF16 1
 
@@ -248,6 +250,104 @@ int curdkv_scores_append(curdkv_ctx* ctx, const void* K_new, const void* V_new, 
  * goes to curdkv_select / curdkv_adaptive_budgets. */
 int curdkv_normalise(curdkv_ctx* ctx, const float* raw, const double* sums, int64_t stride,
                      int64_t n, float* scores, void* stream);
+
+/* ---- around a compressed cache: its rows made, attended to, and held in 4 bits ----
+ *
+ * These calls take one layer at a time: `count` sequences of that layer, kv_heads,
+ * group_size, head_dim and dtype those of the context (its layers, sketches and seed play
+ * no part).  A layer's cache is [count, kv_heads, stride, head_dim] in the storage type:
+ * row j of head h of sequence b starts at element ((b*kv_heads + h)*stride + j)*head_dim
+ * (a contiguous cache of n tokens, as the calls above take it, has stride = n).  Queries
+ * and results are token-major, [count, m, kv_heads*group_size, head_dim], query head
+ * h*group_size + i belonging to KV head h.  Device pointers to rows, codes and tables are
+ * 16-byte aligned.  Arrays of lengths, rows and positions are device memory and are not
+ * looked at on the host: what lies outside the stated ranges is clamped or left out as
+ * said, and nothing is read or written outside the buffers. */
+
+/* Norms of queries and keys for each head, their rotation by position, and the new rows of
+ * the cache, from a layer's projections.
+ * qkv: device, count*m rows of (group_size + 2)*kv_heads heads of head_dim values in the
+ *   storage type: queries, then keys, then values; row_stride elements from one row to the
+ *   next (at least (group_size + 2)*kv_heads*head_dim, a multiple of 16 bytes).  Row b*m + i
+ *   is token i of sequence b.
+ * starts: int32 [count], the cache row of a sequence's first new token; NULL = 0.  Tokens
+ *   whose row lies outside [0, stride) leave the cache as it is.
+ * positions: int32 [count*m]; NULL = the token's cache row.  Clamped to [0, table_rows).
+ * table: float [table_rows, 2, head_dim/2]: cosines, then sines, of a position's angles.
+ * q_weight, k_weight: storage type [head_dim]: y = x / sqrt(mean(x^2) + eps) * weight
+ *   before the rotation; NULL = no norm of queries / of keys.
+ * pairs: 0: channels i and head_dim/2 + i turn together, 1: channels 2i and 2i + 1, by
+ *   (a, b) -> (a cos - b sin, b cos + a sin) of angle i.
+ * Q: written [count, m, kv_heads*group_size, head_dim]; K, V: the layer's cache, of which
+ *   the new tokens' rows are written (values as they are).  Nothing may overlap qkv.
+ * 32 bits throughout, rounded once at the store.  stride <= max_tokens. */
+int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride,
+                  const int32_t* starts, const int32_t* positions, const float* table,
+                  int64_t table_rows, const void* q_weight, const void* k_weight, float eps,
+                  int32_t pairs, void* Q, void* K, void* V, int64_t stride, void* stream);
+
+/* Causal attention of each sequence's last m tokens over its cache, with an optional window
+ * and first tokens that stay visible: of a sequence of `length` tokens, new token i stands at
+ * position p = length - m + i and sees row j where j <= p and (window == 0 or p - j < window
+ * or j < n_sink);
+ *   out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log sum_j exp(scale * q.k_j).
+ * A token that sees nothing (length < m and i < m - length) gets zeros and -infinity; what a
+ * token does not see does not reach it, infinities and NaN included.
+ * lengths: int32 [count], clamped to [0, n]; NULL = n for all.  n <= stride, n <= max_tokens.
+ * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0.
+ * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits,
+ * with a bf16 cache the weights are rounded to bf16 for their product with V.
+ * scratch: device memory of the caller's, 16-byte aligned, for the partial results of few tokens over
+ *   long caches, whose heads are shared out over many workgroups; CURDKV_ATTEND_SCRATCH_BYTES
+ *   are as much as a call ever uses, with less (0 and NULL included) there are fewer shares.
+ *   Its contents mean nothing before or after; calls that overlap in time need one each. */
+int curdkv_attend(curdkv_ctx* ctx, const void* Q, const void* K, const void* V, int64_t count,
+                  int64_t m, int64_t n, int64_t stride, const int32_t* lengths, int64_t window,
+                  int32_t n_sink, float scale, void* out, float* lse, void* scratch,
+                  int64_t scratch_bytes, void* stream);
+
+/* The gather of curdkv_compact into 4 bits (the open microscaling format MXFP4): blocks of 32
+ * channels share a power of two 2^e, e = floor(log2(largest magnitude)) - 2, at least -127,
+ * and a value x is held as the nearest to x/2^e of 0, .5, 1, 1.5, 2, 3, 4, 6 with its sign (ties
+ * to the even code, beyond 6 to 6).  A block that holds an infinity or NaN stands for NaN.
+ * K, V, n, indices: as curdkv_compact takes them; offsets: the same, but in DEVICE memory
+ *   (curdkv_compress_adaptive leaves them there), and total = offsets[last], at most
+ *   layers*kv_heads*n.  An index outside [0, n) leaves its row unwritten.
+ * K_codes, V_codes: [offsets[last], head_dim/2], channel 2i in the low half of byte i;
+ * K_scales, V_scales: [offsets[last], head_dim/32], e + 127, or 255 for NaN. */
+int curdkv_compact_mx(curdkv_ctx* ctx, const void* K, const void* V, int64_t n,
+                      const int32_t* indices, const int64_t* offsets, int64_t total, uint8_t* K_codes,
+                      uint8_t* K_scales, uint8_t* V_codes, uint8_t* V_scales, void* stream);
+
+/* The values that rows in 4 bits stand for, in the storage type (exact): out [rows, head_dim]. */
+int curdkv_expand_mx(curdkv_ctx* ctx, const uint8_t* codes, const uint8_t* scales, int64_t rows,
+                     void* out, void* stream);
+
+/* Attention of m new tokens over the rows that a selection kept and over the tokens since:
+ * every new token sees all kept rows of its head, and, causally, the tail: of `length` tail
+ * tokens, new token i stands at p = length - m + i and sees tail rows j <= p (the new tokens'
+ * own rows are part of the tail).  out, lse, scale and scratch as in curdkv_attend.
+ * K_kept, V_kept: packed rows as the gathers write them; those of KV head h of sequence b are rows
+ *   offsets[b*kv_heads + h] .. offsets[b*kv_heads + h + 1] - 1.
+ * offsets: DEVICE int64 [count*kv_heads + 1], kept within [0, total]; a layer of a larger
+ *   packed cache is its slice of the offsets, with the whole cache's K_kept and V_kept.
+ * total: rows of K_kept and V_kept; rows: how many of them belong to this call's heads (all:
+ *   total).  The work is shared out by their average; uneven heads are read whole all the same.
+ * K_tail, V_tail: [count, kv_heads, tail_stride, head_dim]; tail_lengths: int32 [count], clamped
+ *   to [0, tail_n]; NULL = tail_n.  tail_n = 0: no tail (the pointers may be NULL). */
+int curdkv_attend_kept(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept,
+                       const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,
+                       const void* V_tail, int64_t tail_n, int64_t tail_stride, const int32_t* tail_lengths,
+                       int64_t count, int64_t m, float scale, void* out, float* lse, void* scratch,
+                       int64_t scratch_bytes, void* stream);
+
+/* The same over kept rows held in 4 bits (curdkv_compact_mx); the tail is in the storage type. */
+int curdkv_attend_kept_mx(curdkv_ctx* ctx, const void* Q, const uint8_t* K_codes,
+                          const uint8_t* K_scales, const uint8_t* V_codes, const uint8_t* V_scales,
+                          const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,
+                          const void* V_tail, int64_t tail_n, int64_t tail_stride,
+                          const int32_t* tail_lengths, int64_t count, int64_t m, float scale,
+                          void* out, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
 
 /* Text for an error code; never NULL. */
 const char* curdkv_strerror(int code);

@@ -1,0 +1,58 @@
+// Attention over a cache: what the kernels share.  Notation, for one KV head: its `group` query heads and m tokens make
+// rows R = token * group + head of the products' other side; token t of m stands at position p(t) = length - m + t.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "curdkv_internal.h"
+
+namespace curdkv {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
+typedef float f32x2a __attribute__((ext_vector_type(2)));
+typedef float f32x4a __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2a __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8a __attribute__((ext_vector_type(8)));
+
+constexpr float kLn2 = 0.693147180559945309f;
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2a{a, b}), bf16x2a));
+}
+
+// max / sum over the four lanes l, l^16, l^32, l^48
+__device__ __forceinline__ float quarters_max(float x) {
+    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float quarters_sum(float x) {
+    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r.x) + __uint_as_float(r.y);
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// The rows of a cache that some token of tokens t0 .. t1 (of the m new ones) sees: [0, first) and [low, high).
+struct Seen {
+    int first, low, high;
+    int p0, p1;                        // positions of t0 and t1
+};
+__device__ __forceinline__ Seen seen_rows(int length, int m, int t0, int t1, int window, int sinks) {
+    Seen s;
+    s.p0 = length - m + t0;
+    s.p1 = length - m + t1;
+    s.high = max(0, s.p1 + 1);
+    s.low = window > 0 && (int64_t)s.p0 - window + 1 > 0 ? min(s.p0 - window + 1, s.high) : 0;
+    s.first = min(sinks, s.low);
+    return s;
+}
+__device__ __forceinline__ bool sees(int p, int j, int window, int sinks) {
+    return j <= p && (window <= 0 || p - j < window || j < sinks);
+}
+
+}  // namespace curdkv

@@ -1,0 +1,113 @@
+// Rows of the cache in 4 bits (the open microscaling format): blocks of 32 channels share a power of two 2^e, stored as e + 127,
+//     e = floor(log2(largest magnitude)) - 2, at least -127,
+// and a channel x is held as the nearest to x 2^-e of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign (ties to the even code, beyond 6
+// to 6).  A block that holds an infinity or NaN has the scale 255 and stands for NaN.  64 bytes of codes, channel 2 i in the low
+// half of byte i, and 4 scales a row: 68 bytes instead of 256 (bf16) or 512.
+//
+// compact_mx_kernel is the gather of compact_kernels.hip with that at its end: HBM-bound, a row read whole by 16 (32) lanes of 16
+// bytes, K and V by different workgroups.  Four (eight) neighbouring lanes hold a block: two (three) DPP exchanges find its
+// largest magnitude, on the bits, where NaN counts as larger than all.  All steps are exact but the rounding to a code.
+
+#include "attend_device.h"
+#include "attend_internal.h"
+
+namespace curdkv {
+namespace {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void compact_mx_kernel(const u32x4a* __restrict__ K, const u32x4a* __restrict__ V, int64_t n,
+                                                         const int32_t* __restrict__ indices, const int64_t* __restrict__ offsets,
+                                                         int64_t total, int heads,
+                                                         uint8_t* __restrict__ K_codes, uint8_t* __restrict__ K_scales,
+                                                         uint8_t* __restrict__ V_codes, uint8_t* __restrict__ V_scales) {
+    constexpr int kLanes = BF16 ? 16 : 32, kRows = 256 / kLanes, kValues = BF16 ? 8 : 4;
+    const int c = threadIdx.x % kLanes;
+    const int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
+    if (p >= total) return;                                     // (whole rows of lanes)
+    const int32_t index = indices[p];
+    // The head that owns the workgroup's first row: the last one whose rows begin at or before it.  (Offsets out of order lead to
+    // a wrong head, never outside the cache.)
+    const int64_t p0 = (int64_t)blockIdx.x * kRows;
+    int h = 0;
+    for (int step = 1 << (31 - __builtin_clz(heads)); step; step >>= 1)
+        if (h + step < heads && offsets[h + step] <= p0) h += step;
+    while (h + 1 < heads && offsets[h + 1] <= p) ++h;
+    if (index < 0 || index >= n) return;                        // never read outside the cache
+    const u32x4a raw = __builtin_nontemporal_load((blockIdx.y ? V : K) + ((size_t)h * n + index) * kLanes + c);
+    float x[kValues];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+        const uint32_t bits = BF16 ? (i % 2 ? raw[i / 2] & 0xFFFF0000u : raw[i / 2] << 16) : raw[i % 4];
+        x[i] = __uint_as_float(bits);
+        most = max(most, bits & 0x7FFFFFFFu);
+    }
+    most = max(most, dpp<0xB1>(most));                          // quad_perm xor 1, xor 2
+    most = max(most, dpp<0x4E>(most));
+    if (!BF16) most = max(most, dpp<0x141>(most));              // mirror of eight lanes
+    const uint32_t field = most >> 23, e = field < 2 ? 0 : field - 2;      // e + 127
+    const bool finite = field < 255;
+    const float up = __uint_as_float((254u - e) << 23);         // 2^-e, exact
+    uint32_t codes = 0;
+    if (finite) {
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0] * up, x[1] * up, 1.f, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * up, x[3] * up, 1.f, 1);
+        if (BF16) {
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[kValues - 4] * up, x[kValues - 3] * up, 1.f, 2);
+            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[kValues - 2] * up, x[kValues - 1] * up, 1.f, 3);
+        }
+    }
+    uint8_t* to = (blockIdx.y ? V_codes : K_codes) + p * 64;
+    if (BF16) ((uint32_t*)to)[c] = codes;
+    else ((uint16_t*)to)[c] = (uint16_t)codes;
+    if (c % (kLanes / 4) == 0) (blockIdx.y ? V_scales : K_scales)[p * 4 + c / (kLanes / 4)] = finite ? (uint8_t)e : 255;
+}
+
+// What codes and scales stand for, 8 channels a thread.
+template <bool BF16>
+__global__ __launch_bounds__(256) void expand_mx_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t pieces,
+                                                        void* __restrict__ out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= pieces) return;
+    const uint32_t code = codes[i], e = scales[i / 4];
+    const float unit = __uint_as_float(e ? e << 23 : 1u << 22);             // (255: infinity, times code 0: NaN)
+    float x[8];
+    *(f32x2a*)(x + 0) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 0));
+    *(f32x2a*)(x + 2) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 1));
+    *(f32x2a*)(x + 4) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 2));
+    *(f32x2a*)(x + 6) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 3));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] *= unit;
+    if (BF16) {
+        ((u32x4a*)out)[i] = (u32x4a){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+    } else {
+        ((f32x4a*)out)[2 * i] = (f32x4a){x[0], x[1], x[2], x[3]};
+        ((f32x4a*)out)[2 * i + 1] = (f32x4a){x[4], x[5], x[6], x[7]};
+    }
+}
+
+}  // namespace
+
+hipError_t launch_compact_mx(const curdkv_ctx* ctx, const void* K, const void* V, int64_t n, const int32_t* indices, const int64_t* offsets,
+                             int64_t total, int heads, uint8_t* K_codes, uint8_t* K_scales, uint8_t* V_codes, uint8_t* V_scales, hipStream_t stream) {
+    const auto launch = [&](auto kernel, int rows) {
+        kernel<<<dim3((unsigned)((total + rows - 1) / rows), 2), 256, 0, stream>>>((const u32x4a*)K, (const u32x4a*)V, n, indices, offsets, total,
+                                                                                  heads, K_codes, K_scales, V_codes, V_scales);
+    };
+    if (ctx->cfg.dtype == CURDKV_DTYPE_BF16) launch(compact_mx_kernel<true>, 16);
+    else launch(compact_mx_kernel<false>, 8);
+    return hipGetLastError();
+}
+
+hipError_t launch_expand_mx(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows, void* out, hipStream_t stream) {
+    const int64_t pieces = rows * 16;
+    const unsigned blocks = (unsigned)((pieces + 255) / 256);
+    if (dtype == CURDKV_DTYPE_BF16) expand_mx_kernel<true><<<blocks, 256, 0, stream>>>((const uint32_t*)codes, scales, pieces, out);
+    else expand_mx_kernel<false><<<blocks, 256, 0, stream>>>((const uint32_t*)codes, scales, pieces, out);
+    return hipGetLastError();
+}
+
+}  // namespace curdkv

@@ -23,11 +23,13 @@ CALL_PATH = os.path.join(_HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX"
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_HIP, ERR_OOM, ERR_TOO_LARGE = 0, -1, -2, -3, -4, -5
 DTYPE_F32, DTYPE_BF16 = 0, 1
+ATTEND_SCRATCH_BYTES = 34078720
 _DTYPES = {"fp32": DTYPE_F32, "bf16": DTYPE_BF16}
 
 EXPORTS = ["curdkv_create", "curdkv_destroy", "curdkv_sketch_host", "curdkv_set_sketch",
            "curdkv_uses_fused_kernel", "curdkv_scores", "curdkv_fold", "curdkv_select", "curdkv_compact", "curdkv_compress",
-           "curdkv_adaptive_budgets", "curdkv_adaptive_budgets_noalloc", "curdkv_compress_adaptive", "curdkv_scores_append", "curdkv_normalise", "curdkv_strerror"]
+           "curdkv_adaptive_budgets", "curdkv_adaptive_budgets_noalloc", "curdkv_compress_adaptive", "curdkv_scores_append", "curdkv_normalise",
+           "curdkv_rotate", "curdkv_attend", "curdkv_compact_mx", "curdkv_expand_mx", "curdkv_attend_kept", "curdkv_attend_kept_mx", "curdkv_strerror"]
 
 
 class CurdkvConfig(C.Structure):
@@ -73,6 +75,13 @@ def lib() -> C.CDLL:
     L.curdkv_compress_adaptive.argtypes = [vp, vp, vp, i64, i32, i32, C.c_double, vp, vp, vp, vp, vp, vp, vp]
     L.curdkv_scores_append.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp, vp]
     L.curdkv_normalise.argtypes = [vp, vp, vp, i64, i64, vp, vp]
+    f32 = C.c_float
+    L.curdkv_rotate.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp, f32, i32, vp, vp, vp, i64, vp]
+    L.curdkv_attend.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, vp, i64, i32, f32, vp, vp, vp, i64, vp]
+    L.curdkv_compact_mx.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp, vp]
+    L.curdkv_expand_mx.argtypes = [vp, vp, vp, i64, vp, vp]
+    L.curdkv_attend_kept.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, f32, vp, vp, vp, i64, vp]
+    L.curdkv_attend_kept_mx.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, f32, vp, vp, vp, i64, vp]
     L.curdkv_strerror.argtypes = [C.c_int]
     L.curdkv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -215,6 +224,7 @@ class Context:
             raise CurdkvError(rc, "curdkv_create")
         self._address = self._h.value               # (0 once closed)
         self._heads = self.heads
+        self._own_scratch = None
 
     def close(self):
         h = getattr(self, "_h", None)
@@ -304,3 +314,69 @@ class Context:
         rc = _call.normalise(self._address, raw, sums, stride, n, scores, stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_normalise")
+
+    def _scratch(self, given):
+        """(address, bytes) of the partial results' memory: the caller's tensor, or one that the context keeps from its first attention call on."""
+        if given is None:
+            given = self._own_scratch
+            if given is None:
+                import torch
+                given = self._own_scratch = torch.empty((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
+        return given.data_ptr(), given.numel() * given.element_size()
+
+    def _scale(self, scale) -> float:
+        return self.cfg.head_dim ** -0.5 if scale is None else float(scale)
+
+    def rotate(self, qkv, count: int, m: int, table, Q, K, V, stride: int, starts=None, positions=None, q_weight=None, k_weight=None,
+               eps: float = 1e-5, pairs: bool = False, row_stride: Optional[int] = None, stream=None):
+        """table: a float tensor [rows, 2, head_dim/2] of cosines and sines; row_stride None: the projections' rows lie one after the other."""
+        heads = self.cfg.kv_heads * (self.cfg.group_size + 2)
+        rc = lib().curdkv_rotate(self._h, _ptr(qkv), int(count), int(m), heads * self.cfg.head_dim if row_stride is None else int(row_stride),
+                                 _ptr(starts), _ptr(positions), _ptr(table), int(table.shape[0]), _ptr(q_weight), _ptr(k_weight), float(eps),
+                                 1 if pairs else 0, _ptr(Q), _ptr(K), _ptr(V), int(stride), _stream(stream))
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_rotate")
+
+    def attend(self, Q, K, V, count: int, m: int, n: int, stride: int, out, lengths=None, window: int = 0, n_sink: int = 0, scale=None,
+               lse=None, scratch=None, stream=None):
+        """scale None: 1 / sqrt(head_dim); scratch None: the context's own."""
+        scratch, room = self._scratch(scratch)
+        rc = lib().curdkv_attend(self._h, _ptr(Q), _ptr(K), _ptr(V), int(count), int(m), int(n), int(stride), _ptr(lengths), int(window),
+                                 int(n_sink), self._scale(scale), _ptr(out), _ptr(lse), scratch, room, _stream(stream))
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_attend")
+
+    def compact_mx(self, K, V, n: int, indices, offsets, total: int, K_codes, K_scales, V_codes, V_scales, stream=None):
+        """offsets: a DEVICE tensor, int64 [layers*kv_heads + 1]; total: its last value."""
+        rc = lib().curdkv_compact_mx(self._h, _ptr(K), _ptr(V), int(n), _ptr(indices), _ptr(offsets), int(total), _ptr(K_codes), _ptr(K_scales),
+                                     _ptr(V_codes), _ptr(V_scales), _stream(stream))
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_compact_mx")
+
+    def expand_mx(self, codes, scales, rows: int, out, stream=None):
+        rc = lib().curdkv_expand_mx(self._h, _ptr(codes), _ptr(scales), int(rows), _ptr(out), _stream(stream))
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_expand_mx")
+
+    def attend_kept(self, Q, K_kept, V_kept, offsets, count: int, m: int, total: int, out, K_tail=None, V_tail=None, tail_n: int = 0,
+                    tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None,
+                    scratch=None, stream=None):
+        """offsets: a DEVICE tensor, int64 [count*kv_heads + 1]; rows None: total; scale, scratch: as for attend."""
+        scratch, room = self._scratch(scratch)
+        rc = lib().curdkv_attend_kept(self._h, _ptr(Q), _ptr(K_kept), _ptr(V_kept), _ptr(offsets), int(total),
+                                      int(total if rows is None else rows), _ptr(K_tail), _ptr(V_tail),
+                                      int(tail_n), int(tail_stride), _ptr(tail_lengths), int(count), int(m), self._scale(scale), _ptr(out),
+                                      _ptr(lse), scratch, room, _stream(stream))
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_attend_kept")
+
+    def attend_kept_mx(self, Q, K_codes, K_scales, V_codes, V_scales, offsets, count: int, m: int, total: int, out, K_tail=None, V_tail=None,
+                       tail_n: int = 0, tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None,
+                    scratch=None, stream=None):
+        """offsets: a DEVICE tensor, int64 [count*kv_heads + 1]; rows None: total; scale, scratch: as for attend."""
+        scratch, room = self._scratch(scratch)
+        rc = lib().curdkv_attend_kept_mx(self._h, _ptr(Q), _ptr(K_codes), _ptr(K_scales), _ptr(V_codes), _ptr(V_scales), _ptr(offsets), int(total),
+                                         int(total if rows is None else rows), _ptr(K_tail), _ptr(V_tail), int(tail_n), int(tail_stride), _ptr(tail_lengths), int(count), int(m),
+                                         self._scale(scale), _ptr(out), _ptr(lse), scratch, room, _stream(stream))
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_attend_kept_mx")

@@ -21,6 +21,7 @@ LIB = os.path.join(HERE, "libcurdkv.so")
 CALL = os.path.join(HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["curdkv_api.hip", "scores_kernels.hip", "select_kernels.hip", "split_select.hip", "compact_kernels.hip", "fused_kernel.hip", "adaptive_kernels.hip",
            "sketch_host.cpp"]
+ATTENTION = ["rotate_kernel.hip", "mx_kernels.hip", "attend_split.hip", "attend_api.hip"]
 
 
 def _build_call_module(hipcc: str, verbose: bool) -> None:
@@ -47,7 +48,7 @@ def build(verbose: bool = True) -> str:
            # packed fp32 VALU forms are switched off for all device code
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
-    cmd += ["-x", "hip"] + [os.path.join(HERE, "csrc", s) for s in SOURCES]
+    cmd += ["-x", "hip"] + [os.path.join(HERE, "csrc", s) for s in SOURCES] + [os.path.join(HERE, "attention", s) for s in ATTENTION]
     cmd += ["-o", LIB]
     if verbose:
         print(" ".join(cmd), flush=True)

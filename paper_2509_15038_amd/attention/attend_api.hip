@@ -30,7 +30,9 @@ int check_attend(const curdkv_ctx* ctx, const void* Q, const void* out, int64_t 
 }
 
 int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
-    return launch_attend_split(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
+    // more rows than two row tiles of the split kernel: tiles of 256 rows (limits below)
+    const bool prompt = call.dtype == CURDKV_DTYPE_BF16 && !call.offsets && (int64_t)call.m * call.group > 32;
+    return (prompt ? launch_attend_prompt(ctx, call, (hipStream_t)stream) : launch_attend_split(ctx, call, (hipStream_t)stream)) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }
 
 int run_kept(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept, const uint8_t* K_scales, const uint8_t* V_scales,

@@ -5,8 +5,9 @@
 // which is what the B operand of O^T = V^T P^T takes if the 16 keys of a product are counted in that order; P never leaves its
 // registers.  The rows of all query heads of a KV head stand side by side (R = token * group + head), so that the tokens of a
 // tile are few and little is computed beyond the diagonal.
-// K and V tiles pass through LDS, two buffers each, in rows of 256 bytes whose 16-byte pieces are permuted by row, K so that 16 rows' reads of
-// the same piece, V so that the transposing reads of 4 rows, meet different banks.
+// K and V tiles go from memory straight to LDS, two buffers each, as four columns of 64 bytes a row: what a wave's transposing read of V
+// takes (8 keys, 32 channels) lies side by side; K's 16-byte pieces are permuted within a row's 64 bytes by (row / 2) % 4, so that eight rows' reads of the
+// same piece meet different banks.
 //
 // The reference point of a row's exponentials is its maximum only to within 2^8: it moves, and what has been summed is scaled, when the
 // maximum passes it by more, so that most tiles scale nothing.
@@ -42,11 +43,16 @@ __device__ __forceinline__ float halves_sum(float x) {
     const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r.x) + __uint_as_float(r.y);
 }
-__device__ __forceinline__ int v_permuted(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
+// 64 lanes' 16 bytes from base + at to LDS from `to` on, in order of the lanes.  Nothing waits for it but dma_wait().
+__device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
 template <int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs a) {
-    constexpr int kThreads = WAVES * 64, kStage = kKeys * 16 / kThreads, kTileRows = WAVES * 32;
+    constexpr int kStage = 16 / WAVES, kTileRows = WAVES * 32;
     __shared__ __attribute__((aligned(16))) char Ks[2][kKeys * 256], Vs[2][kKeys * 256];
     const AttendCall& c = a.c;
     const int g = blockIdx.x % a.groups, row_tile = a.row_tiles - 1 - blockIdx.x / a.groups;      // long ones first
@@ -72,33 +78,25 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
 
     const char* Kg = (const char*)c.K + (int64_t)g * c.stride * 256;
     const char* Vg = (const char*)c.V + (int64_t)g * c.stride * 256;
-    u32x4a ks[kStage], vs[kStage];
-    const auto fetch = [&](int tile) {
+    // A tile's 1 KB blocks of 16 rows' columns: this wave's share.
+    const uint32_t k_lds = lds_address(&Ks[0][0]), v_lds = lds_address(&Vs[0][0]);
+    const int d_row = lane >> 2, d_piece = lane & 3;
+    const auto fetch = [&](int tile, int buffer) {
         const int64_t j0 = row_of(tile);
         const int count = count_of(tile);
 #pragma unroll
         for (int i = 0; i < kStage; ++i) {
-            const uint32_t at = min(tid / 16 + i * (kThreads / 16), count - 1) * 256 + tid % 16 * 16;
-            ks[i] = *(const u32x4a*)(Kg + j0 * 256 + at);
-            vs[i] = *(const u32x4a*)(Vg + j0 * 256 + at);
-        }
-    };
-    const auto put = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < kStage; ++i) {
-            const int row = tid / 16 + i * (kThreads / 16), piece = tid % 16;
-            *(u32x4a*)(Ks[buffer] + row * 256 + ((piece ^ (row & 15)) << 4)) = ks[i];
-            *(u32x4a*)(Vs[buffer] + row * 256 + ((piece ^ v_permuted(row)) << 4)) = vs[i];
+            const int block = wave * kStage + i, column = block >> 2, row0 = (block & 3) * 16;
+            const uint32_t row = min(row0 + d_row, count - 1) * 256 + column * 64, to = buffer * (kKeys * 256) + block * 1024;
+            dma16(k_lds + to, Kg + j0 * 256, row + ((d_piece ^ ((d_row >> 1) & 3)) << 4));
+            dma16(v_lds + to, Vg + j0 * 256, row + (d_piece << 4));
         }
     };
 
-    // addresses of this lane's operands within a tile: K row col, piece 2 s + half; V rows 4 half + lane16 / 4 (+ 8), channels 32 db ..
+    // this lane's operands within a tile: K row col, piece 2 x + half; V rows 4 half + lane16 / 4 (+ 8), channels 32 db + ..
     const int l16 = lane & 15, dhalf = (lane >> 4) & 1;
-    const int k_at = col * 256 + ((half ^ (col & 15)) << 4);
-    int v_at[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-        v_at[x] = (4 * half + 8 * x + l16 / 4) * 256 + ((l16 / 4) << 6) + (((dhalf * 2 + (l16 % 4) / 2) ^ (half + 2 * x)) << 4) + (l16 & 1) * 8;
+    const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+    const int v_at = (4 * half + l16 / 4) * 64 + dhalf * 32 + (l16 & 3) * 8;
 
     f32x16a o[4];
 #pragma unroll
@@ -118,7 +116,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
             for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                const u32x4a k = *(const u32x4a*)(Kt + ((k_at ^ (x << 5)) + kb * 8192));
+                const u32x4a k = *(const u32x4a*)(Kt + k_at[x & 1] + (x >> 1) * 4096 + kb * 2048);
                 s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, k), __builtin_bit_cast(bf16x8a, q[x]), s[kb], 0, 0, 0);
             }
         }
@@ -164,8 +162,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
             const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
-                const u32x2 x = read_transposed(Vt + ((v_at[0] ^ (db << 6)) + u * 4096));
-                const u32x2 y = read_transposed(Vt + ((v_at[1] ^ (db << 6)) + u * 4096));
+                const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024);
+                const u32x2 y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
                 u32x4a v = {x.x, x.y, y.x, y.y};
                 if constexpr (MASKED) {
                     // an infinity or NaN must not meet the zero weight of a row that does not see it
@@ -189,7 +187,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // channels 32 db + 8 i + 4 half ..+3: half a piece
-                        const u32x2 v = *(const u32x2*)(Vt + key * 256 + (((db * 4 + i) ^ v_permuted(key)) << 4) + half * 8);
+                        const u32x2 v = *(const u32x2*)(Vt + db * 4096 + key * 64 + i * 16 + half * 8);
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
                             const uint32_t x = w % 2 ? v[w / 2] & 0xFFFF0000u : v[w / 2] << 16;
@@ -201,22 +199,35 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
     };
 
     if (tiles > 0) {
-        fetch(0);
-        put(0);
+        fetch(0, 0);
+        dma_wait();
     }
     __syncthreads();
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int buffer = tile & 1;
-        const bool more = tile + 1 < tiles;
-        if (more) fetch(tile + 1);
-        const int j0 = row_of(tile), count = count_of(tile);
-        // (of this wave's tokens) all see all of the tile; none sees any of it
-        const bool whole = count == kKeys && j0 + kKeys - 1 <= p_first && (c.window <= 0 || p_last - j0 < c.window || j0 + kKeys <= c.sinks);
-        const bool none = j0 > p_last || (c.window > 0 && j0 + kKeys - 1 <= p_first - c.window && j0 >= c.sinks);
-        if (whole) take(std::false_type{}, buffer, j0, count);
-        else if (!none) take(std::true_type{}, buffer, j0, count);
-        if (more) put(buffer ^ 1);
-        __syncthreads();
+    // Tiles that all of the workgroup's tokens see all of, in the middle, have a loop of their own: the accumulators then stay where they are.
+    const int whole_end = first_tiles + max(0, (min(seen.high, seen.p0 + 1) - seen.low) / kKeys);
+    const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;             // rows from `low` on that the last token does not see
+    const int whole_begin = min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end);
+    int tile = 0;
+    for (int part = 0; part < 3; ++part) {
+        if (part == 1) {
+            for (; tile < whole_end; ++tile) {
+                if (tile + 1 < tiles) fetch(tile + 1, (tile & 1) ^ 1);
+                take(std::false_type{}, tile & 1, row_of(tile), kKeys);
+                dma_wait();
+                __syncthreads();
+            }
+        } else {
+            const int end = part == 0 ? whole_begin : tiles;
+            for (; tile < end; ++tile) {
+                if (tile + 1 < tiles) fetch(tile + 1, (tile & 1) ^ 1);
+                const int j0 = row_of(tile);
+                // (none of this wave's tokens sees any of it)
+                const bool none = j0 > p_last || (c.window > 0 && j0 + kKeys - 1 <= p_first - c.window && j0 >= c.sinks);
+                if (!none) take(std::true_type{}, tile & 1, j0, count_of(tile));
+                dma_wait();
+                __syncthreads();
+            }
+        }
     }
 
     sum = halves_sum(sum);
@@ -237,7 +248,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
 }  // namespace
 
 hipError_t launch_attend_prompt(const curdkv_ctx*, const AttendCall& call, hipStream_t stream) {
-    constexpr int kWaves = 8;
+    constexpr int kWaves = 4;
     PromptArgs a;
     a.c = call;
     a.scale_log2 = call.scale * (1.f / kLn2);

@@ -66,10 +66,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
     const auto row_of = [&](int tile) { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
     const auto count_of = [&](int tile) { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
 
-    // this wave's rows
+    // this lane's row
     const int R0 = row_tile * kTileRows + wave * 32;
-    const int w_first = min(R0, a.rows - 1) / c.group, w_last = min(R0 + 31, a.rows - 1) / c.group;
-    const int p_first = length - c.m + w_first, p_last = length - c.m + w_last;
     const int R = min(R0 + col, a.rows - 1), t = R / c.group, p = length - c.m + t;
     const int64_t q_row = (((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group;
     u32x4a q[8];
@@ -81,17 +79,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
     // A tile's 1 KB blocks of 16 rows' columns: this wave's share.
     const uint32_t k_lds = lds_address(&Ks[0][0]), v_lds = lds_address(&Vs[0][0]);
     const int d_row = lane >> 2, d_piece = lane & 3;
-    const auto fetch = [&](int tile, int buffer) {
+    const auto fetch = [&](uint32_t lds, const char* rows, int tile, bool keys) {
         const int64_t j0 = row_of(tile);
         const int count = count_of(tile);
 #pragma unroll
         for (int i = 0; i < kStage; ++i) {
             const int block = wave * kStage + i, column = block >> 2, row0 = (block & 3) * 16;
-            const uint32_t row = min(row0 + d_row, count - 1) * 256 + column * 64, to = buffer * (kKeys * 256) + block * 1024;
-            dma16(k_lds + to, Kg + j0 * 256, row + ((d_piece ^ ((d_row >> 1) & 3)) << 4));
-            dma16(v_lds + to, Vg + j0 * 256, row + (d_piece << 4));
+            const uint32_t row = min(row0 + d_row, count - 1) * 256 + column * 64, piece = keys ? d_piece ^ ((d_row >> 1) & 3) : d_piece;
+            dma16(lds + (tile & 1) * (kKeys * 256) + block * 1024, rows + j0 * 256, row + (piece << 4));
         }
     };
+    const auto fetch_k = [&](int tile) { fetch(k_lds, Kg, tile, true); };
+    const auto fetch_v = [&](int tile) { fetch(v_lds, Vg, tile, false); };
 
     // this lane's operands within a tile: K row col, piece 2 x + half; V rows 4 half + lane16 / 4 (+ 8), channels 32 db + ..
     const int l16 = lane & 15, dhalf = (lane >> 4) & 1;
@@ -105,38 +104,38 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
         for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
     float ref = -INFINITY, sum = 0.f;
 
-    // One tile into the running softmax; MASKED: some of this wave's tokens do not see all of it.
-    const auto take = [&](auto masked, int buffer, int j0, int count) {
-        constexpr bool MASKED = decltype(masked)::value;
-        const char *Kt = Ks[buffer], *Vt = Vs[buffer];
-        f32x16a s[2];
+    float top = -INFINITY;
+    const auto scores = [&](int tile, f32x16a* x) {
+        const char* Kt = Ks[tile & 1];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+            for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const u32x4a k = *(const u32x4a*)(Kt + k_at[x & 1] + (x >> 1) * 4096 + kb * 2048);
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, k), __builtin_bit_cast(bf16x8a, q[x]), s[kb], 0, 0, 0);
+            for (int i = 0; i < 8; ++i) {
+                const u32x4a k = *(const u32x4a*)(Kt + k_at[i & 1] + (i >> 1) * 4096 + kb * 2048);
+                x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, k), __builtin_bit_cast(bf16x8a, q[i]), x[kb], 0, 0, 0);
             }
         }
-        // keys of the tile that this row sees: near < key <= far, and those below `sink`
-        const int far = min(p - j0, count - 1) - half * 4, near = (c.window > 0 ? p - j0 - c.window : -1) - half * 4, sink = c.sinks - j0 - half * 4;
-        if constexpr (MASKED) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = kb * 32 + i / 4 * 8 + i % 4;
-                    s[kb][i] = key <= far && (key > near || key < sink) ? s[kb][i] : -INFINITY;
-                }
-        }
-        float top = s[0][0];
+    };
+    // Keys of a tile that this row sees, counted from the half's first: near < key <= far, and those below `sink`.
+    struct Range {
+        int far, near, sink;
+        __device__ __forceinline__ bool has(int key) const { return key <= far && (key > near || key < sink); }
+    };
+    const auto range_of = [&](int tile) {
+        const int j0 = row_of(tile);
+        return Range{min(p - j0, count_of(tile) - 1) - half * 4, (c.window > 0 ? p - j0 - c.window : -1) - half * 4, c.sinks - j0 - half * 4};
+    };
+    const auto top_of = [&](const f32x16a* x) {
+        float y = x[0][0];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-        top = halves_max(top) * a.scale_log2;
+            for (int i = 0; i < 16; ++i) y = fmaxf(y, x[kb][i]);
+        return halves_max(y) * a.scale_log2;
+    };
+    const auto raise = [&]() {
         if (__any(top > ref + kLoose)) {
             const float next = top > ref + kLoose ? top : ref;
             const float keep = next == ref ? 1.f : __builtin_amdgcn_exp2f(ref - next);
@@ -145,43 +144,53 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
             for (int db = 0; db < 4; ++db) o[db] *= keep;
             ref = next;
         }
-        const float off = MASKED && ref == -INFINITY ? 0.f : ref;
-        uint32_t pb[16];
+    };
+    // A tile that may hold rows that some token does not see.
+    const auto masked_step = [&](int tile) {
+        const Range r = range_of(tile);
+        f32x16a s[2];
+        scores(tile, s);
+        __syncthreads();
+        if (tile + 2 < tiles) fetch_k(tile + 2);
+        if (tile + 1 < tiles) fetch_v(tile + 1);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -off));
-                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i + 1], a.scale_log2, -off));
-                sum += x + y;
-                pb[kb * 8 + i / 2] = pack_bf16(x, y);
-            }
+            for (int i = 0; i < 16; ++i) s[kb][i] = r.has(kb * 32 + i / 4 * 8 + i % 4) ? s[kb][i] : -INFINITY;
+        top = top_of(s);
+        raise();
+        const float off = ref == -INFINITY ? 0.f : ref;
+        const char* Vt = Vs[tile & 1];
         bool bad = false;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
+            u32x4a pu;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int kb = u >> 1, i = (u & 1) * 8 + 2 * j;
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -off));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i + 1], a.scale_log2, -off));
+                sum += x + y;
+                pu[j] = pack_bf16(x, y);
+            }
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
-                const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024);
-                const u32x2 y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
-                u32x4a v = {x.x, x.y, y.x, y.y};
-                if constexpr (MASKED) {
-                    // an infinity or NaN must not meet the zero weight of a row that does not see it
+                const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024), y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
+                u32x4a w = {x.x, x.y, y.x, y.y};
+                // an infinity or NaN must not meet the zero weight of a row that does not see it
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const bool low = (v[w] & 0x7F80u) == 0x7F80u, high = (v[w] & 0x7F800000u) == 0x7F800000u;
-                        bad |= low || high;
-                        v[w] &= (low ? 0xFFFF0000u : ~0u) & (high ? 0x0000FFFFu : ~0u);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const bool low = (w[e] & 0x7F80u) == 0x7F80u, high = (w[e] & 0x7F800000u) == 0x7F800000u;
+                    bad |= low || high;
+                    w[e] &= (low ? 0xFFFF0000u : ~0u) & (high ? 0x0000FFFFu : ~0u);
                 }
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, v), __builtin_bit_cast(bf16x8a, pu), o[db], 0, 0, 0);
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, w), __builtin_bit_cast(bf16x8a, pu), o[db], 0, 0, 0);
             }
         }
-        if (MASKED && __any(bad)) {
+        if (__any(bad)) {
             // They reach the rows that do see them: whatever the weight, an infinity or NaN comes of it.
             for (int key = 0; key < kKeys; ++key) {
-                const int k = key - half * 4;
-                if (!(k <= far && (k > near || k < sink))) continue;
+                if (!r.has(key - half * 4)) continue;
 #pragma unroll
                 for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -196,36 +205,97 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
                     }
             }
         }
+        dma_wait();
+        __syncthreads();
+    };
+    // Tiles begin .. end - 1, of which every token sees all: the next tile's 16 products with this one's exponentials between them, in the order
+    // written (a matrix product every 7 other instructions keeps both pipes busy, and no more operands wait in registers than the next two products
+    // need), then this one's 16 products with the next one's maximum.  `end` is a tile too (its scores are made, and dropped).
+    const auto whole_steps = [&](int begin, int end) {
+        f32x16a s[2];
+        scores(begin, s);
+        top = top_of(s);
+        __syncthreads();
+        for (int tile = begin; tile < end; ++tile) {
+            fetch_k(min(tile + 2, tiles - 1));
+            fetch_v(tile + 1);
+            raise();
+            const char *Kt = Ks[(tile + 1) & 1], *Vt = Vs[tile & 1];
+            f32x16a next[2];
+            uint32_t pb[16];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
+            u32x4a k[2][2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) k[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i < 7)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) k[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, k[i & 1][kb]), __builtin_bit_cast(bf16x8a, q[i]), next[kb], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                    const int kb = i >> 2, at = (i & 3) * 4 + j;
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][at], a.scale_log2, -ref));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][at + 1], a.scale_log2, -ref));
+                    sum += x + y;
+                    pb[kb * 8 + at / 2] = pack_bf16(x, y);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            u32x2 v[2][4][2];
+            const auto values = [&](int u) {
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) v[u & 1][db][x] = read_transposed(Vt + v_at + db * 4096 + u * 1024 + x * 512);
+            };
+            values(0);
+            float most = next[0][0];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (u < 3) values(u + 1);
+                const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    const u32x4a w = {v[u & 1][db][0].x, v[u & 1][db][0].y, v[u & 1][db][1].x, v[u & 1][db][1].y};
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, w), __builtin_bit_cast(bf16x8a, pu), o[db], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            top = halves_max(most) * a.scale_log2;
+            s[0] = next[0];
+            s[1] = next[1];
+            dma_wait();
+            __syncthreads();
+        }
     };
 
     if (tiles > 0) {
-        fetch(0, 0);
+        fetch_k(0);
+        fetch_v(0);
+        if (tiles > 1) fetch_k(1);
         dma_wait();
-    }
-    __syncthreads();
-    // Tiles that all of the workgroup's tokens see all of, in the middle, have a loop of their own: the accumulators then stay where they are.
-    const int whole_end = first_tiles + max(0, (min(seen.high, seen.p0 + 1) - seen.low) / kKeys);
-    const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;             // rows from `low` on that the last token does not see
-    const int whole_begin = min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end);
-    int tile = 0;
-    for (int part = 0; part < 3; ++part) {
-        if (part == 1) {
-            for (; tile < whole_end; ++tile) {
-                if (tile + 1 < tiles) fetch(tile + 1, (tile & 1) ^ 1);
-                take(std::false_type{}, tile & 1, row_of(tile), kKeys);
-                dma_wait();
-                __syncthreads();
-            }
-        } else {
-            const int end = part == 0 ? whole_begin : tiles;
-            for (; tile < end; ++tile) {
-                if (tile + 1 < tiles) fetch(tile + 1, (tile & 1) ^ 1);
-                const int j0 = row_of(tile);
-                // (none of this wave's tokens sees any of it)
-                const bool none = j0 > p_last || (c.window > 0 && j0 + kKeys - 1 <= p_first - c.window && j0 >= c.sinks);
-                if (!none) take(std::true_type{}, tile & 1, j0, count_of(tile));
-                dma_wait();
-                __syncthreads();
+        __syncthreads();
+        const int whole_end = min(first_tiles + max(0, (min(seen.high, seen.p0 + 1) - seen.low) / kKeys), tiles - 1);
+        const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;         // rows from `low` on that the last token does not see
+        const int whole_begin = min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end);
+        int tile = 0;
+        for (int part = 0; part < 2; ++part) {
+            const int end = part == 0 ? max(whole_begin, 0) : tiles;
+            for (; tile < end; ++tile) masked_step(tile);
+            if (part == 0 && tile < whole_end) {
+                whole_steps(tile, whole_end);
+                tile = whole_end;
             }
         }
     }

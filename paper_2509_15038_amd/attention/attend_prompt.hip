@@ -21,6 +21,7 @@ namespace curdkv {
 namespace {
 
 typedef float f32x16a __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2a __attribute__((ext_vector_type(2)));
 typedef short s16x4a __attribute__((ext_vector_type(4)));
 
 constexpr int kKeys = 64;              // of a tile
@@ -34,6 +35,9 @@ struct PromptArgs {
 
 __device__ __forceinline__ u32x2 read_transposed(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4a*)p));
+}
+__device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {      // of either 16 bits
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2a, x), __builtin_bit_cast(u16x2a, y)));
 }
 __device__ __forceinline__ float halves_max(float x) {
     const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -50,10 +54,13 @@ __device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at
 __device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
-template <int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs a) {
-    constexpr int kStage = 16 / WAVES, kTileRows = WAVES * 32;
+// RB: blocks of 32 rows a wave
+template <int WAVES, int RB, int OCC>
+__global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptArgs a) {
+    constexpr int kStage = 16 / WAVES, kTileRows = WAVES * RB * 32;
     __shared__ __attribute__((aligned(16))) char Ks[2][kKeys * 256], Vs[2][kKeys * 256];
+    __shared__ int not_finite;         // a tile whose V holds an infinity or NaN
+    if (threadIdx.x == 0) not_finite = -1;
     const AttendCall& c = a.c;
     const int g = blockIdx.x % a.groups, row_tile = a.row_tiles - 1 - blockIdx.x / a.groups;      // long ones first
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
@@ -66,13 +73,21 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
     const auto row_of = [&](int tile) { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
     const auto count_of = [&](int tile) { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
 
-    // this lane's row
-    const int R0 = row_tile * kTileRows + wave * 32;
-    const int R = min(R0 + col, a.rows - 1), t = R / c.group, p = length - c.m + t;
-    const int64_t q_row = (((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group;
-    u32x4a q[8];
+    // this lane's rows
+    const int R0 = row_tile * kTileRows + wave * (RB * 32);
+    int p[RB];
+    u32x4a q[RB][8];
+    const auto query_row = [&](int rb) {
+        const int R = min(R0 + rb * 32 + col, a.rows - 1), t = R / c.group;
+        return (((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group;
+    };
 #pragma unroll
-    for (int s = 0; s < 8; ++s) q[s] = ((const u32x4a*)((const char*)c.Q + q_row * 256))[2 * s + half];
+    for (int rb = 0; rb < RB; ++rb) {
+        p[rb] = length - c.m + min(R0 + rb * 32 + col, a.rows - 1) / c.group;
+        const u32x4a* from = (const u32x4a*)((const char*)c.Q + query_row(rb) * 256);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) q[rb][s] = from[2 * s + half];
+    }
 
     const char* Kg = (const char*)c.K + (int64_t)g * c.stride * 256;
     const char* Vg = (const char*)c.V + (int64_t)g * c.stride * 256;
@@ -97,37 +112,45 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
     const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
     const int v_at = (4 * half + l16 / 4) * 64 + dhalf * 32 + (l16 & 3) * 8;
 
-    f32x16a o[4];
+    f32x16a o[RB][4];
+    float ref[RB], sum[RB], top[RB];
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+    for (int rb = 0; rb < RB; ++rb) {
+        ref[rb] = -INFINITY, sum[rb] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-    float ref = -INFINITY, sum = 0.f;
-
-    float top = -INFINITY;
-    const auto scores = [&](int tile, f32x16a* x) {
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[rb][db][i] = 0.f;
+    }
+    const auto product = [](u32x4a x, u32x4a y, f32x16a z) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, y), z, 0, 0, 0);
+    };
+    const auto scores = [&](int tile, f32x16a (&x)[RB][2]) {
         const char* Kt = Ks[tile & 1];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[rb][kb][i] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const u32x4a k = *(const u32x4a*)(Kt + k_at[i & 1] + (i >> 1) * 4096 + kb * 2048);
-                x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, k), __builtin_bit_cast(bf16x8a, q[i]), x[kb], 0, 0, 0);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) x[rb][kb] = product(k, q[rb][i], x[rb][kb]);
             }
         }
     };
-    // Keys of a tile that this row sees, counted from the half's first: near < key <= far, and those below `sink`.
+    // Keys of a tile that a row sees, counted from the half's first: near < key <= far, and those below `sink`.
     struct Range {
         int far, near, sink;
         __device__ __forceinline__ bool has(int key) const { return key <= far && (key > near || key < sink); }
     };
-    const auto range_of = [&](int tile) {
+    const auto range_of = [&](int tile, int rb) {
         const int j0 = row_of(tile);
-        return Range{min(p - j0, count_of(tile) - 1) - half * 4, (c.window > 0 ? p - j0 - c.window : -1) - half * 4, c.sinks - j0 - half * 4};
+        return Range{min(p[rb] - j0, count_of(tile) - 1) - half * 4, (c.window > 0 ? p[rb] - j0 - c.window : -1) - half * 4, c.sinks - j0 - half * 4};
     };
-    const auto top_of = [&](const f32x16a* x) {
+    const auto top_of = [&](const f32x16a (&x)[2]) {
         float y = x[0][0];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -136,73 +159,102 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
         return halves_max(y) * a.scale_log2;
     };
     const auto raise = [&]() {
-        if (__any(top > ref + kLoose)) {
-            const float next = top > ref + kLoose ? top : ref;
-            const float keep = next == ref ? 1.f : __builtin_amdgcn_exp2f(ref - next);
-            sum *= keep;
 #pragma unroll
-            for (int db = 0; db < 4; ++db) o[db] *= keep;
-            ref = next;
-        }
+        for (int rb = 0; rb < RB; ++rb)
+            if (__any(top[rb] > ref[rb] + kLoose)) {
+                const float next = top[rb] > ref[rb] + kLoose ? top[rb] : ref[rb];
+                const float keep = next == ref[rb] ? 1.f : __builtin_amdgcn_exp2f(ref[rb] - next);
+                sum[rb] *= keep;
+#pragma unroll
+                for (int db = 0; db < 4; ++db) o[rb][db] *= keep;
+                ref[rb] = next;
+            }
     };
     // A tile that may hold rows that some token does not see.
     const auto masked_step = [&](int tile) {
-        const Range r = range_of(tile);
-        f32x16a s[2];
+        f32x16a s[RB][2];
         scores(tile, s);
+        // Whether the tile of V holds an infinity or NaN: every wave looks at its share of it.
+        const char* Vt = Vs[tile & 1];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 16 / WAVES; ++i) {
+            const u32x4a x = *(const u32x4a*)(Vt + (wave * (16 / WAVES) + i) * 1024 + lane * 16);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) most = max_halves(most, x[w] & 0x7FFF7FFFu);
+        }
+        if ((most & 0xFFFFu) >= 0x7F80u || most >= 0x7F800000u) not_finite = tile;
         __syncthreads();
         if (tile + 2 < tiles) fetch_k(tile + 2);
         if (tile + 1 < tiles) fetch_v(tile + 1);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int rb = 0; rb < RB; ++rb) {
+            const Range r = range_of(tile, rb);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[kb][i] = r.has(kb * 32 + i / 4 * 8 + i % 4) ? s[kb][i] : -INFINITY;
-        top = top_of(s);
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[rb][kb][i] = r.has(kb * 32 + i / 4 * 8 + i % 4) ? s[rb][kb][i] : -INFINITY;
+            top[rb] = top_of(s[rb]);
+        }
         raise();
-        const float off = ref == -INFINITY ? 0.f : ref;
-        const char* Vt = Vs[tile & 1];
-        bool bad = false;
+        uint32_t pb[RB][16];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            u32x4a pu;
+        for (int rb = 0; rb < RB; ++rb) {
+            const float off = ref[rb] == -INFINITY ? 0.f : ref[rb];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int kb = u >> 1, i = (u & 1) * 8 + 2 * j;
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -off));
-                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i + 1], a.scale_log2, -off));
-                sum += x + y;
-                pu[j] = pack_bf16(x, y);
-            }
-#pragma unroll
-            for (int db = 0; db < 4; ++db) {
-                const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024), y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
-                u32x4a w = {x.x, x.y, y.x, y.y};
-                // an infinity or NaN must not meet the zero weight of a row that does not see it
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool low = (w[e] & 0x7F80u) == 0x7F80u, high = (w[e] & 0x7F800000u) == 0x7F800000u;
-                    bad |= low || high;
-                    w[e] &= (low ? 0xFFFF0000u : ~0u) & (high ? 0x0000FFFFu : ~0u);
-                }
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, w), __builtin_bit_cast(bf16x8a, pu), o[db], 0, 0, 0);
+            for (int i = 0; i < 32; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i >> 4][i & 15], a.scale_log2, -off));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i >> 4][(i & 15) + 1], a.scale_log2, -off));
+                sum[rb] += x + y;
+                pb[rb][i / 2] = pack_bf16(x, y);
             }
         }
-        if (__any(bad)) {
-            // They reach the rows that do see them: whatever the weight, an infinity or NaN comes of it.
-            for (int key = 0; key < kKeys; ++key) {
-                if (!r.has(key - half * 4)) continue;
+        const bool finite = __builtin_amdgcn_readfirstlane(not_finite) != tile;
+        if (finite) {
 #pragma unroll
-                for (int db = 0; db < 4; ++db)
+            for (int u = 0; u < 4; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        // channels 32 db + 8 i + 4 half ..+3: half a piece
-                        const u32x2 v = *(const u32x2*)(Vt + db * 4096 + key * 64 + i * 16 + half * 8);
+                for (int db = 0; db < 4; ++db) {
+                    const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024), y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const uint32_t x = w % 2 ? v[w / 2] & 0xFFFF0000u : v[w / 2] << 16;
-                            if ((x & 0x7F800000u) == 0x7F800000u) o[db][4 * i + w] += __uint_as_float(x);
-                        }
+                    for (int rb = 0; rb < RB; ++rb)
+                        o[rb][db] = product((u32x4a){x.x, x.y, y.x, y.y}, (u32x4a){pb[rb][4 * u], pb[rb][4 * u + 1], pb[rb][4 * u + 2], pb[rb][4 * u + 3]}, o[rb][db]);
+                }
+        } else {
+            // An infinity or NaN must not meet the zero weight of a row that does not see it: products with zeros in their place, ..
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024), y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
+                    u32x4a w = {x.x, x.y, y.x, y.y};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+                        if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0x0000FFFFu;
                     }
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) o[rb][db] = product(w, (u32x4a){pb[rb][4 * u], pb[rb][4 * u + 1], pb[rb][4 * u + 2], pb[rb][4 * u + 3]}, o[rb][db]);
+                }
+            // .. and then they reach the rows that do see them: whatever the weight, an infinity or NaN comes of it.
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const Range r = range_of(tile, rb);
+                for (int key = 0; key < kKeys; ++key) {
+                    if (!r.has(key - half * 4)) continue;
+#pragma unroll
+                    for (int db = 0; db < 4; ++db)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            // channels 32 db + 8 i + 4 half ..+3: half a piece
+                            const u32x2 v = *(const u32x2*)(Vt + db * 4096 + key * 64 + i * 16 + half * 8);
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                const uint32_t x = w % 2 ? v[w / 2] & 0xFFFF0000u : v[w / 2] << 16;
+                                if ((x & 0x7F800000u) == 0x7F800000u) o[rb][db][4 * i + w] += __uint_as_float(x);
+                            }
+                        }
+                }
             }
         }
         dma_wait();
@@ -212,21 +264,24 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
     // written (a matrix product every 7 other instructions keeps both pipes busy, and no more operands wait in registers than the next two products
     // need), then this one's 16 products with the next one's maximum.  `end` is a tile too (its scores are made, and dropped).
     const auto whole_steps = [&](int begin, int end) {
-        f32x16a s[2];
+        f32x16a s[RB][2];
         scores(begin, s);
-        top = top_of(s);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) top[rb] = top_of(s[rb]);
         __syncthreads();
         for (int tile = begin; tile < end; ++tile) {
             fetch_k(min(tile + 2, tiles - 1));
             fetch_v(tile + 1);
             raise();
             const char *Kt = Ks[(tile + 1) & 1], *Vt = Vs[tile & 1];
-            f32x16a next[2];
-            uint32_t pb[16];
+            f32x16a next[RB][2];
+            uint32_t pb[RB][16];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) next[rb][kb][i] = 0.f;
             u32x4a k[2][2];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) k[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
@@ -237,17 +292,19 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) k[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-                    next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, k[i & 1][kb]), __builtin_bit_cast(bf16x8a, q[i]), next[kb], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-                for (int j = 0; j < 4; j += 2) {
-                    const int kb = i >> 2, at = (i & 3) * 4 + j;
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][at], a.scale_log2, -ref));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][at + 1], a.scale_log2, -ref));
-                    sum += x + y;
-                    pb[kb * 8 + at / 2] = pack_bf16(x, y);
+                    for (int kb = 0; kb < 2; ++kb) next[rb][kb] = product(k[i & 1][kb], q[rb][i], next[rb][kb]);
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        const int kb = i >> 2, at = (i & 3) * 4 + j;
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][at], a.scale_log2, -ref[rb]));
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][at + 1], a.scale_log2, -ref[rb]));
+                        sum[rb] += x + y;
+                        pb[rb][kb * 8 + at / 2] = pack_bf16(x, y);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
             u32x2 v[2][4][2];
             const auto values = [&](int u) {
@@ -257,24 +314,32 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
                     for (int x = 0; x < 2; ++x) v[u & 1][db][x] = read_transposed(Vt + v_at + db * 4096 + u * 1024 + x * 512);
             };
             values(0);
-            float most = next[0][0];
+            float most[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) most[rb] = next[rb][0][0];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (u < 3) values(u + 1);
-                const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
 #pragma unroll
-                for (int db = 0; db < 4; ++db) {
-                    const u32x4a w = {v[u & 1][db][0].x, v[u & 1][db][0].y, v[u & 1][db][1].x, v[u & 1][db][1].y};
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, w), __builtin_bit_cast(bf16x8a, pu), o[db], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb) {
+                    const u32x4a pu = {pb[rb][4 * u], pb[rb][4 * u + 1], pb[rb][4 * u + 2], pb[rb][4 * u + 3]};
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        const u32x4a w = {v[u & 1][db][0].x, v[u & 1][db][0].y, v[u & 1][db][1].x, v[u & 1][db][1].y};
+                        o[rb][db] = product(w, pu, o[rb][db]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most[rb] = fmaxf(most[rb], next[rb][u >> 1][(u & 1) * 8 + i]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
-                __builtin_amdgcn_sched_barrier(0);
             }
-            top = halves_max(most) * a.scale_log2;
-            s[0] = next[0];
-            s[1] = next[1];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                top[rb] = halves_max(most[rb]) * a.scale_log2;
+                s[rb][0] = next[rb][0];
+                s[rb][1] = next[rb][1];
+            }
             dma_wait();
             __syncthreads();
         }
@@ -300,32 +365,38 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_prompt_kernel(PromptArgs
         }
     }
 
-    sum = halves_sum(sum);
-    if (R0 + col >= a.rows) return;
-    const bool empty = ref == -INFINITY;
-    const float over = empty ? 0.f : 1.f / sum;
-    char* out = (char*)c.out + q_row * 256;
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+    for (int rb = 0; rb < RB; ++rb) {
+        const float total = halves_sum(sum[rb]);
+        const int R = R0 + rb * 32 + col;
+        if (R >= a.rows) continue;
+        const bool empty = ref[rb] == -INFINITY;
+        const float over = empty ? 0.f : 1.f / total;
+        char* out = (char*)c.out + query_row(rb) * 256;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x2 x = {pack_bf16(o[db][4 * i] * over, o[db][4 * i + 1] * over), pack_bf16(o[db][4 * i + 2] * over, o[db][4 * i + 3] * over)};
-            *(u32x2*)(out + (db * 32 + i * 8 + half * 4) * 2) = x;
-        }
-    if (c.lse && half == 0) c.lse[((int64_t)b * c.kv * c.group + head * c.group + R % c.group) * c.m + t] = empty ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x16a& x = o[rb][db];
+                *(u32x2*)(out + (db * 32 + i * 8 + half * 4) * 2) =
+                    (u32x2){pack_bf16(x[4 * i] * over, x[4 * i + 1] * over), pack_bf16(x[4 * i + 2] * over, x[4 * i + 3] * over)};
+            }
+        if (c.lse && half == 0)
+            c.lse[((int64_t)b * c.kv * c.group + head * c.group + R % c.group) * c.m + R / c.group] = empty ? -INFINITY : (ref[rb] + __builtin_amdgcn_logf(total)) * kLn2;
+    }
 }
 
 }  // namespace
 
 hipError_t launch_attend_prompt(const curdkv_ctx*, const AttendCall& call, hipStream_t stream) {
-    constexpr int kWaves = 4;
+    constexpr int kWaves = 4, kBlocks = 1, kOcc = 2;
     PromptArgs a;
     a.c = call;
     a.scale_log2 = call.scale * (1.f / kLn2);
     a.groups = (int)(call.count * call.kv);
     a.rows = call.m * call.group;
-    a.row_tiles = (a.rows + kWaves * 32 - 1) / (kWaves * 32);
-    attend_prompt_kernel<kWaves><<<(unsigned)((int64_t)a.groups * a.row_tiles), kWaves * 64, 0, stream>>>(a);
+    a.row_tiles = (a.rows + kWaves * kBlocks * 32 - 1) / (kWaves * kBlocks * 32);
+    attend_prompt_kernel<kWaves, kBlocks, kOcc><<<(unsigned)((int64_t)a.groups * a.row_tiles), kWaves * 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -48,12 +48,120 @@ __device__ __forceinline__ f32x2a two_f32(uint32_t codes, float unit) {
 }
 __device__ __forceinline__ float unit_of(uint32_t scale) { return __uint_as_float(scale << 23); }   // (2^-127 comes out as 0: it stands for zeros)
 
-__device__ __forceinline__ bool not_finite2(uint32_t x) {     // either half of a pair of bf16
-    return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
+// A lane's part of the running softmax: column R = lane % 16, channels 32 (lane / 16) + 8 j + i in o[i][j].
+struct Running {
+    f32x4a o[8];
+    float top, sum;                    // of R so far (top: of all quarters; sum: of the lane's keys)
+};
+
+// o += V^T P^T for bf16 rows: v[e] the lane's 8 channels of key e of its quarter, p[e] that key's weights.
+__device__ __forceinline__ f32x4a product(u32x4a x, u32x4a y, f32x4a z) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, y), z, 0, 0, 0);
+}
+__device__ __forceinline__ void add_values(const u32x4a* v, const float* p, f32x4a* o) {
+    u32x4a pb;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) pb[u] = pack_bf16(p[2 * u], p[2 * u + 1]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        u32x4a even, odd;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            even[u] = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x05040100u);
+            odd[u] = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x07060302u);
+        }
+        o[2 * w] = product(even, pb, o[2 * w]);
+        o[2 * w + 1] = product(odd, pb, o[2 * w + 1]);
+    }
+}
+// (fp32 products: exact to 2^-24 a product, 1/16 of the bf16 rate, which the rows' bytes still hide)
+__device__ __forceinline__ void add_values(const float (*v)[8], const float* p, f32x4a* o) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][i], p[e], o[i], 0, 0, 0);
+}
+
+// Infinities and NaN in rows that some R does not see must not meet its zero weight.  Zeros take their place, and the R that do see one
+// (seen: a bit for each of the lane's keys) get it whatever its weight: where a product of "is such a value" with "is seen" is not zero.
+constexpr uint32_t kInf16 = 0x7F80u;
+__device__ __forceinline__ bool any_not_finite(const u32x4a* v) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) bad |= (v[e][w] & kInf16) == kInf16 || (v[e][w] & (kInf16 << 16)) == kInf16 << 16;
+    return __any(bad);
+}
+__device__ __forceinline__ bool any_not_finite(const float (*v)[8]) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bad |= (__float_as_uint(v[e][i]) & 0x7F800000u) == 0x7F800000u;
+    return __any(bad);
+}
+__device__ __forceinline__ uint32_t kind_of(uint32_t x, uint32_t inf, uint32_t sign) {      // 0: +inf, 1: -inf, 2: NaN, 3: finite
+    return (x & inf) != inf ? 3u : x == inf ? 0u : x == (inf | sign) ? 1u : 2u;
+}
+__device__ __forceinline__ void spread_not_finite(u32x4a* v, uint32_t seen, f32x4a* o) {
+    u32x4a sees;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sees[u] = (seen >> (2 * u) & 1 ? 0x3F80u : 0u) | (seen >> (2 * u + 1) & 1 ? 0x3F800000u : 0u);
+#pragma unroll 1
+    for (uint32_t kind = 0; kind < 3; ++kind) {
+        const float value = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4a has;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t x = v[2 * u][w] >> (16 * h) & 0xFFFFu, y = v[2 * u + 1][w] >> (16 * h) & 0xFFFFu;
+                    has[u] = (kind_of(x, kInf16, 0x8000u) == kind ? 0x3F80u : 0u) | (kind_of(y, kInf16, 0x8000u) == kind ? 0x3F800000u : 0u);
+                }
+                const f32x4a z = product(has, sees, (f32x4a){0, 0, 0, 0});
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[2 * w + h][j] += z[j] > 0.f ? value : 0.f;
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if ((v[e][w] & kInf16) == kInf16) v[e][w] &= 0xFFFF0000u;
+            if ((v[e][w] & (kInf16 << 16)) == kInf16 << 16) v[e][w] &= 0xFFFFu;
+        }
+}
+__device__ __forceinline__ void spread_not_finite(float (*v)[8], uint32_t seen, f32x4a* o) {
+#pragma unroll 1
+    for (uint32_t kind = 0; kind < 3; ++kind) {
+        const float value = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f32x4a z = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                z = __builtin_amdgcn_mfma_f32_16x16x4f32(kind_of(__float_as_uint(v[e][i]), 0x7F800000u, 0x80000000u) == kind ? 1.f : 0.f, seen >> e & 1 ? 1.f : 0.f, z, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] += z[j] > 0.f ? value : 0.f;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((__float_as_uint(v[e][i]) & 0x7F800000u) == 0x7F800000u) v[e][i] = 0.f;
+}
+template <class V>
+__device__ __forceinline__ void add_values_masked(V* v, const float* p, uint32_t seen, f32x4a* o) {
+    if (any_not_finite(v)) spread_not_finite(v, seen, o);
+    add_values(v, p, o);
 }
 
 // One tile of T keys in registers.  `first`: row of its first key in K and V; `count`: keys of it that there are (>= 1), the last
-// one stands in for those beyond.
+// one stands in for those beyond.  MASKED: some key of it is hidden from some R.
 template <int F> struct Tile;
 
 template <>
@@ -64,6 +172,16 @@ struct Tile<kBf16> {
         const int c = lane & 15, quarter = lane >> 4;
         const char* Kb = (const char*)K + first * 256;
         const char* Vb = (const char*)V + first * 256;
+        if (count == T) {
+            const uint32_t k_at = (c >> 2) * 2048 + (c & 3) * 256 + quarter * 16, v_at = quarter * 2048 + c * 16;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) k[t][s] = *(const u32x4a*)(Kb + k_at + t * 1024 + s * 64);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = *(const u32x4a*)(Vb + v_at + e * 256);
+            return;
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int key = min((c >> 2) * 8 + t * 4 + (c & 3), count - 1);
@@ -82,51 +200,17 @@ struct Tile<kBf16> {
         for (int t = 0; t < 2; ++t) {
             f32x4a a = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, k[t][i]), __builtin_bit_cast(bf16x8a, q.q[i]), a, 0, 0, 0);
+            for (int i = 0; i < 4; ++i) a = product(k[t][i], q.q[i], a);
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[t * 4 + j] = a[j];
         }
     }
-    __device__ __forceinline__ bool values_finite() const {
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) bad |= not_finite2(v[e][w]);
-        return !__any(bad);
-    }
-    // o += V^T P^T; drop: bit e set: key e of the lane's quarter counts as zeros
-    template <bool DROP>
-    __device__ __forceinline__ void values(const float* p, f32x4a* o, uint32_t drop) const {
-        u32x4a pb;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) pb[u] = pack_bf16(p[2 * u], p[2 * u + 1]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            u32x4a even, odd;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                uint32_t x = v[2 * u][w], y = v[2 * u + 1][w];
-                if (DROP) { x = drop >> (2 * u) & 1 ? 0 : x; y = drop >> (2 * u + 1) & 1 ? 0 : y; }
-                even[u] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                odd[u] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-            }
-            o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, even), __builtin_bit_cast(bf16x8a, pb), o[2 * w], 0, 0, 0);
-            o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, odd), __builtin_bit_cast(bf16x8a, pb), o[2 * w + 1], 0, 0, 0);
-        }
+    template <bool MASKED>
+    __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
+        if (MASKED) add_values_masked(v, p, seen, o);
+        else add_values(v, p, o);
     }
 };
-
-// (fp32 products: exact to 2^-24 a product, 1/16 of the bf16 rate, which the rows' bytes still hide)
-template <bool DROP>
-__device__ __forceinline__ void values_f32(const float (*v)[8], const float* p, f32x4a* o, uint32_t drop) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(DROP && (drop >> e & 1) ? 0.f : v[e][i], p[e], o[i], 0, 0, 0);
-}
 
 template <>
 struct Tile<kF32> {
@@ -137,9 +221,18 @@ struct Tile<kF32> {
         const int c = lane & 15, quarter = lane >> 4;
         const char* Kb = (const char*)K + first * 512;
         const char* Vb = (const char*)V + first * 512;
-        const int key = min(c, count - 1);
+        const uint32_t k_at = min(c, count - 1) * 512 + quarter * 16;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) k[s] = *(const f32x4a*)(Kb + (uint32_t)(key * 512 + (s * 4 + quarter) * 16));
+        for (int s = 0; s < 8; ++s) k[s] = *(const f32x4a*)(Kb + k_at + s * 64);
+        if (count == T) {
+            const uint32_t v_at = quarter * 2048 + c * 32;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                *(f32x4a*)&v[e][0] = *(const f32x4a*)(Vb + v_at + e * 512);
+                *(f32x4a*)&v[e][4] = *(const f32x4a*)(Vb + v_at + e * 512 + 16);
+            }
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const char* row = Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 512 + c * 32);
@@ -160,16 +253,11 @@ struct Tile<kF32> {
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] = a[j];
     }
-    __device__ __forceinline__ bool values_finite() const {
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) bad |= (__float_as_uint(v[e][i]) & 0x7F800000u) == 0x7F800000u;
-        return !__any(bad);
+    template <bool MASKED>
+    __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
+        if (MASKED) add_values_masked(v, p, seen, o);
+        else add_values(v, p, o);
     }
-    template <bool DROP>
-    __device__ __forceinline__ void values(const float* p, f32x4a* o, uint32_t drop) const { values_f32<DROP>(v, p, o, drop); }
 };
 
 // Rows in 4 bits: 64 bytes of codes (channel 2 i in the low half of byte i) and 4 scales, a power of two for 32 channels each.
@@ -186,6 +274,21 @@ struct Tile<kMxBf16> {
         const char* Vb = (const char*)V + first * 64;
         const uint8_t* Kc = Ks + first * 4;
         const uint8_t* Vc = Vs + first * 4;
+        if (count == T) {
+            const uint32_t key = (c >> 2) * 8 + (c & 3), k_at = key * 64 + quarter * 16, v_at = quarter * 512 + c * 4;
+            const uint32_t ks_at = key * 4 + quarter, vs_at = quarter * 32 + (c >> 2);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                k[t] = *(const u32x4a*)(Kb + k_at + t * 256);
+                ks[t] = *(Kc + ks_at + t * 16);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = *(const uint32_t*)(Vb + v_at + e * 64);
+                vs[e] = *(Vc + vs_at + e * 4);
+            }
+            return;
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int key = min((c >> 2) * 8 + t * 4 + (c & 3), count - 1);
@@ -209,29 +312,22 @@ struct Tile<kMxBf16> {
             const float unit = unit_of(ks[t]);
             f32x4a a = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u32x4a x = {two_bf16<0>(k[t][i], unit), two_bf16<1>(k[t][i], unit), two_bf16<2>(k[t][i], unit), two_bf16<3>(k[t][i], unit)};
-                a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, q.q[i]), a, 0, 0, 0);
-            }
+            for (int i = 0; i < 4; ++i)
+                a = product((u32x4a){two_bf16<0>(k[t][i], unit), two_bf16<1>(k[t][i], unit), two_bf16<2>(k[t][i], unit), two_bf16<3>(k[t][i], unit)}, q.q[i], a);
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[t * 4 + j] = a[j];
         }
     }
-    __device__ __forceinline__ bool values_finite() const {
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) bad |= vs[e] == 255u;
-        return !__any(bad);
-    }
-    template <bool DROP>
-    __device__ __forceinline__ void values(const float* p, f32x4a* o, uint32_t drop) const {
-        Tile<kBf16> b;
+    template <bool MASKED>
+    __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
+        u32x4a x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float unit = unit_of(vs[e]);
-            b.v[e] = (u32x4a){two_bf16<0>(v[e], unit), two_bf16<1>(v[e], unit), two_bf16<2>(v[e], unit), two_bf16<3>(v[e], unit)};
+            x[e] = (u32x4a){two_bf16<0>(v[e], unit), two_bf16<1>(v[e], unit), two_bf16<2>(v[e], unit), two_bf16<3>(v[e], unit)};
         }
-        b.values<DROP>(p, o, drop);
+        // (a masked tile of kept rows ends them: its other keys repeat the last one, which every R sees, so nothing hidden is not finite alone)
+        add_values(x, p, o);
     }
 };
 
@@ -275,44 +371,24 @@ struct Tile<kMxF32> {
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] = a[j];
     }
-    __device__ __forceinline__ bool values_finite() const {
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= vs[e] == 255u;
-        return !__any(bad);
-    }
-    template <bool DROP>
-    __device__ __forceinline__ void values(const float* p, f32x4a* o, uint32_t drop) const {
+    template <bool MASKED>
+    __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
         float x[4][8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) wide(v[e], unit_of(vs[e]), x[e]);
-        values_f32<DROP>(x, p, o, drop);
+        add_values(x, p, o);
     }
 };
 
-// A lane's part of the running softmax: column R = lane % 16, channels 32 (lane / 16) + 8 j + i in o[i][j].
-struct Running {
-    f32x4a o[8];
-    float top, sum;                    // of R so far (top: of all quarters; sum: of the lane's keys)
-};
-
-// Takes a tile's scores into the running softmax.  hide: keys of the tile that some row does not see are masked by position:
-// key e of quarter q is row j0 + q * (T/4) + e of the cache, or, WINDOW false, a kept row, of which there are `count`.
-template <int F, bool WINDOW>
-__device__ __forceinline__ void take(Running& r, const Tile<F>& x, const Queries& q, float scale_log2, bool hide, int j0, int count, int p,
-                                     const Seen& seen, int window, int sinks, int t0, int t1, int t, int lane) {
+// Takes a tile's scores into the running softmax.  MASKED: of the tile's keys, R sees those with a bit in `seen`.
+template <int F, bool MASKED>
+__device__ __forceinline__ void take(Running& r, Tile<F>& x, const Queries& q, float scale_log2, uint32_t seen) {
     constexpr int E = Tile<F>::T / 4;
-    const int quarter = lane >> 4;
     float s[E];
     x.scores(q, s);
-    if (hide) {
+    if (MASKED)
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = quarter * E + e;
-            const bool see = i < count && (!WINDOW || sees(p, j0 + i, window, sinks));
-            s[e] = see ? s[e] : -INFINITY;
-        }
-    }
+        for (int e = 0; e < E; ++e) s[e] = seen >> e & 1 ? s[e] : -INFINITY;
     float top = s[0];
 #pragma unroll
     for (int e = 1; e < E; ++e) top = fmaxf(top, s[e]);
@@ -324,63 +400,53 @@ __device__ __forceinline__ void take(Running& r, const Tile<F>& x, const Queries
         for (int i = 0; i < 8; ++i) r.o[i] *= keep;
         r.top = top;
     }
-    const float off = r.top == -INFINITY ? 0.f : r.top;
+    const float off = MASKED && r.top == -INFINITY ? 0.f : r.top;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale_log2, -off));
         r.sum += s[e];
     }
-    if (!hide || x.values_finite()) {
-        x.template values<false>(s, r.o, 0u);
-        return;
-    }
-    // A hidden row that holds an infinity or NaN must not meet its zero weight: token by token, with that token's hidden rows as zeros.
-    for (int u = t0; u <= t1; ++u) {
-        uint32_t drop = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = quarter * E + e;
-            if (!(i < count && (!WINDOW || sees(seen.p0 + u - t0, j0 + i, window, sinks)))) drop |= 1u << e;
-        }
-        f32x4a o[8] = {};
-        x.template values<true>(s, o, drop);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (u == t) r.o[i] += o[i];
-    }
+    x.template values<MASKED>(s, seen, r.o);
 }
 
-// What a (head, row tile) has to read: tiles of kept rows, of first rows and of rows near, and chunks of them.
+// What a (head, row tile) has to read: tiles that all its R see all of, in chunks, from the kept rows, the first rows and the rows near; and
+// tiles to be masked: the ends of those three, and where the window's edge and the diagonal pass.
 template <int FA, int FB>
 struct Work {
     static constexpr int TA = Tile<FA == kNone ? kBf16 : FA>::T, TB = Tile<FB>::T;
-    int64_t begin, kept;               // kept rows
-    int64_t kept_tiles, kept_chunks;
-    int first_tiles, cache_tiles, cache_chunks;
+    int64_t begin = 0, kept = 0, kept_tiles = 0, kept_chunks = 0;
     Seen seen;
     int t0, t1;
+    int first_tiles, near_begin, near_end, near_tiles;     // whole first rows; of the tiles from seen.low on: whole ones, and all
+    int cache_tiles, cache_chunks;                         // whole ones of the cache
+    int low_masked, cache_masked;                          // masked ones: before near_begin; all
     __device__ __forceinline__ Work(const SplitArgs& a, int g, int row_tile) {
         const AttendCall& c = a.c;
         t0 = row_tile * kRowTile / c.group;
         t1 = min(c.m - 1, (row_tile * kRowTile + kRowTile - 1) / c.group);
-        begin = 0, kept = 0, kept_tiles = 0, kept_chunks = 0;
         if (FA != kNone) {
             begin = min(max(c.offsets[g], (int64_t)0), c.total);
             kept = min(max(c.offsets[g + 1], begin), c.total) - begin;
-            kept_tiles = (kept + TA - 1) / TA;
+            kept_tiles = kept / TA;
             kept_chunks = (kept_tiles + a.chunk - 1) / a.chunk;
         }
-        const int b = g / c.kv;
-        const int length = c.n > 0 ? (c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n) : 0;
+        const int length = c.n > 0 ? (c.lengths ? min(max(c.lengths[g / c.kv], 0), c.n) : c.n) : 0;
         seen = seen_rows(length, c.m, t0, t1, c.window, c.sinks);
-        first_tiles = (seen.first + TB - 1) / TB;
-        cache_tiles = first_tiles + (seen.high - seen.low + TB - 1) / TB;
+        const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;    // rows from low on that the last token does not see
+        first_tiles = seen.first / TB;
+        near_tiles = (seen.high - seen.low + TB - 1) / TB;
+        near_end = max(0, min(seen.high, seen.p0 + 1) - seen.low) / TB;
+        near_begin = min((hidden + TB - 1) / TB, near_end);
+        cache_tiles = first_tiles + near_end - near_begin;
         cache_chunks = (cache_tiles + a.chunk - 1) / a.chunk;
+        low_masked = (seen.first % TB != 0) + near_begin;
+        cache_masked = low_masked + near_tiles - near_end;
     }
     __device__ __forceinline__ int shares(const SplitArgs& a) const { return (int)min((int64_t)a.shares, max((int64_t)1, kept_chunks + cache_chunks)); }
+    __device__ __forceinline__ int row_of(int tile) const { return tile < first_tiles ? tile * TB : seen.low + (near_begin + tile - first_tiles) * TB; }
 };
 
-// Which tiles a wave takes: chunks share, share + shares, ..; of each its tiles wave, wave + 4, ..
+// Which whole tiles a wave takes: chunks first, first + shares, ..; of each its tiles wave, wave + 4, ..
 struct Walk {
     int64_t chunk, chunks, tiles;
     int shares, per, at, wave;
@@ -399,6 +465,25 @@ struct Walk {
         }
     }
 };
+
+// The walk's tiles one after the other, the next one's loads in flight behind the one at hand.
+template <int F, class L>
+__device__ __forceinline__ void stream(Walk walk, Running& r, const Queries& q, float scale_log2, L load) {
+    Tile<F> x, y;
+    int64_t tx = walk.next(), ty;
+    if (tx < 0) return;
+    load(x, tx);
+    for (;;) {
+        ty = walk.next();
+        load(y, ty < 0 ? tx : ty);
+        take<F, false>(r, x, q, scale_log2, 0u);
+        if (ty < 0) return;
+        tx = walk.next();
+        load(x, tx < 0 ? ty : tx);
+        take<F, false>(r, y, q, scale_log2, 0u);
+        if (tx < 0) return;
+    }
+}
 
 template <int FA, int FB>
 __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(SplitArgs a) {
@@ -423,59 +508,40 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(Split
     for (int i = 0; i < 8; ++i) r.o[i] = (f32x4a){0, 0, 0, 0};
     r.top = -INFINITY;
     r.sum = 0.f;
-    const int p = work.seen.p0 + (t - work.t0);
 
     if constexpr (FA != kNone) {
+        constexpr int T = Tile<FA>::T;
         Tile<FA>::queries(q, q_row, quarter);
-        Walk walk(share, work.kept_chunks, work.kept_tiles, shares, a.chunk, wave);
-        const auto load = [&](Tile<FA>& x, int64_t tile) {
-            x.load(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + tile * Tile<FA>::T, (int)min((int64_t)Tile<FA>::T, work.kept - tile * Tile<FA>::T), lane);
-        };
-        const auto use = [&](const Tile<FA>& x, int64_t tile) {
-            const int count = (int)min((int64_t)Tile<FA>::T, work.kept - tile * Tile<FA>::T);
-            take<FA, false>(r, x, q, a.scale_log2, count < Tile<FA>::T, 0, count, p, work.seen, 0, 0, work.t0, work.t1, t, lane);
-        };
-        Tile<FA> x, y;
-        int64_t tx = walk.next(), ty;
-        if (tx >= 0) load(x, tx);
-        while (tx >= 0) {
-            ty = walk.next();
-            if (ty >= 0) load(y, ty);
-            use(x, tx);
-            if (ty < 0) break;
-            tx = walk.next();
-            if (tx >= 0) load(x, tx);
-            use(y, ty);
+        stream<FA>(Walk(share, work.kept_chunks, work.kept_tiles, shares, a.chunk, wave), r, q, a.scale_log2, [&](Tile<FA>& x, int64_t tile) {
+            x.load(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + tile * T, T, lane);
+        });
+        const int left = (int)(work.kept - work.kept_tiles * T);
+        if (left > 0 && share == shares - 1 && wave == kSplitWaves - 1) {
+            Tile<FA> x;
+            x.load(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + work.kept_tiles * T, left, lane);
+            take<FA, true>(r, x, q, a.scale_log2, (1u << min(max(left - quarter * (T / 4), 0), 8)) - 1u);
         }
     }
-    if (work.cache_tiles > 0) {
-        constexpr int T = Tile<FB>::T;
-        Tile<FB>::queries(q, q_row, quarter);
-        // (chunks of the cache follow those of the kept rows)
-        const int64_t before = work.kept_chunks % shares;
-        Walk walk((share - before + shares) % shares, work.cache_chunks, work.cache_tiles, shares, a.chunk, wave);
-        const int64_t base = (int64_t)g * c.stride;
-        const auto row_of = [&](int tile) { return tile < work.first_tiles ? tile * T : work.seen.low + (tile - work.first_tiles) * T; };
-        const auto count_of = [&](int tile) { return min(T, (tile < work.first_tiles ? work.seen.first : work.seen.high) - row_of(tile)); };
-        const auto load = [&](Tile<FB>& x, int tile) { x.load(c.K, c.V, nullptr, nullptr, base + row_of(tile), count_of(tile), lane); };
-        const auto use = [&](const Tile<FB>& x, int tile) {
-            const int j0 = row_of(tile), count = count_of(tile);
-            // the first token sees the tile's last row, and the last token its first one (or all of it is among the sinks)
-            const bool whole = count == T && j0 + T - 1 <= work.seen.p0 && (c.window <= 0 || work.seen.p1 - j0 < c.window || j0 + T <= c.sinks);
-            take<FB, true>(r, x, q, a.scale_log2, !whole, j0, count, p, work.seen, c.window, c.sinks, work.t0, work.t1, t, lane);
-        };
-        Tile<FB> x, y;
-        int64_t tx = walk.next(), ty;
-        if (tx >= 0) load(x, (int)tx);
-        while (tx >= 0) {
-            ty = walk.next();
-            if (ty >= 0) load(y, (int)ty);
-            use(x, (int)tx);
-            if (ty < 0) break;
-            tx = walk.next();
-            if (tx >= 0) load(x, (int)tx);
-            use(y, (int)ty);
+    constexpr int T = Tile<FB>::T;
+    const int64_t base = (int64_t)g * c.stride;
+    Tile<FB>::queries(q, q_row, quarter);
+    // (chunks of the cache follow those of the kept rows)
+    stream<FB>(Walk((share + shares - work.kept_chunks % shares) % shares, work.cache_chunks, work.cache_tiles, shares, a.chunk, wave), r, q, a.scale_log2,
+               [&](Tile<FB>& x, int64_t tile) { x.load(c.K, c.V, nullptr, nullptr, base + work.row_of((int)tile), T, lane); });
+    // (the last share and its last waves first: they have least of the rest)
+    for (int i = (shares - 1 - share) * kSplitWaves + kSplitWaves - 1 - wave; i < work.cache_masked; i += shares * kSplitWaves) {
+        const int near = i < work.low_masked ? i - (work.seen.first % T != 0) : work.near_end + i - work.low_masked;        // -1: the end of the first rows
+        const int j0 = near < 0 ? work.first_tiles * T : work.seen.low + near * T, count = min(T, (near < 0 ? work.seen.first : work.seen.high) - j0);
+        const int p = work.seen.p0 + (t - work.t0);
+        Tile<FB> x;
+        x.load(c.K, c.V, nullptr, nullptr, base + j0, count, lane);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int e = 0; e < T / 4; ++e) {
+            const int k = quarter * (T / 4) + e;
+            mask |= k < count && sees(p, j0 + k, c.window, c.sinks) ? 1u << e : 0u;
         }
+        take<FB, true>(r, x, q, a.scale_log2, mask);
     }
 
     // the four waves' parts

@@ -56,7 +56,7 @@ extern "C" {
 #define CURDKV_ERR_OOM         -4   /* device or host allocation failed */
 #define CURDKV_ERR_TOO_LARGE   -5   /* more (layer, group) pairs than a non-allocating call's fixed workspace holds */
 
-#define CURDKV_ATTEND_SCRATCH_BYTES 34078720   /* most scratch that an attention call uses (65536 rows of 520 bytes) */
+#define CURDKV_ATTEND_SCRATCH_BYTES 34078720   /* most scratch that an attention call uses (65504 rows of 520 bytes, 16 KB of counters) */
 
 #define CURDKV_DTYPE_F32  0
 #define CURDKV_DTYPE_BF16 1
@@ -300,7 +300,8 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  * scratch: device memory of the caller's, 16-byte aligned, for the partial results of few tokens over
  *   long caches, whose heads are shared out over many workgroups; CURDKV_ATTEND_SCRATCH_BYTES
  *   are as much as a call ever uses, with less (0 and NULL included) there are fewer shares.
- *   Its contents mean nothing before or after; calls that overlap in time need one each. */
+ *   It is cleared (zeros) once, before the first call that it is given to; every call leaves its counters
+ *   cleared.  Calls that overlap in time need one each. */
 int curdkv_attend(curdkv_ctx* ctx, const void* Q, const void* K, const void* V, int64_t count,
                   int64_t m, int64_t n, int64_t stride, const int32_t* lengths, int64_t window,
                   int32_t n_sink, float scale, void* out, float* lse, void* scratch,

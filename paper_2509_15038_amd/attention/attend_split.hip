@@ -11,24 +11,31 @@
 // a lane holding the same 8 channels of the T/4 keys of its quarter; v_perm pairs them up into the A operand of eight products,
 // product i for channels 8 c + i.
 
+#include <algorithm>
+
 #include "attend_device.h"
 #include "attend_internal.h"
 
 namespace curdkv {
 namespace {
 
+typedef short s16x4a __attribute__((ext_vector_type(4)));
+
 constexpr int kSplitWaves = 4;
 constexpr int kRowTile = 16;           // rows R a workgroup handles
+constexpr int kCounters = 4096;        // items at most that share workgroups
+constexpr int64_t kPastCaches = 128 << 20;
 constexpr int64_t kPartBytes = 128 * sizeof(float) + 2 * sizeof(float);     // of a row of partial results
-constexpr int64_t kPartRows = CURDKV_ATTEND_SCRATCH_BYTES / kPartBytes;
 
 struct SplitArgs {
     AttendCall c;
     float scale_log2;
-    int groups, rows, row_tiles;       // count * kv; m * group; tiles of them
-    int shares, chunk;                 // workgroups a head and row tile; tiles of keys in a row
-    float* part_o;                     // [groups * rows][shares][128]
-    f32x2a* part_ml;                   // [groups * rows][shares]: maximum, sum
+    int items, rows, row_tiles;        // heads times tiles of their rows R; m * group; tiles of them
+    int shares;                        // workgroups that share all items; every item is one's of its own where that is 0
+    bool whole;                        // none of them has parts of two items
+    int* arrived;                      // [items]: workgroups that are done with their part of an item; 0 between the calls
+    float* part_o;                     // [shares + 2 items][16][128]: of workgroup w and item i at w + i, which no other pair has
+    f32x2a* part_ml;                   // the same of maxima and sums
 };
 
 enum Format { kNone = -1, kBf16 = 0, kF32 = 1, kMxBf16 = 2, kMxF32 = 3 };
@@ -54,19 +61,25 @@ struct Running {
     float top, sum;                    // of R so far (top: of all quarters; sum: of the lane's keys)
 };
 
-// o += V^T P^T for bf16 rows: v[e] the lane's 8 channels of key e of its quarter, p[e] that key's weights.
+// o += V^T P^T for bf16 rows: v[e] the lane's 8 channels of key e of its quarter, p[e] that key's weights; of 16 keys, or of 32.
 __device__ __forceinline__ f32x4a product(u32x4a x, u32x4a y, f32x4a z) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, y), z, 0, 0, 0);
 }
-__device__ __forceinline__ void add_values(const u32x4a* v, const float* p, f32x4a* o) {
-    u32x4a pb;
+__device__ __forceinline__ f32x4a product(u32x2 x, u32x2 y, f32x4a z) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4a, x), __builtin_bit_cast(s16x4a, y), z, 0, 0, 0);
+}
+template <int E> struct PairsOf;       // E keys of a lane, two to a register
+template <> struct PairsOf<4> { typedef u32x2 type; };
+template <> struct PairsOf<8> { typedef u32x4a type; };
+template <int E>
+__device__ __forceinline__ void add_values(const u32x4a (&v)[E], const float* p, f32x4a* o) {
+    typename PairsOf<E>::type pb, even, odd;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) pb[u] = pack_bf16(p[2 * u], p[2 * u + 1]);
+    for (int u = 0; u < E / 2; ++u) pb[u] = pack_bf16(p[2 * u], p[2 * u + 1]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        u32x4a even, odd;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < E / 2; ++u) {
             even[u] = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x05040100u);
             odd[u] = __builtin_amdgcn_perm(v[2 * u + 1][w], v[2 * u][w], 0x07060302u);
         }
@@ -75,7 +88,7 @@ __device__ __forceinline__ void add_values(const u32x4a* v, const float* p, f32x
     }
 }
 // (fp32 products: exact to 2^-24 a product, 1/16 of the bf16 rate, which the rows' bytes still hide)
-__device__ __forceinline__ void add_values(const float (*v)[8], const float* p, f32x4a* o) {
+__device__ __forceinline__ void add_values(const float (&v)[4][8], const float* p, f32x4a* o) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -85,15 +98,16 @@ __device__ __forceinline__ void add_values(const float (*v)[8], const float* p, 
 // Infinities and NaN in rows that some R does not see must not meet its zero weight.  Zeros take their place, and the R that do see one
 // (seen: a bit for each of the lane's keys) get it whatever its weight: where a product of "is such a value" with "is seen" is not zero.
 constexpr uint32_t kInf16 = 0x7F80u;
-__device__ __forceinline__ bool any_not_finite(const u32x4a* v) {
+template <int E>
+__device__ __forceinline__ bool any_not_finite(const u32x4a (&v)[E]) {
     bool bad = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < E; ++e)
 #pragma unroll
         for (int w = 0; w < 4; ++w) bad |= (v[e][w] & kInf16) == kInf16 || (v[e][w] & (kInf16 << 16)) == kInf16 << 16;
     return __any(bad);
 }
-__device__ __forceinline__ bool any_not_finite(const float (*v)[8]) {
+__device__ __forceinline__ bool any_not_finite(const float (&v)[4][8]) {
     bool bad = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -104,10 +118,11 @@ __device__ __forceinline__ bool any_not_finite(const float (*v)[8]) {
 __device__ __forceinline__ uint32_t kind_of(uint32_t x, uint32_t inf, uint32_t sign) {      // 0: +inf, 1: -inf, 2: NaN, 3: finite
     return (x & inf) != inf ? 3u : x == inf ? 0u : x == (inf | sign) ? 1u : 2u;
 }
-__device__ __forceinline__ void spread_not_finite(u32x4a* v, uint32_t seen, f32x4a* o) {
-    u32x4a sees;
+template <int E>
+__device__ __forceinline__ void spread_not_finite(u32x4a (&v)[E], uint32_t seen, f32x4a* o) {
+    typename PairsOf<E>::type sees, has;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) sees[u] = (seen >> (2 * u) & 1 ? 0x3F80u : 0u) | (seen >> (2 * u + 1) & 1 ? 0x3F800000u : 0u);
+    for (int u = 0; u < E / 2; ++u) sees[u] = (seen >> (2 * u) & 1 ? 0x3F80u : 0u) | (seen >> (2 * u + 1) & 1 ? 0x3F800000u : 0u);
 #pragma unroll 1
     for (uint32_t kind = 0; kind < 3; ++kind) {
         const float value = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
@@ -115,9 +130,8 @@ __device__ __forceinline__ void spread_not_finite(u32x4a* v, uint32_t seen, f32x
         for (int w = 0; w < 4; ++w)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                u32x4a has;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+                for (int u = 0; u < E / 2; ++u) {
                     const uint32_t x = v[2 * u][w] >> (16 * h) & 0xFFFFu, y = v[2 * u + 1][w] >> (16 * h) & 0xFFFFu;
                     has[u] = (kind_of(x, kInf16, 0x8000u) == kind ? 0x3F80u : 0u) | (kind_of(y, kInf16, 0x8000u) == kind ? 0x3F800000u : 0u);
                 }
@@ -127,14 +141,14 @@ __device__ __forceinline__ void spread_not_finite(u32x4a* v, uint32_t seen, f32x
             }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < E; ++e)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             if ((v[e][w] & kInf16) == kInf16) v[e][w] &= 0xFFFF0000u;
             if ((v[e][w] & (kInf16 << 16)) == kInf16 << 16) v[e][w] &= 0xFFFFu;
         }
 }
-__device__ __forceinline__ void spread_not_finite(float (*v)[8], uint32_t seen, f32x4a* o) {
+__device__ __forceinline__ void spread_not_finite(float (&v)[4][8], uint32_t seen, f32x4a* o) {
 #pragma unroll 1
     for (uint32_t kind = 0; kind < 3; ++kind) {
         const float value = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
@@ -155,55 +169,69 @@ __device__ __forceinline__ void spread_not_finite(float (*v)[8], uint32_t seen, 
             if ((__float_as_uint(v[e][i]) & 0x7F800000u) == 0x7F800000u) v[e][i] = 0.f;
 }
 template <class V>
-__device__ __forceinline__ void add_values_masked(V* v, const float* p, uint32_t seen, f32x4a* o) {
+__device__ __forceinline__ void add_values_masked(V& v, const float* p, uint32_t seen, f32x4a* o) {
     if (any_not_finite(v)) spread_not_finite(v, seen, o);
     add_values(v, p, o);
 }
 
 // One tile of T keys in registers.  `first`: row of its first key in K and V; `count`: keys of it that there are (>= 1), the last
-// one stands in for those beyond.  MASKED: some key of it is hidden from some R.
+// one stands in for those beyond.  on = 0: nothing is asked of the tile, and all lanes load from its first bytes (the loads are there all the
+// same: a branch around them would make the compiler wait for all that are in flight).  MASKED: some key of it is hidden from some R.
 template <int F> struct Tile;
+
+// K in whole lines of 128 bytes (a line that passes the caches in halves is fetched twice): an instruction takes 8 rows' 8 pieces of 16 bytes, lane
+// (quarter, c) piece quarter + 4 (c / 8) of row c % 8 of 8.  What the A operand has in lane c < 8 from the second row of 8 and in lane c >= 8 from the
+// first then lies 8 lanes off: x, of rows 0..7, and y, of rows 8..15, become pieces quarter and quarter + 4 of row c.
+__device__ __forceinline__ void to_rows(u32x4a& x, u32x4a& y) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int a = (int)x[i], b = (int)y[i];
+        x[i] = (uint32_t)__builtin_amdgcn_update_dpp(a, b, 0x128, 0xF, 0xC, false);       // row_ror:8, lanes 8..15 of 16
+        y[i] = (uint32_t)__builtin_amdgcn_update_dpp(b, a, 0x128, 0xF, 0x3, false);       // lanes 0..7
+    }
+}
+
+// Rows used once by a call that reads more than the caches hold pass them by.
+template <bool PAST, class T>
+__device__ __forceinline__ T fetched(const void* p) {
+    return PAST ? __builtin_nontemporal_load((const T*)p) : *(const T*)p;
+}
 
 template <>
 struct Tile<kBf16> {
-    static constexpr int T = 32;
-    u32x4a k[2][4], v[8];
-    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t*, const uint8_t*, int64_t first, int count, int lane) {
+    static constexpr int T = 16;
+    u32x4a k[4], v[4];
+    template <bool PAST>
+    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t*, const uint8_t*, int64_t first, int count, int lane, uint32_t on = ~0u) {
         const int c = lane & 15, quarter = lane >> 4;
         const char* Kb = (const char*)K + first * 256;
         const char* Vb = (const char*)V + first * 256;
         if (count == T) {
-            const uint32_t k_at = (c >> 2) * 2048 + (c & 3) * 256 + quarter * 16, v_at = quarter * 2048 + c * 16;
+            const uint32_t k_at = ((c & 7) * 256 + (quarter + (c >> 3) * 4) * 16) & on;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int s = 0; s < 4; ++s) k[s] = fetched<PAST, u32x4a>(Kb + k_at + (s & 1) * 2048 + (s >> 1) * 128);
+            const uint32_t v_at = (quarter * 1024 + c * 16) & on;
 #pragma unroll
-                for (int s = 0; s < 4; ++s) k[t][s] = *(const u32x4a*)(Kb + k_at + t * 1024 + s * 64);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = *(const u32x4a*)(Vb + v_at + e * 256);
+            for (int e = 0; e < 4; ++e) v[e] = fetched<PAST, u32x4a>(Vb + v_at + e * 256);
             return;
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int key = min((c >> 2) * 8 + t * 4 + (c & 3), count - 1);
+        for (int s = 0; s < 4; ++s) k[s] = *(const u32x4a*)(Kb + (uint32_t)(min((s & 1) * 8 + (c & 7), count - 1) * 256 + (quarter + (c >> 3) * 4) * 16 + (s >> 1) * 128));
 #pragma unroll
-            for (int s = 0; s < 4; ++s) k[t][s] = *(const u32x4a*)(Kb + (uint32_t)(key * 256 + (s * 4 + quarter) * 16));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = *(const u32x4a*)(Vb + (uint32_t)(min(quarter * 8 + e, count - 1) * 256 + c * 16));
+        for (int e = 0; e < 4; ++e) v[e] = *(const u32x4a*)(Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 256 + c * 16));
     }
     __device__ __forceinline__ static void queries(Queries& q, const void* row, int quarter) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) q.q[s] = ((const u32x4a*)row)[s * 4 + quarter];
     }
-    __device__ __forceinline__ void scores(const Queries& q, float* s) const {
+    __device__ __forceinline__ void scores(const Queries& q, float* s) {
+        to_rows(k[0], k[1]);
+        to_rows(k[2], k[3]);
+        f32x4a a = {0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4a a = {0, 0, 0, 0};
+        for (int i = 0; i < 4; ++i) a = product(k[i], q.q[i], a);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a = product(k[t][i], q.q[i], a);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[t * 4 + j] = a[j];
-        }
+        for (int j = 0; j < 4; ++j) s[j] = a[j];
     }
     template <bool MASKED>
     __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
@@ -215,24 +243,27 @@ struct Tile<kBf16> {
 template <>
 struct Tile<kF32> {
     static constexpr int T = 16;
-    f32x4a k[8];
+    u32x4a k[8];
     float v[4][8];
-    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t*, const uint8_t*, int64_t first, int count, int lane) {
+    template <bool PAST>
+    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t*, const uint8_t*, int64_t first, int count, int lane, uint32_t on = ~0u) {
         const int c = lane & 15, quarter = lane >> 4;
         const char* Kb = (const char*)K + first * 512;
         const char* Vb = (const char*)V + first * 512;
-        const uint32_t k_at = min(c, count - 1) * 512 + quarter * 16;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) k[s] = *(const f32x4a*)(Kb + k_at + s * 64);
         if (count == T) {
-            const uint32_t v_at = quarter * 2048 + c * 32;
+            const uint32_t k_at = ((c & 7) * 512 + (quarter + (c >> 3) * 4) * 16) & on;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) k[s] = fetched<PAST, u32x4a>(Kb + k_at + (s & 1) * 4096 + (s >> 1) * 128);
+            const uint32_t v_at = (quarter * 2048 + c * 32) & on;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                *(f32x4a*)&v[e][0] = *(const f32x4a*)(Vb + v_at + e * 512);
-                *(f32x4a*)&v[e][4] = *(const f32x4a*)(Vb + v_at + e * 512 + 16);
+                *(f32x4a*)&v[e][0] = fetched<PAST, f32x4a>(Vb + v_at + e * 512);
+                *(f32x4a*)&v[e][4] = fetched<PAST, f32x4a>(Vb + v_at + e * 512 + 16);
             }
             return;
         }
+#pragma unroll
+        for (int s = 0; s < 8; ++s) k[s] = *(const u32x4a*)(Kb + (uint32_t)(min((s & 1) * 8 + (c & 7), count - 1) * 512 + (quarter + (c >> 3) * 4) * 16 + (s >> 1) * 128));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const char* row = Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 512 + c * 32);
@@ -244,12 +275,14 @@ struct Tile<kF32> {
 #pragma unroll
         for (int s = 0; s < 8; ++s) q.q[s] = ((const u32x4a*)row)[s * 4 + quarter];
     }
-    __device__ __forceinline__ void scores(const Queries& q, float* s) const {
+    __device__ __forceinline__ void scores(const Queries& q, float* s) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) to_rows(k[i], k[i + 1]);
         f32x4a a = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][j], __uint_as_float(q.q[i][j]), a, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i][j]), __uint_as_float(q.q[i][j]), a, 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] = a[j];
     }
@@ -265,28 +298,25 @@ struct Tile<kF32> {
 template <>
 struct Tile<kMxBf16> {
     static constexpr int T = 32;
-    u32x4a k[2];
-    uint32_t v[8];
-    uint32_t ks[2], vs[8];
-    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs, int64_t first, int count, int lane) {
+    u32x4a k[2], vs[2];
+    uint32_t v[8], ks[2];
+    template <bool PAST>
+    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs, int64_t first, int count, int lane, uint32_t on = ~0u) {
         const int c = lane & 15, quarter = lane >> 4;
         const char* Kb = (const char*)K + first * 64;
         const char* Vb = (const char*)V + first * 64;
         const uint8_t* Kc = Ks + first * 4;
         const uint8_t* Vc = Vs + first * 4;
         if (count == T) {
-            const uint32_t key = (c >> 2) * 8 + (c & 3), k_at = key * 64 + quarter * 16, v_at = quarter * 512 + c * 4;
-            const uint32_t ks_at = key * 4 + quarter, vs_at = quarter * 32 + (c >> 2);
+            const uint32_t key = (c >> 2) * 8 + (c & 3), k_at = (key * 64 + quarter * 16) & on, v_at = (quarter * 512 + c * 4) & on, ks_at = (key * 4 + quarter) & on;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 k[t] = *(const u32x4a*)(Kb + k_at + t * 256);
                 ks[t] = *(Kc + ks_at + t * 16);
+                __builtin_memcpy(&vs[t], Vc + quarter * 32 + t * 16, 16);       // (rows' scales lie at multiples of 4 bytes)
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = *(const uint32_t*)(Vb + v_at + e * 64);
-                vs[e] = *(Vc + vs_at + e * 4);
-            }
+            for (int e = 0; e < 8; ++e) v[e] = *(const uint32_t*)(Vb + v_at + e * 64);
             return;
         }
 #pragma unroll
@@ -299,7 +329,7 @@ struct Tile<kMxBf16> {
         for (int e = 0; e < 8; ++e) {
             const int key = min(quarter * 8 + e, count - 1);
             v[e] = *(const uint32_t*)(Vb + (uint32_t)(key * 64 + c * 4));
-            vs[e] = Vc[(uint32_t)(key * 4 + (c >> 2))];
+            vs[e / 4][e % 4] = *(const uint32_t*)(Vc + (uint32_t)(key * 4));
         }
     }
     __device__ __forceinline__ static void queries(Queries& q, const void* row, int quarter) {
@@ -320,10 +350,11 @@ struct Tile<kMxBf16> {
     }
     template <bool MASKED>
     __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
-        u32x4a x[8];
+        const int shift = (threadIdx.x >> 2 & 3) * 8;                          // (of the block that the lane's channels lie in)
+u32x4a x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float unit = unit_of(vs[e]);
+            const float unit = unit_of(vs[e / 4][e % 4] >> shift & 255u);
             x[e] = (u32x4a){two_bf16<0>(v[e], unit), two_bf16<1>(v[e], unit), two_bf16<2>(v[e], unit), two_bf16<3>(v[e], unit)};
         }
         // (a masked tile of kept rows ends them: its other keys repeat the last one, which every R sees, so nothing hidden is not finite alone)
@@ -336,7 +367,8 @@ struct Tile<kMxF32> {
     static constexpr int T = 16;
     u32x4a k;
     uint32_t v[4], ks, vs[4];
-    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs, int64_t first, int count, int lane) {
+    template <bool PAST>
+    __device__ __forceinline__ void load(const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs, int64_t first, int count, int lane, uint32_t on = ~0u) {
         const int c = lane & 15, quarter = lane >> 4;
         const int key = min(c, count - 1);
         k = *(const u32x4a*)((const char*)K + first * 64 + (uint32_t)(key * 64 + quarter * 16));
@@ -409,28 +441,45 @@ __device__ __forceinline__ void take(Running& r, Tile<F>& x, const Queries& q, f
     x.template values<MASKED>(s, seen, r.o);
 }
 
-// What a (head, row tile) has to read: tiles that all its R see all of, in chunks, from the kept rows, the first rows and the rows near; and
+// What an item (a head's row tile) has to read: tiles that all its R see all of, from the kept rows, the first rows and the rows near; and
 // tiles to be masked: the ends of those three, and where the window's edge and the diagonal pass.
+struct Head {                          // what a head has, from the call's arrays
+    int64_t begin;                     // first kept row
+    int kept, length;                  // kept rows; rows of the cache
+};
+__device__ __forceinline__ Head head_of(const SplitArgs& a, int g) {
+    const AttendCall& c = a.c;
+    Head h{0, 0, 0};
+    if (c.offsets) {
+        h.begin = min(max(c.offsets[g], (int64_t)0), c.total);
+        h.kept = (int)(min(max(c.offsets[g + 1], h.begin), c.total) - h.begin);
+    }
+    h.length = c.n > 0 ? (c.lengths ? min(max(c.lengths[g / c.kv], 0), c.n) : c.n) : 0;
+    return h;
+}
 template <int FA, int FB>
 struct Work {
     static constexpr int TA = Tile<FA == kNone ? kBf16 : FA>::T, TB = Tile<FB>::T;
-    int64_t begin = 0, kept = 0, kept_tiles = 0, kept_chunks = 0;
+    // What a tile costs, in units that the work is shared out by: its bytes, and the expansion of 4 bits.
+    static constexpr int kUnitA = 1, kUnitB = FA == kMxF32 ? 3 : FA == kMxBf16 ? 2 : 1;
+    int64_t begin = 0;                                     // first kept row
+    int kept = 0, kept_tiles = 0;                          // (an item's rows and all units together are below 2^31: they lie in 288 GB)
     Seen seen;
     int t0, t1;
     int first_tiles, near_begin, near_end, near_tiles;     // whole first rows; of the tiles from seen.low on: whole ones, and all
-    int cache_tiles, cache_chunks;                         // whole ones of the cache
+    int cache_tiles;                                       // whole ones of the cache
     int low_masked, cache_masked;                          // masked ones: before near_begin; all
-    __device__ __forceinline__ Work(const SplitArgs& a, int g, int row_tile) {
+    int kept_all, units;                                   // kept tiles with the last one, which may be short
+    __device__ __forceinline__ Work(const SplitArgs& a, int item) : Work(a, item, head_of(a, item / a.row_tiles)) {}
+    __device__ __forceinline__ Work(const SplitArgs& a, int item, const Head& head) {
         const AttendCall& c = a.c;
+        const int row_tile = item % a.row_tiles, length = head.length;
         t0 = row_tile * kRowTile / c.group;
         t1 = min(c.m - 1, (row_tile * kRowTile + kRowTile - 1) / c.group);
-        if (FA != kNone) {
-            begin = min(max(c.offsets[g], (int64_t)0), c.total);
-            kept = min(max(c.offsets[g + 1], begin), c.total) - begin;
-            kept_tiles = kept / TA;
-            kept_chunks = (kept_tiles + a.chunk - 1) / a.chunk;
-        }
-        const int length = c.n > 0 ? (c.lengths ? min(max(c.lengths[g / c.kv], 0), c.n) : c.n) : 0;
+        begin = head.begin;
+        kept = head.kept;
+        kept_tiles = kept / TA;
+        kept_all = kept_tiles + (kept % TA != 0);
         seen = seen_rows(length, c.m, t0, t1, c.window, c.sinks);
         const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;    // rows from low on that the last token does not see
         first_tiles = seen.first / TB;
@@ -438,211 +487,368 @@ struct Work {
         near_end = max(0, min(seen.high, seen.p0 + 1) - seen.low) / TB;
         near_begin = min((hidden + TB - 1) / TB, near_end);
         cache_tiles = first_tiles + near_end - near_begin;
-        cache_chunks = (cache_tiles + a.chunk - 1) / a.chunk;
         low_masked = (seen.first % TB != 0) + near_begin;
         cache_masked = low_masked + near_tiles - near_end;
+        units = max(1, kept_all * kUnitA + (cache_tiles + cache_masked) * kUnitB);   // (nothing to read: still somebody's to write)
     }
-    __device__ __forceinline__ int shares(const SplitArgs& a) const { return (int)min((int64_t)a.shares, max((int64_t)1, kept_chunks + cache_chunks)); }
     __device__ __forceinline__ int row_of(int tile) const { return tile < first_tiles ? tile * TB : seen.low + (near_begin + tile - first_tiles) * TB; }
 };
 
-// Which whole tiles a wave takes: chunks first, first + shares, ..; of each its tiles wave, wave + 4, ..
-struct Walk {
-    int64_t chunk, chunks, tiles;
-    int shares, per, at, wave;
-    __device__ __forceinline__ Walk(int64_t first, int64_t chunks_, int64_t tiles_, int shares_, int chunk_tiles, int wave_)
-        : chunk(first), chunks(chunks_), tiles(tiles_), shares(shares_), per(chunk_tiles), at(wave_), wave(wave_) {}
-    __device__ __forceinline__ int64_t next() {            // -1: no more
-        for (;;) {
-            if (chunk >= chunks) return -1;
-            const int64_t tile = chunk * per + at;
-            if (at < per && tile < tiles) {
-                at += kSplitWaves;
-                return tile;
-            }
-            at = wave;
-            chunk += shares;
-        }
-    }
-};
-
-// The walk's tiles one after the other, the next one's loads in flight behind the one at hand.
+// Tiles from, from + 4, .. below `end` one after the other, the next one's loads in flight behind the one at hand.
 template <int F, class L>
-__device__ __forceinline__ void stream(Walk walk, Running& r, const Queries& q, float scale_log2, L load) {
+__device__ __forceinline__ void stream(int from, int end, Running& r, const Queries& q, float scale_log2, L load) {
+    if (from >= end) return;
     Tile<F> x, y;
-    int64_t tx = walk.next(), ty;
-    if (tx < 0) return;
-    load(x, tx);
+    load(x, from, ~0u);
     for (;;) {
-        ty = walk.next();
-        load(y, ty < 0 ? tx : ty);
+        const int next = from + kSplitWaves;
+        load(y, next < end ? next : from, next < end ? ~0u : 0u);
         take<F, false>(r, x, q, scale_log2, 0u);
-        if (ty < 0) return;
-        tx = walk.next();
-        load(x, tx < 0 ? ty : tx);
+        if (next >= end) return;
+        from = next + kSplitWaves;
+        load(x, from < end ? from : next, from < end ? ~0u : 0u);
         take<F, false>(r, y, q, scale_log2, 0u);
-        if (tx < 0) return;
+        if (from >= end) return;
     }
 }
 
+__device__ __forceinline__ int ceil_div(int x, int y) { return (x + y - 1) / y; }
+
+// A workgroup's place in the list of all items.
+struct Place {
+    int item, into, size;              // units of the item in front of the share; of the share (0: nothing to do)
+    int first, last;                   // workgroups that have a part of the item
+    Head head;                         // of the item
+};
+// Shares of equal size, whatever the heads' lengths: where a share ends inside an item, its neighbour has the rest, and a workgroup may have parts of
+// several items.  What it takes to end one item and begin the next, about 4 us, counts as kBetween units in front of an item.  Few items (a.whole): every one
+// has workgroups of its own, in proportion to its units, and a share is one part.
+// (Every wave for itself: a lane adds up its items, the lanes' sums are added up by shuffles, and the lane that has the share's begin is asked.)
+__device__ __forceinline__ int added_up(int x) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const int y = __shfl_up(x, k);
+        if (lane >= k) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ Head head_from(const Head& h, int lane) {
+    Head r;
+    r.begin = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)h.begin, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(h.begin >> 32), lane) << 32);
+    r.kept = __builtin_amdgcn_readlane(h.kept, lane);
+    r.length = __builtin_amdgcn_readlane(h.length, lane);
+    return r;
+}
 template <int FA, int FB>
-__global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(SplitArgs a) {
-    __shared__ __attribute__((aligned(16))) float part[kSplitWaves][kRowTile][128 + 4];
-    __shared__ float tops[kSplitWaves][kRowTile], sums[kSplitWaves][kRowTile];
-    const AttendCall& c = a.c;
-    const int share = blockIdx.x % a.shares;
-    const int g = blockIdx.x / a.shares % a.groups, row_tile = blockIdx.x / a.shares / a.groups;
-    const Work<FA, FB> work(a, g, row_tile);
-    const int shares = work.shares(a);
-    if (share >= shares) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
-    const int b = g / c.kv, head = g % c.kv;
-    constexpr int kBytes = FB == kBf16 ? 2 : 4;
-
-    // this lane's query row (rows beyond the last repeat it; nothing of them is written)
-    const int R = min(row_tile * kRowTile + col, a.rows - 1), t = R / c.group;
-    const char* q_row = (const char*)c.Q + ((((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group) * (128 * kBytes);
-    Queries q;
-    Running r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.o[i] = (f32x4a){0, 0, 0, 0};
-    r.top = -INFINITY;
-    r.sum = 0.f;
-
-    if constexpr (FA != kNone) {
-        constexpr int T = Tile<FA>::T;
-        Tile<FA>::queries(q, q_row, quarter);
-        stream<FA>(Walk(share, work.kept_chunks, work.kept_tiles, shares, a.chunk, wave), r, q, a.scale_log2, [&](Tile<FA>& x, int64_t tile) {
-            x.load(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + tile * T, T, lane);
-        });
-        const int left = (int)(work.kept - work.kept_tiles * T);
-        if (left > 0 && share == shares - 1 && wave == kSplitWaves - 1) {
-            Tile<FA> x;
-            x.load(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + work.kept_tiles * T, left, lane);
-            take<FA, true>(r, x, q, a.scale_log2, (1u << min(max(left - quarter * (T / 4), 0), 8)) - 1u);
+struct Places {
+    static constexpr int kBetween = 8, kAtOnce = 4;
+    const SplitArgs& a;
+    int all, shares, at;               // units of all items; workgroups with a share; units in front of the item at hand, without its kBetween
+    __device__ __forceinline__ int begin_of(int share) const { return (int)((int64_t)all * share / shares); }
+    __device__ __forceinline__ int share_of(int unit) const { return (int)((((int64_t)unit + 1) * shares - 1) / all); }     // whose share holds a unit
+    __device__ __forceinline__ void owners(Place& p, int units) const {
+        if (a.whole) return;
+        p.first = share_of(at + kBetween);
+        p.last = share_of(at + kBetween + units - 1);
+    }
+    __device__ __forceinline__ Place find() {
+        const int lane = threadIdx.x & 63, each = (a.items + 63) / 64, from = min(lane * each, a.items), end = min(from + each, a.items), block = blockIdx.x;
+        Place p{0, 0, 0, 0, 0, {0, 0, 0}};
+        int owner;
+        if (a.whole) {                 // (each == 1)
+            const Head head = head_of(a, min(from, a.items - 1) / a.row_tiles);
+            const int mine = lane < a.items ? Work<FA, FB>(a, from, head).units : 0;
+            all = __builtin_amdgcn_readlane(added_up(mine), 63);
+            const int parts = lane < a.items ? min(mine, max(1, (int)((int64_t)mine * a.shares / all))) : 0, parts_up_to = added_up(parts);
+            const uint64_t beyond = __ballot(block < parts_up_to);
+            if (!beyond) return p;
+            owner = __builtin_ctzll(beyond);
+            const int n = __builtin_amdgcn_readlane(parts, owner), units = __builtin_amdgcn_readlane(mine, owner);
+            p.first = __builtin_amdgcn_readlane(parts_up_to, owner) - n;
+            p.last = p.first + n - 1;
+            p.into = (int)((int64_t)units * (block - p.first) / n);
+            p.size = (int)((int64_t)units * (block - p.first + 1) / n) - p.into;
+            p.item = owner;
+            p.head = head_from(head, owner);
+            return p;
         }
-    }
-    constexpr int T = Tile<FB>::T;
-    const int64_t base = (int64_t)g * c.stride;
-    Tile<FB>::queries(q, q_row, quarter);
-    // (chunks of the cache follow those of the kept rows)
-    stream<FB>(Walk((share + shares - work.kept_chunks % shares) % shares, work.cache_chunks, work.cache_tiles, shares, a.chunk, wave), r, q, a.scale_log2,
-               [&](Tile<FB>& x, int64_t tile) { x.load(c.K, c.V, nullptr, nullptr, base + work.row_of((int)tile), T, lane); });
-    // (the last share and its last waves first: they have least of the rest)
-    for (int i = (shares - 1 - share) * kSplitWaves + kSplitWaves - 1 - wave; i < work.cache_masked; i += shares * kSplitWaves) {
-        const int near = i < work.low_masked ? i - (work.seen.first % T != 0) : work.near_end + i - work.low_masked;        // -1: the end of the first rows
-        const int j0 = near < 0 ? work.first_tiles * T : work.seen.low + near * T, count = min(T, (near < 0 ? work.seen.first : work.seen.high) - j0);
-        const int p = work.seen.p0 + (t - work.t0);
-        Tile<FB> x;
-        x.load(c.K, c.V, nullptr, nullptr, base + j0, count, lane);
-        uint32_t mask = 0;
+        // (the loads of four items at a time)
+        Head head[kAtOnce];
+        int units[kAtOnce], mine = 0;
+        for (int i = from; i < end; i += kAtOnce) {
 #pragma unroll
-        for (int e = 0; e < T / 4; ++e) {
-            const int k = quarter * (T / 4) + e;
-            mask |= k < count && sees(p, j0 + k, c.window, c.sinks) ? 1u << e : 0u;
+            for (int k = 0; k < kAtOnce; ++k) head[k] = head_of(a, min(i + k, a.items - 1) / a.row_tiles);
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                units[k] = i + k < end ? Work<FA, FB>(a, i + k, head[k]).units + kBetween : 0;
+                mine += units[k];
+            }
         }
-        take<FB, true>(r, x, q, a.scale_log2, mask);
+        const int up_to = added_up(mine);
+        all = __builtin_amdgcn_readlane(up_to, 63);
+        // (no more shares than tiles: none may be without any between two that have parts of one item)
+        shares = max(1, min(a.shares, (all - a.items * kBetween) / (kBetween + 1)));
+        const int begin = begin_of(block);
+        if (block >= shares) return p;
+        p.size = begin_of(block + 1) - begin;
+        owner = __builtin_ctzll(__ballot(begin < up_to));
+        int front = up_to - mine, i = from;
+        if (each <= kAtOnce) {         // (in its lane's registers)
+            Head mine_head = head[0];
+#pragma unroll
+            for (int k = 0; k + 1 < kAtOnce; ++k)
+                if (i == from + k && begin >= front + units[k]) {
+                    front += units[k];
+                    ++i;
+                    mine_head = head[k + 1];
+                }
+            p.item = __builtin_amdgcn_readlane(i, owner);
+            at = __builtin_amdgcn_readlane(front, owner);
+            p.head = head_from(mine_head, owner);
+        } else {
+            p.item = owner * each;
+            at = __builtin_amdgcn_readlane(front, owner);
+            for (;; ++p.item) {
+                p.head = head_of(a, p.item / a.row_tiles);
+                const int n = Work<FA, FB>(a, p.item, p.head).units + kBetween;
+                if (begin < at + n) break;
+                at += n;
+            }
+        }
+        p.into = begin - at - kBetween;
+        if (p.into < 0) {              // the share begins in front of the item
+            p.size += p.into;
+            p.into = 0;
+        }
+        return p;
     }
+};
 
-    // the four waves' parts
-    r.sum = quarters_sum(r.sum);
-    if (quarter == 0) {
-        tops[wave][col] = r.top;
-        sums[wave][col] = r.sum;
-    }
+__device__ __forceinline__ void store_shared(uint64_t* to, f32x2a x) {
+    __hip_atomic_store(to, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2a load_shared(const uint64_t* from) {
+    return __builtin_bit_cast(f32x2a, __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// Eight channels of row R's result, o un-normalised.
+template <int FB>
+__device__ __forceinline__ void write_row(const AttendCall& c, int g, int R, int d0, float* o, float top, float sum) {
+    const bool empty = top == -INFINITY;
+    const float over = empty ? 0.f : 1.f / sum;
+    const int b = g / c.kv, t = R / c.group, h = (g - b * c.kv) * c.group + R % c.group;
+    const int64_t out_row = ((int64_t)b * c.m + t) * c.kv * c.group + h;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        float* to = &part[wave][col][quarter * 32 + j * 8];
-        *(f32x4a*)to = (f32x4a){r.o[0][j], r.o[1][j], r.o[2][j], r.o[3][j]};
-        *(f32x4a*)(to + 4) = (f32x4a){r.o[4][j], r.o[5][j], r.o[6][j], r.o[7][j]};
-    }
-    __syncthreads();
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
-    const int Rw = row_tile * kRowTile + row;
-    if (Rw >= a.rows) return;
-    float top = tops[0][row], sum = 0.f, o[8] = {};
-#pragma unroll
-    for (int w = 1; w < kSplitWaves; ++w) top = fmaxf(top, tops[w][row]);
-    const float off = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int w = 0; w < kSplitWaves; ++w) {
-        const float weight = __builtin_amdgcn_exp2f(tops[w][row] - off);
-        if (tops[w][row] == -INFINITY) continue;           // (a wave without keys)
-        sum += weight * sums[w][row];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] += weight * part[w][row][d0 + i];
-    }
-    if (a.shares > 1) {
-        const int64_t at = ((int64_t)g * a.rows + Rw) * a.shares + share;
-        *(f32x4a*)(a.part_o + at * 128 + d0) = (f32x4a){o[0], o[1], o[2], o[3]};
-        *(f32x4a*)(a.part_o + at * 128 + d0 + 4) = (f32x4a){o[4], o[5], o[6], o[7]};
-        if (d0 == 0) a.part_ml[at] = (f32x2a){top, sum};
-        return;
-    }
-    const float over = top == -INFINITY ? 0.f : 1.f / sum;
-    const int tw = Rw / c.group, hw = head * c.group + Rw % c.group;
-    const int64_t out_row = ((int64_t)b * c.m + tw) * c.kv * c.group + hw;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = top == -INFINITY ? 0.f : o[i] * over;
+    for (int i = 0; i < 8; ++i) o[i] *= over;
     if (FB == kBf16) {
         *(u32x4a*)((char*)c.out + out_row * 256 + d0 * 2) = (u32x4a){pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7])};
     } else {
         *(f32x4a*)((char*)c.out + out_row * 512 + d0 * 4) = (f32x4a){o[0], o[1], o[2], o[3]};
         *(f32x4a*)((char*)c.out + out_row * 512 + d0 * 4 + 16) = (f32x4a){o[4], o[5], o[6], o[7]};
     }
-    if (c.lse && d0 == 0) c.lse[((int64_t)b * c.kv * c.group + hw) * c.m + tw] = top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (c.lse && d0 == 0) c.lse[((int64_t)b * c.kv * c.group + h) * c.m + t] = empty ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Joins the shares of one row: four waves take every fourth share, a lane two channels.
-template <int FA, int FB>
-__global__ __launch_bounds__(256) void attend_join_kernel(SplitArgs a) {
-    __shared__ float part[4][128], sums[4];
-    const AttendCall& c = a.c;
-    const int g = blockIdx.x / a.rows, R = blockIdx.x % a.rows;
-    const Work<FA, FB> work(a, g, R / kRowTile);
-    const int shares = work.shares(a);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)blockIdx.x * a.shares;
-    float top = -INFINITY;
-    for (int s = lane; s < shares; s += 64) top = fmaxf(top, a.part_ml[at + s].x);
+// The four waves' parts in LDS of the rows that 16 threads of 8 channels each take, put together.
+typedef float WaveParts[kSplitWaves][kRowTile][128 + 4];
+typedef float WaveValues[kSplitWaves][kRowTile];
+__device__ __forceinline__ void merge_waves(const WaveParts& part, const WaveValues& tops, const WaveValues& sums, int row, int d0, float* o, float& top, float& sum) {
+    top = tops[0][row];
 #pragma unroll
-    for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+    for (int w = 1; w < kSplitWaves; ++w) top = fmaxf(top, tops[w][row]);
     const float off = top == -INFINITY ? 0.f : top;
-    f32x2a o = {0, 0};
-    float sum = 0.f;
-#pragma unroll 4
-    for (int s = wave; s < shares; s += 4) {
-        const f32x2a ml = a.part_ml[at + s];
-        const f32x2a x = *(const f32x2a*)(a.part_o + (at + s) * 128 + lane * 2);
-        const float weight = __builtin_amdgcn_exp2f(ml.x - off);
-        sum += weight * ml.y;
-        o += weight * x;
-    }
-    part[wave][lane * 2] = o.x;
-    part[wave][lane * 2 + 1] = o.y;
-    if (lane == 0) sums[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    sum = sums[0] + sums[1] + sums[2] + sums[3];
-    const float over = top == -INFINITY ? 0.f : 1.f / sum;
-    float y[2];
+    sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int d = lane * 2 + i;
-        y[i] = top == -INFINITY ? 0.f : (part[0][d] + part[1][d] + part[2][d] + part[3][d]) * over;
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSplitWaves; ++w) {
+        const float weight = __builtin_amdgcn_exp2f(tops[w][row] - off);
+        sum += weight * sums[w][row];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] += weight * part[w][row][d0 + i];
     }
-    const int b = g / c.kv, t = R / c.group, h = (g % c.kv) * c.group + R % c.group;
-    const int64_t out_row = ((int64_t)b * c.m + t) * c.kv * c.group + h;
-    if (FB == kBf16) ((uint32_t*)c.out)[out_row * 64 + lane] = pack_bf16(y[0], y[1]);
-    else ((f32x2a*)c.out)[out_row * 64 + lane] = (f32x2a){y[0], y[1]};
-    if (c.lse && lane == 0) c.lse[((int64_t)b * c.kv * c.group + h) * c.m + t] = top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <int FA, int FB>
+// Joins workgroups w0 .. w1's parts of an item: a wave takes every fourth, 16 lanes a row.
+template <int FB>
+__device__ __forceinline__ void join(const SplitArgs& a, int item, int w0, int w1, WaveParts& part, WaveValues& tops, WaveValues& sums) {
+    const int g = item / a.row_tiles, wave = threadIdx.x >> 6, R0 = (item - g * a.row_tiles) * kRowTile, rows = min(kRowTile, a.rows - R0);
+    for (int row = threadIdx.x >> 4 & 3; row < rows; row += 4) {
+        const int d0 = (threadIdx.x & 15) * 8;
+        float top = -INFINITY, sum = 0.f, o[8] = {};
+        for (int first = w0 + wave; first <= w1; first += 4 * kSplitWaves) {
+            // (four parts' loads together; the last one again for those beyond it, without weight)
+            f32x2a ml[4], x[4][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t at = ((int64_t)min(first + k * kSplitWaves, w1) + item) * kRowTile + row;
+                ml[k] = load_shared((const uint64_t*)(a.part_ml + at));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[k][i] = load_shared((const uint64_t*)(a.part_o + at * 128 + d0) + i);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (first + k * kSplitWaves > w1) break;
+                const float next = fmaxf(top, ml[k].x), off = next == -INFINITY ? 0.f : next;
+                const float keep = __builtin_amdgcn_exp2f(top - off), weight = __builtin_amdgcn_exp2f(ml[k].x - off);
+                sum = sum * keep + weight * ml[k].y;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = o[i] * keep + weight * x[k][i / 2][i % 2];
+                top = next;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[wave][row][d0 + i] = o[i];
+        if (d0 == 0) tops[wave][row] = top, sums[wave][row] = sum;
+    }
+    __syncthreads();
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
+    if (row >= rows) return;
+    float o[8], top, sum;
+    merge_waves(part, tops, sums, row, d0, o, top, sum);
+    write_row<FB>(a.c, g, R0 + row, d0, o, top, sum);
+}
+
+// An item that the workgroup has a part of, and the workgroups that have others.
+struct Part {
+    int item, first, last;
+};
+
+template <int FA, int FB, bool PAST>
+__global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(SplitArgs a) {
+    __shared__ __attribute__((aligned(16))) WaveParts part;
+    __shared__ WaveValues tops, sums;
+    __shared__ bool last[2];
+    Part begun{-1, 0, 0}, ended{-1, 0, 0};                  // items that another workgroup has begun, or ends
+    const AttendCall& c = a.c;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+    constexpr int kBytes = FB == kBf16 ? 2 : 4;
+    Places<FA, FB> places{a, 0, 0, 0};
+    Place place{(int)blockIdx.x, 0, 0, 0, 0, {0, 0, 0}};
+    if (a.shares > 0) {
+        place = places.find();
+        if (place.size <= 0) return;
+    } else {
+        place.head = head_of(a, place.item / a.row_tiles);
+    }
+    for (int item = place.item;; ++item) {
+        const Work<FA, FB> work(a, item, place.head);
+        const int lo = a.shares > 0 ? place.into : 0, hi = a.shares > 0 ? min(work.units, lo + place.size) : work.units;
+        const int g = item / a.row_tiles, row_tile = item - g * a.row_tiles, b = g / c.kv, head = g % c.kv;
+
+        // this lane's query row (rows beyond the last repeat it; nothing of them is written)
+        const int R = min(row_tile * kRowTile + col, a.rows - 1), t = R / c.group;
+        const char* q_row = (const char*)c.Q + ((((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group) * (128 * kBytes);
+        Queries q;
+        Running r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.o[i] = (f32x4a){0, 0, 0, 0};
+        r.top = -INFINITY;
+        r.sum = 0.f;
+
+        if constexpr (FA != kNone) {
+            constexpr int T = Tile<FA>::T;
+            const int from = min(ceil_div(lo, work.kUnitA), work.kept_all), end = min(ceil_div(hi, work.kUnitA), work.kept_all);
+            if (from < end) {
+                Tile<FA>::queries(q, q_row, quarter);
+                stream<FA>(from + wave, min(end, work.kept_tiles), r, q, a.scale_log2, [&](Tile<FA>& x, int tile, uint32_t on) {
+                    x.template load<PAST>(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + (int64_t)tile * T, T, lane, on);
+                });
+                if (end > work.kept_tiles && wave == (work.kept_tiles - from) % kSplitWaves) {
+                    const int left = work.kept - work.kept_tiles * T;
+                    Tile<FA> x;
+                    x.template load<PAST>(c.K_kept, c.V_kept, c.K_scales, c.V_scales, work.begin + (int64_t)work.kept_tiles * T, left, lane);
+                    take<FA, true>(r, x, q, a.scale_log2, (1u << min(max(left - quarter * (T / 4), 0), T / 4)) - 1u);
+                }
+            }
+        }
+        constexpr int T = Tile<FB>::T;
+        const int all = work.cache_tiles + work.cache_masked, before = work.kept_all * work.kUnitA;
+        const int from = min(ceil_div(max(lo - before, 0), work.kUnitB), all), end = min(ceil_div(max(hi - before, 0), work.kUnitB), all);
+        if (from < end) {
+            const int64_t base = (int64_t)g * c.stride;
+            Tile<FB>::queries(q, q_row, quarter);
+            stream<FB>(from + wave, min(end, work.cache_tiles), r, q, a.scale_log2,
+                       [&](Tile<FB>& x, int tile, uint32_t on) { x.template load<PAST>(c.K, c.V, nullptr, nullptr, base + work.row_of(tile), T, lane, on); });
+            const int masked = max(from, work.cache_tiles) - work.cache_tiles, turn = (max(from, work.cache_tiles) - from) % kSplitWaves;
+            for (int i = masked + (wave - turn + kSplitWaves) % kSplitWaves; i < end - work.cache_tiles; i += kSplitWaves) {
+                const int near = i < work.low_masked ? i - (work.seen.first % T != 0) : work.near_end + i - work.low_masked;        // -1: the end of the first rows
+                const int j0 = near < 0 ? work.first_tiles * T : work.seen.low + near * T, count = min(T, (near < 0 ? work.seen.first : work.seen.high) - j0);
+                const int p = work.seen.p0 + (t - work.t0);
+                Tile<FB> x;
+                x.template load<PAST>(c.K, c.V, nullptr, nullptr, base + j0, count, lane);
+                uint32_t mask = 0;
+#pragma unroll
+                for (int e = 0; e < T / 4; ++e) {
+                    const int k = quarter * (T / 4) + e;
+                    mask |= k < count && sees(p, j0 + k, c.window, c.sinks) ? 1u << e : 0u;
+                }
+                take<FB, true>(r, x, q, a.scale_log2, mask);
+            }
+        }
+
+        // the four waves' parts
+        r.sum = quarters_sum(r.sum);
+        if (quarter == 0) {
+            tops[wave][col] = r.top;
+            sums[wave][col] = r.sum;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float* to = &part[wave][col][quarter * 32 + j * 8];
+            *(f32x4a*)to = (f32x4a){r.o[0][j], r.o[1][j], r.o[2][j], r.o[3][j]};
+            *(f32x4a*)(to + 4) = (f32x4a){r.o[4][j], r.o[5][j], r.o[6][j], r.o[7][j]};
+        }
+        __syncthreads();
+        const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
+        const int Rw = row_tile * kRowTile + row;
+        if (Rw < a.rows) {
+            float o[8], top, sum;
+            merge_waves(part, tops, sums, row, d0, o, top, sum);
+            if (lo > 0 || hi < work.units) {
+                // (past the caches of this XCD: atomic stores and loads of the device's scope are coherent between them)
+                const int64_t at = ((int64_t)blockIdx.x + item) * kRowTile + row;
+                uint64_t* to = (uint64_t*)(a.part_o + at * 128 + d0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) store_shared(to + i, f32x2a{o[2 * i], o[2 * i + 1]});
+                if (d0 == 0) store_shared((uint64_t*)(a.part_ml + at), f32x2a{top, sum});
+            } else {
+                write_row<FB>(c, g, Rw, d0, o, top, sum);
+            }
+        }
+        if (a.shares == 0) return;
+        if (lo > 0 || hi < work.units) {                   // (the first or the last of this workgroup's items)
+            places.owners(place, work.units);
+            (lo > 0 ? begun : ended) = Part{item, place.first, place.last};
+        }
+        places.at += work.units + places.kBetween;
+        place.size -= hi - lo + places.kBetween;
+        place.into = 0;
+        if (place.size <= 0 || item + 1 >= a.items) break;
+        place.head = head_of(a, (item + 1) / a.row_tiles);
+        __syncthreads();                                   // (part, tops and sums are read)
+    }
+    // Of all workgroups that have a part of an item, the last one to be done joins them.
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        last[0] = begun.item >= 0 && __hip_atomic_fetch_add(&a.arrived[begun.item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == begun.last - begun.first;
+        last[1] = ended.item >= 0 && __hip_atomic_fetch_add(&a.arrived[ended.item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == ended.last - ended.first;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k)
+        if (last[k]) {
+            const Part& p = k == 0 ? begun : ended;
+            join<FB>(a, p.item, p.first, p.last, part, tops, sums);
+            if (threadIdx.x == 0) __hip_atomic_store(&a.arrived[p.item], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+        }
+}
+
+template <int FA, int FB, bool PAST>
 hipError_t launch(const SplitArgs& a, hipStream_t stream) {
-    const int64_t blocks = (int64_t)a.shares * a.groups * a.row_tiles;
-    attend_split_kernel<FA, FB><<<(unsigned)blocks, kSplitWaves * 64, 0, stream>>>(a);
-    if (a.shares > 1) attend_join_kernel<FA, FB><<<(unsigned)((int64_t)a.groups * a.rows), 256, 0, stream>>>(a);
+    attend_split_kernel<FA, FB, PAST><<<(unsigned)(a.whole ? a.shares + a.items : a.shares > 0 ? a.shares : a.items), kSplitWaves * 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -652,30 +858,34 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     SplitArgs a;
     a.c = call;
     a.scale_log2 = call.scale * (1.f / kLn2);
-    a.groups = (int)(call.count * call.kv);
     a.rows = call.m * call.group;
     a.row_tiles = (a.rows + kRowTile - 1) / kRowTile;
-    // tiles of keys that a head has on average, as far as the host knows
+    a.items = (int)(call.count * call.kv * a.row_tiles);
+    // A workgroup a unit, that share the tiles of all heads equally, each with a tile a wave at least as far as the host knows; a workgroup an item where
+    // the items alone are many times that, or where there is no room for partial results.
     const bool mx = call.K_scales != nullptr, f32 = call.dtype == CURDKV_DTYPE_F32;
-    const int T = f32 ? 16 : 32;
+    const int T = mx && !f32 ? 32 : 16, row = f32 ? 512 : 256;
     int64_t keys = call.n;
-    if (call.window > 0) keys = min(keys, (int64_t)call.window + call.sinks + call.m);
-    const int64_t kept = call.offsets ? (call.rows + a.groups - 1) / a.groups : 0;
-    const int64_t tiles = (kept + T - 1) / T + (keys + T - 1) / T;
-    const int64_t others = (int64_t)a.groups * a.row_tiles;
-    // two workgroups a unit, in chunks of one tile a wave or more; room for heads of four times the average
-    const int64_t wanted = max((int64_t)1, (2 * ctx->num_cu + others - 1) / others);
-    int64_t chunk = ((tiles + wanted - 1) / wanted + kSplitWaves - 1) / kSplitWaves * kSplitWaves;
-    a.chunk = (int)max((int64_t)kSplitWaves, min(chunk, (int64_t)1 << 20));
-    const int64_t rooms = call.scratch ? min(kPartRows, call.scratch_bytes / kPartBytes) : 0;
-    int64_t shares = call.offsets ? 4 * ((kept + T - 1) / T) / a.chunk + 2 + (keys + T - 1) / T / a.chunk : (tiles + a.chunk - 1) / a.chunk + (call.sinks > 0);
-    shares = max((int64_t)1, min(shares, min(4 * wanted, rooms / ((int64_t)a.groups * a.rows))));
+    if (call.window > 0) keys = std::min(keys, (int64_t)call.window + call.sinks + call.m);
+    const int64_t heads = call.count * call.kv, tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles;
+    int64_t shares = std::min((int64_t)ctx->num_cu, std::max((int64_t)a.items, (tiles + kSplitWaves - 1) / kSplitWaves));
+    const int64_t slot = kRowTile * kPartBytes, room = call.scratch ? (call.scratch_bytes - kCounters * (int64_t)sizeof(int)) / slot : 0;
+    shares = std::min(shares, room - 2 * a.items);
+    if (shares <= a.items / 4 || a.items > kCounters) shares = 0;
     a.shares = (int)shares;
-    a.part_o = (float*)call.scratch;
-    a.part_ml = (f32x2a*)(a.part_o + (int64_t)a.groups * a.rows * a.shares * 128);
-    if (!call.offsets) return f32 ? launch<kNone, kF32>(a, stream) : launch<kNone, kBf16>(a, stream);
-    if (mx) return f32 ? launch<kMxF32, kF32>(a, stream) : launch<kMxBf16, kBf16>(a, stream);
-    return f32 ? launch<kF32, kF32>(a, stream) : launch<kBf16, kBf16>(a, stream);
+    a.whole = 8 * a.items <= a.shares && a.items <= 64;
+    a.arrived = (int*)call.scratch;
+    a.part_o = (float*)(a.arrived + kCounters);
+    a.part_ml = (f32x2a*)(a.part_o + (shares + 2 * a.items) * kRowTile * 128);
+    // (bytes that 256 MB of Infinity Cache would not hold until the next call)
+    const bool past = 2 * row * ((mx ? 0 : call.rows) + heads * keys) > kPastCaches;
+    if (mx) return f32 ? launch<kMxF32, kF32, false>(a, stream) : launch<kMxBf16, kBf16, false>(a, stream);
+    if (!call.offsets) {
+        if (past) return f32 ? launch<kNone, kF32, true>(a, stream) : launch<kNone, kBf16, true>(a, stream);
+        return f32 ? launch<kNone, kF32, false>(a, stream) : launch<kNone, kBf16, false>(a, stream);
+    }
+    if (past) return f32 ? launch<kF32, kF32, true>(a, stream) : launch<kBf16, kBf16, true>(a, stream);
+    return f32 ? launch<kF32, kF32, false>(a, stream) : launch<kBf16, kBf16, false>(a, stream);
 }
 
 }  // namespace curdkv

@@ -321,7 +321,7 @@ class Context:
             given = self._own_scratch
             if given is None:
                 import torch
-                given = self._own_scratch = torch.empty((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
+                given = self._own_scratch = torch.zeros((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
         return given.data_ptr(), given.numel() * given.element_size()
 
     def _scale(self, scale) -> float:

@@ -9,7 +9,7 @@
 // stands for is free: they are picked so that a lane's scores are of T/4 consecutive keys, exactly what the B operand of
 // O^T = V^T P^T wants of its lane, and P never leaves its registers.  V rows are loaded whole, 16 lanes of 8 channels a row,
 // a lane holding the same 8 channels of the T/4 keys of its quarter; v_perm pairs them up into the A operand of eight products,
-// product i for channels 8 c + i.
+// product i for channels 8 eight_of(c) + i.
 
 #include <algorithm>
 
@@ -55,7 +55,7 @@ __device__ __forceinline__ f32x2a two_f32(uint32_t codes, float unit) {
 }
 __device__ __forceinline__ float unit_of(uint32_t scale) { return __uint_as_float(scale << 23); }   // (2^-127 comes out as 0: it stands for zeros)
 
-// A lane's part of the running softmax: column R = lane % 16, channels 32 (lane / 16) + 8 j + i in o[i][j].
+// A lane's part of the running softmax: column R = lane % 16, channels 8 eight_of(4 (lane / 16) + j) + i in o[i][j].
 struct Running {
     f32x4a o[8];
     float top, sum;                    // of R so far (top: of all quarters; sum: of the lane's keys)
@@ -174,6 +174,9 @@ __device__ __forceinline__ void add_values_masked(V& v, const float* p, uint32_t
     add_values(v, p, o);
 }
 
+// Which eight channels a lane c of 16 has of a row of V: those of 4 bits come in whole lines of two rows (below).
+__device__ __forceinline__ int eight_of(int c) { return (c & 7) * 2 + (c >> 3); }
+
 // One tile of T keys in registers.  `first`: row of its first key in K and V; `count`: keys of it that there are (>= 1), the last
 // one stands in for those beyond.  on = 0: nothing is asked of the tile, and all lanes load from its first bytes (the loads are there all the
 // same: a branch around them would make the compiler wait for all that are in flight).  MASKED: some key of it is hidden from some R.
@@ -210,7 +213,7 @@ struct Tile<kBf16> {
             const uint32_t k_at = ((c & 7) * 256 + (quarter + (c >> 3) * 4) * 16) & on;
 #pragma unroll
             for (int s = 0; s < 4; ++s) k[s] = fetched<PAST, u32x4a>(Kb + k_at + (s & 1) * 2048 + (s >> 1) * 128);
-            const uint32_t v_at = (quarter * 1024 + c * 16) & on;
+            const uint32_t v_at = (quarter * 1024 + eight_of(c) * 16) & on;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = fetched<PAST, u32x4a>(Vb + v_at + e * 256);
             return;
@@ -218,7 +221,7 @@ struct Tile<kBf16> {
 #pragma unroll
         for (int s = 0; s < 4; ++s) k[s] = *(const u32x4a*)(Kb + (uint32_t)(min((s & 1) * 8 + (c & 7), count - 1) * 256 + (quarter + (c >> 3) * 4) * 16 + (s >> 1) * 128));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = *(const u32x4a*)(Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 256 + c * 16));
+        for (int e = 0; e < 4; ++e) v[e] = *(const u32x4a*)(Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 256 + eight_of(c) * 16));
     }
     __device__ __forceinline__ static void queries(Queries& q, const void* row, int quarter) {
 #pragma unroll
@@ -254,7 +257,7 @@ struct Tile<kF32> {
             const uint32_t k_at = ((c & 7) * 512 + (quarter + (c >> 3) * 4) * 16) & on;
 #pragma unroll
             for (int s = 0; s < 8; ++s) k[s] = fetched<PAST, u32x4a>(Kb + k_at + (s & 1) * 4096 + (s >> 1) * 128);
-            const uint32_t v_at = (quarter * 2048 + c * 32) & on;
+            const uint32_t v_at = (quarter * 2048 + eight_of(c) * 32) & on;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 *(f32x4a*)&v[e][0] = fetched<PAST, f32x4a>(Vb + v_at + e * 512);
@@ -266,7 +269,7 @@ struct Tile<kF32> {
         for (int s = 0; s < 8; ++s) k[s] = *(const u32x4a*)(Kb + (uint32_t)(min((s & 1) * 8 + (c & 7), count - 1) * 512 + (quarter + (c >> 3) * 4) * 16 + (s >> 1) * 128));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const char* row = Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 512 + c * 32);
+            const char* row = Vb + (uint32_t)(min(quarter * 4 + e, count - 1) * 512 + eight_of(c) * 32);
             *(f32x4a*)&v[e][0] = *(const f32x4a*)row;
             *(f32x4a*)&v[e][4] = *(const f32x4a*)(row + 16);
         }
@@ -308,15 +311,19 @@ struct Tile<kMxBf16> {
         const uint8_t* Kc = Ks + first * 4;
         const uint8_t* Vc = Vs + first * 4;
         if (count == T) {
-            const uint32_t key = (c >> 2) * 8 + (c & 3), k_at = (key * 64 + quarter * 16) & on, v_at = (quarter * 512 + c * 4) & on, ks_at = (key * 4 + quarter) & on;
+            const uint32_t key = (c >> 2) * 8 + (c & 3), k_at = (key * 64 + quarter * 16) & on, v_at = (quarter * 512 + (c >> 3) * 64 + (c & 7) * 8) & on, ks_at = (key * 4 + quarter) & on;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                k[t] = *(const u32x4a*)(Kb + k_at + t * 256);
+                k[t] = fetched<PAST, u32x4a>(Kb + k_at + t * 256);
                 ks[t] = *(Kc + ks_at + t * 16);
                 __builtin_memcpy(&vs[t], Vc + quarter * 32 + t * 16, 16);       // (rows' scales lie at multiples of 4 bytes)
             }
+            // (lanes c < 8 16 channels of the first of two rows, the others of the second: whole lines; values() makes 8 channels of both rows of it)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = *(const uint32_t*)(Vb + v_at + e * 64);
+            for (int e = 0; e < 8; e += 2) {
+                const u32x2 x = fetched<PAST, u32x2>(Vb + v_at + e * 64);
+                v[e] = x.x, v[e + 1] = x.y;
+            }
             return;
         }
 #pragma unroll
@@ -327,8 +334,8 @@ struct Tile<kMxBf16> {
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int key = min(quarter * 8 + e, count - 1);
-            v[e] = *(const uint32_t*)(Vb + (uint32_t)(key * 64 + c * 4));
+            const int key = min(quarter * 8 + e, count - 1), row = min(quarter * 8 + (e & ~1) + (c >> 3), count - 1);
+            v[e] = *(const uint32_t*)(Vb + (uint32_t)(row * 64 + (c & 7) * 8 + (e & 1) * 4));
             vs[e / 4][e % 4] = *(const uint32_t*)(Vc + (uint32_t)(key * 4));
         }
     }
@@ -350,7 +357,13 @@ struct Tile<kMxBf16> {
     }
     template <bool MASKED>
     __device__ __forceinline__ void values(const float* p, uint32_t seen, f32x4a* o) {
-        const int shift = (threadIdx.x >> 2 & 3) * 8;                          // (of the block that the lane's channels lie in)
+        const int shift = (threadIdx.x >> 1 & 3) * 8;                          // (of the block that the lane's channels lie in, eight_of(c) / 4)
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {                                        // (lane c's second dword against lane c ^ 8's first)
+            const int x = (int)v[e], y = (int)v[e + 1];
+            v[e] = (uint32_t)__builtin_amdgcn_update_dpp(x, y, 0x128, 0xF, 0xC, false);
+            v[e + 1] = (uint32_t)__builtin_amdgcn_update_dpp(y, x, 0x128, 0xF, 0x3, false);
+        }
 u32x4a x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -376,8 +389,8 @@ struct Tile<kMxF32> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int row = min(quarter * 4 + e, count - 1);
-            v[e] = *(const uint32_t*)((const char*)V + first * 64 + (uint32_t)(row * 64 + c * 4));
-            vs[e] = (Vs + first * 4)[(uint32_t)(row * 4 + (c >> 2))];
+            v[e] = *(const uint32_t*)((const char*)V + first * 64 + (uint32_t)(row * 64 + eight_of(c) * 4));
+            vs[e] = (Vs + first * 4)[(uint32_t)(row * 4 + (eight_of(c) >> 2))];
         }
     }
     __device__ __forceinline__ static void queries(Queries& q, const void* row, int quarter) {
@@ -670,44 +683,56 @@ __device__ __forceinline__ void merge_waves(const WaveParts& part, const WaveVal
     }
 }
 
-// Joins workgroups w0 .. w1's parts of an item: a wave takes every fourth, 16 lanes a row.
+// Joins workgroups w0 .. w1's parts of an item: 16 lanes a row; the 16 threads' groups of a workgroup share out the parts where there are fewer rows.
 template <int FB>
 __device__ __forceinline__ void join(const SplitArgs& a, int item, int w0, int w1, WaveParts& part, WaveValues& tops, WaveValues& sums) {
-    const int g = item / a.row_tiles, wave = threadIdx.x >> 6, R0 = (item - g * a.row_tiles) * kRowTile, rows = min(kRowTile, a.rows - R0);
-    for (int row = threadIdx.x >> 4 & 3; row < rows; row += 4) {
-        const int d0 = (threadIdx.x & 15) * 8;
-        float top = -INFINITY, sum = 0.f, o[8] = {};
-        for (int first = w0 + wave; first <= w1; first += 4 * kSplitWaves) {
-            // (four parts' loads together; the last one again for those beyond it, without weight)
-            f32x2a ml[4], x[4][4];
+    const int g = item / a.row_tiles, R0 = (item - g * a.row_tiles) * kRowTile, rows = min(kRowTile, a.rows - R0), group = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
+    const int ways = rows <= 4 ? 4 : rows <= 8 ? 2 : 1, row = group % (kRowTile / ways), way = group / (kRowTile / ways);
+    float top = -INFINITY, sum = 0.f, o[8] = {};
+    if (row < rows)
+        for (int first = w0 + way; first <= w1; first += 8 * ways) {
+            // (eight parts' loads together; the last one again for those beyond it, without weight)
+            f32x2a ml[8], x[8][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t at = ((int64_t)min(first + k * kSplitWaves, w1) + item) * kRowTile + row;
+            for (int k = 0; k < 8; ++k) {
+                const int64_t at = ((int64_t)min(first + k * ways, w1) + item) * kRowTile + row;
                 ml[k] = load_shared((const uint64_t*)(a.part_ml + at));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[k][i] = load_shared((const uint64_t*)(a.part_o + at * 128 + d0) + i);
             }
+            float next = top;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (first + k * kSplitWaves > w1) break;
-                const float next = fmaxf(top, ml[k].x), off = next == -INFINITY ? 0.f : next;
-                const float keep = __builtin_amdgcn_exp2f(top - off), weight = __builtin_amdgcn_exp2f(ml[k].x - off);
-                sum = sum * keep + weight * ml[k].y;
+            for (int k = 0; k < 8; ++k) next = fmaxf(next, ml[k].x);
+            const float off = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - off);
+            sum *= keep;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = o[i] * keep + weight * x[k][i / 2][i % 2];
-                top = next;
+            for (int i = 0; i < 8; ++i) o[i] *= keep;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float weight = first + k * ways <= w1 ? __builtin_amdgcn_exp2f(ml[k].x - off) : 0.f;
+                if (weight == 0.f) continue;                // (an infinity without weight stays out)
+                sum += weight * ml[k].y;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] += weight * x[k][i / 2][i % 2];
             }
+            top = next;
         }
+    if (ways > 1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) part[wave][row][d0 + i] = o[i];
-        if (d0 == 0) tops[wave][row] = top, sums[wave][row] = sum;
+        for (int i = 0; i < 8; ++i) part[way][row][d0 + i] = o[i];
+        if (d0 == 0) tops[way][row] = top, sums[way][row] = sum;
+        __syncthreads();
+        if (way > 0 || row >= rows) return;
+        for (int w = 1; w < ways; ++w) {
+            const float other = tops[w][row], next = fmaxf(top, other), off = next == -INFINITY ? 0.f : next;
+            const float keep = __builtin_amdgcn_exp2f(top - off), weight = __builtin_amdgcn_exp2f(other - off);
+            sum = sum * keep + weight * sums[w][row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = o[i] * keep + weight * part[w][row][d0 + i];
+            top = next;
+        }
     }
-    __syncthreads();
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
-    if (row >= rows) return;
-    float o[8], top, sum;
-    merge_waves(part, tops, sums, row, d0, o, top, sum);
-    write_row<FB>(a.c, g, R0 + row, d0, o, top, sum);
+    if (row < rows && way == 0) write_row<FB>(a.c, g, R0 + row, d0, o, top, sum);
 }
 
 // An item that the workgroup has a part of, and the workgroups that have others.
@@ -796,7 +821,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(Split
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float* to = &part[wave][col][quarter * 32 + j * 8];
+            float* to = &part[wave][col][eight_of(quarter * 4 + j) * 8];
             *(f32x4a*)to = (f32x4a){r.o[0][j], r.o[1][j], r.o[2][j], r.o[3][j]};
             *(f32x4a*)(to + 4) = (f32x4a){r.o[4][j], r.o[5][j], r.o[6][j], r.o[7][j]};
         }
@@ -878,8 +903,11 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     a.part_o = (float*)(a.arrived + kCounters);
     a.part_ml = (f32x2a*)(a.part_o + (shares + 2 * a.items) * kRowTile * 128);
     // (bytes that 256 MB of Infinity Cache would not hold until the next call)
-    const bool past = 2 * row * ((mx ? 0 : call.rows) + heads * keys) > kPastCaches;
-    if (mx) return f32 ? launch<kMxF32, kF32, false>(a, stream) : launch<kMxBf16, kBf16, false>(a, stream);
+    const bool past = 2 * ((mx ? 68 : row) * call.rows + row * heads * keys) > kPastCaches;
+    if (mx) {
+        if (past) return f32 ? launch<kMxF32, kF32, true>(a, stream) : launch<kMxBf16, kBf16, true>(a, stream);
+        return f32 ? launch<kMxF32, kF32, false>(a, stream) : launch<kMxBf16, kBf16, false>(a, stream);
+    }
     if (!call.offsets) {
         if (past) return f32 ? launch<kNone, kF32, true>(a, stream) : launch<kNone, kBf16, true>(a, stream);
         return f32 ? launch<kNone, kF32, false>(a, stream) : launch<kNone, kBf16, false>(a, stream);

@@ -1,6 +1,7 @@
 // C ABI of the operators around a compressed cache: argument checks and launches (rotate_kernel.hip, mx_kernels.hip,
 // attend_split.hip).
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 
@@ -9,6 +10,8 @@
 using namespace curdkv;
 
 namespace {
+
+constexpr int64_t kPromptProducts = 200000;    // rows times keys of a KV head from which the prompts' kernel is the faster one
 
 bool aligned16(std::initializer_list<const void*> ptrs) {
     uintptr_t all = 0;
@@ -30,9 +33,15 @@ int check_attend(const curdkv_ctx* ctx, const void* Q, const void* out, int64_t 
 }
 
 int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
-    // more rows than two row tiles of the split kernel: tiles of 256 rows (limits below)
-    const bool prompt = call.dtype == CURDKV_DTYPE_BF16 && !call.offsets && (int64_t)call.m * call.group > 32;
-    return (prompt ? launch_attend_prompt(ctx, call, (hipStream_t)stream) : launch_attend_split(ctx, call, (hipStream_t)stream)) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
+    // Which kernel: the split one takes tiles of 16 rows (tokens times query heads of a KV head), each of which reads the cache, the prompts' ones 128.
+    // bf16, us, split and prompt: 12 tokens of 32 heads over 1000 rows 15 and 24, 32 over 1000 19 and 26, 100 over 1000 26 and 27; 12 over 16000 39 and 32,
+    // 32 over 16000 47 and 35, 100 over 16000 237 and 58; 16 sequences of 32 over 4000 298 and 76.
+    // fp32: 500 tokens of 32 heads 71 and 87, 2048 439 and 349 (128 rows a workgroup have to fill the units twice).
+    const int64_t rows = (int64_t)call.m * call.group, tiles = call.count * call.kv * ((rows + 127) / 128);
+    const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
+    const bool f32 = call.dtype == CURDKV_DTYPE_F32, prompt = !call.offsets && (f32 ? tiles >= 2 * (int64_t)ctx->num_cu : rows > 32 && rows * keys > kPromptProducts);
+    const auto launch = !prompt ? launch_attend_split : f32 ? launch_attend_prompt_f32 : launch_attend_prompt;
+    return launch(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }
 
 int run_kept(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept, const uint8_t* K_scales, const uint8_t* V_scales,

@@ -14,6 +14,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
 typedef float f32x2a __attribute__((ext_vector_type(2)));
 typedef float f32x4a __attribute__((ext_vector_type(4)));
+typedef float f32x16a __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2a __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8a __attribute__((ext_vector_type(8)));
 
@@ -54,5 +55,21 @@ __device__ __forceinline__ Seen seen_rows(int length, int m, int t0, int t1, int
 __device__ __forceinline__ bool sees(int p, int j, int window, int sinks) {
     return j <= p && (window <= 0 || p - j < window || j < sinks);
 }
+
+// sums and maxima of a lane's half wave with the other
+__device__ __forceinline__ float halves_max(float x) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+// 64 lanes' 16 bytes from base + at to LDS from `to` on, in order of the lanes.  Nothing waits for it but dma_wait().
+__device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
 }  // namespace curdkv

@@ -6,6 +6,8 @@
 namespace curdkv {
 
 // Queries and results of one attention call, [count, m, kv * group, 128], and what is attended to.
+constexpr int64_t kScratchCounters = 16384;     // bytes at the start of a call's scratch that are zeros between the calls
+
 struct AttendCall {
     const void* Q;
     void* out;
@@ -30,6 +32,7 @@ struct AttendCall {
 
 hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);
 hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);     // bf16, no kept rows
+hipError_t launch_attend_prompt_f32(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);
 
 hipError_t launch_rotate(const curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride, const int32_t* starts,
                          const int32_t* positions, const float* table, int64_t table_rows, const void* q_weight, const void* k_weight,

@@ -12,6 +12,7 @@
 // The reference point of a row's exponentials is its maximum only to within 2^8: it moves, and what has been summed is scaled, when the
 // maximum passes it by more, so that most tiles scale nothing.
 
+#include <algorithm>
 #include <type_traits>
 
 #include "attend_device.h"
@@ -20,7 +21,6 @@
 namespace curdkv {
 namespace {
 
-typedef float f32x16a __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x2a __attribute__((ext_vector_type(2)));
 typedef short s16x4a __attribute__((ext_vector_type(4)));
 
@@ -31,6 +31,9 @@ struct PromptArgs {
     AttendCall c;
     float scale_log2;
     int groups, rows, row_tiles;
+    int parts;                         // workgroups that share out the tiles of keys of one row tile
+    float* part_o;                     // parts > 1: [parts][groups * row_tiles * 128][128], un-normalised
+    f32x2a* part_ml;                   // the same of reference points and sums
 };
 
 __device__ __forceinline__ u32x2 read_transposed(const char* p) {
@@ -39,20 +42,6 @@ __device__ __forceinline__ u32x2 read_transposed(const char* p) {
 __device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {      // of either 16 bits
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2a, x), __builtin_bit_cast(u16x2a, y)));
 }
-__device__ __forceinline__ float halves_max(float x) {
-    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
-}
-__device__ __forceinline__ float halves_sum(float x) {
-    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r.x) + __uint_as_float(r.y);
-}
-// 64 lanes' 16 bytes from base + at to LDS from `to` on, in order of the lanes.  Nothing waits for it but dma_wait().
-__device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
-}
-__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
 // RB: blocks of 32 rows a wave
 template <int WAVES, int RB, int OCC>
@@ -62,7 +51,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
     __shared__ int not_finite;         // a tile whose V holds an infinity or NaN
     if (threadIdx.x == 0) not_finite = -1;
     const AttendCall& c = a.c;
-    const int g = blockIdx.x % a.groups, row_tile = a.row_tiles - 1 - blockIdx.x / a.groups;      // long ones first
+    const int g = blockIdx.x % a.groups, part = blockIdx.x / a.groups % a.parts;
+    const int row_tile = a.row_tiles - 1 - blockIdx.x / a.groups / a.parts;                        // long ones first
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int b = g / c.kv, head = g % c.kv;
     const int length = c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n;
@@ -70,6 +60,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
     const int t_first = row_tile * kTileRows / c.group, t_last = min(c.m - 1, (row_tile * kTileRows + kTileRows - 1) / c.group);
     const Seen seen = seen_rows(length, c.m, t_first, t_last, c.window, c.sinks);
     const int first_tiles = (seen.first + kKeys - 1) / kKeys, tiles = first_tiles + (seen.high - seen.low + kKeys - 1) / kKeys;
+    const int start = (int)((int64_t)tiles * part / a.parts), stop = (int)((int64_t)tiles * (part + 1) / a.parts);
     const auto row_of = [&](int tile) { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
     const auto count_of = [&](int tile) { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
 
@@ -185,8 +176,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         }
         if ((most & 0xFFFFu) >= 0x7F80u || most >= 0x7F800000u) not_finite = tile;
         __syncthreads();
-        if (tile + 2 < tiles) fetch_k(tile + 2);
-        if (tile + 1 < tiles) fetch_v(tile + 1);
+        if (tile + 2 < stop) fetch_k(tile + 2);
+        if (tile + 1 < stop) fetch_v(tile + 1);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const Range r = range_of(tile, rb);
@@ -270,7 +261,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         for (int rb = 0; rb < RB; ++rb) top[rb] = top_of(s[rb]);
         __syncthreads();
         for (int tile = begin; tile < end; ++tile) {
-            fetch_k(min(tile + 2, tiles - 1));
+            fetch_k(min(tile + 2, stop - 1));
             fetch_v(tile + 1);
             raise();
             const char *Kt = Ks[(tile + 1) & 1], *Vt = Vs[tile & 1];
@@ -345,20 +336,20 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         }
     };
 
-    if (tiles > 0) {
-        fetch_k(0);
-        fetch_v(0);
-        if (tiles > 1) fetch_k(1);
+    if (start < stop) {
+        fetch_k(start);
+        fetch_v(start);
+        if (start + 1 < stop) fetch_k(start + 1);
         dma_wait();
         __syncthreads();
-        const int whole_end = min(first_tiles + max(0, (min(seen.high, seen.p0 + 1) - seen.low) / kKeys), tiles - 1);
+        const int whole_end = min(first_tiles + max(0, (min(seen.high, seen.p0 + 1) - seen.low) / kKeys), stop - 1);
         const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;         // rows from `low` on that the last token does not see
-        const int whole_begin = min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end);
-        int tile = 0;
-        for (int part = 0; part < 2; ++part) {
-            const int end = part == 0 ? max(whole_begin, 0) : tiles;
+        const int whole_begin = max(min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end), start);
+        int tile = start;
+        for (int round = 0; round < 2; ++round) {
+            const int end = round == 0 ? whole_begin : stop;
             for (; tile < end; ++tile) masked_step(tile);
-            if (part == 0 && tile < whole_end) {
+            if (round == 0 && tile < whole_end) {
                 whole_steps(tile, whole_end);
                 tile = whole_end;
             }
@@ -370,6 +361,19 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         const float total = halves_sum(sum[rb]);
         const int R = R0 + rb * 32 + col;
         if (R >= a.rows) continue;
+        if (a.parts > 1) {
+            const int64_t at = ((int64_t)part * a.groups + g) * a.row_tiles * kTileRows + R;
+            float* to = a.part_o + at * 128 + half * 4;
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x16a& x = o[rb][db];
+                    *(f32x4a*)(to + db * 32 + i * 8) = (f32x4a){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+                }
+            if (half == 0) a.part_ml[at] = (f32x2a){ref[rb], total};
+            continue;
+        }
         const bool empty = ref[rb] == -INFINITY;
         const float over = empty ? 0.f : 1.f / total;
         char* out = (char*)c.out + query_row(rb) * 256;
@@ -386,17 +390,50 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
     }
 }
 
+// Joins the parts of four rows, a wave a row, two channels a lane.
+__global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a, int tile_rows) {
+    const AttendCall& c = a.c;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, g = (int)(at / a.rows), R = (int)(at - (int64_t)g * a.rows);
+    if (g >= a.groups) return;
+    const int64_t first = (int64_t)g * a.row_tiles * tile_rows + R, step = (int64_t)a.groups * a.row_tiles * tile_rows;
+    float ref = -INFINITY, sum = 0.f;
+    for (int k = 0; k < a.parts; ++k) ref = fmaxf(ref, a.part_ml[first + k * step].x);
+    const bool empty = ref == -INFINITY;
+    f32x2a o = {0, 0};
+#pragma unroll 4
+    for (int k = 0; k < a.parts; ++k) {
+        const f32x2a ml = a.part_ml[first + k * step], x = *(const f32x2a*)(a.part_o + (first + k * step) * 128 + lane * 2);
+        const float weight = empty ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
+        sum += weight * ml.y;
+        o.x += weight * x.x;
+        o.y += weight * x.y;
+    }
+    const float over = empty ? 0.f : 1.f / sum;
+    const int b = g / c.kv, t = R / c.group, h = (g - b * c.kv) * c.group + R % c.group;
+    ((uint32_t*)c.out)[(((int64_t)b * c.m + t) * c.kv * c.group + h) * 64 + lane] = pack_bf16(o.x * over, o.y * over);
+    if (c.lse && lane == 0) c.lse[((int64_t)b * c.kv * c.group + h) * c.m + t] = empty ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
 }  // namespace
 
-hipError_t launch_attend_prompt(const curdkv_ctx*, const AttendCall& call, hipStream_t stream) {
-    constexpr int kWaves = 4, kBlocks = 1, kOcc = 2;
+hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream) {
+    constexpr int kWaves = 4, kTileRows = kWaves * 32;
     PromptArgs a;
     a.c = call;
     a.scale_log2 = call.scale * (1.f / kLn2);
     a.groups = (int)(call.count * call.kv);
     a.rows = call.m * call.group;
-    a.row_tiles = (a.rows + kWaves * kBlocks * 32 - 1) / (kWaves * kBlocks * 32);
-    attend_prompt_kernel<kWaves, kBlocks, kOcc><<<(unsigned)((int64_t)a.groups * a.row_tiles), kWaves * 64, 0, stream>>>(a);
+    a.row_tiles = (a.rows + kTileRows - 1) / kTileRows;
+    // Few new tokens over a long cache: the tiles of keys shared out until every unit has two workgroups, 8 tiles each at least, as far as there is scratch.
+    const int64_t blocks = (int64_t)a.groups * a.row_tiles, tiles = (call.window > 0 ? std::min(call.n, call.window + call.sinks + call.m) : call.n) / kKeys;
+    const int64_t part_bytes = blocks * kTileRows * (int64_t)(128 * sizeof(float) + sizeof(f32x2a)), room = call.scratch ? call.scratch_bytes - kScratchCounters : 0;
+    int64_t parts = std::min(std::min(2 * ctx->num_cu / blocks, tiles / 8), room / part_bytes);
+    a.parts = parts > 1 ? (int)parts : 1;
+    a.part_o = (float*)((char*)call.scratch + kScratchCounters);
+    a.part_ml = (f32x2a*)(a.part_o + a.parts * blocks * kTileRows * 128);
+    attend_prompt_kernel<kWaves, 1, 2><<<(unsigned)(blocks * a.parts), kWaves * 64, 0, stream>>>(a);
+    if (a.parts > 1) attend_prompt_join_kernel<<<(unsigned)(((int64_t)a.groups * a.rows + 3) / 4), 256, 0, stream>>>(a, kTileRows);
     return hipGetLastError();
 }
 

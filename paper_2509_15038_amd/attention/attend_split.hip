@@ -23,7 +23,7 @@ typedef short s16x4a __attribute__((ext_vector_type(4)));
 
 constexpr int kSplitWaves = 4;
 constexpr int kRowTile = 16;           // rows R a workgroup handles
-constexpr int kCounters = 4096;        // items at most that share workgroups
+constexpr int kCounters = kScratchCounters / sizeof(int);      // items at most that share workgroups
 constexpr int64_t kPastCaches = 128 << 20;
 constexpr int64_t kPartBytes = 128 * sizeof(float) + 2 * sizeof(float);     // of a row of partial results
 
@@ -555,7 +555,7 @@ __device__ __forceinline__ Head head_from(const Head& h, int lane) {
 }
 template <int FA, int FB>
 struct Places {
-    static constexpr int kBetween = 8, kAtOnce = 4;
+    static constexpr int kBetween = FA == kMxBf16 || FA == kMxF32 ? 32 : 16, kAtOnce = 4;
     const SplitArgs& a;
     int all, shares, at;               // units of all items; workgroups with a share; units in front of the item at hand, without its kBetween
     __device__ __forceinline__ int begin_of(int share) const { return (int)((int64_t)all * share / shares); }
@@ -893,7 +893,7 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     int64_t keys = call.n;
     if (call.window > 0) keys = std::min(keys, (int64_t)call.window + call.sinks + call.m);
     const int64_t heads = call.count * call.kv, tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles;
-    int64_t shares = std::min((int64_t)ctx->num_cu, std::max((int64_t)a.items, (tiles + kSplitWaves - 1) / kSplitWaves));
+    int64_t shares = std::min((int64_t)ctx->num_cu * (mx && tiles >= 1024 * (int64_t)ctx->num_cu ? 2 : 1), std::max((int64_t)a.items, (tiles + kSplitWaves - 1) / kSplitWaves));
     const int64_t slot = kRowTile * kPartBytes, room = call.scratch ? (call.scratch_bytes - kCounters * (int64_t)sizeof(int)) / slot : 0;
     shares = std::min(shares, room - 2 * a.items);
     if (shares <= a.items / 4 || a.items > kCounters) shares = 0;

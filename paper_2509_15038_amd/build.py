@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libcurdkv.so")
 CALL = os.path.join(HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["curdkv_api.hip", "scores_kernels.hip", "select_kernels.hip", "split_select.hip", "compact_kernels.hip", "fused_kernel.hip", "adaptive_kernels.hip",
            "sketch_host.cpp"]
-ATTENTION = ["rotate_kernel.hip", "mx_kernels.hip", "attend_split.hip", "attend_prompt.hip", "attend_api.hip"]
+ATTENTION = ["rotate_kernel.hip", "mx_kernels.hip", "attend_split.hip", "attend_prompt.hip", "attend_prompt_f32.hip", "attend_api.hip"]
 
 
 def _build_call_module(hipcc: str, verbose: bool) -> None:

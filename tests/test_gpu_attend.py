@@ -40,6 +40,39 @@ def test_windows(dtype, m, window, sinks):
     U.check_attend(dict(count=3, m=m, n=400, window=window, sinks=sinks, dtype=dtype), seed=window + m)
 
 
+@pytest.mark.parametrize("m,n,window,sinks", [(130, 130, 0, 0), (300, 300, 77, 5), (129, 400, 50, 64), (200, 333, 0, 0)])
+def test_many_heads_in_fp32(m, n, window, sinks):
+    # enough rows for the kernel of prompts
+    U.check_attend(dict(count=3, kv=100, group=1, m=m, n=n, window=window, sinks=sinks, dtype="fp32"), seed=m, lengths=[n, n - 1, m // 2])
+
+
+@pytest.mark.parametrize("spoiled", [False, True])
+def test_many_heads_in_fp32_and_values_that_are_not_finite(spoiled):
+    def spoil(K, V, lens):
+        if spoiled:
+            V[:, ::2, -1, 3], V[:, ::3, -1, 100], V[:, 1, 140] = math.nan, math.inf, -math.inf
+
+    m, n = 150, 260
+    K, V, Q = (U.randn(i, (2, 100, n, D) if i < 3 else (2, m, 200, D), torch.float32) for i in (1, 2, 3))
+    spoil(K, V, None)
+    out, lse = U.run_attend(dict(count=2, kv=100, group=2, m=m, n=n, window=0, sinks=0, dtype="fp32"), Q, K, V, None, n)
+    for b in range(2):
+        seen = U.causal(m, n, n, 0, 0)
+        for h in range(0, 200, 3):
+            k, v = K[b, h // 2], V[b, h // 2]
+            fine = ~(seen & ~torch.isfinite(v).all(1)).any(1)
+            U.check_attention(out[b, fine, h], lse[b, h, fine], U.attention(Q[b, fine, h], k, v, seen[fine], D ** -0.5), "fp32", n, f"head {h}")
+            bad = ~torch.isfinite(v)
+            got = out[b, -1, h]
+            assert bool((torch.isfinite(got) == ~bad.any(0)).all())
+
+
+@pytest.mark.parametrize("count,m,n,window,sinks", [(1, 12, 16000, 0, 0), (1, 40, 9001, 0, 0), (2, 33, 5000, 3000, 4), (1, 100, 4000, 0, 0), (3, 20, 2500, 0, 0), (1, 300, 3000, 2000, 100)])
+def test_a_few_tokens_over_long_caches(count, m, n, window, sinks):
+    # the tiles of keys of one row tile shared out over several workgroups
+    U.check_attend(dict(count=count, kv=2, group=4, m=m, n=n, window=window, sinks=sinks), seed=m, lengths=[n, m + 3, 5][:count])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("m", [1, 5, 64, 200])
 def test_sequences_shorter_than_their_new_tokens(dtype, m):
@@ -151,6 +184,25 @@ def test_lse_is_optional_and_lengths_are_clamped():
     assert torch.equal(a, b) and bool((a[1] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("m", [1, 3, 50])
+def test_less_scratch_and_none(dtype, m):
+    # fewer workgroups share a head; the counters at its start are left cleared
+    n, dt = 5000, U.dtype_of(dtype)
+    K, V, Q = U.randn(1, (2, 2, n, D), dt), U.randn(2, (2, 2, n, D), dt), U.randn(3, (2, m, 8, D), dt)
+    with U.context(2, 4, dtype, n) as ctx:
+        for size in (0, 16, 16384, 16384 + 520 * 40, 16384 + 520 * 700, 16384 + 520 * 5000):
+            out = torch.full_like(Q, float("nan"))
+            scratch = torch.zeros((max(size, 16),), dtype=torch.uint8, device="cuda")[:size]
+            guard = torch.full((4096,), 77, dtype=torch.uint8, device="cuda")
+            ctx.attend(Q, K, V, 2, m, n, n, out, scratch=scratch)
+            torch.cuda.synchronize()
+            assert bool((scratch[:16384] == 0).all()) and bool((guard == 77).all())
+            for h in (0, 7):
+                want = U.attention(Q[1, :, h], K[1, h // 4], V[1, h // 4], U.causal(m, n, n, 0, 0), D ** -0.5)
+                U.check_attention(out[1, :, h], None, want, dtype, n, f"scratch {size}")
+
+
 def test_refusals():
     K, V, Q = U.randn(1, (1, 1, 50, D), torch.bfloat16), U.randn(2, (1, 1, 50, D), torch.bfloat16), U.randn(3, (1, 2, 4, D), torch.bfloat16)
     out = torch.full_like(Q, 7.0)
@@ -158,7 +210,7 @@ def test_refusals():
     with U.context(1, 4, "bf16", 64) as ctx:
         for bad in (dict(Q=None), dict(K=None), dict(V=None), dict(out=None), dict(count=0), dict(m=0), dict(n=0), dict(n=51), dict(n=65, stride=65),
                     dict(stride=49), dict(window=-1), dict(n_sink=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf),
-                    dict(Q=Q.data_ptr() + 2), dict(K=K.data_ptr() + 8), dict(out=out.data_ptr() + 4), dict(m=65)):
+                    dict(scratch=torch.zeros(64, dtype=torch.uint8, device="cuda")[8:]), dict(Q=Q.data_ptr() + 2), dict(K=K.data_ptr() + 8), dict(out=out.data_ptr() + 4), dict(m=65)):
             with pytest.raises(B.CurdkvError) as e:
                 ctx.attend(**dict(good, **bad))
             assert e.value.code == B.ERR_INVALID_ARG, bad

@@ -6,6 +6,7 @@
 namespace curdkv {
 
 // Queries and results of one attention call, [count, m, kv * group, 128], and what is attended to.
+constexpr int64_t kPastCaches = 128 << 20;     // bytes that a call moves from which its rows pass the caches (Infinity Cache: 256 MB)
 constexpr int64_t kScratchCounters = 16384;     // bytes at the start of a call's scratch that are zeros between the calls
 
 struct AttendCall {

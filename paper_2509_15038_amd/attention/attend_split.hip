@@ -24,7 +24,6 @@ typedef short s16x4a __attribute__((ext_vector_type(4)));
 constexpr int kSplitWaves = 4;
 constexpr int kRowTile = 16;           // rows R a workgroup handles
 constexpr int kCounters = kScratchCounters / sizeof(int);      // items at most that share workgroups
-constexpr int64_t kPastCaches = 128 << 20;
 constexpr int64_t kPartBytes = 128 * sizeof(float) + 2 * sizeof(float);     // of a row of partial results
 
 struct SplitArgs {

@@ -41,20 +41,24 @@ __device__ __forceinline__ float eights_sum(float x) {
 template <bool BF16>
 struct Sixteen {                       // 16 channels of a row: a lane's two pieces of eight
     u32x4a raw[BF16 ? 2 : 4];
+    template <bool PAST>
     __device__ __forceinline__ void load(const char* row, int first, int second) {
         constexpr int W = BF16 ? 1 : 2;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            raw[i] = ((const u32x4a*)row)[first * W + i];
-            raw[W + i] = ((const u32x4a*)row)[second * W + i];
+            const u32x4a *x = (const u32x4a*)row + first * W + i, *y = (const u32x4a*)row + second * W + i;
+            raw[i] = PAST ? __builtin_nontemporal_load(x) : *x;
+            raw[W + i] = PAST ? __builtin_nontemporal_load(y) : *y;
         }
     }
+    template <bool PAST>
     __device__ __forceinline__ void store(char* row, int first, int second) const {
         constexpr int W = BF16 ? 1 : 2;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            ((u32x4a*)row)[first * W + i] = raw[i];
-            ((u32x4a*)row)[second * W + i] = raw[W + i];
+            u32x4a *x = (u32x4a*)row + first * W + i, *y = (u32x4a*)row + second * W + i;
+            if (PAST) __builtin_nontemporal_store(raw[i], x), __builtin_nontemporal_store(raw[W + i], y);
+            else *x = raw[i], *y = raw[W + i];
         }
     }
     __device__ __forceinline__ void get(float* x) const {
@@ -77,8 +81,8 @@ struct Sixteen {                       // 16 channels of a row: a lane's two pie
     }
 };
 
-// TOKENS a workgroup; PAIRS: neighbours rotate together.  A lane u of eight holds pairs 8 u .. 8 u + 7.
-template <bool BF16, bool PAIRS, int TOKENS>
+// TOKENS a workgroup; PAIRS: neighbours rotate together; PAST: rows pass the caches.  A lane u of eight holds pairs 8 u .. 8 u + 7.
+template <bool BF16, bool PAIRS, int TOKENS, bool PAST>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     constexpr int kSlots = 32 / TOKENS, kRow = BF16 ? 256 : 512;
     const int u = threadIdx.x & 7, slot = threadIdx.x >> 3;
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     const char* rows = a.qkv + token * a.row_stride;
     for (int h = slot % kSlots; h < heads; h += kSlots) {
         Sixteen<BF16> x;
-        x.load(rows + (int64_t)h * kRow, first, second);
+        x.template load<PAST>(rows + (int64_t)h * kRow, first, second);
         if (h < queries + a.kv) {
             float y[16], z[16];
             x.get(y);
@@ -112,7 +116,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
                 for (int k = 0; k < 16; ++k) sum += y[k] * y[k];
                 const float over = 1.f / sqrtf(eights_sum(sum) * (1.f / 128.f) + a.eps);
                 Sixteen<BF16> w;
-                w.load((const char*)weight, first, second);
+                w.template load<false>((const char*)weight, first, second);
                 w.get(z);
 #pragma unroll
                 for (int k = 0; k < 16; ++k) y[k] = y[k] * over * z[k];
@@ -126,19 +130,22 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
             x.set(z);
         }
         if (h < queries) {
-            x.store(a.Q + (token * queries + h) * kRow, first, second);
+            x.template store<PAST>(a.Q + (token * queries + h) * kRow, first, second);
         } else if (in_cache) {
             const int head = h - queries < a.kv ? h - queries : h - queries - a.kv;
-            x.store((h - queries < a.kv ? a.K : a.V) + ((b * a.kv + head) * a.stride + at) * kRow, first, second);
+            x.template store<PAST>((h - queries < a.kv ? a.K : a.V) + ((b * a.kv + head) * a.stride + at) * kRow, first, second);
         }
     }
 }
 
 template <bool BF16, bool PAIRS>
 hipError_t launch(const curdkv_ctx* ctx, const RotateArgs& a, hipStream_t stream) {
-    // four tokens a workgroup where that still gives every unit four; one, its heads over all lanes, below
-    if (a.tokens >= 16 * (int64_t)ctx->num_cu) rotate_kernel<BF16, PAIRS, 4><<<(unsigned)((a.tokens + 3) / 4), 256, 0, stream>>>(a);
-    else rotate_kernel<BF16, PAIRS, 1><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
+    // Four tokens a workgroup where that still gives every unit four; one, its heads over all lanes, below.  Rows that the caches would not hold until
+    // they are read again pass them by (32768 tokens of 48 heads: 159 us, 144 so).
+    const int64_t bytes = a.tokens * a.kv * (a.group + 2) * (BF16 ? 512 : 1024);
+    if (a.tokens < 16 * (int64_t)ctx->num_cu) rotate_kernel<BF16, PAIRS, 1, false><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
+    else if (bytes <= kPastCaches) rotate_kernel<BF16, PAIRS, 4, false><<<(unsigned)((a.tokens + 3) / 4), 256, 0, stream>>>(a);
+    else rotate_kernel<BF16, PAIRS, 4, true><<<(unsigned)((a.tokens + 3) / 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

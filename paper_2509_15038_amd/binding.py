@@ -1,6 +1,6 @@
 """Binding of libcurdkv.so: the same entry points as include/curdkv.h,
-argument marshalling only, by ctypes and, for the calls that a program makes over and over, the module _call where it has been
-built for this interpreter.  Every step of the path runs in the HIP kernels.
+argument marshalling only, by ctypes and, for the calls that a program makes over and over, the modules _call and _attend where they
+have been built for this interpreter.  Every step of the path runs in the HIP kernels.
 
 torch appears here only as the owner of device memory and streams: tensors are
 passed as raw pointers.  If the compiled library is missing the import of any
@@ -20,6 +20,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcurdkv.so")
 CALL_PATH = os.path.join(_HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+ATTEND_PATH = os.path.join(_HERE, "_attend" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_HIP, ERR_OOM, ERR_TOO_LARGE = 0, -1, -2, -3, -4, -5
 DTYPE_F32, DTYPE_BF16 = 0, 1
@@ -87,6 +88,7 @@ def lib() -> C.CDLL:
     for name in EXPORTS[:-1]:
         getattr(L, name).restype = C.c_int
     _bind_calls(L)
+    _bind_attend(L)
     _lib = L
     return L
 
@@ -208,6 +210,39 @@ def _bind_calls(L) -> None:
     _call = module
 
 
+class _AttendByCtypes:
+    """The functions of the module _attend by ctypes: the C entries' arguments in their order, tensors and None for pointers, and a stream."""
+
+    def __init__(self, L):
+        for name in _ATTEND:
+            entry = getattr(L, "curdkv_" + name)
+            setattr(self, name, self._function(entry, [t is C.c_void_p for t in entry.argtypes]))
+
+    @staticmethod
+    def _function(entry, pointers):
+        def call(*a):
+            if len(a) != len(pointers):
+                raise TypeError(f"expected {len(pointers)} arguments, got {len(a)}")
+            return entry(*[_ptr(x) if p else x if isinstance(x, float) else int(x) for x, p in zip(a[:-1], pointers)], _stream(a[-1]))
+        return call
+
+
+_ATTEND = ("rotate", "attend", "compact_mx", "expand_mx", "attend_kept", "attend_kept_mx")
+_attend = None                                      # the module _attend bound to the library, or _AttendByCtypes; set by lib()
+
+
+def _bind_attend(L) -> None:
+    global _attend
+    if not os.path.exists(ATTEND_PATH):             # (not built for this interpreter)
+        _attend = _AttendByCtypes(L)
+        return
+    spec = importlib.util.spec_from_file_location("paper_2509_15038_amd._attend", ATTEND_PATH)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.bind(*[C.cast(getattr(L, "curdkv_" + name), C.c_void_p).value for name in _ATTEND], _ptr, _stream)
+    _attend = module
+
+
 class Context:
     """Owns one curdkv_ctx.  Methods mirror the C entry points and return the raw
     status code through CurdkvError on failure."""
@@ -224,7 +259,9 @@ class Context:
             raise CurdkvError(rc, "curdkv_create")
         self._address = self._h.value               # (0 once closed)
         self._heads = self.heads
-        self._own_scratch = None
+        self._own_scratch = None                    # (address, bytes) once an attention call has needed it
+        self._scale = self.cfg.head_dim ** -0.5
+        self._row = self.cfg.kv_heads * (self.cfg.group_size + 2) * self.cfg.head_dim
 
     def close(self):
         h = getattr(self, "_h", None)
@@ -318,65 +355,54 @@ class Context:
     def _scratch(self, given):
         """(address, bytes) of the partial results' memory: the caller's tensor, or one that the context keeps from its first attention call on."""
         if given is None:
-            given = self._own_scratch
-            if given is None:
+            if self._own_scratch is None:
                 import torch
-                given = self._own_scratch = torch.zeros((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
+                self._scratch_tensor = torch.zeros((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
+                self._own_scratch = self._scratch_tensor.data_ptr(), ATTEND_SCRATCH_BYTES
+            return self._own_scratch
         return given.data_ptr(), given.numel() * given.element_size()
-
-    def _scale(self, scale) -> float:
-        return self.cfg.head_dim ** -0.5 if scale is None else float(scale)
 
     def rotate(self, qkv, count: int, m: int, table, Q, K, V, stride: int, starts=None, positions=None, q_weight=None, k_weight=None,
                eps: float = 1e-5, pairs: bool = False, row_stride: Optional[int] = None, stream=None):
         """table: a float tensor [rows, 2, head_dim/2] of cosines and sines; row_stride None: the projections' rows lie one after the other."""
-        heads = self.cfg.kv_heads * (self.cfg.group_size + 2)
-        rc = lib().curdkv_rotate(self._h, _ptr(qkv), int(count), int(m), heads * self.cfg.head_dim if row_stride is None else int(row_stride),
-                                 _ptr(starts), _ptr(positions), _ptr(table), int(table.shape[0]), _ptr(q_weight), _ptr(k_weight), float(eps),
-                                 1 if pairs else 0, _ptr(Q), _ptr(K), _ptr(V), int(stride), _stream(stream))
+        rc = _attend.rotate(self._address, qkv, count, m, self._row if row_stride is None else row_stride, starts, positions, table, table.shape[0],
+                            q_weight, k_weight, float(eps), 1 if pairs else 0, Q, K, V, stride, stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_rotate")
 
     def attend(self, Q, K, V, count: int, m: int, n: int, stride: int, out, lengths=None, window: int = 0, n_sink: int = 0, scale=None,
                lse=None, scratch=None, stream=None):
         """scale None: 1 / sqrt(head_dim); scratch None: the context's own."""
-        scratch, room = self._scratch(scratch)
-        rc = lib().curdkv_attend(self._h, _ptr(Q), _ptr(K), _ptr(V), int(count), int(m), int(n), int(stride), _ptr(lengths), int(window),
-                                 int(n_sink), self._scale(scale), _ptr(out), _ptr(lse), scratch, room, _stream(stream))
+        rc = _attend.attend(self._address, Q, K, V, count, m, n, stride, lengths, window, n_sink, self._scale if scale is None else float(scale), out, lse,
+                            *self._scratch(scratch), stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_attend")
 
     def compact_mx(self, K, V, n: int, indices, offsets, total: int, K_codes, K_scales, V_codes, V_scales, stream=None):
         """offsets: a DEVICE tensor, int64 [layers*kv_heads + 1]; total: its last value."""
-        rc = lib().curdkv_compact_mx(self._h, _ptr(K), _ptr(V), int(n), _ptr(indices), _ptr(offsets), int(total), _ptr(K_codes), _ptr(K_scales),
-                                     _ptr(V_codes), _ptr(V_scales), _stream(stream))
+        rc = _attend.compact_mx(self._address, K, V, n, indices, offsets, total, K_codes, K_scales, V_codes, V_scales, stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_compact_mx")
 
     def expand_mx(self, codes, scales, rows: int, out, stream=None):
-        rc = lib().curdkv_expand_mx(self._h, _ptr(codes), _ptr(scales), int(rows), _ptr(out), _stream(stream))
+        rc = _attend.expand_mx(self._address, codes, scales, rows, out, stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_expand_mx")
 
     def attend_kept(self, Q, K_kept, V_kept, offsets, count: int, m: int, total: int, out, K_tail=None, V_tail=None, tail_n: int = 0,
-                    tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None,
-                    scratch=None, stream=None):
+                    tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None, scratch=None, stream=None):
         """offsets: a DEVICE tensor, int64 [count*kv_heads + 1]; rows None: total; scale, scratch: as for attend."""
-        scratch, room = self._scratch(scratch)
-        rc = lib().curdkv_attend_kept(self._h, _ptr(Q), _ptr(K_kept), _ptr(V_kept), _ptr(offsets), int(total),
-                                      int(total if rows is None else rows), _ptr(K_tail), _ptr(V_tail),
-                                      int(tail_n), int(tail_stride), _ptr(tail_lengths), int(count), int(m), self._scale(scale), _ptr(out),
-                                      _ptr(lse), scratch, room, _stream(stream))
+        rc = _attend.attend_kept(self._address, Q, K_kept, V_kept, offsets, total, total if rows is None else rows, K_tail, V_tail, tail_n, tail_stride,
+                                 tail_lengths, count, m, self._scale if scale is None else float(scale), out, lse, *self._scratch(scratch), stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_attend_kept")
 
     def attend_kept_mx(self, Q, K_codes, K_scales, V_codes, V_scales, offsets, count: int, m: int, total: int, out, K_tail=None, V_tail=None,
-                       tail_n: int = 0, tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None,
-                    scratch=None, stream=None):
+                       tail_n: int = 0, tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None, scratch=None,
+                       stream=None):
         """offsets: a DEVICE tensor, int64 [count*kv_heads + 1]; rows None: total; scale, scratch: as for attend."""
-        scratch, room = self._scratch(scratch)
-        rc = lib().curdkv_attend_kept_mx(self._h, _ptr(Q), _ptr(K_codes), _ptr(K_scales), _ptr(V_codes), _ptr(V_scales), _ptr(offsets), int(total),
-                                         int(total if rows is None else rows), _ptr(K_tail), _ptr(V_tail), int(tail_n), int(tail_stride), _ptr(tail_lengths), int(count), int(m),
-                                         self._scale(scale), _ptr(out), _ptr(lse), scratch, room, _stream(stream))
+        rc = _attend.attend_kept_mx(self._address, Q, K_codes, K_scales, V_codes, V_scales, offsets, total, total if rows is None else rows, K_tail,
+                                    V_tail, tail_n, tail_stride, tail_lengths, count, m, self._scale if scale is None else float(scale), out, lse,
+                                    *self._scratch(scratch), stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_attend_kept_mx")

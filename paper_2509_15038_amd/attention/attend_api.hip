@@ -88,7 +88,7 @@ int curdkv_attend(curdkv_ctx* ctx, const void* Q, const void* K, const void* V, 
     c.Q = Q, c.out = out, c.lse = lse, c.count = count;
     c.kv = ctx->cfg.kv_heads, c.group = ctx->cfg.group_size, c.m = (int)m, c.dtype = ctx->cfg.dtype, c.scale = scale;
     c.K = K, c.V = V, c.stride = stride, c.lengths = lengths, c.n = (int)n;
-    c.window = window < n ? (int)window : 0, c.sinks = n_sink;     // (a window of n tokens hides nothing)
+    c.window = window < n ? (int)window : 0, c.sinks = (int)std::min<int64_t>(n_sink, n);     // (a window of n tokens hides nothing)
     c.scratch = scratch, c.scratch_bytes = scratch_bytes;
     return run_attend(ctx, c, stream);
 }

@@ -13,7 +13,6 @@
 // maximum passes it by more, so that most tiles scale nothing.
 
 #include <algorithm>
-#include <type_traits>
 
 #include "attend_device.h"
 #include "attend_internal.h"
@@ -26,6 +25,7 @@ typedef short s16x4a __attribute__((ext_vector_type(4)));
 
 constexpr int kKeys = 64;              // of a tile
 constexpr float kLoose = 8.f;
+constexpr int kWaves = 4, kTileRows = kWaves * 32;        // rows R of a workgroup
 
 struct PromptArgs {
     AttendCall c;
@@ -43,10 +43,8 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {      //
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2a, x), __builtin_bit_cast(u16x2a, y)));
 }
 
-// RB: blocks of 32 rows a wave
-template <int WAVES, int RB, int OCC>
-__global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptArgs a) {
-    constexpr int kStage = 16 / WAVES, kTileRows = WAVES * RB * 32;
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArgs a) {
+    constexpr int kStage = 16 / kWaves;
     __shared__ __attribute__((aligned(16))) char Ks[2][kKeys * 256], Vs[2][kKeys * 256];
     __shared__ int not_finite;         // a tile whose V holds an infinity or NaN
     if (threadIdx.x == 0) not_finite = -1;
@@ -65,20 +63,12 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
     const auto count_of = [&](int tile) { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
 
     // this lane's rows
-    const int R0 = row_tile * kTileRows + wave * (RB * 32);
-    int p[RB];
-    u32x4a q[RB][8];
-    const auto query_row = [&](int rb) {
-        const int R = min(R0 + rb * 32 + col, a.rows - 1), t = R / c.group;
-        return (((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group;
-    };
+    const int R0 = row_tile * kTileRows + wave * 32;
+    const int R = min(R0 + col, a.rows - 1), t = R / c.group, p = length - c.m + t;
+    const int64_t query_row = (((int64_t)b * c.m + t) * c.kv + head) * c.group + R % c.group;
+    u32x4a q[8];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        p[rb] = length - c.m + min(R0 + rb * 32 + col, a.rows - 1) / c.group;
-        const u32x4a* from = (const u32x4a*)((const char*)c.Q + query_row(rb) * 256);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) q[rb][s] = from[2 * s + half];
-    }
+    for (int s = 0; s < 8; ++s) q[s] = ((const u32x4a*)((const char*)c.Q + query_row * 256))[2 * s + half];
 
     const char* Kg = (const char*)c.K + (int64_t)g * c.stride * 256;
     const char* Vg = (const char*)c.V + (int64_t)g * c.stride * 256;
@@ -103,32 +93,25 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
     const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
     const int v_at = (4 * half + l16 / 4) * 64 + dhalf * 32 + (l16 & 3) * 8;
 
-    f32x16a o[RB][4];
-    float ref[RB], sum[RB], top[RB];
+    f32x16a o[4];
+    float ref = -INFINITY, sum = 0.f, top;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        ref[rb] = -INFINITY, sum[rb] = 0.f;
+    for (int db = 0; db < 4; ++db)
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[rb][db][i] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
     const auto product = [](u32x4a x, u32x4a y, f32x16a z) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, y), z, 0, 0, 0);
     };
-    const auto scores = [&](int tile, f32x16a (&x)[RB][2]) {
+    const auto scores = [&](int tile, f32x16a (&x)[2]) {
         const char* Kt = Ks[tile & 1];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[rb][kb][i] = 0.f;
+            for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const u32x4a k = *(const u32x4a*)(Kt + k_at[i & 1] + (i >> 1) * 4096 + kb * 2048);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) x[rb][kb] = product(k, q[rb][i], x[rb][kb]);
+                x[kb] = product(k, q[i], x[kb]);
             }
         }
     };
@@ -137,9 +120,9 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         int far, near, sink;
         __device__ __forceinline__ bool has(int key) const { return key <= far && (key > near || key < sink); }
     };
-    const auto range_of = [&](int tile, int rb) {
+    const auto range_of = [&](int tile) {
         const int j0 = row_of(tile);
-        return Range{min(p[rb] - j0, count_of(tile) - 1) - half * 4, (c.window > 0 ? p[rb] - j0 - c.window : -1) - half * 4, c.sinks - j0 - half * 4};
+        return Range{min(p - j0, count_of(tile) - 1) - half * 4, (c.window > 0 ? p - j0 - c.window : -1) - half * 4, c.sinks - j0 - half * 4};
     };
     const auto top_of = [&](const f32x16a (&x)[2]) {
         float y = x[0][0];
@@ -150,27 +133,25 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         return halves_max(y) * a.scale_log2;
     };
     const auto raise = [&]() {
+        if (__any(top > ref + kLoose)) {
+            const float next = top > ref + kLoose ? top : ref;
+            const float keep = next == ref ? 1.f : __builtin_amdgcn_exp2f(ref - next);
+            sum *= keep;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-            if (__any(top[rb] > ref[rb] + kLoose)) {
-                const float next = top[rb] > ref[rb] + kLoose ? top[rb] : ref[rb];
-                const float keep = next == ref[rb] ? 1.f : __builtin_amdgcn_exp2f(ref[rb] - next);
-                sum[rb] *= keep;
-#pragma unroll
-                for (int db = 0; db < 4; ++db) o[rb][db] *= keep;
-                ref[rb] = next;
-            }
+            for (int db = 0; db < 4; ++db) o[db] *= keep;
+            ref = next;
+        }
     };
     // A tile that may hold rows that some token does not see.
     const auto masked_step = [&](int tile) {
-        f32x16a s[RB][2];
+        f32x16a s[2];
         scores(tile, s);
         // Whether the tile of V holds an infinity or NaN: every wave looks at its share of it.
         const char* Vt = Vs[tile & 1];
         uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 16 / WAVES; ++i) {
-            const u32x4a x = *(const u32x4a*)(Vt + (wave * (16 / WAVES) + i) * 1024 + lane * 16);
+        for (int i = 0; i < 16 / kWaves; ++i) {
+            const u32x4a x = *(const u32x4a*)(Vt + (wave * (16 / kWaves) + i) * 1024 + lane * 16);
 #pragma unroll
             for (int w = 0; w < 4; ++w) most = max_halves(most, x[w] & 0x7FFF7FFFu);
         }
@@ -178,27 +159,21 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         __syncthreads();
         if (tile + 2 < stop) fetch_k(tile + 2);
         if (tile + 1 < stop) fetch_v(tile + 1);
+        const Range r = range_of(tile);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const Range r = range_of(tile, rb);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[rb][kb][i] = r.has(kb * 32 + i / 4 * 8 + i % 4) ? s[rb][kb][i] : -INFINITY;
-            top[rb] = top_of(s[rb]);
-        }
+            for (int i = 0; i < 16; ++i) s[kb][i] = r.has(kb * 32 + i / 4 * 8 + i % 4) ? s[kb][i] : -INFINITY;
+        top = top_of(s);
         raise();
-        uint32_t pb[RB][16];
+        uint32_t pb[16];
+        const float off = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const float off = ref[rb] == -INFINITY ? 0.f : ref[rb];
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i >> 4][i & 15], a.scale_log2, -off));
-                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][i >> 4][(i & 15) + 1], a.scale_log2, -off));
-                sum[rb] += x + y;
-                pb[rb][i / 2] = pack_bf16(x, y);
-            }
+        for (int i = 0; i < 32; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], a.scale_log2, -off));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][(i & 15) + 1], a.scale_log2, -off));
+            sum += x + y;
+            pb[i / 2] = pack_bf16(x, y);
         }
         const bool finite = __builtin_amdgcn_readfirstlane(not_finite) != tile;
         if (finite) {
@@ -207,9 +182,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
                     const u32x2 x = read_transposed(Vt + v_at + db * 4096 + u * 1024), y = read_transposed(Vt + v_at + db * 4096 + u * 1024 + 512);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-                        o[rb][db] = product((u32x4a){x.x, x.y, y.x, y.y}, (u32x4a){pb[rb][4 * u], pb[rb][4 * u + 1], pb[rb][4 * u + 2], pb[rb][4 * u + 3]}, o[rb][db]);
+                    o[db] = product((u32x4a){x.x, x.y, y.x, y.y}, (u32x4a){pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]}, o[db]);
                 }
         } else {
             // An infinity or NaN must not meet the zero weight of a row that does not see it: products with zeros in their place, ..
@@ -224,28 +197,24 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
                         if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
                         if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0x0000FFFFu;
                     }
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) o[rb][db] = product(w, (u32x4a){pb[rb][4 * u], pb[rb][4 * u + 1], pb[rb][4 * u + 2], pb[rb][4 * u + 3]}, o[rb][db]);
+                    o[db] = product(w, (u32x4a){pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]}, o[db]);
                 }
             // .. and then they reach the rows that do see them: whatever the weight, an infinity or NaN comes of it.
+            const Range r = range_of(tile);
+            for (int key = 0; key < kKeys; ++key) {
+                if (!r.has(key - half * 4)) continue;
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const Range r = range_of(tile, rb);
-                for (int key = 0; key < kKeys; ++key) {
-                    if (!r.has(key - half * 4)) continue;
+                for (int db = 0; db < 4; ++db)
 #pragma unroll
-                    for (int db = 0; db < 4; ++db)
+                    for (int i = 0; i < 4; ++i) {
+                        // channels 32 db + 8 i + 4 half ..+3: half a piece
+                        const u32x2 v = *(const u32x2*)(Vt + db * 4096 + key * 64 + i * 16 + half * 8);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            // channels 32 db + 8 i + 4 half ..+3: half a piece
-                            const u32x2 v = *(const u32x2*)(Vt + db * 4096 + key * 64 + i * 16 + half * 8);
-#pragma unroll
-                            for (int w = 0; w < 4; ++w) {
-                                const uint32_t x = w % 2 ? v[w / 2] & 0xFFFF0000u : v[w / 2] << 16;
-                                if ((x & 0x7F800000u) == 0x7F800000u) o[rb][db][4 * i + w] += __uint_as_float(x);
-                            }
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t x = w % 2 ? v[w / 2] & 0xFFFF0000u : v[w / 2] << 16;
+                            if ((x & 0x7F800000u) == 0x7F800000u) o[db][4 * i + w] += __uint_as_float(x);
                         }
-                }
+                    }
             }
         }
         dma_wait();
@@ -255,24 +224,21 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
     // written (a matrix product every 7 other instructions keeps both pipes busy, and no more operands wait in registers than the next two products
     // need), then this one's 16 products with the next one's maximum.  `end` is a tile too (its scores are made, and dropped).
     const auto whole_steps = [&](int begin, int end) {
-        f32x16a s[RB][2];
+        f32x16a s[2];
         scores(begin, s);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) top[rb] = top_of(s[rb]);
+        top = top_of(s);
         __syncthreads();
         for (int tile = begin; tile < end; ++tile) {
             fetch_k(min(tile + 2, stop - 1));
             fetch_v(tile + 1);
             raise();
             const char *Kt = Ks[(tile + 1) & 1], *Vt = Vs[tile & 1];
-            f32x16a next[RB][2];
-            uint32_t pb[RB][16];
+            f32x16a next[2];
+            uint32_t pb[16];
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) next[rb][kb][i] = 0.f;
+                for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
             u32x4a k[2][2];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) k[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
@@ -283,19 +249,16 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) k[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
+                for (int kb = 0; kb < 2; ++kb) next[kb] = product(k[i & 1][kb], q[i], next[kb]);
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) next[rb][kb] = product(k[i & 1][kb], q[rb][i], next[rb][kb]);
-#pragma unroll
-                    for (int j = 0; j < 4; j += 2) {
-                        const int kb = i >> 2, at = (i & 3) * 4 + j;
-                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][at], a.scale_log2, -ref[rb]));
-                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][at + 1], a.scale_log2, -ref[rb]));
-                        sum[rb] += x + y;
-                        pb[rb][kb * 8 + at / 2] = pack_bf16(x, y);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int j = 0; j < 4; j += 2) {
+                    const int kb = i >> 2, at = (i & 3) * 4 + j;
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][at], a.scale_log2, -ref));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][at + 1], a.scale_log2, -ref));
+                    sum += x + y;
+                    pb[kb * 8 + at / 2] = pack_bf16(x, y);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
             u32x2 v[2][4][2];
             const auto values = [&](int u) {
@@ -305,32 +268,24 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
                     for (int x = 0; x < 2; ++x) v[u & 1][db][x] = read_transposed(Vt + v_at + db * 4096 + u * 1024 + x * 512);
             };
             values(0);
-            float most[RB];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) most[rb] = next[rb][0][0];
+            float most = next[0][0];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (u < 3) values(u + 1);
+                const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    const u32x4a pu = {pb[rb][4 * u], pb[rb][4 * u + 1], pb[rb][4 * u + 2], pb[rb][4 * u + 3]};
-#pragma unroll
-                    for (int db = 0; db < 4; ++db) {
-                        const u32x4a w = {v[u & 1][db][0].x, v[u & 1][db][0].y, v[u & 1][db][1].x, v[u & 1][db][1].y};
-                        o[rb][db] = product(w, pu, o[rb][db]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) most[rb] = fmaxf(most[rb], next[rb][u >> 1][(u & 1) * 8 + i]);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int db = 0; db < 4; ++db) {
+                    const u32x4a w = {v[u & 1][db][0].x, v[u & 1][db][0].y, v[u & 1][db][1].x, v[u & 1][db][1].y};
+                    o[db] = product(w, pu, o[db]);
                 }
-            }
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                top[rb] = halves_max(most[rb]) * a.scale_log2;
-                s[rb][0] = next[rb][0];
-                s[rb][1] = next[rb][1];
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            top = halves_max(most) * a.scale_log2;
+            s[0] = next[0];
+            s[1] = next[1];
             dma_wait();
             __syncthreads();
         }
@@ -346,57 +301,53 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attend_prompt_kernel(PromptAr
         const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;         // rows from `low` on that the last token does not see
         const int whole_begin = max(min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end), start);
         int tile = start;
-        for (int round = 0; round < 2; ++round) {
-            const int end = round == 0 ? whole_begin : stop;
+        for (int turn = 0; turn < 2; ++turn) {             // masked tiles, whole ones, masked ones
+            const int end = turn == 0 ? whole_begin : stop;
             for (; tile < end; ++tile) masked_step(tile);
-            if (round == 0 && tile < whole_end) {
+            if (turn == 0 && tile < whole_end) {
                 whole_steps(tile, whole_end);
                 tile = whole_end;
             }
         }
     }
 
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const float total = halves_sum(sum[rb]);
-        const int R = R0 + rb * 32 + col;
-        if (R >= a.rows) continue;
-        if (a.parts > 1) {
-            const int64_t at = ((int64_t)part * a.groups + g) * a.row_tiles * kTileRows + R;
-            float* to = a.part_o + at * 128 + half * 4;
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x16a& x = o[rb][db];
-                    *(f32x4a*)(to + db * 32 + i * 8) = (f32x4a){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-                }
-            if (half == 0) a.part_ml[at] = (f32x2a){ref[rb], total};
-            continue;
-        }
-        const bool empty = ref[rb] == -INFINITY;
-        const float over = empty ? 0.f : 1.f / total;
-        char* out = (char*)c.out + query_row(rb) * 256;
+    const float total = halves_sum(sum);
+    if (R0 + col >= a.rows) return;
+    if (a.parts > 1) {
+        const int64_t at = ((int64_t)part * a.groups + g) * a.row_tiles * kTileRows + R;
+        float* to = a.part_o + at * 128 + half * 4;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x16a& x = o[rb][db];
-                *(u32x2*)(out + (db * 32 + i * 8 + half * 4) * 2) =
-                    (u32x2){pack_bf16(x[4 * i] * over, x[4 * i + 1] * over), pack_bf16(x[4 * i + 2] * over, x[4 * i + 3] * over)};
+                const f32x16a& x = o[db];
+                *(f32x4a*)(to + db * 32 + i * 8) = (f32x4a){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
             }
-        if (c.lse && half == 0)
-            c.lse[((int64_t)b * c.kv * c.group + head * c.group + R % c.group) * c.m + R / c.group] = empty ? -INFINITY : (ref[rb] + __builtin_amdgcn_logf(total)) * kLn2;
+        if (half == 0) a.part_ml[at] = (f32x2a){ref, total};
+        return;
     }
+    const bool empty = ref == -INFINITY;
+    const float over = empty ? 0.f : 1.f / total;
+    char* out = (char*)c.out + query_row * 256;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x16a& x = o[db];
+            *(u32x2*)(out + (db * 32 + i * 8 + half * 4) * 2) =
+                (u32x2){pack_bf16(x[4 * i] * over, x[4 * i + 1] * over), pack_bf16(x[4 * i + 2] * over, x[4 * i + 3] * over)};
+        }
+    if (c.lse && half == 0)
+        c.lse[((int64_t)b * c.kv * c.group + head * c.group + R % c.group) * c.m + t] = empty ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 // Joins the parts of four rows, a wave a row, two channels a lane.
-__global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a, int tile_rows) {
+__global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a) {
     const AttendCall& c = a.c;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, g = (int)(at / a.rows), R = (int)(at - (int64_t)g * a.rows);
     if (g >= a.groups) return;
-    const int64_t first = (int64_t)g * a.row_tiles * tile_rows + R, step = (int64_t)a.groups * a.row_tiles * tile_rows;
+    const int64_t first = (int64_t)g * a.row_tiles * kTileRows + R, step = (int64_t)a.groups * a.row_tiles * kTileRows;
     float ref = -INFINITY, sum = 0.f;
     for (int k = 0; k < a.parts; ++k) ref = fmaxf(ref, a.part_ml[first + k * step].x);
     const bool empty = ref == -INFINITY;
@@ -418,7 +369,6 @@ __global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a, i
 }  // namespace
 
 hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream) {
-    constexpr int kWaves = 4, kTileRows = kWaves * 32;
     PromptArgs a;
     a.c = call;
     a.scale_log2 = call.scale * (1.f / kLn2);
@@ -426,14 +376,14 @@ hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, h
     a.rows = call.m * call.group;
     a.row_tiles = (a.rows + kTileRows - 1) / kTileRows;
     // Few new tokens over a long cache: the tiles of keys shared out until every unit has two workgroups, 8 tiles each at least, as far as there is scratch.
-    const int64_t blocks = (int64_t)a.groups * a.row_tiles, tiles = (call.window > 0 ? std::min(call.n, call.window + call.sinks + call.m) : call.n) / kKeys;
+    const int64_t blocks = (int64_t)a.groups * a.row_tiles, tiles = (call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n) / kKeys;
     const int64_t part_bytes = blocks * kTileRows * (int64_t)(128 * sizeof(float) + sizeof(f32x2a)), room = call.scratch ? call.scratch_bytes - kScratchCounters : 0;
     int64_t parts = std::min(std::min(2 * ctx->num_cu / blocks, tiles / 8), room / part_bytes);
     a.parts = parts > 1 ? (int)parts : 1;
     a.part_o = (float*)((char*)call.scratch + kScratchCounters);
     a.part_ml = (f32x2a*)(a.part_o + a.parts * blocks * kTileRows * 128);
-    attend_prompt_kernel<kWaves, 1, 2><<<(unsigned)(blocks * a.parts), kWaves * 64, 0, stream>>>(a);
-    if (a.parts > 1) attend_prompt_join_kernel<<<(unsigned)(((int64_t)a.groups * a.rows + 3) / 4), 256, 0, stream>>>(a, kTileRows);
+    attend_prompt_kernel<<<(unsigned)(blocks * a.parts), kWaves * 64, 0, stream>>>(a);
+    if (a.parts > 1) attend_prompt_join_kernel<<<(unsigned)(((int64_t)a.groups * a.rows + 3) / 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

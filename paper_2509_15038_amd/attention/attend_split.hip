@@ -888,19 +888,29 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     a.rows = call.m * call.group;
     a.row_tiles = (a.rows + kRowTile - 1) / kRowTile;
     a.items = (int)(call.count * call.kv * a.row_tiles);
-    // A workgroup a unit, that share the tiles of all heads equally, each with a tile a wave at least as far as the host knows; a workgroup an item where
-    // the items alone are many times that, or where there is no room for partial results.
+    // How many workgroups share the tiles (as far as the host knows them) of all items; 0: every item has one.
     const bool mx = call.K_scales != nullptr, f32 = call.dtype == CURDKV_DTYPE_F32;
     const int T = mx && !f32 ? 32 : 16, row = f32 ? 512 : 256;
-    int64_t keys = call.n;
-    if (call.window > 0) keys = std::min(keys, (int64_t)call.window + call.sinks + call.m);
-    const int64_t heads = call.count * call.kv, tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles;
-    int64_t shares = std::min((int64_t)ctx->num_cu * (mx && tiles >= 1024 * (int64_t)ctx->num_cu ? 2 : 1), std::max((int64_t)a.items, (tiles + kSplitWaves - 1) / kSplitWaves));
-    const int64_t slot = kRowTile * kPartBytes, room = call.scratch ? (call.scratch_bytes - kCounters * (int64_t)sizeof(int)) / slot : 0;
-    shares = std::min(shares, room - 2 * a.items);
-    if (shares <= a.items / 4 || a.items > kCounters) shares = 0;
+    const int64_t units = ctx->num_cu, heads = call.count * call.kv, slot = kRowTile * kPartBytes;
+    const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
+    const int64_t tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles, room = call.scratch ? (call.scratch_bytes - kCounters * (int64_t)sizeof(int)) / slot : 0;
+    // One a unit, with a tile a wave at least (two: one token over 131072 rows 100 us, so 91).  4 bits, whose expansion wants two waves a SIMD, two a unit
+    // where they have long to go (320 us, so 295; 32 tiles a unit: 18, 20).
+    const int64_t wanted = std::min(units * (mx && tiles >= 1024 * units ? 2 : 1), std::max((int64_t)a.items, (tiles + kSplitWaves - 1) / kSplitWaves));
+    int64_t shares = std::min(wanted, room - 2 * a.items);
+    // Few items: each its own workgroups, which have less to look up and to join (64 heads of up to 2000 rows 18.1 us, so 15.6, of 4 bits 21.5, so 14.7); where few share one
+    // for long, equal shares of all of them count for more (64 heads of 16000 in 4 bits 41, so 49).
+    a.whole = a.items <= 64 && 2 * a.items <= shares && (8 * a.items <= shares || tiles <= 64 * shares);
+    // To share costs a join: 3 us, 10 where a workgroup may have parts of several items.  Not shared and shared, us: 8 heads of 500 rows 8.6 and 10.1, of
+    // 1000 12.9 and 11.2; 64 of up to 500 8.8 and 11.1, of 1000 13.3 and 12.7; 256 of 500 10 and 20, of 2000 32 and 36, of 8000 102 and 91; 1024 of 1000 57 and
+    // 65, of 2000 109 and 100.  fp32's tiles take twice as long: 8 of 250 11.6 and 12.3, of 400 14.9 and 13.2; 128 of 1000 28 and 27.  Kept rows differ more from head to
+    // head: 8 of about 250 11.3 and 10.9, 400 in 4 bits 10.5 and 11.1, 600 12.8 and 11.0; 256 of 500 27.9 and 26.4, of 1000 61 and 40, in 4 bits 26.6 and 24.3.
+    const int64_t least = (a.whole ? 48 : 128) / (f32 ? 2 : 1) / (call.offsets ? 4 : 1);
+    // Equal ones in whole turns of all units are shared out already: 256 heads of 4000 rows 81 and 87, through windows of 4096 69 and 74 (264 heads: 106 and 77).
+    const bool equal = !call.offsets && (!call.lengths || (call.window > 0 && 2 * (int64_t)call.window <= call.n)) && a.items % units == 0;
+    if (tiles < least * a.items || equal || a.items > kCounters || (shares < wanted && shares < a.items)) shares = 0;
     a.shares = (int)shares;
-    a.whole = 8 * a.items <= a.shares && a.items <= 64;
+    a.whole = a.whole && shares > 0;
     a.arrived = (int*)call.scratch;
     a.part_o = (float*)(a.arrived + kCounters);
     a.part_ml = (f32x2a*)(a.part_o + (shares + 2 * a.items) * kRowTile * 128);

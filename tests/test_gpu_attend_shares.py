@@ -1,0 +1,47 @@
+"""Attention of a few tokens where workgroups share heads: each head its own workgroups, equal shares of all of them with parts of several heads in one, more
+heads than units, and the sides of the rules between these and a workgroup a head."""
+
+import numpy as np
+import pytest
+import torch
+
+from tests import attend_util as U
+from tests.test_gpu_attend_kept import FORMS, check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count,n", [(1, 750), (1, 900), (1, 8200), (32, 383), (32, 900), (31, 1700)])
+def test_heads_with_workgroups_of_their_own(dtype, count, n):
+    U.check_attend(dict(count=count, kv=2, m=1, n=n, dtype=dtype), seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count,m,n,window", [(33, 1, 2100, 0), (65, 2, 2200, 0), (150, 1, 2050, 0), (65, 1, 4200, 2500), (9, 9, 2300, 0)])
+def test_equal_shares_of_all_heads(dtype, count, m, n, window):
+    U.check_attend(dict(count=count, kv=2, group=2 if m > 1 else 4, m=m, n=n, window=window, sinks=4, dtype=dtype), seed=count)
+
+
+@pytest.mark.parametrize("count", [128, 129])
+def test_whole_turns_of_the_units(count):
+    U.check_attend(dict(count=count, kv=2, group=1, m=1, n=2100), seed=count, lengths="full")
+
+
+@pytest.mark.parametrize("dtype,mx", FORMS)
+@pytest.mark.parametrize("heads,mean,most", [(3, 180, 300), (32, 400, 1500), (35, 700, 9000), (150, 600, 2000), (300, 600, 700), (520, 550, 2100)])
+def test_kept_rows(dtype, mx, heads, mean, most):
+    rng = np.random.default_rng(heads)
+    budgets = np.minimum(rng.exponential(mean, heads * 2).astype(int) + mean // 4, most)
+    budgets[rng.integers(0, heads * 2, 3)] = 0
+    budgets[-1] = 0
+    check(dtype, mx, heads, 2, 2, 1, budgets, 20, rng.integers(0, 21, heads), seed=heads)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_all_rows_in_one_head(mx):
+    # 4 and 150 heads; one has all the rows, the others nothing but, some of them, a row since
+    for heads in (4, 150):
+        budgets = np.zeros(heads, dtype=int)
+        budgets[heads // 2] = 20000
+        check("bf16", mx, heads, 1, 4, 1, budgets, 1, np.arange(heads) % 2, seed=heads)

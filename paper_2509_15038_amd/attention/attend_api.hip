@@ -36,10 +36,10 @@ int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
     // Which kernel: the split one takes tiles of 16 rows (tokens times query heads of a KV head), each of which reads the cache, the prompts' ones 128.
     // bf16, us, split and prompt: 12 tokens of 32 heads over 1000 rows 15 and 24, 32 over 1000 19 and 26, 100 over 1000 26 and 27; 12 over 16000 39 and 32,
     // 32 over 16000 47 and 35, 100 over 16000 237 and 58; 16 sequences of 32 over 4000 298 and 76.
-    // fp32: 500 tokens of 32 heads 71 and 87, 2048 439 and 349 (128 rows a workgroup have to fill the units twice).
+    // fp32: prompts of 8 heads 600 tokens 65 and 69, 800 93 and 89, 2400 572 and 344; 64 tokens of 4 sequences over 500 rows 32 and 61, of 16 116 and 65.
     const int64_t rows = (int64_t)call.m * call.group, tiles = call.count * call.kv * ((rows + 127) / 128);
     const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
-    const bool f32 = call.dtype == CURDKV_DTYPE_F32, prompt = !call.offsets && (f32 ? tiles >= 2 * (int64_t)ctx->num_cu : rows > 32 && rows * keys > kPromptProducts);
+    const bool f32 = call.dtype == CURDKV_DTYPE_F32, prompt = !call.offsets && (f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 32 && rows * keys > kPromptProducts);
     const auto launch = !prompt ? launch_attend_split : f32 ? launch_attend_prompt_f32 : launch_attend_prompt;
     return launch(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }

@@ -1,5 +1,5 @@
-// C ABI of the operators around a compressed cache: argument checks and launches (rotate_kernel.hip, mx_kernels.hip,
-// attend_split.hip).
+// C ABI of the operators around a compressed cache: argument checks and launches (rotate_kernel.hip, mx_kernels.hip, attend_split.hip, attend_prompt.hip,
+// attend_prompt_f32.hip).
 
 #include <algorithm>
 #include <cmath>
@@ -11,7 +11,8 @@ using namespace curdkv;
 
 namespace {
 
-constexpr int64_t kPromptProducts = 200000;    // rows times keys of a KV head from which the prompts' kernel is the faster one
+// Tiles of 16 rows, and these times the keys, from which the prompts' kernel is the faster one (run_attend).
+constexpr int64_t kPromptItems = 600, kPromptProducts = 400000;
 
 bool aligned16(std::initializer_list<const void*> ptrs) {
     uintptr_t all = 0;
@@ -34,12 +35,14 @@ int check_attend(const curdkv_ctx* ctx, const void* Q, const void* out, int64_t 
 
 int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
     // Which kernel: the split one takes tiles of 16 rows (tokens times query heads of a KV head), each of which reads the cache, the prompts' ones 128.
-    // bf16, us, split and prompt: 12 tokens of 32 heads over 1000 rows 15 and 24, 32 over 1000 19 and 26, 100 over 1000 26 and 27; 12 over 16000 39 and 32,
-    // 32 over 16000 47 and 35, 100 over 16000 237 and 58; 16 sequences of 32 over 4000 298 and 76.
+    // bf16, us, split and prompt, 8 heads of 4 a sequence: 9 tokens over 500 rows 9 and 15, over 8000 25 and 25, 32 over 8000 30 and 27; 8 sequences of 9 over 2000 23 and 24, of
+    // 16 27 and 25, of 9 over 8000 77 and 50; 32 of 9 over 500 23 and 17, of 8 over 500 15 and 17, over 2000 57 and 50; prompts of 200 tokens 9.5 and 11.2, 300 14.2 and 13.5; 8 of
+    // up to 64 12 and 9.  One tile of 16 a head: 32 sequences of 4 tokens over 8000 100 and 164.
     // fp32: prompts of 8 heads 600 tokens 65 and 69, 800 93 and 89, 2400 572 and 344; 64 tokens of 4 sequences over 500 rows 32 and 61, of 16 116 and 65.
-    const int64_t rows = (int64_t)call.m * call.group, tiles = call.count * call.kv * ((rows + 127) / 128);
+    const int64_t rows = (int64_t)call.m * call.group, heads = call.count * call.kv, items = heads * ((rows + 15) / 16), tiles = heads * ((rows + 127) / 128);
     const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
-    const bool f32 = call.dtype == CURDKV_DTYPE_F32, prompt = !call.offsets && (f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 32 && rows * keys > kPromptProducts);
+    const bool f32 = call.dtype == CURDKV_DTYPE_F32;
+    const bool prompt = !call.offsets && (f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 16 && (items > kPromptItems || items * keys > kPromptProducts));
     const auto launch = !prompt ? launch_attend_split : f32 ? launch_attend_prompt_f32 : launch_attend_prompt;
     return launch(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }

@@ -294,9 +294,10 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  * A token that sees nothing (length < m and i < m - length) gets zeros and -infinity; what a
  * token does not see does not reach it, infinities and NaN included.
  * lengths: int32 [count], clamped to [0, n]; NULL = n for all.  n <= stride, n <= max_tokens.
- * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0.
+ * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0; m <= max_tokens.
  * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits,
- * with a bf16 cache the weights are rounded to bf16 for their product with V.
+ * with a bf16 cache the weights are rounded to bf16 for their product with V; with an fp32 cache every
+ * product is good to 2^-22 of itself at least.
  * scratch: device memory of the caller's, 16-byte aligned, for the partial results of few tokens over
  *   long caches, whose heads are shared out over many workgroups; CURDKV_ATTEND_SCRATCH_BYTES
  *   are as much as a call ever uses, with less (0 and NULL included) there are fewer shares.

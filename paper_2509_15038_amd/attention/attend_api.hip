@@ -25,7 +25,7 @@ int check_attend(const curdkv_ctx* ctx, const void* Q, const void* out, int64_t 
                  const void* scratch, int64_t scratch_bytes) {
     if (!ctx || !Q || !out) return CURDKV_ERR_INVALID_ARG;
     if (!on_device_of(ctx)) return CURDKV_ERR_INVALID_ARG;
-    if (count < 1 || m < 1 || n < 0 || n > ctx->cfg.max_tokens || m > ctx->cfg.max_tokens || stride < n) return CURDKV_ERR_INVALID_ARG;
+    if (count < 1 || m < 1 || n < 0 || n > ctx->cfg.max_tokens || stride < n) return CURDKV_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !std::isfinite(scale)) return CURDKV_ERR_INVALID_ARG;
     if (scratch_bytes < 0 || !aligned16({Q, out, scratch})) return CURDKV_ERR_INVALID_ARG;
     const int64_t most = (1LL << 31) - 1, heads = (int64_t)ctx->cfg.kv_heads * ctx->cfg.group_size;
@@ -86,7 +86,7 @@ int curdkv_attend(curdkv_ctx* ctx, const void* Q, const void* K, const void* V, 
                   const int32_t* lengths, int64_t window, int32_t n_sink, float scale, void* out, float* lse, void* scratch, int64_t scratch_bytes, void* stream) {
     const int rc = check_attend(ctx, Q, out, count, m, n, stride, scale, scratch, scratch_bytes);
     if (rc != CURDKV_OK) return rc;
-    if (!K || !V || n < 1 || window < 0 || n_sink < 0 || !aligned16({K, V})) return CURDKV_ERR_INVALID_ARG;
+    if (!K || !V || n < 1 || m > ctx->cfg.max_tokens || window < 0 || n_sink < 0 || !aligned16({K, V})) return CURDKV_ERR_INVALID_ARG;
     AttendCall c{};
     c.Q = Q, c.out = out, c.lse = lse, c.count = count;
     c.kv = ctx->cfg.kv_heads, c.group = ctx->cfg.group_size, c.m = (int)m, c.dtype = ctx->cfg.dtype, c.scale = scale;

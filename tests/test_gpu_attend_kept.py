@@ -211,3 +211,22 @@ def test_refusals():
             assert e.value.code == B.ERR_INVALID_ARG, bad
         torch.cuda.synchronize()
         assert bool((out == 7).all())
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_more_new_tokens_than_any_cache_holds(mx):
+    # max_tokens bounds caches and tails; the tokens that look at kept rows may be more
+    K, V, Q = (U.randn(i, (70, D) if i < 3 else (1, 6, 4, D), torch.bfloat16) for i in (1, 2, 3))
+    Kt, Vt, off, out = K[:1].clone(), V[:1].clone(), torch.tensor([0, 70], device="cuda"), torch.empty_like(Q)
+    with U.context(1, 4, "bf16", 1) as ctx:
+        if mx:
+            (Kc, Ks, k), (Vc, Vs, v) = pack("bf16", K), pack("bf16", V)
+            ctx.attend_kept_mx(Q, Kc, Ks, Vc, Vs, off, 1, 6, 70, out, K_tail=Kt, V_tail=Vt, tail_n=1, tail_stride=1)
+        else:
+            k, v = K, V
+            ctx.attend_kept(Q, K, V, off, 1, 6, 70, out, K_tail=Kt, V_tail=Vt, tail_n=1, tail_stride=1)
+        torch.cuda.synchronize()
+    seen = torch.cat([torch.ones((6, 70), dtype=torch.bool, device="cuda"), U.causal(6, 1, 1, 0, 0)], 1)
+    for h in range(4):
+        want = U.attention(Q[0, :, h], torch.cat([k.double(), Kt.double()]), torch.cat([v.double(), Vt.double()]), seen, D ** -0.5)
+        U.check_attention(out[0, :, h], None, want, "bf16", 71)

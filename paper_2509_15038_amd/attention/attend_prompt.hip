@@ -1,5 +1,9 @@
 // Attention of many tokens (prompts) over a bf16 cache: tiles of 64 keys against 32 rows R a wave, the softmax's maximum and sum running
-// along.  Bound by the matrix units and the exponentials: 4 * 128 flops and one exponential for a visible (row, key).
+// along.  Bound by the matrix units and the exponentials: 4 * 128 flops and one exponential for a visible (row, key).  Measured: 8192 tokens of 32 heads (550
+// Gflop) 531 us, 1040 Tflop/s; 32768 through windows of 4096 (2064 Gflop) 2043 us, 1010 Tflop/s; a library product of 8192^3 reaches 1240.  What holds it there is the
+// power that the numbers' switching costs: zeros in place of random ones take 413 us, and the product 1780 Tflop/s.
+// Four waves of 32 rows: eight share a tile's loads (4096 tokens 164 us, so 154), but with windows, whose tiles have masks, wait for each other (500: 148, so 161); 64 rows
+// a wave leave one wave a SIMD (973 Tflop/s, so 904).
 //
 // S^T = K Q^T by mfma_f32_32x32x16_bf16: a lane has the scores of one row R = lane % 32, for the keys 8 i + 4 (lane / 32) + 0..3 of 32,
 // which is what the B operand of O^T = V^T P^T takes if the 16 keys of a product are counted in that order; P never leaves its
@@ -10,7 +14,8 @@
 // same piece meet different banks.
 //
 // The reference point of a row's exponentials is its maximum only to within 2^8: it moves, and what has been summed is scaled, when the
-// maximum passes it by more, so that most tiles scale nothing.
+// maximum passes it by more, so that most tiles scale nothing.  Weights are then up to 2^8; in bf16 they are rounded by 2^-8 of themselves for their product with V, as
+// weights up to 1 are, and their sum takes them in 32 bits.
 
 #include <algorithm>
 

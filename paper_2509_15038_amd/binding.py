@@ -353,11 +353,15 @@ class Context:
             raise CurdkvError(rc, "curdkv_normalise")
 
     def _scratch(self, given):
-        """(address, bytes) of the partial results' memory: the caller's tensor, or one that the context keeps from its first attention call on."""
+        """(address, bytes) of the partial results' memory: the caller's tensor, or one that the context keeps from its first attention call on.  Calls
+        that overlap in time, on several streams, need a tensor each (zeros once, ATTEND_SCRATCH_BYTES)."""
         if given is None:
             if self._own_scratch is None:
                 import torch
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("a context's first attention call allocates its scratch: make one before recording, or give it scratch")
                 self._scratch_tensor = torch.zeros((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
+                torch.cuda.current_stream().synchronize()   # (cleared before any stream uses it)
                 self._own_scratch = self._scratch_tensor.data_ptr(), ATTEND_SCRATCH_BYTES
             return self._own_scratch
         return given.data_ptr(), given.numel() * given.element_size()

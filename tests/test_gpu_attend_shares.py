@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2509_15038_amd import binding as B
 from tests import attend_util as U
 from tests.test_gpu_attend_kept import FORMS, check
 
@@ -45,3 +46,38 @@ def test_all_rows_in_one_head(mx):
         budgets = np.zeros(heads, dtype=int)
         budgets[heads // 2] = 20000
         check("bf16", mx, heads, 1, 4, 1, budgets, 1, np.arange(heads) % 2, seed=heads)
+
+
+def test_the_first_call_on_another_stream():
+    # the context's scratch is cleared on the current stream, which is busy; the call is on another one
+    K, V, Q = (U.randn(i, (1, 2, 5000, U.D) if i < 3 else (1, 1, 8, U.D), torch.bfloat16) for i in (1, 2, 3))
+    out, side = torch.empty_like(Q), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    dirty = torch.full((B.ATTEND_SCRATCH_BYTES,), 255, dtype=torch.uint8, device="cuda")
+    del dirty                                                                        # (what the allocator gives out next)
+    with U.context(2, 4, "bf16", 5000) as ctx:
+        torch.cuda._sleep(100_000_000)
+        for _ in range(3):
+            ctx.attend(Q, K, V, 1, 1, 5000, 5000, out, stream=side)
+        torch.cuda.synchronize()
+        assert bool((ctx._scratch_tensor[:16384] == 0).all())
+    for h in range(8):
+        want = U.attention(Q[0, :, h], K[0, h // 4], V[0, h // 4], U.causal(1, 5000, 5000, 0, 0), U.D ** -0.5)
+        U.check_attention(out[0, :, h], None, want, "bf16", 5000)
+
+
+def test_a_first_call_is_not_recorded():
+    K, V, Q = (U.randn(i, (1, 2, 100, U.D) if i < 3 else (1, 1, 8, U.D), torch.bfloat16) for i in (1, 2, 3))
+    out, scratch = torch.empty_like(Q), torch.zeros(B.ATTEND_SCRATCH_BYTES, dtype=torch.uint8, device="cuda")
+    with U.context(2, 4, "bf16", 100) as ctx:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            with pytest.raises(RuntimeError):
+                ctx.attend(Q, K, V, 1, 1, 100, 100, out)
+            ctx.attend(Q, K, V, 1, 1, 100, 100, out, scratch=scratch)
+        graph.replay()
+        torch.cuda.synchronize()
+        recorded = out.clone()
+        ctx.attend(Q, K, V, 1, 1, 100, 100, out)
+        torch.cuda.synchronize()
+        assert torch.equal(recorded, out)

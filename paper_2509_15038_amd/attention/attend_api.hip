@@ -103,7 +103,7 @@ int curdkv_compact_mx(curdkv_ctx* ctx, const void* K, const void* V, int64_t n, 
     if (n < 1 || n > ctx->cfg.max_tokens || total < 0 || total > ctx->heads * n || !aligned16({K, V, K_codes, V_codes})) return CURDKV_ERR_INVALID_ARG;
     if (total == 0) return CURDKV_OK;
     if (!indices || !K_codes || !K_scales || !V_codes || !V_scales) return CURDKV_ERR_INVALID_ARG;
-    if (total > (1LL << 34)) return CURDKV_ERR_UNSUPPORTED;            // (the grid is 32 bits)
+    if (total > (1LL << 29)) return CURDKV_ERR_UNSUPPORTED;            // (a launch's threads are counted in 32 bits)
     return launch_compact_mx(ctx, K, V, n, indices, offsets, total, ctx->heads, K_codes, K_scales, V_codes, V_scales, (hipStream_t)stream) == hipSuccess
                ? CURDKV_OK : CURDKV_ERR_HIP;
 }
@@ -113,7 +113,7 @@ int curdkv_expand_mx(curdkv_ctx* ctx, const uint8_t* codes, const uint8_t* scale
     if (!on_device_of(ctx)) return CURDKV_ERR_INVALID_ARG;
     if (rows == 0) return CURDKV_OK;
     if (!codes || !scales || !out || !aligned16({codes, out})) return CURDKV_ERR_INVALID_ARG;
-    if (rows > (1LL << 31) - 1) return CURDKV_ERR_UNSUPPORTED;
+    if (rows > (1LL << 31) - 1) return CURDKV_ERR_UNSUPPORTED;         // (more than the memory holds)
     return launch_expand_mx(ctx->cfg.dtype, codes, scales, rows, out, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }
 

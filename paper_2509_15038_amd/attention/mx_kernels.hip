@@ -139,9 +139,15 @@ hipError_t launch_compact_mx(const curdkv_ctx* ctx, const void* K, const void* V
 }
 
 hipError_t launch_expand_mx(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows, void* out, hipStream_t stream) {
-    const int64_t pieces = rows * 16;
-    const auto launch = [&](auto kernel) { kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, stream>>>((const uint32_t*)codes, scales, pieces, out); };
     const bool bf16 = dtype == CURDKV_DTYPE_BF16;
+    // (a launch's threads are counted in 32 bits: 2^27 rows each)
+    const auto launch = [&](auto kernel) {
+        for (int64_t first = 0; first < rows; first += 1 << 27) {
+            const int64_t pieces = (rows - first < 1 << 27 ? rows - first : 1 << 27) * 16;
+            kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, stream>>>((const uint32_t*)(codes + first * 64), scales + first * 4, pieces,
+                                                                         (char*)out + first * (bf16 ? 256 : 512));
+        }
+    };
     if (rows * ((bf16 ? 256 : 512) + 68) > kPastCaches) bf16 ? launch(expand_mx_kernel<true, true>) : launch(expand_mx_kernel<false, true>);
     else bf16 ? launch(expand_mx_kernel<true, false>) : launch(expand_mx_kernel<false, false>);
     return hipGetLastError();

@@ -107,3 +107,17 @@ def test_nothing_kept_and_refusals():
         ctx.compact_mx(K, K, 64, torch.full((64,), 64, dtype=torch.int32, device="cuda"), torch.tensor([0, 32, 64], device="cuda"), 64, c, s, c.clone(), s.clone())
         torch.cuda.synchronize()
         assert bool((c == 9).all()) and bool((s == 9).all()) and bool((out == 3).all())
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    # 2^28 rows are 2^32 pieces of eight channels; the last rows alone are looked at
+    rows, last = 2 ** 28 + 77, 200
+    x = U.randn(9, (last, D), torch.bfloat16)
+    value, codes, scales = U.four_bits(x)
+    far = [torch.empty((rows, w), dtype=torch.uint8, device="cuda") for w in (64, 4)]
+    far[0][-last:], far[1][-last:] = codes.cuda(), scales.cuda()
+    out = torch.empty((rows, D), dtype=torch.bfloat16, device="cuda")
+    with U.context(1, 4, "bf16", 64) as ctx:
+        ctx.expand_mx(*far, rows, out)
+        torch.cuda.synchronize()
+    assert torch.equal(out[-last:].double().cpu(), value)

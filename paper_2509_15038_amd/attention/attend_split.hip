@@ -13,11 +13,12 @@
 //
 // Measured: a token over 131072 rows of 8 heads (537 MB) 91 us, 5.9 TB/s; of 32 sequences through windows of 4096 (404 MB) 66 us, 6.1 TB/s; 4 tokens of 8 sequences over
 // 6553 kept rows a head (217 MB) 50 us, 4.3 TB/s; 32 sequences over 13107 kept rows a head in 4 bits (490 MB with their tails) 105 us, 4.7 TB/s: the heads' ends inside the shares
-// (3 us each) and the join (4 us).  One sequence over 3276 kept rows a head 16 us: a chain of latencies, of which reading is 2.
+// (3 us each) and the join (4 us).  One sequence over 3276 kept rows a head 13 us: a chain of latencies, of which reading is 3.
 // A workgroup of four waves a unit, each with two tiles of 16 keys (32 KB) in flight: more workgroups only add to what there is to join (launch_attend_split).
 // A wave's next tile is asked for without a branch: in front of one the compiler waits for all that is in flight.
 
 #include <algorithm>
+#include <cmath>
 
 #include "attend_device.h"
 #include "attend_internal.h"
@@ -901,9 +902,12 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     const int64_t units = ctx->num_cu, heads = call.count * call.kv, slot = kRowTile * kPartBytes;
     const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
     const int64_t tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles, room = call.scratch ? (call.scratch_bytes - kCounters * (int64_t)sizeof(int)) / slot : 0;
-    // One a unit, with a tile a wave at least (two: one token over 131072 rows 100 us, so 91).  4 bits, whose expansion wants two waves a SIMD, two a unit
-    // where they have long to go (320 us, so 295; 32 tiles a unit: 18, 20).
-    const int64_t wanted = std::min(units * (mx && tiles >= 1024 * units ? 2 : 1), std::max((int64_t)a.items, (tiles + kSplitWaves - 1) / kSplitWaves));
+    // One a unit at most (two: one token over 131072 rows 100 us, so 91).  4 bits, whose expansion wants two waves a SIMD, two a unit
+    // where they have long to go (320 us, so 295; 32 tiles a unit: 18, 20).  A tile a wave at least, and no more parts of an item than pay: its tiles over the parts are read
+    // in a time of their own, its parts are counted and joined in theirs, and the two together are least where parts^2 is about the tiles, or twice them in fp32 (one token of 8
+    // heads over 4000 rows 14.7 us with as many as there are units, so 13.1; in 4 bits 18.2, so 13.1; of one head over 16000 48.5, so 17.1).
+    const int64_t most = (int64_t)std::sqrt((f32 ? 2.0 : 1.0) * a.items * tiles);
+    const int64_t wanted = std::min(units * (mx && tiles >= 1024 * units ? 2 : 1), std::max((int64_t)a.items, std::min(most, (tiles + kSplitWaves - 1) / kSplitWaves)));
     int64_t shares = std::min(wanted, room - 2 * a.items);
     // Few items: each its own workgroups, which have less to look up and to join (64 heads of up to 2000 rows 18.1 us, so 15.6, of 4 bits 21.5, so 14.7); where few share one
     // for long, equal shares of all of them count for more (64 heads of 16000 in 4 bits 41, so 49).

@@ -79,6 +79,9 @@ __device__ __forceinline__ u32x2 read_transposed(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4a*)p));
 }
 
+// (a lambda that is not inlined would leave what it refers to in memory)
+#define ALWAYS_INLINE __attribute__((always_inline))
+
 template <int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kernel(PromptF32Args a) {
     constexpr int kTileRows = WAVES * 32, kBlocks = 16 / WAVES, kEvery = 3 * WAVES / 4;
@@ -93,8 +96,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
     const int t_first = row_tile * kTileRows / c.group, t_last = min(c.m - 1, (row_tile * kTileRows + kTileRows - 1) / c.group);
     const Seen seen = seen_rows(length, c.m, t_first, t_last, c.window, c.sinks);
     const int first_tiles = (seen.first + kKeys - 1) / kKeys, tiles = first_tiles + (seen.high - seen.low + kKeys - 1) / kKeys;
-    const auto row_of = [&](int tile) { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
-    const auto count_of = [&](int tile) { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
+    const auto row_of = [&](int tile) ALWAYS_INLINE { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
+    const auto count_of = [&](int tile) ALWAYS_INLINE { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
 
     const int R0 = row_tile * kTileRows + wave * 32, R = min(R0 + col, a.rows - 1), t = R / c.group, p = length - c.m + t;
     const int p_first = length - c.m + min(R0, a.rows - 1) / c.group, p_last = length - c.m + min(R0 + 31, a.rows - 1) / c.group;
@@ -112,7 +115,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
     const char* Kg = (const char*)c.K + (int64_t)g * c.stride * 512;
     const char* Vg = (const char*)c.V + (int64_t)g * c.stride * 512;
     const uint32_t raw_lds = lds_address(&raw[0][0]);
-    const auto fetch = [&](int tile) {
+    const auto fetch = [&](int tile) ALWAYS_INLINE {
         const int64_t j0 = row_of(tile);
         const int count = count_of(tile);
 #pragma unroll
@@ -124,28 +127,30 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
         }
     };
     // This wave's rows of a tile into parts: 32 pieces of eight channels a block, K's by lanes 0..31, V's by the others.  Block i; `odd` as above.
+    // (eight lanes write 128 bytes side by side)
+    const int piece_row = col >> 2 & 1, piece_at = (col & 3) + (col >> 3) * 4;
     struct Piece {
         f32x4a x, y;
         Parts z;
     };
-    const auto read_piece = [&](Piece& e, int i) {
-        const f32x4a* from = (const f32x4a*)(raw[half] + (wave * kBlocks + i) * 1024) + col * 2;
+    const auto read_piece = [&](Piece& e, int i) ALWAYS_INLINE {
+        const f32x4a* from = (const f32x4a*)(raw[half] + (wave * kBlocks + i) * 1024 + piece_row * 512) + piece_at * 2;
         e.x = from[0], e.y = from[1];
     };
-    const auto part_pair = [&](Piece& e, int j, float& odd) {
+    const auto part_pair = [&](Piece& e, int j, float& odd) ALWAYS_INLINE {
         const f32x4a& x = j < 2 ? e.x : e.y;
         uint32_t h, m, l;
         apart(x[j % 2 * 2], x[j % 2 * 2 + 1], h, m, l, odd);
         e.z.h[j] = h, e.z.m[j] = m, e.z.l[j] = l;
     };
-    const auto write_piece = [&](const Piece& e, int tile, int i) {
-        const int row = (wave * kBlocks + i) * 2 + (col >> 4), piece = col & 15;
-        char* at = (half ? Vs[tile & 1] : Ks[tile & 1]) + (piece >> 2) * (kKeys * 64) + row * 64 + (((piece & 3) ^ (half ? 0 : (row >> 1) & 3)) << 4);
+    const auto write_piece = [&](const Piece& e, int tile, int i) ALWAYS_INLINE {
+        const int row = (wave * kBlocks + i) * 2 + piece_row;
+        char* at = (half ? Vs[tile & 1] : Ks[tile & 1]) + (piece_at >> 2) * (kKeys * 64) + row * 64 + (((piece_at & 3) ^ (half ? 0 : (row >> 1) & 3)) << 4);
         *(u32x4a*)at = e.z.h;
         *(u32x4a*)(at + kPart) = e.z.m;
         *(u32x4a*)(at + 2 * kPart) = e.z.l;
     };
-    const auto take_apart = [&](int tile, int i, float& odd, bool careful) {
+    const auto take_apart = [&](int tile, int i, float& odd, bool careful) ALWAYS_INLINE {
         Piece e;
         read_piece(e, i);
 #pragma unroll
@@ -153,13 +158,13 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
         if (careful) keep_whole(e.z, e.x, e.y);
         write_piece(e, tile, i);
     };
-    const auto taken_apart = [&](int tile, float odd) {
+    const auto taken_apart = [&](int tile, float odd) ALWAYS_INLINE {
         if (odd == odd) return;
 #pragma unroll 1
         for (int i = 0; i < kBlocks; ++i) take_apart(tile, i, odd, true);
         not_finite[tile & 1] = tile;
     };
-    const auto take_all_apart = [&](int tile) {
+    const auto take_all_apart = [&](int tile) ALWAYS_INLINE {
         float odd = 0.f;
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) take_apart(tile, i, odd, false);
@@ -178,7 +183,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
     float top = -INFINITY, sum = 0.f;
 
     // Takes a tile's scores into the running softmax: s become the weights.
-    const auto weigh = [&](auto masked, f32x16a& s, int far, int near, int sink) {
+    const auto weigh = [&](auto masked, f32x16a& s, int far, int near, int sink) ALWAYS_INLINE {
         if (decltype(masked)::value)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -204,14 +209,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
         }
     };
     // Between the products of scores the next tile, where there is one, is taken apart.
-    const auto take = [&](auto masked, int tile, bool more, int far, int near, int sink) {
+    const auto take = [&](auto masked, int tile, bool more, int far, int near, int sink) ALWAYS_INLINE {
         const char *Kt = Ks[tile & 1], *Vt = Vs[tile & 1];
         f32x16a s, small;
         float odd = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f, small[i] = 0.f;
         Parts k[2];
-        const auto load_keys = [&](int i) {
+        const auto load_keys = [&](int i) ALWAYS_INLINE {
             const char* at = Kt + k_at[i & 1] + (i >> 1) * (kKeys * 64);
             k[i & 1].h = *(const u32x4a*)at;
             k[i & 1].m = *(const u32x4a*)(at + kPart);
@@ -248,7 +253,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
             if (tile + 2 < tiles) fetch(tile + 2);
         }
         Parts v[2][2];
-        const auto load_values = [&](int j) {                            // of 16 keys j / 2, channels 64 (j % 2) + 0..63
+        const auto load_values = [&](int j) ALWAYS_INLINE {                            // of 16 keys j / 2, channels 64 (j % 2) + 0..63
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
                 const char* at = Vt + v_at + ((j & 1) * 2 + d) * (kKeys * 64) + (j >> 1) * 1024;
@@ -265,7 +270,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
         weigh(masked, s, far, near, sink);
         float unused = 0.f;
         Parts w[2];
-        const auto weights = [&](int u) {
+        const auto weights = [&](int u) ALWAYS_INLINE {
             w[u] = apart((f32x4a){s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3]}, (f32x4a){s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]}, unused);
         };
         weights(0);
@@ -291,7 +296,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    const auto take_whole_numbers = [&](int tile, int far, int near, int sink) {
+    const auto take_whole_numbers = [&](int tile, int far, int near, int sink) ALWAYS_INLINE {
         const char *Kt = Ks[tile & 1], *Vt = Vs[tile & 1];
         f32x16a s;
 #pragma unroll

@@ -18,6 +18,7 @@
 // A wave's next tile is asked for without a branch: in front of one the compiler waits for all that is in flight.
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "attend_device.h"
@@ -38,7 +39,9 @@ struct SplitArgs {
     float scale_log2;
     int items, rows, row_tiles;        // heads times tiles of their rows R; m * group; tiles of them
     int shares;                        // workgroups that share all items; every item is one's of its own where that is 0
-    bool whole;                        // none of them has parts of two items
+    bool whole;                        // every item has workgroups of its own, as long as the shares are few tiles
+    int least;                         // tiles of an item, on average, from which it pays to share it (3/8 of them in workgroups of its own)
+    float weight;                      // parts of an item squared over its tiles, where reading and joining are in balance
     int* arrived;                      // [items]: workgroups that are done with their part of an item; 0 between the calls
     float* part_o;                     // [shares + 2 items][16][128]: of workgroup w and item i at w + i, which no other pair has
     f32x2a* part_ml;                   // the same of maxima and sums
@@ -536,6 +539,7 @@ __device__ __forceinline__ int ceil_div(int x, int y) { return (x + y - 1) / y; 
 // A workgroup's place in the list of all items.
 struct Place {
     int item, into, size;              // units of the item in front of the share; of the share (0: nothing to do)
+    int end;                           // the share has no part of this item and those after it
     int first, last;                   // workgroups that have a part of the item
     Head head;                         // of the item
 };
@@ -560,38 +564,45 @@ __device__ __forceinline__ Head head_from(const Head& h, int lane) {
     r.length = __builtin_amdgcn_readlane(h.length, lane);
     return r;
 }
+// Each item its own workgroups: shares of all items that are equal count for more where few share one for long.
+__host__ __device__ __forceinline__ bool few_enough(int items, int64_t shares, int64_t tiles) { return 8 * items <= shares || tiles <= 64 * shares; }
 template <int FA, int FB>
 struct Places {
     static constexpr int kBetween = FA == kMxBf16 || FA == kMxF32 ? 32 : 16, kAtOnce = 4;
     const SplitArgs& a;
     int all, shares, at;               // units of all items; workgroups with a share; units in front of the item at hand, without its kBetween
+    bool whole;                        // workgroups have parts of one item each
     __device__ __forceinline__ int begin_of(int share) const { return (int)((int64_t)all * share / shares); }
     __device__ __forceinline__ int share_of(int unit) const { return (int)((((int64_t)unit + 1) * shares - 1) / all); }     // whose share holds a unit
     __device__ __forceinline__ void owners(Place& p, int units) const {
-        if (a.whole) return;
+        if (whole) return;
         p.first = share_of(at + kBetween);
         p.last = share_of(at + kBetween + units - 1);
     }
     __device__ __forceinline__ Place find() {
         const int lane = threadIdx.x & 63, each = (a.items + 63) / 64, from = min(lane * each, a.items), end = min(from + each, a.items), block = blockIdx.x;
-        Place p{0, 0, 0, 0, 0, {0, 0, 0}};
+        Place p{0, 0, 0, a.items, 0, 0, {0, 0, 0}};
         int owner;
         if (a.whole) {                 // (each == 1)
             const Head head = head_of(a, min(from, a.items - 1) / a.row_tiles);
-            const int mine = lane < a.items ? Work<FA, FB>(a, from, head).units : 0;
-            all = __builtin_amdgcn_readlane(added_up(mine), 63);
-            const int parts = lane < a.items ? min(mine, max(1, (int)((int64_t)mine * a.shares / all))) : 0, parts_up_to = added_up(parts);
-            const uint64_t beyond = __ballot(block < parts_up_to);
-            if (!beyond) return p;
-            owner = __builtin_ctzll(beyond);
-            const int n = __builtin_amdgcn_readlane(parts, owner), units = __builtin_amdgcn_readlane(mine, owner);
-            p.first = __builtin_amdgcn_readlane(parts_up_to, owner) - n;
-            p.last = p.first + n - 1;
-            p.into = (int)((int64_t)units * (block - p.first) / n);
-            p.size = (int)((int64_t)units * (block - p.first + 1) / n) - p.into;
-            p.item = owner;
-            p.head = head_from(head, owner);
-            return p;
+            const int mine = lane < a.items ? Work<FA, FB>(a, from, head).units : 0, tiles = __builtin_amdgcn_readlane(added_up(mine), 63);
+            whole = few_enough(a.items, a.shares, tiles);
+            if (whole) {
+                // (the host knows the largest lengths that there may be; here are those that there are: 8 sequences of 250 tokens in caches of 16384 18 us by the caches' size, so 9)
+                const int some = min(a.shares, max(a.items, (int)__builtin_sqrtf(a.weight * (float)a.items * (float)tiles)));
+                const int parts = lane >= a.items ? 0 : tiles < a.least * 3 / 8 * a.items ? 1 : min(mine, max(1, (int)((int64_t)mine * some / tiles))), parts_up_to = added_up(parts);
+                const uint64_t beyond = __ballot(block < parts_up_to);
+                if (!beyond) return p;
+                owner = __builtin_ctzll(beyond);
+                const int n = __builtin_amdgcn_readlane(parts, owner), units = __builtin_amdgcn_readlane(mine, owner);
+                p.first = __builtin_amdgcn_readlane(parts_up_to, owner) - n;
+                p.last = p.first + n - 1;
+                p.into = (int)((int64_t)units * (block - p.first) / n);
+                p.size = (int)((int64_t)units * (block - p.first + 1) / n) - p.into;
+                p.item = owner;
+                p.head = head_from(head, owner);
+                return p;
+            }
         }
         // (the loads of four items at a time)
         Head head[kAtOnce];
@@ -607,6 +618,14 @@ struct Places {
         }
         const int up_to = added_up(mine);
         all = __builtin_amdgcn_readlane(up_to, 63);
+        const int tiles = all - a.items * kBetween;
+        if (tiles < a.least * a.items) {                               // little to read, in fact: items as they are
+            const int places = min(a.items, a.shares);
+            p.item = (int)((int64_t)a.items * block / places);
+            p.end = (int)((int64_t)a.items * (block + 1) / places);
+            if (block < places) p.head = head_of(a, p.item / a.row_tiles), p.size = INT_MAX;
+            return p;
+        }
         // (no more shares than tiles: none may be without any between two that have parts of one item)
         shares = max(1, min(a.shares, (all - a.items * kBetween) / (kBetween + 1)));
         const int begin = begin_of(block);
@@ -756,8 +775,8 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(Split
     const AttendCall& c = a.c;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
     constexpr int kBytes = FB == kBf16 ? 2 : 4;
-    Places<FA, FB> places{a, 0, 0, 0};
-    Place place{(int)blockIdx.x, 0, 0, 0, 0, {0, 0, 0}};
+    Places<FA, FB> places{a, 0, 0, 0, false};
+    Place place{(int)blockIdx.x, 0, 0, a.items, 0, 0, {0, 0, 0}};
     if (a.shares > 0) {
         place = places.find();
         if (place.size <= 0) return;
@@ -766,7 +785,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(Split
     }
     for (int item = place.item;; ++item) {
         const Work<FA, FB> work(a, item, place.head);
-        const int lo = a.shares > 0 ? place.into : 0, hi = a.shares > 0 ? min(work.units, lo + place.size) : work.units;
+        const int lo = a.shares > 0 ? place.into : 0, hi = a.shares > 0 ? lo + min(work.units - lo, place.size) : work.units;
         const int g = item / a.row_tiles, row_tile = item - g * a.row_tiles, b = g / c.kv, head = g % c.kv;
 
         // this lane's query row (rows beyond the last repeat it; nothing of them is written)
@@ -857,7 +876,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(Split
         places.at += work.units + places.kBetween;
         place.size -= hi - lo + places.kBetween;
         place.into = 0;
-        if (place.size <= 0 || item + 1 >= a.items) break;
+        if (place.size <= 0 || item + 1 >= place.end) break;
         place.head = head_of(a, (item + 1) / a.row_tiles);
         __syncthreads();                                   // (part, tops and sums are read)
     }
@@ -906,17 +925,19 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     // where they have long to go (320 us, so 295; 32 tiles a unit: 18, 20).  A tile a wave at least, and no more parts of an item than pay: its tiles over the parts are read
     // in a time of their own, its parts are counted and joined in theirs, and the two together are least where parts^2 is about the tiles, or twice them in fp32 (one token of 8
     // heads over 4000 rows 14.7 us with as many as there are units, so 13.1; in 4 bits 18.2, so 13.1; of one head over 16000 48.5, so 17.1).
-    const int64_t most = (int64_t)std::sqrt((f32 ? 2.0 : 1.0) * a.items * tiles);
+    a.weight = f32 ? 2.f : 1.f;
+    const int64_t most = (int64_t)std::sqrt((double)a.weight * a.items * tiles);
     const int64_t wanted = std::min(units * (mx && tiles >= 1024 * units ? 2 : 1), std::max((int64_t)a.items, std::min(most, (tiles + kSplitWaves - 1) / kSplitWaves)));
     int64_t shares = std::min(wanted, room - 2 * a.items);
     // Few items: each its own workgroups, which have less to look up and to join (64 heads of up to 2000 rows 18.1 us, so 15.6, of 4 bits 21.5, so 14.7); where few share one
     // for long, equal shares of all of them count for more (64 heads of 16000 in 4 bits 41, so 49).
-    a.whole = a.items <= 64 && 2 * a.items <= shares && (8 * a.items <= shares || tiles <= 64 * shares);
+    a.whole = a.items <= 64 && 2 * a.items <= shares;
     // To share costs a join: 3 us, 10 where a workgroup may have parts of several items.  Not shared and shared, us: 8 heads of 500 rows 8.6 and 10.1, of
     // 1000 12.9 and 11.2; 64 of up to 500 8.8 and 11.1, of 1000 13.3 and 12.7; 256 of 500 10 and 20, of 2000 32 and 36, of 8000 102 and 91; 1024 of 1000 57 and
     // 65, of 2000 109 and 100.  fp32's tiles take twice as long: 8 of 250 11.6 and 12.3, of 400 14.9 and 13.2; 128 of 1000 28 and 27.  Kept rows differ more from head to
     // head: 8 of about 250 11.3 and 10.9, 400 in 4 bits 10.5 and 11.1, 600 12.8 and 11.0; 256 of 500 27.9 and 26.4, of 1000 61 and 40, in 4 bits 26.6 and 24.3.
-    const int64_t least = (a.whole ? 48 : 128) / (f32 ? 2 : 1) / (call.offsets ? 4 : 1);
+    a.least = 128 / (f32 ? 2 : 1) / (call.offsets ? 4 : 1);
+    const int64_t least = a.whole && few_enough(a.items, shares, tiles) ? a.least * 3 / 8 : a.least;
     // Equal ones in whole turns of all units are shared out already: 256 heads of 4000 rows 81 and 87, through windows of 4096 69 and 74 (264 heads: 106 and 77).
     const bool equal = !call.offsets && (!call.lengths || (call.window > 0 && 2 * (int64_t)call.window <= call.n)) && a.items % units == 0;
     if (tiles < least * a.items || equal || a.items > kCounters || (shares < wanted && shares < a.items)) shares = 0;

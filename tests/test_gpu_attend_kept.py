@@ -28,8 +28,9 @@ def pack(ctx_dtype, rows):
     return codes, scales, value.cuda()
 
 
-def check(dtype, mx, count, kv, group, m, budgets, tail_n, tails, seed=0, before=0, spoil=None, stream=None, tail_stride=None):
-    """budgets: kept rows of every head; before: rows of other layers in front of them in the packed arrays."""
+def check(dtype, mx, count, kv, group, m, budgets, tail_n, tails, seed=0, before=0, spoil=None, stream=None, tail_stride=None, rows_known=True):
+    """budgets: kept rows of every head; before: rows of other layers in front of them in the packed arrays; rows_known: the call is told how many are its
+    heads'."""
     dt, budgets = U.dtype_of(dtype), np.asarray(budgets)
     off = before + np.concatenate([[0], np.cumsum(budgets)]).astype(np.int64)
     total = int(off[-1])
@@ -45,7 +46,7 @@ def check(dtype, mx, count, kv, group, m, budgets, tail_n, tails, seed=0, before
     offsets = torch.from_numpy(off).cuda()
     out = Guarded((count * m * kv * group, D), dt, float("nan"))
     lse = Guarded((count * kv * group, m), torch.float32, float("nan"))
-    since = dict(K_tail=Kt, V_tail=Vt, tail_n=tail_n, tail_stride=tail_stride, lse=lse.t, stream=stream, rows=int(budgets.sum()),
+    since = dict(K_tail=Kt, V_tail=Vt, tail_n=tail_n, tail_stride=tail_stride, lse=lse.t, stream=stream, rows=int(budgets.sum()) if rows_known else None,
                  tail_lengths=None if tails is None else torch.from_numpy(lens.astype(np.int32)).cuda())
     with U.context(kv, group, dtype, max(tail_n, m, 1)) as ctx:
         if mx:

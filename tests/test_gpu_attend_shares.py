@@ -81,3 +81,22 @@ def test_a_first_call_is_not_recorded():
         ctx.attend(Q, K, V, 1, 1, 100, 100, out)
         torch.cuda.synchronize()
         assert torch.equal(recorded, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count,n,longest", [(1, 16000, 40), (1, 16000, 700), (4, 16000, 3000), (30, 6000, 90), (30, 6000, 2000), (40, 5000, 60), (40, 5000, 1500), (200, 4200, 50), (200, 4200, 0)])
+def test_lengths_far_below_what_there_may_be(dtype, count, n, longest):
+    # the host shares out by the cache's size, the device by the lengths that there are
+    rng = np.random.default_rng(n + longest)
+    lengths = rng.integers(0, longest + 1, count)
+    lengths[-1] = longest
+    U.check_attend(dict(count=count, kv=2, group=2, m=1, n=n, dtype=dtype), seed=longest, lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMS)
+@pytest.mark.parametrize("heads", [3, 40, 130])
+def test_a_layer_with_little_of_a_large_packed_cache(dtype, mx, heads):
+    # rows not given: the host takes all rows for this layer's
+    rng = np.random.default_rng(heads)
+    budgets = rng.integers(0, 90, heads * 2)
+    check(dtype, mx, heads, 2, 2, 1, budgets, 5, rng.integers(0, 6, heads), seed=heads, before=200000 if heads > 3 else 30000, rows_known=False)

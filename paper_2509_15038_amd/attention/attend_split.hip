@@ -583,9 +583,12 @@ struct Places {
         const int lane = threadIdx.x & 63, each = (a.items + 63) / 64, from = min(lane * each, a.items), end = min(from + each, a.items), block = blockIdx.x;
         Place p{0, 0, 0, a.items, 0, 0, {0, 0, 0}};
         int owner;
+        Head head[kAtOnce];
+        int units[kAtOnce], mine = 0;
         if (a.whole) {                 // (each == 1)
-            const Head head = head_of(a, min(from, a.items - 1) / a.row_tiles);
-            const int mine = lane < a.items ? Work<FA, FB>(a, from, head).units : 0, tiles = __builtin_amdgcn_readlane(added_up(mine), 63);
+            head[0] = head_of(a, min(from, a.items - 1) / a.row_tiles);
+            mine = lane < a.items ? Work<FA, FB>(a, from, head[0]).units : 0;
+            const int tiles = __builtin_amdgcn_readlane(added_up(mine), 63);
             whole = few_enough(a.items, a.shares, tiles);
             if (whole) {
                 // (the host knows the largest lengths that there may be; here are those that there are: 8 sequences of 250 tokens in caches of 16384 18 us by the caches' size, so 9)
@@ -600,14 +603,16 @@ struct Places {
                 p.into = (int)((int64_t)units * (block - p.first) / n);
                 p.size = (int)((int64_t)units * (block - p.first + 1) / n) - p.into;
                 p.item = owner;
-                p.head = head_from(head, owner);
+                p.head = head_from(head[0], owner);
                 return p;
             }
+            if (lane < a.items) mine += kBetween;
+            units[0] = mine;
+#pragma unroll
+            for (int k = 1; k < kAtOnce; ++k) units[k] = 0, head[k] = head[0];
         }
         // (the loads of four items at a time)
-        Head head[kAtOnce];
-        int units[kAtOnce], mine = 0;
-        for (int i = from; i < end; i += kAtOnce) {
+        for (int i = a.whole ? end : from; i < end; i += kAtOnce) {
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) head[k] = head_of(a, min(i + k, a.items - 1) / a.row_tiles);
 #pragma unroll

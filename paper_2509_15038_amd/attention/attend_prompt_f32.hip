@@ -2,7 +2,7 @@
 // what is left rounded to bf16, l the rest, which bf16 holds).  Of the nine products of parts the six that count, h h, h m, m h, h l, m m and l h, go through
 // mfma_f32_32x32x16_bf16, summed in 32 bits: what is left out is below 2^-22 of a product, and a sixth of the bf16 rate is 2.7 times the
 // rate of mfma_f32_32x32x2, whose kernel took 4770 us for a prompt of 8000 tokens (8 heads of 4; 524 Gflop), this 2586: 203 Tflop/s, 1220 of bf16, which is
-// where the library's products of such numbers end as well.  Bound by the matrix units, 3072 clocks for 32 keys and 32 rows of a wave, and short of workgroups below some
+// where the library's products of such numbers end as well.  Bound by the matrix units, 96 products of 32 clocks for 32 keys and 32 rows of a wave, and short of workgroups below some
 // 2000 tokens (1000: 110 us).
 //
 // Tiles of 32 keys come to LDS as they are, 1 KB blocks of two rows by the wave that then takes them apart and writes the parts, between the products of

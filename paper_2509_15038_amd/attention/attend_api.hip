@@ -40,9 +40,12 @@ int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
     // up to 64 12 and 9.  One tile of 16 a head: 32 sequences of 4 tokens over 8000 100 and 164.
     // fp32: prompts of 8 heads 600 tokens 65 and 69, 800 93 and 89, 2400 572 and 344; 64 tokens of 4 sequences over 500 rows 32 and 61, of 16 116 and 65.
     const int64_t rows = (int64_t)call.m * call.group, heads = call.count * call.kv, items = heads * ((rows + 15) / 16), tiles = heads * ((rows + 127) / 128);
-    const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
+    const int64_t keys = (call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n) + call.rows / heads;
     const bool f32 = call.dtype == CURDKV_DTYPE_F32;
-    const bool prompt = !call.offsets && (f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 16 && (items > kPromptItems || items * keys > kPromptProducts));
+    // Kept rows in bf16: workgroups do not share out heads of uneven lengths there, which costs more the fewer rows a tile of 128 has: 64 tokens over 3276 rows of 8 uneven heads 41 and
+    // 44, 200 92 and 61, 1000 301 and 195 (even heads 4 sequences of 300 103, uneven ones 281); 32 sequences of 6 over 3000 135 and 302.
+    const bool prompt = call.offsets ? !call.K_scales && !f32 && rows >= 256 && (items > kPromptItems || items * keys > 2 * kPromptProducts)
+                        : f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 16 && (items > kPromptItems || items * keys > kPromptProducts);
     const auto launch = !prompt ? launch_attend_split : f32 ? launch_attend_prompt_f32 : launch_attend_prompt;
     return launch(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }

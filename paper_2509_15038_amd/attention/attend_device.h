@@ -8,6 +8,9 @@
 
 #include "curdkv_internal.h"
 
+// (a lambda of a kernel's that is not inlined would leave what it refers to in memory)
+#define ALWAYS_INLINE __attribute__((always_inline))
+
 namespace curdkv {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -68,6 +71,10 @@ __device__ __forceinline__ float halves_sum(float x) {
 // 64 lanes' 16 bytes from base + at to LDS from `to` on, in order of the lanes.  Nothing waits for it but dma_wait().
 __device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
+}
+// A value that is the same in all lanes, where the compiler does not see it.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
 }
 __device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }

@@ -32,7 +32,7 @@ struct AttendCall {
 };
 
 hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);
-hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);     // bf16, no kept rows
+hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);     // bf16; kept rows not in 4 bits
 hipError_t launch_attend_prompt_f32(const curdkv_ctx* ctx, const AttendCall& call, hipStream_t stream);
 
 hipError_t launch_rotate(const curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride, const int32_t* starts,

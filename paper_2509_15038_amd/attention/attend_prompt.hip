@@ -48,6 +48,8 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t x, uint32_t y) {      //
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2a, x), __builtin_bit_cast(u16x2a, y)));
 }
 
+// KEPT: kept rows, which all tokens see, are the first tiles (there is no window then); the cache is the tokens since.
+template <bool KEPT>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArgs a) {
     constexpr int kStage = 16 / kWaves;
     __shared__ __attribute__((aligned(16))) char Ks[2][kKeys * 256], Vs[2][kKeys * 256];
@@ -62,10 +64,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
 
     const int t_first = row_tile * kTileRows / c.group, t_last = min(c.m - 1, (row_tile * kTileRows + kTileRows - 1) / c.group);
     const Seen seen = seen_rows(length, c.m, t_first, t_last, c.window, c.sinks);
-    const int first_tiles = (seen.first + kKeys - 1) / kKeys, tiles = first_tiles + (seen.high - seen.low + kKeys - 1) / kKeys;
+    int64_t kept_begin = 0;
+    int first = seen.first;
+    if (KEPT) {
+        const int64_t begin = min(max(c.offsets[g], (int64_t)0), c.total);
+        first = __builtin_amdgcn_readfirstlane((int)(min(max(c.offsets[g + 1], begin), c.total) - begin));
+        kept_begin = uniform(begin);
+    }
+    const int first_tiles = (first + kKeys - 1) / kKeys, tiles = first_tiles + (seen.high - seen.low + kKeys - 1) / kKeys;
     const int start = (int)((int64_t)tiles * part / a.parts), stop = (int)((int64_t)tiles * (part + 1) / a.parts);
-    const auto row_of = [&](int tile) { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
-    const auto count_of = [&](int tile) { return min(kKeys, (tile < first_tiles ? seen.first : seen.high) - row_of(tile)); };
+    const auto row_of = [&](int tile) ALWAYS_INLINE { return tile < first_tiles ? tile * kKeys : seen.low + (tile - first_tiles) * kKeys; };
+    const auto count_of = [&](int tile) ALWAYS_INLINE { return min(kKeys, (tile < first_tiles ? first : seen.high) - row_of(tile)); };
 
     // this lane's rows
     const int R0 = row_tile * kTileRows + wave * 32;
@@ -80,18 +89,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
     // A tile's 1 KB blocks of 16 rows' columns: this wave's share.
     const uint32_t k_lds = lds_address(&Ks[0][0]), v_lds = lds_address(&Vs[0][0]);
     const int d_row = lane >> 2, d_piece = lane & 3;
-    const auto fetch = [&](uint32_t lds, const char* rows, int tile, bool keys) {
-        const int64_t j0 = row_of(tile);
+    const auto fetch = [&](uint32_t lds, const char* rows, const void* kept, int tile, bool keys) ALWAYS_INLINE {
+        const char* from = rows + (int64_t)row_of(tile) * 256;
+        uint32_t to = lds + (tile & 1) * (kKeys * 256) + wave * (kStage * 1024);
+        if (KEPT) {
+            if (tile < first_tiles) from = (const char*)kept + (kept_begin + tile * kKeys) * 256;
+            from = (const char*)uniform((int64_t)from);
+            to = __builtin_amdgcn_readfirstlane(to);
+        }
         const int count = count_of(tile);
 #pragma unroll
         for (int i = 0; i < kStage; ++i) {
             const int block = wave * kStage + i, column = block >> 2, row0 = (block & 3) * 16;
             const uint32_t row = min(row0 + d_row, count - 1) * 256 + column * 64, piece = keys ? d_piece ^ ((d_row >> 1) & 3) : d_piece;
-            dma16(lds + (tile & 1) * (kKeys * 256) + block * 1024, rows + j0 * 256, row + (piece << 4));
+            dma16(to + i * 1024, from, row + (piece << 4));
         }
     };
-    const auto fetch_k = [&](int tile) { fetch(k_lds, Kg, tile, true); };
-    const auto fetch_v = [&](int tile) { fetch(v_lds, Vg, tile, false); };
+    const auto fetch_k = [&](int tile) ALWAYS_INLINE { fetch(k_lds, Kg, c.K_kept, tile, true); };
+    const auto fetch_v = [&](int tile) ALWAYS_INLINE { fetch(v_lds, Vg, c.V_kept, tile, false); };
 
     // this lane's operands within a tile: K row col, piece 2 x + half; V rows 4 half + lane16 / 4 (+ 8), channels 32 db + ..
     const int l16 = lane & 15, dhalf = (lane >> 4) & 1;
@@ -104,10 +119,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-    const auto product = [](u32x4a x, u32x4a y, f32x16a z) {
+    const auto product = [](u32x4a x, u32x4a y, f32x16a z) ALWAYS_INLINE {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, y), z, 0, 0, 0);
     };
-    const auto scores = [&](int tile, f32x16a (&x)[2]) {
+    const auto scores = [&](int tile, f32x16a (&x)[2]) ALWAYS_INLINE {
         const char* Kt = Ks[tile & 1];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -125,11 +140,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
         int far, near, sink;
         __device__ __forceinline__ bool has(int key) const { return key <= far && (key > near || key < sink); }
     };
-    const auto range_of = [&](int tile) {
+    const auto range_of = [&](int tile) ALWAYS_INLINE {
+        if (KEPT && tile < first_tiles) return Range{count_of(tile) - 1 - half * 4, -5, 0};
         const int j0 = row_of(tile);
         return Range{min(p - j0, count_of(tile) - 1) - half * 4, (c.window > 0 ? p - j0 - c.window : -1) - half * 4, c.sinks - j0 - half * 4};
     };
-    const auto top_of = [&](const f32x16a (&x)[2]) {
+    const auto top_of = [&](const f32x16a (&x)[2]) ALWAYS_INLINE {
         float y = x[0][0];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -137,7 +153,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
             for (int i = 0; i < 16; ++i) y = fmaxf(y, x[kb][i]);
         return halves_max(y) * a.scale_log2;
     };
-    const auto raise = [&]() {
+    const auto raise = [&]() ALWAYS_INLINE {
         if (__any(top > ref + kLoose)) {
             const float next = top > ref + kLoose ? top : ref;
             const float keep = next == ref ? 1.f : __builtin_amdgcn_exp2f(ref - next);
@@ -148,7 +164,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
         }
     };
     // A tile that may hold rows that some token does not see.
-    const auto masked_step = [&](int tile) {
+    const auto masked_step = [&](int tile) ALWAYS_INLINE {
         f32x16a s[2];
         scores(tile, s);
         // Whether the tile of V holds an infinity or NaN: every wave looks at its share of it.
@@ -228,7 +244,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
     // Tiles begin .. end - 1, of which every token sees all: the next tile's 16 products with this one's exponentials between them, in the order
     // written (a matrix product every 7 other instructions keeps both pipes busy, and no more operands wait in registers than the next two products
     // need), then this one's 16 products with the next one's maximum.  `end` is a tile too (its scores are made, and dropped).
-    const auto whole_steps = [&](int begin, int end) {
+    const auto whole_steps = [&](int begin, int end) ALWAYS_INLINE {
         f32x16a s[2];
         scores(begin, s);
         top = top_of(s);
@@ -266,7 +282,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
                 __builtin_amdgcn_sched_barrier(0);
             }
             u32x2 v[2][4][2];
-            const auto values = [&](int u) {
+            const auto values = [&](int u) ALWAYS_INLINE {
 #pragma unroll
                 for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -306,6 +322,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
         const int hidden = c.window > 0 ? max(0, seen.p1 - c.window + 1 - seen.low) : 0;         // rows from `low` on that the last token does not see
         const int whole_begin = max(min(first_tiles + (hidden + kKeys - 1) / kKeys, whole_end), start);
         int tile = start;
+        if (KEPT && tile < min(first / kKeys, stop - 1)) {
+            whole_steps(tile, min(first / kKeys, stop - 1));
+            tile = min(first / kKeys, stop - 1);
+        }
         for (int turn = 0; turn < 2; ++turn) {             // masked tiles, whole ones, masked ones
             const int end = turn == 0 ? whole_begin : stop;
             for (; tile < end; ++tile) masked_step(tile);
@@ -381,13 +401,14 @@ hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, h
     a.rows = call.m * call.group;
     a.row_tiles = (a.rows + kTileRows - 1) / kTileRows;
     // Few new tokens over a long cache: the tiles of keys shared out until every unit has two workgroups, 8 tiles each at least, as far as there is scratch.
-    const int64_t blocks = (int64_t)a.groups * a.row_tiles, tiles = (call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n) / kKeys;
+    const int64_t blocks = (int64_t)a.groups * a.row_tiles, tiles = ((call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n) + call.rows / a.groups) / kKeys;
     const int64_t part_bytes = blocks * kTileRows * (int64_t)(128 * sizeof(float) + sizeof(f32x2a)), room = call.scratch ? call.scratch_bytes - kScratchCounters : 0;
     int64_t parts = std::min(std::min(2 * ctx->num_cu / blocks, tiles / 8), room / part_bytes);
     a.parts = parts > 1 ? (int)parts : 1;
     a.part_o = (float*)((char*)call.scratch + kScratchCounters);
     a.part_ml = (f32x2a*)(a.part_o + a.parts * blocks * kTileRows * 128);
-    attend_prompt_kernel<<<(unsigned)(blocks * a.parts), kWaves * 64, 0, stream>>>(a);
+    if (call.offsets) attend_prompt_kernel<true><<<(unsigned)(blocks * a.parts), kWaves * 64, 0, stream>>>(a);
+    else attend_prompt_kernel<false><<<(unsigned)(blocks * a.parts), kWaves * 64, 0, stream>>>(a);
     if (a.parts > 1) attend_prompt_join_kernel<<<(unsigned)(((int64_t)a.groups * a.rows + 3) / 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }

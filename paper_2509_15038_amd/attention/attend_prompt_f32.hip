@@ -79,9 +79,6 @@ __device__ __forceinline__ u32x2 read_transposed(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4a*)p));
 }
 
-// (a lambda that is not inlined would leave what it refers to in memory)
-#define ALWAYS_INLINE __attribute__((always_inline))
-
 template <int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kernel(PromptF32Args a) {
     constexpr int kTileRows = WAVES * 32, kBlocks = 16 / WAVES, kEvery = 3 * WAVES / 4;

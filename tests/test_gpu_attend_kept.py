@@ -231,3 +231,33 @@ def test_more_new_tokens_than_any_cache_holds(mx):
     for h in range(4):
         want = U.attention(Q[0, :, h], torch.cat([k.double(), Kt.double()]), torch.cat([v.double(), Vt.double()]), seen, D ** -0.5)
         U.check_attention(out[0, :, h], None, want, "bf16", 71)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMS)
+@pytest.mark.parametrize("count,kv,m,budgets,tail,tails", [
+    (2, 2, 300, [64, 128, 1000, 0], 300, None), (2, 2, 333, [1, 63, 65, 700], 400, [400, 90]), (1, 2, 70, [6000, 3001], 70, None), (1, 1, 500, [0], 500, None),
+    (1, 2, 200, [640, 6400], 0, None), (3, 2, 130, [130, 64, 0, 31, 2000, 192], 131, [131, 0, 130]), (1, 8, 1000, [300, 64, 5, 1, 0, 700, 128, 60], 1000, None)])
+def test_prompts_over_kept_rows(dtype, mx, count, kv, m, budgets, tail, tails):
+    check(dtype, mx, count, kv, 4, m, budgets, tail, tails, seed=m)
+
+
+@pytest.mark.parametrize("row", [3, 63, 64, 127, 129])
+def test_a_prompt_over_kept_rows_that_are_not_finite(row):
+    # everybody sees kept rows: an infinity of a value reaches every result of its channel, in whole tiles and the last one, and no other channel
+    m, kept = 300, 130
+    K, V, Q = (U.randn(i, (kept, D) if i < 3 else (1, m, 4, D), torch.bfloat16) for i in (1, 2, 3))
+    V[row, 17], V[row, 90] = math.inf, math.nan
+    Kt, Vt = U.randn(4, (1, 1, m, D), torch.bfloat16), U.randn(5, (1, 1, m, D), torch.bfloat16)
+    Kt[0, 0, -1], Vt[0, 0, -1] = math.nan, math.inf                                     # the last token's own row, hidden from the others
+    out = torch.empty_like(Q)
+    with U.context(1, 4, "bf16", m) as ctx:
+        ctx.attend_kept(Q, K, V, torch.tensor([0, kept], device="cuda"), 1, m, kept, out, K_tail=Kt, V_tail=Vt, tail_n=m, tail_stride=m)
+        torch.cuda.synchronize()
+    seen = torch.cat([torch.ones((m, kept), dtype=torch.bool, device="cuda"), U.causal(m, m, m, 0, 0)], 1)[:-1]
+    clean = torch.where(torch.isfinite(V), V, 0.0)
+    for h in range(4):
+        got = out[0, :-1, h].double()
+        assert bool((got[:, 17] == math.inf).all()) and bool(torch.isnan(got[:, 90]).all())
+        want = U.attention(Q[0, :-1, h], torch.cat([K, Kt[0, 0]])[:, :], torch.cat([clean, Vt[0, 0]]), seen, D ** -0.5)
+        got[:, 17], got[:, 90] = want[0][:, 17], want[0][:, 90]
+        U.check_attention(got, None, want, "bf16", kept + m)

@@ -291,8 +291,9 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  * position p = length - m + i and sees row j where j <= p and (window == 0 or p - j < window
  * or j < n_sink);
  *   out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log sum_j exp(scale * q.k_j).
- * A token that sees nothing (length < m and i < m - length) gets zeros and -infinity; what a
- * token does not see does not reach it, infinities and NaN included.
+ * A token that sees nothing (length < m and i < m - length), or only keys whose scores are
+ * -infinity, gets zeros and -infinity; a key of such a score weighs nothing.  What a token does
+ * not see does not reach it, infinities and NaN included.
  * lengths: int32 [count], clamped to [0, n]; NULL = n for all.  n <= stride, n <= max_tokens.
  * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0; m <= max_tokens.
  * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits,

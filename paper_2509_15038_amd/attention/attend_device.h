@@ -2,6 +2,7 @@
 // rows R = token * group + head of the products' other side; token t of m stands at position p(t) = length - m + t.
 #pragma once
 
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -22,6 +23,9 @@ typedef __bf16 bf16x2a __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8a __attribute__((ext_vector_type(8)));
 
 constexpr float kLn2 = 0.693147180559945309f;
+// The reference of a row that has met no score yet, or none but -infinity (a hidden key's, or an infinite key's): exp2(-infinity - kNoScore) is the weight 0 that such
+// a key has, where -infinity in its place would make NaN of the difference.
+constexpr float kNoScore = -FLT_MAX;
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2a{a, b}), bf16x2a));

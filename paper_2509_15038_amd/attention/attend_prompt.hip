@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
     const int v_at = (4 * half + l16 / 4) * 64 + dhalf * 32 + (l16 & 3) * 8;
 
     f32x16a o[4];
-    float ref = -INFINITY, sum = 0.f, top;
+    float ref = kNoScore, sum = 0.f, top;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -188,11 +188,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
         top = top_of(s);
         raise();
         uint32_t pb[16];
-        const float off = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], a.scale_log2, -off));
-            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][(i & 15) + 1], a.scale_log2, -off));
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], a.scale_log2, -ref));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][(i & 15) + 1], a.scale_log2, -ref));
             sum += x + y;
             pb[i / 2] = pack_bf16(x, y);
         }
@@ -351,7 +350,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
         if (half == 0) a.part_ml[at] = (f32x2a){ref, total};
         return;
     }
-    const bool empty = ref == -INFINITY;
+    const bool empty = ref == kNoScore;
     const float over = empty ? 0.f : 1.f / total;
     char* out = (char*)c.out + query_row * 256;
 #pragma unroll
@@ -373,14 +372,14 @@ __global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a) {
     const int lane = threadIdx.x & 63, g = (int)(at / a.rows), R = (int)(at - (int64_t)g * a.rows);
     if (g >= a.groups) return;
     const int64_t first = (int64_t)g * a.row_tiles * kTileRows + R, step = (int64_t)a.groups * a.row_tiles * kTileRows;
-    float ref = -INFINITY, sum = 0.f;
+    float ref = kNoScore, sum = 0.f;
     for (int k = 0; k < a.parts; ++k) ref = fmaxf(ref, a.part_ml[first + k * step].x);
-    const bool empty = ref == -INFINITY;
+    const bool empty = ref == kNoScore;
     f32x2a o = {0, 0};
 #pragma unroll 4
     for (int k = 0; k < a.parts; ++k) {
         const f32x2a ml = a.part_ml[first + k * step], x = *(const f32x2a*)(a.part_o + (first + k * step) * 128 + lane * 2);
-        const float weight = empty ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
+        const float weight = __builtin_amdgcn_exp2f(ml.x - ref);
         sum += weight * ml.y;
         o.x += weight * x.x;
         o.y += weight * x.y;

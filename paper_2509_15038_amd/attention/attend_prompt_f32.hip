@@ -177,7 +177,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-    float top = -INFINITY, sum = 0.f;
+    float top = kNoScore, sum = 0.f;
 
     // Takes a tile's scores into the running softmax: s become the weights.
     const auto weigh = [&](auto masked, f32x16a& s, int far, int near, int sink) ALWAYS_INLINE {
@@ -198,10 +198,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
             for (int db = 0; db < 4; ++db) o[db] *= keep;
             top = next;
         }
-        const float off = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, -off));
+            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, -top));
             sum += s[i];
         }
     };
@@ -376,7 +375,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
 
     sum = halves_sum(sum);
     if (R0 + col >= a.rows) return;
-    const bool empty = top == -INFINITY;
+    const bool empty = top == kNoScore;
     const float over = empty ? 0.f : 1.f / sum;
     char* out = (char*)c.out + q_row * 512;
 #pragma unroll

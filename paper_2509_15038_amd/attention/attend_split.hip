@@ -448,16 +448,15 @@ __device__ __forceinline__ void take(Running& r, Tile<F>& x, const Queries& q, f
     for (int e = 1; e < E; ++e) top = fmaxf(top, s[e]);
     top = fmaxf(r.top, quarters_max(top) * scale_log2);
     if (__any(top > r.top)) {
-        const float keep = top > r.top ? __builtin_amdgcn_exp2f(r.top - top) : 1.f;       // (-inf before the first key: 0)
+        const float keep = top > r.top ? __builtin_amdgcn_exp2f(r.top - top) : 1.f;       // (0 before the first key)
         r.sum *= keep;
 #pragma unroll
         for (int i = 0; i < 8; ++i) r.o[i] *= keep;
         r.top = top;
     }
-    const float off = MASKED && r.top == -INFINITY ? 0.f : r.top;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale_log2, -off));
+        s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale_log2, -r.top));
         r.sum += s[e];
     }
     x.template values<MASKED>(s, seen, r.o);
@@ -679,7 +678,7 @@ __device__ __forceinline__ f32x2a load_shared(const uint64_t* from) {
 // Eight channels of row R's result, o un-normalised.
 template <int FB>
 __device__ __forceinline__ void write_row(const AttendCall& c, int g, int R, int d0, float* o, float top, float sum) {
-    const bool empty = top == -INFINITY;
+    const bool empty = top == kNoScore;
     const float over = empty ? 0.f : 1.f / sum;
     const int b = g / c.kv, t = R / c.group, h = (g - b * c.kv) * c.group + R % c.group;
     const int64_t out_row = ((int64_t)b * c.m + t) * c.kv * c.group + h;
@@ -701,13 +700,12 @@ __device__ __forceinline__ void merge_waves(const WaveParts& part, const WaveVal
     top = tops[0][row];
 #pragma unroll
     for (int w = 1; w < kSplitWaves; ++w) top = fmaxf(top, tops[w][row]);
-    const float off = top == -INFINITY ? 0.f : top;
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
 #pragma unroll
     for (int w = 0; w < kSplitWaves; ++w) {
-        const float weight = __builtin_amdgcn_exp2f(tops[w][row] - off);
+        const float weight = __builtin_amdgcn_exp2f(tops[w][row] - top);
         sum += weight * sums[w][row];
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] += weight * part[w][row][d0 + i];
@@ -719,7 +717,7 @@ template <int FB>
 __device__ __forceinline__ void join(const SplitArgs& a, int item, int w0, int w1, WaveParts& part, WaveValues& tops, WaveValues& sums) {
     const int g = item / a.row_tiles, R0 = (item - g * a.row_tiles) * kRowTile, rows = min(kRowTile, a.rows - R0), group = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
     const int ways = rows <= 4 ? 4 : rows <= 8 ? 2 : 1, row = group % (kRowTile / ways), way = group / (kRowTile / ways);
-    float top = -INFINITY, sum = 0.f, o[8] = {};
+    float top = kNoScore, sum = 0.f, o[8] = {};
     if (row < rows)
         for (int first = w0 + way; first <= w1; first += 8 * ways) {
             // (eight parts' loads together; the last one again for those beyond it, left out)
@@ -734,14 +732,14 @@ __device__ __forceinline__ void join(const SplitArgs& a, int item, int w0, int w
             float next = top;
 #pragma unroll
             for (int k = 0; k < 8; ++k) next = fmaxf(next, ml[k].x);
-            const float off = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - off);
+            const float keep = __builtin_amdgcn_exp2f(top - next);
             sum *= keep;
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] *= keep;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 if (first + k * ways > w1) continue;
-                const float weight = __builtin_amdgcn_exp2f(ml[k].x - off);
+                const float weight = __builtin_amdgcn_exp2f(ml[k].x - next);
                 sum += weight * ml[k].y;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] += weight * x[k][i / 2][i % 2];
@@ -755,8 +753,8 @@ __device__ __forceinline__ void join(const SplitArgs& a, int item, int w0, int w
         __syncthreads();
         if (way > 0 || row >= rows) return;
         for (int w = 1; w < ways; ++w) {
-            const float other = tops[w][row], next = fmaxf(top, other), off = next == -INFINITY ? 0.f : next;
-            const float keep = __builtin_amdgcn_exp2f(top - off), weight = __builtin_amdgcn_exp2f(other - off);
+            const float other = tops[w][row], next = fmaxf(top, other);
+            const float keep = __builtin_amdgcn_exp2f(top - next), weight = __builtin_amdgcn_exp2f(other - next);
             sum = sum * keep + weight * sums[w][row];
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = o[i] * keep + weight * part[w][row][d0 + i];
@@ -800,7 +798,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void attend_split_kernel(Split
         Running r;
 #pragma unroll
         for (int i = 0; i < 8; ++i) r.o[i] = (f32x4a){0, 0, 0, 0};
-        r.top = -INFINITY;
+        r.top = kNoScore;
         r.sum = 0.f;
 
         if constexpr (FA != kNone) {

@@ -293,7 +293,9 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  *   out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log sum_j exp(scale * q.k_j).
  * A token that sees nothing (length < m and i < m - length), or only keys whose scores are
  * -infinity, gets zeros and -infinity; a key of such a score weighs nothing.  What a token does
- * not see does not reach it, infinities and NaN included.
+ * not see does not reach it, infinities and NaN included.  A score of +infinity or NaN that it
+ * sees makes its result and lse NaN, and a value that is not finite makes its channel so,
+ * whatever the key weighs.
  * lengths: int32 [count], clamped to [0, n]; NULL = n for all.  n <= stride, n <= max_tokens.
  * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0; m <= max_tokens.
  * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits,

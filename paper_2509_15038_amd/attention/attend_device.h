@@ -25,6 +25,7 @@ typedef __bf16 bf16x8a __attribute__((ext_vector_type(8)));
 constexpr float kLn2 = 0.693147180559945309f;
 // The reference of a row that has met no score yet, or none but -infinity (a hidden key's, or an infinite key's): exp2(-infinity - kNoScore) is the weight 0 that such
 // a key has, where -infinity in its place would make NaN of the difference.
+// A row is empty where its weights' sum is 0: the largest key weighs something, and a NaN among the scores, which maxima pass over, makes NaN of the sum.
 constexpr float kNoScore = -FLT_MAX;
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {

@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_prompt_kernel(PromptArg
         if (half == 0) a.part_ml[at] = (f32x2a){ref, total};
         return;
     }
-    const bool empty = ref == kNoScore;
+    const bool empty = total == 0.f;
     const float over = empty ? 0.f : 1.f / total;
     char* out = (char*)c.out + query_row * 256;
 #pragma unroll
@@ -374,7 +374,6 @@ __global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a) {
     const int64_t first = (int64_t)g * a.row_tiles * kTileRows + R, step = (int64_t)a.groups * a.row_tiles * kTileRows;
     float ref = kNoScore, sum = 0.f;
     for (int k = 0; k < a.parts; ++k) ref = fmaxf(ref, a.part_ml[first + k * step].x);
-    const bool empty = ref == kNoScore;
     f32x2a o = {0, 0};
 #pragma unroll 4
     for (int k = 0; k < a.parts; ++k) {
@@ -384,6 +383,7 @@ __global__ __launch_bounds__(256) void attend_prompt_join_kernel(PromptArgs a) {
         o.x += weight * x.x;
         o.y += weight * x.y;
     }
+    const bool empty = sum == 0.f;
     const float over = empty ? 0.f : 1.f / sum;
     const int b = g / c.kv, t = R / c.group, h = (g - b * c.kv) * c.group + R % c.group;
     ((uint32_t*)c.out)[(((int64_t)b * c.m + t) * c.kv * c.group + h) * 64 + lane] = pack_bf16(o.x * over, o.y * over);

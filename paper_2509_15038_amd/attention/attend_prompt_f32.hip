@@ -375,7 +375,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attend_prompt_f32_kerne
 
     sum = halves_sum(sum);
     if (R0 + col >= a.rows) return;
-    const bool empty = top == kNoScore;
+    const bool empty = sum == 0.f;
     const float over = empty ? 0.f : 1.f / sum;
     char* out = (char*)c.out + q_row * 512;
 #pragma unroll

@@ -678,7 +678,7 @@ __device__ __forceinline__ f32x2a load_shared(const uint64_t* from) {
 // Eight channels of row R's result, o un-normalised.
 template <int FB>
 __device__ __forceinline__ void write_row(const AttendCall& c, int g, int R, int d0, float* o, float top, float sum) {
-    const bool empty = top == kNoScore;
+    const bool empty = sum == 0.f;
     const float over = empty ? 0.f : 1.f / sum;
     const int b = g / c.kv, t = R / c.group, h = (g - b * c.kv) * c.group + R % c.group;
     const int64_t out_row = ((int64_t)b * c.m + t) * c.kv * c.group + h;

@@ -1,4 +1,5 @@
-"""Attention where tokens see keys whose scores are not finite: keys of score -infinity weigh nothing, wherever they lie and whichever kernel takes them."""
+"""Attention where tokens see keys whose scores are not finite: keys of score -infinity weigh nothing, wherever they lie and whichever kernel takes them, and
+NaN is NaN in the log-sum too."""
 
 import math
 
@@ -93,3 +94,53 @@ def test_first_rows_of_4_bits_that_weigh_nothing():
     for h in range(8):
         k, v = (x.view(kv, kept, D)[h // 4] for x in held)
         U.check_attention(out[0, :, h], lse[h], U.attention(Q[0, :, h], k, v, seen, D ** -0.5), "bf16", kept, f"head {h}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count,kv,m,n,window,sinks", SHAPES)
+def test_a_query_of_nan(dtype, count, kv, m, n, window, sinks):
+    # its token has NaN, in the log-sum too, and no other
+    Q, K, V = inputs(dtype, count, kv, m, n, 0, "infinite")
+    t = m // 2
+    Q[:, t, 1, 77] = math.nan
+    out, lse = U.run_attend(dict(count=count, kv=kv, group=4, m=m, n=n, window=window, sinks=sinks, dtype=dtype), Q, K, V, None, n)
+    assert bool(torch.isnan(out[:, t, 1]).all()) and bool(torch.isnan(lse[:, 1, t]).all())
+    assert int(torch.isnan(out).sum()) == count * D and int(torch.isnan(lse).sum()) == count
+    assert not bool(torch.isinf(lse).any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count,kv,m,n,window,sinks", SHAPES)
+def test_nothing_but_keys_of_nan(dtype, count, kv, m, n, window, sinks):
+    # a token that sees something has NaN, one before the sequence's first zeros and -infinity; other heads are right
+    Q, K, V = inputs(dtype, count, kv, m, n, 0, "infinite")
+    K[:, 0] = math.nan
+    length = n if m == 1 else m - 1
+    lengths = torch.full((count,), length, dtype=torch.int32, device="cuda")
+    out, lse = U.run_attend(dict(count=count, kv=kv, group=4, m=m, n=n, window=window, sinks=sinks, dtype=dtype), Q, K, V, lengths, n)
+    none = m - min(m, length)
+    assert bool(torch.isnan(out[:, none:, :4]).all()) and bool(torch.isnan(lse[:, :4, none:]).all())
+    assert bool((out[:, :none] == 0).all()) and bool((lse[:, :, :none] == -math.inf).all())
+    seen = U.causal(m, n, length, window, sinks)
+    want = U.attention(Q[-1, :, 5], K[-1, 1], V[-1, 1], seen, D ** -0.5)
+    U.check_attention(out[-1, :, 5], lse[-1, 5], want, dtype, n)
+
+
+@pytest.mark.parametrize("dtype,mx", [("bf16", False), ("fp32", False), ("bf16", True), ("fp32", True)])
+@pytest.mark.parametrize("m", [1, 400])
+def test_a_query_of_nan_over_kept_rows(dtype, mx, m):
+    kv, kept = 8, 500
+    Q, K, V = inputs(dtype, 1, kv, m, kept, 0, "infinite")
+    Q[0, 0, 2, 9] = math.nan
+    out, lse = torch.empty_like(Q), torch.empty((kv * 4, m), device="cuda")
+    offsets = torch.arange(kv + 1, device="cuda") * kept
+    with U.B.Context(1, kv, 4, D, 32, dtype, kept, 1) as ctx:
+        if mx:
+            codes = [torch.empty((kv * kept, w), dtype=torch.uint8, device="cuda") for w in (64, 4, 64, 4)]
+            ctx.compact_mx(K, V, kept, torch.arange(kept, dtype=torch.int32, device="cuda").repeat(kv), offsets, kv * kept, *codes)
+            ctx.attend_kept_mx(Q, *codes, offsets, 1, m, kv * kept, out, lse=lse)
+        else:
+            ctx.attend_kept(Q, K, V, offsets, 1, m, kv * kept, out, lse=lse)
+        torch.cuda.synchronize()
+    assert bool(torch.isnan(out[0, 0, 2]).all()) and bool(torch.isnan(lse[2, 0])) and int(torch.isnan(out).sum()) == D and int(torch.isnan(lse).sum()) == 1
+    assert not bool(torch.isinf(lse).any())

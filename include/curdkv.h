@@ -56,7 +56,7 @@ extern "C" {
 #define CURDKV_ERR_OOM         -4   /* device or host allocation failed */
 #define CURDKV_ERR_TOO_LARGE   -5   /* more (layer, group) pairs than a non-allocating call's fixed workspace holds */
 
-#define CURDKV_ATTEND_SCRATCH_BYTES 34078720   /* most scratch that an attention call uses (65504 rows of 520 bytes, 16 KB of counters) */
+#define CURDKV_ATTEND_SCRATCH_BYTES 38354944   /* most scratch that an attention call uses (16 KB of counters, 73728 rows of 520 bytes) */
 
 #define CURDKV_DTYPE_F32  0
 #define CURDKV_DTYPE_BF16 1

@@ -403,6 +403,10 @@ hipError_t launch_attend_prompt(const curdkv_ctx* ctx, const AttendCall& call, h
     const int64_t blocks = (int64_t)a.groups * a.row_tiles, tiles = ((call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n) + call.rows / a.groups) / kKeys;
     const int64_t part_bytes = blocks * kTileRows * (int64_t)(128 * sizeof(float) + sizeof(f32x2a)), room = call.scratch ? call.scratch_bytes - kScratchCounters : 0;
     int64_t parts = std::min(std::min(2 * ctx->num_cu / blocks, tiles / 8), room / part_bytes);
+    // Two parts, which fill what one workgroup a unit leaves idle, take longer than one over short caches, and a join: 8 heads of 4, 768 new tokens (192 workgroups) over 3000 rows one
+    // part 59 us, two 62, over 4000 74 and 72, 6000 108 and 98; 1024 (256) over 2000 43 and 54, 6000 111 and 112, 16000 283 and 260.  (Kept rows: heads are uneven, and parts of them
+    // less so: 1024 tokens over 500 to 3276 of them 113 and 113, 4 sequences of 256 196 and 158.)
+    if (parts == 2 && !call.offsets && 2 * tiles < blocks - 70) parts = 1;
     a.parts = parts > 1 ? (int)parts : 1;
     a.part_o = (float*)((char*)call.scratch + kScratchCounters);
     a.part_ml = (f32x2a*)(a.part_o + a.parts * blocks * kTileRows * 128);

@@ -43,7 +43,7 @@ struct SplitArgs {
     int least;                         // tiles of an item, on average, from which it pays to share it (3/8 of them in workgroups of its own)
     float weight;                      // parts of an item squared over its tiles, where reading and joining are in balance
     int* arrived;                      // [items]: workgroups that are done with their part of an item; 0 between the calls
-    float* part_o;                     // [shares + 2 items][16][128]: of workgroup w and item i at w + i, which no other pair has
+    float* part_o;                     // [slots][16][128]: of workgroup w and item i at w + i, which no other pair has
     f32x2a* part_ml;                   // the same of maxima and sums
 };
 
@@ -923,7 +923,7 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     const int T = mx && !f32 ? 32 : 16, row = f32 ? 512 : 256;
     const int64_t units = ctx->num_cu, heads = call.count * call.kv, slot = kRowTile * kPartBytes;
     const int64_t keys = call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n;
-    const int64_t tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles, room = call.scratch ? (call.scratch_bytes - kCounters * (int64_t)sizeof(int)) / slot : 0;
+    const int64_t tiles = (call.rows / T + heads * (keys / T + 1)) * a.row_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / slot : 0;
     // One a unit at most (two: one token over 131072 rows 100 us, so 91).  4 bits, whose expansion wants two waves a SIMD, two a unit
     // where they have long to go (320 us, so 295; 32 tiles a unit: 18, 20).  A tile a wave at least, and no more parts of an item than pay: its tiles over the parts are read
     // in a time of their own, its parts are counted and joined in theirs, and the two together are least where parts^2 is about the tiles, or twice them in fp32 (one token of 8
@@ -931,7 +931,10 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     a.weight = f32 ? 2.f : 1.f;
     const int64_t most = (int64_t)std::sqrt((double)a.weight * a.items * tiles);
     const int64_t wanted = std::min(units * (mx && tiles >= 1024 * units ? 2 : 1), std::max((int64_t)a.items, std::min(most, (tiles + kSplitWaves - 1) / kSplitWaves)));
-    int64_t shares = std::min(wanted, room - 2 * a.items);
+    // (slots of partial results: a workgroup and an item add up to less than shares + items, and than shares + 2 items where every item has workgroups of its own, of which
+    // there may be shares + items)
+    const int64_t between = (a.items <= 64 ? 2 : 1) * (int64_t)a.items;
+    int64_t shares = std::min(wanted, room - between);
     // Few items: each its own workgroups, which have less to look up and to join (64 heads of up to 2000 rows 18.1 us, so 15.6, of 4 bits 21.5, so 14.7); where few share one
     // for long, equal shares of all of them count for more (64 heads of 16000 in 4 bits 41, so 49).
     a.whole = a.items <= 64 && 2 * a.items <= shares;
@@ -940,6 +943,10 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     // 65, of 2000 109 and 100.  fp32's tiles take twice as long: 8 of 250 11.6 and 12.3, of 400 14.9 and 13.2; 128 of 1000 28 and 27.  Kept rows differ more from head to
     // head: 8 of about 250 11.3 and 10.9, 400 in 4 bits 10.5 and 11.1, 600 12.8 and 11.0; 256 of 500 27.9 and 26.4, of 1000 61 and 40, in 4 bits 26.6 and 24.3.
     a.least = 128 / (f32 ? 2 : 1) / (call.offsets ? 4 : 1);
+    // More items than find() holds in registers, four a lane, are looked up one after the other: 10 us and more.  Uneven kept rows, not shared and shared: in 4 bits 384 heads of
+    // 1000 25 and 33, of 1500 35 and 31, 1536 of 1000 56 and 89, of 2000 107 and 104, 3200 of 1000 101 and 143, of 3000 248 and 234; in bf16 1536 of 500 91 and 106, of 1000 169 and 139,
+    // 3200 of 1000 340 and 271; 3200 of 300 in 4 bits under fp32 132 and 176.
+    if (call.offsets && a.items > 4 * 64) a.least += (mx && !f32 ? 16 : 0) + (a.items - 256) / 128;
     const int64_t least = a.whole && few_enough(a.items, shares, tiles) ? a.least * 3 / 8 : a.least;
     // Equal ones in whole turns of all units are shared out already: 256 heads of 4000 rows 81 and 87, through windows of 4096 69 and 74 (264 heads: 106 and 77).
     const bool equal = !call.offsets && (!call.lengths || (call.window > 0 && 2 * (int64_t)call.window <= call.n)) && a.items % units == 0;
@@ -948,7 +955,7 @@ hipError_t launch_attend_split(const curdkv_ctx* ctx, const AttendCall& call, hi
     a.whole = a.whole && shares > 0;
     a.arrived = (int*)call.scratch;
     a.part_o = (float*)(a.arrived + kCounters);
-    a.part_ml = (f32x2a*)(a.part_o + (shares + 2 * a.items) * kRowTile * 128);
+    a.part_ml = (f32x2a*)(a.part_o + (shares + between) * kRowTile * 128);
     // (bytes that 256 MB of Infinity Cache would not hold until the next call: one token over 131072 rows 105 us through the caches, 91 past them; 64 tokens in fp32 over 4000
     // rows, which 16 tiles of their rows read one after the other, 59 and 75)
     const bool past = 2 * ((mx ? 68 : row) * call.rows + row * heads * keys) > kPastCaches;

@@ -24,7 +24,7 @@ ATTEND_PATH = os.path.join(_HERE, "_attend" + (sysconfig.get_config_var("EXT_SUF
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_HIP, ERR_OOM, ERR_TOO_LARGE = 0, -1, -2, -3, -4, -5
 DTYPE_F32, DTYPE_BF16 = 0, 1
-ATTEND_SCRATCH_BYTES = 34078720
+ATTEND_SCRATCH_BYTES = 38354944
 _DTYPES = {"fp32": DTYPE_F32, "bf16": DTYPE_BF16}
 
 EXPORTS = ["curdkv_create", "curdkv_destroy", "curdkv_sketch_host", "curdkv_set_sketch",

@@ -484,7 +484,7 @@ struct Work {
     // What a tile costs, in units that the work is shared out by: its bytes, and the expansion of 4 bits.
     static constexpr int kUnitA = 1, kUnitB = FA == kMxF32 ? 3 : FA == kMxBf16 ? 2 : 1;
     int64_t begin = 0;                                     // first kept row
-    int kept = 0, kept_tiles = 0;                          // (an item's rows and all units together are below 2^31: they lie in 288 GB)
+    int kept = 0, kept_tiles = 0;                          // (a head's rows are below 2^31, an item's units below 2^28)
     Seen seen;
     int t0, t1;
     int first_tiles, near_begin, near_end, near_tiles;     // whole first rows; of the tiles from seen.low on: whole ones, and all
@@ -568,6 +568,9 @@ __host__ __device__ __forceinline__ bool few_enough(int items, int64_t shares, i
 template <int FA, int FB>
 struct Places {
     static constexpr int kBetween = FA == kMxBf16 || FA == kMxF32 ? 32 : 16, kAtOnce = 4;
+    // A lane's items have less than this many units, so that those of 64 lanes are below 2^31 (a head's rows count once for each of its row tiles: memory does not bound them).  Where
+    // a lane has more, heads are of a million rows at least, or of 140 GB with few items, and every item has one workgroup.
+    static constexpr int kMostUnits = (1 << 25) - 1;
     const SplitArgs& a;
     int all, shares, at;               // units of all items; workgroups with a share; units in front of the item at hand, without its kBetween
     bool whole;                        // workgroups have parts of one item each
@@ -578,6 +581,14 @@ struct Places {
         p.first = share_of(at + kBetween);
         p.last = share_of(at + kBetween + units - 1);
     }
+    __device__ __forceinline__ Place by_items(int block) const {       // items as they are
+        const int places = min(a.items, a.shares);
+        Place p{0, 0, 0, a.items, 0, 0, {0, 0, 0}};
+        p.item = (int)((int64_t)a.items * block / places);
+        p.end = (int)((int64_t)a.items * (block + 1) / places);
+        if (block < places) p.head = head_of(a, p.item / a.row_tiles), p.size = INT_MAX;
+        return p;
+    }
     __device__ __forceinline__ Place find() {
         const int lane = threadIdx.x & 63, each = (a.items + 63) / 64, from = min(lane * each, a.items), end = min(from + each, a.items), block = blockIdx.x;
         Place p{0, 0, 0, a.items, 0, 0, {0, 0, 0}};
@@ -587,6 +598,7 @@ struct Places {
         if (a.whole) {                 // (each == 1)
             head[0] = head_of(a, min(from, a.items - 1) / a.row_tiles);
             mine = lane < a.items ? Work<FA, FB>(a, from, head[0]).units : 0;
+            if (__any(mine >= kMostUnits)) return by_items(block);
             const int tiles = __builtin_amdgcn_readlane(added_up(mine), 63);
             whole = few_enough(a.items, a.shares, tiles);
             if (whole) {
@@ -617,19 +629,14 @@ struct Places {
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
                 units[k] = i + k < end ? Work<FA, FB>(a, i + k, head[k]).units + kBetween : 0;
-                mine += units[k];
+                mine = min(mine + units[k], kMostUnits);
             }
         }
+        if (__any(mine >= kMostUnits)) return by_items(block);
         const int up_to = added_up(mine);
         all = __builtin_amdgcn_readlane(up_to, 63);
         const int tiles = all - a.items * kBetween;
-        if (tiles < a.least * a.items) {                               // little to read, in fact: items as they are
-            const int places = min(a.items, a.shares);
-            p.item = (int)((int64_t)a.items * block / places);
-            p.end = (int)((int64_t)a.items * (block + 1) / places);
-            if (block < places) p.head = head_of(a, p.item / a.row_tiles), p.size = INT_MAX;
-            return p;
-        }
+        if (tiles < a.least * a.items) return by_items(block);         // little to read, in fact
         // (no more shares than tiles: none may be without any between two that have parts of one item)
         shares = max(1, min(a.shares, (all - a.items * kBetween) / (kBetween + 1)));
         const int begin = begin_of(block);

@@ -1,0 +1,40 @@
+"""Attention calls whose counts are large: sums of work beyond 31 bits, and sizes that a launch does not take."""
+
+import pytest
+import torch
+
+from paper_2509_15038_amd import binding as B
+from tests import attend_util as U
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+def test_more_work_than_31_bits_count():
+    # 4096 tiles of 16 queries over one head of 20 million rows in 4 bits, 2.6e9 tiles of keys in all.  All keys are zeros but 60, which score 40 and more: the others weigh
+    # 2e7 e^-40 < 2^-30 together, and the result is that over the 60
+    rows, m, group = 20_000_000, 16384, 4
+    g = torch.Generator(device="cuda").manual_seed(1)
+    at = torch.cat([torch.tensor([0, 31, 32, rows // 2, rows - 33, rows - 32, rows - 1], device="cuda"), torch.randint(0, rows, (53,), generator=g, device="cuda")]).unique()
+    K_codes, K_scales = torch.zeros((rows, 64), dtype=torch.uint8, device="cuda"), torch.full((rows, 4), 125, dtype=torch.uint8, device="cuda")
+    K_codes[at] = torch.randint(0, 256, (at.numel(), 64), generator=g, device="cuda").to(torch.uint8)
+    K_codes[at, 0] = 7                                                  # channel 0: 6; channel 1: 0
+    V_codes = torch.randint(0, 256, (rows, 64), generator=g, device="cuda", dtype=torch.uint8)
+    Q = U.randn(2, (1, m, group, D), torch.bfloat16)
+    Q[..., 0] = 360.0                                                   # 360 * 6 / 4 / sqrt(128) = 47.7, the other channels +-3
+    out, lse = torch.empty_like(Q), torch.empty((group, m), device="cuda")
+    held = [torch.empty((at.numel(), D), dtype=torch.bfloat16, device="cuda") for _ in "KV"]
+    with U.context(1, group, "bf16", 64) as ctx:
+        ctx.attend_kept_mx(Q, K_codes, K_scales, V_codes, K_scales, torch.tensor([0, rows], device="cuda"), 1, m, rows, out, lse=lse)
+        for x, codes in zip(held, (K_codes, V_codes)):
+            ctx.expand_mx(codes[at].contiguous(), K_scales[at].contiguous(), at.numel(), x)
+        torch.cuda.synchronize()
+    some = torch.tensor([0, 1, 3, 4, 5, 511, 4097, 8191, 12345, m - 2, m - 1], device="cuda")
+    for h in range(group):
+        want = U.attention(Q[0, some, h], held[0], held[1], torch.ones((some.numel(), at.numel()), dtype=torch.bool, device="cuda"), D ** -0.5)
+        assert float((Q[0, some, h].double() @ held[0].double().T).min()) * D ** -0.5 > 40
+        U.check_attention(out[0, some, h], lse[h, some], want, "bf16", at.numel(), f"head {h}")
+    # every token's own sum, by the same 60 keys in 32 bits
+    x = torch.matmul(Q[0].float(), held[0].float().T.contiguous()) * D ** -0.5
+    off = (torch.logsumexp(x.double(), -1).T - lse.double()).abs().max()
+    assert float(off) < 2 * 128 * 2.0 ** -24 * 200, float(off)           # (scores are sums of 128 products, of magnitudes below 200 together)

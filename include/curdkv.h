@@ -336,7 +336,7 @@ int curdkv_expand_mx(curdkv_ctx* ctx, const uint8_t* codes, const uint8_t* scale
  *   offsets[b*kv_heads + h] .. offsets[b*kv_heads + h + 1] - 1.
  * offsets: DEVICE int64 [count*kv_heads + 1], kept within [0, total]; a layer of a larger
  *   packed cache is its slice of the offsets, with the whole cache's K_kept and V_kept.
- * total: rows of K_kept and V_kept; rows: how many of them belong to this call's heads (all:
+ * total: rows of K_kept and V_kept, below 2^31; rows: how many of them belong to this call's heads (all:
  *   total).  The work is shared out by their average; uneven heads are read whole all the same.
  * K_tail, V_tail: [count, kv_heads, tail_stride, head_dim]; tail_lengths: int32 [count], clamped
  *   to [0, tail_n]; NULL = tail_n.  tail_n = 0: no tail (the pointers may be NULL). */

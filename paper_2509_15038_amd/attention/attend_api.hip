@@ -57,6 +57,7 @@ int run_kept(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_k
     if (rc != CURDKV_OK) return rc;
     if (!offsets || total < 0 || rows < 0 || rows > total || (total > 0 && (!K_kept || !V_kept)) || (tail_n > 0 && (!K_tail || !V_tail))) return CURDKV_ERR_INVALID_ARG;
     if (!aligned16({K_kept, V_kept, K_tail, V_tail})) return CURDKV_ERR_INVALID_ARG;
+    if (total > (1LL << 31) - 1) return CURDKV_ERR_UNSUPPORTED;        // (a head's rows are counted in 32 bits)
     AttendCall c{};
     c.Q = Q, c.out = out, c.lse = lse, c.count = count;
     c.kv = ctx->cfg.kv_heads, c.group = ctx->cfg.group_size, c.m = (int)m, c.dtype = ctx->cfg.dtype, c.scale = scale;

@@ -38,3 +38,21 @@ def test_more_work_than_31_bits_count():
     x = torch.matmul(Q[0].float(), held[0].float().T.contiguous()) * D ** -0.5
     off = (torch.logsumexp(x.double(), -1).T - lse.double()).abs().max()
     assert float(off) < 2 * 128 * 2.0 ** -24 * 200, float(off)           # (scores are sums of 128 products, of magnitudes below 200 together)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_more_rows_than_31_bits_count(mx):
+    # refused before anything is launched: the arrays are small ones
+    K, Q = U.randn(1, (64, D), torch.bfloat16), U.randn(3, (1, 1, 4, D), torch.bfloat16)
+    codes, scales = torch.zeros((64, 64), dtype=torch.uint8, device="cuda"), torch.zeros((64, 4), dtype=torch.uint8, device="cuda")
+    off, out = torch.tensor([0, 64], device="cuda"), torch.full_like(Q, 7.0)
+    with U.context(1, 4, "bf16", 64) as ctx:
+        call = (lambda total: ctx.attend_kept_mx(Q, codes, scales, codes, scales, off, 1, 1, total, out)) if mx else \
+            (lambda total: ctx.attend_kept(Q, K, K, off, 1, 1, total, out))
+        for total in (2 ** 31, 2 ** 40):
+            with pytest.raises(B.CurdkvError) as e:
+                call(total)
+            assert e.value.code == B.ERR_UNSUPPORTED
+        torch.cuda.synchronize()
+        assert bool((out == 7).all())
+        call(64)

@@ -10,6 +10,8 @@
 // Everything between load and store is in 32 bits; the store is the one rounding.
 // Measured: 32768 tokens of 32 + 8 + 8 heads with norms (822 MB) 140 us, 5.9 TB/s; one token of 4 sequences 4.0 us a call, the kernel 3.5.
 
+#include <algorithm>
+
 #include "attend_device.h"
 #include "attend_internal.h"
 
@@ -27,6 +29,7 @@ struct RotateArgs {
     int kv, group;
     char *Q, *K, *V;
     int64_t stride;
+    int64_t first;                     // a launch's first token
 };
 
 template <int CTRL>
@@ -87,7 +90,7 @@ template <bool BF16, bool PAIRS, int TOKENS, bool PAST>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     constexpr int kSlots = 32 / TOKENS, kRow = BF16 ? 256 : 512;
     const int u = threadIdx.x & 7, slot = threadIdx.x >> 3;
-    const int64_t token = (int64_t)blockIdx.x * TOKENS + slot / kSlots;
+    const int64_t token = a.first + (int64_t)blockIdx.x * TOKENS + slot / kSlots;
     if (token >= a.tokens) return;
     const int64_t b = token / a.m, i = token - b * a.m;
     const int first = PAIRS ? 2 * u : u, second = PAIRS ? 2 * u + 1 : u + 8;       // pieces of eight channels
@@ -140,13 +143,20 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
 }
 
 template <bool BF16, bool PAIRS>
-hipError_t launch(const curdkv_ctx* ctx, const RotateArgs& a, hipStream_t stream) {
+hipError_t launch(const curdkv_ctx* ctx, RotateArgs a, hipStream_t stream) {
     // Four tokens a workgroup where that still gives every unit four; one, its heads over all lanes, below.  Rows that the caches would not hold until
     // they are read again pass them by (32768 tokens of 48 heads: 159 us, 144 so).
     const int64_t bytes = a.tokens * a.kv * (a.group + 2) * (BF16 ? 512 : 1024);
-    if (a.tokens < 16 * (int64_t)ctx->num_cu) rotate_kernel<BF16, PAIRS, 1, false><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
-    else if (bytes <= kPastCaches) rotate_kernel<BF16, PAIRS, 4, false><<<(unsigned)((a.tokens + 3) / 4), 256, 0, stream>>>(a);
-    else rotate_kernel<BF16, PAIRS, 4, true><<<(unsigned)((a.tokens + 3) / 4), 256, 0, stream>>>(a);
+    if (a.tokens < 16 * (int64_t)ctx->num_cu) {
+        rotate_kernel<BF16, PAIRS, 1, false><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    // (a launch's threads are counted in 32 bits: 2^25 tokens each)
+    for (; a.first < a.tokens; a.first += 1 << 25) {
+        const unsigned blocks = (unsigned)((std::min(a.tokens - a.first, (int64_t)1 << 25) + 3) / 4);
+        if (bytes <= kPastCaches) rotate_kernel<BF16, PAIRS, 4, false><<<blocks, 256, 0, stream>>>(a);
+        else rotate_kernel<BF16, PAIRS, 4, true><<<blocks, 256, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 
@@ -157,7 +167,7 @@ hipError_t launch_rotate(const curdkv_ctx* ctx, const void* qkv, int64_t count, 
                          float eps, bool pairs, void* Q, void* K, void* V, int64_t stride, hipStream_t stream) {
     const bool bf16 = ctx->cfg.dtype == CURDKV_DTYPE_BF16;
     const RotateArgs a{(const char*)qkv, m, count * m, row_stride * (bf16 ? 2 : 4), starts, positions, table, table_rows, q_weight, k_weight, eps,
-                       ctx->cfg.kv_heads, ctx->cfg.group_size, (char*)Q, (char*)K, (char*)V, stride};
+                       ctx->cfg.kv_heads, ctx->cfg.group_size, (char*)Q, (char*)K, (char*)V, stride, 0};
     if (bf16) return pairs ? launch<true, true>(ctx, a, stream) : launch<true, false>(ctx, a, stream);
     return pairs ? launch<false, true>(ctx, a, stream) : launch<false, false>(ctx, a, stream);
 }

@@ -56,3 +56,29 @@ def test_more_rows_than_31_bits_count(mx):
         torch.cuda.synchronize()
         assert bool((out == 7).all())
         call(64)
+
+
+def test_more_tokens_than_a_launch_has_threads_for():
+    # 2^26 tokens of 3 heads and some (51 GB): the last ones, those around a launch's end and the first are looked at
+    m = 2 ** 26 + 37
+    qkv, Q = torch.empty((m, 3 * D), dtype=torch.bfloat16, device="cuda"), torch.empty((m, D), dtype=torch.bfloat16, device="cuda")
+    K, V = (torch.full((64, D), 5.0, dtype=torch.bfloat16, device="cuda") for _ in "KV")
+    some = torch.tensor([*range(40), 2 ** 25 - 1, 2 ** 25, 2 ** 25 + 1, 2 ** 26 - 1, 2 ** 26, *range(m - 30, m)], device="cuda")
+    qkv[some] = U.randn(1, (some.numel(), 3 * D), torch.bfloat16)
+    Q[some] = float("nan")
+    angle = torch.arange(50, device="cuda")[:, None] * 0.01 * torch.arange(1, 65, device="cuda")[None]
+    table = torch.stack([angle.cos(), angle.sin()], 1).contiguous()
+    start = 31                                                         # (the first 33 tokens have a row of the cache; positions beyond the table are its last)
+    with U.context(1, 1, "bf16", 64) as ctx:
+        ctx.rotate(qkv, 1, m, table, Q, K, V, 64, starts=torch.tensor([start], dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+    x = qkv[some].double().view(-1, 3, D)
+    turn = table.double()[(some + start).clamp(max=49)]
+    cos, sin = turn[:, None, 0], turn[:, None, 1]
+    a, b = x[:, :2, :64], x[:, :2, 64:]
+    want = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+    size = torch.cat([(a * cos).abs() + (b * sin).abs(), (b * cos).abs() + (a * sin).abs()], -1)
+    limit = 2.0 ** -8 * 1.01 * want.abs() + 4 * 2.0 ** -24 * size      # (a bf16 significand has 8 bits; two products and a sum in 32)
+    assert bool(((Q[some].double() - want[:, 0]).abs() <= limit[:, 0]).all())
+    assert bool(((K[start:].double() - want[:33, 1]).abs() <= limit[:33, 1]).all()) and torch.equal(V[start:].double(), x[:33, 2])
+    assert bool((K[:start] == 5).all()) and bool((V[:start] == 5).all())

@@ -297,6 +297,8 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  * sees makes its result and lse NaN, and a value that is not finite makes its channel so,
  * whatever the key weighs.
  * lengths: int32 [count], clamped to [0, n]; NULL = n for all.  n <= stride, n <= max_tokens.
+ * count*m*kv_heads*group_size < 2^31, and m*kv_heads*group_size < 2^28 where 16 queries of a KV head
+ * make a workgroup (few tokens; fp32 and 4-bit kept rows); else CURDKV_ERR_UNSUPPORTED.
  * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0; m <= max_tokens.
  * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits,
  * with a bf16 cache the weights are rounded to bf16 for their product with V; with an fp32 cache every

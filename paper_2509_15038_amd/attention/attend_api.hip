@@ -13,6 +13,7 @@ namespace {
 
 // Tiles of 16 rows, and these times the keys, from which the prompts' kernel is the faster one (run_attend).
 constexpr int64_t kPromptItems = 600, kPromptProducts = 400000;
+constexpr int64_t kMostBlocks = (1 << 24) - 1;     // workgroups of a launch
 
 bool aligned16(std::initializer_list<const void*> ptrs) {
     uintptr_t all = 0;
@@ -47,7 +48,25 @@ int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
     const bool prompt = call.offsets ? !call.K_scales && !f32 && rows >= 256 && (items > kPromptItems || items * keys > 2 * kPromptProducts)
                         : f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 16 && (items > kPromptItems || items * keys > kPromptProducts);
     const auto launch = !prompt ? launch_attend_split : f32 ? launch_attend_prompt_f32 : launch_attend_prompt;
-    return launch(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
+    // A launch's threads are counted in 32 bits: so many workgroups of 256 threads and more (of 512 for fp32 prompts).  Whole sequences a launch.
+    const int64_t blocks = call.kv * (prompt ? (rows + 127) / 128 * (f32 ? 2 : 1) : (rows + 15) / 16), at_once = kMostBlocks / blocks;
+    if (call.count <= at_once) return launch(ctx, call, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
+    if (at_once < 1) return CURDKV_ERR_UNSUPPORTED;
+    const int64_t bytes = f32 ? 4 : 2, queries = (int64_t)call.kv * rows;
+    for (int64_t b = 0; b < call.count; b += at_once) {
+        AttendCall some = call;
+        some.count = std::min(at_once, call.count - b);
+        some.Q = (const char*)call.Q + b * queries * kHeadDim * bytes;
+        some.out = (char*)call.out + b * queries * kHeadDim * bytes;
+        if (call.lse) some.lse = call.lse + b * queries;
+        if (call.K) some.K = (const char*)call.K + b * call.kv * call.stride * kHeadDim * bytes;
+        if (call.V) some.V = (const char*)call.V + b * call.kv * call.stride * kHeadDim * bytes;
+        if (call.lengths) some.lengths = call.lengths + b;
+        if (call.offsets) some.offsets = call.offsets + b * call.kv;
+        some.rows = call.rows * some.count / call.count;                // (as far as the host knows)
+        if (launch(ctx, some, (hipStream_t)stream) != hipSuccess) return CURDKV_ERR_HIP;
+    }
+    return CURDKV_OK;
 }
 
 int run_kept(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept, const uint8_t* K_scales, const uint8_t* V_scales,

@@ -82,3 +82,36 @@ def test_more_tokens_than_a_launch_has_threads_for():
     assert bool(((Q[some].double() - want[:, 0]).abs() <= limit[:, 0]).all())
     assert bool(((K[start:].double() - want[:33, 1]).abs() <= limit[:33, 1]).all()) and torch.equal(V[start:].double(), x[:33, 2])
     assert bool((K[:start] == 5).all()) and bool((V[:start] == 5).all())
+
+
+@pytest.mark.parametrize("kept", [False, True])
+def test_more_sequences_than_a_launch_has_workgroups_for(kept):
+    # 2^24 sequences and some, of no row or one, which is the result then
+    count = 2 ** 24 + 41
+    Q, V = (torch.randint(-99, 99, (count, D), dtype=torch.int8, device="cuda").to(torch.bfloat16) for _ in "QV")
+    have = torch.randint(0, 2, (count,), device="cuda").to(torch.int32)
+    out, lse = torch.full_like(Q, 7.0), torch.full((count,), 7.0, device="cuda")
+    with U.context(1, 1, "bf16", 1) as ctx:
+        if kept:
+            offsets = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), have.long().cumsum(0)])
+            ctx.attend_kept(Q, V, V, offsets, count, 1, count, out, lse=lse, scale=1e-9)
+            want = V[(offsets[1:] - 1).clamp(min=0)]
+        else:
+            ctx.attend(Q, V, V, count, 1, 1, 1, out, lengths=have, lse=lse, scale=1e-9)
+            want = V
+        torch.cuda.synchronize()
+    assert torch.equal(out, torch.where(have[:, None] > 0, want, 0.0))
+    assert torch.equal(torch.isinf(lse), have == 0) and float(lse[have > 0].abs().max()) < 128 * 99 ** 2 * 1.01e-9
+
+
+def test_one_sequence_of_more_than_a_launch_has_workgroups_for():
+    # refused before anything is launched: the arrays are small ones
+    K, Q = U.randn(1, (64, D), torch.bfloat16), U.randn(3, (1, 1, 4, D), torch.bfloat16)
+    codes, scales = torch.zeros((64, 64), dtype=torch.uint8, device="cuda"), torch.zeros((64, 4), dtype=torch.uint8, device="cuda")
+    off, out = torch.tensor([0, 64], device="cuda"), torch.full_like(Q, 7.0)
+    with U.context(1, 4, "bf16", 64) as ctx:
+        with pytest.raises(B.CurdkvError) as e:
+            ctx.attend_kept_mx(Q, codes, scales, codes, scales, off, 1, 2 ** 26, 64, out)
+        assert e.value.code == B.ERR_UNSUPPORTED
+        torch.cuda.synchronize()
+    assert bool((out == 7).all())

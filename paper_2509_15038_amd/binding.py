@@ -358,6 +358,10 @@ class Context:
         if given is None:
             if self._own_scratch is None:
                 import torch
+                # (a call of no rows launches nothing, and is refused where the context's device is not the current one: memory of another would be kept)
+                rc = _attend.expand_mx(self._address, None, None, 0, None, 0)
+                if rc != OK:
+                    raise CurdkvError(rc, "scratch of an attention call")
                 if torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("a context's first attention call allocates its scratch: make one before recording, or give it scratch")
                 self._scratch_tensor = torch.zeros((ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")

@@ -22,6 +22,7 @@ def test_the_constant_covers_every_call():
 
 def test_a_first_call_on_another_device_leaves_no_scratch_behind(monkeypatch):
     # the current device is in `current`; the entry points refuse a context of device 0 elsewhere
+    B.lib()                                                             # (binds the module that is replaced below)
     current, made, seen = [1], [], []
 
     def entry(*a):

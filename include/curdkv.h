@@ -326,7 +326,8 @@ int curdkv_compact_mx(curdkv_ctx* ctx, const void* K, const void* V, int64_t n,
                       const int32_t* indices, const int64_t* offsets, int64_t total, uint8_t* K_codes,
                       uint8_t* K_scales, uint8_t* V_codes, uint8_t* V_scales, void* stream);
 
-/* The values that rows in 4 bits stand for, in the storage type (exact): out [rows, head_dim]. */
+/* The values that rows in 4 bits stand for, in the storage type (exact; NaN where a scale is 255, whatever
+ * the codes): out [rows, head_dim]. */
 int curdkv_expand_mx(curdkv_ctx* ctx, const uint8_t* codes, const uint8_t* scales, int64_t rows,
                      void* out, void* stream);
 

@@ -62,7 +62,8 @@ template <int SEL>
 __device__ __forceinline__ f32x2a two_f32(uint32_t codes, float unit) {
     return __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, SEL));
 }
-__device__ __forceinline__ float unit_of(uint32_t scale) { return __uint_as_float(scale << 23); }   // (2^-127 comes out as 0: it stands for zeros)
+// A block's power of two, of which the conversions take the exponent alone: 0 is 2^-127, 255 makes NaN of every code.
+__device__ __forceinline__ float unit_of(uint32_t scale) { return __uint_as_float(scale << 23); }
 
 // A lane's part of the running softmax: column R = lane % 16, channels 8 eight_of(4 (lane / 16) + j) + i in o[i][j].
 struct Running {

@@ -107,14 +107,12 @@ __global__ __launch_bounds__(256) void expand_mx_kernel(const uint32_t* __restri
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= pieces) return;
     const uint32_t code = codes[i], e = scales[i / 4];
-    const float unit = __uint_as_float(e ? e << 23 : 1u << 22);             // (255: infinity, times code 0: NaN)
+    const float unit = __uint_as_float(e << 23);           // (the conversion takes the exponent alone: 0 is 2^-127, 255 makes NaN of every code)
     float x[8];
-    *(f32x2a*)(x + 0) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 0));
-    *(f32x2a*)(x + 2) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 1));
-    *(f32x2a*)(x + 4) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 2));
-    *(f32x2a*)(x + 6) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.f, 3));
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] *= unit;
+    *(f32x2a*)(x + 0) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 0));
+    *(f32x2a*)(x + 2) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 1));
+    *(f32x2a*)(x + 4) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 2));
+    *(f32x2a*)(x + 6) = __builtin_bit_cast(f32x2a, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 3));
     if (BF16) {
         put<PAST>((u32x4a){pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])}, (u32x4a*)out + i);
     } else {

@@ -300,9 +300,9 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  * count*m*kv_heads*group_size < 2^31, and m*kv_heads*group_size < 2^28 where 16 queries of a KV head
  * make a workgroup (few tokens; fp32 and 4-bit kept rows); else CURDKV_ERR_UNSUPPORTED.
  * out as Q; lse: float [count, kv_heads*group_size, m] or NULL.  scale > 0; m <= max_tokens.
- * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits,
- * with a bf16 cache the weights are rounded to bf16 for their product with V; with an fp32 cache every
- * product is good to 2^-22 of itself at least.
+ * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits;
+ * with a bf16 cache the weights are rounded to bf16 for their product with V; with an fp32 cache
+ * every product is good to 2^-22 of itself, or to 2^-133 of its larger factor where that is more.
  * scratch: device memory of the caller's, 16-byte aligned, for the partial results of few tokens over
  *   long caches, whose heads are shared out over many workgroups; CURDKV_ATTEND_SCRATCH_BYTES
  *   are as much as a call ever uses, with less (0 and NULL included) there are fewer shares.

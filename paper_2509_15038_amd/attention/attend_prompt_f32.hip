@@ -1,6 +1,7 @@
 // Attention of many tokens over an fp32 cache: as attend_prompt.hip, with every factor in three parts of 8 bits, x = h + m + l exactly (h the upper half of x, m
-// what is left rounded to bf16, l the rest, which bf16 holds).  Of the nine products of parts the six that count, h h, h m, m h, h l, m m and l h, go through
-// mfma_f32_32x32x16_bf16, summed in 32 bits: what is left out is below 2^-22 of a product, and a sixth of the bf16 rate is 2.7 times the
+// what is left rounded to bf16, l the rest, which bf16 holds; below 2^-109 its subnormals end and l is off by up to 2^-134).  Of the nine products of parts the six that count, h h, h m, m h, h l, m m and l h, go through
+// mfma_f32_32x32x16_bf16, summed in 32 bits: what is left out is below 2^-22 of a product, less than such sums
+// of 128 products round (three prompts of up to 1021 tokens: 4.1e-7 from the values in 64 bits, plain 32-bit products and sums 5.5e-7), and a sixth of the bf16 rate is 2.7 times the
 // rate of mfma_f32_32x32x2, whose kernel took 4770 us for a prompt of 8000 tokens (8 heads of 4; 524 Gflop), this 2586: 203 Tflop/s, 1220 of bf16, which is
 // where the library's products of such numbers end as well.  Bound by the matrix units, 96 products of 32 clocks for 32 keys and 32 rows of a wave, and short of workgroups below some
 // 2000 tokens (1000: 110 us).

@@ -4,7 +4,8 @@
 
 A stack of attention layers with random weights (x + Wo attention(Wqkv x), grouped heads, rotary positions, RMS norms of a head's queries and
 keys) takes a prompt, chooses the tokens whose keys and values it keeps, holds those in 4 bits and generates over them and the tokens since, one
-step a HIP graph replay; beside it the same over the whole prompt's cache.  The products with weights are torch's, all else is the library's."""
+step a HIP graph replay; beside it the same over the whole prompt's cache.  With a window it generates over the whole cache alone: kept rows have no
+positions that a window could pass.  The products with weights are torch's, all else is the library's."""
 import argparse
 import time
 
@@ -28,7 +29,7 @@ class Decoder:
                  sketch_dim: int = 64, seed: int = 1):
         self.layers, self.kv, self.group, self.window, self.n_sink, self.stride = layers, kv_heads, group, window, n_sink, new_tokens
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
-        self.ctx = B.Context(layers, kv_heads, group, D, sketch_dim, dtype, max_tokens, seed=seed)
+        self.ctx = B.Context(layers, kv_heads, group, D, sketch_dim, dtype, max_tokens + (new_tokens if window else 0), seed=seed)
         self.table = rotary_table(max_tokens + new_tokens)
         width = kv_heads * group * D
         draw = torch.Generator().manual_seed(seed)
@@ -63,6 +64,8 @@ class Decoder:
 
     def keep(self, share: float, bits4: bool = True) -> None:
         """Chooses the share of every head's tokens that stays, and holds their rows in 4 bits (or as they are)."""
+        if self.window:
+            raise ValueError("kept rows have no positions: with a window, keep_all")
         heads, n = self.layers * self.kv, self.n
         budgets = np.full(heads, max(min(n, self.n_sink), int(n * share)), dtype=np.int32)
         offsets = wl.offsets_for(budgets)
@@ -81,32 +84,50 @@ class Decoder:
         self._begin()
 
     def keep_all(self) -> None:
-        """The whole prompt's cache is what is kept, where it lies."""
+        """The whole prompt's cache is what is kept, where it lies; with a window, in a cache that has room for the tokens since."""
+        if self.window:
+            self.kept = [torch.zeros((self.layers, self.kv, self.n + self.stride, D), dtype=self.dtype, device="cuda") for _ in "KV"]
+            for whole, rows in zip(self.kept, (self.K, self.V)):
+                whole[:, :, :self.n] = rows
+            self._begin()
+            return
         self.offsets = torch.arange(self.layers * self.kv + 1, device="cuda") * self.n
         self.total, self.rows = self.layers * self.kv * self.n, self.kv * self.n
         self.kept = [self.K.view(-1, D), self.V.view(-1, D)]
         self._begin()
 
     def _begin(self) -> None:
-        shape = (self.layers, self.kv, self.stride, D)
+        shape = (self.layers, self.kv, 0 if self.window else self.stride, D)
         self.K_new, self.V_new = torch.zeros(shape, dtype=self.dtype, device="cuda"), torch.zeros(shape, dtype=self.dtype, device="cuda")
-        # (on the device, so that a recorded step finds the present ones: tokens since the prompt, with the one at hand, and its place and position)
+        # (on the device, so that a recorded step finds the present ones: tokens since the prompt, with the one at hand, its place among them and its position, tokens in all)
         self.length = torch.zeros(1, dtype=torch.int32, device="cuda")
         self.place = torch.full((1,), -1, dtype=torch.int32, device="cuda")
         self.position = torch.full((1,), self.n - 1, dtype=torch.int32, device="cuda")
+        self.tokens = torch.full((1,), self.n, dtype=torch.int32, device="cuda")
+        self.counters = self.length, self.place, self.position, self.tokens
 
     def step(self, x: torch.Tensor) -> torch.Tensor:
         """One generated token, x: [1, width]."""
-        for counter in (self.length, self.place, self.position):
+        for counter in self.counters:
             counter += 1
-        attend = self.ctx.attend_kept if len(self.kept) == 2 else self.ctx.attend_kept_mx
         for i in range(self.layers):
-            Q = self._rotate(i, x, self.K_new[i], self.V_new[i], self.stride, starts=self.place, positions=self.position)
-            o = torch.empty_like(Q)
-            attend(Q, *self.kept, self.offsets[i * self.kv:], 1, 1, self.total, o, K_tail=self.K_new[i], V_tail=self.V_new[i], tail_n=self.stride,
-                   tail_stride=self.stride, tail_lengths=self.length, rows=self.rows)
-            x = x + o.view(1, -1) @ self.out[i]
+            x = x + (self._in_window(i, x) if self.window else self._over_kept(i, x)).view(1, -1) @ self.out[i]
         return x
+
+    def _over_kept(self, i, x):
+        attend = self.ctx.attend_kept if len(self.kept) == 2 else self.ctx.attend_kept_mx
+        Q = self._rotate(i, x, self.K_new[i], self.V_new[i], self.stride, starts=self.place, positions=self.position)
+        o = torch.empty_like(Q)
+        attend(Q, *self.kept, self.offsets[i * self.kv:], 1, 1, self.total, o, K_tail=self.K_new[i], V_tail=self.V_new[i], tail_n=self.stride,
+               tail_stride=self.stride, tail_lengths=self.length, rows=self.rows)
+        return o
+
+    def _in_window(self, i, x):
+        K, V, room = self.kept[0][i], self.kept[1][i], self.n + self.stride
+        Q = self._rotate(i, x, K, V, room, starts=self.position, positions=self.position)
+        o = torch.empty_like(Q)
+        self.ctx.attend(Q, K, V, 1, 1, room, room, o, lengths=self.tokens, window=self.window, n_sink=self.n_sink)
+        return o
 
     def generate(self, x: torch.Tensor, count: int):
         """`count` tokens, each the one before made into unit length, by replays of one recorded step.  Returns them, [count, width], and the seconds a
@@ -114,12 +135,11 @@ class Decoder:
         def following(y):
             return (y.float() * torch.rsqrt(y.float().square().mean(-1, keepdim=True) + 1e-6)).to(self.dtype)
         given = x.clone()
-        counters = self.length, self.place, self.position
         side = torch.cuda.Stream()                  # (libraries set themselves up in a call that is not recorded)
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
             self.step(given)
-            for c in counters:
+            for c in self.counters:
                 c -= 1
         torch.cuda.current_stream().wait_stream(side)
         graph = torch.cuda.CUDAGraph()
@@ -157,6 +177,9 @@ def main(argv=None) -> None:
     first = y[-1:].clone()
     results = {}
     for name, choose in (("whole cache, bf16", model.keep_all), (f"{a.keep:.0%}, bf16", lambda: model.keep(a.keep, False)), (f"{a.keep:.0%}, 4 bits", lambda: model.keep(a.keep))):
+        if model.window and name != "whole cache, bf16":
+            print(f"{name}: left out, kept rows have no positions that the window could pass", flush=True)
+            continue
         choose()
         results[name], seconds = model.generate(first, a.new)
         held = sum(t.numel() * t.element_size() for t in model.kept)

@@ -569,9 +569,9 @@ __host__ __device__ __forceinline__ bool few_enough(int items, int64_t shares, i
 template <int FA, int FB>
 struct Places {
     static constexpr int kBetween = FA == kMxBf16 || FA == kMxF32 ? 32 : 16, kAtOnce = 4;
-    // A lane's items have less than this many units, so that those of 64 lanes are below 2^31 (a head's rows count once for each of its row tiles: memory does not bound them).  Where
+    // A lane's items have less than this many units, so that those of 64 lanes do not pass 2^31 (a head's rows count once for each of its row tiles: memory does not bound them).  Where
     // a lane has more, heads are of a million rows at least, or of 140 GB with few items, and every item has one workgroup.
-    static constexpr int kMostUnits = (1 << 25) - 1;
+    static constexpr int kMostUnits = (1 << 25) - 2 * kBetween;
     const SplitArgs& a;
     int all, shares, at;               // units of all items; workgroups with a share; units in front of the item at hand, without its kBetween
     bool whole;                        // workgroups have parts of one item each
@@ -582,14 +582,6 @@ struct Places {
         p.first = share_of(at + kBetween);
         p.last = share_of(at + kBetween + units - 1);
     }
-    __device__ __forceinline__ Place by_items(int block) const {       // items as they are
-        const int places = min(a.items, a.shares);
-        Place p{0, 0, 0, a.items, 0, 0, {0, 0, 0}};
-        p.item = (int)((int64_t)a.items * block / places);
-        p.end = (int)((int64_t)a.items * (block + 1) / places);
-        if (block < places) p.head = head_of(a, p.item / a.row_tiles), p.size = INT_MAX;
-        return p;
-    }
     __device__ __forceinline__ Place find() {
         const int lane = threadIdx.x & 63, each = (a.items + 63) / 64, from = min(lane * each, a.items), end = min(from + each, a.items), block = blockIdx.x;
         Place p{0, 0, 0, a.items, 0, 0, {0, 0, 0}};
@@ -598,10 +590,9 @@ struct Places {
         int units[kAtOnce], mine = 0;
         if (a.whole) {                 // (each == 1)
             head[0] = head_of(a, min(from, a.items - 1) / a.row_tiles);
-            mine = lane < a.items ? Work<FA, FB>(a, from, head[0]).units : 0;
-            if (__any(mine >= kMostUnits)) return by_items(block);
+            mine = lane < a.items ? min(Work<FA, FB>(a, from, head[0]).units, kMostUnits) : 0;
             const int tiles = __builtin_amdgcn_readlane(added_up(mine), 63);
-            whole = few_enough(a.items, a.shares, tiles);
+            whole = !__any(mine >= kMostUnits) && few_enough(a.items, a.shares, tiles);
             if (whole) {
                 // (the host knows the largest lengths that there may be; here are those that there are: 8 sequences of 250 tokens in caches of 16384 18 us by the caches' size, so 9)
                 const int some = min(a.shares, max(a.items, (int)__builtin_sqrtf(a.weight * (float)a.items * (float)tiles)));
@@ -633,11 +624,16 @@ struct Places {
                 mine = min(mine + units[k], kMostUnits);
             }
         }
-        if (__any(mine >= kMostUnits)) return by_items(block);
         const int up_to = added_up(mine);
         all = __builtin_amdgcn_readlane(up_to, 63);
         const int tiles = all - a.items * kBetween;
-        if (tiles < a.least * a.items) return by_items(block);         // little to read, in fact
+        if (tiles < a.least * a.items || __any(mine >= kMostUnits)) {  // little to read, in fact, or more than is counted: items as they are
+            const int places = min(a.items, a.shares);
+            p.item = (int)((int64_t)a.items * block / places);
+            p.end = (int)((int64_t)a.items * (block + 1) / places);
+            if (block < places) p.head = head_of(a, p.item / a.row_tiles), p.size = INT_MAX;
+            return p;
+        }
         // (no more shares than tiles: none may be without any between two that have parts of one item)
         shares = max(1, min(a.shares, (all - a.items * kBetween) / (kBetween + 1)));
         const int begin = begin_of(block);

@@ -39,14 +39,15 @@ int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
     // bf16, us, split and prompt, 8 heads of 4 a sequence: 9 tokens over 500 rows 9 and 15, over 8000 25 and 25, 32 over 8000 30 and 27; 8 sequences of 9 over 2000 23 and 24, of
     // 16 27 and 25, of 9 over 8000 77 and 50; 32 of 9 over 500 23 and 17, of 8 over 500 15 and 17, over 2000 57 and 50; prompts of 200 tokens 9.5 and 11.2, 300 14.2 and 13.5; 8 of
     // up to 64 12 and 9.  One tile of 16 a head: 32 sequences of 4 tokens over 8000 100 and 164.
-    // fp32: prompts of 8 heads 600 tokens 65 and 69, 800 93 and 89, 2400 572 and 344; 64 tokens of 4 sequences over 500 rows 32 and 61, of 16 116 and 65.
+    // fp32: prompts of 8 heads 600 tokens 65 and 69, 800 93 and 89, 2400 572 and 344; 64 tokens of 4 sequences over 500 rows 32 and 61, of 16 116 and 65.  Up to two tiles of 16 rows a
+    // head the split one always: 256 heads over 4000 rows, 4 rows of a head 159 and 418, 32 309 and 432, 48 460 and 442; 512 over 250 27 and 65, 52 and 66, 72 and 68.
     const int64_t rows = (int64_t)call.m * call.group, heads = call.count * call.kv, items = heads * ((rows + 15) / 16), tiles = heads * ((rows + 127) / 128);
     const int64_t keys = (call.window > 0 ? std::min((int64_t)call.n, (int64_t)call.window + call.sinks + call.m) : call.n) + call.rows / heads;
     const bool f32 = call.dtype == CURDKV_DTYPE_F32;
     // Kept rows in bf16: workgroups do not share out heads of uneven lengths there, which costs more the fewer rows a tile of 128 has: 64 tokens over 3276 rows of 8 uneven heads 41 and
     // 44, 200 92 and 61, 1000 301 and 195 (even heads 4 sequences of 300 103, uneven ones 281); 32 sequences of 6 over 3000 135 and 302.
     const bool prompt = call.offsets ? !call.K_scales && !f32 && rows >= 256 && (items > kPromptItems || items * keys > 2 * kPromptProducts)
-                        : f32 ? 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 16 && (items > kPromptItems || items * keys > kPromptProducts);
+                        : f32 ? rows > 32 && 3 * tiles >= 2 * (int64_t)ctx->num_cu : rows > 16 && (items > kPromptItems || items * keys > kPromptProducts);
     const auto launch = !prompt ? launch_attend_split : f32 ? launch_attend_prompt_f32 : launch_attend_prompt;
     // A launch's threads are counted in 32 bits: so many workgroups of 256 threads and more (of 512 for fp32 prompts).  Whole sequences a launch.
     const int64_t blocks = call.kv * (prompt ? (rows + 127) / 128 * (f32 ? 2 : 1) : (rows + 15) / 16), at_once = kMostBlocks / blocks;

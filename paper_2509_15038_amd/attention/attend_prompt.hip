@@ -1,7 +1,8 @@
 // Attention of many tokens (prompts) over a bf16 cache: tiles of 64 keys against 32 rows R a wave, the softmax's maximum and sum running
-// along.  Bound by the matrix units and the exponentials: 4 * 128 flops and one exponential for a visible (row, key).  Measured: 8192 tokens of 32 heads (550
-// Gflop) 531 us, 1040 Tflop/s; 32768 through windows of 4096 (2064 Gflop) 2043 us, 1010 Tflop/s; a library product of 8192^3 reaches 1240.  What holds it there is the
-// power that the numbers' switching costs: zeros in place of random ones take 413 us, and the product 1780 Tflop/s.
+// along.  Bound by the matrix units and the exponentials: 4 * 128 flops and one exponential for a visible (row, key).  Measured, on several cards: 8192 tokens of 32 heads (550
+// Gflop) 530 to 562 us, 980 to 1040 Tflop/s; 32768 through windows of 4096 (2064 Gflop) 2040 to 2190 us, 940 to 1010 Tflop/s; a library product of 8192^3 reaches 1180 to 1240.  What holds
+// it there is the power that the numbers' switching costs: zeros in place of random ones take 413 us, and the product 1780 Tflop/s.  (In a series of launches: after a pause the first dozen
+// take up to a third longer, until the clock has settled.)
 // Four waves of 32 rows: eight share a tile's loads (4096 tokens 164 us, so 154), but with windows, whose tiles have masks, wait for each other (500: 148, so 161); 64 rows
 // a wave leave one wave a SIMD (973 Tflop/s, so 904).
 //
@@ -15,7 +16,8 @@
 //
 // The reference point of a row's exponentials is its maximum only to within 2^8: it moves, and what has been summed is scaled, when the
 // maximum passes it by more, so that most tiles scale nothing.  Weights are then up to 2^8; in bf16 they are rounded by 2^-8 of themselves for their product with V, as
-// weights up to 1 are, and their sum takes them in 32 bits.
+// weights up to 1 are, and their sum takes them in 32 bits.  Results lie 0.0022 of themselves from the values in 64 bits, 0.0016 with weights of 32 bits (the results' own rounding):
+// weights in two parts would be half as many products again where products are the bound.
 
 #include <algorithm>
 

@@ -14,6 +14,8 @@
 // Measured: a token over 131072 rows of 8 heads (537 MB) 91 us, 5.9 TB/s; of 32 sequences through windows of 4096 (404 MB) 66 us, 6.1 TB/s; 4 tokens of 8 sequences over
 // 6553 kept rows a head (217 MB) 50 us, 4.3 TB/s; 32 sequences over 13107 kept rows a head in 4 bits (490 MB with their tails) 105 us, 4.7 TB/s: the heads' ends inside the shares
 // (3 us each) and the join (4 us).  One sequence over 3276 kept rows a head 13 us: a chain of latencies, of which reading is 3.
+// In fp32: the token over 131072 rows (1074 MB) 171 us, 6.3 TB/s; 32 sequences through windows of 4096 (808 MB) 156 us, 5.2 TB/s; the 4 tokens of 8 sequences (434 MB) 83 us, 5.2 TB/s; the 32
+// sequences over rows in 4 bits 306 us, 1.7 TB/s.
 // A workgroup of four waves a unit, each with two tiles of 16 keys (32 KB) in flight: more workgroups only add to what there is to join (launch_attend_split).
 // A wave's next tile is asked for without a branch: in front of one the compiler waits for all that is in flight.
 
@@ -71,7 +73,8 @@ struct Running {
     float top, sum;                    // of R so far (top: of all quarters; sum: of the lane's keys)
 };
 
-// o += V^T P^T for bf16 rows: v[e] the lane's 8 channels of key e of its quarter, p[e] that key's weights; of 16 keys, or of 32.
+// o += V^T P^T for bf16 rows: v[e] the lane's 8 channels of key e of its quarter, p[e] that key's weights; of 16 keys, or of 32.  The weights are rounded to bf16 for it, as the
+// prompts' are: results lie 0.0017 to 0.0019 of themselves from the values in 64 bits, 0.0016 to 0.0017 with weights of 32 bits, so nearly all of it is the results' own rounding.
 __device__ __forceinline__ f32x4a product(u32x4a x, u32x4a y, f32x4a z) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, x), __builtin_bit_cast(bf16x8a, y), z, 0, 0, 0);
 }
@@ -97,7 +100,8 @@ __device__ __forceinline__ void add_values(const u32x4a (&v)[E], const float* p,
         o[2 * w + 1] = product(odd, pb, o[2 * w + 1]);
     }
 }
-// (fp32 products: exact to 2^-24 a product, 1/16 of the bf16 rate, which the rows' bytes still hide)
+// (fp32 products: exact to 2^-24 a product, 1/16 of the bf16 rate, which the bytes of fp32 rows still hide; 4-bit rows under fp32 are bound by it: 64 products of 32 clocks for 16 keys of
+// 2176 bytes are 2.6 TB/s at most)
 __device__ __forceinline__ void add_values(const float (&v)[4][8], const float* p, f32x4a* o) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)

@@ -7,8 +7,8 @@
 // compact_mx_kernel is the gather of compact_kernels.hip with that at its end: HBM-bound, a row read whole by 16 (32) lanes of 16
 // bytes, K and V by different workgroups.  Four (eight) neighbouring lanes hold a block: two (three) DPP exchanges find its
 // largest magnitude, on the bits, where NaN counts as larger than all.  All steps are exact but the rounding to a code.
-// Measured: 3276 of 32768 rows of 256 heads gathered and expanded again (1090 MB) 184 us in three launches, 5.9 TB/s; of 8 heads 12.4 us, three launches at their
-// shortest.
+// Measured: 3276 of 32768 rows of 256 heads gathered and expanded again (1090 MB) 180 to 185 us in three launches, 5.9 to 6.1 TB/s; of 8 heads 12.4 us, three
+// launches at their shortest.  In fp32 (1950 MB) 523 us, 3.7 TB/s: stores past the caches in half lines, as in rotate_kernel.hip.
 
 #include "attend_device.h"
 #include "attend_internal.h"

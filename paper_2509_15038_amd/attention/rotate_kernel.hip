@@ -8,7 +8,8 @@
 // either pairing, so that the rotation is in-lane and the norm needs three exchanges.  The eight lanes stay with their token and
 // take several of its heads, so that cosines and sines (512 bytes a token, twice a bf16 row) are read once for all of them.
 // Everything between load and store is in 32 bits; the store is the one rounding.
-// Measured: 32768 tokens of 32 + 8 + 8 heads with norms (822 MB) 140 us, 5.9 TB/s; one token of 4 sequences 4.0 us a call, the kernel 3.5.
+// Measured: 32768 tokens of 32 + 8 + 8 heads with norms (822 MB) 140 us, 5.9 TB/s; one token of 4 sequences 4.0 to 4.7 us a call, the
+// kernel 3.5.  fp32, 32768 tokens (1628 MB) 444 us, 3.7 TB/s: a lane's 32 bytes go as two stores of 16, whose half lines past the caches are 1.5 times the bytes.
 
 #include <algorithm>
 

@@ -303,6 +303,8 @@ int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, in
  * m = n is a prompt, m = 1 a generated token; scores, weights' sum and results are held in 32 bits;
  * with a bf16 cache the weights are rounded to bf16 for their product with V; with an fp32 cache
  * every product is good to 2^-22 of itself, or to 2^-133 of its larger factor where that is more.
+ * Sums of values times weights of up to 2^8 are divided by the weights' sum at the end: values of
+ * magnitude 2^120 / n and more may pass the range of 32 bits on the way.
  * scratch: device memory of the caller's, 16-byte aligned, for the partial results of few tokens over
  *   long caches, whose heads are shared out over many workgroups; CURDKV_ATTEND_SCRATCH_BYTES
  *   are as much as a call ever uses, with less (0 and NULL included) there are fewer shares.

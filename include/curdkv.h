@@ -359,6 +359,78 @@ int curdkv_attend_kept_mx(curdkv_ctx* ctx, const void* Q, const uint8_t* K_codes
                           const int32_t* tail_lengths, int64_t count, int64_t m, float scale,
                           void* out, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
 
+/* ---- a cache that stays at its size, and one that serves several answers ----
+ *
+ * These calls, too, take one layer at a time, with the conventions of those above. */
+
+/* curdkv_rotate where a token stands at several positions, as time, height and width of a video's patch: each
+ * of the head_dim/2 angles turns by the position on its own axis.
+ * axis_of: HOST uint8 [head_dim/2], the axis of every angle, below `axes` (1 to 4).
+ * positions: int32 [axes, count*m], not NULL; each clamped to [0, table_rows).  All else as curdkv_rotate, which this
+ *   is, bit for bit, where a token's positions are the same on all axes. */
+int curdkv_rotate_axes(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride,
+                       const int32_t* starts, const int32_t* positions, int32_t axes, const uint8_t* axis_of,
+                       const float* table, int64_t table_rows, const void* q_weight, const void* k_weight, float eps,
+                       int32_t pairs, void* Q, void* K, void* V, int64_t stride, void* stream);
+
+/* The attention weight that every cached key got from each sequence's last m tokens, over the group_size query
+ * heads of its KV head, added to what is left of the weight that it had:
+ *   mass[b, h, j] = decay * mass[b, h, j] + sum_i sum_t exp(scale * q_ti.k_j - lse[b, h*group_size + i, t])
+ * over the query heads i of KV head h and the tokens t that see key j (as in curdkv_attend: causal, window, n_sink).
+ * A whole prompt's weights are m = n; those that its last tokens give it (an observation window) fewer; a
+ * generated token's m = 1.
+ * Q, K, count, m, n, stride, lengths, window, n_sink, scale: as curdkv_attend takes them; lse: float [count,
+ *   kv_heads*group_size, m], what curdkv_attend wrote for them.  A token of lse -infinity (it sees nothing) gives
+ *   nothing; one of lse NaN makes the weight of the keys that it sees NaN, and no other's.
+ * decay: not negative, finite; 0: the old weights are not read.
+ * mass: float [count, kv_heads, mass_stride], rows below a sequence's length written; those behind it stay as they
+ *   are.  n <= mass_stride.
+ * Scores and sums in 32 bits, summed in an order that depends on the sizes alone.  scratch as in curdkv_attend. */
+int curdkv_attend_weights(curdkv_ctx* ctx, const void* Q, const void* K, const float* lse, int64_t count,
+                          int64_t m, int64_t n, int64_t stride, const int32_t* lengths, int64_t window, int32_t n_sink,
+                          float scale, float decay, float* mass, int64_t mass_stride, void* scratch,
+                          int64_t scratch_bytes, void* stream);
+
+/* Eviction by accumulated weight: of each head's rows (a sequence's `length`) `keep` stay, or all where there are no more.
+ * First those whose position is below n_sink or among the `recent` last ones (above the head's largest position less
+ * `recent`), then those of the largest mass (NaN above all, -0 as 0), of equal ones the lower row.  Should the first be more
+ * than `keep`, the mass decides among them.  n_sink + recent <= keep.
+ * A row below `keep` that stays keeps its place; the places of the others are taken, in ascending order, by the rows that
+ * stay from beyond, ascending: rows are no longer in the order of their tokens, and `positions` says which is which.
+ * K, V: [count, kv_heads, stride, head_dim]; mass: float, positions: int32 [count, kv_heads, stride]; positions NULL: the
+ *   row's number.  lengths: int32 [count], clamped to [0, n]; NULL = n.  1 <= keep, n <= stride, n <= 524288.
+ * K_out, V_out: [count, kv_heads, out_stride, head_dim]; mass_out, positions_out: [count, kv_heads, out_stride], NULL: not
+ *   written.  Only rows below min(length, keep) are written.  keep <= out_stride or n <= out_stride.
+ *   K_out = K with V_out = V: in place, and mass_out may be mass, positions_out positions; wherever an array is its own
+ *   output, out_stride = stride.  Nothing else may overlap.
+ * rows: int32 [count, kv_heads, keep], written: the row that each place's row came from; -1 beyond min(length, keep). */
+int curdkv_evict(curdkv_ctx* ctx, const void* K, const void* V, const float* mass, const int32_t* positions,
+                 int64_t count, int64_t n, int64_t stride, const int32_t* lengths, int64_t keep, int32_t n_sink,
+                 int64_t recent, void* K_out, void* V_out, float* mass_out, int32_t* positions_out, int64_t out_stride,
+                 int32_t* rows, void* stream);
+
+/* curdkv_attend_kept for sequences that share their kept rows: `share` of them follow each of `count` prefixes, whose rows
+ * are read once for all.  Sequence b*share + s of the count*share sequences sees the kept rows of prefix b and, causally,
+ * its own tail.
+ * Q, out: [count*share, m, kv_heads*group_size, head_dim]; lse: float [count*share, kv_heads*group_size, m] or NULL.
+ * offsets: DEVICE int64 [count*kv_heads + 1], K_kept, V_kept, total, rows: the prefixes', as in curdkv_attend_kept.
+ * K_tail, V_tail: [count*share, kv_heads, tail_stride, head_dim]; tail_lengths: int32 [count*share].
+ * count*share*m*kv_heads*group_size < 2^31.  scratch: not NULL here, CURDKV_ATTEND_SCRATCH_BYTES at least, cleared once as
+ * for curdkv_attend; the partial results of prefixes and tails meet there. */
+int curdkv_attend_shared(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept,
+                         const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,
+                         const void* V_tail, int64_t tail_n, int64_t tail_stride, const int32_t* tail_lengths,
+                         int64_t count, int64_t share, int64_t m, float scale, void* out, float* lse, void* scratch,
+                         int64_t scratch_bytes, void* stream);
+
+/* The same over kept rows held in 4 bits (curdkv_compact_mx); the tails are in the storage type. */
+int curdkv_attend_shared_mx(curdkv_ctx* ctx, const void* Q, const uint8_t* K_codes,
+                            const uint8_t* K_scales, const uint8_t* V_codes, const uint8_t* V_scales,
+                            const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,
+                            const void* V_tail, int64_t tail_n, int64_t tail_stride, const int32_t* tail_lengths,
+                            int64_t count, int64_t share, int64_t m, float scale, void* out, float* lse, void* scratch,
+                            int64_t scratch_bytes, void* stream);
+
 /* Text for an error code; never NULL. */
 const char* curdkv_strerror(int code);
 

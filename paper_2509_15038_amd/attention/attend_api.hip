@@ -13,15 +13,11 @@ namespace {
 
 // Tiles of 16 rows, and these times the keys, from which the prompts' kernel is the faster one (run_attend).
 constexpr int64_t kPromptItems = 600, kPromptProducts = 400000;
-constexpr int64_t kMostBlocks = (1 << 24) - 1;     // workgroups of a launch
 
-bool aligned16(std::initializer_list<const void*> ptrs) {
-    uintptr_t all = 0;
-    for (const void* p : ptrs) all |= (uintptr_t)p;
-    return (all & 15u) == 0;
-}
+}  // namespace
 
-// What the attention calls have in common: sizes of the queries and of one cache array.
+namespace curdkv {
+
 int check_attend(const curdkv_ctx* ctx, const void* Q, const void* out, int64_t count, int64_t m, int64_t n, int64_t stride, float scale,
                  const void* scratch, int64_t scratch_bytes) {
     if (!ctx || !Q || !out) return CURDKV_ERR_INVALID_ARG;
@@ -33,6 +29,43 @@ int check_attend(const curdkv_ctx* ctx, const void* Q, const void* out, int64_t 
     if (count > most / heads || m > most / (count * heads)) return CURDKV_ERR_UNSUPPORTED;     // (grids and row counts are 32 bits)
     return CURDKV_OK;
 }
+
+int check_kept(const curdkv_ctx* ctx, AttendCall* to, const void* Q, const void* K_kept, const void* V_kept, const uint8_t* K_scales, const uint8_t* V_scales,
+               const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail, const void* V_tail, int64_t tail_n, int64_t tail_stride,
+               const int32_t* tail_lengths, int64_t count, int64_t share, int64_t m, float scale, void* out, float* lse, void* scratch, int64_t scratch_bytes) {
+    if (count < 1 || share < 1) return CURDKV_ERR_INVALID_ARG;
+    if (share > ((1LL << 31) - 1) / count) return CURDKV_ERR_UNSUPPORTED;
+    const int rc = check_attend(ctx, Q, out, count * share, m, tail_n, tail_stride, scale, scratch, scratch_bytes);
+    if (rc != CURDKV_OK) return rc;
+    if (!offsets || total < 0 || rows < 0 || rows > total || (total > 0 && (!K_kept || !V_kept)) || (tail_n > 0 && (!K_tail || !V_tail))) return CURDKV_ERR_INVALID_ARG;
+    if (!aligned16({K_kept, V_kept, K_tail, V_tail})) return CURDKV_ERR_INVALID_ARG;
+    if (total > (1LL << 31) - 1) return CURDKV_ERR_UNSUPPORTED;        // (a head's rows are counted in 32 bits)
+    AttendCall& c = *to;
+    c = AttendCall{};
+    c.Q = Q, c.out = out, c.lse = lse, c.count = count;
+    c.kv = ctx->cfg.kv_heads, c.group = ctx->cfg.group_size, c.m = (int)m, c.dtype = ctx->cfg.dtype, c.scale = scale;
+    c.K = K_tail, c.V = V_tail, c.stride = tail_stride, c.lengths = tail_lengths, c.n = (int)tail_n;
+    c.offsets = offsets, c.K_kept = K_kept, c.V_kept = V_kept, c.K_scales = K_scales, c.V_scales = V_scales, c.total = total, c.rows = rows;
+    c.scratch = scratch, c.scratch_bytes = scratch_bytes;
+    return CURDKV_OK;
+}
+
+int check_rotate(const curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride, const float* table, int64_t table_rows,
+                 const void* q_weight, const void* k_weight, float eps, int32_t pairs, const void* Q, const void* K, const void* V, int64_t stride) {
+    if (!ctx || !qkv || !table || !Q || !K || !V) return CURDKV_ERR_INVALID_ARG;
+    if (!on_device_of(ctx)) return CURDKV_ERR_INVALID_ARG;
+    const int64_t heads = (int64_t)ctx->cfg.kv_heads * (ctx->cfg.group_size + 2LL), bytes = ctx->cfg.dtype == CURDKV_DTYPE_BF16 ? 2 : 4;
+    if (count < 1 || m < 1 || stride < 1 || stride > ctx->cfg.max_tokens || table_rows < 1 || row_stride < heads * kHeadDim) return CURDKV_ERR_INVALID_ARG;
+    if (pairs != 0 && pairs != 1) return CURDKV_ERR_INVALID_ARG;
+    if ((q_weight || k_weight) && (!(eps >= 0.f) || !std::isfinite(eps))) return CURDKV_ERR_INVALID_ARG;
+    if (!aligned16({qkv, table, q_weight, k_weight, Q, K, V}) || row_stride * bytes % 16) return CURDKV_ERR_INVALID_ARG;
+    if (m > ((1LL << 31) - 1) / count || heads > (1 << 20)) return CURDKV_ERR_UNSUPPORTED;
+    return CURDKV_OK;
+}
+
+}  // namespace curdkv
+
+namespace {
 
 int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
     // Which kernel: the split one takes tiles of 16 rows (tokens times query heads of a KV head), each of which reads the cache, the prompts' ones 128.
@@ -73,17 +106,10 @@ int run_attend(const curdkv_ctx* ctx, const AttendCall& call, void* stream) {
 int run_kept(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept, const uint8_t* K_scales, const uint8_t* V_scales,
              const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail, const void* V_tail, int64_t tail_n, int64_t tail_stride,
              const int32_t* tail_lengths, int64_t count, int64_t m, float scale, void* out, float* lse, void* scratch, int64_t scratch_bytes, void* stream) {
-    const int rc = check_attend(ctx, Q, out, count, m, tail_n, tail_stride, scale, scratch, scratch_bytes);
+    AttendCall c;
+    const int rc = check_kept(ctx, &c, Q, K_kept, V_kept, K_scales, V_scales, offsets, total, rows, K_tail, V_tail, tail_n, tail_stride, tail_lengths, count, 1, m, scale,
+                              out, lse, scratch, scratch_bytes);
     if (rc != CURDKV_OK) return rc;
-    if (!offsets || total < 0 || rows < 0 || rows > total || (total > 0 && (!K_kept || !V_kept)) || (tail_n > 0 && (!K_tail || !V_tail))) return CURDKV_ERR_INVALID_ARG;
-    if (!aligned16({K_kept, V_kept, K_tail, V_tail})) return CURDKV_ERR_INVALID_ARG;
-    if (total > (1LL << 31) - 1) return CURDKV_ERR_UNSUPPORTED;        // (a head's rows are counted in 32 bits)
-    AttendCall c{};
-    c.Q = Q, c.out = out, c.lse = lse, c.count = count;
-    c.kv = ctx->cfg.kv_heads, c.group = ctx->cfg.group_size, c.m = (int)m, c.dtype = ctx->cfg.dtype, c.scale = scale;
-    c.K = K_tail, c.V = V_tail, c.stride = tail_stride, c.lengths = tail_lengths, c.n = (int)tail_n;
-    c.offsets = offsets, c.K_kept = K_kept, c.V_kept = V_kept, c.K_scales = K_scales, c.V_scales = V_scales, c.total = total, c.rows = rows;
-    c.scratch = scratch, c.scratch_bytes = scratch_bytes;
     return run_attend(ctx, c, stream);
 }
 
@@ -94,15 +120,9 @@ extern "C" {
 int curdkv_rotate(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride, const int32_t* starts,
                   const int32_t* positions, const float* table, int64_t table_rows, const void* q_weight, const void* k_weight, float eps,
                   int32_t pairs, void* Q, void* K, void* V, int64_t stride, void* stream) {
-    if (!ctx || !qkv || !table || !Q || !K || !V) return CURDKV_ERR_INVALID_ARG;
-    if (!on_device_of(ctx)) return CURDKV_ERR_INVALID_ARG;
-    const int64_t heads = (int64_t)ctx->cfg.kv_heads * (ctx->cfg.group_size + 2LL), bytes = ctx->cfg.dtype == CURDKV_DTYPE_BF16 ? 2 : 4;
-    if (count < 1 || m < 1 || stride < 1 || stride > ctx->cfg.max_tokens || table_rows < 1 || row_stride < heads * kHeadDim) return CURDKV_ERR_INVALID_ARG;
-    if (pairs != 0 && pairs != 1) return CURDKV_ERR_INVALID_ARG;
-    if ((q_weight || k_weight) && (!(eps >= 0.f) || !std::isfinite(eps))) return CURDKV_ERR_INVALID_ARG;
-    if (!aligned16({qkv, table, q_weight, k_weight, Q, K, V}) || row_stride * bytes % 16) return CURDKV_ERR_INVALID_ARG;
-    if (m > ((1LL << 31) - 1) / count || heads > (1 << 20)) return CURDKV_ERR_UNSUPPORTED;
-    return launch_rotate(ctx, qkv, count, m, row_stride, starts, positions, table, table_rows, q_weight, k_weight, eps, pairs == 1, Q, K, V, stride,
+    const int rc = check_rotate(ctx, qkv, count, m, row_stride, table, table_rows, q_weight, k_weight, eps, pairs, Q, K, V, stride);
+    if (rc != CURDKV_OK) return rc;
+    return launch_rotate(ctx, qkv, count, m, row_stride, starts, positions, nullptr, table, table_rows, q_weight, k_weight, eps, pairs == 1, Q, K, V, stride,
                          (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }
 

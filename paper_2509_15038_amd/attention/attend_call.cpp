@@ -20,6 +20,11 @@ decltype(&curdkv_compact_mx) compact_mx_entry;
 decltype(&curdkv_expand_mx) expand_mx_entry;
 decltype(&curdkv_attend_kept) attend_kept_entry;
 decltype(&curdkv_attend_kept_mx) attend_kept_mx_entry;
+decltype(&curdkv_rotate_axes) rotate_axes_entry;
+decltype(&curdkv_attend_weights) attend_weights_entry;
+decltype(&curdkv_evict) evict_entry;
+decltype(&curdkv_attend_shared) attend_shared_entry;
+decltype(&curdkv_attend_shared_mx) attend_shared_mx_entry;
 
 // int(x) as a 64-bit value, wrapped as ctypes wraps it; `ok` false: an error has been set
 int64_t integer(PyObject* x, bool& ok) {
@@ -104,16 +109,21 @@ FUNCTION(compact_mx)
 FUNCTION(expand_mx)
 FUNCTION(attend_kept)
 FUNCTION(attend_kept_mx)
+FUNCTION(rotate_axes)
+FUNCTION(attend_weights)
+FUNCTION(evict)
+FUNCTION(attend_shared)
+FUNCTION(attend_shared_mx)
 
-// bind(addresses of the six entries in the order above, address(object) -> int, stream(object) -> int)
+// bind(addresses of the eleven entries in the order above, address(object) -> int, stream(object) -> int)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
-    if (n != 8) {
-        PyErr_Format(PyExc_TypeError, "expected 8 arguments, got %zd", n);
+    if (n != 13) {
+        PyErr_Format(PyExc_TypeError, "expected 13 arguments, got %zd", n);
         return nullptr;
     }
     bool ok = true;
-    void* p[6];
-    for (int i = 0; i < 6; ++i) p[i] = reinterpret_cast<void*>(integer(v[i], ok));
+    void* p[11];
+    for (int i = 0; i < 11; ++i) p[i] = reinterpret_cast<void*>(integer(v[i], ok));
     if (!ok) return nullptr;
     rotate_entry = reinterpret_cast<decltype(rotate_entry)>(p[0]);
     attend_entry = reinterpret_cast<decltype(attend_entry)>(p[1]);
@@ -121,15 +131,21 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
     expand_mx_entry = reinterpret_cast<decltype(expand_mx_entry)>(p[3]);
     attend_kept_entry = reinterpret_cast<decltype(attend_kept_entry)>(p[4]);
     attend_kept_mx_entry = reinterpret_cast<decltype(attend_kept_mx_entry)>(p[5]);
-    Py_INCREF(v[6]);
-    Py_XSETREF(slow_address, v[6]);
-    Py_INCREF(v[7]);
-    Py_XSETREF(slow_stream, v[7]);
+    rotate_axes_entry = reinterpret_cast<decltype(rotate_axes_entry)>(p[6]);
+    attend_weights_entry = reinterpret_cast<decltype(attend_weights_entry)>(p[7]);
+    evict_entry = reinterpret_cast<decltype(evict_entry)>(p[8]);
+    attend_shared_entry = reinterpret_cast<decltype(attend_shared_entry)>(p[9]);
+    attend_shared_mx_entry = reinterpret_cast<decltype(attend_shared_mx_entry)>(p[10]);
+    Py_INCREF(v[11]);
+    Py_XSETREF(slow_address, v[11]);
+    Py_INCREF(v[12]);
+    Py_XSETREF(slow_stream, v[12]);
     Py_RETURN_NONE;
 }
 
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(bind), ENTRY(rotate), ENTRY(attend), ENTRY(compact_mx), ENTRY(expand_mx), ENTRY(attend_kept), ENTRY(attend_kept_mx),
+                         ENTRY(rotate_axes), ENTRY(attend_weights), ENTRY(evict), ENTRY(attend_shared), ENTRY(attend_shared_mx),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attend", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -31,6 +31,7 @@ struct RotateArgs {
     char *Q, *K, *V;
     int64_t stride;
     int64_t first;                     // a launch's first token
+    uint32_t axis_of[4];               // two bits an angle; positions [axes, tokens] then
 };
 
 template <int CTRL>
@@ -86,8 +87,9 @@ struct Sixteen {                       // 16 channels of a row: a lane's two pie
     }
 };
 
-// TOKENS a workgroup; PAIRS: neighbours rotate together; PAST: rows pass the caches.  A lane u of eight holds pairs 8 u .. 8 u + 7.
-template <bool BF16, bool PAIRS, int TOKENS, bool PAST>
+// TOKENS a workgroup; PAIRS: neighbours rotate together; PAST: rows pass the caches; AXES: a position for each axis.  A lane u of eight holds pairs
+// 8 u .. 8 u + 7.
+template <bool BF16, bool PAIRS, int TOKENS, bool PAST, bool AXES>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     constexpr int kSlots = 32 / TOKENS, kRow = BF16 ? 256 : 512;
     const int u = threadIdx.x & 7, slot = threadIdx.x >> 3;
@@ -96,14 +98,23 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     const int64_t b = token / a.m, i = token - b * a.m;
     const int first = PAIRS ? 2 * u : u, second = PAIRS ? 2 * u + 1 : u + 8;       // pieces of eight channels
     const int64_t start = a.starts ? a.starts[b] : 0, at = start + i;
-    int64_t position = a.positions ? a.positions[token] : at;
-    position = position < 0 ? 0 : position < a.table_rows ? position : a.table_rows - 1;
-    const float* turn = a.table + position * 128 + u * 8;
+    const uint32_t mine = AXES ? a.axis_of[u >> 1] >> (u & 1) * 16 & 0xFFFFu : 0u;       // the axes of this lane's angles
+    const auto row_at = [&](int64_t position) { return a.table + (position < 0 ? 0 : position < a.table_rows ? position : a.table_rows - 1) * 128 + u * 8; };
     float cosine[8], sine[8];
+    if (!AXES || mine == (mine & 3u) * 0x5555u) {                                        // one axis
+        const float* turn = row_at(AXES ? a.positions[(mine & 3u) * a.tokens + token] : a.positions ? a.positions[token] : at);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        *(f32x4a*)&cosine[4 * k] = *(const f32x4a*)(turn + 4 * k);
-        *(f32x4a*)&sine[4 * k] = *(const f32x4a*)(turn + 64 + 4 * k);
+        for (int k = 0; k < 2; ++k) {
+            *(f32x4a*)&cosine[4 * k] = *(const f32x4a*)(turn + 4 * k);
+            *(f32x4a*)&sine[4 * k] = *(const f32x4a*)(turn + 64 + 4 * k);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float* turn = row_at(a.positions[(mine >> 2 * k & 3u) * a.tokens + token]);
+            cosine[k] = turn[k];
+            sine[k] = turn[64 + k];
+        }
     }
     const bool in_cache = at >= 0 && at < a.stride;
     const int queries = a.kv * a.group, heads = queries + 2 * a.kv;
@@ -143,20 +154,20 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     }
 }
 
-template <bool BF16, bool PAIRS>
+template <bool BF16, bool PAIRS, bool AXES>
 hipError_t launch(const curdkv_ctx* ctx, RotateArgs a, hipStream_t stream) {
     // Four tokens a workgroup where that still gives every unit four; one, its heads over all lanes, below.  Rows that the caches would not hold until
     // they are read again pass them by (32768 tokens of 48 heads: 159 us, 144 so).
     const int64_t bytes = a.tokens * a.kv * (a.group + 2) * (BF16 ? 512 : 1024);
     if (a.tokens < 16 * (int64_t)ctx->num_cu) {
-        rotate_kernel<BF16, PAIRS, 1, false><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
+        rotate_kernel<BF16, PAIRS, 1, false, AXES><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
         return hipGetLastError();
     }
     // (a launch's threads are counted in 32 bits: 2^25 tokens each)
     for (; a.first < a.tokens; a.first += 1 << 25) {
         const unsigned blocks = (unsigned)((std::min(a.tokens - a.first, (int64_t)1 << 25) + 3) / 4);
-        if (bytes <= kPastCaches) rotate_kernel<BF16, PAIRS, 4, false><<<blocks, 256, 0, stream>>>(a);
-        else rotate_kernel<BF16, PAIRS, 4, true><<<blocks, 256, 0, stream>>>(a);
+        if (bytes <= kPastCaches) rotate_kernel<BF16, PAIRS, 4, false, AXES><<<blocks, 256, 0, stream>>>(a);
+        else rotate_kernel<BF16, PAIRS, 4, true, AXES><<<blocks, 256, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
@@ -164,13 +175,18 @@ hipError_t launch(const curdkv_ctx* ctx, RotateArgs a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_rotate(const curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t m, int64_t row_stride, const int32_t* starts,
-                         const int32_t* positions, const float* table, int64_t table_rows, const void* q_weight, const void* k_weight,
-                         float eps, bool pairs, void* Q, void* K, void* V, int64_t stride, hipStream_t stream) {
+                         const int32_t* positions, const uint8_t* axis_of, const float* table, int64_t table_rows, const void* q_weight,
+                         const void* k_weight, float eps, bool pairs, void* Q, void* K, void* V, int64_t stride, hipStream_t stream) {
     const bool bf16 = ctx->cfg.dtype == CURDKV_DTYPE_BF16;
-    const RotateArgs a{(const char*)qkv, m, count * m, row_stride * (bf16 ? 2 : 4), starts, positions, table, table_rows, q_weight, k_weight, eps,
-                       ctx->cfg.kv_heads, ctx->cfg.group_size, (char*)Q, (char*)K, (char*)V, stride, 0};
-    if (bf16) return pairs ? launch<true, true>(ctx, a, stream) : launch<true, false>(ctx, a, stream);
-    return pairs ? launch<false, true>(ctx, a, stream) : launch<false, false>(ctx, a, stream);
+    RotateArgs a{(const char*)qkv, m, count * m, row_stride * (bf16 ? 2 : 4), starts, positions, table, table_rows, q_weight, k_weight, eps,
+                 ctx->cfg.kv_heads, ctx->cfg.group_size, (char*)Q, (char*)K, (char*)V, stride, 0, {}};
+    if (!axis_of) {
+        if (bf16) return pairs ? launch<true, true, false>(ctx, a, stream) : launch<true, false, false>(ctx, a, stream);
+        return pairs ? launch<false, true, false>(ctx, a, stream) : launch<false, false, false>(ctx, a, stream);
+    }
+    for (int i = 0; i < kHeadDim / 2; ++i) a.axis_of[i / 16] |= (uint32_t)(axis_of[i] & 3) << i % 16 * 2;
+    if (bf16) return pairs ? launch<true, true, true>(ctx, a, stream) : launch<true, false, true>(ctx, a, stream);
+    return pairs ? launch<false, true, true>(ctx, a, stream) : launch<false, false, true>(ctx, a, stream);
 }
 
 }  // namespace curdkv

@@ -30,7 +30,8 @@ _DTYPES = {"fp32": DTYPE_F32, "bf16": DTYPE_BF16}
 EXPORTS = ["curdkv_create", "curdkv_destroy", "curdkv_sketch_host", "curdkv_set_sketch",
            "curdkv_uses_fused_kernel", "curdkv_scores", "curdkv_fold", "curdkv_select", "curdkv_compact", "curdkv_compress",
            "curdkv_adaptive_budgets", "curdkv_adaptive_budgets_noalloc", "curdkv_compress_adaptive", "curdkv_scores_append", "curdkv_normalise",
-           "curdkv_rotate", "curdkv_attend", "curdkv_compact_mx", "curdkv_expand_mx", "curdkv_attend_kept", "curdkv_attend_kept_mx", "curdkv_strerror"]
+           "curdkv_rotate", "curdkv_attend", "curdkv_compact_mx", "curdkv_expand_mx", "curdkv_attend_kept", "curdkv_attend_kept_mx",
+           "curdkv_rotate_axes", "curdkv_attend_weights", "curdkv_evict", "curdkv_attend_shared", "curdkv_attend_shared_mx", "curdkv_strerror"]
 
 
 class CurdkvConfig(C.Structure):
@@ -83,6 +84,11 @@ def lib() -> C.CDLL:
     L.curdkv_expand_mx.argtypes = [vp, vp, vp, i64, vp, vp]
     L.curdkv_attend_kept.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, f32, vp, vp, vp, i64, vp]
     L.curdkv_attend_kept_mx.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, f32, vp, vp, vp, i64, vp]
+    L.curdkv_rotate_axes.argtypes = [vp, vp, i64, i64, i64, vp, vp, i32, vp, vp, i64, vp, vp, f32, i32, vp, vp, vp, i64, vp]
+    L.curdkv_attend_weights.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, vp, i64, i32, f32, f32, vp, i64, vp, i64, vp]
+    L.curdkv_evict.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i64, i32, i64, vp, vp, vp, vp, i64, vp, vp]
+    L.curdkv_attend_shared.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, i64, f32, vp, vp, vp, i64, vp]
+    L.curdkv_attend_shared_mx.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, i64, f32, vp, vp, vp, i64, vp]
     L.curdkv_strerror.argtypes = [C.c_int]
     L.curdkv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -227,7 +233,8 @@ class _AttendByCtypes:
         return call
 
 
-_ATTEND = ("rotate", "attend", "compact_mx", "expand_mx", "attend_kept", "attend_kept_mx")
+_ATTEND = ("rotate", "attend", "compact_mx", "expand_mx", "attend_kept", "attend_kept_mx", "rotate_axes", "attend_weights", "evict", "attend_shared",
+           "attend_shared_mx")
 _attend = None                                      # the module _attend bound to the library, or _AttendByCtypes; set by lib()
 
 
@@ -414,3 +421,50 @@ class Context:
                                     *self._scratch(scratch), stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_attend_kept_mx")
+
+    def rotate_axes(self, qkv, count: int, m: int, table, positions, axis_of: np.ndarray, Q, K, V, stride: int, starts=None, q_weight=None, k_weight=None,
+                    eps: float = 1e-5, pairs: bool = False, row_stride: Optional[int] = None, stream=None):
+        """positions: int32 [axes, count*m] on the device; axis_of: a host array, uint8 [head_dim/2]; all else as for rotate."""
+        assert isinstance(axis_of, np.ndarray) and axis_of.dtype == np.uint8 and axis_of.size == self.cfg.head_dim // 2 and axis_of.flags.c_contiguous, \
+            f"expected a contiguous array of {self.cfg.head_dim // 2} uint8"
+        rc = _attend.rotate_axes(self._address, qkv, count, m, self._row if row_stride is None else row_stride, starts, positions, positions.shape[0],
+                                 _host_ptr(axis_of), table, table.shape[0], q_weight, k_weight, float(eps), 1 if pairs else 0, Q, K, V, stride, stream)
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_rotate_axes")
+
+    def attend_weights(self, Q, K, lse, count: int, m: int, n: int, stride: int, mass, mass_stride: Optional[int] = None, lengths=None, window: int = 0,
+                       n_sink: int = 0, scale=None, decay: float = 1.0, scratch=None, stream=None):
+        """mass_stride None: stride; scale, scratch: as for attend."""
+        rc = _attend.attend_weights(self._address, Q, K, lse, count, m, n, stride, lengths, window, n_sink, self._scale if scale is None else float(scale),
+                                    float(decay), mass, stride if mass_stride is None else mass_stride, *self._scratch(scratch), stream)
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_attend_weights")
+
+    def evict(self, K, V, mass, count: int, n: int, stride: int, keep: int, rows, positions=None, lengths=None, n_sink: int = 0, recent: int = 0, K_out=None,
+              V_out=None, mass_out=None, positions_out=None, out_stride: Optional[int] = None, stream=None):
+        """K_out None: in place, and so are mass and positions unless they are given places of their own."""
+        if K_out is None:
+            K_out, V_out = K, V
+            mass_out, positions_out = mass if mass_out is None else mass_out, positions if positions_out is None else positions_out
+        rc = _attend.evict(self._address, K, V, mass, positions, count, n, stride, lengths, keep, n_sink, recent, K_out, V_out, mass_out, positions_out,
+                           stride if out_stride is None else out_stride, rows, stream)
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_evict")
+
+    def attend_shared(self, Q, K_kept, V_kept, offsets, count: int, share: int, m: int, total: int, out, K_tail=None, V_tail=None, tail_n: int = 0,
+                      tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None, scratch=None, stream=None):
+        """offsets: a DEVICE tensor, int64 [count*kv_heads + 1]; rows None: total; scale, scratch: as for attend."""
+        rc = _attend.attend_shared(self._address, Q, K_kept, V_kept, offsets, total, total if rows is None else rows, K_tail, V_tail, tail_n, tail_stride,
+                                   tail_lengths, count, share, m, self._scale if scale is None else float(scale), out, lse, *self._scratch(scratch), stream)
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_attend_shared")
+
+    def attend_shared_mx(self, Q, K_codes, K_scales, V_codes, V_scales, offsets, count: int, share: int, m: int, total: int, out, K_tail=None, V_tail=None,
+                         tail_n: int = 0, tail_stride: int = 0, tail_lengths=None, rows: Optional[int] = None, scale=None, lse=None, scratch=None,
+                         stream=None):
+        """offsets: a DEVICE tensor, int64 [count*kv_heads + 1]; rows None: total; scale, scratch: as for attend."""
+        rc = _attend.attend_shared_mx(self._address, Q, K_codes, K_scales, V_codes, V_scales, offsets, total, total if rows is None else rows, K_tail, V_tail,
+                                      tail_n, tail_stride, tail_lengths, count, share, m, self._scale if scale is None else float(scale), out, lse,
+                                      *self._scratch(scratch), stream)
+        if rc != OK:
+            raise CurdkvError(rc, "curdkv_attend_shared_mx")

@@ -1,9 +1,13 @@
 // The attention weight that every key of a cache got from a sequence's last m tokens, summed over them and the query heads of its KV head:
 //     mass[j] = decay mass[j] + sum over rows R = (token, head) that see j of exp(scale q_R.k_j - lse_R),
 // lse_R being the logarithm of the row's softmax denominator, which the attention has written.  With it no maximum has to be found: every weight is at
-// most 1 (as far as lse is what the scores make it), and a key's sum is its own affair: one wave's, in a fixed order, without atomics.
-// S = Q K^T: 16 rows R are the A operand of mfma_f32_16x16x32_bf16 (16x16x4 for fp32), 16 keys the B operand, so that a lane holds four rows' scores of
-// one key, and adds their weights up in a register until all rows are through.
+// most 1 (as far as lse is what the scores make it), and a key's sum is its own affair: one wave's, or a few waves' that are added up in order, without atomics.
+//
+// Few rows (weights_few_kernel): S = Q K^T by mfma_f32_16x16x32_bf16 (16x16x4 for fp32), 16 rows R by 16 keys; the rows stay in registers, a wave goes over keys.
+// Many rows (weights_many_kernel): S^T = K Q^T by mfma_f32_32x32x16_bf16 (32x32x2); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves
+// share, and each lane adds up the weights of its own R, key by key, until all rows are through.
+
+#include <algorithm>
 
 #include "attend_device.h"
 #include "attend_internal.h"
@@ -14,7 +18,10 @@ namespace {
 struct WeightsArgs {
     WeightsCall c;
     float scale_log2;
-    int rows, key_tiles;               // m * group; workgroups of 64 keys a head
+    int groups, rows, key_tiles;       // count * kv; m * group; tiles of keys a head
+    int tiles_each;                    // few rows: tiles of 16 keys that a wave goes over
+    int chunk, chunks;                 // many rows: that a workgroup takes
+    float* part;                       // chunks > 1: [chunks][groups][key_tiles * keys of a tile], of the chunks that see some key of the tile
 };
 
 // Tokens of the m that see some key of j0 .. j1: [first, last].
@@ -26,6 +33,13 @@ __device__ __forceinline__ Tokens tokens_that_see(int length, int m, int j0, int
     const int64_t last = window > 0 && j0 >= sinks ? min((int64_t)m - 1, (int64_t)j1 + window - 1 - p0) : (int64_t)m - 1;
     return {(int)min(max((int64_t)j0 - p0, (int64_t)0), (int64_t)m), (int)max(last, (int64_t)-1)};
 }
+__device__ __forceinline__ int length_of(const WeightsCall& c, int b) { return __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n); }
+__device__ __forceinline__ void add_to(const WeightsCall& c, int g, int j, float sum) {
+    float* to = c.mass + (int64_t)g * c.mass_stride + j;
+    *to = c.decay == 0.f ? sum : __builtin_fmaf(c.decay, *to, sum);
+}
+
+// ---- few rows
 
 template <bool BF16> struct Operand;   // 128 channels of the row of lane % 16, those of the lane's quarter
 template <> struct Operand<true> {
@@ -58,47 +72,272 @@ template <> struct Operand<false> {
     }
 };
 
-template <bool BF16>
-__global__ __launch_bounds__(256) void weights_kernel(WeightsArgs a) {
+// 16 TILES rows R at most.  A wave takes tiles_each tiles of 16 keys, the next one's rows on their way while it works on one.
+template <bool BF16, int TILES>
+__global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
     constexpr int kRow = BF16 ? 256 : 512;
     const WeightsCall& c = a.c;
-    const int g = blockIdx.x / a.key_tiles, b = g / c.kv, head = g % c.kv;
-    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
-    const int j0 = (blockIdx.x % a.key_tiles * 4 + (threadIdx.x >> 6)) * 16;
-    const int length = c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n;
-    if (j0 >= length) return;
-    const int j = j0 + col, j1 = min(j0 + 15, length - 1);
-    Operand<BF16> k, q;
-    k.load((const char*)c.K + ((int64_t)g * c.stride + min(j, length - 1)) * kRow, quarter);
-    const Tokens t = tokens_that_see(length, c.m, j0, j1, c.window, c.sinks);
-    float sum = 0.f;
-    for (int R0 = t.first * c.group & ~15; R0 < (t.last + 1) * c.group; R0 += 16) {
-        const auto row_of = [&](int R) { return (((int64_t)b * c.m + R / c.group) * c.kv + head) * c.group + R % c.group; };
-        q.load((const char*)c.Q + row_of(min(R0 + col, a.rows - 1)) * kRow, quarter);
-        const f32x4a s = Operand<BF16>::product(q, k);
+    const int g = blockIdx.x % a.groups, b = g / c.kv, head = g % c.kv;
+    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int length = length_of(c, b), tiles = (length + 15) / 16;
+    int tile = (blockIdx.x / a.groups * 4 + wave) * a.tiles_each;
+    const int end = min(tile + a.tiles_each, tiles);
+    if (tile >= end) return;
+    const char* keys = (const char*)c.K + (int64_t)g * c.stride * kRow;
+    Operand<BF16> k, next, q[TILES];
+    next.load(keys + (int64_t)min(tile * 16 + col, length - 1) * kRow, quarter);
+    // rows 16 u + col as the operand; of rows 16 u + 4 quarter + i, whose scores come back, the position (below all where the row gives nothing) and -lse
+    int p[TILES][4];
+    float less[TILES][4];
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+        const int R = min(u * 16 + col, a.rows - 1);
+        q[u].load((const char*)c.Q + ((((int64_t)b * c.m + R / c.group) * c.kv + head) * c.group + R % c.group) * kRow, quarter);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int R = R0 + 4 * quarter + i, at = min(R, a.rows - 1), token = at / c.group;
+            const int r = u * 16 + 4 * quarter + i, at = min(r, a.rows - 1), token = at / c.group;
             const float lse = c.lse[((int64_t)b * c.kv * c.group + head * c.group + at % c.group) * c.m + token];
-            const bool seen = R < a.rows && j < length && lse != -INFINITY && sees(length - c.m + token, j, c.window, c.sinks);
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, -lse * (1.f / kLn2)));
-            sum += seen ? w : 0.f;
+            p[u][i] = r < a.rows && lse != -INFINITY ? length - c.m + token : -1;
+            less[u][i] = -lse * (1.f / kLn2);
         }
     }
-    sum = quarters_sum(sum);
-    if (quarter == 0 && j < length) {
-        float* to = c.mass + (int64_t)g * c.mass_stride + j;
-        *to = c.decay == 0.f ? sum : __builtin_fmaf(c.decay, *to, sum);
+    for (; tile < end; ++tile) {
+        k = next;
+        next.load(keys + (int64_t)min(tile * 16 + 16 + col, length - 1) * kRow, quarter);
+        const int j = tile * 16 + col;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < TILES; ++u) {
+            const f32x4a s = Operand<BF16>::product(q[u], k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less[u][i]));
+                sum += sees(p[u][i], j, c.window, c.sinks) ? w : 0.f;
+            }
+        }
+        sum = quarters_sum(sum);
+        if (quarter == 0 && j < length) add_to(c, g, j, sum);
     }
+}
+
+// ---- many rows
+
+// 64 lanes' 16 bytes, each from an address of its own, to LDS from `to` on (as dma16).
+__device__ __forceinline__ void dma16_from(uint32_t to, const char* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+
+// A row R as (token, head of the group), moved on without a division.
+struct Row {
+    int t, i;
+    __device__ __forceinline__ Row() {}
+    __device__ __forceinline__ Row(int R, int group) : t(R / group), i(R % group) {}
+    __device__ __forceinline__ void on(int tokens, int heads, int group) {
+        t += tokens, i += heads;
+        if (i >= group) i -= group, ++t;
+    }
+};
+
+template <bool BF16> struct Many;
+template <> struct Many<true> {
+    static constexpr int kBlocks = 2, kStage = 64, kRow = 256;     // of 32 keys a wave; rows a stage of 16 KB
+    u32x4a x[8];
+    __device__ __forceinline__ void load(const char* row, int half) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) x[s] = ((const u32x4a*)row)[2 * s + half];
+    }
+};
+template <> struct Many<false> {
+    static constexpr int kBlocks = 1, kStage = 32, kRow = 512;
+    f32x4a x[16];
+    __device__ __forceinline__ void load(const char* row, int half) {
+#pragma unroll
+        for (int s = 0; s < 16; ++s) x[s] = ((const f32x4a*)row)[2 * s + half];
+    }
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
+    typedef Many<BF16> M;
+    constexpr int kKeys = M::kBlocks * 32, kStage = M::kStage;
+    __shared__ __attribute__((aligned(16))) char Qs[2][16384];
+    const WeightsCall& c = a.c;
+    const int g = blockIdx.x % a.groups, key_tile = blockIdx.x / a.groups % a.key_tiles, chunk = blockIdx.x / a.groups / a.key_tiles, b = g / c.kv, head = g % c.kv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int length = length_of(c, b), j0 = key_tile * (4 * kKeys), j1 = min(j0 + 4 * kKeys, length) - 1;
+    if (j0 > j1) return;
+    const Tokens seeing = tokens_that_see(length, c.m, j0, j1, c.window, c.sinks);
+    const int begin = max(chunk * a.chunk, seeing.first * c.group / kStage * kStage), end = min(min((chunk + 1) * a.chunk, a.rows), (seeing.last + 1) * c.group);
+    const bool nothing = begin >= end;                             // (without parts the old weights may still have to fade)
+    if (nothing && a.chunks > 1) return;
+
+    const int k0 = j0 + wave * kKeys, k1 = min(k0 + kKeys, length) - 1;        // this wave's keys
+    M keys[M::kBlocks];
+#pragma unroll
+    for (int kb = 0; kb < M::kBlocks; ++kb) keys[kb].load((const char*)c.K + ((int64_t)g * c.stride + min(k0 + kb * 32 + col, length - 1)) * M::kRow, half);
+    float sums[M::kBlocks * 16];
+#pragma unroll
+    for (int i = 0; i < M::kBlocks * 16; ++i) sums[i] = 0.f;
+
+    // Rows R on their way into LDS: columns of 64 bytes a row, pieces permuted by (row / 2) % 4; this lane's is row d_row of a stage, four columns of it from `column` on.
+    const int64_t per_token = (int64_t)c.kv * c.group * M::kRow;
+    const char* queries = (const char*)c.Q + ((int64_t)b * c.m * c.kv + head) * c.group * M::kRow;
+    const int d_row = (BF16 ? wave : wave & 1) * 16 + (lane >> 2), column = BF16 ? 0 : (wave >> 1) * 4;
+    const int piece = (lane & 3) ^ ((d_row >> 1) & 3);
+    const int stage_tokens = kStage / c.group, stage_heads = kStage % c.group, last_t = (a.rows - 1) / c.group, last_i = c.group - 1;
+    Row from(begin + d_row, c.group);
+    const uint32_t lds = lds_address(&Qs[0][0]);
+    const auto ask = [&](int buffer) ALWAYS_INLINE {
+        const bool there = from.t <= last_t;
+        const char* at = queries + (there ? from.t : last_t) * per_token + (there ? from.i : last_i) * M::kRow + column * 64 + piece * 16;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + buffer * 16384 + column * (kStage * 64) + (BF16 ? wave : wave & 1) * 1024);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dma16_from(to + i * (kStage * 64), at + i * 64);
+        from.on(stage_tokens, stage_heads, c.group);
+    };
+    // The rows that this lane has scores of, R = 32 u + col of a stage: position and -lse.
+    constexpr int kTiles = kStage / 32;
+    const float* lse_of_head = c.lse + ((int64_t)b * c.kv + head) * c.group * c.m;
+    Row mine[kTiles];
+#pragma unroll
+    for (int u = 0; u < kTiles; ++u) mine[u] = Row(begin + u * 32 + col, c.group);
+    float lse[kTiles], next_lse[kTiles];
+    int p[kTiles];
+    const auto ask_lse = [&]() ALWAYS_INLINE {
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            const bool there = mine[u].t <= last_t;
+            next_lse[u] = lse_of_head[(int64_t)(there ? mine[u].i : last_i) * c.m + (there ? mine[u].t : last_t)];
+        }
+    };
+    if (!nothing) {
+        ask(0);
+        ask_lse();
+        dma_wait();
+    }
+    __syncthreads();
+    const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+    for (int R0 = begin, buffer = 0; R0 < end; R0 += kStage, buffer ^= 1) {
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            lse[u] = next_lse[u];
+            p[u] = mine[u].t <= last_t ? length - c.m + mine[u].t : -1;
+            mine[u].on(stage_tokens, stage_heads, c.group);
+        }
+        if (R0 + kStage < end) {
+            ask(buffer ^ 1);
+            ask_lse();
+        }
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            // positions of the tile's rows, lowest (in lane 0) and highest; rows that are none stand at -1
+            const int low = __builtin_amdgcn_readfirstlane(p[u]), last = __builtin_amdgcn_readlane(p[u], 31), high = last < 0 ? length - 1 : last;
+            if (k0 > k1 || high < k0) continue;
+            const bool whole = last >= 0 && low >= k1 && (c.window <= 0 || high - k0 < c.window || k1 < c.sinks) && !__any(lse[u] == -INFINITY);
+            const float less = -lse[u] * (1.f / kLn2);
+            const char* Qt = Qs[buffer] + u * 2048;
+#pragma unroll
+            for (int kb = 0; kb < M::kBlocks; ++kb) {
+                f32x16a s;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 0.f;
+                if constexpr (BF16) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * (kStage * 64));
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q), s, 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const f32x4a q = *(const f32x4a*)(Qt + k_at[i & 1] + (i >> 1) * (kStage * 64));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].x[i][e], q[e], s, 0, 0, 0);
+                    }
+                }
+                if (whole) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less));
+                } else {
+                    const int at = lse[u] == -INFINITY ? -1 : p[u];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less));
+                        sums[kb * 16 + i] += sees(at, k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4, c.window, c.sinks) ? w : 0.f;
+                    }
+                }
+            }
+        }
+        dma_wait();
+        __syncthreads();
+    }
+    // Each key's sum over the 32 lanes of its half: at every step a lane keeps half of the keys and gives away the others'.
+    int width = M::kBlocks * 16, d = 16;
+    if constexpr (!BF16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[i] += __shfl_xor(sums[i], 16);
+        d = 8;
+    }
+#pragma unroll
+    for (; d > 0; d >>= 1) {
+        width >>= 1;
+        const bool upper = col & d;
+#pragma unroll
+        for (int i = 0; i < width; ++i) {
+            const float give = upper ? sums[i] : sums[i + width], keep = upper ? sums[i + width] : sums[i];
+            sums[i] = keep + __shfl_xor(give, d);
+        }
+    }
+    const int i = col & 15, kb = BF16 ? col >> 4 : 0, j = k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4;
+    if (j >= length || (!BF16 && col >= 16)) return;
+    if (a.chunks > 1) a.part[((int64_t)chunk * a.groups + g) * a.key_tiles * (4 * kKeys) + j] = sums[0];
+    else add_to(c, g, j, sums[0]);
+}
+
+// Adds up the chunks that see a key's tile, in order.
+template <bool BF16>
+__global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
+    constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kStage;
+    const WeightsCall& c = a.c;
+    const int g = blockIdx.x % a.groups, j = blockIdx.x / a.groups * 256 + threadIdx.x, length = length_of(c, g / c.kv);
+    if (j >= length) return;
+    const int j0 = j / kKeys * kKeys;
+    const Tokens seeing = tokens_that_see(length, c.m, j0, min(j0 + kKeys, length) - 1, c.window, c.sinks);
+    const int begin = seeing.first * c.group / kStage * kStage, end = min(a.rows, (seeing.last + 1) * c.group);
+    float sum = 0.f;
+    if (begin < end)
+        for (int chunk = begin / a.chunk; chunk <= (end - 1) / a.chunk; ++chunk) sum += a.part[((int64_t)chunk * a.groups + g) * a.key_tiles * kKeys + j];
+    add_to(c, g, j, sum);
 }
 
 }  // namespace
 
 hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStream_t stream) {
-    WeightsArgs a{call, call.scale * (1.f / kLn2), call.m * call.group, (call.n + 63) / 64};
-    const unsigned blocks = (unsigned)(call.count * call.kv * a.key_tiles);
-    if (call.dtype == CURDKV_DTYPE_BF16) weights_kernel<true><<<blocks, 256, 0, stream>>>(a);
-    else weights_kernel<false><<<blocks, 256, 0, stream>>>(a);
+    const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
+    WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, 1, nullptr};
+    if (a.rows <= 32) {
+        const int64_t tiles = (call.n + 15) / 16, waves = 16 * (int64_t)ctx->num_cu;
+        a.tiles_each = (int)std::max<int64_t>(1, std::min<int64_t>(8, a.groups * tiles / waves));
+        const int64_t blocks = a.groups * ((tiles + 4 * a.tiles_each - 1) / (4 * a.tiles_each));
+        const auto launch = [&](auto kernel) { kernel<<<(unsigned)blocks, 256, 0, stream>>>(a); };
+        if (a.rows <= 16) bf16 ? launch(weights_few_kernel<true, 1>) : launch(weights_few_kernel<false, 1>);
+        else bf16 ? launch(weights_few_kernel<true, 2>) : launch(weights_few_kernel<false, 2>);
+        return hipGetLastError();
+    }
+    const int keys = bf16 ? 256 : 128, stage = bf16 ? 64 : 32;
+    a.key_tiles = (call.n + keys - 1) / keys;
+    // Rows shared out over workgroups until there are eight for every unit, half of them above the diagonal, eight stages each at least, as far as there is scratch.
+    const int64_t blocks = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (blocks * keys * (int64_t)sizeof(float)) : 0;
+    const int64_t chunks = std::max<int64_t>(1, std::min(std::min<int64_t>(16 * (int64_t)ctx->num_cu / blocks, a.rows / (8 * stage)), std::min(room, kMostBlocks / blocks)));
+    a.chunk = (int)(((a.rows + chunks - 1) / chunks + stage - 1) / stage * stage);
+    a.chunks = (a.rows + a.chunk - 1) / a.chunk;
+    a.part = (float*)((char*)call.scratch + kScratchCounters);
+    const auto launch = [&](auto kernel, int64_t n) { kernel<<<(unsigned)n, 256, 0, stream>>>(a); };
+    bf16 ? launch(weights_many_kernel<true>, blocks * a.chunks) : launch(weights_many_kernel<false>, blocks * a.chunks);
+    if (a.chunks > 1) {
+        const int64_t joins = (int64_t)a.groups * ((call.n + 255) / 256);
+        bf16 ? launch(weights_join_kernel<true>, joins) : launch(weights_join_kernel<false>, joins);
+    }
     return hipGetLastError();
 }
 

@@ -19,7 +19,7 @@ struct WeightsArgs {
     WeightsCall c;
     float scale_log2;
     int groups, rows, key_tiles;       // count * kv; m * group; tiles of keys a head
-    int tiles_each;                    // few rows: tiles of 16 keys that a wave goes over
+    int shares;                        // few rows: workgroups that share a head's keys
     int chunk, chunks;                 // many rows: that a workgroup takes
     float* part;                       // chunks > 1: [chunks][groups][key_tiles * keys of a tile], of the chunks that see some key of the tile
 };
@@ -72,20 +72,52 @@ template <> struct Operand<false> {
     }
 };
 
-// 16 TILES rows R at most.  A wave takes tiles_each tiles of 16 keys, the next one's rows on their way while it works on one.
-template <bool BF16, int TILES>
+// Keys come in whole lines of 128 bytes: an instruction takes 8 rows' 8 pieces of 16 bytes, lane (quarter, c) piece quarter + 4 (c / 8) of row c % 8 of 8.  What the operand has in lane
+// c < 8 from the second row of 8 and in lane c >= 8 from the first then lies 8 lanes off: x, of rows 0..7, and y, of rows 8..15, become pieces quarter and quarter + 4 of row c.
+template <class T>
+__device__ __forceinline__ void to_rows(T& x, T& y) {
+    u32x4a u = __builtin_bit_cast(u32x4a, x), v = __builtin_bit_cast(u32x4a, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int a = (int)u[i], b = (int)v[i];
+        u[i] = (uint32_t)__builtin_amdgcn_update_dpp(a, b, 0x128, 0xF, 0xC, false);       // row_ror:8, lanes 8..15 of 16
+        v[i] = (uint32_t)__builtin_amdgcn_update_dpp(b, a, 0x128, 0xF, 0x3, false);       // lanes 0..7
+    }
+    x = __builtin_bit_cast(T, u), y = __builtin_bit_cast(T, v);
+}
+#ifndef TE
+#define TE 4
+#endif
+#ifndef AH
+#define AH 1
+#endif
+#ifndef WV
+#define WV 16
+#endif
+
+// 16 TILES rows R at most.  A wave takes the 64 keys of a step 16 at a time, kAhead more of them on their way, and reads and writes their weights together.
+// PAST: keys pass the caches.
+template <bool BF16, int TILES, bool PAST>
 __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
-    constexpr int kRow = BF16 ? 256 : 512;
+    constexpr int kRow = BF16 ? 256 : 512, kPieces = BF16 ? 4 : 8, kAhead = BF16 ? AH : 1;
     const WeightsCall& c = a.c;
-    const int g = blockIdx.x % a.groups, b = g / c.kv, head = g % c.kv;
+    const int head = blockIdx.x % c.kv, share = blockIdx.x / c.kv % a.shares, b = blockIdx.x / c.kv / a.shares, g = b * c.kv + head;
     const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int length = length_of(c, b), tiles = (length + 15) / 16;
-    int tile = (blockIdx.x / a.groups * 4 + wave) * a.tiles_each;
-    const int end = min(tile + a.tiles_each, tiles);
-    if (tile >= end) return;
+    const int length = length_of(c, b), steps = (length + 63) / 64;
+    const int first = (int)((int64_t)steps * (share * 4 + wave) / (4 * a.shares)), end = (int)((int64_t)steps * (share * 4 + wave + 1) / (4 * a.shares));
+    if (first >= end) return;
     const char* keys = (const char*)c.K + (int64_t)g * c.stride * kRow;
-    Operand<BF16> k, next, q[TILES];
-    next.load(keys + (int64_t)min(tile * 16 + col, length - 1) * kRow, quarter);
+    float* mass = c.mass + (int64_t)g * c.mass_stride;
+    Operand<BF16> ahead[4], q[TILES];
+    const auto ask = [&](Operand<BF16>& k, int j0) ALWAYS_INLINE {
+#pragma unroll
+        for (int s = 0; s < kPieces; ++s) {
+            const auto* from = (const decltype(k.x[s] + 0)*)(keys + (int64_t)min(j0 + (col & 7) + (s & 1) * 8, length - 1) * kRow + (quarter + (col >> 3) * 4 + (s >> 1) * 8) * 16);
+            k.x[s] = PAST ? __builtin_nontemporal_load(from) : *from;
+        }
+    };
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) ask(ahead[x], first * 64 + x * 16);
     // rows 16 u + col as the operand; of rows 16 u + 4 quarter + i, whose scores come back, the position (below all where the row gives nothing) and -lse
     int p[TILES][4];
     float less[TILES][4];
@@ -101,22 +133,30 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
             less[u][i] = -lse * (1.f / kLn2);
         }
     }
-    for (; tile < end; ++tile) {
-        k = next;
-        next.load(keys + (int64_t)min(tile * 16 + 16 + col, length - 1) * kRow, quarter);
-        const int j = tile * 16 + col;
-        float sum = 0.f;
+    for (int step = first; step < end; ++step) {
+        const int j = step * 64 + lane;
+        const float old = mass[min(j, length - 1)];
+        float mine = 0.f;
 #pragma unroll
-        for (int u = 0; u < TILES; ++u) {
-            const f32x4a s = Operand<BF16>::product(q[u], k);
+        for (int x = 0; x < 4; ++x) {
+            ask(ahead[(x + kAhead) % 4], step * 64 + (x + kAhead) * 16);
+            Operand<BF16> k = ahead[x];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less[u][i]));
-                sum += sees(p[u][i], j, c.window, c.sinks) ? w : 0.f;
+            for (int s = 0; s < kPieces; s += 2) to_rows(k.x[s], k.x[s + 1]);
+            float sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < TILES; ++u) {
+                const f32x4a s = Operand<BF16>::product(q[u], k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less[u][i]));
+                    sum += sees(p[u][i], step * 64 + x * 16 + col, c.window, c.sinks) ? w : 0.f;
+                }
             }
+            sum = quarters_sum(sum);
+            mine = quarter == x ? sum : mine;
         }
-        sum = quarters_sum(sum);
-        if (quarter == 0 && j < length) add_to(c, g, j, sum);
+        if (j < length) mass[j] = c.decay == 0.f ? mine : __builtin_fmaf(c.decay, old, mine);
     }
 }
 
@@ -155,6 +195,18 @@ template <> struct Many<false> {
         for (int s = 0; s < 16; ++s) x[s] = ((const f32x4a*)row)[2 * s + half];
     }
 };
+
+// Sums of 2 W values over 2 W lanes, value `lane` to each lane's x[0]: at every step a lane keeps half of them and gives away the others'.
+template <int W, int N>
+__device__ __forceinline__ void spread(float (&x)[N], int lane) {
+    const bool upper = lane & W;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const float give = upper ? x[i] : x[i + W], keep = upper ? x[i + W] : x[i];
+        x[i] = keep + __shfl_xor(give, W);
+    }
+    if constexpr (W > 1) spread<W / 2>(x, lane);
+}
 
 template <bool BF16>
 __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
@@ -217,6 +269,15 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     }
     __syncthreads();
     const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+    // bf16: the scores of the last block of 32 x 32 wait for the next one's products, between which their exponentials go
+    f32x16a s[2];
+    float waiting = -INFINITY;                                     // the -lse of s[1], of this wave's second 32 keys
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[1][i] = 0.f;
+    const auto weigh = [&](f32x16a& x, int kb, float less) ALWAYS_INLINE {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
+    };
     for (int R0 = begin, buffer = 0; R0 < end; R0 += kStage, buffer ^= 1) {
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
@@ -228,41 +289,61 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
             ask(buffer ^ 1);
             ask_lse();
         }
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            // positions of the tile's rows, lowest (in lane 0) and highest; rows that are none stand at -1
-            const int low = __builtin_amdgcn_readfirstlane(p[u]), last = __builtin_amdgcn_readlane(p[u], 31), high = last < 0 ? length - 1 : last;
-            if (k0 > k1 || high < k0) continue;
-            const bool whole = last >= 0 && low >= k1 && (c.window <= 0 || high - k0 < c.window || k1 < c.sinks) && !__any(lse[u] == -INFINITY);
-            const float less = -lse[u] * (1.f / kLn2);
-            const char* Qt = Qs[buffer] + u * 2048;
-#pragma unroll
-            for (int kb = 0; kb < M::kBlocks; ++kb) {
-                f32x16a s;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = 0.f;
-                if constexpr (BF16) {
+        // positions of the stage's rows, lowest (in lane 0) and highest; rows that are none stand at -1
+        const int low = __builtin_amdgcn_readfirstlane(p[0]), last = __builtin_amdgcn_readlane(p[kTiles - 1], 31), high = last < 0 ? length - 1 : last;
+        const bool whole = last >= 0 && low >= k1 && (c.window <= 0 || high - k0 < c.window || k1 < c.sinks) && !__any(lse[0] == -INFINITY || lse[kTiles - 1] == -INFINITY);
+        if (k0 > k1 || high < k0) {
+        } else if (BF16 && whole) {
+            if constexpr (BF16) {
+                const auto block = [&](const u32x4a (&q)[8], int kb, f32x16a& x, f32x16a& before, int kb_before, float less) ALWAYS_INLINE {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * (kStage * 64));
-                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q), s, 0, 0, 0);
-                    }
-                } else {
+                        const f32x16a zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q[i]), i == 0 ? zero : x, 0, 0, 0);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const f32x4a q = *(const f32x4a*)(Qt + k_at[i & 1] + (i >> 1) * (kStage * 64));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].x[i][e], q[e], s, 0, 0, 0);
+                        for (int e = 2 * i; e < 2 * i + 2; ++e) sums[kb_before * 16 + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(before[e], a.scale_log2, less));
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                };
+#pragma unroll
+                for (int u = 0; u < kTiles; ++u) {
+                    u32x4a q[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[i] = *(const u32x4a*)(Qs[buffer] + u * 2048 + k_at[i & 1] + (i >> 1) * (kStage * 64));
+                    const float less = -lse[u] * (1.f / kLn2);
+                    block(q, 0, s[0], s[1], 1, waiting);
+                    block(q, 1, s[1], s[0], 0, less);
+                    waiting = less;
                 }
-                if (whole) {
+            }
+        } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less));
-                } else {
-                    const int at = lse[u] == -INFINITY ? -1 : p[u];
+            for (int u = 0; u < kTiles; ++u) {
+                const int at = lse[u] == -INFINITY ? -1 : p[u];
+                const float less = -lse[u] * (1.f / kLn2);
+                const char* Qt = Qs[buffer] + u * 2048;
+#pragma unroll
+                for (int kb = 0; kb < M::kBlocks; ++kb) {
+                    f32x16a x;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < (BF16 ? 8 : 16); ++i) {
+                        const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * (kStage * 64));
+                        if constexpr (BF16) {
+                            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q), x, 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].x[i][e], __uint_as_float(q[e]), x, 0, 0, 0);
+                        }
+                    }
+                    if (!BF16 && whole) {
+                        weigh(x, kb, less);
+                        continue;
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, less));
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
                         sums[kb * 16 + i] += sees(at, k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4, c.window, c.sinks) ? w : 0.f;
                     }
                 }
@@ -271,23 +352,12 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
         dma_wait();
         __syncthreads();
     }
-    // Each key's sum over the 32 lanes of its half: at every step a lane keeps half of the keys and gives away the others'.
-    int width = M::kBlocks * 16, d = 16;
+    if constexpr (BF16) weigh(s[1], 1, waiting);
     if constexpr (!BF16) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) sums[i] += __shfl_xor(sums[i], 16);
-        d = 8;
     }
-#pragma unroll
-    for (; d > 0; d >>= 1) {
-        width >>= 1;
-        const bool upper = col & d;
-#pragma unroll
-        for (int i = 0; i < width; ++i) {
-            const float give = upper ? sums[i] : sums[i + width], keep = upper ? sums[i + width] : sums[i];
-            sums[i] = keep + __shfl_xor(give, d);
-        }
-    }
+    spread<M::kBlocks * 8>(sums, col);
     const int i = col & 15, kb = BF16 ? col >> 4 : 0, j = k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4;
     if (j >= length || (!BF16 && col >= 16)) return;
     if (a.chunks > 1) a.part[((int64_t)chunk * a.groups + g) * a.key_tiles * (4 * kKeys) + j] = sums[0];
@@ -316,12 +386,15 @@ hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStr
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
     WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, 1, nullptr};
     if (a.rows <= 32) {
-        const int64_t tiles = (call.n + 15) / 16, waves = 16 * (int64_t)ctx->num_cu;
-        a.tiles_each = (int)std::max<int64_t>(1, std::min<int64_t>(8, a.groups * tiles / waves));
-        const int64_t blocks = a.groups * ((tiles + 4 * a.tiles_each - 1) / (4 * a.tiles_each));
-        const auto launch = [&](auto kernel) { kernel<<<(unsigned)blocks, 256, 0, stream>>>(a); };
-        if (a.rows <= 16) bf16 ? launch(weights_few_kernel<true, 1>) : launch(weights_few_kernel<false, 1>);
-        else bf16 ? launch(weights_few_kernel<true, 2>) : launch(weights_few_kernel<false, 2>);
+        const int64_t steps = (call.n + 63) / 64, waves = WV * (int64_t)ctx->num_cu;
+        const int64_t each = std::max<int64_t>(1, std::min<int64_t>(TE, a.groups * steps / waves));
+        a.shares = (int)((steps + 4 * each - 1) / (4 * each));
+        const bool past = (int64_t)a.groups * call.n * (bf16 ? 256 : 512) > kPastCaches;
+        const auto launch = [&](auto kernel) { kernel<<<(unsigned)((int64_t)a.groups * a.shares), 256, 0, stream>>>(a); };
+        if (bf16 && a.rows <= 16) past ? launch(weights_few_kernel<true, 1, true>) : launch(weights_few_kernel<true, 1, false>);
+        else if (bf16) past ? launch(weights_few_kernel<true, 2, true>) : launch(weights_few_kernel<true, 2, false>);
+        else if (a.rows <= 16) past ? launch(weights_few_kernel<false, 1, true>) : launch(weights_few_kernel<false, 1, false>);
+        else past ? launch(weights_few_kernel<false, 2, true>) : launch(weights_few_kernel<false, 2, false>);
         return hipGetLastError();
     }
     const int keys = bf16 ? 256 : 128, stage = bf16 ? 64 : 32;

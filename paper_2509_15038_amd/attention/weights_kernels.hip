@@ -85,6 +85,12 @@ __device__ __forceinline__ void to_rows(T& x, T& y) {
     }
     x = __builtin_bit_cast(T, u), y = __builtin_bit_cast(T, v);
 }
+#ifndef CM
+#define CM 24
+#endif
+#ifndef CS
+#define CS 2
+#endif
 #ifndef TE
 #define TE 4
 #endif
@@ -167,20 +173,9 @@ __device__ __forceinline__ void dma16_from(uint32_t to, const char* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 
-// A row R as (token, head of the group), moved on without a division.
-struct Row {
-    int t, i;
-    __device__ __forceinline__ Row() {}
-    __device__ __forceinline__ Row(int R, int group) : t(R / group), i(R % group) {}
-    __device__ __forceinline__ void on(int tokens, int heads, int group) {
-        t += tokens, i += heads;
-        if (i >= group) i -= group, ++t;
-    }
-};
-
 template <bool BF16> struct Many;
 template <> struct Many<true> {
-    static constexpr int kBlocks = 2, kStage = 64, kRow = 256;     // of 32 keys a wave; rows a stage of 16 KB
+    static constexpr int kBlocks = 2, kTiles = 4, kRow = 256;      // of 32 keys a wave; tiles of 32 rows a stage of 32 KB
     u32x4a x[8];
     __device__ __forceinline__ void load(const char* row, int half) {
 #pragma unroll
@@ -188,11 +183,25 @@ template <> struct Many<true> {
     }
 };
 template <> struct Many<false> {
-    static constexpr int kBlocks = 1, kStage = 32, kRow = 512;
+    static constexpr int kBlocks = 1, kTiles = 2, kRow = 512;
     f32x4a x[16];
     __device__ __forceinline__ void load(const char* row, int half) {
 #pragma unroll
         for (int s = 0; s < 16; ++s) x[s] = ((const f32x4a*)row)[2 * s + half];
+    }
+};
+
+// Where a row R = (token, head of the group) lies, moved on by `step` rows at a time without a division; units are the caller's.
+struct Walk {
+    int64_t at, step, wrap;            // step: of the whole tokens and the heads of a move; wrap: from a token's end to the next one's start
+    int i, heads, group;
+    __device__ __forceinline__ Walk(int R, int move, int group_, int64_t per_token, int64_t per_head)
+        : at(R / group_ * per_token + R % group_ * per_head), step(move / group_ * per_token + move % group_ * per_head), wrap(per_token - group_ * per_head),
+          i(R % group_), heads(move % group_), group(group_) {}
+    __device__ __forceinline__ void on() {
+        at += step;
+        i += heads;
+        if (i >= group) i -= group, at += wrap;
     }
 };
 
@@ -211,19 +220,32 @@ __device__ __forceinline__ void spread(float (&x)[N], int lane) {
 template <bool BF16>
 __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     typedef Many<BF16> M;
-    constexpr int kKeys = M::kBlocks * 32, kStage = M::kStage;
-    __shared__ __attribute__((aligned(16))) char Qs[2][16384];
+    constexpr int kKeys = M::kBlocks * 32, kTiles = M::kTiles, kStage = kTiles * 32;
+    __shared__ __attribute__((aligned(16))) char Qs[2][32768];
+    __shared__ float Ls[2][kStage];                                // -lse of a stage's rows, in units of log 2
     const WeightsCall& c = a.c;
     const int g = blockIdx.x % a.groups, key_tile = blockIdx.x / a.groups % a.key_tiles, chunk = blockIdx.x / a.groups / a.key_tiles, b = g / c.kv, head = g % c.kv;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int length = length_of(c, b), j0 = key_tile * (4 * kKeys), j1 = min(j0 + 4 * kKeys, length) - 1;
     if (j0 > j1) return;
     const Tokens seeing = tokens_that_see(length, c.m, j0, j1, c.window, c.sinks);
     const int begin = max(chunk * a.chunk, seeing.first * c.group / kStage * kStage), end = min(min((chunk + 1) * a.chunk, a.rows), (seeing.last + 1) * c.group);
-    const bool nothing = begin >= end;                             // (without parts the old weights may still have to fade)
-    if (nothing && a.chunks > 1) return;
+    const int stages = (end - begin + kStage - 1) / kStage;        // (none: without parts the old weights may still have to fade)
+    if (stages <= 0 && a.chunks > 1) return;
 
-    const int k0 = j0 + wave * kKeys, k1 = min(k0 + kKeys, length) - 1;        // this wave's keys
+    // This wave's keys; the stages of which its keys are seen at all, and those whose rows all see all of them.
+    const int k0 = j0 + wave * kKeys, k1 = min(k0 + kKeys, length) - 1;
+    int seen_from = 0, seen_to = 0, whole_from = 0, whole_to = 0;
+    if (k0 <= k1) {
+        const Tokens some = tokens_that_see(length, c.m, k0, k1, c.window, c.sinks);
+        seen_from = (max(some.first * c.group, begin) - begin) / kStage;
+        seen_to = min(stages, ((some.last + 1) * c.group - begin + kStage - 1) / kStage);
+        const int64_t all_first = max((int64_t)k1 - (length - c.m), (int64_t)0) * c.group;     // the first row that sees k1, and the first that does not see k0 any more
+        const int64_t all_end = c.window > 0 && k1 >= c.sinks ? min((int64_t)a.rows, max((int64_t)k0 + c.window - (length - c.m), (int64_t)0) * c.group) : (int64_t)a.rows;
+        whole_from = (int)min(max(all_first - begin + kStage - 1, (int64_t)0) / kStage, (int64_t)stages);
+        whole_to = (int)min(max(all_end - begin, (int64_t)0) / kStage, (int64_t)stages);
+        if (whole_to <= whole_from) whole_from = whole_to = stages;
+    }
     M keys[M::kBlocks];
 #pragma unroll
     for (int kb = 0; kb < M::kBlocks; ++kb) keys[kb].load((const char*)c.K + ((int64_t)g * c.stride + min(k0 + kb * 32 + col, length - 1)) * M::kRow, half);
@@ -231,128 +253,140 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
 #pragma unroll
     for (int i = 0; i < M::kBlocks * 16; ++i) sums[i] = 0.f;
 
-    // Rows R on their way into LDS: columns of 64 bytes a row, pieces permuted by (row / 2) % 4; this lane's is row d_row of a stage, four columns of it from `column` on.
-    const int64_t per_token = (int64_t)c.kv * c.group * M::kRow;
-    const char* queries = (const char*)c.Q + ((int64_t)b * c.m * c.kv + head) * c.group * M::kRow;
-    const int d_row = (BF16 ? wave : wave & 1) * 16 + (lane >> 2), column = BF16 ? 0 : (wave >> 1) * 4;
-    const int piece = (lane & 3) ^ ((d_row >> 1) & 3);
-    const int stage_tokens = kStage / c.group, stage_heads = kStage % c.group, last_t = (a.rows - 1) / c.group, last_i = c.group - 1;
-    Row from(begin + d_row, c.group);
-    const uint32_t lds = lds_address(&Qs[0][0]);
-    const auto ask = [&](int buffer) ALWAYS_INLINE {
-        const bool there = from.t <= last_t;
-        const char* at = queries + (there ? from.t : last_t) * per_token + (there ? from.i : last_i) * M::kRow + column * 64 + piece * 16;
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + buffer * 16384 + column * (kStage * 64) + (BF16 ? wave : wave & 1) * 1024);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dma16_from(to + i * (kStage * 64), at + i * 64);
-        from.on(stage_tokens, stage_heads, c.group);
-    };
-    // The rows that this lane has scores of, R = 32 u + col of a stage: position and -lse.
-    constexpr int kTiles = kStage / 32;
+    // Rows on their way into LDS: tiles of 32 rows, in columns of 64 bytes a row, pieces of 16 permuted by (row / 2) % 4.  A wave has eight blocks of 16 rows' columns: of bf16 a
+    // tile's, of fp32 half of a tile's.
+    constexpr int kHalves = BF16 ? 2 : 1, kColumns = M::kRow / 64;
+    const int tile_of = BF16 ? wave : wave >> 1, half_of = BF16 ? 0 : wave & 1, piece = (lane & 3) ^ ((lane >> 3) & 3);
+    const int64_t per_token = (int64_t)c.kv * c.group * M::kRow, last_row = (a.rows - 1) / c.group * per_token + (c.group - 1) * M::kRow;
+    const char* queries = (const char*)c.Q + ((int64_t)b * c.m * c.kv + head) * c.group * M::kRow + piece * 16;
+    Walk low(begin + tile_of * 32 + half_of * 16 + (lane >> 2), kStage, c.group, per_token, M::kRow);
+    Walk high(begin + tile_of * 32 + 16 + (lane >> 2), kStage, c.group, per_token, M::kRow);           // (bf16: the tile's other half)
     const float* lse_of_head = c.lse + ((int64_t)b * c.kv + head) * c.group * c.m;
-    Row mine[kTiles];
-#pragma unroll
-    for (int u = 0; u < kTiles; ++u) mine[u] = Row(begin + u * 32 + col, c.group);
-    float lse[kTiles], next_lse[kTiles];
-    int p[kTiles];
-    const auto ask_lse = [&]() ALWAYS_INLINE {
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            const bool there = mine[u].t <= last_t;
-            next_lse[u] = lse_of_head[(int64_t)(there ? mine[u].i : last_i) * c.m + (there ? mine[u].t : last_t)];
+    Walk less_of(begin + tid % kStage, kStage, c.group, 1, c.m);
+    float next_less = 0.f;
+    const uint32_t lds = lds_address(&Qs[0][0]) + tile_of * (kColumns * 2048) + half_of * 1024;
+    const auto ask = [&](int stage) ALWAYS_INLINE {
+        int64_t at[2] = {low.at, high.at}, l = less_of.at;
+        if (begin + (stage + 1) * kStage > a.rows) {               // (what is behind the last row is not used)
+            const int R = begin + stage * kStage + tile_of * 32 + half_of * 16 + (lane >> 2);
+            if (R >= a.rows) at[0] = last_row;
+            if (R + 16 >= a.rows) at[1] = last_row;
+            if (begin + stage * kStage + tid % kStage >= a.rows) l = 0;
         }
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (stage & 1) * 32768);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < kColumns; ++i) dma16_from(to + h * 1024 + i * 2048, queries + at[h] + i * 64);
+        next_less = lse_of_head[l];
+        low.on();
+        if (BF16) high.on();
+        less_of.on();
     };
-    if (!nothing) {
-        ask(0);
-        ask_lse();
-        dma_wait();
-    }
-    __syncthreads();
-    const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
-    // bf16: the scores of the last block of 32 x 32 wait for the next one's products, between which their exponentials go
-    f32x16a s[2];
-    float waiting = -INFINITY;                                     // the -lse of s[1], of this wave's second 32 keys
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[1][i] = 0.f;
-    const auto weigh = [&](f32x16a& x, int kb, float less) ALWAYS_INLINE {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
-    };
-    for (int R0 = begin, buffer = 0; R0 < end; R0 += kStage, buffer ^= 1) {
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            lse[u] = next_lse[u];
-            p[u] = mine[u].t <= last_t ? length - c.m + mine[u].t : -1;
-            mine[u].on(stage_tokens, stage_heads, c.group);
-        }
-        if (R0 + kStage < end) {
-            ask(buffer ^ 1);
-            ask_lse();
-        }
-        // positions of the stage's rows, lowest (in lane 0) and highest; rows that are none stand at -1
-        const int low = __builtin_amdgcn_readfirstlane(p[0]), last = __builtin_amdgcn_readlane(p[kTiles - 1], 31), high = last < 0 ? length - 1 : last;
-        const bool whole = last >= 0 && low >= k1 && (c.window <= 0 || high - k0 < c.window || k1 < c.sinks) && !__any(lse[0] == -INFINITY || lse[kTiles - 1] == -INFINITY);
-        if (k0 > k1 || high < k0) {
-        } else if (BF16 && whole) {
-            if constexpr (BF16) {
-                const auto block = [&](const u32x4a (&q)[8], int kb, f32x16a& x, f32x16a& before, int kb_before, float less) ALWAYS_INLINE {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const f32x16a zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q[i]), i == 0 ? zero : x, 0, 0, 0);
-#pragma unroll
-                        for (int e = 2 * i; e < 2 * i + 2; ++e) sums[kb_before * 16 + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(before[e], a.scale_log2, less));
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                };
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u) {
-                    u32x4a q[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) q[i] = *(const u32x4a*)(Qs[buffer] + u * 2048 + k_at[i & 1] + (i >> 1) * (kStage * 64));
-                    const float less = -lse[u] * (1.f / kLn2);
-                    block(q, 0, s[0], s[1], 1, waiting);
-                    block(q, 1, s[1], s[0], 0, less);
-                    waiting = less;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int u = 0; u < kTiles; ++u) {
-                const int at = lse[u] == -INFINITY ? -1 : p[u];
-                const float less = -lse[u] * (1.f / kLn2);
-                const char* Qt = Qs[buffer] + u * 2048;
-#pragma unroll
-                for (int kb = 0; kb < M::kBlocks; ++kb) {
-                    f32x16a x;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < (BF16 ? 8 : 16); ++i) {
-                        const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * (kStage * 64));
-                        if constexpr (BF16) {
-                            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q), x, 0, 0, 0);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].x[i][e], __uint_as_float(q[e]), x, 0, 0, 0);
-                        }
-                    }
-                    if (!BF16 && whole) {
-                        weigh(x, kb, less);
-                        continue;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
-                        sums[kb * 16 + i] += sees(at, k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4, c.window, c.sinks) ? w : 0.f;
-                    }
-                }
-            }
-        }
+    const auto arrive = [&](int stage) ALWAYS_INLINE {
+        if (tid < kStage) Ls[stage & 1][tid] = next_less == -INFINITY ? -INFINITY : -next_less * (1.f / kLn2);     // (a row that sees nothing weighs nothing)
         dma_wait();
         __syncthreads();
+    };
+    const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+    // A stage of which some rows do not see some of the wave's keys, or are none.
+    const auto masked_stage = [&](int stage) ALWAYS_INLINE {
+#pragma unroll 1
+        for (int u = 0; u < kTiles; ++u) {
+            const int R = begin + stage * kStage + u * 32 + col;
+            const float less = Ls[stage & 1][u * 32 + col];
+            const int at = R < a.rows && less != -INFINITY ? length - c.m + R / c.group : -1;
+            const char* Qt = Qs[stage & 1] + u * (kColumns * 2048);
+#pragma unroll
+            for (int kb = 0; kb < M::kBlocks; ++kb) {
+                f32x16a x;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+                for (int i = 0; i < M::kRow / 32; ++i) {
+                    const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048);
+                    if constexpr (BF16) {
+                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q), x, 0, 0, 0);
+                    } else {
+                        const f32x4a y = __builtin_bit_cast(f32x4a, q);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].x[i][e], y[e], x, 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
+                    sums[kb * 16 + i] += sees(at, k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4, c.window, c.sinks) ? w : 0.f;
+                }
+            }
+        }
+    };
+    if (stages > 0) {
+        ask(0);
+        arrive(0);
     }
-    if constexpr (BF16) weigh(s[1], 1, waiting);
+    int stage = 0;
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {                         // stages with masks, whole ones, some with masks again
+        const int until = turn == 0 ? min(whole_from, stages) : stages;
+#pragma unroll 1
+        for (; stage < until; ++stage) {
+            if (stage + 1 < stages) ask(stage + 1);
+            if (stage >= seen_from && stage < seen_to) masked_stage(stage);
+            if (stage + 1 < stages) arrive(stage + 1);
+        }
+        if (turn == 1 || stage >= whole_to) continue;
+        if constexpr (BF16) {
+            // The scores of the last block of 32 x 32 wait for the next one's products, between which their exponentials go.
+            f32x16a s[2];
+            float waiting = -INFINITY;                             // the -lse of s[1], of this wave's second 32 keys
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[1][i] = 0.f;
+            const auto weigh = [&](const f32x16a& x, int kb, float less, int first, int count) ALWAYS_INLINE {
+#pragma unroll
+                for (int i = first; i < first + count; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
+            };
+            u32x4a q[8];
+            const auto read = [&](const char* Qt, int i) ALWAYS_INLINE { q[i] = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048); };
+            const auto block = [&](int kb, f32x16a& x, const f32x16a& before, float less, const char* Qt) ALWAYS_INLINE {
+                const f32x16a zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q[i]), i == 0 ? zero : x, 0, 0, 0);
+                    if (kb == 1) read(Qt, i);                                      // (the next tile's)
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i == 1) weigh(before, 1 - kb, less, 0, 3);                 // (a product's results are not there at once)
+                    if (i > 1 && i < 7) weigh(before, 1 - kb, less, 2 * i - 1, 2);
+                    if (i == 7) weigh(before, 1 - kb, less, 13, 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+#pragma unroll 1
+            for (; stage < whole_to; ++stage) {
+                if (stage + 1 < stages) ask(stage + 1);
+                const char* Qt = Qs[stage & 1];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) read(Qt, i);
+#pragma unroll 1
+                for (int u = 0; u < kTiles; ++u) {
+                    const float less = Ls[stage & 1][u * 32 + col];
+                    Qt += u + 1 < kTiles ? kColumns * 2048 : 0;
+                    block(0, s[0], s[1], waiting, Qt);
+                    block(1, s[1], s[0], less, Qt);
+                    waiting = less;
+                }
+                if (stage + 1 < stages) arrive(stage + 1);
+            }
+            weigh(s[1], 1, waiting, 0, 16);
+        } else {
+#pragma unroll 1
+            for (; stage < whole_to; ++stage) {
+                if (stage + 1 < stages) ask(stage + 1);
+                masked_stage(stage);
+                if (stage + 1 < stages) arrive(stage + 1);
+            }
+        }
+    }
     if constexpr (!BF16) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) sums[i] += __shfl_xor(sums[i], 16);
@@ -367,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
 // Adds up the chunks that see a key's tile, in order.
 template <bool BF16>
 __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
-    constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kStage;
+    constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kTiles * 32;
     const WeightsCall& c = a.c;
     const int g = blockIdx.x % a.groups, j = blockIdx.x / a.groups * 256 + threadIdx.x, length = length_of(c, g / c.kv);
     if (j >= length) return;
@@ -397,11 +431,11 @@ hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStr
         else past ? launch(weights_few_kernel<false, 2, true>) : launch(weights_few_kernel<false, 2, false>);
         return hipGetLastError();
     }
-    const int keys = bf16 ? 256 : 128, stage = bf16 ? 64 : 32;
+    const int keys = bf16 ? 256 : 128, stage = bf16 ? 128 : 64;
     a.key_tiles = (call.n + keys - 1) / keys;
     // Rows shared out over workgroups until there are eight for every unit, half of them above the diagonal, eight stages each at least, as far as there is scratch.
     const int64_t blocks = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (blocks * keys * (int64_t)sizeof(float)) : 0;
-    const int64_t chunks = std::max<int64_t>(1, std::min(std::min<int64_t>(16 * (int64_t)ctx->num_cu / blocks, a.rows / (8 * stage)), std::min(room, kMostBlocks / blocks)));
+    const int64_t chunks = std::max<int64_t>(1, std::min(std::min<int64_t>(CM * (int64_t)ctx->num_cu / blocks, a.rows / (CS * stage)), std::min(room, kMostBlocks / blocks)));
     a.chunk = (int)(((a.rows + chunks - 1) / chunks + stage - 1) / stage * stage);
     a.chunks = (a.rows + a.chunk - 1) / a.chunk;
     a.part = (float*)((char*)call.scratch + kScratchCounters);

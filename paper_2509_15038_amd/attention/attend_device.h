@@ -77,6 +77,9 @@ __device__ __forceinline__ float halves_sum(float x) {
 __device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
 }
+// Loaded by here: the compiler, which does not count copies into LDS, would else wait for such a register's load, and with it for the copies asked for since, where it is first used.
+template <class T>
+__device__ __forceinline__ void loaded(T& x) { asm volatile("" : "+v"(x)); }
 // A value that is the same in all lanes, where the compiler does not see it.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);

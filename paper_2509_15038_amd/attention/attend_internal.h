@@ -11,6 +11,20 @@ namespace curdkv {
 constexpr int64_t kPastCaches = 128 << 20;     // bytes that a call moves from which its rows pass the caches (Infinity Cache: 256 MB)
 constexpr int64_t kScratchCounters = 16384;     // bytes at the start of a call's scratch that are zeros between the calls
 
+// Division of 0 .. 2^31 - 1 by a number of the host's, by a product and a shift: with 2^(s-1) < d <= 2^s and m = floor(2^32 (2^s - d) / d) + 1, n / d = (n + floor(m n / 2^32)) / 2^s.
+struct Divisor {
+    uint32_t d, m, s;
+    Divisor() = default;
+    explicit Divisor(int64_t by) : d((uint32_t)by), m(0), s(0) {
+        while (((uint64_t)1 << s) < d) ++s;
+        m = (uint32_t)((((((uint64_t)1 << s) - d) << 32) / d) + 1);
+    }
+#ifdef __HIP__
+    __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+    __device__ __forceinline__ int rest(int n, int quotient) const { return n - quotient * (int)d; }
+#endif
+};
+
 struct AttendCall {
     const void* Q;
     void* out;

@@ -347,6 +347,8 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, const 
         ask(0);
         arrive(0);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) loaded(w.q[i]);
     for (int tile = 0; tile < tiles; ++tile) {
         if (tile + 1 < tiles) ask(tile + 1);
         const char *Kt = lds + (tile & 1) * 32768, *Vt = Kt + 16384;

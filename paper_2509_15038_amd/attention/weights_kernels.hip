@@ -20,8 +20,9 @@ struct WeightsArgs {
     float scale_log2;
     int groups, rows, key_tiles;       // count * kv; m * group; tiles of keys a head
     int shares;                        // few rows: workgroups that share a head's keys
-    int chunk, chunks;                 // many rows: that a workgroup takes
-    float* part;                       // chunks > 1: [chunks][groups][key_tiles * keys of a tile], of the chunks that see some key of the tile
+    int chunk, first_chunk, chunks;    // many rows: that a workgroup takes, counted from the first that sees a key of its tile; this launch's chunks
+    float* part;                       // chunks > 1: [chunks][groups][key_tiles * keys of a tile], of the chunks that there are
+    Divisor by_groups, by_key_tiles, by_kv, by_group;
 };
 
 // Tokens of the m that see some key of j0 .. j1: [first, last].
@@ -191,19 +192,33 @@ template <> struct Many<false> {
     }
 };
 
-// Where a row R = (token, head of the group) lies, moved on by `step` rows at a time without a division; units are the caller's.
+// Where a row R = (token, head of the group) lies, moved on by as many rows at a time without a division; units are the caller's.
 struct Walk {
-    int64_t at, step, wrap;            // step: of the whole tokens and the heads of a move; wrap: from a token's end to the next one's start
-    int i, heads, group;
-    __device__ __forceinline__ Walk(int R, int move, int group_, int64_t per_token, int64_t per_head)
-        : at(R / group_ * per_token + R % group_ * per_head), step(move / group_ * per_token + move % group_ * per_head), wrap(per_token - group_ * per_head),
-          i(R % group_), heads(move % group_), group(group_) {}
-    __device__ __forceinline__ void on() {
-        at += step;
+    uint32_t at;
+    int i;
+    __device__ __forceinline__ Walk(int R, const Divisor& group, uint32_t per_token, uint32_t per_head) {
+        const int t = group.of(R);
+        i = group.rest(R, t);
+        at = t * per_token + i * per_head;
+    }
+    // heads: of the move beyond whole tokens; step: of all of it; wrap: from a token's end to the next one's start
+    __device__ __forceinline__ void on(int heads, uint32_t step, uint32_t wrap, int group) {
         i += heads;
-        if (i >= group) i -= group, at += wrap;
+        at += step;
+        const bool over = i >= group;
+        i -= over ? group : 0;
+        at += over ? wrap : 0;
     }
 };
+
+// The rows that a tile's keys j0 .. j1 are seen by, from the start of a stage on: [begin, end).
+struct Span {
+    int begin, end;
+};
+__device__ __forceinline__ Span rows_that_see(const WeightsArgs& a, int length, int j0, int j1, int stage) {
+    const Tokens t = tokens_that_see(length, a.c.m, j0, j1, a.c.window, a.c.sinks);
+    return {t.first * a.c.group / stage * stage, (t.last + 1) * a.c.group};
+}
 
 // Sums of 2 W values over 2 W lanes, value `lane` to each lane's x[0]: at every step a lane keeps half of them and gives away the others'.
 template <int W, int N>
@@ -224,17 +239,59 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     __shared__ __attribute__((aligned(16))) char Qs[2][32768];
     __shared__ float Ls[2][kStage];                                // -lse of a stage's rows, in units of log 2
     const WeightsCall& c = a.c;
-    const int g = blockIdx.x % a.groups, key_tile = blockIdx.x / a.groups % a.key_tiles, chunk = blockIdx.x / a.groups / a.key_tiles, b = g / c.kv, head = g % c.kv;
+    // Chunks that begin at the diagonal, which have masks and take longest, first.
+    const int tile = a.by_groups.of(blockIdx.x), part = a.by_key_tiles.of(tile), chunk = a.first_chunk + part, key_tile = a.by_key_tiles.rest(tile, part);
+    const int g = a.by_groups.rest(blockIdx.x, tile), b = a.by_kv.of(g), head = a.by_kv.rest(g, b);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int length = length_of(c, b), j0 = key_tile * (4 * kKeys), j1 = min(j0 + 4 * kKeys, length) - 1;
     if (j0 > j1) return;
-    const Tokens seeing = tokens_that_see(length, c.m, j0, j1, c.window, c.sinks);
-    const int begin = max(chunk * a.chunk, seeing.first * c.group / kStage * kStage), end = min(min((chunk + 1) * a.chunk, a.rows), (seeing.last + 1) * c.group);
-    const int stages = (end - begin + kStage - 1) / kStage;        // (none: without parts the old weights may still have to fade)
-    if (stages <= 0 && a.chunks > 1) return;
+    const Span span = rows_that_see(a, length, j0, j1, kStage);
+    if (chunk > 0 && chunk >= (span.end - span.begin + a.chunk - 1) / a.chunk) return;     // (the first is there anyway: the old weights may have to fade)
+    const int begin = span.begin + chunk * a.chunk, stages = (min(a.chunk, span.end - begin) + kStage - 1) / kStage;
+
+    // Rows on their way into LDS: tiles of 32 rows, in columns of 64 bytes a row, pieces of 16 permuted by (row / 2) % 4.  A wave has eight blocks of 16 rows' columns: of bf16 a
+    // tile's, of fp32 half of a tile's.
+    constexpr int kHalves = BF16 ? 2 : 1, kColumns = M::kRow / 64;
+    const int tile_of = BF16 ? wave : wave >> 1, half_of = BF16 ? 0 : wave & 1, piece = (lane & 3) ^ ((lane >> 3) & 3), my_row = tile_of * 32 + half_of * 16 + (lane >> 2);
+    const uint32_t per_token = c.kv * c.group * M::kRow, over = per_token - c.group * M::kRow;
+    const int first_token = a.by_group.of(begin), first_row = first_token * c.group;               // (offsets count from here)
+    const int move_tokens = a.by_group.of(kStage), move_heads = a.by_group.rest(kStage, move_tokens);
+    const char* queries = (const char*)uniform((int64_t)((const char*)c.Q + ((((int64_t)b * c.m + first_token) * c.kv + head) * c.group) * M::kRow));
+    Walk low(begin - first_row + my_row, a.by_group, per_token, M::kRow), high(begin - first_row + my_row + 16, a.by_group, per_token, M::kRow);       // (bf16: two halves of a tile)
+    const float* lse_of_head = (const float*)uniform((int64_t)(c.lse + ((int64_t)b * c.kv + head) * c.group * c.m + first_token));
+    Walk less_of(begin - first_row + tid % kStage, a.by_group, 1, c.m);
+    float next_less = 0.f;
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(&Qs[0][0]) + tile_of * (kColumns * 2048) + half_of * 1024);
+    const auto ask = [&](int stage) ALWAYS_INLINE {
+        uint32_t at[2] = {low.at + piece * 16, high.at + piece * 16}, l = less_of.at;
+        if (begin + (stage + 1) * kStage > a.rows) {               // (what is behind the last row is not used)
+            const int R = begin + stage * kStage;
+            if (R + my_row >= a.rows) at[0] = piece * 16;
+            if (R + my_row + 16 >= a.rows) at[1] = piece * 16;
+            if (R + tid % kStage >= a.rows) l = 0;
+        }
+        const uint32_t to = lds + (stage & 1) * 32768;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < kColumns; ++i) dma16(to + h * 1024 + i * 2048, queries, at[h] + i * 64);
+        next_less = lse_of_head[l];
+        low.on(move_heads, move_tokens * per_token + move_heads * M::kRow, over, c.group);
+        if (BF16) high.on(move_heads, move_tokens * per_token + move_heads * M::kRow, over, c.group);
+        less_of.on(move_heads, move_tokens + move_heads * c.m, 1 - c.group * c.m, c.group);
+    };
+    const auto arrive = [&](int stage) ALWAYS_INLINE {
+        if (tid < kStage) Ls[stage & 1][tid] = next_less == -INFINITY ? -INFINITY : -next_less * (1.f / kLn2);     // (a row that sees nothing weighs nothing)
+        dma_wait();
+        __syncthreads();
+    };
+    if (stages > 0) ask(0);
 
     // This wave's keys; the stages of which its keys are seen at all, and those whose rows all see all of them.
     const int k0 = j0 + wave * kKeys, k1 = min(k0 + kKeys, length) - 1;
+    M keys[M::kBlocks];
+#pragma unroll
+    for (int kb = 0; kb < M::kBlocks; ++kb) keys[kb].load((const char*)c.K + ((int64_t)g * c.stride + min(k0 + kb * 32 + col, length - 1)) * M::kRow, half);
     int seen_from = 0, seen_to = 0, whole_from = 0, whole_to = 0;
     if (k0 <= k1) {
         const Tokens some = tokens_that_see(length, c.m, k0, k1, c.window, c.sinks);
@@ -246,48 +303,9 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
         whole_to = (int)min(max(all_end - begin, (int64_t)0) / kStage, (int64_t)stages);
         if (whole_to <= whole_from) whole_from = whole_to = stages;
     }
-    M keys[M::kBlocks];
-#pragma unroll
-    for (int kb = 0; kb < M::kBlocks; ++kb) keys[kb].load((const char*)c.K + ((int64_t)g * c.stride + min(k0 + kb * 32 + col, length - 1)) * M::kRow, half);
     float sums[M::kBlocks * 16];
 #pragma unroll
     for (int i = 0; i < M::kBlocks * 16; ++i) sums[i] = 0.f;
-
-    // Rows on their way into LDS: tiles of 32 rows, in columns of 64 bytes a row, pieces of 16 permuted by (row / 2) % 4.  A wave has eight blocks of 16 rows' columns: of bf16 a
-    // tile's, of fp32 half of a tile's.
-    constexpr int kHalves = BF16 ? 2 : 1, kColumns = M::kRow / 64;
-    const int tile_of = BF16 ? wave : wave >> 1, half_of = BF16 ? 0 : wave & 1, piece = (lane & 3) ^ ((lane >> 3) & 3);
-    const int64_t per_token = (int64_t)c.kv * c.group * M::kRow, last_row = (a.rows - 1) / c.group * per_token + (c.group - 1) * M::kRow;
-    const char* queries = (const char*)c.Q + ((int64_t)b * c.m * c.kv + head) * c.group * M::kRow + piece * 16;
-    Walk low(begin + tile_of * 32 + half_of * 16 + (lane >> 2), kStage, c.group, per_token, M::kRow);
-    Walk high(begin + tile_of * 32 + 16 + (lane >> 2), kStage, c.group, per_token, M::kRow);           // (bf16: the tile's other half)
-    const float* lse_of_head = c.lse + ((int64_t)b * c.kv + head) * c.group * c.m;
-    Walk less_of(begin + tid % kStage, kStage, c.group, 1, c.m);
-    float next_less = 0.f;
-    const uint32_t lds = lds_address(&Qs[0][0]) + tile_of * (kColumns * 2048) + half_of * 1024;
-    const auto ask = [&](int stage) ALWAYS_INLINE {
-        int64_t at[2] = {low.at, high.at}, l = less_of.at;
-        if (begin + (stage + 1) * kStage > a.rows) {               // (what is behind the last row is not used)
-            const int R = begin + stage * kStage + tile_of * 32 + half_of * 16 + (lane >> 2);
-            if (R >= a.rows) at[0] = last_row;
-            if (R + 16 >= a.rows) at[1] = last_row;
-            if (begin + stage * kStage + tid % kStage >= a.rows) l = 0;
-        }
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (stage & 1) * 32768);
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-            for (int i = 0; i < kColumns; ++i) dma16_from(to + h * 1024 + i * 2048, queries + at[h] + i * 64);
-        next_less = lse_of_head[l];
-        low.on();
-        if (BF16) high.on();
-        less_of.on();
-    };
-    const auto arrive = [&](int stage) ALWAYS_INLINE {
-        if (tid < kStage) Ls[stage & 1][tid] = next_less == -INFINITY ? -INFINITY : -next_less * (1.f / kLn2);     // (a row that sees nothing weighs nothing)
-        dma_wait();
-        __syncthreads();
-    };
     const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
     // A stage of which some rows do not see some of the wave's keys, or are none.
     const auto masked_stage = [&](int stage) ALWAYS_INLINE {
@@ -295,7 +313,14 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
         for (int u = 0; u < kTiles; ++u) {
             const int R = begin + stage * kStage + u * 32 + col;
             const float less = Ls[stage & 1][u * 32 + col];
-            const int at = R < a.rows && less != -INFINITY ? length - c.m + R / c.group : -1;
+            // the keys that this lane's row sees, from k0 + 4 half on: up to `far`, but for those at `near` and below that are not below `first`
+            const int at = R < a.rows && less != -INFINITY ? length - c.m + a.by_group.of(R) : -1, far = at - k0 - half * 4;
+            uint64_t seen = far < 0 ? 0 : far >= 63 ? ~0ull : (2ull << far) - 1;
+            if (c.window > 0) {
+                const int64_t near = (int64_t)far - c.window, first = (int64_t)c.sinks - k0 - half * 4;
+                seen &= (near < 0 ? ~0ull : near >= 63 ? 0ull : ~((2ull << near) - 1)) | (first <= 0 ? 0ull : first >= 64 ? ~0ull : (1ull << first) - 1);
+            }
+            if (!__any(seen != 0)) continue;
             const char* Qt = Qs[stage & 1] + u * (kColumns * 2048);
 #pragma unroll
             for (int kb = 0; kb < M::kBlocks; ++kb) {
@@ -315,16 +340,17 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
-                    sums[kb * 16 + i] += sees(at, k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4, c.window, c.sinks) ? w : 0.f;
+                    const uint32_t keep = (int)((uint32_t)(seen >> (kb * 32)) << (31 - (i / 4 * 8 + i % 4))) >> 31;        // all bits, or none
+                    sums[kb * 16 + i] += __uint_as_float(__float_as_uint(__builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less))) & keep);
                 }
             }
         }
     };
-    if (stages > 0) {
-        ask(0);
-        arrive(0);
-    }
+    if (stages > 0) arrive(0);
+#pragma unroll
+    for (int kb = 0; kb < M::kBlocks; ++kb)
+#pragma unroll
+        for (int i = 0; i < M::kRow / 32; ++i) loaded(keys[kb].x[i]);
     int stage = 0;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {                         // stages with masks, whole ones, some with masks again
@@ -337,47 +363,50 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
         }
         if (turn == 1 || stage >= whole_to) continue;
         if constexpr (BF16) {
-            // The scores of the last block of 32 x 32 wait for the next one's products, between which their exponentials go.
-            f32x16a s[2];
-            float waiting = -INFINITY;                             // the -lse of s[1], of this wave's second 32 keys
+            // The scores of one tile wait for the next one's products, between which their exponentials go: two products, of either 32 keys, then two scores' of each.
+            f32x16a s[2][2];
+            float less[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[1][i] = 0.f;
-            const auto weigh = [&](const f32x16a& x, int kb, float less, int first, int count) ALWAYS_INLINE {
-#pragma unroll
-                for (int i = first; i < first + count; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
-            };
-            u32x4a q[8];
-            const auto read = [&](const char* Qt, int i) ALWAYS_INLINE { q[i] = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048); };
-            const auto block = [&](int kb, f32x16a& x, const f32x16a& before, float less, const char* Qt) ALWAYS_INLINE {
+            for (int i = 0; i < 16; ++i) s[1][0][i] = s[1][1][i] = 0.f;
+            u32x4a q[4];
+            const auto read = [&](const char* Qt, int i) ALWAYS_INLINE { q[i & 3] = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048); };
+            const auto tile = [&](int now, const char* Qt, const char* next) ALWAYS_INLINE {
                 const f32x16a zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q[i]), i == 0 ? zero : x, 0, 0, 0);
-                    if (kb == 1) read(Qt, i);                                      // (the next tile's)
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (i == 1) weigh(before, 1 - kb, less, 0, 3);                 // (a product's results are not there at once)
-                    if (i > 1 && i < 7) weigh(before, 1 - kb, less, 2 * i - 1, 2);
-                    if (i == 7) weigh(before, 1 - kb, less, 13, 3);
-                    __builtin_amdgcn_sched_barrier(0);
+                    if (i < 6) read(Qt, i + 2);
+                    else read(next, i - 6);
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        s[now][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q[i & 3]), i == 0 ? zero : s[now][kb], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int e = 2 * i; e < 2 * i + 2; ++e)
+                            sums[kb * 16 + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[now ^ 1][kb][e], a.scale_log2, less[now ^ 1]));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             };
 #pragma unroll 1
             for (; stage < whole_to; ++stage) {
                 if (stage + 1 < stages) ask(stage + 1);
                 const char* Qt = Qs[stage & 1];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) read(Qt, i);
+                read(Qt, 0);
+                read(Qt, 1);
 #pragma unroll 1
-                for (int u = 0; u < kTiles; ++u) {
-                    const float less = Ls[stage & 1][u * 32 + col];
-                    Qt += u + 1 < kTiles ? kColumns * 2048 : 0;
-                    block(0, s[0], s[1], waiting, Qt);
-                    block(1, s[1], s[0], less, Qt);
-                    waiting = less;
+                for (int u = 0; u < kTiles; u += 2) {
+                    less[0] = Ls[stage & 1][u * 32 + col];
+                    tile(0, Qt, Qt + 8192);
+                    less[1] = Ls[stage & 1][u * 32 + 32 + col];
+                    tile(1, Qt + 8192, u + 2 < kTiles ? Qt + 16384 : Qt);
+                    Qt += 16384;
                 }
                 if (stage + 1 < stages) arrive(stage + 1);
             }
-            weigh(s[1], 1, waiting, 0, 16);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[kb * 16 + i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][kb][i], a.scale_log2, less[1]));
         } else {
 #pragma unroll 1
             for (; stage < whole_to; ++stage) {
@@ -394,7 +423,7 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     spread<M::kBlocks * 8>(sums, col);
     const int i = col & 15, kb = BF16 ? col >> 4 : 0, j = k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4;
     if (j >= length || (!BF16 && col >= 16)) return;
-    if (a.chunks > 1) a.part[((int64_t)chunk * a.groups + g) * a.key_tiles * (4 * kKeys) + j] = sums[0];
+    if (a.chunks > 1) a.part[((int64_t)part * a.groups + g) * a.key_tiles * (4 * kKeys) + j] = sums[0];
     else add_to(c, g, j, sums[0]);
 }
 
@@ -405,12 +434,9 @@ __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
     const WeightsCall& c = a.c;
     const int g = blockIdx.x % a.groups, j = blockIdx.x / a.groups * 256 + threadIdx.x, length = length_of(c, g / c.kv);
     if (j >= length) return;
-    const int j0 = j / kKeys * kKeys;
-    const Tokens seeing = tokens_that_see(length, c.m, j0, min(j0 + kKeys, length) - 1, c.window, c.sinks);
-    const int begin = seeing.first * c.group / kStage * kStage, end = min(a.rows, (seeing.last + 1) * c.group);
+    const Span span = rows_that_see(a, length, j / kKeys * kKeys, min(j / kKeys * kKeys + kKeys, length) - 1, kStage);
     float sum = 0.f;
-    if (begin < end)
-        for (int chunk = begin / a.chunk; chunk <= (end - 1) / a.chunk; ++chunk) sum += a.part[((int64_t)chunk * a.groups + g) * a.key_tiles * kKeys + j];
+    for (int part = 0; part < a.chunks && (a.first_chunk + part) * a.chunk < span.end - span.begin; ++part) sum += a.part[((int64_t)part * a.groups + g) * a.key_tiles * kKeys + j];
     add_to(c, g, j, sum);
 }
 
@@ -418,7 +444,7 @@ __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
 
 hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStream_t stream) {
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
-    WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, 1, nullptr};
+    WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, 0, 1, nullptr, Divisor(call.count * call.kv), Divisor(1), Divisor(call.kv), Divisor(call.group)};
     if (a.rows <= 32) {
         const int64_t steps = (call.n + 63) / 64, waves = WV * (int64_t)ctx->num_cu;
         const int64_t each = std::max<int64_t>(1, std::min<int64_t>(TE, a.groups * steps / waves));
@@ -433,17 +459,25 @@ hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStr
     }
     const int keys = bf16 ? 256 : 128, stage = bf16 ? 128 : 64;
     a.key_tiles = (call.n + keys - 1) / keys;
-    // Rows shared out over workgroups until there are eight for every unit, half of them above the diagonal, eight stages each at least, as far as there is scratch.
-    const int64_t blocks = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (blocks * keys * (int64_t)sizeof(float)) : 0;
-    const int64_t chunks = std::max<int64_t>(1, std::min(std::min<int64_t>(CM * (int64_t)ctx->num_cu / blocks, a.rows / (CS * stage)), std::min(room, kMostBlocks / blocks)));
-    a.chunk = (int)(((a.rows + chunks - 1) / chunks + stage - 1) / stage * stage);
-    a.chunks = (a.rows + a.chunk - 1) / a.chunk;
+    a.by_key_tiles = Divisor(a.key_tiles);
+    // Rows shared out over workgroups until there are twelve for every unit, half of them above the diagonal, two stages each at least; 2^31 bytes of queries at most.
+    const int64_t blocks = (int64_t)a.groups * a.key_tiles, most = ((int64_t)1 << 31) / (call.kv * (bf16 ? 256 : 512)) / stage * stage;
+    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(CM * (int64_t)ctx->num_cu / blocks, a.rows / (CS * stage)));
+    a.chunk = (int)std::min(((a.rows + wanted - 1) / wanted + stage - 1) / stage * stage, most);
+    const int all = (a.rows + a.chunk - 1) / a.chunk;              // (counted from a stage's start: no more of them than of all rows)
+    // As many at once as there is scratch for; the weights of one launch are the old ones of the next.
+    const int64_t room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (blocks * keys * (int64_t)sizeof(float)) : 0;
+    const int at_once = (int)std::max<int64_t>(1, std::min<int64_t>(all, std::min(room, kMostBlocks / blocks)));
     a.part = (float*)((char*)call.scratch + kScratchCounters);
     const auto launch = [&](auto kernel, int64_t n) { kernel<<<(unsigned)n, 256, 0, stream>>>(a); };
-    bf16 ? launch(weights_many_kernel<true>, blocks * a.chunks) : launch(weights_many_kernel<false>, blocks * a.chunks);
-    if (a.chunks > 1) {
-        const int64_t joins = (int64_t)a.groups * ((call.n + 255) / 256);
-        bf16 ? launch(weights_join_kernel<true>, joins) : launch(weights_join_kernel<false>, joins);
+    for (a.first_chunk = 0; a.first_chunk < all; a.first_chunk += at_once) {
+        a.chunks = std::min(at_once, all - a.first_chunk);
+        bf16 ? launch(weights_many_kernel<true>, blocks * a.chunks) : launch(weights_many_kernel<false>, blocks * a.chunks);
+        if (a.chunks > 1) {
+            const int64_t joins = (int64_t)a.groups * ((call.n + 255) / 256);
+            bf16 ? launch(weights_join_kernel<true>, joins) : launch(weights_join_kernel<false>, joins);
+        }
+        a.c.decay = 1.f;
     }
     return hipGetLastError();
 }

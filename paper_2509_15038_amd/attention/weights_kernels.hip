@@ -19,10 +19,10 @@ struct WeightsArgs {
     WeightsCall c;
     float scale_log2;
     int groups, rows, key_tiles;       // count * kv; m * group; tiles of keys a head
-    int shares;                        // few rows: workgroups that share a head's keys
-    int chunk, first_chunk, chunks;    // many rows: that a workgroup takes, counted from the first that sees a key of its tile; this launch's chunks
-    float* part;                       // chunks > 1: [chunks][groups][key_tiles * keys of a tile], of the chunks that there are
-    Divisor by_groups, by_key_tiles, by_kv, by_group;
+    int shares;                        // workgroups that share a head's keys; of many rows: its products (0: a workgroup has a tile of keys)
+    int most;                          // many rows: stages whose queries lie within 2^31 bytes
+    float* part;                       // many rows, shared: [groups][shares + key_tiles][keys of a tile], of share s and tile t at s + t, which no other pair has
+    Divisor by_groups, by_kv, by_group;
 };
 
 // Tokens of the m that see some key of j0 .. j1: [first, last].
@@ -35,9 +35,9 @@ __device__ __forceinline__ Tokens tokens_that_see(int length, int m, int j0, int
     return {(int)min(max((int64_t)j0 - p0, (int64_t)0), (int64_t)m), (int)max(last, (int64_t)-1)};
 }
 __device__ __forceinline__ int length_of(const WeightsCall& c, int b) { return __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n); }
-__device__ __forceinline__ void add_to(const WeightsCall& c, int g, int j, float sum) {
+__device__ __forceinline__ void add_to(const WeightsCall& c, int g, int j, float sum, float decay) {
     float* to = c.mass + (int64_t)g * c.mass_stride + j;
-    *to = c.decay == 0.f ? sum : __builtin_fmaf(c.decay, *to, sum);
+    *to = decay == 0.f ? sum : __builtin_fmaf(decay, *to, sum);
 }
 
 // ---- few rows
@@ -86,27 +86,11 @@ __device__ __forceinline__ void to_rows(T& x, T& y) {
     }
     x = __builtin_bit_cast(T, u), y = __builtin_bit_cast(T, v);
 }
-#ifndef CM
-#define CM 24
-#endif
-#ifndef CS
-#define CS 2
-#endif
-#ifndef TE
-#define TE 4
-#endif
-#ifndef AH
-#define AH 1
-#endif
-#ifndef WV
-#define WV 16
-#endif
-
-// 16 TILES rows R at most.  A wave takes the 64 keys of a step 16 at a time, kAhead more of them on their way, and reads and writes their weights together.
+// 16 TILES rows R at most.  A wave takes the 64 keys of a step 16 at a time, the next 16 on their way, and reads and writes their weights together.
 // PAST: keys pass the caches.
 template <bool BF16, int TILES, bool PAST>
 __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
-    constexpr int kRow = BF16 ? 256 : 512, kPieces = BF16 ? 4 : 8, kAhead = BF16 ? AH : 1;
+    constexpr int kRow = BF16 ? 256 : 512, kPieces = BF16 ? 4 : 8;
     const WeightsCall& c = a.c;
     const int head = blockIdx.x % c.kv, share = blockIdx.x / c.kv % a.shares, b = blockIdx.x / c.kv / a.shares, g = b * c.kv + head;
     const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -115,7 +99,7 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
     if (first >= end) return;
     const char* keys = (const char*)c.K + (int64_t)g * c.stride * kRow;
     float* mass = c.mass + (int64_t)g * c.mass_stride;
-    Operand<BF16> ahead[4], q[TILES];
+    Operand<BF16> ahead[2], q[TILES];
     const auto ask = [&](Operand<BF16>& k, int j0) ALWAYS_INLINE {
 #pragma unroll
         for (int s = 0; s < kPieces; ++s) {
@@ -123,8 +107,7 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
             k.x[s] = PAST ? __builtin_nontemporal_load(from) : *from;
         }
     };
-#pragma unroll
-    for (int x = 0; x < kAhead; ++x) ask(ahead[x], first * 64 + x * 16);
+    ask(ahead[0], first * 64);
     // rows 16 u + col as the operand; of rows 16 u + 4 quarter + i, whose scores come back, the position (below all where the row gives nothing) and -lse
     int p[TILES][4];
     float less[TILES][4];
@@ -146,8 +129,8 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
         float mine = 0.f;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            ask(ahead[(x + kAhead) % 4], step * 64 + (x + kAhead) * 16);
-            Operand<BF16> k = ahead[x];
+            ask(ahead[(x + 1) % 2], step * 64 + x * 16 + 16);
+            Operand<BF16> k = ahead[x % 2];
 #pragma unroll
             for (int s = 0; s < kPieces; s += 2) to_rows(k.x[s], k.x[s + 1]);
             float sum = 0.f;
@@ -211,14 +194,47 @@ struct Walk {
     }
 };
 
-// The rows that a tile's keys j0 .. j1 are seen by, from the start of a stage on: [begin, end).
+// The rows that keys j0 .. j1 are seen by, from the start of a stage on: its first one, and how many.
 struct Span {
-    int begin, end;
+    int begin, stages;
 };
 __device__ __forceinline__ Span rows_that_see(const WeightsArgs& a, int length, int j0, int j1, int stage) {
     const Tokens t = tokens_that_see(length, a.c.m, j0, j1, a.c.window, a.c.sinks);
-    return {t.first * a.c.group / stage * stage, (t.last + 1) * a.c.group};
+    const int begin = t.first * a.c.group / stage * stage, end = (t.last + 1) * a.c.group;
+    return {begin, j0 <= j1 && begin < end ? (end - begin + stage - 1) / stage : 0};
 }
+
+// A head's products are shared out over `shares` workgroups by the cost of its tiles of keys, one after the other: their stages, and kTileCost for the keys and the masks at a tile's
+// first ones.  Share s has what lies in [total s / shares, total (s + 1) / shares).
+constexpr int kTileCost = 6;
+template <int KEYS, int STAGE>
+struct Shares {
+    const WeightsArgs& a;
+    int length;
+    __device__ __forceinline__ int stages(int tile) const {
+        return tile < a.key_tiles ? rows_that_see(a, length, tile * KEYS, min(tile * KEYS + KEYS, length) - 1, STAGE).stages : 0;
+    }
+    static __device__ __forceinline__ int cost(int stages) { return stages > 0 ? stages + kTileCost : 0; }
+    // sum over the lanes up to and with this one
+    static __device__ __forceinline__ int up_to(int x) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(x, d);
+            if (lane >= d) x += y;
+        }
+        return x;
+    }
+    // the cost of the tiles below `tile`
+    __device__ __forceinline__ int64_t below(int tile) const {
+        int64_t sum = 0;
+        for (int base = 0; base < tile; base += 64) {
+            const int at = base + (int)(threadIdx.x & 63);
+            sum += __builtin_amdgcn_readlane(up_to(at < tile ? cost(stages(at)) : 0), 63);
+        }
+        return sum;
+    }
+};
 
 // Sums of 2 W values over 2 W lanes, value `lane` to each lane's x[0]: at every step a lane keeps half of them and gives away the others'.
 template <int W, int N>
@@ -232,22 +248,15 @@ __device__ __forceinline__ void spread(float (&x)[N], int lane) {
     if constexpr (W > 1) spread<W / 2>(x, lane);
 }
 
+// Stages from .. to - 1 of a tile of keys; `more`: the same workgroup has written this tile's sums before.
 template <bool BF16>
-__global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
+__device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[32768], float (*Ls)[Many<BF16>::kTiles * 32], int g, int b, int head, int length, int key_tile, int begin,
+                                            int stages, float* part, bool more) {
     typedef Many<BF16> M;
     constexpr int kKeys = M::kBlocks * 32, kTiles = M::kTiles, kStage = kTiles * 32;
-    __shared__ __attribute__((aligned(16))) char Qs[2][32768];
-    __shared__ float Ls[2][kStage];                                // -lse of a stage's rows, in units of log 2
     const WeightsCall& c = a.c;
-    // Chunks that begin at the diagonal, which have masks and take longest, first.
-    const int tile = a.by_groups.of(blockIdx.x), part = a.by_key_tiles.of(tile), chunk = a.first_chunk + part, key_tile = a.by_key_tiles.rest(tile, part);
-    const int g = a.by_groups.rest(blockIdx.x, tile), b = a.by_kv.of(g), head = a.by_kv.rest(g, b);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
-    const int length = length_of(c, b), j0 = key_tile * (4 * kKeys), j1 = min(j0 + 4 * kKeys, length) - 1;
-    if (j0 > j1) return;
-    const Span span = rows_that_see(a, length, j0, j1, kStage);
-    if (chunk > 0 && chunk >= (span.end - span.begin + a.chunk - 1) / a.chunk) return;     // (the first is there anyway: the old weights may have to fade)
-    const int begin = span.begin + chunk * a.chunk, stages = (min(a.chunk, span.end - begin) + kStage - 1) / kStage;
+    const int j0 = key_tile * (4 * kKeys);
 
     // Rows on their way into LDS: tiles of 32 rows, in columns of 64 bytes a row, pieces of 16 permuted by (row / 2) % 4.  A wave has eight blocks of 16 rows' columns: of bf16 a
     // tile's, of fp32 half of a tile's.
@@ -285,6 +294,7 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
         dma_wait();
         __syncthreads();
     };
+    __syncthreads();                                               // (nobody reads the tile's before any more)
     if (stages > 0) ask(0);
 
     // This wave's keys; the stages of which its keys are seen at all, and those whose rows all see all of them.
@@ -423,31 +433,70 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     spread<M::kBlocks * 8>(sums, col);
     const int i = col & 15, kb = BF16 ? col >> 4 : 0, j = k0 + kb * 32 + i / 4 * 8 + i % 4 + half * 4;
     if (j >= length || (!BF16 && col >= 16)) return;
-    if (a.chunks > 1) a.part[((int64_t)part * a.groups + g) * a.key_tiles * (4 * kKeys) + j] = sums[0];
-    else add_to(c, g, j, sums[0]);
+    if (part) part[j - j0] = more ? part[j - j0] + sums[0] : sums[0];
+    else add_to(c, g, j, sums[0], more ? 1.f : c.decay);
 }
 
-// Adds up the chunks that see a key's tile, in order.
+template <bool BF16>
+__global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
+    constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kTiles * 32;
+    __shared__ __attribute__((aligned(16))) char Qs[2][32768];
+    __shared__ float Ls[2][kStage];                                // -lse of a stage's rows, in units of log 2
+    const WeightsCall& c = a.c;
+    // Neighbours in a head are neighbours in an XCD, whose caches then hold one head's queries.
+    const int at = a.by_groups.of(blockIdx.x), g = a.by_groups.rest(blockIdx.x, at), b = a.by_kv.of(g), head = a.by_kv.rest(g, b), length = length_of(c, b);
+    const auto run = [&](int tile, int from, int to, float* part) ALWAYS_INLINE {
+        const Span span = rows_that_see(a, length, tile * kKeys, min(tile * kKeys + kKeys, length) - 1, kStage);
+        for (int s = from; s == from || s < to; s += a.most)
+            tile_stages<BF16>(a, Qs, Ls, g, b, head, length, tile, span.begin + s * kStage, min(a.most, to - s), part, s > from);
+    };
+    if (a.shares == 0) {
+        if (at * kKeys < length) run(at, 0, rows_that_see(a, length, at * kKeys, min(at * kKeys + kKeys, length) - 1, kStage).stages, nullptr);
+        return;
+    }
+    const Shares<kKeys, kStage> shares{a, length};
+    const int64_t total = shares.below(a.key_tiles), low = total * at / a.shares, high = total * (at + 1) / a.shares;
+    int64_t before = 0;
+    for (int base = 0; base < a.key_tiles && before < high; base += 64) {
+        const int stages = shares.stages(base + (int)(threadIdx.x & 63)), sum = shares.up_to(shares.cost(stages));
+        const int64_t mine = before + sum - stages;                // where the tile's stages begin
+        const int from = (int)min(max(low - mine, (int64_t)0), (int64_t)stages), to = (int)min(max(high - mine, (int64_t)0), (int64_t)stages);
+        before += __builtin_amdgcn_readlane(sum, 63);
+        for (uint64_t some = __ballot(from < to); some; some &= some - 1) {
+            const int l = __builtin_ctzll(some), tile = base + l;
+            run(tile, __builtin_amdgcn_readlane(from, l), __builtin_amdgcn_readlane(to, l), a.part + ((int64_t)g * (a.shares + a.key_tiles) + at + tile) * kKeys);
+        }
+    }
+}
+
+// Adds up the shares of a key's tile, in order; a wave's keys are of one tile.
 template <bool BF16>
 __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
     constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kTiles * 32;
     const WeightsCall& c = a.c;
-    const int g = blockIdx.x % a.groups, j = blockIdx.x / a.groups * 256 + threadIdx.x, length = length_of(c, g / c.kv);
-    if (j >= length) return;
-    const Span span = rows_that_see(a, length, j / kKeys * kKeys, min(j / kKeys * kKeys + kKeys, length) - 1, kStage);
+    const int block = a.by_groups.of(blockIdx.x), g = a.by_groups.rest(blockIdx.x, block), j = block * 256 + threadIdx.x, length = length_of(c, a.by_kv.of(g));
+    const int tile = __builtin_amdgcn_readfirstlane(j / kKeys);
+    const Shares<kKeys, kStage> shares{a, length};
+    const int stages = shares.stages(tile);
     float sum = 0.f;
-    for (int part = 0; part < a.chunks && (a.first_chunk + part) * a.chunk < span.end - span.begin; ++part) sum += a.part[((int64_t)part * a.groups + g) * a.key_tiles * kKeys + j];
-    add_to(c, g, j, sum);
+    if (stages > 0) {
+        // the share of position x is the largest s with total s / shares <= x
+        const int64_t total = shares.below(a.key_tiles), first = shares.below(tile) + kTileCost;
+        const int from = (int)(((first + 1) * a.shares - 1) / total), to = (int)(((first + stages) * a.shares - 1) / total);
+        const float* part = a.part + ((int64_t)g * (a.shares + a.key_tiles) + tile) * kKeys + j % kKeys;
+        for (int s = from; s <= to; ++s) sum += j < length ? part[(int64_t)s * kKeys] : 0.f;
+    }
+    if (j < length) add_to(c, g, j, sum, c.decay);
 }
 
 }  // namespace
 
 hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStream_t stream) {
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
-    WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, 0, 1, nullptr, Divisor(call.count * call.kv), Divisor(1), Divisor(call.kv), Divisor(call.group)};
+    WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, nullptr, Divisor(call.count * call.kv), Divisor(call.kv), Divisor(call.group)};
     if (a.rows <= 32) {
-        const int64_t steps = (call.n + 63) / 64, waves = WV * (int64_t)ctx->num_cu;
-        const int64_t each = std::max<int64_t>(1, std::min<int64_t>(TE, a.groups * steps / waves));
+        const int64_t steps = (call.n + 63) / 64, waves = 16 * (int64_t)ctx->num_cu;
+        const int64_t each = std::max<int64_t>(1, std::min<int64_t>(4, a.groups * steps / waves));
         a.shares = (int)((steps + 4 * each - 1) / (4 * each));
         const bool past = (int64_t)a.groups * call.n * (bf16 ? 256 : 512) > kPastCaches;
         const auto launch = [&](auto kernel) { kernel<<<(unsigned)((int64_t)a.groups * a.shares), 256, 0, stream>>>(a); };
@@ -459,25 +508,18 @@ hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStr
     }
     const int keys = bf16 ? 256 : 128, stage = bf16 ? 128 : 64;
     a.key_tiles = (call.n + keys - 1) / keys;
-    a.by_key_tiles = Divisor(a.key_tiles);
-    // Rows shared out over workgroups until there are twelve for every unit, half of them above the diagonal, two stages each at least; 2^31 bytes of queries at most.
-    const int64_t blocks = (int64_t)a.groups * a.key_tiles, most = ((int64_t)1 << 31) / (call.kv * (bf16 ? 256 : 512)) / stage * stage;
-    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(CM * (int64_t)ctx->num_cu / blocks, a.rows / (CS * stage)));
-    a.chunk = (int)std::min(((a.rows + wanted - 1) / wanted + stage - 1) / stage * stage, most);
-    const int all = (a.rows + a.chunk - 1) / a.chunk;              // (counted from a stage's start: no more of them than of all rows)
-    // As many at once as there is scratch for; the weights of one launch are the old ones of the next.
-    const int64_t room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (blocks * keys * (int64_t)sizeof(float)) : 0;
-    const int at_once = (int)std::max<int64_t>(1, std::min<int64_t>(all, std::min(room, kMostBlocks / blocks)));
+    a.most = (int)(((int64_t)1 << 31) / (call.kv * (bf16 ? 256 : 512)) / stage);
+    // Two workgroups a unit, each with an equal share of a head's products, where tiles of keys would leave units idle at the end; their sums lie in scratch, as far as there is any.
+    const int64_t tiles = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (a.groups * (int64_t)keys * 4) - a.key_tiles : 0;
+    const int64_t shares = std::min(std::min<int64_t>(2 * (int64_t)ctx->num_cu / a.groups, room), std::max<int64_t>(1, (int64_t)((a.rows + stage - 1) / stage) * a.key_tiles));
+    a.shares = tiles < 2 * (int64_t)ctx->num_cu && a.rows > 2 * stage && shares > 1 ? (int)shares : 0;
     a.part = (float*)((char*)call.scratch + kScratchCounters);
     const auto launch = [&](auto kernel, int64_t n) { kernel<<<(unsigned)n, 256, 0, stream>>>(a); };
-    for (a.first_chunk = 0; a.first_chunk < all; a.first_chunk += at_once) {
-        a.chunks = std::min(at_once, all - a.first_chunk);
-        bf16 ? launch(weights_many_kernel<true>, blocks * a.chunks) : launch(weights_many_kernel<false>, blocks * a.chunks);
-        if (a.chunks > 1) {
-            const int64_t joins = (int64_t)a.groups * ((call.n + 255) / 256);
-            bf16 ? launch(weights_join_kernel<true>, joins) : launch(weights_join_kernel<false>, joins);
-        }
-        a.c.decay = 1.f;
+    const int64_t blocks = a.shares ? (int64_t)a.groups * a.shares : tiles;
+    bf16 ? launch(weights_many_kernel<true>, blocks) : launch(weights_many_kernel<false>, blocks);
+    if (a.shares) {
+        const int64_t joins = (int64_t)a.groups * ((call.n + 255) / 256);
+        bf16 ? launch(weights_join_kernel<true>, joins) : launch(weights_join_kernel<false>, joins);
     }
     return hipGetLastError();
 }

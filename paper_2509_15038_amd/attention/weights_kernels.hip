@@ -484,7 +484,8 @@ __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
         const int64_t total = shares.below(a.key_tiles), first = shares.below(tile) + kTileCost;
         const int from = (int)(((first + 1) * a.shares - 1) / total), to = (int)(((first + stages) * a.shares - 1) / total);
         const float* part = a.part + ((int64_t)g * (a.shares + a.key_tiles) + tile) * kKeys + j % kKeys;
-        for (int s = from; s <= to; ++s) sum += j < length ? part[(int64_t)s * kKeys] : 0.f;
+        for (int s = from; s <= to; ++s)                           // (a share of nothing, where there are more shares than cost, has written nothing)
+            if (j < length && total * s / a.shares < total * (s + 1) / a.shares) sum += part[(int64_t)s * kKeys];
     }
     if (j < length) add_to(c, g, j, sum, c.decay);
 }

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2509_15038_amd import binding as B
 from tests import attend_util as U
 from tests.gpu_util import Guarded
 
@@ -197,6 +198,16 @@ def test_results_do_not_change_from_run_to_run_and_graphs_replay():
                     graph.replay()
                     torch.cuda.synchronize()
                     assert torch.equal(mass, wants[3 * turn + i]), (dtype, m, few, i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_scratch_that_holds_something(dtype):
+    # partial sums of other calls lie in scratch: short sequences among long ones, for which there are more shares than products
+    scratch = torch.zeros((B.ATTEND_SCRATCH_BYTES,), dtype=torch.uint8, device="cuda")
+    scratch[16384:].view(torch.float32).fill_(1e9)
+    for m, n in ((300, 300), (700, 700), (64, 1500)):
+        check(dtype, 3, 2, 4, m, n, lengths=[n, n // 3, 40], decay=0.0, scratch=scratch)
+        check(dtype, 3, 2, 4, m, n, lengths=[65, 1, 0], window=50, sinks=2, scratch=scratch)
 
 
 def test_another_stream():

@@ -86,6 +86,7 @@ struct EvictCall {
     char *K_out, *V_out;
     float* mass_out;
     int32_t *positions_out, *rows;
+    bool moves;                        // the selection moves the rows itself
 };
 hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_t stream);
 

@@ -7,6 +7,9 @@
 // digits over order-preserving keys; then bitmaps in LDS, one bit a row, of the rows that stay and of those that tie with the last; all that is left
 // (the first of the tied, ranks of holes and of those that fill them) are counts of bits.  evict_move_kernel copies rows, 16 bytes a lane.
 
+#include <algorithm>
+#include <type_traits>
+
 #include "attend_device.h"
 #include "attend_internal.h"
 
@@ -55,11 +58,29 @@ __device__ __forceinline__ int bit_of_rank(uint64_t x, int k) {
     return at;
 }
 
+constexpr int kBins = 4096, kFineBins = 1024;      // 12 bits of a key, then 10, then 10
+constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place
+
+// Counts into bins; a wave whose lanes all count into one does so at once.
+__device__ __forceinline__ void count_into(uint32_t* bins, uint32_t bin, bool counts) {
+    const uint64_t who = __ballot(counts);
+    if (!who) return;
+    const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
+    if (__ballot(counts && bin == one) == who) {
+        if ((threadIdx.x & 63) == 0) atomicAdd(bins + one, (uint32_t)__popcll(who));
+    } else if (counts) {
+        atomicAdd(bins + bin, 1u);
+    }
+}
+
+// A thread has rows tid, tid + 1024, ..: up to ROWS of them in registers, or, where the head is LONG, so many at a time, read again for every pass.
+template <int ROWS, bool LONG>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
     extern __shared__ uint64_t bits[];                     // [words] rows that stay; [words] tied rows, then {those from beyond, holes} before the word
-    __shared__ uint32_t hist[kWaves][256];
+    uint32_t* bins = (uint32_t*)bits;                      // before that: [kBins] of the rows that are not protected, and that are; [kFineBins] of the last two digits
     __shared__ int waves[kWaves];
-    __shared__ int newest_all, many_first, found_bin, found_need;
+    __shared__ int newest_all, found_bin, found_need, many_moved;
+    __shared__ int moved[kMostMoved][2];
     const int g = blockIdx.x, b = g / c.kv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int length = c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n, stays = min(length, c.keep);
     const float* mass = c.mass + (int64_t)g * c.stride;
@@ -77,77 +98,114 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
         for (int i = tid; i < length; i += kThreads) place(i, i);
         return;
     }
-    // The newest position, and how many rows are protected.
-    if (tid == 0) newest_all = INT32_MIN, many_first = 0;
-    __syncthreads();
-    int newest = INT32_MIN;
-    if (!positions) newest = length - 1;
-    else for (int i = tid; i < length; i += kThreads) newest = max(newest, positions[i]);
+    const int batches = LONG ? (length + ROWS * kThreads - 1) / (ROWS * kThreads) : 1;
+    const auto row_of = [&](int batch, int k) ALWAYS_INLINE { return (batch * ROWS + k) * kThreads + tid; };
+    for (int i = tid; i < 2 * kBins + 2 * kFineBins; i += kThreads) bins[i] = 0;
+    if (tid == 0) newest_all = INT32_MIN, many_moved = 0;
+    // The newest position.
+    uint32_t key[ROWS];
+    int at[ROWS], newest = INT32_MIN;
+    const auto load_positions = [&](int batch) ALWAYS_INLINE {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int i = min(row_of(batch, k), length - 1);
+            at[k] = positions ? positions[i] : i;
+        }
+    };
+    const auto load_keys = [&](int batch) ALWAYS_INLINE {
+        float x[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) x[k] = mass[min(row_of(batch, k), length - 1)];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) key[k] = weight_key(x[k]);
+    };
+    if (!LONG) load_keys(0);
+    for (int batch = 0; batch < batches; ++batch) {
+        load_positions(batch);
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) newest = max(newest, at[k]);
+    }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) newest = max(newest, __shfl_xor(newest, d));
+    __syncthreads();
     if (lane == 0) atomicMax(&newest_all, newest);
     __syncthreads();
+    // Which of a thread's rows there are, and which are protected, a bit each.
     const int64_t after = (int64_t)newest_all - c.recent;
-    const auto protects = [&](int i) ALWAYS_INLINE {
-        const int p = positions ? positions[i] : i;
-        return p < c.sinks || p > after;
-    };
-    int first = 0;
-    for (int i = tid; i < length; i += kThreads) first += protects(i);
+    uint32_t in = 0, first = 0;
+    const auto look = [&](int batch) ALWAYS_INLINE {
+        in = first = 0;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) first += __shfl_xor(first, d);
-    if (lane == 0) atomicAdd(&many_first, first);
+        for (int k = 0; k < ROWS; ++k) {
+            in |= (uint32_t)(row_of(batch, k) < length) << k;
+            first |= (uint32_t)(at[k] < c.sinks || at[k] > after) << k;
+        }
+    };
+    if (!LONG) look(0);
+    const auto each_batch = [&](auto&& what) ALWAYS_INLINE {
+        for (int batch = 0; batch < batches; ++batch) {
+            if (LONG) {
+                load_positions(batch);
+                load_keys(batch);
+                look(batch);
+            }
+            what(batch);
+        }
+    };
+    each_batch([&](int) ALWAYS_INLINE {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) count_into(bins, (key[k] >> 20) + (first >> k & 1) * kBins, in >> k & 1);
+    });
     __syncthreads();
-    // Among which rows the weight decides, how many of them stay, and the key of the last of these.
+    // Among which rows the weight decides, how many of them stay, and the key of the last of these: the digit at which the count from the largest on reaches that many.
+    int many_first;
+    before_me((int)(bins[kBins + 4 * tid] + bins[kBins + 4 * tid + 1] + bins[kBins + 4 * tid + 2] + bins[kBins + 4 * tid + 3]), waves, &many_first);
     const bool among_first = many_first >= stays;
     int need = among_first ? stays : stays - many_first;
-    uint32_t last = 0, known = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < kWaves * 256; i += kThreads) (&hist[0][0])[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < length; i += kThreads) {
-            const uint32_t key = weight_key(mass[i]);
-            if (protects(i) == among_first && (key & known) == last) atomicAdd(&hist[wave][key >> shift & 255], 1u);
-        }
-        __syncthreads();
-        if (wave == 0) {
-            // lane l has bins 255 - 4 l .. 252 - 4 l, so that sums run from the largest digit on
-            int count[4], mine = 0;
+    const auto find = [&](const uint32_t* from, auto each) ALWAYS_INLINE {         // each: bins a thread, from the largest down
+        constexpr int E = decltype(each)::value;
+        const int top = E * kThreads - 1 - E * tid;
+        int mine = 0, all;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                count[i] = 0;
-                for (int w = 0; w < kWaves; ++w) count[i] += hist[w][255 - 4 * lane - i];
-                mine += count[i];
-            }
-            int sum = mine;
+        for (int i = 0; i < E; ++i) mine += from[top - i];
+        int above = before_me(mine, waves, &all);
+        if (above < need && above + mine >= need) {
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int y = __shfl_up(sum, d);
-                if (lane >= d) sum += y;
-            }
-            int above = sum - mine;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (above < need && above + count[i] >= need) found_bin = 255 - 4 * lane - i, found_need = need - above;
-                above += count[i];
+            for (int i = 0; i < E; ++i) {
+                const int count = from[top - i];
+                if (above < need && above + count >= need) found_bin = top - i, found_need = need - above;
+                above += count;
             }
         }
         __syncthreads();
-        last |= (uint32_t)found_bin << shift;
-        known |= 255u << shift;
-        need = found_need;             // (rows of the last key that stay, in the end)
+        need = found_need;
+        return (uint32_t)found_bin;
+    };
+    uint32_t last = find(bins + (among_first ? kBins : 0), std::integral_constant<int, 4>{});
+#pragma unroll
+    for (int digit = 0; digit < 2; ++digit) {
+        uint32_t* fine = bins + 2 * kBins + digit * kFineBins;
+        const int shift = 10 - 10 * digit;
+        each_batch([&](int) ALWAYS_INLINE {
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                count_into(fine, key[k] >> shift & (kFineBins - 1), (in >> k & 1) && (first >> k & 1) == among_first && key[k] >> (shift + 10) == last);
+        });
         __syncthreads();
+        last = last << 10 | find(fine, std::integral_constant<int, 1>{});
     }
     // The bitmaps, and of the tied rows the first `need`.
     const int words = (length + 63) / 64;
     uint64_t* tied = bits + words;
-    for (int w = wave; w < words; w += kWaves) {
-        const int i = w * 64 + lane, at = min(i, length - 1);
-        const uint32_t key = weight_key(mass[at]);
-        const bool is_first = protects(at), in = i < length;
-        const uint64_t above = __ballot(in && (is_first == among_first ? key > last : is_first)), ties = __ballot(in && is_first == among_first && key == last);
-        if (lane == 0) bits[w] = above, tied[w] = ties;
-    }
+    each_batch([&](int batch) ALWAYS_INLINE {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int w = (batch * ROWS + k) * kWaves + wave;
+            const bool there = in >> k & 1, is_first = first >> k & 1;
+            const uint64_t above = __ballot(there && (is_first == among_first ? key[k] > last : is_first)), ties = __ballot(there && is_first == among_first && key[k] == last);
+            if (lane == 0 && w < words) bits[w] = above, tied[w] = ties;
+        }
+    });
     __syncthreads();
     const int each = (words + kThreads - 1) / kThreads, w0 = min(tid * each, words), w1 = min(w0 + each, words);
     int mine = 0, total;
@@ -184,8 +242,20 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
                 else high = mid - 1;
             }
             source = low * 64 + bit_of_rank(bits[low] & ~low_of(low), rank - before[low].x);
+            if (c.moves) {
+                const int k = atomicAdd(&many_moved, 1);
+                moved[k][0] = i, moved[k][1] = source;
+            }
         }
         place(i, source);
+    }
+    if (!c.moves) return;
+    __syncthreads();
+    const int shift = c.dtype == CURDKV_DTYPE_BF16 ? 4 : 5;        // a row's pieces of 16 bytes; K, then V
+    for (int i = tid; i < many_moved << (shift + 1); i += kThreads) {
+        const int piece = i & ((1 << shift) - 1), k = i >> (shift + 1);
+        u32x4a* array = (u32x4a*)(i >> shift & 1 ? c.V_out : c.K_out);
+        array[(((int64_t)g * c.stride + moved[k][0]) << shift) + piece] = array[(((int64_t)g * c.stride + moved[k][1]) << shift) + piece];
     }
 }
 
@@ -206,11 +276,19 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int blocks
 
 hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_t stream) {
     const unsigned heads = (unsigned)(call.count * call.kv);
-    const size_t lds = (size_t)((call.n + 63) / 64) * 16;
-    const hipError_t e = lds <= 40 * 1024 ? hipSuccess
-                                          : hipFuncSetAttribute((const void*)evict_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kEvictMostRows / 64 * 16));
+    const size_t lds = std::max((size_t)((call.n + 63) / 64) * 16, (2 * kBins + 2 * kFineBins) * sizeof(uint32_t));
+    EvictCall select = call;
+    select.moves = call.K_out == call.K && call.n - call.keep <= kMostMoved;       // (in place; no more rows move than leave)
+    const auto launch = [&](auto kernel) {
+        const hipError_t e = lds <= 48 * 1024 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kEvictMostRows / 64 * 16));
+        if (e == hipSuccess) kernel<<<heads, kThreads, lds, stream>>>(select);
+        return e;
+    };
+    const hipError_t e = call.n <= 4 * kThreads ? launch(evict_select_kernel<4, false>) : call.n <= 8 * kThreads ? launch(evict_select_kernel<8, false>)
+                         : call.n <= 16 * kThreads ? launch(evict_select_kernel<16, false>) : call.n <= 32 * kThreads ? launch(evict_select_kernel<32, false>)
+                                                                                              : launch(evict_select_kernel<16, true>);
     if (e != hipSuccess) return e;
-    evict_select_kernel<<<heads, kThreads, lds, stream>>>(call);
+    if (select.moves) return hipGetLastError();
     const int keep = call.keep < call.n ? call.keep : call.n;
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
     const int blocks = bf16 ? (keep + 15) / 16 : (keep + 7) / 8;

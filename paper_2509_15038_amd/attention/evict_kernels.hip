@@ -3,8 +3,9 @@
 // rows below `keep` that stay keep their places, the holes among them are filled, in order, by the rows that stay from beyond: what moves is as few rows as leave,
 // sources lie at or beyond `keep` and destinations below, so that a cache can be its own target with no order among the moves.
 //
-// evict_select_kernel, a workgroup a head: the newest position, how many rows are protected, the weight of the last row that stays by a radix search of four
-// digits over order-preserving keys; then bitmaps in LDS, one bit a row, of the rows that stay and of those that tie with the last; all that is left
+// evict_select_kernel, a workgroup a head.  A row's key is its weight's bits in an order that integers have, the largest for a protected row and 0 for what is none, so that the `keep`
+// largest keys stay (should there be more protected rows, they have their weights' keys and all others 0).  The last key that stays is found digit by digit, 12 bits of all keys, then
+// 10 and 10 of the few that share these.  Then bitmaps in LDS, one bit a row, of the rows that stay and of those that tie with the last; all that is left
 // (the first of the tied, ranks of holes and of those that fill them) are counts of bits.  evict_move_kernel copies rows, 16 bytes a lane.
 
 #include <algorithm>
@@ -17,34 +18,50 @@ namespace curdkv {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kBins = 4096, kFineBins = 1024;      // 12 bits of a key, then 10, then 10
+constexpr int kListed = 2048;                      // keys of one bin that are kept apart
+constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place
 
-// Larger is better: weights in order, -0 as 0, NaN above all.
+// Larger is better: 0 for what is none, weights in order, -0 as 0, NaN above all, and above that the protected.
+constexpr uint32_t kProtected = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t weight_key(float x) {
-    if (x != x) return 0xFFFFFFFFu;
+    if (x != x) return kProtected - 1;
     const uint32_t b = __float_as_uint(x + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Exclusive sums of x over the workgroup's threads, and the total.
-__device__ __forceinline__ int before_me(int x, int* waves, int* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int sum = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(sum, d);
-        if (lane >= d) sum += y;
-    }
-    __syncthreads();                   // (the last use of `waves`)
+// Sum over a wave's lanes up to and with this one.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved_by(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int up_to(int x) {
+    x += moved_by<0x111, 0xF>(x);                  // row_shr:1, 2, 4, 8
+    x += moved_by<0x112, 0xF>(x);
+    x += moved_by<0x114, 0xF>(x);
+    x += moved_by<0x118, 0xF>(x);
+    x += moved_by<0x142, 0xA>(x);                  // row_bcast:15 into rows 1 and 3, row_bcast:31 into 2 and 3
+    x += moved_by<0x143, 0xC>(x);
+    return x;
+}
+// Sum over the workgroup's threads below this one; `waves`: not used by the calls right before and after.
+__device__ __forceinline__ int before_me(int x, int* waves) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sum = up_to(x);
     if (lane == 63) waves[wave] = sum;
     __syncthreads();
-    int before = 0, all = 0;
+    int before = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += waves[w];
-        all += waves[w];
-    }
-    *total = all;
+    for (int w = 0; w < kWaves; ++w) before += w < wave ? waves[w] : 0;
     return before + sum - x;
+}
+
+// By every wave alone: the largest x with at least `need` counted at x and above; `need` becomes how many of those at x are needed.  count(l): of lane l's, from the largest down.
+struct Found {
+    int lane, need;
+};
+template <class C>
+__device__ __forceinline__ Found find(int need, const C& count) {
+    const int mine = count((int)(threadIdx.x & 63)), sum = up_to(mine);
+    const int lane = __builtin_ctzll(__ballot(sum >= need));
+    return {lane, need - (__builtin_amdgcn_readlane(sum, lane) - __builtin_amdgcn_readlane(mine, lane))};
 }
 
 // The place of the set bit of x that has k set bits below it (k < their number).
@@ -58,159 +75,229 @@ __device__ __forceinline__ int bit_of_rank(uint64_t x, int k) {
     return at;
 }
 
-constexpr int kBins = 4096, kFineBins = 1024;      // 12 bits of a key, then 10, then 10
-constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place
+// Four numbers that lie anywhere.
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// Counts into bins; a wave whose lanes all count into one does so at once.
-__device__ __forceinline__ void count_into(uint32_t* bins, uint32_t bin, bool counts) {
-    const uint64_t who = __ballot(counts);
-    if (!who) return;
-    const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
-    if (__ballot(counts && bin == one) == who) {
-        if ((threadIdx.x & 63) == 0) atomicAdd(bins + one, (uint32_t)__popcll(who));
-    } else if (counts) {
-        atomicAdd(bins + bin, 1u);
-    }
-}
-
-// A thread has rows tid, tid + 1024, ..: up to ROWS of them in registers, or, where the head is LONG, so many at a time, read again for every pass.
+// A thread has four rows in every 4096: up to ROWS of them in registers, or, where the head is LONG, so many at a time, read again for every pass.
 template <int ROWS, bool LONG>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
-    extern __shared__ uint64_t bits[];                     // [words] rows that stay; [words] tied rows, then {those from beyond, holes} before the word
-    uint32_t* bins = (uint32_t*)bits;                      // before that: [kBins] of the rows that are not protected, and that are; [kFineBins] of the last two digits
-    __shared__ int waves[kWaves];
-    __shared__ int newest_all, found_bin, found_need, many_moved;
+    constexpr int kCopies = ROWS > 4 ? 2 : 1;              // of the first digit's bins, for neighbouring lanes
+    extern __shared__ __attribute__((aligned(16))) uint64_t bits[];                     // [words] rows that stay; [words] tied rows, then {those from beyond, holes} before the word
+    uint32_t* bins = (uint32_t*)bits;                      // before that
+    __shared__ __attribute__((aligned(16))) uint32_t fine[2][kFineBins], listed[kListed];
+    __shared__ int coarse[64], waves[3][kWaves];
+    __shared__ int newest_all, many_first, many_listed, many_moved;
     __shared__ int moved[kMostMoved][2];
-    const int g = blockIdx.x, b = g / c.kv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int g = blockIdx.x, b = g / c.kv, tid = threadIdx.x, lane = tid & 63;
     const int length = c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n, stays = min(length, c.keep);
     const float* mass = c.mass + (int64_t)g * c.stride;
     const int32_t* positions = c.positions ? c.positions + (int64_t)g * c.stride : nullptr;
     int32_t* rows = c.rows + (int64_t)g * c.keep;
     float* mass_out = c.mass_out ? c.mass_out + (int64_t)g * c.out_stride : nullptr;
     int32_t* positions_out = c.positions_out ? c.positions_out + (int64_t)g * c.out_stride : nullptr;
-    const auto place = [&](int i, int source) ALWAYS_INLINE {      // what goes with row i of the output
-        rows[i] = source;
-        if (mass_out && (mass_out != mass || source != i)) mass_out[i] = mass[source];
-        if (positions_out && (positions_out != positions || source != i)) positions_out[i] = positions ? positions[source] : source;
+    // what goes with rows i + 1024 e of the output (source < 0: nothing); where rows are moved by another kernel, that does it
+    const auto place = [&](int i, const int (&source)[4]) ALWAYS_INLINE {
+        float w[4];
+        int p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int from = max(source[e], 0), to = i + e * kThreads;
+            if (source[e] >= 0) rows[to] = from;
+            if (!c.moves) continue;
+            if (mass_out && (mass_out != mass || from != to)) w[e] = mass[from];
+            if (positions_out && positions && (positions_out != positions || from != to)) p[e] = positions[from];
+        }
+        if (!c.moves) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int from = source[e], to = i + e * kThreads;
+            if (from < 0) continue;
+            if (mass_out && (mass_out != mass || from != to)) mass_out[to] = w[e];
+            if (positions_out && (positions_out != positions || from != to)) positions_out[to] = positions ? p[e] : from;
+        }
     };
     for (int i = stays + tid; i < c.keep; i += kThreads) rows[i] = -1;
     if (length <= c.keep) {
-        for (int i = tid; i < length; i += kThreads) place(i, i);
+        for (int i = tid; i < length; i += 4 * kThreads) {
+            int source[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) source[e] = i + e * kThreads < length ? i + e * kThreads : -1;
+            place(i, source);
+        }
         return;
     }
     const int batches = LONG ? (length + ROWS * kThreads - 1) / (ROWS * kThreads) : 1;
-    const auto row_of = [&](int batch, int k) ALWAYS_INLINE { return (batch * ROWS + k) * kThreads + tid; };
-    for (int i = tid; i < 2 * kBins + 2 * kFineBins; i += kThreads) bins[i] = 0;
-    if (tid == 0) newest_all = INT32_MIN, many_moved = 0;
-    // The newest position.
+    const auto row_of = [&](int batch, int k) ALWAYS_INLINE { return batch * (ROWS * kThreads) + (k / 4 * kThreads + tid) * 4 + k % 4; };
+    // The newest position; meanwhile the bins are cleared.
     uint32_t key[ROWS];
-    int at[ROWS], newest = INT32_MIN;
-    const auto load_positions = [&](int batch) ALWAYS_INLINE {
+    uint32_t at[ROWS], x[ROWS];
+    int newest = INT32_MIN;
+    const auto load = [&](const void* from, int batch, uint32_t* to) ALWAYS_INLINE {
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const int i = min(row_of(batch, k), length - 1);
-            at[k] = positions ? positions[i] : i;
+        for (int k = 0; k < ROWS; k += 4) {
+            const int i = row_of(batch, k);
+            u32x4a y;
+            if (i + 3 < length) {
+                y = *(const u32x4u*)((const uint32_t*)from + i);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = ((const uint32_t*)from)[min(i + e, length - 1)];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[k + e] = y[e];
         }
     };
-    const auto load_keys = [&](int batch) ALWAYS_INLINE {
-        float x[ROWS];
+    const auto load_positions = [&](int batch) ALWAYS_INLINE {
+        if (positions) load(positions, batch, at);
+        else
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) x[k] = mass[min(row_of(batch, k), length - 1)];
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) key[k] = weight_key(x[k]);
+            for (int k = 0; k < ROWS; ++k) at[k] = min(row_of(batch, k), length - 1);
     };
-    if (!LONG) load_keys(0);
+    const auto load_weights = [&](int batch) ALWAYS_INLINE { load(mass, batch, x); };
+    if (!LONG) {
+        load_positions(0);
+        load_weights(0);
+    }
+    for (int i = tid; i < kBins * kCopies / 4; i += kThreads) ((u32x4a*)bins)[i] = (u32x4a){0, 0, 0, 0};
+    fine[0][tid] = fine[1][tid] = 0;
+    if (tid == 0) newest_all = INT32_MIN, many_first = many_listed = many_moved = 0;
     for (int batch = 0; batch < batches; ++batch) {
-        load_positions(batch);
+        if (LONG) load_positions(batch);
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) newest = max(newest, at[k]);
+        for (int k = 0; k < ROWS; ++k) newest = max(newest, (int)at[k]);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) newest = max(newest, __shfl_xor(newest, d));
     __syncthreads();
     if (lane == 0) atomicMax(&newest_all, newest);
     __syncthreads();
-    // Which of a thread's rows there are, and which are protected, a bit each.
-    const int64_t after = (int64_t)newest_all - c.recent;
-    uint32_t in = 0, first = 0;
-    const auto look = [&](int batch) ALWAYS_INLINE {
-        in = first = 0;
+    // How many rows are protected.
+    const int from_on = (int)max((int64_t)newest_all - c.recent + (c.recent > 0), (int64_t)INT32_MIN);
+    const bool any_recent = c.recent > 0;
+    const auto protects = [&](int p) ALWAYS_INLINE { return (p < c.sinks) | (any_recent & (p >= from_on)); };
+    int first = 0;
+    for (int batch = 0; batch < batches; ++batch) {
+        if (LONG) load_positions(batch);
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) first += protects(at[k]) && row_of(batch, k) < length;
+    }
+    first = up_to(first);
+    if (lane == 63) atomicAdd(&many_first, first);
+    __syncthreads();
+    const bool among_first = many_first > stays;
+    int need = among_first ? stays : stays - many_first;           // of the rows whose weights decide
+    const auto make_keys = [&](int batch) ALWAYS_INLINE {
+        if (LONG) {
+            load_positions(batch);
+            load_weights(batch);
+        }
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
-            in |= (uint32_t)(row_of(batch, k) < length) << k;
-            first |= (uint32_t)(at[k] < c.sinks || at[k] > after) << k;
+            const bool is_first = protects(at[k]);
+            const uint32_t by_weight = weight_key(__uint_as_float(x[k]));
+            key[k] = row_of(batch, k) >= length ? 0u : is_first == among_first ? by_weight : is_first ? kProtected : 0u;
         }
     };
-    if (!LONG) look(0);
+    if (!LONG) make_keys(0);
     const auto each_batch = [&](auto&& what) ALWAYS_INLINE {
         for (int batch = 0; batch < batches; ++batch) {
-            if (LONG) {
-                load_positions(batch);
-                load_keys(batch);
-                look(batch);
-            }
+            if (LONG) make_keys(batch);
             what(batch);
         }
     };
-    each_batch([&](int) ALWAYS_INLINE {
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) count_into(bins, (key[k] >> 20) + (first >> k & 1) * kBins, in >> k & 1);
-    });
-    __syncthreads();
-    // Among which rows the weight decides, how many of them stay, and the key of the last of these: the digit at which the count from the largest on reaches that many.
-    int many_first;
-    before_me((int)(bins[kBins + 4 * tid] + bins[kBins + 4 * tid + 1] + bins[kBins + 4 * tid + 2] + bins[kBins + 4 * tid + 3]), waves, &many_first);
-    const bool among_first = many_first >= stays;
-    int need = among_first ? stays : stays - many_first;
-    const auto find = [&](const uint32_t* from, auto each) ALWAYS_INLINE {         // each: bins a thread, from the largest down
-        constexpr int E = decltype(each)::value;
-        const int top = E * kThreads - 1 - E * tid;
-        int mine = 0, all;
-#pragma unroll
-        for (int i = 0; i < E; ++i) mine += from[top - i];
-        int above = before_me(mine, waves, &all);
-        if (above < need && above + mine >= need) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const int count = from[top - i];
-                if (above < need && above + count >= need) found_bin = top - i, found_need = need - above;
-                above += count;
-            }
-        }
-        __syncthreads();
-        need = found_need;
-        return (uint32_t)found_bin;
-    };
-    uint32_t last = find(bins + (among_first ? kBins : 0), std::integral_constant<int, 4>{});
-#pragma unroll
-    for (int digit = 0; digit < 2; ++digit) {
-        uint32_t* fine = bins + 2 * kBins + digit * kFineBins;
-        const int shift = 10 - 10 * digit;
+    uint32_t last = kProtected - 1;                                // the last key that stays; where the protected are all that do, above it
+    if (need > 0) {
         each_batch([&](int) ALWAYS_INLINE {
 #pragma unroll
             for (int k = 0; k < ROWS; ++k)
-                count_into(fine, key[k] >> shift & (kFineBins - 1), (in >> k & 1) && (first >> k & 1) == among_first && key[k] >> (shift + 10) == last);
+                if (key[k] - 1 < kProtected - 1) atomicAdd(bins + (key[k] >> 20) * kCopies + (lane & (kCopies - 1)), 1u);
         });
         __syncthreads();
-        last = last << 10 | find(fine, std::integral_constant<int, 1>{});
+        int four = 0;                                              // of bins 4 tid .. 4 tid + 3, and then of 64 bins
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const u32x4a y = ((const u32x4a*)bins)[tid * kCopies + i];
+            four += y[0] + y[1] + y[2] + y[3];
+        }
+        four += moved_by<0x111, 0xF>(four);
+        four += moved_by<0x112, 0xF>(four);
+        four += moved_by<0x114, 0xF>(four);
+        four += moved_by<0x118, 0xF>(four);
+        if ((lane & 15) == 15) coarse[tid >> 4] = four;
+        __syncthreads();
+        Found f = find(need, [&](int l) { return coarse[63 - l]; });
+        const int top = (63 - f.lane) * 64 + 63;
+        const auto in_bin = [&](int bin) {
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) sum += bins[bin * kCopies + i];
+            return sum;
+        };
+        f = find(f.need, [&](int l) { return in_bin(top - l); });
+        last = top - f.lane;
+        need = f.need;
+        const bool few = in_bin(last) <= kListed;
+        if (few) {
+            each_batch([&](int) ALWAYS_INLINE {
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k)
+                    if (key[k] >> 20 == last && key[k] - 1 < kProtected - 1) listed[atomicAdd(&many_listed, 1)] = key[k];
+            });
+            __syncthreads();
+        }
+        const int many = many_listed;
+#pragma unroll
+        for (int digit = 0; digit < 2; ++digit) {
+            const int shift = 10 - 10 * digit;
+            const auto count = [&](uint32_t k) ALWAYS_INLINE {
+                if (k >> (shift + 10) == last && k - 1 < kProtected - 1) atomicAdd(fine[digit] + (k >> shift & (kFineBins - 1)), 1u);
+            };
+            if (few) {
+                for (int i = tid; i < many; i += kThreads) count(listed[i]);
+            } else {
+                each_batch([&](int) ALWAYS_INLINE {
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k) count(key[k]);
+                });
+            }
+            __syncthreads();
+            f = find(need, [&](int l) {
+                int sum = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const u32x4a y = ((const u32x4a*)fine[digit])[(63 - l) * 4 + i];
+                    sum += y[0] + y[1] + y[2] + y[3];
+                }
+                return sum;
+            });
+            const int of16 = (63 - f.lane) * 16 + 15;
+            f = find(f.need, [&](int l) { return l < 16 ? (int)fine[digit][of16 - l] : 0; });
+            last = last << 10 | (of16 - f.lane);
+            need = f.need;
+        }
     }
-    // The bitmaps, and of the tied rows the first `need`.
+    // The bitmaps, four lanes' rows written together, and of the tied rows the first `need`.
     const int words = (length + 63) / 64;
     uint64_t* tied = bits + words;
+    __syncthreads();                                               // (nobody reads bins any more)
     each_batch([&](int batch) ALWAYS_INLINE {
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const int w = (batch * ROWS + k) * kWaves + wave;
-            const bool there = in >> k & 1, is_first = first >> k & 1;
-            const uint64_t above = __ballot(there && (is_first == among_first ? key[k] > last : is_first)), ties = __ballot(there && is_first == among_first && key[k] == last);
-            if (lane == 0 && w < words) bits[w] = above, tied[w] = ties;
+        for (int k = 0; k < ROWS; k += 4) {
+            uint32_t y = 0;                                        // above, and 16 bits on, tied
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y |= (key[k + e] > last ? 1u << e : 0u) | (key[k + e] == last ? 0x10000u << e : 0u);
+            y <<= (lane & 3) * 4;
+            y |= (uint32_t)moved_by<0xB1, 0xF>((int)y);            // (quad_perm: xor 1, xor 2)
+            y |= (uint32_t)moved_by<0x4E, 0xF>((int)y);
+            const int sixteen = row_of(batch, k) >> 4;
+            if ((lane & 3) == 0 && sixteen < words * 4) ((uint16_t*)bits)[sixteen] = (uint16_t)y, ((uint16_t*)tied)[sixteen] = (uint16_t)(y >> 16);
         }
     });
     __syncthreads();
     const int each = (words + kThreads - 1) / kThreads, w0 = min(tid * each, words), w1 = min(w0 + each, words);
-    int mine = 0, total;
+    int mine = 0;
     for (int w = w0; w < w1; ++w) mine += __popcll(tied[w]);
-    int ahead = before_me(mine, waves, &total), holes = 0, beyond = 0;
+    int ahead = before_me(mine, waves[0]), holes = 0, beyond = 0;
     const auto low_of = [&](int w) ALWAYS_INLINE { return stays >= w * 64 + 64 ? ~0ull : stays <= w * 64 ? 0ull : (1ull << (stays - w * 64)) - 1; };   // rows below stays
     for (int w = w0; w < w1; ++w) {
         uint64_t x = tied[w];
@@ -221,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
         holes += __popcll(~bits[w] & low_of(w));
         beyond += __popcll(bits[w] & ~low_of(w));
     }
-    int holes_before = before_me(holes, waves, &total), beyond_before = before_me(beyond, waves, &total);
+    int holes_before = before_me(holes, waves[1]), beyond_before = before_me(beyond, waves[2]);
     u32x2* before = (u32x2*)tied;      // (a thread's own words)
     for (int w = w0; w < w1; ++w) {
         before[w] = (u32x2){(uint32_t)beyond_before, (uint32_t)holes_before};
@@ -229,25 +316,34 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
         beyond_before += __popcll(bits[w] & ~low_of(w));
     }
     __syncthreads();
-    for (int i = tid; i < stays; i += kThreads) {
-        const int w = i >> 6;
-        const uint64_t x = bits[w], below = (1ull << (i & 63)) - 1;
-        int source = i;
-        if (!(x >> (i & 63) & 1)) {
-            const uint32_t rank = before[w].y + __popcll(~x & below);
-            int low = stays >> 6, high = words - 1;        // the last word with at most `rank` before it
-            while (low < high) {
-                const int mid = (low + high + 1) >> 1;
-                if (before[mid].x <= rank) low = mid;
-                else high = mid - 1;
-            }
-            source = low * 64 + bit_of_rank(bits[low] & ~low_of(low), rank - before[low].x);
+    int step = 1;                                                  // the largest power of two below `words`
+    while (step * 2 < words) step *= 2;
+    for (int i0 = tid; i0 < stays; i0 += 4 * kThreads) {
+        int source[4], low[4];
+        uint32_t rank[4];
+        bool hole[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = i0 + e * kThreads, w = min(i, stays - 1) >> 6;
+            const uint64_t x = bits[w];
+            hole[e] = i < stays && !(x >> (i & 63) & 1);
+            rank[e] = before[w].y + __popcll(~x & ((1ull << (i & 63)) - 1));
+            source[e] = i < stays ? i : -1;
+            low[e] = 0;
+        }
+        for (int d = step; d > 0; d >>= 1)                         // the last word with at most `rank` from beyond before it
+#pragma unroll
+            for (int e = 0; e < 4; ++e) low[e] += low[e] + d < words && before[min(low[e] + d, words - 1)].x <= rank[e] ? d : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (!hole[e]) continue;
+            source[e] = low[e] * 64 + bit_of_rank(bits[low[e]] & ~low_of(low[e]), rank[e] - before[low[e]].x);
             if (c.moves) {
                 const int k = atomicAdd(&many_moved, 1);
-                moved[k][0] = i, moved[k][1] = source;
+                moved[k][0] = i0 + e * kThreads, moved[k][1] = source[e];
             }
         }
-        place(i, source);
+        place(i0, source);
     }
     if (!c.moves) return;
     __syncthreads();
@@ -265,7 +361,11 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int blocks
     const int g = blockIdx.x / blocks, i = blockIdx.x % blocks * kRows + threadIdx.x / LANES, piece = threadIdx.x % LANES;
     if (i >= c.keep) return;
     const int source = c.rows[(int64_t)g * c.keep + i];
-    if (source < 0 || (c.K_out == c.K && source == i)) return;
+    if (source < 0) return;
+    if (piece == 0 && c.mass_out && (c.mass_out != c.mass || source != i)) c.mass_out[(int64_t)g * c.out_stride + i] = c.mass[(int64_t)g * c.stride + source];
+    if (piece == 1 && c.positions_out && (c.positions_out != c.positions || source != i))
+        c.positions_out[(int64_t)g * c.out_stride + i] = c.positions ? c.positions[(int64_t)g * c.stride + source] : source;
+    if (c.K_out == c.K && source == i) return;
     const int64_t from = ((int64_t)g * c.stride + source) * LANES + piece, to = ((int64_t)g * c.out_stride + i) * LANES + piece;
     const u32x4a k = ((const u32x4a*)c.K)[from], v = ((const u32x4a*)c.V)[from];
     ((u32x4a*)c.K_out)[to] = k;
@@ -276,7 +376,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int blocks
 
 hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_t stream) {
     const unsigned heads = (unsigned)(call.count * call.kv);
-    const size_t lds = std::max((size_t)((call.n + 63) / 64) * 16, (2 * kBins + 2 * kFineBins) * sizeof(uint32_t));
+    const size_t lds = std::max((size_t)((call.n + 63) / 64) * 16, kBins * (call.n > 4 * kThreads ? 2 : 1) * sizeof(uint32_t));
     EvictCall select = call;
     select.moves = call.K_out == call.K && call.n - call.keep <= kMostMoved;       // (in place; no more rows move than leave)
     const auto launch = [&](auto kernel) {
@@ -300,6 +400,10 @@ hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_
         part.K += h * call.stride * row, part.V += h * call.stride * row;
         part.K_out += h * call.out_stride * row, part.V_out += h * call.out_stride * row;
         part.rows += (int64_t)h * call.keep;
+        part.mass += h * call.stride;
+        if (part.mass_out) part.mass_out += h * call.out_stride;
+        if (part.positions) part.positions += h * call.stride;
+        if (part.positions_out) part.positions_out += h * call.out_stride;
         if (bf16) evict_move_kernel<16><<<some * blocks, 256, 0, stream>>>(part, blocks);
         else evict_move_kernel<32><<<some * blocks, 256, 0, stream>>>(part, blocks);
         h += some;

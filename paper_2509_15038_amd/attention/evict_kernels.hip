@@ -21,6 +21,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 4096, kFineBins = 1024;      // 12 bits of a key, then 10, then 10
 constexpr int kListed = 2048;                      // keys of one bin that are kept apart
 constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place
+constexpr int kFewLeave = 8;                       // rows that are found one by one (a token's one of 3277: 13.6 us by digits, so KFEW)
 
 // Larger is better: 0 for what is none, weights in order, -0 as 0, NaN above all, and above that the protected.
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
@@ -51,6 +52,27 @@ __device__ __forceinline__ int before_me(int x, int* waves) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) before += w < wave ? waves[w] : 0;
     return before + sum - x;
+}
+
+// The smallest key of a wave's lanes, and the highest row that has it.
+struct Worst {
+    uint32_t key;
+    int row;
+};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void lower(uint32_t& x) { x = min(x, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)x, CTRL, ROWS, 0xF, false)); }
+__device__ __forceinline__ uint32_t lowest(uint32_t x) {       // (as up_to)
+    lower<0x111, 0xF>(x);
+    lower<0x112, 0xF>(x);
+    lower<0x114, 0xF>(x);
+    lower<0x118, 0xF>(x);
+    lower<0x142, 0xA>(x);
+    lower<0x143, 0xC>(x);
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ Worst worst_of(uint32_t key, int row) {
+    const uint32_t least = lowest(key);
+    return {least, ~(int)lowest(key == least ? ~(uint32_t)row : ~0u)};
 }
 
 // By every wave alone: the largest x with at least `need` counted at x and above; `need` becomes how many of those at x are needed.  count(l): of lane l's, from the largest down.
@@ -114,6 +136,16 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
             if (from < 0) continue;
             if (mass_out && (mass_out != mass || from != to)) mass_out[to] = w[e];
             if (positions_out && (positions_out != positions || from != to)) positions_out[to] = positions ? p[e] : from;
+        }
+    };
+    const auto move_rows = [&]() ALWAYS_INLINE {
+        if (!c.moves) return;
+        __syncthreads();
+        const int shift = c.dtype == CURDKV_DTYPE_BF16 ? 4 : 5;        // a row's pieces of 16 bytes; K, then V
+        for (int i = tid; i < many_moved << (shift + 1); i += kThreads) {
+            const int piece = i & ((1 << shift) - 1), k = i >> (shift + 1);
+            u32x4a* array = (u32x4a*)(i >> shift & 1 ? c.V_out : c.K_out);
+            array[(((int64_t)g * c.stride + moved[k][0]) << shift) + piece] = array[(((int64_t)g * c.stride + moved[k][1]) << shift) + piece];
         }
     };
     for (int i = stays + tid; i < c.keep; i += kThreads) rows[i] = -1;
@@ -205,6 +237,58 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
             what(batch);
         }
     };
+    const int leave = length - stays;
+    if (!LONG && leave <= kFewLeave) {
+        // Few leave: the smallest key of all, of equal ones the highest row, as often as that.
+        __shared__ Worst worst[2][kWaves];
+        int gone[kFewLeave] = {};
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) key[k] = row_of(0, k) < length ? key[k] : kProtected;
+#pragma unroll
+        for (int r = 0; r < kFewLeave; ++r) {
+            if (r >= leave) continue;
+            uint32_t least = kProtected;
+            int row = 0;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)                         // (rows ascending: the last of equal ones; what is none, or gone, has the largest key)
+                if (key[k] <= least) least = key[k], row = row_of(0, k);
+            const Worst mine = worst_of(least, row);
+            if (lane == 0) worst[r & 1][tid >> 6] = mine;
+            __syncthreads();
+            const Worst of = worst[r & 1][lane & (kWaves - 1)];
+            gone[r] = worst_of(of.key, of.row).row;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) key[k] = row_of(0, k) == gone[r] ? kProtected : key[k];
+        }
+        // the k-th of those below `stays`, ascending, is the place of the k-th row from there on that is none of them
+        const auto is_gone = [&](int i) ALWAYS_INLINE {
+            bool y = false;
+#pragma unroll
+            for (int q = 0; q < kFewLeave; ++q) y |= q < leave && gone[q] == i;
+            return y;
+        };
+        for (int i0 = tid; i0 < stays; i0 += 4 * kThreads) {
+            int source[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = i0 + e * kThreads;
+                source[e] = i < stays ? i : -1;
+                if (i >= stays || !is_gone(i)) continue;
+                int rank = 0;
+#pragma unroll
+                for (int q = 0; q < kFewLeave; ++q) rank += q < leave && gone[q] < i;
+                for (int j = stays; j < length; ++j)
+                    if (!is_gone(j) && rank-- == 0) source[e] = j;
+                if (c.moves) {
+                    const int k = atomicAdd(&many_moved, 1);
+                    moved[k][0] = i, moved[k][1] = source[e];
+                }
+            }
+            place(i0, source);
+        }
+        move_rows();
+        return;
+    }
     uint32_t last = kProtected - 1;                                // the last key that stays; where the protected are all that do, above it
     if (need > 0) {
         each_batch([&](int) ALWAYS_INLINE {
@@ -345,14 +429,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
         }
         place(i0, source);
     }
-    if (!c.moves) return;
-    __syncthreads();
-    const int shift = c.dtype == CURDKV_DTYPE_BF16 ? 4 : 5;        // a row's pieces of 16 bytes; K, then V
-    for (int i = tid; i < many_moved << (shift + 1); i += kThreads) {
-        const int piece = i & ((1 << shift) - 1), k = i >> (shift + 1);
-        u32x4a* array = (u32x4a*)(i >> shift & 1 ? c.V_out : c.K_out);
-        array[(((int64_t)g * c.stride + moved[k][0]) << shift) + piece] = array[(((int64_t)g * c.stride + moved[k][1]) << shift) + piece];
-    }
+    move_rows();
 }
 
 template <int LANES>

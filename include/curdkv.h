@@ -383,6 +383,7 @@ int curdkv_rotate_axes(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t 
  *   kv_heads*group_size, m], what curdkv_attend wrote for them.  A token of lse -infinity (it sees nothing) gives
  *   nothing; one of lse NaN makes the weight of the keys that it sees NaN, and no other's.
  * decay: not negative, finite; 0: the old weights are not read.
+ * kv_heads <= 16384.
  * mass: float [count, kv_heads, mass_stride], rows below a sequence's length written; those behind it stay as they
  *   are.  n <= mass_stride.
  * Scores and sums in 32 bits, summed in an order that depends on the sizes alone.  scratch as in curdkv_attend. */
@@ -415,7 +416,7 @@ int curdkv_evict(curdkv_ctx* ctx, const void* K, const void* V, const float* mas
  * Q, out: [count*share, m, kv_heads*group_size, head_dim]; lse: float [count*share, kv_heads*group_size, m] or NULL.
  * offsets: DEVICE int64 [count*kv_heads + 1], K_kept, V_kept, total, rows: the prefixes', as in curdkv_attend_kept.
  * K_tail, V_tail: [count*share, kv_heads, tail_stride, head_dim]; tail_lengths: int32 [count*share].
- * count*share*m*kv_heads*group_size < 2^31.  scratch: not NULL here, CURDKV_ATTEND_SCRATCH_BYTES at least, cleared once as
+ * count*share*m*kv_heads*group_size < 2^31, kv_heads*group_size <= 16384, kv_heads <= 1024.  scratch: not NULL here, CURDKV_ATTEND_SCRATCH_BYTES at least, cleared once as
  * for curdkv_attend; the partial results of prefixes and tails meet there. */
 int curdkv_attend_shared(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept,
                          const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,

@@ -77,6 +77,18 @@ __device__ __forceinline__ float halves_sum(float x) {
 __device__ __forceinline__ void dma16(uint32_t to, const void* base, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
 }
+// Sum over a wave's lanes up to and with this one.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved_by(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int up_to(int x) {
+    x += moved_by<0x111, 0xF>(x);                  // row_shr:1, 2, 4, 8
+    x += moved_by<0x112, 0xF>(x);
+    x += moved_by<0x114, 0xF>(x);
+    x += moved_by<0x118, 0xF>(x);
+    x += moved_by<0x142, 0xA>(x);                  // row_bcast:15 into rows 1 and 3, row_bcast:31 into 2 and 3
+    x += moved_by<0x143, 0xC>(x);
+    return x;
+}
 // Loaded by here: the compiler, which does not count copies into LDS, would else wait for such a register's load, and with it for the copies asked for since, where it is first used.
 template <class T>
 __device__ __forceinline__ void loaded(T& x) { asm volatile("" : "+v"(x)); }

@@ -1,12 +1,12 @@
 // Attention of many sequences over the kept rows that they share, and over their own tails: of two sets of keys with (M1, L1, o1) and (M2, L2, o2), o un-normalised,
 // the whole has M = max, L = L1 2^(M1-M) + L2 2^(M2-M) and o likewise (scores in units of log 2).  So the rows R of all of a prefix's
-// sequences (R = (sequence, token, head)) stand side by side over its kept rows, which are read once for 128 of them (or 32), each
+// sequences (R = (sequence, token, head)) stand side by side over its kept rows, which are read once for a tile of 128 of them (64, 32), each
 // sequence's own over its tail, and a second kernel joins what they found.
 //
-// One launch: workgroups of kept rows (a prefix's KV head, 128 or 32 rows R, a part of the keys), then those of tails (a sequence's KV head, 32 rows R).
+// One launch: workgroups of tails (a sequence's KV head, 32 rows R), then those of kept rows, which share out all heads' tiles evenly, whatever the heads' lengths.
 // S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a row, V read transposed, P from
-// the registers that S^T leaves it in.  With 128 rows the four waves have 32 each and share tiles of 64 keys; with 32 each wave has tiles of 32 keys of its own and the waves are joined
-// in LDS.  Rows in 4 bits are expanded on their way into LDS, exactly.
+// the registers that S^T leaves it in.  With 128 rows the four waves have 32 each and all of a tile's 64 keys, with 64 rows 32 each and half of the keys; with 32 rows each wave has
+// tiles of 32 keys of its own; waves of the same rows are joined in LDS.  Rows in 4 bits are expanded on their way into LDS, exactly.
 // fp32: mfma_f32_32x32x2, operands straight from memory.
 
 #include <algorithm>
@@ -14,6 +14,9 @@
 #include "attend_device.h"
 #include "attend_internal.h"
 
+#ifndef SP
+#define SP 2
+#endif
 namespace curdkv {
 namespace {
 
@@ -28,17 +31,22 @@ struct SharedArgs {
     int share;
     // this launch's slice: sequences s0 .. s0 + ns - 1 of prefixes b0 .. b0 + nb - 1, tokens t0 .. t0 + nt - 1
     int b0, nb, s0, ns, t0, nt;
-    int rows, tiles;                   // of a prefix's KV head: ns * nt * group, and tiles of kTile (or 4 kTile) of them
-    int parts;                         // that its kept rows are shared out over
-    int tail_tiles;                    // of a sequence's nt * group rows
-    int64_t kept_blocks, slots;        // slots: rows R of all heads, nb * kv * rows
-    float* part_o;                     // [parts + 1][slots][128], un-normalised; part `parts` is the tail's
-    f32x2a* part_ml;                   // the same of reference points and sums; sum 0: nothing seen, o not written
+    int rows, tile_rows, tiles;        // of a prefix's KV head: ns * nt * group, and tiles of tile_rows of them
+    int shares;                        // workgroups that share out the kept rows
+    int tail_tiles;                    // tiles of 32 of a sequence's nt * group rows
+    int64_t tail_blocks;
+    // un-normalised partial results of 128 floats a row, and their reference points and sums (sum 0: nothing seen, o not written): of share s and item i, (head, tile), at s + i, which
+    // no other pair has, [shares + items][tile_rows], then of the tails [nb * kv][rows]
+    float* part_o;
+    f32x2a* part_ml;
+    int32_t* part_of_item;             // the first and the last share that have tiles of an item (of a head without kept rows: not written)
+    int64_t tail_at;                   // rows before the tails'
+    Divisor by_group, by_per;          // by the group; by a sequence's rows, nt * group
 };
 
-// Rows R of a workgroup: first + col of `rows` of prefix g's head, or of one sequence's.
+// Rows R of a workgroup, first .. end - 1 of a head's (or of one sequence's), and where row R's partial result lies, at + R.
 struct Rows {
-    int64_t slot;                      // of row 0
+    int64_t at;
     int first, end;
 };
 
@@ -63,11 +71,25 @@ __device__ __forceinline__ u32x4a eight_bf16(uint32_t codes, float unit) {
 
 // The global row of row R of prefix bi's head (of the slice), and its token.
 __device__ __forceinline__ int64_t query_row(const SharedArgs& a, int bi, int head, int R, int* token) {
-    const int per = a.nt * a.c.group, s = R / per, t = R % per / a.c.group;
+    const int s = a.by_per.of(R), in = a.by_per.rest(R, s), t = a.by_group.of(in);
     *token = a.t0 + t;
-    return ((((int64_t)(a.b0 + bi) * a.share + a.s0 + s) * a.c.m + a.t0 + t) * a.c.kv + head) * a.c.group + R % a.c.group;
+    return ((((int64_t)(a.b0 + bi) * a.share + a.s0 + s) * a.c.m + a.t0 + t) * a.c.kv + head) * a.c.group + a.by_group.rest(in, t);
 }
 
+// The kept rows of head g of the slice: where they begin, and how many there are.
+struct Kept {
+    int64_t at;
+    int count;
+};
+__device__ __forceinline__ Kept kept_rows(const SharedArgs& a, int g) {
+    const int64_t* offsets = a.c.offsets + (int64_t)a.b0 * a.c.kv + g;
+    const int64_t begin = min(max(offsets[0], (int64_t)0), a.c.total);
+    return {begin, (int)(min(max(offsets[1], begin), a.c.total) - begin)};
+}
+// The kept rows' tiles of 64 keys are shared out by their cost, head after head and within a head row tile after row tile: a tile each, and kItemCost for every (head, row tile).
+// Share s has [total s / shares, total (s + 1) / shares), of no more shares than the total.
+constexpr int kItemCost = 2;
+__device__ __forceinline__ int cost_of(int count) { return count > 0 ? (count + 63) / 64 + kItemCost : 0; }
 // A wave's 32 rows R over tiles of KEYS keys in LDS.
 struct Wave {
     u32x4a q[8];
@@ -82,7 +104,8 @@ struct Wave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
     }
-    template <int KB>
+    // KB blocks of 32 keys, columns STRIDE bytes apart
+    template <int KB, int STRIDE>
     __device__ __forceinline__ void scores(const char* Kt, int col, int half, f32x16a (&x)[KB]) const {
         const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
 #pragma unroll
@@ -90,18 +113,20 @@ struct Wave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[kb] = product(*(const u32x4a*)(Kt + k_at[i & 1] + (i >> 1) * (KB * 2048) + kb * 2048), q[i], x[kb]);
+            for (int i = 0; i < 8; ++i) x[kb] = product(*(const u32x4a*)(Kt + k_at[i & 1] + (i >> 1) * STRIDE + kb * 2048), q[i], x[kb]);
         }
     }
-    // scores -> weights (relative to `ref`, which moves when it lies too far below), pairs of bf16 in the order of the next product
     template <int KB>
-    __device__ __forceinline__ void weigh(f32x16a (&x)[KB], float scale_log2, uint32_t (&pb)[KB * 8]) {
+    __device__ __forceinline__ float top_of(const f32x16a (&x)[KB], float scale_log2) const {
         float top = x[0][0];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
-        top = halves_max(top) * scale_log2;
+        return halves_max(top) * scale_log2;
+    }
+    // the reference point moves where it lies too far below
+    __device__ __forceinline__ void raise(float top) {
         if (__any(top > ref + kLoose)) {
             const float next = top > ref + kLoose ? top : ref, keep = next == ref ? 1.f : __builtin_amdgcn_exp2f(ref - next);
             sum *= keep;
@@ -109,23 +134,28 @@ struct Wave {
             for (int db = 0; db < 4; ++db) o[db] *= keep;
             ref = next;
         }
-#pragma unroll
-        for (int i = 0; i < KB * 16; i += 2) {
-            const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 4][i & 15], scale_log2, -ref));
-            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 4][(i & 15) + 1], scale_log2, -ref));
-            sum += u + v;
-            pb[i / 2] = pack_bf16(u, v);
-        }
     }
-    template <int KB, bool FINITE>     // !FINITE: zeros in the place of infinities and NaN
+    // the weights of scores i and i + 1, a pair of bf16
+    template <int KB>
+    __device__ __forceinline__ uint32_t weigh(const f32x16a (&x)[KB], int i, float scale_log2) {
+        const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 4][i & 15], scale_log2, -ref));
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 4][(i & 15) + 1], scale_log2, -ref));
+        sum += u + v;
+        return pack_bf16(u, v);
+    }
+    template <int STRIDE>
+    static __device__ __forceinline__ u32x4a value(const char* Vt, int v_at, int u, int db) {
+        const char* p = Vt + v_at + db * STRIDE + u * 1024;
+        const u32x2 x = read_transposed(p), y = read_transposed(p + 512);
+        return (u32x4a){x.x, x.y, y.x, y.y};
+    }
+    template <int KB, int STRIDE, bool FINITE>     // !FINITE: zeros in the place of infinities and NaN
     __device__ __forceinline__ void values(const char* Vt, int v_at, const uint32_t (&pb)[KB * 8]) {
 #pragma unroll
         for (int u = 0; u < KB * 2; ++u)
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
-                const char* p = Vt + v_at + db * (KB * 2048) + u * 1024;
-                const u32x2 x = read_transposed(p), y = read_transposed(p + 512);
-                u32x4a w = {x.x, x.y, y.x, y.y};
+                u32x4a w = value<STRIDE>(Vt, v_at, u, db);
                 if (!FINITE)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -136,9 +166,14 @@ struct Wave {
             }
     }
 };
+// Scores of keys beyond `far` (counted from the half's first) are -infinity.
+template <int KB>
+__device__ __forceinline__ void hide(f32x16a (&s)[KB], int far) {
+#pragma unroll
+    for (int i = 0; i < KB * 16; ++i) s[i >> 4][i & 15] = (i >> 4) * 32 + (i & 15) / 4 * 8 + i % 4 <= far ? s[i >> 4][i & 15] : -INFINITY;
+}
 
-// Where tiles of 32 KB keys come from, into LDS as four columns of 64 bytes a row (K's pieces of 16 bytes permuted by (row / 2) % 4); keys `begin` .. `end` - 1 of rows
-// at K, V.  PER: tiles between this wave's (each wave its own, LANES = 64) or 1 (all four waves together, LANES = 256).
+// Tiles of 32 or 64 keys in LDS: four columns of 64 bytes a row, K's pieces of 16 bytes permuted by (row / 2) % 4.
 __device__ __forceinline__ uint32_t piece_at(int row, int column, int piece, bool keys, int keys_of_tile) {
     return column * (keys_of_tile * 64) + row * 64 + ((keys ? piece ^ ((row >> 1) & 3) : piece) << 4);
 }
@@ -180,23 +215,26 @@ __device__ __forceinline__ void clear_beyond(char* tile, int count, int thread) 
 }
 
 // A partial result of 32 rows R: O^T's lanes (column R, channels 32 db + 8 i + 4 half ..) to rows of 128 floats.
-__device__ __forceinline__ void store_part(const Wave& w, float* to, int half, float scale) {
+__device__ __forceinline__ void store_part(const Wave& w, float* to, int half) {
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            *(f32x4a*)(to + db * 32 + i * 8 + half * 4) = (f32x4a){w.o[db][4 * i] * scale, w.o[db][4 * i + 1] * scale, w.o[db][4 * i + 2] * scale, w.o[db][4 * i + 3] * scale};
+            *(f32x4a*)(to + db * 32 + i * 8 + half * 4) = (f32x4a){w.o[db][4 * i], w.o[db][4 * i + 1], w.o[db][4 * i + 2], w.o[db][4 * i + 3]};
 }
 
-// The parts of four waves over the same 32 rows R, through 64 KB of LDS: one partial result.
+// The parts of four waves, WAVES of them over the same 32 rows R (wave % (4 / WAVES) says which), through 64 KB of LDS.
+template <int WAVES>
 __device__ __forceinline__ void join_waves(Wave& w, char* lds, f32x2a (*ml)[kTile], float* part_o, f32x2a* part_ml, const Rows& r) {
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    constexpr int kSets = 4 / WAVES;                               // of 32 rows
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5, set = wave % kSets;
     const float sum = halves_sum(w.sum);
+    __syncthreads();                   // (nobody reads tiles any more)
     if (half == 0) ml[wave][col] = (f32x2a){w.ref, sum};
-    __syncthreads();                   // (and nobody reads tiles any more)
-    float ref = ml[0][col].x;
+    __syncthreads();
+    float ref = ml[set][col].x;
 #pragma unroll
-    for (int k = 1; k < 4; ++k) ref = fmaxf(ref, ml[k][col].x);
+    for (int k = 1; k < WAVES; ++k) ref = fmaxf(ref, ml[set + k * kSets][col].x);
     // (16-byte pieces permuted by the row, so that the rows of a store meet different banks)
     const float scale = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.ref - ref);
     float* to = (float*)lds + (wave * kTile + col) * 128;
@@ -207,55 +245,49 @@ __device__ __forceinline__ void join_waves(Wave& w, char* lds, f32x2a (*ml)[kTil
             *(f32x4a*)(to + ((db * 8 + i * 2 + half) ^ (col & 7)) * 4) =
                 (f32x4a){w.o[db][4 * i] * scale, w.o[db][4 * i + 1] * scale, w.o[db][4 * i + 2] * scale, w.o[db][4 * i + 3] * scale};
     __syncthreads();
-    const int row = tid >> 3, R = r.first + row;
-    if (R >= r.end) return;
-    float m = ml[0][row].x, l = 0.f;
 #pragma unroll
-    for (int k = 1; k < 4; ++k) m = fmaxf(m, ml[k][row].x);
+    for (int s = 0; s < kSets; ++s) {
+        const int row = tid >> 3, R = r.first + s * kTile + row;
+        if (R >= r.end) continue;
+        float m = ml[s][row].x, l = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) l += ml[k][row].y == 0.f ? 0.f : ml[k][row].y * __builtin_amdgcn_exp2f(ml[k][row].x - m);
-    if ((tid & 7) == 0) part_ml[r.slot + R] = (f32x2a){m, l};
-    if (l == 0.f) return;
+        for (int k = 1; k < WAVES; ++k) m = fmaxf(m, ml[s + k * kSets][row].x);
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const int piece = (tid & 7) + p * 8;
-        f32x4a x = {0, 0, 0, 0};
+        for (int k = 0; k < WAVES; ++k) l += ml[s + k * kSets][row].y == 0.f ? 0.f : ml[s + k * kSets][row].y * __builtin_amdgcn_exp2f(ml[s + k * kSets][row].x - m);
+        if ((tid & 7) == 0) part_ml[r.at + R] = (f32x2a){m, l};
+        if (l == 0.f) continue;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x += *(const f32x4a*)((const float*)lds + (k * kTile + row) * 128 + (piece ^ (row & 7)) * 4);
-        *(f32x4a*)(part_o + (r.slot + R) * 128 + piece * 4) = x;
+        for (int p = 0; p < 4; ++p) {
+            const int piece = (tid & 7) + p * 8;
+            f32x4a x = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) x += *(const f32x4a*)((const float*)lds + ((s + k * kSets) * kTile + row) * 128 + (piece ^ (row & 7)) * 4);
+            *(f32x4a*)(part_o + (r.at + R) * 128 + piece * 4) = x;
+        }
     }
 }
 
-// Tokens' positions hide a tail's later rows: key j is seen at p where j <= p.
-// A tile that some row of the 32 does not see whole, by one wave: infinities and NaN among its values must not meet the zero weights of rows that do not see them.
-template <int KB>
-__device__ __forceinline__ void hidden_step(Wave& w, const char* Kt, const char* Vt, int v_at, int j0, int p, float scale_log2, int col, int half, int lane) {
-    f32x16a s[KB];
-    w.scores<KB>(Kt, col, half, s);
-    const int far = p - j0 - half * 4;
-#pragma unroll
-    for (int i = 0; i < KB * 16; ++i) s[i >> 4][i & 15] = (i >> 4) * 32 + (i & 15) / 4 * 8 + i % 4 <= far ? s[i >> 4][i & 15] : -INFINITY;
-    uint32_t pb[KB * 8];
-    w.weigh<KB>(s, scale_log2, pb);
+// Infinities and NaN among a tile's values must not meet the zero weights of rows that do not see them: key j of 32 is seen where j <= far, of this half.  One wave.
+__device__ __forceinline__ void hidden_values(Wave& w, const char* Vt, int v_at, const uint32_t (&pb)[8], int far, int half, int lane) {
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < KB * 8; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const u32x4a x = *(const u32x4a*)(Vt + i * 1024 + lane * 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7F80u) == 0x7F80u || (x[e] & 0x7F800000u) == 0x7F800000u;
     }
     if (!__any(bad)) {
-        w.values<KB, true>(Vt, v_at, pb);
+        w.values<1, 2048, true>(Vt, v_at, pb);
         return;
     }
-    w.values<KB, false>(Vt, v_at, pb);
-    for (int key = 0; key < KB * 32; ++key) {
-        if (key > p - j0) break;
+    w.values<1, 2048, false>(Vt, v_at, pb);
+    for (int key = 0; key < 32; ++key) {
+        if (key - half * 4 > far) break;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const u32x2 v = *(const u32x2*)(Vt + db * (KB * 2048) + key * 64 + i * 16 + half * 8);
+                const u32x2 v = *(const u32x2*)(Vt + db * 2048 + key * 64 + i * 16 + half * 8);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t x = e % 2 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16;
@@ -265,10 +297,15 @@ __device__ __forceinline__ void hidden_step(Wave& w, const char* Kt, const char*
     }
 }
 
-// 32 rows R, each wave over tiles of 32 keys of its own.  TAIL: row R's token stands at p.
+template <int LEFT>
+__device__ __forceinline__ void dma_wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LEFT) : "memory"); }      // all but the last LEFT
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// 32 rows R, each wave over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values while they are.
+// TAIL: row R's token stands at p.
 template <bool MX, bool TAIL>
 __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
-                                         int begin, int end, int p, int p_low, const char* row, const Rows& r, float* part_o, f32x2a* part_ml) {
+                                         int begin, int end, int p, int p_low, const char* row, const Rows& r) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
     char *Kt = lds + wave * 16384, *Vt = Kt + 8192;
@@ -276,149 +313,265 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, f32x2a 
     Wave w;
     w.begin(row, half);
     const int tiles = (end - begin + 31) / 32;
+    Codes<2> k, v;
+    const auto key_of = [&](int tile) ALWAYS_INLINE { return begin + tile * 32; };
+    const auto count_of = [&](int tile) ALWAYS_INLINE { return min(32, end - key_of(tile)); };
+    const auto ask_k = [&](int tile) ALWAYS_INLINE {
+        if constexpr (MX) k.load((const uint8_t*)K, K_scales, key_of(tile) + min(lane >> 1, count_of(tile) - 1), (lane & 1) * 2);
+        else fetch_bf16<32, 8>(k_lds, (const char*)K + (int64_t)key_of(tile) * 256, count_of(tile), true, 0, lane);
+    };
+    const auto ask_v = [&](int tile) ALWAYS_INLINE {
+        if constexpr (MX) v.load((const uint8_t*)V, V_scales, key_of(tile) + min(lane >> 1, count_of(tile) - 1), (lane & 1) * 2);
+        else fetch_bf16<32, 8>(v_lds, (const char*)V + (int64_t)key_of(tile) * 256, count_of(tile), false, 0, lane);
+    };
+    __syncthreads();                   // (nobody reads the item's before any more)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) loaded(w.q[i]);
+    if (wave < tiles) {
+        ask_k(wave);
+        ask_v(wave);
+    }
     for (int tile = wave; tile < tiles; tile += 4) {
-        const int j0 = begin + tile * 32, count = min(32, end - j0);
-        if constexpr (MX) {
-            Codes<2> k, v;
-            const int at = min(lane >> 1, count - 1);
-            k.load((const uint8_t*)K, K_scales, j0 + at, (lane & 1) * 2);
-            v.load((const uint8_t*)V, V_scales, j0 + at, (lane & 1) * 2);
-            k.store(Kt, lane >> 1, (lane & 1) * 2, true, 32);
-            v.store(Vt, lane >> 1, (lane & 1) * 2, false, 32);
-        } else {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            fetch_bf16<32, 8>(k_lds, (const char*)K + (int64_t)j0 * 256, count, true, 0, lane);
-            fetch_bf16<32, 8>(v_lds, (const char*)V + (int64_t)j0 * 256, count, false, 0, lane);
-            dma_wait();
-        }
-        if (count < 32) clear_beyond<32, 64>(Vt, count, lane);
-        if (count < 32 || (TAIL && j0 + 31 > p_low)) {
-            hidden_step<1>(w, Kt, Vt, v_at, j0, TAIL ? min(p, end - 1) : end - 1, a.scale_log2, col, half, lane);
-            continue;
-        }
+        const int j0 = key_of(tile), count = count_of(tile), last = TAIL ? min(p, end - 1) : end - 1;
+        const bool more = tile + 4 < tiles, hidden = count < 32 || (TAIL && j0 + 31 > p_low);
+        if constexpr (MX) k.store(Kt, lane >> 1, (lane & 1) * 2, true, 32);
+        else dma_wait_but<8>();
         f32x16a s[1];
         uint32_t pb[8];
-        w.scores<1>(Kt, col, half, s);
-        w.weigh<1>(s, a.scale_log2, pb);
-        w.values<1, true>(Vt, v_at, pb);
+        w.scores<1, 2048>(Kt, col, half, s);
+        if constexpr (MX) v.store(Vt, lane >> 1, (lane & 1) * 2, false, 32);
+        lds_wait();
+        if (more) ask_k(tile + 4);
+        if (hidden) hide<1>(s, last - j0 - half * 4);
+        w.raise(w.top_of<1>(s, a.scale_log2));
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) pb[i / 2] = w.weigh<1>(s, i, a.scale_log2);
+        if constexpr (!MX) {
+            if (more) dma_wait_but<8>();
+            else dma_wait();
+        }
+        if (count < 32) clear_beyond<32, 64>(Vt, count, lane);
+        if (hidden) hidden_values(w, Vt, v_at, pb, last - j0 - half * 4, half, lane);
+        else w.values<1, 2048, true>(Vt, v_at, pb);
+        lds_wait();
+        if (more) ask_v(tile + 4);
     }
-    __syncthreads();
-    join_waves(w, lds, ml, part_o, part_ml, r);
+    join_waves<4>(w, lds, ml, a.part_o, a.part_ml, r);
 }
 
-// 128 rows R, 32 a wave, tiles of 64 keys for all.
-template <bool MX>
-__device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales, int begin, int end,
-                                          const char* row, const Rows& r, float* part_o, f32x2a* part_ml) {
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
+// 32 SETS rows R, 32 a wave, tiles of 64 keys for all; with two sets, a wave has half of a tile's keys.  The next tile's products go with this one's exponentials between them,
+// this one's products with V with the next one's maximum: K is a tile ahead of V.
+template <bool MX, int SETS>
+__device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
+                                          int begin, int end, const char* row, const Rows& r) {
+    constexpr int KB = SETS / 2;       // blocks of 32 keys a wave
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15, part = wave / SETS;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
     Wave w;
     w.begin(row, half);
     const int tiles = (end - begin + 63) / 64;
     const auto count_of = [&](int tile) ALWAYS_INLINE { return min(64, end - begin - tile * 64); };
     Codes<1> k, v;
-    const auto ask = [&](int tile) ALWAYS_INLINE {         // 4 bits: this thread's share into registers; bf16: the wave's on its way into LDS
+    // K of a tile, V of a tile: 4 bits: this thread's share into registers, and from there into LDS; bf16: the wave's on its way into LDS
+    const auto ask = [&](bool keys, int tile) ALWAYS_INLINE {
         const int64_t j0 = begin + tile * 64;
         if constexpr (MX) {
             const int at = min(tid >> 2, count_of(tile) - 1);
-            k.load((const uint8_t*)K, K_scales, j0 + at, tid & 3);
-            v.load((const uint8_t*)V, V_scales, j0 + at, tid & 3);
+            if (keys) k.load((const uint8_t*)K, K_scales, j0 + at, tid & 3);
+            else v.load((const uint8_t*)V, V_scales, j0 + at, tid & 3);
         } else {
-            char* to = lds + (tile & 1) * 32768;
-            fetch_bf16<64, 4>(lds_address(to), (const char*)K + j0 * 256, count_of(tile), true, wave * 4, lane);
-            fetch_bf16<64, 4>(lds_address(to + 16384), (const char*)V + j0 * 256, count_of(tile), false, wave * 4, lane);
+            fetch_bf16<64, 4>(lds_address(lds + (tile & 1) * 16384 + (keys ? 0 : 32768)), (const char*)(keys ? K : V) + j0 * 256, count_of(tile), keys, wave * 4, lane);
         }
     };
-    const auto arrive = [&](int tile) ALWAYS_INLINE {
-        char* to = lds + (tile & 1) * 32768;
+    const auto store = [&](bool keys, int tile) ALWAYS_INLINE {
         if constexpr (MX) {
-            k.store(to, tid >> 2, tid & 3, true, 64);
-            v.store(to + 16384, tid >> 2, tid & 3, false, 64);
-        } else {
-            dma_wait();
+            if (keys) k.store(lds + (tile & 1) * 16384, tid >> 2, tid & 3, true, 64);
+            else v.store(lds + (tile & 1) * 16384 + 32768, tid >> 2, tid & 3, false, 64);
         }
-        if (count_of(tile) < 64) {
+    };
+    const auto arrive = [&](int values) ALWAYS_INLINE {            // values: the tile whose V is among what comes
+        if constexpr (!MX) dma_wait();
+        if (values < tiles && count_of(values) < 64) {
             __syncthreads();
-            clear_beyond<64, 256>(to + 16384, count_of(tile), tid);
+            clear_beyond<64, 256>(lds + (values & 1) * 16384 + 32768, count_of(values), tid);
         }
         __syncthreads();
     };
+    const auto keys_of = [&](int tile) ALWAYS_INLINE { return lds + (tile & 1) * 16384 + part * 2048; };
+    const auto values_of = [&](int tile) ALWAYS_INLINE { return lds + (tile & 1) * 16384 + 32768 + part * 2048; };
+    const auto mask = [&](f32x16a (&s)[KB], int tile) ALWAYS_INLINE {
+        if (count_of(tile) < 64) hide<KB>(s, count_of(tile) - 1 - part * 32 - half * 4);
+    };
+    __syncthreads();                   // (nobody reads the item's before any more)
     if (tiles > 0) {
-        ask(0);
-        arrive(0);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) loaded(w.q[i]);
-    for (int tile = 0; tile < tiles; ++tile) {
-        if (tile + 1 < tiles) ask(tile + 1);
-        const char *Kt = lds + (tile & 1) * 32768, *Vt = Kt + 16384;
-        f32x16a s[2];
-        uint32_t pb[16];
-        w.scores<2>(Kt, col, half, s);
-        const int count = count_of(tile);
-        if (count < 64) {
-            const int far = count - 1 - half * 4;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = (i >> 4) * 32 + (i & 15) / 4 * 8 + i % 4 <= far ? s[i >> 4][i & 15] : -INFINITY;
+        ask(true, 0);
+        ask(false, 0);
+        store(true, 0);
+        store(false, 0);
+        if (tiles > 1) {
+            ask(true, 1);
+            store(true, 1);
         }
-        w.weigh<2>(s, a.scale_log2, pb);
-        w.values<2, true>(Vt, v_at, pb);
-        if (tile + 1 < tiles) arrive(tile + 1);
+        arrive(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) loaded(w.q[i]);
+        f32x16a s[KB];
+        w.scores<KB, 4096>(keys_of(0), col, half, s);
+        mask(s, 0);
+        float top = w.top_of<KB>(s, a.scale_log2);
+        __syncthreads();               // (K of tile 0 is read)
+        const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+#pragma unroll 1
+        for (int tile = 0; tile < tiles - 1; ++tile) {
+            if (tile + 2 < tiles) ask(true, tile + 2);
+            ask(false, tile + 1);
+            w.raise(top);
+            const char *Kt = keys_of(tile + 1), *Vt = values_of(tile);
+            f32x16a next[KB];
+            uint32_t pb[KB * 8];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
+            u32x4a kk[2][KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) kk[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i < 7)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) kk[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) next[kb] = product(kk[i & 1][kb], w.q[i], next[kb]);
+#pragma unroll
+                for (int j = 0; j < 2 * KB; j += 2) pb[(i * 2 * KB + j) / 2] = w.weigh<KB>(s, i * 2 * KB + j, a.scale_log2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            u32x4a vv[2][4];
+#pragma unroll
+            for (int db = 0; db < 4; ++db) vv[0][db] = Wave::value<4096>(Vt, v_at, 0, db);
+            if (tile + 2 == tiles) mask(next, tile + 1);
+            float most = next[0][0];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 2 * KB; ++u) {
+                if (u < 2 * KB - 1)
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) vv[(u + 1) & 1][db] = Wave::value<4096>(Vt, v_at, u + 1, db);
+                const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
+#pragma unroll
+                for (int db = 0; db < 4; ++db) w.o[db] = product(vv[u & 1][db], pu, w.o[db]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            top = halves_max(most) * a.scale_log2;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) s[kb] = next[kb];
+            if (tile + 2 < tiles) store(true, tile + 2);
+            store(false, tile + 1);
+            arrive(tile + 1);
+        }
+        w.raise(top);
+        uint32_t pb[KB * 8];
+#pragma unroll
+        for (int i = 0; i < KB * 16; i += 2) pb[i / 2] = w.weigh<KB>(s, i, a.scale_log2);
+        w.values<KB, 4096, true>(values_of(tiles - 1), v_at, pb);
+    }
+    if constexpr (SETS == 2) {
+        join_waves<2>(w, lds, ml, a.part_o, a.part_ml, r);
+        return;
     }
     const float sum = halves_sum(w.sum);
     const int R = r.first + wave * 32 + col;
     if (R >= r.end) return;
-    if (half == 0) part_ml[r.slot + R] = (f32x2a){w.ref, sum};
-    if (sum != 0.f) store_part(w, part_o + (r.slot + R) * 128, half, 1.f);
+    if (half == 0) a.part_ml[r.at + R] = (f32x2a){w.ref, sum};
+    if (sum != 0.f) store_part(w, a.part_o + (r.at + R) * 128, half);
 }
 
-// The kept rows of prefix head g of the slice that part `part` has: [begin, end) of the arrays.
-struct Kept {
-    int64_t at;                        // of row 0
-    int begin, end;
+// A tail: its rows R, its token's positions, its keys.
+struct Tail {
+    int bi, head, R0, R1, length, p_low, p_high;
+    int64_t sequence;
 };
-__device__ __forceinline__ Kept kept_rows(const SharedArgs& a, int g, int part) {
+__device__ __forceinline__ Tail tail_of(const SharedArgs& a, int64_t i) {
+    Tail t;
     const AttendCall& c = a.c;
-    const int64_t* offsets = c.offsets + (int64_t)a.b0 * c.kv + g;
-    const int64_t begin = min(max(offsets[0], (int64_t)0), c.total), count = min(max(offsets[1], begin), c.total) - begin, tiles = (count + 63) / 64;
-    return {uniform(begin), __builtin_amdgcn_readfirstlane((int)(tiles * part / a.parts * 64)),
-            __builtin_amdgcn_readfirstlane((int)min(count, tiles * (part + 1) / a.parts * 64))};
+    t.head = (int)(i % c.kv);
+    const int tile = (int)(i / c.kv % a.tail_tiles), s = (int)(i / c.kv / a.tail_tiles % a.ns), per = a.nt * c.group;
+    t.bi = (int)(i / c.kv / a.tail_tiles / a.ns);
+    t.sequence = (int64_t)(a.b0 + t.bi) * a.share + a.s0 + s;
+    t.length = __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[t.sequence], 0), c.n) : c.n);
+    t.R0 = s * per + tile * kTile, t.R1 = s * per + min(per, (tile + 1) * kTile);
+    t.p_low = t.length - c.m + a.t0 + tile * kTile / c.group;
+    t.p_high = t.length - c.m + a.t0 + (t.R1 - 1 - s * per) / c.group;
+    return t;
 }
+__device__ __forceinline__ Rows rows_of_tail(const SharedArgs& a, const Tail& t) { return {a.tail_at + ((int64_t)t.bi * a.c.kv + t.head) * a.rows, t.R0, t.R1}; }
 
-template <bool MX, bool MANY>
+// This workgroup's share of the kept rows: item(head of the slice, row tile, its number, kept rows, first and last tile of 64 keys).
+template <class F>
+__device__ __forceinline__ void each_item(const SharedArgs& a, int share, const F& item) {
+    const int heads = a.nb * a.c.kv, lane = threadIdx.x & 63;
+    const auto head_of = [&](int base) ALWAYS_INLINE { return base + lane < heads ? kept_rows(a, base + lane) : Kept{0, 0}; };
+    Kept mine = head_of(0);
+    int cost = cost_of(mine.count), sum = up_to(cost);
+    int64_t total = __builtin_amdgcn_readlane(sum, 63), before = 0;
+    for (int base = 64; base < heads; base += 64) total += __builtin_amdgcn_readlane(up_to(cost_of(head_of(base).count)), 63);
+    total *= a.tiles;
+    const int shares = (int)min((int64_t)a.shares, total);
+    if (share >= shares) return;
+    const int64_t low = total * share / shares, high = total * (share + 1) / shares;
+    for (int base = 0; base < heads && before * a.tiles < high; base += 64) {
+        if (base > 0) mine = head_of(base), cost = cost_of(mine.count), sum = up_to(cost);
+        const int64_t begin = (before + sum - cost) * a.tiles;     // of the head
+        before += __builtin_amdgcn_readlane(sum, 63);
+        for (uint64_t some = __ballot(cost > 0 && begin < high && begin + (int64_t)cost * a.tiles > low); some; some &= some - 1) {
+            const int l = __builtin_ctzll(some), each = __builtin_amdgcn_readlane(cost, l), count = __builtin_amdgcn_readlane(mine.count, l);
+            const int64_t from = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)begin, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(begin >> 32), l) << 32);
+            const int64_t at = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine.at, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine.at >> 32), l) << 32);
+            for (int tile = (int)(max(low - from, (int64_t)0) / each); tile < a.tiles; ++tile) {
+                const int64_t first = from + (int64_t)tile * each + kItemCost;      // where the tiles of keys begin
+                if (first - kItemCost >= high) break;
+                const int x = (int)min(max(low - first, (int64_t)0), (int64_t)(each - kItemCost)), y = (int)min(max(high - first, (int64_t)0), (int64_t)(each - kItemCost));
+                if (x >= y) continue;
+                if (threadIdx.x == 0 && x == 0) a.part_of_item[2 * ((base + l) * a.tiles + tile)] = share;
+                if (threadIdx.x == 0 && y == each - kItemCost) a.part_of_item[2 * ((base + l) * a.tiles + tile) + 1] = share;
+                item(base + l, tile, Kept{at, count}, x * 64, min(y * 64, count));
+            }
+        }
+    }
+}
+// Where the partial results of share s and (head g, row tile) begin.
+__device__ __forceinline__ int64_t part_of(const SharedArgs& a, int share, int g, int tile) { return ((int64_t)share + (int64_t)g * a.tiles + tile) * a.tile_rows; }
+
+template <bool MX, int SETS>
 __global__ __launch_bounds__(256, 2) void attend_shared_kernel(SharedArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[65536];
     __shared__ f32x2a ml[4][kTile];
     const AttendCall& c = a.c;
     const int tid = threadIdx.x, col = tid & 31;
-    if (blockIdx.x < a.kept_blocks) {
-        constexpr int kRows = MANY ? 4 * kTile : kTile;
-        const int heads = a.nb * c.kv, g = blockIdx.x % heads, part = blockIdx.x / heads % a.parts, tile = blockIdx.x / heads / a.parts;
-        const int bi = g / c.kv, head = g % c.kv, R = min(tile * kRows + (MANY ? (tid >> 6) * 32 : 0) + col, a.rows - 1);
-        int token;
-        const char* row = (const char*)c.Q + query_row(a, bi, head, R, &token) * 256;
-        const Rows r = {(int64_t)g * a.rows, tile * kRows, a.rows};
-        const Kept k = kept_rows(a, g, part);
-        const int width = MX ? 64 : 256;
-        const char *K = (const char*)c.K_kept + k.at * width, *V = (const char*)c.V_kept + k.at * width;
-        float* part_o = a.part_o + part * a.slots * 128;
-        f32x2a* part_ml = a.part_ml + part * a.slots;
-        if constexpr (MANY) many_rows<MX>(a, lds, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, k.begin, k.end, row, r, part_o, part_ml);
-        else few_rows<MX, false>(a, lds, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, k.begin, k.end, 0, 0, row, r, part_o, part_ml);
+    int token;
+    if (blockIdx.x < a.tail_blocks) {
+        const Tail t = tail_of(a, blockIdx.x);
+        const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 256;
+        const int64_t from = (t.sequence * c.kv + t.head) * c.stride * 256;
+        few_rows<false, true>(a, lds, ml, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
+                              rows_of_tail(a, t));
         return;
     }
-    const int64_t i = blockIdx.x - a.kept_blocks;
-    const int head = (int)(i % c.kv), tile = (int)(i / c.kv % a.tail_tiles), s = (int)(i / c.kv / a.tail_tiles % a.ns), bi = (int)(i / c.kv / a.tail_tiles / a.ns);
-    const int64_t sequence = (int64_t)(a.b0 + bi) * a.share + a.s0 + s;
-    const int per = a.nt * c.group, length = __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[sequence], 0), c.n) : c.n);
-    const int R0 = s * per + tile * kTile, R1 = s * per + min(per, (tile + 1) * kTile);
-    int token;
-    const char* row = (const char*)c.Q + query_row(a, bi, head, min(R0 + col, R1 - 1), &token) * 256;
-    const int p = length - c.m + token, p_low = length - c.m + a.t0 + tile * kTile / c.group, p_high = length - c.m + a.t0 + (R1 - 1 - s * per) / c.group;
-    const Rows r = {((int64_t)bi * c.kv + head) * a.rows, R0, R1};
-    const int64_t from = (sequence * c.kv + head) * c.stride * 256;
-    few_rows<false, true>(a, lds, ml, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, p_high + 1), p, p_low, row, r,
-                          a.part_o + a.parts * a.slots * 128, a.part_ml + a.parts * a.slots);
+    // (neighbours in the list are neighbours in an XCD)
+    const int block = (int)(blockIdx.x - a.tail_blocks), eighth = a.shares >> 3, share = block < eighth * 8 ? (block & 7) * eighth + (block >> 3) : block;
+    each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
+        const int bi = g / c.kv, head = g % c.kv, R = min(tile * (SETS * kTile) + (tid >> 6) % SETS * 32 + col, a.rows - 1);
+        const char* row = (const char*)c.Q + query_row(a, bi, head, R, &token) * 256;
+        const Rows r = {part_of(a, share, g, tile) - tile * (SETS * kTile), tile * (SETS * kTile), min(a.rows, (tile + 1) * (SETS * kTile))};
+        const int width = MX ? 64 : 256;
+        const char *K = (const char*)c.K_kept + k.at * width, *V = (const char*)c.V_kept + k.at * width;
+        if constexpr (SETS > 1) many_rows<MX, SETS>(a, lds, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, row, r);
+        else few_rows<MX, false>(a, lds, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row, r);
+    });
 }
 
 // ---- fp32: a wave's 32 rows R, 32 keys at a time, operands straight from memory; the four waves take tiles in turn and are joined.
@@ -450,7 +603,7 @@ struct Source32 {                      // keys' rows of one head
 
 template <bool MX, bool TAIL>
 __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const Source32<MX>& from, int begin, int end, int p, int p_low,
-                                         const char* row, const Rows& r, float* part_o, f32x2a* part_ml) {
+                                         const char* row, const Rows& r) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     f32x4a q[16];
     Wave w;                            // (its o, ref and sum)
@@ -521,8 +674,7 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
             for (int db = 0; db < 4; ++db) w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], x[i], w.o[db], 0, 0, 0);
         }
     }
-    __syncthreads();
-    join_waves(w, lds, ml, part_o, part_ml, r);
+    join_waves<4>(w, lds, ml, a.part_o, a.part_ml, r);
 }
 
 template <bool MX>
@@ -532,46 +684,74 @@ __global__ __launch_bounds__(256) void attend_shared_f32_kernel(SharedArgs a) {
     const AttendCall& c = a.c;
     const int col = threadIdx.x & 31;
     int token;
-    if (blockIdx.x < a.kept_blocks) {
-        const int heads = a.nb * c.kv, g = blockIdx.x % heads, part = blockIdx.x / heads % a.parts, tile = blockIdx.x / heads / a.parts;
-        const char* row = (const char*)c.Q + query_row(a, g / c.kv, g % c.kv, min(tile * kTile + col, a.rows - 1), &token) * 512;
-        const Kept k = kept_rows(a, g, part);
-        const int width = MX ? 64 : 512;
-        const Source32<MX> from = {(const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4};
-        rows_f32<MX, false>(a, lds, ml, from, k.begin, k.end, 0, 0, row, {(int64_t)g * a.rows, tile * kTile, a.rows}, a.part_o + part * a.slots * 128,
-                            a.part_ml + part * a.slots);
+    if (blockIdx.x < a.tail_blocks) {
+        const Tail t = tail_of(a, blockIdx.x);
+        const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 512;
+        const int64_t at = (t.sequence * c.kv + t.head) * c.stride * 512;
+        rows_f32<false, true>(a, lds, ml, Source32<false>{(const char*)c.K + at, (const char*)c.V + at, nullptr, nullptr}, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
+                              rows_of_tail(a, t));
         return;
     }
-    const int64_t i = blockIdx.x - a.kept_blocks;
-    const int head = (int)(i % c.kv), tile = (int)(i / c.kv % a.tail_tiles), s = (int)(i / c.kv / a.tail_tiles % a.ns), bi = (int)(i / c.kv / a.tail_tiles / a.ns);
-    const int64_t sequence = (int64_t)(a.b0 + bi) * a.share + a.s0 + s;
-    const int per = a.nt * c.group, length = __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[sequence], 0), c.n) : c.n);
-    const int R0 = s * per + tile * kTile, R1 = s * per + min(per, (tile + 1) * kTile);
-    const char* row = (const char*)c.Q + query_row(a, bi, head, min(R0 + col, R1 - 1), &token) * 512;
-    const int p = length - c.m + token, p_low = length - c.m + a.t0 + tile * kTile / c.group, p_high = length - c.m + a.t0 + (R1 - 1 - s * per) / c.group;
-    const int64_t at = (sequence * c.kv + head) * c.stride * 512;
-    rows_f32<false, true>(a, lds, ml, Source32<false>{(const char*)c.K + at, (const char*)c.V + at, nullptr, nullptr}, 0, max(0, p_high + 1), p, p_low, row,
-                          {((int64_t)bi * c.kv + head) * a.rows, R0, R1}, a.part_o + a.parts * a.slots * 128, a.part_ml + a.parts * a.slots);
+    const int block = (int)(blockIdx.x - a.tail_blocks), eighth = a.shares >> 3, share = block < eighth * 8 ? (block & 7) * eighth + (block >> 3) : block;
+    each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
+        const char* row = (const char*)c.Q + query_row(a, g / c.kv, g % c.kv, min(tile * kTile + col, a.rows - 1), &token) * 512;
+        const int width = MX ? 64 : 512;
+        const Source32<MX> from = {(const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4};
+        rows_f32<MX, false>(a, lds, ml, from, begin, end, 0, 0, row, {part_of(a, share, g, tile) - tile * kTile, tile * kTile, min(a.rows, (tile + 1) * kTile)});
+    });
 }
 
-// Joins the parts of four rows, a wave a row, two channels a lane.
+// Joins the parts of four rows, a wave a row, two channels a lane: the shares that have tiles of its item, in order, and its tail's.
 template <bool BF16>
 __global__ __launch_bounds__(256) void attend_shared_join_kernel(SharedArgs a) {
     const AttendCall& c = a.c;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= a.slots) return;
-    const int lane = threadIdx.x & 63, g = (int)(at / a.rows), R = (int)(at - (int64_t)g * a.rows), head = g % c.kv;
-    float ref = kNoScore, sum = 0.f;
-    for (int k = 0; k <= a.parts; ++k) ref = fmaxf(ref, a.part_ml[at + k * a.slots].x);
+    const int quads = (a.rows + 3) / 4, g = blockIdx.x / quads, R = __builtin_amdgcn_readfirstlane(blockIdx.x % quads * 4 + (threadIdx.x >> 6));
+    if (R >= a.rows) return;
+    const int lane = threadIdx.x & 63, head = g % c.kv, tile = R / a.tile_rows, item = g * a.tiles + tile;
+    const int64_t at = part_of(a, 0, g, tile) + R - tile * a.tile_rows, tail = a.tail_at + (int64_t)g * a.rows + R;
+    const int first = a.part_of_item[2 * item], final = a.part_of_item[2 * item + 1];
+    const f32x2a last = a.part_ml[tail], of_last = *(const f32x2a*)(a.part_o + tail * 128 + lane * 2);
+    const bool any = kept_rows(a, g).count > 0;
+    const int from = __builtin_amdgcn_readfirstlane(any ? first : 0), to = __builtin_amdgcn_readfirstlane(any ? final : -1);
+    // 64 shares at a time, a lane each, then their rows of 512 bytes, sixteen on their way
+    float ref = last.y == 0.f ? kNoScore : last.x;
+    for (int s = from + lane; s <= to; s += 64)
+        ref = fmaxf(ref, a.part_ml[at + (int64_t)s * a.tile_rows].x);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
+    float sum = 0.f;
     f32x2a o = {0, 0};
-    for (int k = 0; k <= a.parts; ++k) {
-        const f32x2a ml = a.part_ml[at + k * a.slots];
-        if (ml.y == 0.f) continue;     // (nothing seen, o not written)
-        const f32x2a x = *(const f32x2a*)(a.part_o + (at + k * a.slots) * 128 + lane * 2);
-        const float weight = __builtin_amdgcn_exp2f(ml.x - ref);
+    for (int base = from; base <= to; base += 64) {
+        const int s = base + lane;
+        f32x2a ml = {0, 0};
+        if (s <= to) ml = a.part_ml[at + (int64_t)s * a.tile_rows];
+        const float weight = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
         sum += weight * ml.y;
-        o.x += weight * x.x;
-        o.y += weight * x.y;
+        const uint64_t some = __ballot(ml.y != 0.f);
+        const int many = min(64, to - base + 1);
+        for (int k = 0; k < many; k += 16) {
+            f32x2a x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int of = min(k + e, many - 1);
+                x[e] = *(const f32x2a*)(a.part_o + (at + (int64_t)(base + of) * a.tile_rows) * 128 + lane * 2);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (k + e < many && (some >> (k + e) & 1)) {
+                    const float w = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(weight), k + e));
+                    o.x += w * x[e].x;
+                    o.y += w * x[e].y;
+                }
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (last.y != 0.f) {
+        const float w = __builtin_amdgcn_exp2f(last.x - ref);
+        sum += w * last.y;
+        o.x += w * of_last.x;
+        o.y += w * of_last.y;
     }
     const bool empty = sum == 0.f;
     const float over = empty ? 0.f : 1.f / sum;
@@ -580,8 +760,9 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(SharedArgs a) {
     if (BF16) ((uint32_t*)c.out)[row * 64 + lane] = pack_bf16(o.x * over, o.y * over);
     else ((f32x2a*)c.out)[row * 64 + lane] = (f32x2a){o.x * over, o.y * over};
     if (c.lse && lane == 0) {
-        const int64_t sequence = (int64_t)(a.b0 + g / c.kv) * a.share + a.s0 + R / (a.nt * c.group);
-        c.lse[(sequence * c.kv * c.group + head * c.group + R % c.group) * c.m + token] = empty ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+        const int s = a.by_per.of(R), in = a.by_per.rest(R, s);
+        const int64_t sequence = (int64_t)(a.b0 + g / c.kv) * a.share + a.s0 + s;
+        c.lse[(sequence * c.kv * c.group + head * c.group + a.by_group.rest(in, a.by_group.of(in))) * c.m + token] = empty ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }
 
@@ -593,11 +774,27 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
     a.scale_log2 = call.scale * (1.f / kLn2);
     a.share = share;
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16, mx = call.K_scales != nullptr;
-    // A slice's partial results, of its kept rows and its tails, have to lie in scratch: whole prefixes, else sequences of one, else tokens of one.
-    const int64_t room = (call.scratch_bytes - kScratchCounters) / (int64_t)(128 * sizeof(float) + sizeof(f32x2a)) / 2;
-    const int64_t heads = (int64_t)call.kv * call.group;
-    const int64_t tokens = std::min<int64_t>(call.m, room / heads), sequences = tokens < call.m ? 1 : std::min<int64_t>(share, room / (heads * tokens));
-    const int64_t prefixes = sequences < share ? 1 : std::min<int64_t>(call.count, room / (heads * tokens * sequences));
+    // A slice's partial results, of its kept rows and its tails, have to lie in scratch: whole prefixes, else sequences of one, else tokens of one.  Rows R of a head fill tiles of 128,
+    // up to three times their number where few fill one of 32; a share of a tile more.
+    const int64_t room = (call.scratch_bytes - kScratchCounters) / (int64_t)(128 * sizeof(float) + sizeof(f32x2a));
+    const int64_t most = room - 1024;
+    const auto padded = [&](int64_t prefixes, int64_t sequences, int64_t tokens) {       // partial results of one share, and of the tails
+        const int64_t rows = sequences * tokens * call.group, tile = !bf16 || rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+        return prefixes * call.kv * ((rows + tile - 1) / tile * tile + rows);
+    };
+    const auto fitting = [&](int64_t of, const auto& size) {       // the most of them that fit
+        int64_t x = 1, y = of;                                     // x fits (cache_api.hip sees to one token of one sequence)
+        while (x < y) {
+            const int64_t z = (x + y + 1) / 2;
+            if (size(z) <= most) x = z;
+            else y = z - 1;
+        }
+        return x;
+    };
+    const int64_t tokens = fitting(call.m, [&](int64_t x) { return padded(1, 1, x); });
+    const int64_t sequences = tokens < call.m ? 1 : fitting(share, [&](int64_t x) { return padded(1, x, tokens); });
+    const int64_t prefixes = sequences < share ? 1 : fitting(call.count, [&](int64_t x) { return padded(x, sequences, tokens); });
+    a.by_group = Divisor(call.group);
     for (int64_t b = 0; b < call.count; b += prefixes)
         for (int64_t s = 0; s < share; s += sequences)
             for (int64_t t = 0; t < call.m; t += tokens) {
@@ -605,22 +802,26 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 a.s0 = (int)s, a.ns = (int)std::min<int64_t>(sequences, share - s);
                 a.t0 = (int)t, a.nt = (int)std::min<int64_t>(tokens, call.m - t);
                 a.rows = a.ns * a.nt * call.group;
-                const bool many = bf16 && a.rows > kTile;
-                a.tiles = (a.rows + (many ? 4 : 1) * kTile - 1) / ((many ? 4 : 1) * kTile);
+                a.by_per = Divisor(a.nt * call.group);
+                const int sets = !bf16 || a.rows <= kTile ? 1 : a.rows <= 2 * kTile ? 2 : 4;
+                a.tile_rows = sets * kTile;
+                a.tiles = (a.rows + a.tile_rows - 1) / a.tile_rows;
                 a.tail_tiles = (a.nt * call.group + kTile - 1) / kTile;
-                a.slots = (int64_t)a.nb * call.kv * a.rows;
-                // Parts of the kept rows until every unit has two workgroups, 4 tiles of 64 keys each at least, as far as there is scratch.
-                const int64_t blocks = (int64_t)a.nb * call.kv * a.tiles, tiles = call.rows / (call.count * call.kv) / 64;
-                a.parts = (int)std::max<int64_t>(1, std::min(std::min(2 * ctx->num_cu / blocks, tiles / 4), 2 * room / a.slots - 1));
-                a.kept_blocks = blocks * a.parts;
+                a.tail_blocks = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
+                // Shares of the kept rows until every unit has two workgroups, SP tiles of 64 keys each at least, as far as there is scratch.
+                const int64_t items = (int64_t)a.nb * call.kv * a.tiles, tail_rows = (int64_t)a.nb * call.kv * a.rows;
+                const int64_t tiles = (call.rows / (call.count * call.kv) / 64 + 1) * items;
+                a.shares = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(2 * (int64_t)ctx->num_cu, tiles / SP), (room - 1024 - tail_rows) / a.tile_rows - items));
+                a.tail_at = (a.shares + items) * a.tile_rows;
                 a.part_o = (float*)((char*)call.scratch + kScratchCounters);
-                a.part_ml = (f32x2a*)(a.part_o + (a.parts + 1) * a.slots * 128);
-                const int64_t all = a.kept_blocks + (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
-                const auto launch = [&](auto kernel) { kernel<<<(unsigned)all, 256, 0, stream>>>(a); };
+                a.part_ml = (f32x2a*)(a.part_o + (a.tail_at + tail_rows) * 128);
+                a.part_of_item = (int32_t*)(a.part_ml + a.tail_at + tail_rows);
+                const auto launch = [&](auto kernel) { kernel<<<(unsigned)(a.tail_blocks + a.shares), 256, 0, stream>>>(a); };
                 if (!bf16) mx ? launch(attend_shared_f32_kernel<true>) : launch(attend_shared_f32_kernel<false>);
-                else if (many) mx ? launch(attend_shared_kernel<true, true>) : launch(attend_shared_kernel<false, true>);
-                else mx ? launch(attend_shared_kernel<true, false>) : launch(attend_shared_kernel<false, false>);
-                const unsigned joins = (unsigned)((a.slots + 3) / 4);
+                else if (sets == 4) mx ? launch(attend_shared_kernel<true, 4>) : launch(attend_shared_kernel<false, 4>);
+                else if (sets == 2) mx ? launch(attend_shared_kernel<true, 2>) : launch(attend_shared_kernel<false, 2>);
+                else mx ? launch(attend_shared_kernel<true, 1>) : launch(attend_shared_kernel<false, 1>);
+                const unsigned joins = (unsigned)((int64_t)a.nb * call.kv * ((a.rows + 3) / 4));
                 if (bf16) attend_shared_join_kernel<true><<<joins, 256, 0, stream>>>(a);
                 else attend_shared_join_kernel<false><<<joins, 256, 0, stream>>>(a);
                 const hipError_t e = hipGetLastError();

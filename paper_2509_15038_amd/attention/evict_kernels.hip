@@ -31,18 +31,6 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Sum over a wave's lanes up to and with this one.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int moved_by(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
-__device__ __forceinline__ int up_to(int x) {
-    x += moved_by<0x111, 0xF>(x);                  // row_shr:1, 2, 4, 8
-    x += moved_by<0x112, 0xF>(x);
-    x += moved_by<0x114, 0xF>(x);
-    x += moved_by<0x118, 0xF>(x);
-    x += moved_by<0x142, 0xA>(x);                  // row_bcast:15 into rows 1 and 3, row_bcast:31 into 2 and 3
-    x += moved_by<0x143, 0xC>(x);
-    return x;
-}
 // Sum over the workgroup's threads below this one; `waves`: not used by the calls right before and after.
 __device__ __forceinline__ int before_me(int x, int* waves) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sum = up_to(x);

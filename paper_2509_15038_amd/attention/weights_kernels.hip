@@ -215,16 +215,6 @@ struct Shares {
         return tile < a.key_tiles ? rows_that_see(a, length, tile * KEYS, min(tile * KEYS + KEYS, length) - 1, STAGE).stages : 0;
     }
     static __device__ __forceinline__ int cost(int stages) { return stages > 0 ? stages + kTileCost : 0; }
-    // sum over the lanes up to and with this one
-    static __device__ __forceinline__ int up_to(int x) {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
-        }
-        return x;
-    }
     // the cost of the tiles below `tile`
     __device__ __forceinline__ int64_t below(int tile) const {
         int64_t sum = 0;
@@ -458,7 +448,7 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     const int64_t total = shares.below(a.key_tiles), low = total * at / a.shares, high = total * (at + 1) / a.shares;
     int64_t before = 0;
     for (int base = 0; base < a.key_tiles && before < high; base += 64) {
-        const int stages = shares.stages(base + (int)(threadIdx.x & 63)), sum = shares.up_to(shares.cost(stages));
+        const int stages = shares.stages(base + (int)(threadIdx.x & 63)), sum = up_to(shares.cost(stages));
         const int64_t mine = before + sum - stages;                // where the tile's stages begin
         const int from = (int)min(max(low - mine, (int64_t)0), (int64_t)stages), to = (int)min(max(high - mine, (int64_t)0), (int64_t)stages);
         before += __builtin_amdgcn_readlane(sum, 63);

@@ -142,8 +142,8 @@ def test_shared_scales_and_heads(checks):
     a = shared(checks, True)
     assert call(checks, "attend_shared_mx", a, Ks=None) == (BAD, 0) and call(checks, "attend_shared_mx", a, Vs=None) == (BAD, 0)
     assert call(checks, "attend_shared_mx", a, Ks=None, Vs=None, total=0, rows=0) == (OK, 1)
-    assert call(checks, "attend_shared", dict(shared(checks), ctx=checks.made(256, 128, 1, 1000, 0))) == (OK, 1)
-    assert call(checks, "attend_shared", dict(shared(checks), ctx=checks.made(256, 129, 1, 1000, 0))) == (NO, 0)
+    for kv, group, code in ((128, 128, OK), (128, 129, NO), (1024, 16, OK), (1025, 1, NO), (1, 2 ** 14, OK), (1, 2 ** 14 + 1, NO)):
+        assert call(checks, "attend_shared", dict(shared(checks), ctx=checks.made(kv, group, 1, 1000, 0))) == (code, int(code == OK)), (kv, group)
 
 
 def test_another_device_than_the_current_one(checks):

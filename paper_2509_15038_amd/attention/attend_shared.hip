@@ -41,7 +41,7 @@ struct SharedArgs {
     f32x2a* part_ml;
     int32_t* part_of_item;             // the first and the last share that have tiles of an item (of a head without kept rows: not written)
     int64_t tail_at;                   // rows before the tails'
-    Divisor by_group, by_per;          // by the group; by a sequence's rows, nt * group
+    Divisor by_group, by_per, by_kv, by_tail_tiles, by_ns, by_quads;       // by_per: by a sequence's rows, nt * group; by_quads: by fours of a head's rows
 };
 
 // Rows R of a workgroup, first .. end - 1 of a head's (or of one sequence's), and where row R's partial result lies, at + R.
@@ -87,7 +87,7 @@ __device__ __forceinline__ Kept kept_rows(const SharedArgs& a, int g) {
     return {begin, (int)(min(max(offsets[1], begin), a.c.total) - begin)};
 }
 // The kept rows' tiles of 64 keys are shared out by their cost, head after head and within a head row tile after row tile: a tile each, and kItemCost for every (head, row tile).
-// Share s has [total s / shares, total (s + 1) / shares), of no more shares than the total.
+// Shares are equal, the first of them longer by one, and no more than the total.
 constexpr int kItemCost = 2;
 __device__ __forceinline__ int cost_of(int count) { return count > 0 ? (count + 63) / 64 + kItemCost : 0; }
 // A wave's 32 rows R over tiles of KEYS keys in LDS.
@@ -495,21 +495,27 @@ struct Tail {
     int bi, head, R0, R1, length, p_low, p_high;
     int64_t sequence;
 };
-__device__ __forceinline__ Tail tail_of(const SharedArgs& a, int64_t i) {
+__device__ __forceinline__ Tail tail_of(const SharedArgs& a, int i) {
     Tail t;
     const AttendCall& c = a.c;
-    t.head = (int)(i % c.kv);
-    const int tile = (int)(i / c.kv % a.tail_tiles), s = (int)(i / c.kv / a.tail_tiles % a.ns), per = a.nt * c.group;
-    t.bi = (int)(i / c.kv / a.tail_tiles / a.ns);
+    const int tiles = a.by_kv.of(i), sequences = a.by_tail_tiles.of(tiles), tile = a.by_tail_tiles.rest(tiles, sequences), per = a.nt * c.group;
+    t.head = a.by_kv.rest(i, tiles);
+    t.bi = a.by_ns.of(sequences);
+    const int s = a.by_ns.rest(sequences, t.bi);
     t.sequence = (int64_t)(a.b0 + t.bi) * a.share + a.s0 + s;
     t.length = __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[t.sequence], 0), c.n) : c.n);
     t.R0 = s * per + tile * kTile, t.R1 = s * per + min(per, (tile + 1) * kTile);
-    t.p_low = t.length - c.m + a.t0 + tile * kTile / c.group;
-    t.p_high = t.length - c.m + a.t0 + (t.R1 - 1 - s * per) / c.group;
+    t.p_low = t.length - c.m + a.t0 + a.by_group.of(tile * kTile);
+    t.p_high = t.length - c.m + a.t0 + a.by_group.of(t.R1 - 1 - s * per);
     return t;
 }
 __device__ __forceinline__ Rows rows_of_tail(const SharedArgs& a, const Tail& t) { return {a.tail_at + ((int64_t)t.bi * a.c.kv + t.head) * a.rows, t.R0, t.R1}; }
 
+// a / b of numbers below 2^53 (fewer steps than a division of 64 bits).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    const int64_t q = (int64_t)((double)a / (double)b);
+    return q - (q * b > a) + ((q + 1) * b <= a);
+}
 // This workgroup's share of the kept rows: item(head of the slice, row tile, its number, kept rows, first and last tile of 64 keys).
 template <class F>
 __device__ __forceinline__ void each_item(const SharedArgs& a, int share, const F& item) {
@@ -520,9 +526,9 @@ __device__ __forceinline__ void each_item(const SharedArgs& a, int share, const 
     int64_t total = __builtin_amdgcn_readlane(sum, 63), before = 0;
     for (int base = 64; base < heads; base += 64) total += __builtin_amdgcn_readlane(up_to(cost_of(head_of(base).count)), 63);
     total *= a.tiles;
-    const int shares = (int)min((int64_t)a.shares, total);
-    if (share >= shares) return;
-    const int64_t low = total * share / shares, high = total * (share + 1) / shares;
+    const int64_t per = quotient(total, a.shares), longer = total - per * a.shares;
+    const int64_t low = per * share + min((int64_t)share, longer), high = per * (share + 1) + min((int64_t)share + 1, longer);
+    if (low == high) return;
     for (int base = 0; base < heads && before * a.tiles < high; base += 64) {
         if (base > 0) mine = head_of(base), cost = cost_of(mine.count), sum = up_to(cost);
         const int64_t begin = (before + sum - cost) * a.tiles;     // of the head
@@ -531,7 +537,7 @@ __device__ __forceinline__ void each_item(const SharedArgs& a, int share, const 
             const int l = __builtin_ctzll(some), each = __builtin_amdgcn_readlane(cost, l), count = __builtin_amdgcn_readlane(mine.count, l);
             const int64_t from = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)begin, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(begin >> 32), l) << 32);
             const int64_t at = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine.at, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine.at >> 32), l) << 32);
-            for (int tile = (int)(max(low - from, (int64_t)0) / each); tile < a.tiles; ++tile) {
+            for (int tile = low > from ? (int)quotient(low - from, each) : 0; tile < a.tiles; ++tile) {
                 const int64_t first = from + (int64_t)tile * each + kItemCost;      // where the tiles of keys begin
                 if (first - kItemCost >= high) break;
                 const int x = (int)min(max(low - first, (int64_t)0), (int64_t)(each - kItemCost)), y = (int)min(max(high - first, (int64_t)0), (int64_t)(each - kItemCost));
@@ -564,7 +570,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared_kernel(SharedArgs a) {
     // (neighbours in the list are neighbours in an XCD)
     const int block = (int)(blockIdx.x - a.tail_blocks), eighth = a.shares >> 3, share = block < eighth * 8 ? (block & 7) * eighth + (block >> 3) : block;
     each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
-        const int bi = g / c.kv, head = g % c.kv, R = min(tile * (SETS * kTile) + (tid >> 6) % SETS * 32 + col, a.rows - 1);
+        const int bi = a.by_kv.of(g), head = a.by_kv.rest(g, bi), R = min(tile * (SETS * kTile) + (tid >> 6) % SETS * 32 + col, a.rows - 1);
         const char* row = (const char*)c.Q + query_row(a, bi, head, R, &token) * 256;
         const Rows r = {part_of(a, share, g, tile) - tile * (SETS * kTile), tile * (SETS * kTile), min(a.rows, (tile + 1) * (SETS * kTile))};
         const int width = MX ? 64 : 256;
@@ -694,7 +700,7 @@ __global__ __launch_bounds__(256) void attend_shared_f32_kernel(SharedArgs a) {
     }
     const int block = (int)(blockIdx.x - a.tail_blocks), eighth = a.shares >> 3, share = block < eighth * 8 ? (block & 7) * eighth + (block >> 3) : block;
     each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
-        const char* row = (const char*)c.Q + query_row(a, g / c.kv, g % c.kv, min(tile * kTile + col, a.rows - 1), &token) * 512;
+        const char* row = (const char*)c.Q + query_row(a, a.by_kv.of(g), a.by_kv.rest(g, a.by_kv.of(g)), min(tile * kTile + col, a.rows - 1), &token) * 512;
         const int width = MX ? 64 : 512;
         const Source32<MX> from = {(const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4};
         rows_f32<MX, false>(a, lds, ml, from, begin, end, 0, 0, row, {part_of(a, share, g, tile) - tile * kTile, tile * kTile, min(a.rows, (tile + 1) * kTile)});
@@ -705,37 +711,42 @@ __global__ __launch_bounds__(256) void attend_shared_f32_kernel(SharedArgs a) {
 template <bool BF16>
 __global__ __launch_bounds__(256) void attend_shared_join_kernel(SharedArgs a) {
     const AttendCall& c = a.c;
-    const int quads = (a.rows + 3) / 4, g = blockIdx.x / quads, R = __builtin_amdgcn_readfirstlane(blockIdx.x % quads * 4 + (threadIdx.x >> 6));
+    const int g = a.by_quads.of(blockIdx.x), R = __builtin_amdgcn_readfirstlane(a.by_quads.rest(blockIdx.x, g) * 4 + (threadIdx.x >> 6));
     if (R >= a.rows) return;
-    const int lane = threadIdx.x & 63, head = g % c.kv, tile = R / a.tile_rows, item = g * a.tiles + tile;
-    const int64_t at = part_of(a, 0, g, tile) + R - tile * a.tile_rows, tail = a.tail_at + (int64_t)g * a.rows + R;
+    const int lane = threadIdx.x & 63, bi = a.by_kv.of(g), head = a.by_kv.rest(g, bi), tile = R / a.tile_rows, item = g * a.tiles + tile;
     const int first = a.part_of_item[2 * item], final = a.part_of_item[2 * item + 1];
-    const f32x2a last = a.part_ml[tail], of_last = *(const f32x2a*)(a.part_o + tail * 128 + lane * 2);
     const bool any = kept_rows(a, g).count > 0;
+    const int64_t at = part_of(a, 0, g, tile) + R - tile * a.tile_rows, tail = a.tail_at + (int64_t)g * a.rows + R;
+    const f32x2a last = a.part_ml[tail], of_last = *(const f32x2a*)(a.part_o + tail * 128 + lane * 2);
     const int from = __builtin_amdgcn_readfirstlane(any ? first : 0), to = __builtin_amdgcn_readfirstlane(any ? final : -1);
     // 64 shares at a time, a lane each, then their rows of 512 bytes, sixteen on their way
     float ref = last.y == 0.f ? kNoScore : last.x;
-    for (int s = from + lane; s <= to; s += 64)
-        ref = fmaxf(ref, a.part_ml[at + (int64_t)s * a.tile_rows].x);
+    const auto rows_of = [&](f32x2a (&x)[16], int base, int many) ALWAYS_INLINE {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = *(const f32x2a*)(a.part_o + (at + (int64_t)(base + min(e, many - 1)) * a.tile_rows) * 128 + lane * 2);
+    };
+    f32x2a x[16];
+    if (any) rows_of(x, from, min(16, to - from + 1));
+    f32x2a ml = {0, 0};
+    if (from + lane <= to) ml = a.part_ml[at + (int64_t)(from + lane) * a.tile_rows];
+    if (ml.y != 0.f) ref = fmaxf(ref, ml.x);
+    for (int s = from + 64 + lane; s <= to; s += 64) ref = fmaxf(ref, a.part_ml[at + (int64_t)s * a.tile_rows].x);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
     float sum = 0.f;
     f32x2a o = {0, 0};
     for (int base = from; base <= to; base += 64) {
         const int s = base + lane;
-        f32x2a ml = {0, 0};
-        if (s <= to) ml = a.part_ml[at + (int64_t)s * a.tile_rows];
+        if (base > from) {
+            ml = (f32x2a){0, 0};
+            if (s <= to) ml = a.part_ml[at + (int64_t)s * a.tile_rows];
+        }
         const float weight = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
         sum += weight * ml.y;
-        const uint64_t some = __ballot(ml.y != 0.f);
+        const uint64_t some = __ballot(ml.y != 0.f);               // (nothing seen: the row is not written)
         const int many = min(64, to - base + 1);
         for (int k = 0; k < many; k += 16) {
-            f32x2a x[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int of = min(k + e, many - 1);
-                x[e] = *(const f32x2a*)(a.part_o + (at + (int64_t)(base + of) * a.tile_rows) * 128 + lane * 2);
-            }
+            if (base > from || k > 0) rows_of(x, base + k, min(16, many - k));
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if (k + e < many && (some >> (k + e) & 1)) {
@@ -756,12 +767,12 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(SharedArgs a) {
     const bool empty = sum == 0.f;
     const float over = empty ? 0.f : 1.f / sum;
     int token;
-    const int64_t row = query_row(a, g / c.kv, head, R, &token);
+    const int64_t row = query_row(a, bi, head, R, &token);
     if (BF16) ((uint32_t*)c.out)[row * 64 + lane] = pack_bf16(o.x * over, o.y * over);
     else ((f32x2a*)c.out)[row * 64 + lane] = (f32x2a){o.x * over, o.y * over};
     if (c.lse && lane == 0) {
         const int s = a.by_per.of(R), in = a.by_per.rest(R, s);
-        const int64_t sequence = (int64_t)(a.b0 + g / c.kv) * a.share + a.s0 + s;
+        const int64_t sequence = (int64_t)(a.b0 + bi) * a.share + a.s0 + s;
         c.lse[(sequence * c.kv * c.group + head * c.group + a.by_group.rest(in, a.by_group.of(in))) * c.m + token] = empty ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }
@@ -794,7 +805,7 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
     const int64_t tokens = fitting(call.m, [&](int64_t x) { return padded(1, 1, x); });
     const int64_t sequences = tokens < call.m ? 1 : fitting(share, [&](int64_t x) { return padded(1, x, tokens); });
     const int64_t prefixes = sequences < share ? 1 : fitting(call.count, [&](int64_t x) { return padded(x, sequences, tokens); });
-    a.by_group = Divisor(call.group);
+    a.by_group = Divisor(call.group), a.by_kv = Divisor(call.kv);
     for (int64_t b = 0; b < call.count; b += prefixes)
         for (int64_t s = 0; s < share; s += sequences)
             for (int64_t t = 0; t < call.m; t += tokens) {
@@ -807,6 +818,7 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 a.tile_rows = sets * kTile;
                 a.tiles = (a.rows + a.tile_rows - 1) / a.tile_rows;
                 a.tail_tiles = (a.nt * call.group + kTile - 1) / kTile;
+                a.by_tail_tiles = Divisor(a.tail_tiles), a.by_ns = Divisor(a.ns), a.by_quads = Divisor((a.rows + 3) / 4);
                 a.tail_blocks = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
                 // Shares of the kept rows until every unit has two workgroups, SP tiles of 64 keys each at least, as far as there is scratch.
                 const int64_t items = (int64_t)a.nb * call.kv * a.tiles, tail_rows = (int64_t)a.nb * call.kv * a.rows;

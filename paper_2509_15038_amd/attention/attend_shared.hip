@@ -1,11 +1,11 @@
 // Attention of many sequences over the kept rows that they share, and over their own tails: of two sets of keys with (M1, L1, o1) and (M2, L2, o2), o un-normalised,
 // the whole has M = max, L = L1 2^(M1-M) + L2 2^(M2-M) and o likewise (scores in units of log 2).  So the rows R of all of a prefix's
-// sequences (R = (sequence, token, head)) stand side by side over its kept rows, which are read once for a tile of 128 of them (64, 32), each
+// sequences (R = (sequence, token, head)) stand side by side over its kept rows, which are read once for a tile of up to 256 of them, each
 // sequence's own over its tail, and a second kernel joins what they found.
 //
 // One launch: workgroups of tails (a sequence's KV head, 32 rows R), then those of kept rows, which share out all heads' tiles evenly, whatever the heads' lengths.
 // S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a row, V read transposed, P from
-// the registers that S^T leaves it in.  With 128 rows the four waves have 32 each and all of a tile's 64 keys, with 64 rows 32 each and half of the keys; with 32 rows each wave has
+// the registers that S^T leaves it in.  With 256 (128) rows eight (four) waves have 32 each and all of a tile's 64 keys, with 64 rows 32 each and half of the keys; with 32 rows each wave has
 // tiles of 32 keys of its own; waves of the same rows are joined in LDS.  Rows in 4 bits are expanded on their way into LDS, exactly.
 // fp32: mfma_f32_32x32x2, operands straight from memory.
 
@@ -14,9 +14,6 @@
 #include "attend_device.h"
 #include "attend_internal.h"
 
-#ifndef SP
-#define SP 2
-#endif
 namespace curdkv {
 namespace {
 
@@ -223,10 +220,10 @@ __device__ __forceinline__ void store_part(const Wave& w, float* to, int half) {
             *(f32x4a*)(to + db * 32 + i * 8 + half * 4) = (f32x4a){w.o[db][4 * i], w.o[db][4 * i + 1], w.o[db][4 * i + 2], w.o[db][4 * i + 3]};
 }
 
-// The parts of four waves, WAVES of them over the same 32 rows R (wave % (4 / WAVES) says which), through 64 KB of LDS.
-template <int WAVES>
+// The parts of W waves, WAVES of them over the same 32 rows R (wave % (W / WAVES) says which), through 16 KB of LDS each.
+template <int WAVES, int W>
 __device__ __forceinline__ void join_waves(Wave& w, char* lds, f32x2a (*ml)[kTile], float* part_o, f32x2a* part_ml, const Rows& r) {
-    constexpr int kSets = 4 / WAVES;                               // of 32 rows
+    constexpr int kSets = W / WAVES;                               // of 32 rows
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5, set = wave % kSets;
     const float sum = halves_sum(w.sum);
     __syncthreads();                   // (nobody reads tiles any more)
@@ -248,7 +245,7 @@ __device__ __forceinline__ void join_waves(Wave& w, char* lds, f32x2a (*ml)[kTil
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
         const int row = tid >> 3, R = r.first + s * kTile + row;
-        if (R >= r.end) continue;
+        if (row >= kTile || R >= r.end) continue;
         float m = ml[s][row].x, l = 0.f;
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) m = fmaxf(m, ml[s + k * kSets][row].x);
@@ -303,15 +300,14 @@ __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)"
 
 // 32 rows R, each wave over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values while they are.
 // TAIL: row R's token stands at p.
-template <bool MX, bool TAIL>
-__device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
+template <bool MX, bool TAIL, int W>
+__device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
                                          int begin, int end, int p, int p_low, const char* row, const Rows& r) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
     char *Kt = lds + wave * 16384, *Vt = Kt + 8192;
-    const uint32_t k_lds = lds_address(Kt), v_lds = lds_address(Vt);
+    const uint32_t k_lds = lds_at + wave * 16384, v_lds = k_lds + 8192;
     Wave w;
-    w.begin(row, half);
     const int tiles = (end - begin + 31) / 32;
     Codes<2> k, v;
     const auto key_of = [&](int tile) ALWAYS_INLINE { return begin + tile * 32; };
@@ -325,15 +321,16 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, f32x2a 
         else fetch_bf16<32, 8>(v_lds, (const char*)V + (int64_t)key_of(tile) * 256, count_of(tile), false, 0, lane);
     };
     __syncthreads();                   // (nobody reads the item's before any more)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) loaded(w.q[i]);
     if (wave < tiles) {
         ask_k(wave);
         ask_v(wave);
     }
-    for (int tile = wave; tile < tiles; tile += 4) {
+    w.begin(row, half);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) loaded(w.q[i]);
+    for (int tile = wave; tile < tiles; tile += W) {
         const int j0 = key_of(tile), count = count_of(tile), last = TAIL ? min(p, end - 1) : end - 1;
-        const bool more = tile + 4 < tiles, hidden = count < 32 || (TAIL && j0 + 31 > p_low);
+        const bool more = tile + W < tiles, hidden = count < 32 || (TAIL && j0 + 31 > p_low);
         if constexpr (MX) k.store(Kt, lane >> 1, (lane & 1) * 2, true, 32);
         else dma_wait_but<8>();
         f32x16a s[1];
@@ -341,7 +338,7 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, f32x2a 
         w.scores<1, 2048>(Kt, col, half, s);
         if constexpr (MX) v.store(Vt, lane >> 1, (lane & 1) * 2, false, 32);
         lds_wait();
-        if (more) ask_k(tile + 4);
+        if (more) ask_k(tile + W);
         if (hidden) hide<1>(s, last - j0 - half * 4);
         w.raise(w.top_of<1>(s, a.scale_log2));
 #pragma unroll
@@ -354,46 +351,67 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, f32x2a 
         if (hidden) hidden_values(w, Vt, v_at, pb, last - j0 - half * 4, half, lane);
         else w.values<1, 2048, true>(Vt, v_at, pb);
         lds_wait();
-        if (more) ask_v(tile + 4);
+        if (more) ask_v(tile + W);
     }
-    join_waves<4>(w, lds, ml, a.part_o, a.part_ml, r);
+    join_waves<W, W>(w, lds, ml, a.part_o, a.part_ml, r);
 }
 
 // 32 SETS rows R, 32 a wave, tiles of 64 keys for all; with two sets, a wave has half of a tile's keys.  The next tile's products go with this one's exponentials between them,
-// this one's products with V with the next one's maximum: K is a tile ahead of V.
+// this one's products with V with the next one's maximum: K is a tile ahead of V.  Rows in 4 bits are asked for three tiles before that (a tile is 9 KB, and 512 workgroups of them are
+// no more than a latency's worth).
 template <bool MX, int SETS>
-__device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
+__device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
                                           int begin, int end, const char* row, const Rows& r) {
-    constexpr int KB = SETS / 2;       // blocks of 32 keys a wave
+    constexpr int KB = SETS > 2 ? 2 : 1, W = SETS > 4 ? 8 : 4;     // blocks of 32 keys a wave; waves
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15, part = wave / SETS;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
+    const bool works = r.first + wave % SETS * kTile < r.end;      // (a wave without rows helps with the tiles)
     Wave w;
-    w.begin(row, half);
     const int tiles = (end - begin + 63) / 64;
     const auto count_of = [&](int tile) ALWAYS_INLINE { return min(64, end - begin - tile * 64); };
-    Codes<1> k, v;
-    // K of a tile, V of a tile: 4 bits: this thread's share into registers, and from there into LDS; bf16: the wave's on its way into LDS
-    const auto ask = [&](bool keys, int tile) ALWAYS_INLINE {
-        const int64_t j0 = begin + tile * 64;
+    // bf16: K or V of a tile on its way into LDS
+    const auto fetch = [&](bool keys, int tile) ALWAYS_INLINE {
+        if constexpr (!MX)
+            fetch_bf16<64, 16 / W>(lds_at + (tile & 1) * 16384 + (keys ? 0 : 32768), (const char*)(keys ? K : V) + (int64_t)(begin + tile * 64) * 256, count_of(tile), keys,
+                                   wave * (16 / W), lane);
+    };
+    // 4 bits: a thread's 32 channels of a row of K, and of V (of eight waves, four take K and four V), into registers and from there into LDS
+    constexpr int kAhead = 1;
+    Codes<1> codes[MX ? kAhead : 1][W == 8 ? 1 : 2];
+    const int my_row = (tid & 255) >> 2, column = tid & 3;
+    const auto load = [&](Codes<1>& x, bool keys, int tile) ALWAYS_INLINE {
+        const int t = min(tile, tiles - 1);
+        const int64_t at = begin + t * 64 + min(my_row, count_of(t) - 1);
+        x.load((const uint8_t*)(keys ? K : V), keys ? K_scales : V_scales, at, column);
+    };
+    const auto store = [&](const Codes<1>& x, bool keys, int tile) ALWAYS_INLINE {
+        if (tile < tiles) x.store(lds + (tile & 1) * 16384 + (keys ? 0 : 32768), my_row, column, keys, 64);
+    };
+    const auto ask_both = [&](int slot, int tile) ALWAYS_INLINE {  // K of tile + 1, V of tile
         if constexpr (MX) {
-            const int at = min(tid >> 2, count_of(tile) - 1);
-            if (keys) k.load((const uint8_t*)K, K_scales, j0 + at, tid & 3);
-            else v.load((const uint8_t*)V, V_scales, j0 + at, tid & 3);
-        } else {
-            fetch_bf16<64, 4>(lds_address(lds + (tile & 1) * 16384 + (keys ? 0 : 32768)), (const char*)(keys ? K : V) + j0 * 256, count_of(tile), keys, wave * 4, lane);
+            if constexpr (W == 8) {
+                load(codes[slot][0], wave < 4, wave < 4 ? tile + 1 : tile);
+            } else {
+                load(codes[slot][0], true, tile + 1);
+                load(codes[slot][1], false, tile);
+            }
         }
     };
-    const auto store = [&](bool keys, int tile) ALWAYS_INLINE {
+    const auto store_both = [&](int slot, int tile) ALWAYS_INLINE {
         if constexpr (MX) {
-            if (keys) k.store(lds + (tile & 1) * 16384, tid >> 2, tid & 3, true, 64);
-            else v.store(lds + (tile & 1) * 16384 + 32768, tid >> 2, tid & 3, false, 64);
+            if constexpr (W == 8) {
+                store(codes[slot][0], wave < 4, wave < 4 ? tile + 1 : tile);
+            } else {
+                store(codes[slot][0], true, tile + 1);
+                store(codes[slot][1], false, tile);
+            }
         }
     };
     const auto arrive = [&](int values) ALWAYS_INLINE {            // values: the tile whose V is among what comes
         if constexpr (!MX) dma_wait();
         if (values < tiles && count_of(values) < 64) {
             __syncthreads();
-            clear_beyond<64, 256>(lds + (values & 1) * 16384 + 32768, count_of(values), tid);
+            clear_beyond<64, W * 64>(lds + (values & 1) * 16384 + 32768, count_of(values), tid);
         }
         __syncthreads();
     };
@@ -403,15 +421,22 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, f32x2a
         if (count_of(tile) < 64) hide<KB>(s, count_of(tile) - 1 - part * 32 - half * 4);
     };
     __syncthreads();                   // (nobody reads the item's before any more)
-    if (tiles > 0) {
-        ask(true, 0);
-        ask(false, 0);
-        store(true, 0);
-        store(false, 0);
-        if (tiles > 1) {
-            ask(true, 1);
-            store(true, 1);
+    // (begin < end)
+    {
+        if constexpr (MX) {
+            Codes<1> k;
+            if (W == 4 || wave < 4) load(k, true, 0);
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) ask_both(x, x);
+            if (W == 4 || wave < 4) store(k, true, 0);
+            store_both(0, 0);
+            ask_both(0, kAhead);
+        } else {
+            fetch(true, 0);
+            fetch(false, 0);
+            if (tiles > 1) fetch(true, 1);
         }
+        w.begin(row, half);
         arrive(0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) loaded(w.q[i]);
@@ -421,66 +446,89 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, f32x2a
         float top = w.top_of<KB>(s, a.scale_log2);
         __syncthreads();               // (K of tile 0 is read)
         const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+        // slot: of what comes with this step, K of tile + 2 and V of tile + 1
+        const auto step = [&](int tile, int slot) ALWAYS_INLINE {
+            if constexpr (!MX) {
+                if (tile + 2 < tiles) fetch(true, tile + 2);
+                fetch(false, tile + 1);
+            }
+            if (works) {
+                w.raise(top);
+                const char *Kt = keys_of(tile + 1), *Vt = values_of(tile);
+                f32x16a next[KB];
+                uint32_t pb[KB * 8];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
+                u32x4a kk[2][KB];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) kk[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (i < 7)
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb) kk[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) next[kb] = product(kk[i & 1][kb], w.q[i], next[kb]);
+#pragma unroll
+                    for (int j = 0; j < 2 * KB; j += 2) pb[(i * 2 * KB + j) / 2] = w.weigh<KB>(s, i * 2 * KB + j, a.scale_log2);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                u32x4a vv[KB][4];                                  // (KB of 1: two steps, no more registers for them)
+#pragma unroll
+                for (int db = 0; db < 4; ++db) vv[0][db] = Wave::value<4096>(Vt, v_at, 0, db);
+                if (tile + 2 == tiles) mask(next, tile + 1);
+                float most = next[0][0];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < 2 * KB; ++u) {
+                    if (KB > 1 && u < 2 * KB - 1)
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) vv[(u + 1) % KB][db] = Wave::value<4096>(Vt, v_at, u + 1, db);
+                    if (KB == 1 && u > 0)
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) vv[0][db] = Wave::value<4096>(Vt, v_at, u, db);
+                    const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) w.o[db] = product(vv[u % KB][db], pu, w.o[db]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                top = halves_max(most) * a.scale_log2;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) s[kb] = next[kb];
+            }
+            store_both(slot, tile + 1);
+            ask_both(slot, tile + 1 + kAhead);
+            arrive(tile + 1);
+        };
+        int tile = 0;
+        if constexpr (MX) {
 #pragma unroll 1
-        for (int tile = 0; tile < tiles - 1; ++tile) {
-            if (tile + 2 < tiles) ask(true, tile + 2);
-            ask(false, tile + 1);
+            while (tile < tiles - 1) {
+#pragma unroll
+                for (int x = 1; x <= kAhead; ++x) {
+                    step(tile++, x % kAhead);
+                    if (tile >= tiles - 1) break;
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (; tile < tiles - 1; ++tile) step(tile, 0);
+        }
+        if (works) {
             w.raise(top);
-            const char *Kt = keys_of(tile + 1), *Vt = values_of(tile);
-            f32x16a next[KB];
             uint32_t pb[KB * 8];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
-            u32x4a kk[2][KB];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) kk[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (i < 7)
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) kk[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) next[kb] = product(kk[i & 1][kb], w.q[i], next[kb]);
-#pragma unroll
-                for (int j = 0; j < 2 * KB; j += 2) pb[(i * 2 * KB + j) / 2] = w.weigh<KB>(s, i * 2 * KB + j, a.scale_log2);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            u32x4a vv[2][4];
-#pragma unroll
-            for (int db = 0; db < 4; ++db) vv[0][db] = Wave::value<4096>(Vt, v_at, 0, db);
-            if (tile + 2 == tiles) mask(next, tile + 1);
-            float most = next[0][0];
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int u = 0; u < 2 * KB; ++u) {
-                if (u < 2 * KB - 1)
-#pragma unroll
-                    for (int db = 0; db < 4; ++db) vv[(u + 1) & 1][db] = Wave::value<4096>(Vt, v_at, u + 1, db);
-                const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
-#pragma unroll
-                for (int db = 0; db < 4; ++db) w.o[db] = product(vv[u & 1][db], pu, w.o[db]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            top = halves_max(most) * a.scale_log2;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) s[kb] = next[kb];
-            if (tile + 2 < tiles) store(true, tile + 2);
-            store(false, tile + 1);
-            arrive(tile + 1);
+            for (int i = 0; i < KB * 16; i += 2) pb[i / 2] = w.weigh<KB>(s, i, a.scale_log2);
+            w.values<KB, 4096, true>(values_of(tiles - 1), v_at, pb);
         }
-        w.raise(top);
-        uint32_t pb[KB * 8];
-#pragma unroll
-        for (int i = 0; i < KB * 16; i += 2) pb[i / 2] = w.weigh<KB>(s, i, a.scale_log2);
-        w.values<KB, 4096, true>(values_of(tiles - 1), v_at, pb);
     }
     if constexpr (SETS == 2) {
-        join_waves<2>(w, lds, ml, a.part_o, a.part_ml, r);
+        join_waves<2, 4>(w, lds, ml, a.part_o, a.part_ml, r);
         return;
     }
     const float sum = halves_sum(w.sum);
@@ -553,18 +601,20 @@ __device__ __forceinline__ void each_item(const SharedArgs& a, int share, const 
 __device__ __forceinline__ int64_t part_of(const SharedArgs& a, int share, int g, int tile) { return ((int64_t)share + (int64_t)g * a.tiles + tile) * a.tile_rows; }
 
 template <bool MX, int SETS>
-__global__ __launch_bounds__(256, 2) void attend_shared_kernel(SharedArgs a) {
-    __shared__ __attribute__((aligned(16))) char lds[65536];
-    __shared__ f32x2a ml[4][kTile];
+__global__ __launch_bounds__(SETS > 4 ? 512 : 256, 2) void attend_shared_kernel(SharedArgs a) {
+    constexpr int W = SETS > 4 ? 8 : 4;
+    __shared__ __attribute__((aligned(16))) char lds[W * 16384];
+    __shared__ f32x2a ml[W][kTile];
     const AttendCall& c = a.c;
+    const uint32_t lds_at = lds_address(&lds[0]);
     const int tid = threadIdx.x, col = tid & 31;
     int token;
     if (blockIdx.x < a.tail_blocks) {
         const Tail t = tail_of(a, blockIdx.x);
         const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 256;
         const int64_t from = (t.sequence * c.kv + t.head) * c.stride * 256;
-        few_rows<false, true>(a, lds, ml, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
-                              rows_of_tail(a, t));
+        few_rows<false, true, W>(a, lds, lds_at, ml, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
+                                 rows_of_tail(a, t));
         return;
     }
     // (neighbours in the list are neighbours in an XCD)
@@ -575,8 +625,8 @@ __global__ __launch_bounds__(256, 2) void attend_shared_kernel(SharedArgs a) {
         const Rows r = {part_of(a, share, g, tile) - tile * (SETS * kTile), tile * (SETS * kTile), min(a.rows, (tile + 1) * (SETS * kTile))};
         const int width = MX ? 64 : 256;
         const char *K = (const char*)c.K_kept + k.at * width, *V = (const char*)c.V_kept + k.at * width;
-        if constexpr (SETS > 1) many_rows<MX, SETS>(a, lds, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, row, r);
-        else few_rows<MX, false>(a, lds, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row, r);
+        if constexpr (SETS > 1) many_rows<MX, SETS>(a, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, row, r);
+        else few_rows<MX, false, W>(a, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row, r);
     });
 }
 
@@ -680,7 +730,7 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
             for (int db = 0; db < 4; ++db) w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], x[i], w.o[db], 0, 0, 0);
         }
     }
-    join_waves<4>(w, lds, ml, a.part_o, a.part_ml, r);
+    join_waves<4, 4>(w, lds, ml, a.part_o, a.part_ml, r);
 }
 
 template <bool MX>
@@ -785,12 +835,12 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
     a.scale_log2 = call.scale * (1.f / kLn2);
     a.share = share;
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16, mx = call.K_scales != nullptr;
-    // A slice's partial results, of its kept rows and its tails, have to lie in scratch: whole prefixes, else sequences of one, else tokens of one.  Rows R of a head fill tiles of 128,
-    // up to three times their number where few fill one of 32; a share of a tile more.
+    // A slice's partial results, of its kept rows and its tails, have to lie in scratch: whole prefixes, else sequences of one, else tokens of one.  Rows R of a head fill tiles of
+    // 32 to 256, and a share is a tile more.
     const int64_t room = (call.scratch_bytes - kScratchCounters) / (int64_t)(128 * sizeof(float) + sizeof(f32x2a));
     const int64_t most = room - 1024;
     const auto padded = [&](int64_t prefixes, int64_t sequences, int64_t tokens) {       // partial results of one share, and of the tails
-        const int64_t rows = sequences * tokens * call.group, tile = !bf16 || rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+        const int64_t rows = sequences * tokens * call.group, tile = !bf16 || rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
         return prefixes * call.kv * ((rows + tile - 1) / tile * tile + rows);
     };
     const auto fitting = [&](int64_t of, const auto& size) {       // the most of them that fit
@@ -814,22 +864,23 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 a.t0 = (int)t, a.nt = (int)std::min<int64_t>(tokens, call.m - t);
                 a.rows = a.ns * a.nt * call.group;
                 a.by_per = Divisor(a.nt * call.group);
-                const int sets = !bf16 || a.rows <= kTile ? 1 : a.rows <= 2 * kTile ? 2 : 4;
+                const int sets = !bf16 || a.rows <= kTile ? 1 : a.rows <= 2 * kTile ? 2 : a.rows <= 4 * kTile ? 4 : 8;
                 a.tile_rows = sets * kTile;
                 a.tiles = (a.rows + a.tile_rows - 1) / a.tile_rows;
                 a.tail_tiles = (a.nt * call.group + kTile - 1) / kTile;
                 a.by_tail_tiles = Divisor(a.tail_tiles), a.by_ns = Divisor(a.ns), a.by_quads = Divisor((a.rows + 3) / 4);
                 a.tail_blocks = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
-                // Shares of the kept rows until every unit has two workgroups, SP tiles of 64 keys each at least, as far as there is scratch.
+                // Shares of the kept rows until every unit has eight waves, four tiles of 64 keys each at least (two, up to 64 shares), as far as there is scratch.
                 const int64_t items = (int64_t)a.nb * call.kv * a.tiles, tail_rows = (int64_t)a.nb * call.kv * a.rows;
                 const int64_t tiles = (call.rows / (call.count * call.kv) / 64 + 1) * items;
-                a.shares = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(2 * (int64_t)ctx->num_cu, tiles / SP), (room - 1024 - tail_rows) / a.tile_rows - items));
+                a.shares = (int)std::max<int64_t>(1, std::min(std::min<int64_t>((sets > 4 ? 1 : 2) * (int64_t)ctx->num_cu, std::max(std::min<int64_t>(64, tiles / 2), tiles / 4)), (room - 1024 - tail_rows) / a.tile_rows - items));
                 a.tail_at = (a.shares + items) * a.tile_rows;
                 a.part_o = (float*)((char*)call.scratch + kScratchCounters);
                 a.part_ml = (f32x2a*)(a.part_o + (a.tail_at + tail_rows) * 128);
                 a.part_of_item = (int32_t*)(a.part_ml + a.tail_at + tail_rows);
-                const auto launch = [&](auto kernel) { kernel<<<(unsigned)(a.tail_blocks + a.shares), 256, 0, stream>>>(a); };
+                const auto launch = [&](auto kernel) { kernel<<<(unsigned)(a.tail_blocks + a.shares), sets > 4 ? 512 : 256, 0, stream>>>(a); };
                 if (!bf16) mx ? launch(attend_shared_f32_kernel<true>) : launch(attend_shared_f32_kernel<false>);
+                else if (sets == 8) mx ? launch(attend_shared_kernel<true, 8>) : launch(attend_shared_kernel<false, 8>);
                 else if (sets == 4) mx ? launch(attend_shared_kernel<true, 4>) : launch(attend_shared_kernel<false, 4>);
                 else if (sets == 2) mx ? launch(attend_shared_kernel<true, 2>) : launch(attend_shared_kernel<false, 2>);
                 else mx ? launch(attend_shared_kernel<true, 1>) : launch(attend_shared_kernel<false, 1>);

@@ -4,7 +4,7 @@
 // most 1 (as far as lse is what the scores make it), and a key's sum is its own affair: one wave's, or a few waves' that are added up in order, without atomics.
 //
 // Few rows (weights_few_kernel): S = Q K^T by mfma_f32_16x16x32_bf16 (16x16x4 for fp32), 16 rows R by 16 keys; the rows stay in registers, a wave goes over keys.
-// Many rows (weights_many_kernel): S^T = K Q^T by mfma_f32_32x32x16_bf16 (32x32x2); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves
+// Many rows (weights_many_kernel): S^T = K Q^T by mfma_f32_32x32x16_bf16 (fp32: six products of parts); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves
 // share, and each lane adds up the weights of its own R, key by key, until all rows are through.
 
 #include <algorithm>
@@ -166,12 +166,54 @@ template <> struct Many<true> {
         for (int s = 0; s < 8; ++s) x[s] = ((const u32x4a*)row)[2 * s + half];
     }
 };
+// fp32: a number x is three of 8 bits, x = h + m + l exactly (h its upper half, m what is left rounded to bf16, l the rest, whose last bits end at 2^-133); of the nine products of parts the six
+// that count go through the bf16 units, and what is left out is below 2^-22 of a product.  Infinities and NaN are h alone, and what holds one goes through products of 32 bits.
+struct Parts {                         // of eight channels
+    u32x4a h, m, l;
+};
+__device__ __forceinline__ Parts parts_of(f32x4a x, f32x4a y, bool& odd) {
+    Parts p;
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = i < 2 ? x[2 * i] : y[2 * i - 4], b = i < 2 ? x[2 * i + 1] : y[2 * i - 3];
+        const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+        most = max(most, max(u & 0x7FFFFFFFu, v & 0x7FFFFFFFu));
+        p.h[i] = __builtin_amdgcn_perm(v, u, 0x07060302u);
+        const float r = a - __uint_as_float(u & 0xFFFF0000u), s = b - __uint_as_float(v & 0xFFFF0000u);
+        p.m[i] = pack_bf16(r, s);
+        p.l[i] = pack_bf16(r - __uint_as_float(p.m[i] << 16), s - __uint_as_float(p.m[i] & 0xFFFF0000u));
+    }
+    if (most >= 0x7F800000u) {
+        odd = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t u = __float_as_uint(i < 4 ? x[i] : y[i - 4]), low = i % 2 ? 0xFFFFu : 0xFFFF0000u;       // (low: of the other channel of the pair)
+            if ((u & 0x7F800000u) != 0x7F800000u) continue;
+            const uint32_t h = u & 0x7FFFFFu ? 0x7FC0u : u >> 16;
+            p.h[i / 2] = (p.h[i / 2] & low) | (i % 2 ? h << 16 : h);
+            p.m[i / 2] &= low;
+            p.l[i / 2] &= low;
+        }
+    }
+    return p;
+}
+__device__ __forceinline__ float whole(const Parts& p, int i) {    // channel i again
+    const auto of = [&](uint32_t x) { return __uint_as_float(i % 2 ? x & 0xFFFF0000u : x << 16); };
+    return of(p.h[i / 2]) + (of(p.m[i / 2]) + of(p.l[i / 2]));
+}
 template <> struct Many<false> {
     static constexpr int kBlocks = 1, kTiles = 2, kRow = 512;
-    f32x4a x[16];
+    Parts x[8];
+    bool odd;                          // of any lane's
     __device__ __forceinline__ void load(const char* row, int half) {
+        f32x4a y[16];
 #pragma unroll
-        for (int s = 0; s < 16; ++s) x[s] = ((const f32x4a*)row)[2 * s + half];
+        for (int s = 0; s < 8; ++s) y[2 * s] = ((const f32x4a*)row)[4 * s + 2 * half], y[2 * s + 1] = ((const f32x4a*)row)[4 * s + 2 * half + 1];
+        bool mine = false;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) x[s] = parts_of(y[2 * s], y[2 * s + 1], mine);
+        odd = __any(mine);
     }
 };
 
@@ -240,7 +282,7 @@ __device__ __forceinline__ void spread(float (&x)[N], int lane) {
 
 // Stages from .. to - 1 of a tile of keys; `more`: the same workgroup has written this tile's sums before.
 template <bool BF16>
-__device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[32768], float (*Ls)[Many<BF16>::kTiles * 32], int g, int b, int head, int length, int key_tile, int begin,
+__device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[32768], float (*Ls)[Many<BF16>::kTiles * 32], int* odd, int g, int b, int head, int length, int key_tile, int begin,
                                             int stages, float* part, bool more) {
     typedef Many<BF16> M;
     constexpr int kKeys = M::kBlocks * 32, kTiles = M::kTiles, kStage = kTiles * 32;
@@ -248,40 +290,62 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int j0 = key_tile * (4 * kKeys);
 
-    // Rows on their way into LDS: tiles of 32 rows, in columns of 64 bytes a row, pieces of 16 permuted by (row / 2) % 4.  A wave has eight blocks of 16 rows' columns: of bf16 a
-    // tile's, of fp32 half of a tile's.
-    constexpr int kHalves = BF16 ? 2 : 1, kColumns = M::kRow / 64;
-    const int tile_of = BF16 ? wave : wave >> 1, half_of = BF16 ? 0 : wave & 1, piece = (lane & 3) ^ ((lane >> 3) & 3), my_row = tile_of * 32 + half_of * 16 + (lane >> 2);
+    // Rows on their way into LDS: tiles of 32 rows, in columns of 64 bytes a row, pieces of 16 permuted by (row / 2) % 4.  bf16: a wave has a tile, in eight blocks of 16 rows' columns;
+    // two stages of room.  fp32: a thread has 32 channels of a row, takes them apart and writes a column of each part, parts 16 KB apart; one stage of room, the next one's rows wait
+    // in registers.
+    const int piece = (lane & 3) ^ ((lane >> 3) & 3), my_row = BF16 ? wave * 32 + (lane >> 2) : tid >> 2;
     const uint32_t per_token = c.kv * c.group * M::kRow, over = per_token - c.group * M::kRow;
     const int first_token = a.by_group.of(begin), first_row = first_token * c.group;               // (offsets count from here)
     const int move_tokens = a.by_group.of(kStage), move_heads = a.by_group.rest(kStage, move_tokens);
     const char* queries = (const char*)uniform((int64_t)((const char*)c.Q + ((((int64_t)b * c.m + first_token) * c.kv + head) * c.group) * M::kRow));
-    Walk low(begin - first_row + my_row, a.by_group, per_token, M::kRow), high(begin - first_row + my_row + 16, a.by_group, per_token, M::kRow);       // (bf16: two halves of a tile)
+    Walk low(begin - first_row + my_row, a.by_group, per_token, M::kRow), high(begin - first_row + my_row + 16, a.by_group, per_token, M::kRow);       // (bf16: the tile's halves)
     const float* lse_of_head = (const float*)uniform((int64_t)(c.lse + ((int64_t)b * c.kv + head) * c.group * c.m + first_token));
     Walk less_of(begin - first_row + tid % kStage, a.by_group, 1, c.m);
     float next_less = 0.f;
-    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(&Qs[0][0]) + tile_of * (kColumns * 2048) + half_of * 1024);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(&Qs[0][0]) + wave * 8192);
+    f32x4a raw[BF16 ? 1 : 8];
     const auto ask = [&](int stage) ALWAYS_INLINE {
-        uint32_t at[2] = {low.at + piece * 16, high.at + piece * 16}, l = less_of.at;
+        const uint32_t within = BF16 ? piece * 16 : (tid & 3) * 128;
+        uint32_t at[2] = {low.at + within, high.at + within}, l = less_of.at;
         if (begin + (stage + 1) * kStage > a.rows) {               // (what is behind the last row is not used)
             const int R = begin + stage * kStage;
-            if (R + my_row >= a.rows) at[0] = piece * 16;
-            if (R + my_row + 16 >= a.rows) at[1] = piece * 16;
+            if (R + my_row >= a.rows) at[0] = within;
+            if (R + my_row + 16 >= a.rows) at[1] = within;
             if (R + tid % kStage >= a.rows) l = 0;
         }
-        const uint32_t to = lds + (stage & 1) * 32768;
+        if constexpr (BF16) {
+            const uint32_t to = lds + (stage & 1) * 32768;
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < kColumns; ++i) dma16(to + h * 1024 + i * 2048, queries, at[h] + i * 64);
+                for (int i = 0; i < 4; ++i) dma16(to + h * 1024 + i * 2048, queries, at[h] + i * 64);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i] = *(const f32x4a*)(queries + at[0] + i * 16);
+        }
         next_less = lse_of_head[l];
         low.on(move_heads, move_tokens * per_token + move_heads * M::kRow, over, c.group);
         if (BF16) high.on(move_heads, move_tokens * per_token + move_heads * M::kRow, over, c.group);
         less_of.on(move_heads, move_tokens + move_heads * c.m, 1 - c.group * c.m, c.group);
     };
     const auto arrive = [&](int stage) ALWAYS_INLINE {
+        if constexpr (!BF16) {
+            if (tid == 0) odd[stage & 1] = 0;
+            __syncthreads();                                       // (nobody reads the stage before any more)
+            bool mine = false;
+            char* to = Qs[0] + (my_row >> 5) * 8192 + (tid & 3) * 2048 + (my_row & 31) * 64;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Parts p = parts_of(raw[2 * i], raw[2 * i + 1], mine);
+                const int of = (i ^ ((my_row >> 1) & 3)) << 4;
+                *(u32x4a*)(to + of) = p.h;
+                *(u32x4a*)(to + 16384 + of) = p.m;
+                *(u32x4a*)(to + 32768 + of) = p.l;
+            }
+            if (mine) odd[stage & 1] = 1;
+        }
         if (tid < kStage) Ls[stage & 1][tid] = next_less == -INFINITY ? -INFINITY : -next_less * (1.f / kLn2);     // (a row that sees nothing weighs nothing)
-        dma_wait();
+        if constexpr (BF16) dma_wait();
         __syncthreads();
     };
     __syncthreads();                                               // (nobody reads the tile's before any more)
@@ -321,21 +385,46 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
                 seen &= (near < 0 ? ~0ull : near >= 63 ? 0ull : ~((2ull << near) - 1)) | (first <= 0 ? 0ull : first >= 64 ? ~0ull : (1ull << first) - 1);
             }
             if (!__any(seen != 0)) continue;
-            const char* Qt = Qs[stage & 1] + u * (kColumns * 2048);
+            const char* Qt = Qs[BF16 ? stage & 1 : 0] + u * 8192;
 #pragma unroll
             for (int kb = 0; kb < M::kBlocks; ++kb) {
                 f32x16a x;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = 0.f;
+                if constexpr (BF16) {
 #pragma unroll
-                for (int i = 0; i < M::kRow / 32; ++i) {
-                    const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048);
-                    if constexpr (BF16) {
+                    for (int i = 0; i < 8; ++i) {
+                        const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048);
                         x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, keys[kb].x[i]), __builtin_bit_cast(bf16x8a, q), x, 0, 0, 0);
-                    } else {
-                        const f32x4a y = __builtin_bit_cast(f32x4a, q);
+                    }
+                } else {
+                    Parts q[2];
+                    const auto read = [&](int i) ALWAYS_INLINE {
+                        const char* from = Qt + k_at[i & 1] + (i >> 1) * 2048;
+                        q[i & 1] = {*(const u32x4a*)from, *(const u32x4a*)(from + 16384), *(const u32x4a*)(from + 32768)};
+                    };
+                    read(0);
+                    if (!keys[0].odd && odd[stage & 1] == 0) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(keys[kb].x[i][e], y[e], x, 0, 0, 0);
+                        for (int i = 0; i < 8; ++i) {
+                            if (i < 7) read(i + 1);
+                            const Parts &k = keys[0].x[i], &r = q[i & 1];
+                            const auto add = [&](u32x4a y, u32x4a z) ALWAYS_INLINE {
+                                x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, y), __builtin_bit_cast(bf16x8a, z), x, 0, 0, 0);
+                            };
+                            add(k.l, r.h), add(k.h, r.l), add(k.m, r.m), add(k.m, r.h), add(k.h, r.m), add(k.h, r.h);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (i < 7) read(i + 1);
+                            Parts k = keys[0].x[i];
+                            loaded(k.h), loaded(k.m), loaded(k.l);             // (put together here, not before the loop)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(whole(k, e), whole(q[i & 1], e), x, 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
                     }
                 }
 #pragma unroll
@@ -347,10 +436,11 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
         }
     };
     if (stages > 0) arrive(0);
+    if constexpr (BF16)
 #pragma unroll
-    for (int kb = 0; kb < M::kBlocks; ++kb)
+        for (int kb = 0; kb < M::kBlocks; ++kb)
 #pragma unroll
-        for (int i = 0; i < M::kRow / 32; ++i) loaded(keys[kb].x[i]);
+            for (int i = 0; i < 8; ++i) loaded(keys[kb].x[i]);
     int stage = 0;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {                         // stages with masks, whole ones, some with masks again
@@ -432,13 +522,14 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kTiles * 32;
     __shared__ __attribute__((aligned(16))) char Qs[2][32768];
     __shared__ float Ls[2][kStage];                                // -lse of a stage's rows, in units of log 2
+    __shared__ int odd[2];                                         // (fp32) whether a stage's rows hold an infinity or NaN
     const WeightsCall& c = a.c;
     // Neighbours in a head are neighbours in an XCD, whose caches then hold one head's queries.
     const int at = a.by_groups.of(blockIdx.x), g = a.by_groups.rest(blockIdx.x, at), b = a.by_kv.of(g), head = a.by_kv.rest(g, b), length = length_of(c, b);
     const auto run = [&](int tile, int from, int to, float* part) ALWAYS_INLINE {
         const Span span = rows_that_see(a, length, tile * kKeys, min(tile * kKeys + kKeys, length) - 1, kStage);
         for (int s = from; s == from || s < to; s += a.most)
-            tile_stages<BF16>(a, Qs, Ls, g, b, head, length, tile, span.begin + s * kStage, min(a.most, to - s), part, s > from);
+            tile_stages<BF16>(a, Qs, Ls, odd, g, b, head, length, tile, span.begin + s * kStage, min(a.most, to - s), part, s > from);
     };
     if (a.shares == 0) {
         if (at * kKeys < length) run(at, 0, rows_that_see(a, length, at * kKeys, min(at * kKeys + kKeys, length) - 1, kStage).stages, nullptr);

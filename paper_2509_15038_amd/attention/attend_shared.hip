@@ -101,16 +101,21 @@ struct Wave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
     }
+    // where step i's operand lies in its column, k_at being step 0's
+    template <int STRIDE>
+    static __device__ __forceinline__ int key_at(int k_at, int i) {
+        return k_at ^ ((2 * (i & 1) ^ (STRIDE == 4096 ? i >> 1 : 0)) << 4);
+    }
     // KB blocks of 32 keys, columns STRIDE bytes apart
     template <int KB, int STRIDE>
     __device__ __forceinline__ void scores(const char* Kt, int col, int half, f32x16a (&x)[KB]) const {
-        const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+        const int k_at = col * 64 + ((half ^ ((col >> 1) & 3)) << 4);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[kb] = product(*(const u32x4a*)(Kt + k_at[i & 1] + (i >> 1) * STRIDE + kb * 2048), q[i], x[kb]);
+            for (int i = 0; i < 8; ++i) x[kb] = product(*(const u32x4a*)(Kt + key_at<STRIDE>(k_at, i) + (i >> 1) * STRIDE + kb * 2048), q[i], x[kb]);
         }
     }
     template <int KB>
@@ -142,7 +147,7 @@ struct Wave {
     }
     template <int STRIDE>
     static __device__ __forceinline__ u32x4a value(const char* Vt, int v_at, int u, int db) {
-        const char* p = Vt + v_at + db * STRIDE + u * 1024;
+        const char* p = Vt + (STRIDE == 4096 ? v_at ^ (db << 4) : v_at) + db * STRIDE + u * 1024;
         const u32x2 x = read_transposed(p), y = read_transposed(p + 512);
         return (u32x4a){x.x, x.y, y.x, y.y};
     }
@@ -170,9 +175,13 @@ __device__ __forceinline__ void hide(f32x16a (&s)[KB], int far) {
     for (int i = 0; i < KB * 16; ++i) s[i >> 4][i & 15] = (i >> 4) * 32 + (i & 15) / 4 * 8 + i % 4 <= far ? s[i >> 4][i & 15] : -INFINITY;
 }
 
-// Tiles of 32 or 64 keys in LDS: four columns of 64 bytes a row, K's pieces of 16 bytes permuted by (row / 2) % 4.
+// Tiles of 32 or 64 keys in LDS: four columns of 64 bytes a row, K's pieces of 16 bytes permuted by (row / 2) % 4, and in tiles of 64 keys all by the column: four lanes that store a row
+// in 4 bits have a column each, and would meet the same banks (16 answers over 131072 rows: 78 us without, 68 with).
+__device__ __forceinline__ int permuted(int piece, int row, int column, bool keys, int keys_of_tile) {
+    return piece ^ (keys_of_tile == 64 ? column : 0) ^ (keys ? (row >> 1) & 3 : 0);
+}
 __device__ __forceinline__ uint32_t piece_at(int row, int column, int piece, bool keys, int keys_of_tile) {
-    return column * (keys_of_tile * 64) + row * 64 + ((keys ? piece ^ ((row >> 1) & 3) : piece) << 4);
+    return column * (keys_of_tile * 64) + row * 64 + (permuted(piece, row, column, keys, keys_of_tile) << 4);
 }
 // 1 KB blocks of 16 rows' columns, block first .. first + COUNT - 1 of a tile, straight into LDS.
 template <int KEYS, int COUNT>
@@ -181,8 +190,8 @@ __device__ __forceinline__ void fetch_bf16(uint32_t lds, const char* rows, int c
     lds = __builtin_amdgcn_readfirstlane(lds);
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
-        const int block = first + i, column = block / (KEYS / 16), row = block % (KEYS / 16) * 16 + (lane >> 2), piece = lane & 3;
-        dma16(lds + block * 1024, rows, min(row, count - 1) * 256 + column * 64 + ((keys ? piece ^ ((row >> 1) & 3) : piece) << 4));
+        const int block = first + i, column = block / (KEYS / 16), row = block % (KEYS / 16) * 16 + (lane >> 2);
+        dma16(lds + block * 1024, rows, min(row, count - 1) * 256 + column * 64 + (permuted(lane & 3, row, column, keys, KEYS) << 4));
     }
 }
 // Rows in 4 bits: a lane's share of a tile, 16 or 32 bytes of codes of one row, and its scales.
@@ -357,8 +366,7 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, uint32_
 }
 
 // 32 SETS rows R, 32 a wave, tiles of 64 keys for all; with two sets, a wave has half of a tile's keys.  The next tile's products go with this one's exponentials between them,
-// this one's products with V with the next one's maximum: K is a tile ahead of V.  Rows in 4 bits are asked for three tiles before that (a tile is 9 KB, and 512 workgroups of them are
-// no more than a latency's worth).
+// this one's products with V with the next one's maximum: K is a tile ahead of V.  Rows in 4 bits wait in registers for a tile (two and three tiles were slower: spills).
 template <bool MX, int SETS>
 __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
                                           int begin, int end, const char* row, const Rows& r) {
@@ -376,8 +384,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
                                    wave * (16 / W), lane);
     };
     // 4 bits: a thread's 32 channels of a row of K, and of V (of eight waves, four take K and four V), into registers and from there into LDS
-    constexpr int kAhead = 1;
-    Codes<1> codes[MX ? kAhead : 1][W == 8 ? 1 : 2];
+    Codes<1> codes[W == 8 ? 1 : 2];
     const int my_row = (tid & 255) >> 2, column = tid & 3;
     const auto load = [&](Codes<1>& x, bool keys, int tile) ALWAYS_INLINE {
         const int t = min(tile, tiles - 1);
@@ -387,24 +394,20 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
     const auto store = [&](const Codes<1>& x, bool keys, int tile) ALWAYS_INLINE {
         if (tile < tiles) x.store(lds + (tile & 1) * 16384 + (keys ? 0 : 32768), my_row, column, keys, 64);
     };
-    const auto ask_both = [&](int slot, int tile) ALWAYS_INLINE {  // K of tile + 1, V of tile
-        if constexpr (MX) {
-            if constexpr (W == 8) {
-                load(codes[slot][0], wave < 4, wave < 4 ? tile + 1 : tile);
-            } else {
-                load(codes[slot][0], true, tile + 1);
-                load(codes[slot][1], false, tile);
-            }
+    const auto ask_both = [&](int tile) ALWAYS_INLINE {            // K of tile + 1, V of tile
+        if constexpr (MX && W == 8) {
+            load(codes[0], wave < 4, wave < 4 ? tile + 1 : tile);
+        } else if constexpr (MX) {
+            load(codes[0], true, tile + 1);
+            load(codes[1], false, tile);
         }
     };
-    const auto store_both = [&](int slot, int tile) ALWAYS_INLINE {
-        if constexpr (MX) {
-            if constexpr (W == 8) {
-                store(codes[slot][0], wave < 4, wave < 4 ? tile + 1 : tile);
-            } else {
-                store(codes[slot][0], true, tile + 1);
-                store(codes[slot][1], false, tile);
-            }
+    const auto store_both = [&](int tile) ALWAYS_INLINE {
+        if constexpr (MX && W == 8) {
+            store(codes[0], wave < 4, wave < 4 ? tile + 1 : tile);
+        } else if constexpr (MX) {
+            store(codes[0], true, tile + 1);
+            store(codes[1], false, tile);
         }
     };
     const auto arrive = [&](int values) ALWAYS_INLINE {            // values: the tile whose V is among what comes
@@ -426,11 +429,10 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
         if constexpr (MX) {
             Codes<1> k;
             if (W == 4 || wave < 4) load(k, true, 0);
-#pragma unroll
-            for (int x = 0; x < kAhead; ++x) ask_both(x, x);
+            ask_both(0);
             if (W == 4 || wave < 4) store(k, true, 0);
-            store_both(0, 0);
-            ask_both(0, kAhead);
+            store_both(0);
+            ask_both(1);
         } else {
             fetch(true, 0);
             fetch(false, 0);
@@ -445,9 +447,8 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
         mask(s, 0);
         float top = w.top_of<KB>(s, a.scale_log2);
         __syncthreads();               // (K of tile 0 is read)
-        const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
-        // slot: of what comes with this step, K of tile + 2 and V of tile + 1
-        const auto step = [&](int tile, int slot) ALWAYS_INLINE {
+        const int k_at = col * 64 + ((half ^ ((col >> 1) & 3)) << 4);
+        const auto step = [&](int tile) ALWAYS_INLINE {            // (with it come K of tile + 2 and V of tile + 1)
             if constexpr (!MX) {
                 if (tile + 2 < tiles) fetch(true, tile + 2);
                 fetch(false, tile + 1);
@@ -463,13 +464,13 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
                     for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
                 u32x4a kk[2][KB];
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb) kk[0][kb] = *(const u32x4a*)(Kt + k_at[0] + kb * 2048);
+                for (int kb = 0; kb < KB; ++kb) kk[0][kb] = *(const u32x4a*)(Kt + k_at + kb * 2048);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (i < 7)
 #pragma unroll
-                        for (int kb = 0; kb < KB; ++kb) kk[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + k_at[(i + 1) & 1] + ((i + 1) >> 1) * 4096 + kb * 2048);
+                        for (int kb = 0; kb < KB; ++kb) kk[(i + 1) & 1][kb] = *(const u32x4a*)(Kt + Wave::key_at<4096>(k_at, i + 1) + ((i + 1) >> 1) * 4096 + kb * 2048);
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) next[kb] = product(kk[i & 1][kb], w.q[i], next[kb]);
 #pragma unroll
@@ -501,24 +502,12 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) s[kb] = next[kb];
             }
-            store_both(slot, tile + 1);
-            ask_both(slot, tile + 1 + kAhead);
+            store_both(tile + 1);
+            ask_both(tile + 2);
             arrive(tile + 1);
         };
-        int tile = 0;
-        if constexpr (MX) {
 #pragma unroll 1
-            while (tile < tiles - 1) {
-#pragma unroll
-                for (int x = 1; x <= kAhead; ++x) {
-                    step(tile++, x % kAhead);
-                    if (tile >= tiles - 1) break;
-                }
-            }
-        } else {
-#pragma unroll 1
-            for (; tile < tiles - 1; ++tile) step(tile, 0);
-        }
+        for (int tile = 0; tile < tiles - 1; ++tile) step(tile);
         if (works) {
             w.raise(top);
             uint32_t pb[KB * 8];

@@ -31,7 +31,7 @@ struct SharedArgs {
     int rows, tile_rows, tiles;        // of a prefix's KV head: ns * nt * group, and tiles of tile_rows of them
     int shares;                        // workgroups that share out the kept rows
     int tail_tiles;                    // tiles of 32 of a sequence's nt * group rows
-    int64_t tail_blocks;
+    int64_t tails, tail_blocks;        // a workgroup of 512 threads has two
     // un-normalised partial results of 128 floats a row, and their reference points and sums (sum 0: nothing seen, o not written): of share s and item i, (head, tile), at s + i, which
     // no other pair has, [shares + items][tile_rows], then of the tails [nb * kv][rows]
     float* part_o;
@@ -229,11 +229,11 @@ __device__ __forceinline__ void store_part(const Wave& w, float* to, int half) {
             *(f32x4a*)(to + db * 32 + i * 8 + half * 4) = (f32x4a){w.o[db][4 * i], w.o[db][4 * i + 1], w.o[db][4 * i + 2], w.o[db][4 * i + 3]};
 }
 
-// The parts of W waves, WAVES of them over the same 32 rows R (wave % (W / WAVES) says which), through 16 KB of LDS each.
+// The parts of W waves (threads tid of them), WAVES of them over the same 32 rows R (wave % (W / WAVES) says which), through 16 KB of LDS each.
 template <int WAVES, int W>
-__device__ __forceinline__ void join_waves(Wave& w, char* lds, f32x2a (*ml)[kTile], float* part_o, f32x2a* part_ml, const Rows& r) {
+__device__ __forceinline__ void join_waves(Wave& w, int tid, char* lds, f32x2a (*ml)[kTile], float* part_o, f32x2a* part_ml, const Rows& r) {
     constexpr int kSets = W / WAVES;                               // of 32 rows
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5, set = wave % kSets;
+    const int wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5, set = wave % kSets;
     const float sum = halves_sum(w.sum);
     __syncthreads();                   // (nobody reads tiles any more)
     if (half == 0) ml[wave][col] = (f32x2a){w.ref, sum};
@@ -307,12 +307,12 @@ template <int LEFT>
 __device__ __forceinline__ void dma_wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LEFT) : "memory"); }      // all but the last LEFT
 __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// 32 rows R, each wave over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values while they are.
+// 32 rows R of W waves (threads tid of them), each wave over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values while they are.
 // TAIL: row R's token stands at p.
 template <bool MX, bool TAIL, int W>
-__device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
+__device__ __forceinline__ void few_rows(const SharedArgs& a, int tid, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
                                          int begin, int end, int p, int p_low, const char* row, const Rows& r) {
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
     char *Kt = lds + wave * 16384, *Vt = Kt + 8192;
     const uint32_t k_lds = lds_at + wave * 16384, v_lds = k_lds + 8192;
@@ -362,7 +362,7 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, char* lds, uint32_
         lds_wait();
         if (more) ask_v(tile + W);
     }
-    join_waves<W, W>(w, lds, ml, a.part_o, a.part_ml, r);
+    join_waves<W, W>(w, tid, lds, ml, a.part_o, a.part_ml, r);
 }
 
 // 32 SETS rows R, 32 a wave, tiles of 64 keys for all; with two sets, a wave has half of a tile's keys.  The next tile's products go with this one's exponentials between them,
@@ -517,7 +517,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
         }
     }
     if constexpr (SETS == 2) {
-        join_waves<2, 4>(w, lds, ml, a.part_o, a.part_ml, r);
+        join_waves<2, 4>(w, tid, lds, ml, a.part_o, a.part_ml, r);
         return;
     }
     const float sum = halves_sum(w.sum);
@@ -599,11 +599,15 @@ __global__ __launch_bounds__(SETS > 4 ? 512 : 256, 2) void attend_shared_kernel(
     const int tid = threadIdx.x, col = tid & 31;
     int token;
     if (blockIdx.x < a.tail_blocks) {
-        const Tail t = tail_of(a, blockIdx.x);
+        const int of = W > 4 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;       // (a tail takes four waves; the second of the last two may be none, and writes nothing)
+        const int64_t i = (int64_t)blockIdx.x * (W / 4) + of;
+        const Tail t = tail_of(a, (int)min(i, a.tails - 1));
+        Rows r = rows_of_tail(a, t);
+        if (i >= a.tails) r.end = r.first;
         const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 256;
         const int64_t from = (t.sequence * c.kv + t.head) * c.stride * 256;
-        few_rows<false, true, W>(a, lds, lds_at, ml, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
-                                 rows_of_tail(a, t));
+        few_rows<false, true, 4>(a, tid & 255, lds + of * 65536, lds_at + of * 65536, ml + of * 4, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, t.p_high + 1),
+                                 t.length - c.m + token, t.p_low, row, r);
         return;
     }
     // (neighbours in the list are neighbours in an XCD)
@@ -615,7 +619,7 @@ __global__ __launch_bounds__(SETS > 4 ? 512 : 256, 2) void attend_shared_kernel(
         const int width = MX ? 64 : 256;
         const char *K = (const char*)c.K_kept + k.at * width, *V = (const char*)c.V_kept + k.at * width;
         if constexpr (SETS > 1) many_rows<MX, SETS>(a, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, row, r);
-        else few_rows<MX, false, W>(a, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row, r);
+        else few_rows<MX, false, W>(a, tid, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row, r);
     });
 }
 
@@ -719,7 +723,7 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
             for (int db = 0; db < 4; ++db) w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], x[i], w.o[db], 0, 0, 0);
         }
     }
-    join_waves<4, 4>(w, lds, ml, a.part_o, a.part_ml, r);
+    join_waves<4, 4>(w, tid, lds, ml, a.part_o, a.part_ml, r);
 }
 
 template <bool MX>
@@ -858,7 +862,8 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 a.tiles = (a.rows + a.tile_rows - 1) / a.tile_rows;
                 a.tail_tiles = (a.nt * call.group + kTile - 1) / kTile;
                 a.by_tail_tiles = Divisor(a.tail_tiles), a.by_ns = Divisor(a.ns), a.by_quads = Divisor((a.rows + 3) / 4);
-                a.tail_blocks = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
+                a.tails = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
+                a.tail_blocks = sets > 4 ? (a.tails + 1) / 2 : a.tails;
                 // Shares of the kept rows until every unit has eight waves, four tiles of 64 keys each at least (two, up to 64 shares), as far as there is scratch.
                 const int64_t items = (int64_t)a.nb * call.kv * a.tiles, tail_rows = (int64_t)a.nb * call.kv * a.rows;
                 const int64_t tiles = (call.rows / (call.count * call.kv) / 64 + 1) * items;

@@ -325,3 +325,11 @@ def test_scratch_serves_the_other_attention_calls_in_turn():
     assert torch.equal(a, b)
     # two ways to the same: each within 2^-7 of sum w |v| (its bf16 weights and result), which is below 2 here
     assert float((a.double() - c.double()).abs().max()) <= 2 * 2.0 ** -7 * 2
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("share,kv", [(33, 1), (65, 1), (37, 3)])
+def test_odd_numbers_of_tails_beside_many_rows(mx, share, kv):
+    # (two tails share a workgroup there; one of the last two is none)
+    rng = np.random.default_rng(share)
+    check("bf16", mx, 1, share, kv, 4, 1, rng.integers(1, 400, kv), 70, rng.integers(0, 71, share))

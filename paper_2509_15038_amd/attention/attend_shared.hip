@@ -623,54 +623,95 @@ __global__ __launch_bounds__(SETS > 4 ? 512 : 256, 2) void attend_shared_kernel(
     });
 }
 
-// ---- fp32: a wave's 32 rows R, 32 keys at a time, operands straight from memory; the four waves take tiles in turn and are joined.
-template <bool MX>
-struct Source32 {                      // keys' rows of one head
-    const char *K, *V;
-    const uint8_t *K_scales, *V_scales;
-    // channels of row j that QK's operand has in this half: 4 at step s (0 .. 15)
-    __device__ __forceinline__ f32x4a key(int j, int s, int half) const {
-        if constexpr (MX) {
-            const uint32_t codes = ((const uint16_t*)K)[(int64_t)j * 32 + 2 * s + half];
-            const float unit = unit_of(K_scales[(int64_t)j * 4 + s / 4]);
-            const f32x2a x = two_f32<0>(codes, unit), y = two_f32<1>(codes, unit);
-            return (f32x4a){x.x, x.y, y.x, y.y};
-        } else {
-            return ((const f32x4a*)(K + (int64_t)j * 512))[2 * s + half];
+// ---- fp32: a wave's 32 rows R, 32 keys at a time, operands straight from memory; the four waves take tiles in turn and are joined.  A wave has a unit to itself and 512 registers: a tile's
+// values are on their way while its scores are made, and the next one's keys while the values are used.
+
+// 32 keys' operands: of QK the channels that `key` has at steps 0 .. 15 in either half, `channel` being the first of step 0; of PV channel 32 db + lane % 32 of key i / 4 * 8 + i % 4 + 4 half.
+template <bool MX> struct Operands32;
+template <> struct Operands32<false> {
+    static constexpr int kHalf = 1, kStep = 2;                     // fours of channels from half to half, and from step to step
+    f32x4a k[16];
+    float v[16][4];
+    __device__ __forceinline__ void ask_keys(const char* K, const uint8_t*, int64_t row, int half) {
+#pragma unroll
+        for (int s = 0; s < 16; ++s) k[s] = ((const f32x4a*)(K + row * 512))[2 * s + half];
+    }
+    __device__ __forceinline__ void ask_values(const char* V, const uint8_t*, int64_t row, int i, int col) {
+#pragma unroll
+        for (int db = 0; db < 4; ++db) v[i][db] = ((const float*)(V + row * 512))[db * 32 + col];
+    }
+    // channels channel .. channel + 3 of a row of V
+    static __device__ __forceinline__ f32x4a four(const char* V, const uint8_t*, int64_t row, int channel) { return *(const f32x4a*)((const float*)(V + row * 512) + channel); }
+    __device__ __forceinline__ f32x4a key(int s) const { return k[s]; }
+    __device__ __forceinline__ float value(int i, int db, int) const { return v[i][db]; }
+};
+template <> struct Operands32<true> {
+    typedef uint32_t u32u __attribute__((aligned(1)));
+    static constexpr int kHalf = 16, kStep = 1;
+    u32x4a k[2];
+    uint32_t k_scale[2], v_scale[16];
+    uint8_t v[16][4];
+    __device__ __forceinline__ void ask_keys(const char* K, const uint8_t* scales, int64_t row, int half) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            k[x] = ((const u32x4a*)(K + row * 64))[half * 2 + x];
+            k_scale[x] = scales[row * 4 + half * 2 + x];
         }
     }
-    __device__ __forceinline__ float value(int j, int channel) const {
-        if constexpr (MX) {
-            const uint32_t codes = ((const uint8_t*)V)[(int64_t)j * 64 + channel / 2];
-            const f32x2a x = two_f32<0>(codes, unit_of(V_scales[(int64_t)j * 4 + channel / 32]));
-            return channel & 1 ? x.y : x.x;
-        } else {
-            return ((const float*)(V + (int64_t)j * 512))[channel];
-        }
+    __device__ __forceinline__ void ask_values(const char* V, const uint8_t* scales, int64_t row, int i, int col) {
+        v_scale[i] = *(const u32u*)(scales + row * 4);
+#pragma unroll
+        for (int db = 0; db < 4; ++db) v[i][db] = ((const uint8_t*)V)[row * 64 + db * 16 + col / 2];
+    }
+    static __device__ __forceinline__ f32x4a four(const char* V, const uint8_t* scales, int64_t row, int channel) {
+        const uint32_t codes = *(const uint16_t*)(V + row * 64 + channel / 2);
+        const float unit = unit_of(scales[row * 4 + channel / 32]);
+        const f32x2a x = two_f32<0>(codes, unit), y = two_f32<1>(codes, unit);
+        return (f32x4a){x.x, x.y, y.x, y.y};
+    }
+    __device__ __forceinline__ f32x4a key(int s) const {
+        const uint32_t codes = k[s >> 3][s >> 1 & 3];
+        const float unit = unit_of(k_scale[s >> 3]);
+        const f32x2a x = s & 1 ? two_f32<2>(codes, unit) : two_f32<0>(codes, unit), y = s & 1 ? two_f32<3>(codes, unit) : two_f32<1>(codes, unit);
+        return (f32x4a){x.x, x.y, y.x, y.y};
+    }
+    __device__ __forceinline__ float value(int i, int db, int col) const {
+        const f32x2a x = two_f32<0>(v[i][db], unit_of(v_scale[i] >> (8 * db) & 0xFF));
+        return col & 1 ? x.y : x.x;
     }
 };
 
 template <bool MX, bool TAIL>
-__device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const Source32<MX>& from, int begin, int end, int p, int p_low,
-                                         const char* row, const Rows& r) {
+__device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const char* K, const char* V, const uint8_t* K_scales, const uint8_t* V_scales, int begin, int end,
+                                         int p, int p_low, const char* row, const Rows& r) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    typedef Operands32<MX> Operands;
+    Operands from;
     f32x4a q[16];
     Wave w;                            // (its o, ref and sum)
+    const int tiles = (end - begin + 31) / 32;
+    const auto ask_keys = [&](int tile) ALWAYS_INLINE { from.ask_keys(K, K_scales, min(begin + tile * 32 + col, end - 1), half); };
+    if (wave < tiles) ask_keys(wave);
     w.begin(row, half);
 #pragma unroll
-    for (int s = 0; s < 16; ++s) q[s] = ((const f32x4a*)row)[2 * s + half];
-    const int tiles = (end - begin + 31) / 32;
+    for (int s = 0; s < 16; ++s) q[s] = ((const f32x4a*)row)[Operands::kStep * s + Operands::kHalf * half];
+#pragma unroll 1
     for (int tile = wave; tile < tiles; tile += 4) {
         const int j0 = begin + tile * 32, count = min(32, end - j0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) from.ask_values(V, V_scales, j0 + min(i / 4 * 8 + i % 4 + half * 4, count - 1), i, col);
+        __builtin_amdgcn_sched_barrier(0);
         f32x16a x;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = 0.f;
 #pragma unroll
         for (int s = 0; s < 16; ++s) {
-            const f32x4a k = from.key(j0 + min(col, count - 1), s, half);
+            const f32x4a k = from.key(s);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[s][e], x, 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (tile + 4 < tiles) ask_keys(tile + 4);
         const bool hidden = count < 32 || (TAIL && j0 + 31 > p_low);
         const int last = TAIL ? min(p, end - 1) : end - 1;
         if (hidden)
@@ -692,36 +733,36 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
             x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, -w.ref));
             w.sum += x[i];
         }
+        const auto odd = [](float y) ALWAYS_INLINE { return (__float_as_uint(y) & 0x7F800000u) == 0x7F800000u; };
+        if (!hidden) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int key = i / 4 * 8 + i % 4 + half * 4;  // of this half
-            float v[4];
-            bool bad = false;
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int db = 0; db < 4; ++db) w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(from.value(i, db, col), x[i], w.o[db], 0, 0, 0);
+            continue;
+        }
+        // An infinity or NaN goes to the rows that see its key, whatever the weight, and meets no other's.
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
-                v[db] = key < count ? from.value(j0 + min(key, count - 1), db * 32 + col) : 0.f;
-                bad |= (__float_as_uint(v[db]) & 0x7F800000u) == 0x7F800000u;
+                const float y = from.value(i, db, col), z = i / 4 * 8 + i % 4 + half * 4 < count ? y : 0.f;
+                bad |= odd(z);
+                w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(odd(z) ? 0.f : z, x[i], w.o[db], 0, 0, 0);
             }
-            if (hidden && __any(bad)) {
-                // Such a value goes to the rows that see its key, whatever the weight: column R is lane % 32, and the value of channel 32 db + n is lane n's of the key's half.
+        if (__any(bad))
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    const bool sees_it = j0 + i / 4 * 8 + i % 4 + h * 4 <= last;
-#pragma unroll
-                    for (int db = 0; db < 4; ++db)
-#pragma unroll
-                        for (int n = 0; n < 16; ++n) {
-                            const float y = __shfl(v[db], h * 32 + n / 4 * 8 + n % 4 + half * 4);
-                            if ((__float_as_uint(y) & 0x7F800000u) == 0x7F800000u && sees_it) w.o[db][n] += y;
-                        }
-                }
+            for (int key = 0; key < count; ++key)
 #pragma unroll
                 for (int db = 0; db < 4; ++db)
-                    if ((__float_as_uint(v[db]) & 0x7F800000u) == 0x7F800000u) v[db] = 0.f;
-            }
 #pragma unroll
-            for (int db = 0; db < 4; ++db) w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], x[i], w.o[db], 0, 0, 0);
-        }
+                    for (int n = 0; n < 16; n += 4) {
+                        const f32x4a y = Operands::four(V, V_scales, j0 + key, db * 32 + n * 2 + half * 4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (j0 + key <= last && odd(y[e])) w.o[db][n + e] += y[e];
+                    }
     }
     join_waves<4, 4>(w, tid, lds, ml, a.part_o, a.part_ml, r);
 }
@@ -737,7 +778,7 @@ __global__ __launch_bounds__(256) void attend_shared_f32_kernel(SharedArgs a) {
         const Tail t = tail_of(a, blockIdx.x);
         const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 512;
         const int64_t at = (t.sequence * c.kv + t.head) * c.stride * 512;
-        rows_f32<false, true>(a, lds, ml, Source32<false>{(const char*)c.K + at, (const char*)c.V + at, nullptr, nullptr}, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
+        rows_f32<false, true>(a, lds, ml, (const char*)c.K + at, (const char*)c.V + at, nullptr, nullptr, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
                               rows_of_tail(a, t));
         return;
     }
@@ -745,8 +786,8 @@ __global__ __launch_bounds__(256) void attend_shared_f32_kernel(SharedArgs a) {
     each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
         const char* row = (const char*)c.Q + query_row(a, a.by_kv.of(g), a.by_kv.rest(g, a.by_kv.of(g)), min(tile * kTile + col, a.rows - 1), &token) * 512;
         const int width = MX ? 64 : 512;
-        const Source32<MX> from = {(const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4};
-        rows_f32<MX, false>(a, lds, ml, from, begin, end, 0, 0, row, {part_of(a, share, g, tile) - tile * kTile, tile * kTile, min(a.rows, (tile + 1) * kTile)});
+        rows_f32<MX, false>(a, lds, ml, (const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row,
+                            {part_of(a, share, g, tile) - tile * kTile, tile * kTile, min(a.rows, (tile + 1) * kTile)});
     });
 }
 

@@ -905,10 +905,11 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 a.by_tail_tiles = Divisor(a.tail_tiles), a.by_ns = Divisor(a.ns), a.by_quads = Divisor((a.rows + 3) / 4);
                 a.tails = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
                 a.tail_blocks = sets > 4 ? (a.tails + 1) / 2 : a.tails;
-                // Shares of the kept rows until every unit has eight waves, four tiles of 64 keys each at least (two, up to 64 shares), as far as there is scratch.
+                // Shares of the kept rows until every unit has eight waves (fp32: four, whose registers fill it: 16 answers over 13107 rows 66 us with twice as many, 53 so), four tiles of 64
+                // keys each at least (two, up to 64 shares), as far as there is scratch.
                 const int64_t items = (int64_t)a.nb * call.kv * a.tiles, tail_rows = (int64_t)a.nb * call.kv * a.rows;
                 const int64_t tiles = (call.rows / (call.count * call.kv) / 64 + 1) * items;
-                a.shares = (int)std::max<int64_t>(1, std::min(std::min<int64_t>((sets > 4 ? 1 : 2) * (int64_t)ctx->num_cu, std::max(std::min<int64_t>(64, tiles / 2), tiles / 4)), (room - 1024 - tail_rows) / a.tile_rows - items));
+                a.shares = (int)std::max<int64_t>(1, std::min(std::min<int64_t>((sets > 4 || !bf16 ? 1 : 2) * (int64_t)ctx->num_cu, std::max(std::min<int64_t>(64, tiles / 2), tiles / 4)), (room - 1024 - tail_rows) / a.tile_rows - items));
                 a.tail_at = (a.shares + items) * a.tile_rows;
                 a.part_o = (float*)((char*)call.scratch + kScratchCounters);
                 a.part_ml = (f32x2a*)(a.part_o + (a.tail_at + tail_rows) * 128);

@@ -3,12 +3,15 @@
 // sequences (R = (sequence, token, head)) stand side by side over its kept rows, which are read once for a tile of up to 256 of them, each
 // sequence's own over its tail, and a second kernel joins what they found.
 //
-// One launch: workgroups of tails (a sequence's KV head, 32 rows R), then those of kept rows, which share out all heads' tiles evenly, whatever the heads' lengths.
-// S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a row, V read transposed, P from
-// the registers that S^T leaves it in.  With 256 (128) rows eight (four) waves have 32 each and all of a tile's 64 keys, with 64 rows 32 each and half of the keys; with 32 rows each wave has
-// tiles of 32 keys of its own; waves of the same rows are joined in LDS.  Rows in 4 bits are expanded on their way into LDS, exactly.
-// fp32: mfma_f32_32x32x2, operands straight from memory.
-
+// One launch: workgroups of tails (a sequence's KV head, 32 rows R, by four waves that take tiles of 32 keys in turn and are joined in LDS), then those of kept rows, which share out all heads'
+// tiles evenly, whatever the heads' lengths.  S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a
+// row, V read transposed, P from the registers that S^T leaves it in.  Four (eight) waves have 32 of 128 (256) rows each and all of a tile's 64 keys.  Rows in 4 bits are expanded on their way
+// into LDS, exactly.  fp32: mfma_f32_32x32x2, operands straight from memory.
+// Weights are rounded to bf16 for their product with V (half a step of 2^-8, as the values themselves have been); sums are of what was not rounded.
+//
+// Bound by: over long prefixes the products, whose power lowers the clock (64 sequences over 131072 kept rows of 8 heads, 137 GFLOP, 177 us: 780 TFLOP/s; 557 MB); in 4 bits the expansion,
+// which every 128 rows take anew (4 prompts of 13107 kept rows and 64 answers with 513 tokens each, 124 MB, 59 us, of which the tails' 83 MB 13 us); over short ones the chain of two
+// launches, a few tiles and the join (16 answers over 3276 rows, 21 MB, 19 us).  fp32: 16 answers over 13107 rows 53 us, of which the products of 32 bits 25.
 #include <algorithm>
 
 #include "attend_device.h"
@@ -229,18 +232,14 @@ __device__ __forceinline__ void store_part(const Wave& w, float* to, int half) {
             *(f32x4a*)(to + db * 32 + i * 8 + half * 4) = (f32x4a){w.o[db][4 * i], w.o[db][4 * i + 1], w.o[db][4 * i + 2], w.o[db][4 * i + 3]};
 }
 
-// The parts of W waves (threads tid of them), WAVES of them over the same 32 rows R (wave % (W / WAVES) says which), through 16 KB of LDS each.
-template <int WAVES, int W>
+// The parts of four waves (threads tid of them) over the same 32 rows R, through 16 KB of LDS each.
 __device__ __forceinline__ void join_waves(Wave& w, int tid, char* lds, f32x2a (*ml)[kTile], float* part_o, f32x2a* part_ml, const Rows& r) {
-    constexpr int kSets = W / WAVES;                               // of 32 rows
-    const int wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5, set = wave % kSets;
+    const int wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const float sum = halves_sum(w.sum);
     __syncthreads();                   // (nobody reads tiles any more)
     if (half == 0) ml[wave][col] = (f32x2a){w.ref, sum};
     __syncthreads();
-    float ref = ml[set][col].x;
-#pragma unroll
-    for (int k = 1; k < WAVES; ++k) ref = fmaxf(ref, ml[set + k * kSets][col].x);
+    const float ref = fmaxf(fmaxf(ml[0][col].x, ml[1][col].x), fmaxf(ml[2][col].x, ml[3][col].x));
     // (16-byte pieces permuted by the row, so that the rows of a store meet different banks)
     const float scale = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.ref - ref);
     float* to = (float*)lds + (wave * kTile + col) * 128;
@@ -251,25 +250,21 @@ __device__ __forceinline__ void join_waves(Wave& w, int tid, char* lds, f32x2a (
             *(f32x4a*)(to + ((db * 8 + i * 2 + half) ^ (col & 7)) * 4) =
                 (f32x4a){w.o[db][4 * i] * scale, w.o[db][4 * i + 1] * scale, w.o[db][4 * i + 2] * scale, w.o[db][4 * i + 3] * scale};
     __syncthreads();
+    const int row = tid >> 3, R = r.first + row;
+    if (R >= r.end) return;
+    const float m = fmaxf(fmaxf(ml[0][row].x, ml[1][row].x), fmaxf(ml[2][row].x, ml[3][row].x));
+    float l = 0.f;
 #pragma unroll
-    for (int s = 0; s < kSets; ++s) {
-        const int row = tid >> 3, R = r.first + s * kTile + row;
-        if (row >= kTile || R >= r.end) continue;
-        float m = ml[s][row].x, l = 0.f;
+    for (int k = 0; k < 4; ++k) l += ml[k][row].y == 0.f ? 0.f : ml[k][row].y * __builtin_amdgcn_exp2f(ml[k][row].x - m);
+    if ((tid & 7) == 0) part_ml[r.at + R] = (f32x2a){m, l};
+    if (l == 0.f) return;
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k) m = fmaxf(m, ml[s + k * kSets][row].x);
+    for (int p = 0; p < 4; ++p) {
+        const int piece = (tid & 7) + p * 8;
+        f32x4a x = {0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) l += ml[s + k * kSets][row].y == 0.f ? 0.f : ml[s + k * kSets][row].y * __builtin_amdgcn_exp2f(ml[s + k * kSets][row].x - m);
-        if ((tid & 7) == 0) part_ml[r.at + R] = (f32x2a){m, l};
-        if (l == 0.f) continue;
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const int piece = (tid & 7) + p * 8;
-            f32x4a x = {0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < WAVES; ++k) x += *(const f32x4a*)((const float*)lds + ((s + k * kSets) * kTile + row) * 128 + (piece ^ (row & 7)) * 4);
-            *(f32x4a*)(part_o + (r.at + R) * 128 + piece * 4) = x;
-        }
+        for (int k = 0; k < 4; ++k) x += *(const f32x4a*)((const float*)lds + (k * kTile + row) * 128 + (piece ^ (row & 7)) * 4);
+        *(f32x4a*)(part_o + (r.at + R) * 128 + piece * 4) = x;
     }
 }
 
@@ -307,29 +302,19 @@ template <int LEFT>
 __device__ __forceinline__ void dma_wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LEFT) : "memory"); }      // all but the last LEFT
 __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// 32 rows R of W waves (threads tid of them), each wave over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values while they are.
-// TAIL: row R's token stands at p.
-template <bool MX, bool TAIL, int W>
-__device__ __forceinline__ void few_rows(const SharedArgs& a, int tid, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
-                                         int begin, int end, int p, int p_low, const char* row, const Rows& r) {
+// A tail's 32 rows R, by four waves (threads tid of them), each over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values
+// while they are.  Row R's token stands at p, the first row's at p_low.
+__device__ __forceinline__ void tail_rows(const SharedArgs& a, int tid, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const char* K, const char* V, int end, int p, int p_low,
+                                          const char* row, const Rows& r) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
     char *Kt = lds + wave * 16384, *Vt = Kt + 8192;
     const uint32_t k_lds = lds_at + wave * 16384, v_lds = k_lds + 8192;
     Wave w;
-    const int tiles = (end - begin + 31) / 32;
-    Codes<2> k, v;
-    const auto key_of = [&](int tile) ALWAYS_INLINE { return begin + tile * 32; };
-    const auto count_of = [&](int tile) ALWAYS_INLINE { return min(32, end - key_of(tile)); };
-    const auto ask_k = [&](int tile) ALWAYS_INLINE {
-        if constexpr (MX) k.load((const uint8_t*)K, K_scales, key_of(tile) + min(lane >> 1, count_of(tile) - 1), (lane & 1) * 2);
-        else fetch_bf16<32, 8>(k_lds, (const char*)K + (int64_t)key_of(tile) * 256, count_of(tile), true, 0, lane);
-    };
-    const auto ask_v = [&](int tile) ALWAYS_INLINE {
-        if constexpr (MX) v.load((const uint8_t*)V, V_scales, key_of(tile) + min(lane >> 1, count_of(tile) - 1), (lane & 1) * 2);
-        else fetch_bf16<32, 8>(v_lds, (const char*)V + (int64_t)key_of(tile) * 256, count_of(tile), false, 0, lane);
-    };
-    __syncthreads();                   // (nobody reads the item's before any more)
+    const int tiles = (end + 31) / 32, last = min(p, end - 1);
+    const auto count_of = [&](int tile) ALWAYS_INLINE { return min(32, end - tile * 32); };
+    const auto ask_k = [&](int tile) ALWAYS_INLINE { fetch_bf16<32, 8>(k_lds, K + (int64_t)tile * 8192, count_of(tile), true, 0, lane); };
+    const auto ask_v = [&](int tile) ALWAYS_INLINE { fetch_bf16<32, 8>(v_lds, V + (int64_t)tile * 8192, count_of(tile), false, 0, lane); };
     if (wave < tiles) {
         ask_k(wave);
         ask_v(wave);
@@ -337,43 +322,39 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, int tid, char* lds
     w.begin(row, half);
 #pragma unroll
     for (int i = 0; i < 8; ++i) loaded(w.q[i]);
-    for (int tile = wave; tile < tiles; tile += W) {
-        const int j0 = key_of(tile), count = count_of(tile), last = TAIL ? min(p, end - 1) : end - 1;
-        const bool more = tile + W < tiles, hidden = count < 32 || (TAIL && j0 + 31 > p_low);
-        if constexpr (MX) k.store(Kt, lane >> 1, (lane & 1) * 2, true, 32);
-        else dma_wait_but<8>();
+    for (int tile = wave; tile < tiles; tile += 4) {
+        const int j0 = tile * 32, count = count_of(tile);
+        const bool more = tile + 4 < tiles, hidden = count < 32 || j0 + 31 > p_low;
+        dma_wait_but<8>();
         f32x16a s[1];
         uint32_t pb[8];
         w.scores<1, 2048>(Kt, col, half, s);
-        if constexpr (MX) v.store(Vt, lane >> 1, (lane & 1) * 2, false, 32);
         lds_wait();
-        if (more) ask_k(tile + W);
+        if (more) ask_k(tile + 4);
         if (hidden) hide<1>(s, last - j0 - half * 4);
         w.raise(w.top_of<1>(s, a.scale_log2));
 #pragma unroll
         for (int i = 0; i < 16; i += 2) pb[i / 2] = w.weigh<1>(s, i, a.scale_log2);
-        if constexpr (!MX) {
-            if (more) dma_wait_but<8>();
-            else dma_wait();
-        }
+        if (more) dma_wait_but<8>();
+        else dma_wait();
         if (count < 32) clear_beyond<32, 64>(Vt, count, lane);
         if (hidden) hidden_values(w, Vt, v_at, pb, last - j0 - half * 4, half, lane);
         else w.values<1, 2048, true>(Vt, v_at, pb);
         lds_wait();
-        if (more) ask_v(tile + W);
+        if (more) ask_v(tile + 4);
     }
-    join_waves<W, W>(w, tid, lds, ml, a.part_o, a.part_ml, r);
+    join_waves(w, tid, lds, ml, a.part_o, a.part_ml, r);
 }
 
-// 32 SETS rows R, 32 a wave, tiles of 64 keys for all; with two sets, a wave has half of a tile's keys.  The next tile's products go with this one's exponentials between them,
+// 32 SETS rows R, 32 a wave, tiles of 64 keys for all.  The next tile's products go with this one's exponentials between them,
 // this one's products with V with the next one's maximum: K is a tile ahead of V.  Rows in 4 bits wait in registers for a tile (two and three tiles were slower: spills).
 template <bool MX, int SETS>
-__device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
+__device__ __forceinline__ void kept_rows_of(const SharedArgs& a, char* lds, uint32_t lds_at, const void* K, const void* V, const uint8_t* K_scales, const uint8_t* V_scales,
                                           int begin, int end, const char* row, const Rows& r) {
-    constexpr int KB = SETS > 2 ? 2 : 1, W = SETS > 4 ? 8 : 4;     // blocks of 32 keys a wave; waves
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15, part = wave / SETS;
+    constexpr int KB = 2, W = SETS;                                // blocks of 32 keys; waves
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int v_at = (4 * half + l16 / 4) * 64 + (lane >> 4 & 1) * 32 + (l16 & 3) * 8;
-    const bool works = r.first + wave % SETS * kTile < r.end;      // (a wave without rows helps with the tiles)
+    const bool works = r.first + wave * kTile < r.end;      // (a wave without rows helps with the tiles)
     Wave w;
     const int tiles = (end - begin + 63) / 64;
     const auto count_of = [&](int tile) ALWAYS_INLINE { return min(64, end - begin - tile * 64); };
@@ -418,10 +399,10 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
         }
         __syncthreads();
     };
-    const auto keys_of = [&](int tile) ALWAYS_INLINE { return lds + (tile & 1) * 16384 + part * 2048; };
-    const auto values_of = [&](int tile) ALWAYS_INLINE { return lds + (tile & 1) * 16384 + 32768 + part * 2048; };
+    const auto keys_of = [&](int tile) ALWAYS_INLINE { return lds + (tile & 1) * 16384; };
+    const auto values_of = [&](int tile) ALWAYS_INLINE { return lds + (tile & 1) * 16384 + 32768; };
     const auto mask = [&](f32x16a (&s)[KB], int tile) ALWAYS_INLINE {
-        if (count_of(tile) < 64) hide<KB>(s, count_of(tile) - 1 - part * 32 - half * 4);
+        if (count_of(tile) < 64) hide<KB>(s, count_of(tile) - 1 - half * 4);
     };
     __syncthreads();                   // (nobody reads the item's before any more)
     // (begin < end)
@@ -477,7 +458,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
                     for (int j = 0; j < 2 * KB; j += 2) pb[(i * 2 * KB + j) / 2] = w.weigh<KB>(s, i * 2 * KB + j, a.scale_log2);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                u32x4a vv[KB][4];                                  // (KB of 1: two steps, no more registers for them)
+                u32x4a vv[2][4];
 #pragma unroll
                 for (int db = 0; db < 4; ++db) vv[0][db] = Wave::value<4096>(Vt, v_at, 0, db);
                 if (tile + 2 == tiles) mask(next, tile + 1);
@@ -485,15 +466,12 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int u = 0; u < 2 * KB; ++u) {
-                    if (KB > 1 && u < 2 * KB - 1)
+                    if (u < 2 * KB - 1)
 #pragma unroll
-                        for (int db = 0; db < 4; ++db) vv[(u + 1) % KB][db] = Wave::value<4096>(Vt, v_at, u + 1, db);
-                    if (KB == 1 && u > 0)
-#pragma unroll
-                        for (int db = 0; db < 4; ++db) vv[0][db] = Wave::value<4096>(Vt, v_at, u, db);
+                        for (int db = 0; db < 4; ++db) vv[(u + 1) & 1][db] = Wave::value<4096>(Vt, v_at, u + 1, db);
                     const u32x4a pu = {pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]};
 #pragma unroll
-                    for (int db = 0; db < 4; ++db) w.o[db] = product(vv[u % KB][db], pu, w.o[db]);
+                    for (int db = 0; db < 4; ++db) w.o[db] = product(vv[u & 1][db], pu, w.o[db]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) most = fmaxf(most, next[u >> 1][(u & 1) * 8 + i]);
                     __builtin_amdgcn_sched_barrier(0);
@@ -515,10 +493,6 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, char* lds, uint32
             for (int i = 0; i < KB * 16; i += 2) pb[i / 2] = w.weigh<KB>(s, i, a.scale_log2);
             w.values<KB, 4096, true>(values_of(tiles - 1), v_at, pb);
         }
-    }
-    if constexpr (SETS == 2) {
-        join_waves<2, 4>(w, tid, lds, ml, a.part_o, a.part_ml, r);
-        return;
     }
     const float sum = halves_sum(w.sum);
     const int R = r.first + wave * 32 + col;
@@ -590,36 +564,34 @@ __device__ __forceinline__ void each_item(const SharedArgs& a, int share, const 
 __device__ __forceinline__ int64_t part_of(const SharedArgs& a, int share, int g, int tile) { return ((int64_t)share + (int64_t)g * a.tiles + tile) * a.tile_rows; }
 
 template <bool MX, int SETS>
-__global__ __launch_bounds__(SETS > 4 ? 512 : 256, 2) void attend_shared_kernel(SharedArgs a) {
-    constexpr int W = SETS > 4 ? 8 : 4;
-    __shared__ __attribute__((aligned(16))) char lds[W * 16384];
-    __shared__ f32x2a ml[W][kTile];
+__global__ __launch_bounds__(SETS * 64, 2) void attend_shared_kernel(SharedArgs a) {
+    __shared__ __attribute__((aligned(16))) char lds[SETS * 16384];
+    __shared__ f32x2a ml[SETS][kTile];
     const AttendCall& c = a.c;
     const uint32_t lds_at = lds_address(&lds[0]);
     const int tid = threadIdx.x, col = tid & 31;
     int token;
     if (blockIdx.x < a.tail_blocks) {
-        const int of = W > 4 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;       // (a tail takes four waves; the second of the last two may be none, and writes nothing)
-        const int64_t i = (int64_t)blockIdx.x * (W / 4) + of;
+        const int of = SETS > 4 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;       // (a tail takes four waves; the second of the last two may be none, and writes nothing)
+        const int64_t i = (int64_t)blockIdx.x * (SETS / 4) + of;
         const Tail t = tail_of(a, (int)min(i, a.tails - 1));
         Rows r = rows_of_tail(a, t);
         if (i >= a.tails) r.end = r.first;
         const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 256;
         const int64_t from = (t.sequence * c.kv + t.head) * c.stride * 256;
-        few_rows<false, true, 4>(a, tid & 255, lds + of * 65536, lds_at + of * 65536, ml + of * 4, (const char*)c.K + from, (const char*)c.V + from, nullptr, nullptr, 0, max(0, t.p_high + 1),
-                                 t.length - c.m + token, t.p_low, row, r);
+        tail_rows(a, tid & 255, lds + of * 65536, lds_at + of * 65536, ml + of * 4, (const char*)c.K + from, (const char*)c.V + from, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
+                  r);
         return;
     }
     // (neighbours in the list are neighbours in an XCD)
     const int block = (int)(blockIdx.x - a.tail_blocks), eighth = a.shares >> 3, share = block < eighth * 8 ? (block & 7) * eighth + (block >> 3) : block;
     each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
-        const int bi = a.by_kv.of(g), head = a.by_kv.rest(g, bi), R = min(tile * (SETS * kTile) + (tid >> 6) % SETS * 32 + col, a.rows - 1);
+        const int bi = a.by_kv.of(g), head = a.by_kv.rest(g, bi), R = min(tile * (SETS * kTile) + (tid >> 6) * kTile + col, a.rows - 1);
         const char* row = (const char*)c.Q + query_row(a, bi, head, R, &token) * 256;
         const Rows r = {part_of(a, share, g, tile) - tile * (SETS * kTile), tile * (SETS * kTile), min(a.rows, (tile + 1) * (SETS * kTile))};
         const int width = MX ? 64 : 256;
         const char *K = (const char*)c.K_kept + k.at * width, *V = (const char*)c.V_kept + k.at * width;
-        if constexpr (SETS > 1) many_rows<MX, SETS>(a, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, row, r);
-        else few_rows<MX, false, W>(a, tid, lds, lds_at, ml, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row, r);
+        kept_rows_of<MX, SETS>(a, lds, lds_at, K, V, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, row, r);
     });
 }
 
@@ -764,7 +736,7 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
                             if (j0 + key <= last && odd(y[e])) w.o[db][n + e] += y[e];
                     }
     }
-    join_waves<4, 4>(w, tid, lds, ml, a.part_o, a.part_ml, r);
+    join_waves(w, tid, lds, ml, a.part_o, a.part_ml, r);
 }
 
 template <bool MX>
@@ -874,7 +846,7 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
     const int64_t room = (call.scratch_bytes - kScratchCounters) / (int64_t)(128 * sizeof(float) + sizeof(f32x2a));
     const int64_t most = room - 1024;
     const auto padded = [&](int64_t prefixes, int64_t sequences, int64_t tokens) {       // partial results of one share, and of the tails
-        const int64_t rows = sequences * tokens * call.group, tile = !bf16 || rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+        const int64_t rows = sequences * tokens * call.group, tile = !bf16 ? 32 : rows <= 128 ? 128 : 256;
         return prefixes * call.kv * ((rows + tile - 1) / tile * tile + rows);
     };
     const auto fitting = [&](int64_t of, const auto& size) {       // the most of them that fit
@@ -898,18 +870,23 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 a.t0 = (int)t, a.nt = (int)std::min<int64_t>(tokens, call.m - t);
                 a.rows = a.ns * a.nt * call.group;
                 a.by_per = Divisor(a.nt * call.group);
-                const int sets = !bf16 || a.rows <= kTile ? 1 : a.rows <= 2 * kTile ? 2 : a.rows <= 4 * kTile ? 4 : 8;
+                // Tiles of 256 rows, whose kept rows are read half as often, where there are twelve tiles of keys for every unit (64 answers: over 13107 rows 44 us so and 38 by 128, over 32768
+                // 66 and 72, over 131072 177 and 197); of 128 also where there are fewer rows (16 answers over 13107: 28.3 us by 64, 26.7 so; 8 answers: 27.1 by 32, 22.5 so).
+                const int64_t tiles_a_head = call.rows / (call.count * call.kv) / 64 + 1, heads = (int64_t)a.nb * call.kv;
+                const int sets = !bf16 ? 1 : a.rows <= 128 || tiles_a_head * heads * ((a.rows + 255) / 256) < 12 * (int64_t)ctx->num_cu ? 4 : 8;
                 a.tile_rows = sets * kTile;
                 a.tiles = (a.rows + a.tile_rows - 1) / a.tile_rows;
                 a.tail_tiles = (a.nt * call.group + kTile - 1) / kTile;
                 a.by_tail_tiles = Divisor(a.tail_tiles), a.by_ns = Divisor(a.ns), a.by_quads = Divisor((a.rows + 3) / 4);
                 a.tails = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
                 a.tail_blocks = sets > 4 ? (a.tails + 1) / 2 : a.tails;
-                // Shares of the kept rows until every unit has eight waves (fp32: four, whose registers fill it: 16 answers over 13107 rows 66 us with twice as many, 53 so), four tiles of 64
-                // keys each at least (two, up to 64 shares), as far as there is scratch.
-                const int64_t items = (int64_t)a.nb * call.kv * a.tiles, tail_rows = (int64_t)a.nb * call.kv * a.rows;
-                const int64_t tiles = (call.rows / (call.count * call.kv) / 64 + 1) * items;
-                a.shares = (int)std::max<int64_t>(1, std::min(std::min<int64_t>((sets > 4 || !bf16 ? 1 : 2) * (int64_t)ctx->num_cu, std::max(std::min<int64_t>(64, tiles / 2), tiles / 4)), (room - 1024 - tail_rows) / a.tile_rows - items));
+                // Shares of the kept rows: four tiles of 64 keys each (two, up to 64 shares), up to a workgroup a unit; eight, up to two a unit (256 rows, and fp32, whose registers fill it: one),
+                // as far as there is scratch.  (16 answers over 13107 rows: 28.3 us with four tiles up to two workgroups, 24.0 so; over 300 rows 18.6 with four tiles, 13.8 so; fp32, 13107
+                // rows: 66 with two workgroups, 53 so.)
+                const int64_t items = heads * a.tiles, tail_rows = heads * a.rows, tiles = tiles_a_head * items;
+                const int64_t useful = std::max({std::min<int64_t>(64, tiles / 2), std::min<int64_t>(ctx->num_cu, tiles / 4), tiles / 8});
+                const int64_t units = (sets == 4 ? 2 : 1) * (int64_t)ctx->num_cu;
+                a.shares = (int)std::max<int64_t>(1, std::min({useful, units, (room - 1024 - tail_rows) / a.tile_rows - items}));
                 a.tail_at = (a.shares + items) * a.tile_rows;
                 a.part_o = (float*)((char*)call.scratch + kScratchCounters);
                 a.part_ml = (f32x2a*)(a.part_o + (a.tail_at + tail_rows) * 128);
@@ -917,9 +894,7 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 const auto launch = [&](auto kernel) { kernel<<<(unsigned)(a.tail_blocks + a.shares), sets > 4 ? 512 : 256, 0, stream>>>(a); };
                 if (!bf16) mx ? launch(attend_shared_f32_kernel<true>) : launch(attend_shared_f32_kernel<false>);
                 else if (sets == 8) mx ? launch(attend_shared_kernel<true, 8>) : launch(attend_shared_kernel<false, 8>);
-                else if (sets == 4) mx ? launch(attend_shared_kernel<true, 4>) : launch(attend_shared_kernel<false, 4>);
-                else if (sets == 2) mx ? launch(attend_shared_kernel<true, 2>) : launch(attend_shared_kernel<false, 2>);
-                else mx ? launch(attend_shared_kernel<true, 1>) : launch(attend_shared_kernel<false, 1>);
+                else mx ? launch(attend_shared_kernel<true, 4>) : launch(attend_shared_kernel<false, 4>);
                 const unsigned joins = (unsigned)((int64_t)a.nb * call.kv * ((a.rows + 3) / 4));
                 if (bf16) attend_shared_join_kernel<true><<<joins, 256, 0, stream>>>(a);
                 else attend_shared_join_kernel<false><<<joins, 256, 0, stream>>>(a);

@@ -333,3 +333,11 @@ def test_odd_numbers_of_tails_beside_many_rows(mx, share, kv):
     # (two tails share a workgroup there; one of the last two is none)
     rng = np.random.default_rng(share)
     check("bf16", mx, 1, share, kv, 4, 1, rng.integers(1, 400, kv), 70, rng.integers(0, 71, share))
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("share,kv,keep,m", [(33, 1, 200000, 1), (37, 3, 70001, 1), (80, 2, 100100, 2), (64, 8, 25000, 1)])
+def test_many_rows_over_long_prefixes(mx, share, kv, keep, m):
+    # (tiles of 256 rows, two tails a workgroup, an odd number of them)
+    rng = np.random.default_rng(share)
+    check("bf16", mx, 1, share, kv, 4, m, keep - rng.integers(0, 70, kv), 40, rng.integers(0, 41, share), heads=2, seed=share)

@@ -247,7 +247,7 @@ __device__ __forceinline__ Span rows_that_see(const WeightsArgs& a, int length, 
 }
 
 // A head's products are shared out over `shares` workgroups by the cost of its tiles of keys, one after the other: their stages, and kTileCost for the keys and the masks at a tile's
-// first ones.  Share s has what lies in [total s / shares, total (s + 1) / shares).
+// first ones.  Share s of n, no more than the total, has what lies in [total s / n, total (s + 1) / n).
 constexpr int kTileCost = 6;
 template <int KEYS, int STAGE>
 struct Shares {
@@ -536,7 +536,9 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
         return;
     }
     const Shares<kKeys, kStage> shares{a, length};
-    const int64_t total = shares.below(a.key_tiles), low = total * at / a.shares, high = total * (at + 1) / a.shares;
+    const int64_t total = shares.below(a.key_tiles), parts = min((int64_t)a.shares, total);
+    if (at >= parts) return;
+    const int64_t low = total * at / parts, high = total * (at + 1) / parts;
     int64_t before = 0;
     for (int base = 0; base < a.key_tiles && before < high; base += 64) {
         const int stages = shares.stages(base + (int)(threadIdx.x & 63)), sum = up_to(shares.cost(stages));
@@ -561,12 +563,17 @@ __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
     const int stages = shares.stages(tile);
     float sum = 0.f;
     if (stages > 0) {
-        // the share of position x is the largest s with total s / shares <= x
-        const int64_t total = shares.below(a.key_tiles), first = shares.below(tile) + kTileCost;
-        const int from = (int)(((first + 1) * a.shares - 1) / total), to = (int)(((first + stages) * a.shares - 1) / total);
+        // the share of position x is the largest s with total s / parts <= x
+        const int64_t total = shares.below(a.key_tiles), first = shares.below(tile) + kTileCost, parts = min((int64_t)a.shares, total);
+        const int from = (int)(((first + 1) * parts - 1) / total), to = (int)(((first + stages) * parts - 1) / total);
         const float* part = a.part + ((int64_t)g * (a.shares + a.key_tiles) + tile) * kKeys + j % kKeys;
-        for (int s = from; s <= to; ++s)                           // (a share of nothing, where there are more shares than cost, has written nothing)
-            if (j < length && total * s / a.shares < total * (s + 1) / a.shares) sum += part[(int64_t)s * kKeys];
+        for (int s = from; s <= to && j < length; s += 8) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = part[(int64_t)min(s + e, to) * kKeys];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += s + e <= to ? x[e] : 0.f;
+        }
     }
     if (j < length) add_to(c, g, j, sum, c.decay);
 }

@@ -92,7 +92,7 @@ typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
 template <int ROWS, bool LONG>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
     constexpr int kCopies = ROWS > 4 ? 2 : 1;              // of the first digit's bins, for neighbouring lanes
-    extern __shared__ __attribute__((aligned(16))) uint64_t bits[];                     // [words] rows that stay; [words] tied rows, then {those from beyond, holes} before the word
+    extern __shared__ __attribute__((aligned(16))) uint64_t bits[];                     // [words] rows that stay; [words] tied rows, then {those from beyond, holes} before the word; a list
     uint32_t* bins = (uint32_t*)bits;                      // before that
     __shared__ __attribute__((aligned(16))) uint32_t fine[2][kFineBins], listed[kListed];
     __shared__ int coarse[64], waves[3][kWaves];
@@ -195,14 +195,13 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
     const int from_on = (int)max((int64_t)newest_all - c.recent + (c.recent > 0), (int64_t)INT32_MIN);
     const bool any_recent = c.recent > 0;
     const auto protects = [&](int p) ALWAYS_INLINE { return (p < c.sinks) | (any_recent & (p >= from_on)); };
-    int first = 0;
+    int first = 0;                                                 // of the wave
     for (int batch = 0; batch < batches; ++batch) {
         if (LONG) load_positions(batch);
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) first += protects(at[k]) && row_of(batch, k) < length;
+        for (int k = 0; k < ROWS; ++k) first += __popcll(__ballot(protects(at[k]) && row_of(batch, k) < length));
     }
-    first = up_to(first);
-    if (lane == 63) atomicAdd(&many_first, first);
+    if (lane == 0) atomicAdd(&many_first, first);
     __syncthreads();
     const bool among_first = many_first > stays;
     int need = among_first ? stays : stays - many_first;           // of the rows whose weights decide
@@ -211,12 +210,15 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
             load_positions(batch);
             load_weights(batch);
         }
+        if (among_first)
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const bool is_first = protects(at[k]);
-            const uint32_t by_weight = weight_key(__uint_as_float(x[k]));
-            key[k] = row_of(batch, k) >= length ? 0u : is_first == among_first ? by_weight : is_first ? kProtected : 0u;
-        }
+            for (int k = 0; k < ROWS; ++k) key[k] = protects(at[k]) ? weight_key(__uint_as_float(x[k])) : 0u;
+        else
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) key[k] = protects(at[k]) ? kProtected : weight_key(__uint_as_float(x[k]));
+        if (row_of(batch, ROWS - 4) + 3 >= length)
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) key[k] = row_of(batch, k) < length ? key[k] : 0u;
     };
     if (!LONG) make_keys(0);
     const auto each_batch = [&](auto&& what) ALWAYS_INLINE {
@@ -310,10 +312,15 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
         need = f.need;
         const bool few = in_bin(last) <= kListed;
         if (few) {
+            const uint32_t low = max(last << 20, 1u), span = min(last << 20 | 0xFFFFFu, kProtected - 1) - low;
             each_batch([&](int) ALWAYS_INLINE {
 #pragma unroll
-                for (int k = 0; k < ROWS; ++k)
-                    if (key[k] >> 20 == last && key[k] - 1 < kProtected - 1) listed[atomicAdd(&many_listed, 1)] = key[k];
+                for (int k = 0; k < ROWS; k += 4) {
+                    if (min(min(key[k] - low, key[k + 1] - low), min(key[k + 2] - low, key[k + 3] - low)) > span) continue;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key[k + e] - low <= span) listed[atomicAdd(&many_listed, 1)] = key[k + e];
+                }
             });
             __syncthreads();
         }
@@ -388,6 +395,17 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
         beyond_before += __popcll(bits[w] & ~low_of(w));
     }
     __syncthreads();
+    // The rows from beyond, by rank: a list of them, or, where that has no room, looked for by the words' counts.
+    uint16_t* from_beyond = (uint16_t*)(bits + 2 * words);
+    if constexpr (!LONG) {
+        const int w = tid >> 1, upper = tid & 1;
+        if (w < words) {
+            const uint64_t x = bits[w] & ~low_of(w);
+            uint32_t mine = (uint32_t)(x >> (32 * upper)), rank = before[w].x + (upper ? __popc((uint32_t)x) : 0);
+            for (; mine; mine &= mine - 1) from_beyond[rank++] = (uint16_t)(w * 64 + upper * 32 + __builtin_ctz(mine));
+        }
+        __syncthreads();
+    }
     int step = 1;                                                  // the largest power of two below `words`
     while (step * 2 < words) step *= 2;
     for (int i0 = tid; i0 < stays; i0 += 4 * kThreads) {
@@ -403,13 +421,13 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
             source[e] = i < stays ? i : -1;
             low[e] = 0;
         }
-        for (int d = step; d > 0; d >>= 1)                         // the last word with at most `rank` from beyond before it
+        for (int d = LONG ? step : 0; d > 0; d >>= 1)              // the last word with at most `rank` from beyond before it
 #pragma unroll
             for (int e = 0; e < 4; ++e) low[e] += low[e] + d < words && before[min(low[e] + d, words - 1)].x <= rank[e] ? d : 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (!hole[e]) continue;
-            source[e] = low[e] * 64 + bit_of_rank(bits[low[e]] & ~low_of(low[e]), rank[e] - before[low[e]].x);
+            source[e] = LONG ? low[e] * 64 + bit_of_rank(bits[low[e]] & ~low_of(low[e]), rank[e] - before[low[e]].x) : from_beyond[rank[e]];
             if (c.moves) {
                 const int k = atomicAdd(&many_moved, 1);
                 moved[k][0] = i0 + e * kThreads, moved[k][1] = source[e];
@@ -441,7 +459,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, int blocks
 
 hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_t stream) {
     const unsigned heads = (unsigned)(call.count * call.kv);
-    const size_t lds = std::max((size_t)((call.n + 63) / 64) * 16, kBins * (call.n > 4 * kThreads ? 2 : 1) * sizeof(uint32_t));
+    const bool is_long = call.n > 32 * kThreads;
+    const int64_t most_moved = call.n > call.keep ? std::min<int64_t>(call.n - call.keep, call.keep) : 0;
+    const size_t lds = std::max((size_t)((call.n + 63) / 64) * 16 + (is_long ? 0 : most_moved * 2), kBins * (call.n > 4 * kThreads ? 2 : 1) * sizeof(uint32_t));
     EvictCall select = call;
     select.moves = call.K_out == call.K && call.n - call.keep <= kMostMoved;       // (in place; no more rows move than leave)
     const auto launch = [&](auto kernel) {

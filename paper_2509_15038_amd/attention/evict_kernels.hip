@@ -191,17 +191,39 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
     __syncthreads();
     if (lane == 0) atomicMax(&newest_all, newest);
     __syncthreads();
-    // How many rows are protected.
+    // How many rows are protected: whose position, less the sinks, is not below `open`.
     const int from_on = (int)max((int64_t)newest_all - c.recent + (c.recent > 0), (int64_t)INT32_MIN);
-    const bool any_recent = c.recent > 0;
-    const auto protects = [&](int p) ALWAYS_INLINE { return (p < c.sinks) | (any_recent & (p >= from_on)); };
-    int first = 0;                                                 // of the wave
+    const uint32_t open = c.recent > 0 ? (uint32_t)max((int64_t)from_on - c.sinks, (int64_t)0) : 0x80000000u - (uint32_t)c.sinks;
+    // (what the passes over the rows find is not kept from one to the next, as masks of 64 lanes it would fill more registers than there are)
+    const auto apart = [&](uint32_t (&y)[ROWS]) ALWAYS_INLINE {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) loaded(y[k]);
+    };
+    // fours of rows of which all lanes have whole ones, and, otherwise, one by one those below `length`
+    const auto each_row = [&](int batch, auto&& what, auto&& beyond) ALWAYS_INLINE {
+        const int wave_row = batch * (ROWS * kThreads) + __builtin_amdgcn_readfirstlane(tid >> 6) * 256;
+#pragma unroll
+        for (int k = 0; k < ROWS; k += 4) {
+            if (wave_row + k * kThreads + 256 <= length) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) what(k + e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (row_of(batch, k + e) < length) what(k + e);
+                    else beyond(k + e);
+                }
+            }
+        }
+    };
+    int first = 0;
     for (int batch = 0; batch < batches; ++batch) {
         if (LONG) load_positions(batch);
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) first += __popcll(__ballot(protects(at[k]) && row_of(batch, k) < length));
+        apart(at);
+        each_row(batch, [&](int k) ALWAYS_INLINE { first += at[k] - (uint32_t)c.sinks >= open; }, [](int) {});
     }
-    if (lane == 0) atomicAdd(&many_first, first);
+    first = up_to(first);
+    if (lane == 63) atomicAdd(&many_first, first);
     __syncthreads();
     const bool among_first = many_first > stays;
     int need = among_first ? stays : stays - many_first;           // of the rows whose weights decide
@@ -210,21 +232,21 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
             load_positions(batch);
             load_weights(batch);
         }
-        if (among_first)
-#pragma unroll
-            for (int k = 0; k < ROWS; ++k) key[k] = protects(at[k]) ? weight_key(__uint_as_float(x[k])) : 0u;
-        else
-#pragma unroll
-            for (int k = 0; k < ROWS; ++k) key[k] = protects(at[k]) ? kProtected : weight_key(__uint_as_float(x[k]));
-        if (row_of(batch, ROWS - 4) + 3 >= length)
-#pragma unroll
-            for (int k = 0; k < ROWS; ++k) key[k] = row_of(batch, k) < length ? key[k] : 0u;
+        apart(at);
+        each_row(batch, [&](int k) ALWAYS_INLINE {
+            const uint32_t by_weight = weight_key(__uint_as_float(x[k]));
+            const bool is_first = at[k] - (uint32_t)c.sinks >= open;
+            if (among_first) key[k] = is_first ? by_weight : 0u;
+            else key[k] = is_first ? kProtected : by_weight;
+        }, [&](int k) ALWAYS_INLINE { key[k] = 0u; });
+        apart(key);
     };
     if (!LONG) make_keys(0);
     const auto each_batch = [&](auto&& what) ALWAYS_INLINE {
         for (int batch = 0; batch < batches; ++batch) {
             if (LONG) make_keys(batch);
             what(batch);
+            apart(key);
         }
     };
     const int leave = length - stays;

@@ -417,8 +417,9 @@ int curdkv_evict(curdkv_ctx* ctx, const void* K, const void* V, const float* mas
  * Q, out: [count*share, m, kv_heads*group_size, head_dim]; lse: float [count*share, kv_heads*group_size, m] or NULL.
  * offsets: DEVICE int64 [count*kv_heads + 1], K_kept, V_kept, total, rows: the prefixes', as in curdkv_attend_kept.
  * K_tail, V_tail: [count*share, kv_heads, tail_stride, head_dim]; tail_lengths: int32 [count*share].
- * count*share*m*kv_heads*group_size < 2^31, kv_heads*group_size <= 16384, kv_heads <= 1024.  scratch: not NULL here, CURDKV_ATTEND_SCRATCH_BYTES at least, cleared once as
- * for curdkv_attend; the partial results of prefixes and tails meet there. */
+ * count*share*m*kv_heads*group_size < 2^31, kv_heads*group_size <= 16384, kv_heads <= 1024.  scratch: not NULL here,
+ * CURDKV_ATTEND_SCRATCH_BYTES at least, cleared once as for curdkv_attend; the partial results of prefixes and tails meet
+ * there. */
 int curdkv_attend_shared(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept,
                          const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,
                          const void* V_tail, int64_t tail_n, int64_t tail_stride, const int32_t* tail_lengths,

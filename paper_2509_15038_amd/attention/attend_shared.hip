@@ -10,7 +10,7 @@
 // Weights are rounded to bf16 for their product with V (half a step of 2^-8, as the values themselves have been); sums are of what was not rounded.
 //
 // Bound by: over long prefixes the products, whose power lowers the clock (64 sequences over 131072 kept rows of 8 heads, 137 GFLOP, 177 us: 780 TFLOP/s; 557 MB); in 4 bits the expansion,
-// which every 128 rows take anew (4 prompts of 13107 kept rows and 64 answers with 513 tokens each, 124 MB, 59 us, of which the tails' 83 MB 13 us); over short ones the chain of two
+// which every 128 rows take anew (4 prompts of 13107 kept rows, 16 answers to each with up to 513 tokens, 124 MB, 59 us, of which the tails' 83 MB 13); over short ones the chain of two
 // launches, a few tiles and the join (16 answers over 3276 rows, 21 MB, 19 us).  fp32: 16 answers over 13107 rows 53 us, of which the products of 32 bits 25.
 #include <algorithm>
 

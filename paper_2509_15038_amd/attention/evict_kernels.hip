@@ -7,6 +7,10 @@
 // largest keys stay (should there be more protected rows, they have their weights' keys and all others 0).  The last key that stays is found digit by digit, 12 bits of all keys, then
 // 10 and 10 of the few that share these.  Then bitmaps in LDS, one bit a row, of the rows that stay and of those that tie with the last; all that is left
 // (the first of the tied, ranks of holes and of those that fill them) are counts of bits.  evict_move_kernel copies rows, 16 bytes a lane.
+//
+// Bound by: of many heads, the copy (128 heads of up to 16384 rows, 4096 of which stay and move: 495 MB, 107 us, of which the copy 90 at 5 TB/s); of few heads, one unit's vector
+// instructions, of which one for every row takes 0.25 us at 32768 rows (8 heads, 10 % stay: 28 us, selection 21 and copy 6; 131072 rows 132); of a generated token, a chain of latencies
+// and the launch (32 sequences of 8 heads, one of 3277 rows leaves each: 8.5 us).
 
 #include <algorithm>
 #include <type_traits>
@@ -20,8 +24,8 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 4096, kFineBins = 1024;      // 12 bits of a key, then 10, then 10
 constexpr int kListed = 2048;                      // keys of one bin that are kept apart
-constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place
-constexpr int kFewLeave = 8;                       // rows that are found one by one (a token's one of 3277: 13.6 us by digits, so KFEW)
+constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place (24 of 3300 of 256 heads 14.7 us, 53.6 by another kernel; 100 of 1001 of 64 heads 11.9, 15.3)
+constexpr int kFewLeave = 8;                       // rows that are found one by one (of 256 heads of some 3280: one 8.5 us, 13.6 by digits; four 10.3, 14.1; eight 11.0, 12.1)
 
 // Larger is better: 0 for what is none, weights in order, -0 as 0, NaN above all, and above that the protected.
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
@@ -91,7 +95,7 @@ typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
 // A thread has four rows in every 4096: up to ROWS of them in registers, or, where the head is LONG, so many at a time, read again for every pass.
 template <int ROWS, bool LONG>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c) {
-    constexpr int kCopies = ROWS > 4 ? 2 : 1;              // of the first digit's bins, for neighbouring lanes
+    constexpr int kCopies = ROWS > 4 ? 2 : 1;              // of the first digit's bins, for neighbouring lanes (32768 rows: one 30.9 us, two 30.1, four 30.2)
     extern __shared__ __attribute__((aligned(16))) uint64_t bits[];                     // [words] rows that stay; [words] tied rows, then {those from beyond, holes} before the word; a list
     uint32_t* bins = (uint32_t*)bits;                      // before that
     __shared__ __attribute__((aligned(16))) uint32_t fine[2][kFineBins], listed[kListed];

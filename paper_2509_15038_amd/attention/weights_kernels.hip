@@ -6,6 +6,13 @@
 // Few rows (weights_few_kernel): S = Q K^T by mfma_f32_16x16x32_bf16 (16x16x4 for fp32), 16 rows R by 16 keys; the rows stay in registers, a wave goes over keys.
 // Many rows (weights_many_kernel): S^T = K Q^T by mfma_f32_32x32x16_bf16 (fp32: six products of parts); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves
 // share, and each lane adds up the weights of its own R, key by key, until all rows are through.
+//
+// Few rows or many: 32 rows over 32768 keys of 8 heads 17.9 us by the former, 20.3 by the latter; 16 rows 17.2 and 20.1; one token of 32 sequences over 8192 keys 97 and 137.
+// Bound by: few rows, HBM (a token of 32 sequences over up to 4096 rows, 137 MB, 31 us, 4.4 TB/s; one over 131072, 268 MB, 47 us, 5.7); many rows, the exponentials and sums between the
+// products (2900 clocks a 128 by 64 block, of products 2048) and the power that lowers the clock: a prompt of 8192 tokens, 32 heads, 275 GFLOP, 277 us, 1000 TFLOP/s; with one stage of rows
+// (32 tokens' 128 rows over 32768 keys, 67 MB, 23 us), keys that arrive before their products begin; fp32 (three ragged prompts of up to 1021 tokens, window 257) 31.5 us, a chain of
+// latencies: a tile's keys, a few stages, the join.
+// Each weight is rounded nowhere: scores, exponentials and sums are of 32 bits.
 
 #include <algorithm>
 
@@ -87,7 +94,7 @@ __device__ __forceinline__ void to_rows(T& x, T& y) {
     x = __builtin_bit_cast(T, u), y = __builtin_bit_cast(T, v);
 }
 // 16 TILES rows R at most.  A wave takes the 64 keys of a step 16 at a time, the next 16 on their way, and reads and writes their weights together.
-// PAST: keys pass the caches.
+// PAST: keys pass the caches (268 MB of them 47 us, 55 through the caches; 67 MB 17.8 and 16.5).
 template <bool BF16, int TILES, bool PAST>
 __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
     constexpr int kRow = BF16 ? 256 : 512, kPieces = BF16 ? 4 : 8;
@@ -166,8 +173,9 @@ template <> struct Many<true> {
         for (int s = 0; s < 8; ++s) x[s] = ((const u32x4a*)row)[2 * s + half];
     }
 };
-// fp32: a number x is three of 8 bits, x = h + m + l exactly (h its upper half, m what is left rounded to bf16, l the rest, whose last bits end at 2^-133); of the nine products of parts the six
-// that count go through the bf16 units, and what is left out is below 2^-22 of a product.  Infinities and NaN are h alone, and what holds one goes through products of 32 bits.
+// fp32: a number x is three of 8 bits, x = h + m + l exactly (h its upper half, m what is left rounded to bf16, l the rest, whose last bits end at 2^-133); of the nine products of parts the
+// six that count go through the bf16 units, and what is left out is below 2^-22 of a product (2000 tokens over 2000, 16 GFLOP: 115 us, by products of 32 bits 164).  Infinities and NaN are h
+// alone, and what holds one goes through products of 32 bits.
 struct Parts {                         // of eight channels
     u32x4a h, m, l;
 };
@@ -599,6 +607,7 @@ hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStr
     a.key_tiles = (call.n + keys - 1) / keys;
     a.most = (int)(((int64_t)1 << 31) / (call.kv * (bf16 ? 256 : 512)) / stage);
     // Two workgroups a unit, each with an equal share of a head's products, where tiles of keys would leave units idle at the end; their sums lie in scratch, as far as there is any.
+    // (1021 tokens over 1021: 22 us so, 85 by tiles; 2000 over 2000: 45 and 146.  Up to two stages of rows there is little to share: 128 rows over 32768 keys 47.7 and 47.9.)
     const int64_t tiles = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (a.groups * (int64_t)keys * 4) - a.key_tiles : 0;
     const int64_t shares = std::min(std::min<int64_t>(2 * (int64_t)ctx->num_cu / a.groups, room), std::max<int64_t>(1, (int64_t)((a.rows + stage - 1) / stage) * a.key_tiles));
     a.shares = tiles < 2 * (int64_t)ctx->num_cu && a.rows > 2 * stage && shares > 1 ? (int)shares : 0;

@@ -384,7 +384,7 @@ int curdkv_rotate_axes(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t 
  *   nothing, but to keys of score NaN or +infinity; one of lse NaN makes the weight of the keys that it sees NaN, and no
  *   other's.
  * decay: not negative, finite; 0: the old weights are not read.
- * kv_heads <= 16384.
+ * kv_heads <= 16384, kv_heads*group_size <= 2^20.
  * mass: float [count, kv_heads, mass_stride], rows below a sequence's length written; those behind it stay as they
  *   are.  n <= mass_stride.
  * Scores and sums in 32 bits, summed in an order that depends on the sizes alone.  scratch as in curdkv_attend. */
@@ -400,7 +400,7 @@ int curdkv_attend_weights(curdkv_ctx* ctx, const void* Q, const void* K, const f
  * A row below `keep` that stays keeps its place; the places of the others are taken, in ascending order, by the rows that
  * stay from beyond, ascending: rows are no longer in the order of their tokens, and `positions` says which is which.
  * K, V: [count, kv_heads, stride, head_dim]; mass: float, positions: int32 [count, kv_heads, stride]; positions NULL: the
- *   row's number.  lengths: int32 [count], clamped to [0, n]; NULL = n.  1 <= keep, n <= stride, n <= 524288.
+ *   row's number.  lengths: int32 [count], clamped to [0, n]; NULL = n.  1 <= keep <= 2^30, n <= stride, n <= 524288.
  * K_out, V_out: [count, kv_heads, out_stride, head_dim]; mass_out, positions_out: [count, kv_heads, out_stride], NULL: not
  *   written.  Only rows below min(length, keep) are written.  keep <= out_stride or n <= out_stride.
  *   K_out = K with V_out = V: in place, and mass_out may be mass, positions_out positions; wherever an array is its own

@@ -46,7 +46,8 @@ int curdkv_attend_weights(curdkv_ctx* ctx, const void* Q, const void* K, const f
     if (rc != CURDKV_OK) return rc;
     if (!K || !lse || !mass || n < 1 || m > ctx->cfg.max_tokens || window < 0 || n_sink < 0 || mass_stride < n || !aligned16({K})) return CURDKV_ERR_INVALID_ARG;
     if (!(decay >= 0.f) || !std::isfinite(decay)) return CURDKV_ERR_INVALID_ARG;
-    if ((n + 63) / 64 > kMostBlocks / (count * ctx->cfg.kv_heads) || ctx->cfg.kv_heads > 1 << 14) return CURDKV_ERR_UNSUPPORTED;      // (more rows than the memory holds)
+    if ((n + 63) / 64 > kMostBlocks / (count * ctx->cfg.kv_heads)) return CURDKV_ERR_UNSUPPORTED;      // (more rows than the memory holds)
+    if (ctx->cfg.kv_heads > 1 << 14 || (int64_t)ctx->cfg.kv_heads * ctx->cfg.group_size > 1 << 20) return CURDKV_ERR_UNSUPPORTED;      // (offsets among a few tokens' queries have 32 bits)
     WeightsCall c{};
     c.Q = Q, c.K = K, c.lse = lse, c.count = count, c.stride = stride;
     c.kv = ctx->cfg.kv_heads, c.group = ctx->cfg.group_size, c.m = (int)m, c.n = (int)n, c.dtype = ctx->cfg.dtype;
@@ -67,7 +68,7 @@ int curdkv_evict(curdkv_ctx* ctx, const void* K, const void* V, const float* mas
     if ((K_out == K || mass_out == mass || (positions && positions_out == positions)) && out_stride != stride) return CURDKV_ERR_INVALID_ARG;
     if (!aligned16({K, V, K_out, V_out})) return CURDKV_ERR_INVALID_ARG;
     const int64_t heads = (int64_t)ctx->cfg.kv_heads;
-    if (n > kEvictMostRows || keep > (1LL << 31) - 1 || count > (1 << 20) / heads) return CURDKV_ERR_UNSUPPORTED;
+    if (n > kEvictMostRows || keep > 1LL << 30 || count > (1 << 20) / heads) return CURDKV_ERR_UNSUPPORTED;
     EvictCall c{};
     c.K = (const char*)K, c.V = (const char*)V, c.mass = mass, c.positions = positions, c.lengths = lengths;
     c.count = count, c.stride = stride, c.out_stride = out_stride, c.recent = recent;

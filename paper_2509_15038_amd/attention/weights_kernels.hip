@@ -159,11 +159,6 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
 
 // ---- many rows
 
-// 64 lanes' 16 bytes, each from an address of its own, to LDS from `to` on (as dma16).
-__device__ __forceinline__ void dma16_from(uint32_t to, const char* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
-}
-
 template <bool BF16> struct Many;
 template <> struct Many<true> {
     static constexpr int kBlocks = 2, kTiles = 4, kRow = 256;      // of 32 keys a wave; tiles of 32 rows a stage of 32 KB

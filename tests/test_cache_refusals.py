@@ -146,6 +146,14 @@ def test_shared_scales_and_heads(checks):
         assert call(checks, "attend_shared", dict(shared(checks), ctx=checks.made(kv, group, 1, 1000, 0))) == (code, int(code == OK)), (kv, group)
 
 
+def test_numbers_of_heads_and_rows_at_their_ends(checks):
+    for kv, group, code in ((1, 2 ** 20, OK), (1, 2 ** 20 + 1, NO), (2 ** 14, 64, OK), (2 ** 14, 65, NO), (2 ** 14 + 1, 1, NO)):
+        assert call(checks, "attend_weights", dict(weights(checks), ctx=checks.made(kv, group, 1, 1000, 0)), count=1, m=1) == (code, int(code == OK)), (kv, group)
+    place = dict(K_out=6 * P, V_out=7 * P, mass_out=None, positions_out=None)
+    assert call(checks, "evict", evict(checks), keep=2 ** 30, **place) == (OK, 1)
+    assert call(checks, "evict", evict(checks), keep=2 ** 30 + 1, **place) == (NO, 0)
+
+
 def test_another_device_than_the_current_one(checks):
     for name, given in (("rotate_axes", axes(checks)), ("attend_weights", weights(checks)), ("evict", evict(checks)), ("attend_shared", shared(checks)), ("attend_shared_mx", shared(checks, True))):
         assert call(checks, name, given, ctx=checks.made(2, 4, 1, 1000, 1)) == (BAD, 0), name

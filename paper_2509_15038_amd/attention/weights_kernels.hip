@@ -3,15 +3,18 @@
 // lse_R being the logarithm of the row's softmax denominator, which the attention has written.  With it no maximum has to be found: every weight is at
 // most 1 (as far as lse is what the scores make it), and a key's sum is its own affair: one wave's, or a few waves' that are added up in order, without atomics.
 //
-// Few rows (weights_few_kernel): S = Q K^T by mfma_f32_16x16x32_bf16 (16x16x4 for fp32), 16 rows R by 16 keys; the rows stay in registers, a wave goes over keys.
-// Many rows (weights_many_kernel): S^T = K Q^T by mfma_f32_32x32x16_bf16 (fp32: six products of parts); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves
-// share, and each lane adds up the weights of its own R, key by key, until all rows are through.
+// Few rows, up to 32 of fp32 or over keys that pass the caches, up to 16 over few keys (weights_few_kernel): S = Q K^T by mfma_f32_16x16x32_bf16 (16x16x4 for fp32), 16 rows R by 16 keys; the rows stay in registers, a
+// wave goes over keys, whose lines it reads whole.
+// Up to 128 rows (weights_some_kernel): S^T = K Q^T by mfma_f32_32x32x16_bf16, 32 keys by 32 rows R; the rows stay in LDS, a wave goes over keys; each lane adds up the weights of its own R, key
+// by key.
+// Many rows (weights_many_kernel): the same (fp32: six products of parts); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves share.
 //
-// Few rows or many: 32 rows over 32768 keys of 8 heads 17.9 us by the former, 20.3 by the latter; 16 rows 17.2 and 20.1; one token of 32 sequences over 8192 keys 97 and 137.
-// Bound by: few rows, HBM (a token of 32 sequences over up to 4096 rows, 137 MB, 31 us, 4.4 TB/s; one over 131072, 268 MB, 47 us, 5.7); many rows, the exponentials and sums between the
-// products (2900 clocks a 128 by 64 block, of products 2048) and the power that lowers the clock: a prompt of 8192 tokens, 32 heads, 275 GFLOP, 277 us, 1000 TFLOP/s; with one stage of rows
-// (32 tokens' 128 rows over 32768 keys, 67 MB, 23 us), keys that arrive before their products begin; fp32 (three ragged prompts of up to 1021 tokens, window 257) 31.5 us, a chain of
-// latencies: a tile's keys, a few stages, the join.
+// Which of them: one token over 4097 keys of 8 heads 5.2 us by the first and 5.7 by the second, over 32768 16.5 and 13.8; 8 tokens' 32 rows 17.9 and 13.1 (by the third 20.3); over 131072 keys,
+// past the caches, 47 and 56; 32 tokens over 32768 18.6 by the second, 23 by the third.
+// Bound by: few rows, HBM (a token of 32 sequences over up to 4096 rows, 137 MB, 31 us, 4.4 TB/s; one over 131072, 268 MB, 47 us, 5.7); up to 128, HBM at 4.4 TB/s after 3 us of start (32
+// tokens over 32768 keys, 67 MB, 18.6 us); many rows, the exponentials and sums between the products (2900 clocks a 128 by 64 block, of products 2048) and the power that lowers the clock: a
+// prompt of 8192 tokens, 32 heads, 275 GFLOP, 277 us, 1000 TFLOP/s; fp32 (three ragged prompts of up to 1021 tokens, window 257) 31.5 us, a chain of latencies: a tile's keys, a few stages,
+// the join.
 // Each weight is rounded nowhere: scores, exponentials and sums are of 32 bits.
 
 #include <algorithm>
@@ -555,6 +558,80 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     }
 }
 
+// ---- up to 128 rows, bf16: they lie in LDS once for all, and each wave goes over blocks of 32 keys of its own, the next one on its way (two on their way: 19.3 us where one takes 18.4).
+__global__ __launch_bounds__(256, 3) void weights_some_kernel(WeightsArgs a) {
+    __shared__ __attribute__((aligned(16))) char Qs[32768];
+    __shared__ float less_of[128];
+    __shared__ int place_of[128];
+    const WeightsCall& c = a.c;
+    const int head = blockIdx.x % c.kv, share = blockIdx.x / c.kv % a.shares, b = blockIdx.x / c.kv / a.shares, g = b * c.kv + head;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int length = length_of(c, b), blocks = (length + 31) / 32, tiles = (a.rows + 31) / 32;
+    const int first = (int)((int64_t)blocks * share / a.shares), end = (int)((int64_t)blocks * (share + 1) / a.shares);
+    if (first >= end) return;
+    const char* queries = (const char*)uniform((int64_t)((const char*)c.Q + ((int64_t)b * c.m * c.kv + head) * c.group * 256));
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(&Qs[0]) + wave * 8192);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                                  // (columns of 64 bytes a row, as in tile_stages)
+        const int R = min(wave * 32 + h * 16 + (lane >> 2), a.rows - 1), token = a.by_group.of(R);
+        const uint32_t at = (uint32_t)(token * c.kv * c.group + a.by_group.rest(R, token)) * 256 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dma16(lds + h * 1024 + i * 2048, queries, at + i * 64);
+    }
+    const char* keys = (const char*)c.K + (int64_t)g * c.stride * 256;
+    Many<true> next;
+    if (first + wave < end) next.load(keys + (int64_t)min((first + wave) * 32 + col, length - 1) * 256, half);
+    if (tid < 128) {                                               // of a row -lse in units of log 2, and its position (below all where it gives nothing)
+        const int R = min(tid, a.rows - 1), token = a.by_group.of(R);
+        const float lse = c.lse[(((int64_t)b * c.kv + head) * c.group + a.by_group.rest(R, token)) * c.m + token];
+        less_of[tid] = -lse * (1.f / kLn2);
+        place_of[tid] = tid < a.rows && lse != -INFINITY ? length - c.m + token : -1;
+    }
+    dma_wait();
+    __syncthreads();
+    const int k_at[2] = {col * 64 + ((half ^ ((col >> 1) & 3)) << 4), col * 64 + (((2 + half) ^ ((col >> 1) & 3)) << 4)};
+    const int mine = (col & 15) / 4 * 8 + col % 4 + half * 4;      // the key of a block whose sum comes to this lane
+    float* mass = c.mass + (int64_t)g * c.mass_stride;
+#pragma unroll 1
+    for (int block = first + wave; block < end; block += 4) {
+        const int k0 = block * 32, j = k0 + mine;
+        const Many<true> key = next;
+        if (block + 4 < end) next.load(keys + (int64_t)min(k0 + 128 + col, length - 1) * 256, half);
+        const float old = mass[min(j, length - 1)];
+        float sums[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[i] = 0.f;
+#pragma unroll 1
+        for (int u = 0; u < tiles; ++u) {                          // (not unrolled: a launch of few blocks pays for the code that it fetches)
+            const char* Qt = Qs + u * 8192;
+            const float less = less_of[u * 32 + col];
+            const int p = place_of[u * 32 + col];
+            f32x16a x;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const u32x4a q = *(const u32x4a*)(Qt + k_at[i & 1] + (i >> 1) * 2048);
+                x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8a, key.x[i]), __builtin_bit_cast(bf16x8a, q), x, 0, 0, 0);
+            }
+            if (__all(k0 + 31 <= p && (c.window == 0 || k0 + 31 < c.sinks || p - k0 < c.window))) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, less));
+                    sums[i] += sees(p, k0 + i / 4 * 8 + i % 4 + half * 4, c.window, c.sinks) ? w : 0.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[i] += __shfl_xor(sums[i], 16);
+        spread<8>(sums, col);
+        if (j < length && col < 16) mass[j] = c.decay == 0.f ? sums[0] : __builtin_fmaf(c.decay, old, sums[0]);
+    }
+}
+
 // Adds up the shares of a key's tile, in order; a wave's keys are of one tile.
 template <bool BF16>
 __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
@@ -586,23 +663,29 @@ __global__ __launch_bounds__(256) void weights_join_kernel(WeightsArgs a) {
 hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStream_t stream) {
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
     WeightsArgs a{call, call.scale * (1.f / kLn2), (int)(call.count * call.kv), call.m * call.group, 0, 0, 0, nullptr, Divisor(call.count * call.kv), Divisor(call.kv), Divisor(call.group)};
-    if (a.rows <= 32) {
+    const bool past = (int64_t)a.groups * call.n * (bf16 ? 256 : 512) > kPastCaches;
+    if (a.rows <= 32 && (past || !bf16 || (a.rows <= 16 && (int64_t)a.groups * call.n <= 512 * (int64_t)ctx->num_cu))) {
         const int64_t steps = (call.n + 63) / 64, waves = 16 * (int64_t)ctx->num_cu;
         const int64_t each = std::max<int64_t>(1, std::min<int64_t>(4, a.groups * steps / waves));
         a.shares = (int)((steps + 4 * each - 1) / (4 * each));
-        const bool past = (int64_t)a.groups * call.n * (bf16 ? 256 : 512) > kPastCaches;
         const auto launch = [&](auto kernel) { kernel<<<(unsigned)((int64_t)a.groups * a.shares), 256, 0, stream>>>(a); };
         if (bf16 && a.rows <= 16) past ? launch(weights_few_kernel<true, 1, true>) : launch(weights_few_kernel<true, 1, false>);
-        else if (bf16) past ? launch(weights_few_kernel<true, 2, true>) : launch(weights_few_kernel<true, 2, false>);
+        else if (bf16) launch(weights_few_kernel<true, 2, true>);
         else if (a.rows <= 16) past ? launch(weights_few_kernel<false, 1, true>) : launch(weights_few_kernel<false, 1, false>);
         else past ? launch(weights_few_kernel<false, 2, true>) : launch(weights_few_kernel<false, 2, false>);
+        return hipGetLastError();
+    }
+    if (bf16 && a.rows <= 128) {                                   // two workgroups a unit, as far as each of their waves has a block of keys (three: 19.2 us where two take 18.6)
+        const int64_t blocks = (call.n + 31) / 32;
+        a.shares = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 3) / 4, 2 * (int64_t)ctx->num_cu / a.groups));
+        weights_some_kernel<<<(unsigned)((int64_t)a.groups * a.shares), 256, 0, stream>>>(a);
         return hipGetLastError();
     }
     const int keys = bf16 ? 256 : 128, stage = bf16 ? 128 : 64;
     a.key_tiles = (call.n + keys - 1) / keys;
     a.most = (int)(((int64_t)1 << 31) / (call.kv * (bf16 ? 256 : 512)) / stage);
     // Two workgroups a unit, each with an equal share of a head's products, where tiles of keys would leave units idle at the end; their sums lie in scratch, as far as there is any.
-    // (1021 tokens over 1021: 22 us so, 85 by tiles; 2000 over 2000: 45 and 146.  Up to two stages of rows there is little to share: 128 rows over 32768 keys 47.7 and 47.9.)
+    // (1021 tokens over 1021: 22 us so, 85 by tiles; 2000 over 2000: 45 and 146.  Up to two stages of rows there is little to share.)
     const int64_t tiles = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (a.groups * (int64_t)keys * 4) - a.key_tiles : 0;
     const int64_t shares = std::min(std::min<int64_t>(2 * (int64_t)ctx->num_cu / a.groups, room), std::max<int64_t>(1, (int64_t)((a.rows + stage - 1) / stage) * a.key_tiles));
     a.shares = tiles < 2 * (int64_t)ctx->num_cu && a.rows > 2 * stage && shares > 1 ? (int)shares : 0;

@@ -215,3 +215,11 @@ def test_another_stream():
     torch.cuda.synchronize()
     scratch = torch.zeros((0,), dtype=torch.uint8, device="cuda")
     check("bf16", 2, 2, 4, 100, 300, stream=side, scratch=scratch)
+
+
+@pytest.mark.parametrize("m,n,kv,group,count", [(1, 20011, 8, 4, 1), (4, 20011, 8, 4, 1), (8, 20011, 2, 4, 3), (9, 20011, 2, 4, 2), (32, 9001, 2, 4, 2), (11, 9001, 2, 11, 2), (1, 40003, 8, 4, 2),
+                                                (8, 40003, 8, 4, 2), (5, 40003, 8, 7, 2)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 5)])
+def test_which_kernel_takes_few_rows_of_long_caches(m, n, kv, group, count, window, sinks):
+    # (few rows over few keys, over many, past the caches; up to 128 rows)
+    check("bf16", count=count, kv=kv, group=group, m=m, n=n, window=window, sinks=sinks, decay=0.5, seed=m + n)

@@ -10,9 +10,9 @@
 // Many rows (weights_many_kernel): the same (fp32: six products of parts); a wave's keys stay in registers, rows R go through LDS in stages of 16 KB that four waves share.
 //
 // Which of them: one token over 4097 keys of 8 heads 5.2 us by the first and 5.7 by the second, over 32768 16.5 and 13.8; 8 tokens' 32 rows 17.9 and 13.1 (by the third 20.3); over 131072 keys,
-// past the caches, 47 and 56; 32 tokens over 32768 18.6 by the second, 23 by the third.
-// Bound by: few rows, HBM (a token of 32 sequences over up to 4096 rows, 137 MB, 31 us, 4.4 TB/s; one over 131072, 268 MB, 47 us, 5.7); up to 128, HBM at 4.4 TB/s after 3 us of start (32
-// tokens over 32768 keys, 67 MB, 18.6 us); many rows, the exponentials and sums between the products (2900 clocks a 128 by 64 block, of products 2048) and the power that lowers the clock: a
+// past the caches, 46 and 56; 32 tokens over 32768 19 by the second, 23 by the third.  Keys that a window hides from all rows are not read (a token over 131072 with a window of 4096: 13 us).
+// Bound by: few rows, HBM (a token of 32 sequences over up to 4096 rows, 137 MB, 31 us, 4.4 TB/s; one over 131072, 268 MB, 46 us, 5.8); up to 128, HBM at 4.4 TB/s after 3 us of start (32
+// tokens over 32768 keys, 67 MB, 19 us); many rows, the exponentials and sums between the products (2900 clocks a 128 by 64 block, of products 2048) and the power that lowers the clock: a
 // prompt of 8192 tokens, 32 heads, 275 GFLOP, 277 us, 1000 TFLOP/s; fp32 (three ragged prompts of up to 1021 tokens, window 257) 31.5 us, a chain of latencies: a tile's keys, a few stages,
 // the join.
 // Each weight is rounded nowhere: scores, exponentials and sums are of 32 bits.
@@ -45,6 +45,8 @@ __device__ __forceinline__ Tokens tokens_that_see(int length, int m, int j0, int
     return {(int)min(max((int64_t)j0 - p0, (int64_t)0), (int64_t)m), (int)max(last, (int64_t)-1)};
 }
 __device__ __forceinline__ int length_of(const WeightsCall& c, int b) { return __builtin_amdgcn_readfirstlane(c.lengths ? min(max(c.lengths[b], 0), c.n) : c.n); }
+// Whether any of the m tokens sees one of keys j0 .. j1 (below the length): the first one's window reaches lowest.
+__device__ __forceinline__ bool any_sees(const WeightsCall& c, int length, int j0, int j1) { return (c.window == 0) | (j0 < c.sinks) | (c.window > length - c.m - j1); }
 __device__ __forceinline__ void add_to(const WeightsCall& c, int g, int j, float sum, float decay) {
     float* to = c.mass + (int64_t)g * c.mass_stride + j;
     *to = decay == 0.f ? sum : __builtin_fmaf(decay, *to, sum);
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
             k.x[s] = PAST ? __builtin_nontemporal_load(from) : *from;
         }
     };
-    ask(ahead[0], first * 64);
+    if (any_sees(c, length, first * 64, first * 64 + 63)) ask(ahead[0], first * 64);
     // rows 16 u + col as the operand; of rows 16 u + 4 quarter + i, whose scores come back, the position (below all where the row gives nothing) and -lse
     int p[TILES][4];
     float less[TILES][4];
@@ -135,8 +137,14 @@ __global__ __launch_bounds__(256) void weights_few_kernel(WeightsArgs a) {
     }
     for (int step = first; step < end; ++step) {
         const int j = step * 64 + lane;
-        const float old = mass[min(j, length - 1)];
+        const bool seen = any_sees(c, length, step * 64, step * 64 + 63);
+        const float old = seen || c.decay != 1.f ? mass[min(j, length - 1)] : 0.f;
         float mine = 0.f;
+        if (!seen) {
+            if (j < length && c.decay != 1.f) mass[j] = c.decay == 0.f ? 0.f : c.decay * old;
+            if (any_sees(c, length, step * 64 + 64, step * 64 + 127)) ask(ahead[0], step * 64 + 64);
+            continue;
+        }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             ask(ahead[(x + 1) % 2], step * 64 + x * 16 + 16);
@@ -567,8 +575,8 @@ __global__ __launch_bounds__(256, 3) void weights_some_kernel(WeightsArgs a) {
     const int head = blockIdx.x % c.kv, share = blockIdx.x / c.kv % a.shares, b = blockIdx.x / c.kv / a.shares, g = b * c.kv + head;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int length = length_of(c, b), blocks = (length + 31) / 32, tiles = (a.rows + 31) / 32;
-    const int first = (int)((int64_t)blocks * share / a.shares), end = (int)((int64_t)blocks * (share + 1) / a.shares);
-    if (first >= end) return;
+    const int first = share * 4, step = a.shares * 4;              // (neighbours' blocks are neighbours, so that what a window hides is shared out evenly)
+    if (first >= blocks) return;
     const char* queries = (const char*)uniform((int64_t)((const char*)c.Q + ((int64_t)b * c.m * c.kv + head) * c.group * 256));
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(&Qs[0]) + wave * 8192);
 #pragma unroll
@@ -580,7 +588,10 @@ __global__ __launch_bounds__(256, 3) void weights_some_kernel(WeightsArgs a) {
     }
     const char* keys = (const char*)c.K + (int64_t)g * c.stride * 256;
     Many<true> next;
-    if (first + wave < end) next.load(keys + (int64_t)min((first + wave) * 32 + col, length - 1) * 256, half);
+    const auto ask = [&](int block) ALWAYS_INLINE {
+        if ((block < blocks) & any_sees(c, length, block * 32, block * 32 + 31)) next.load(keys + (int64_t)min(block * 32 + col, length - 1) * 256, half);
+    };
+    ask(first + wave);
     if (tid < 128) {                                               // of a row -lse in units of log 2, and its position (below all where it gives nothing)
         const int R = min(tid, a.rows - 1), token = a.by_group.of(R);
         const float lse = c.lse[(((int64_t)b * c.kv + head) * c.group + a.by_group.rest(R, token)) * c.m + token];
@@ -593,16 +604,17 @@ __global__ __launch_bounds__(256, 3) void weights_some_kernel(WeightsArgs a) {
     const int mine = (col & 15) / 4 * 8 + col % 4 + half * 4;      // the key of a block whose sum comes to this lane
     float* mass = c.mass + (int64_t)g * c.mass_stride;
 #pragma unroll 1
-    for (int block = first + wave; block < end; block += 4) {
+    for (int block = first + wave; block < blocks; block += step) {
         const int k0 = block * 32, j = k0 + mine;
         const Many<true> key = next;
-        if (block + 4 < end) next.load(keys + (int64_t)min(k0 + 128 + col, length - 1) * 256, half);
+        ask(block + step);
         const float old = mass[min(j, length - 1)];
         float sums[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) sums[i] = 0.f;
+        const int seen_tiles = any_sees(c, length, k0, k0 + 31) ? tiles : 0;
 #pragma unroll 1
-        for (int u = 0; u < tiles; ++u) {                          // (not unrolled: a launch of few blocks pays for the code that it fetches)
+        for (int u = 0; u < seen_tiles; ++u) {                     // (not unrolled: a launch of few blocks pays for the code that it fetches)
             const char* Qt = Qs + u * 8192;
             const float less = less_of[u * 32 + col];
             const int p = place_of[u * 32 + col];

@@ -3,15 +3,15 @@
 // sequences (R = (sequence, token, head)) stand side by side over its kept rows, which are read once for a tile of up to 256 of them, each
 // sequence's own over its tail, and a second kernel joins what they found.
 //
-// One launch: workgroups of tails (a sequence's KV head, 32 rows R, by four waves that take tiles of 32 keys in turn and are joined in LDS), then those of kept rows, which share out all heads'
-// tiles evenly, whatever the heads' lengths.  S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a
+// One launch: workgroups of tails (a sequence's KV head, 32 rows R, by four waves that take tiles of 32 keys in turn and are joined in LDS, or by one), then those of kept rows, which share out
+// all heads' tiles evenly, whatever the heads' lengths.  S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a
 // row, V read transposed, P from the registers that S^T leaves it in.  Four (eight) waves have 32 of 128 (256) rows each and all of a tile's 64 keys.  Rows in 4 bits are expanded on their way
 // into LDS, exactly.  fp32: mfma_f32_32x32x2, operands straight from memory.
 // Weights are rounded to bf16 for their product with V (half a step of 2^-8, as the values themselves have been); sums are of what was not rounded.
 //
 // Bound by: over long prefixes the products, whose power lowers the clock (64 sequences over 131072 kept rows of 8 heads, 137 GFLOP, 177 us: 780 TFLOP/s; 557 MB); in 4 bits the expansion,
 // which every 128 rows take anew (4 prompts of 13107 kept rows, 16 answers to each with up to 513 tokens, 124 MB, 59 us, of which the tails' 83 MB 13); over short ones the chain of two
-// launches, a few tiles and the join (16 answers over 3276 rows, 21 MB, 19 us).  fp32: 16 answers over 13107 rows 53 us, of which the products of 32 bits 25.
+// launches, a few tiles and the join (16 answers over 3276 rows, 21 MB, 18.4 us).  fp32: 16 answers over 13107 rows 53 us, of which the products of 32 bits 25.
 #include <algorithm>
 
 #include "attend_device.h"
@@ -32,11 +32,13 @@ struct SharedArgs {
     // this launch's slice: sequences s0 .. s0 + ns - 1 of prefixes b0 .. b0 + nb - 1, tokens t0 .. t0 + nt - 1
     int b0, nb, s0, ns, t0, nt;
     int rows, tile_rows, tiles;        // of a prefix's KV head: ns * nt * group, and tiles of tile_rows of them
+    int slot_rows;                     // of a part: a tile's, where there is but one no more than there are
     int shares;                        // workgroups that share out the kept rows
     int tail_tiles;                    // tiles of 32 of a sequence's nt * group rows
-    int64_t tails, tail_blocks;        // a workgroup of 512 threads has two
+    int tail_waves;                    // of a tail: four, or, where there are many tails, one
+    int64_t tails, tail_blocks;
     // un-normalised partial results of 128 floats a row, and their reference points and sums (sum 0: nothing seen, o not written): of share s and item i, (head, tile), at s + i, which
-    // no other pair has, [shares + items][tile_rows], then of the tails [nb * kv][rows]
+    // no other pair has, [shares + items][slot_rows], then of the tails [nb * kv][rows]
     float* part_o;
     f32x2a* part_ml;
     int32_t* part_of_item;             // the first and the last share that have tiles of an item (of a head without kept rows: not written)
@@ -232,6 +234,14 @@ __device__ __forceinline__ void store_part(const Wave& w, float* to, int half) {
             *(f32x4a*)(to + db * 32 + i * 8 + half * 4) = (f32x4a){w.o[db][4 * i], w.o[db][4 * i + 1], w.o[db][4 * i + 2], w.o[db][4 * i + 3]};
 }
 
+// That of a wave of its own.
+__device__ __forceinline__ void store_wave(const SharedArgs& a, const Wave& w, const Rows& r, int col, int half) {
+    const float sum = halves_sum(w.sum);
+    if (r.first + col >= r.end) return;
+    if (half == 0) a.part_ml[r.at + r.first + col] = (f32x2a){w.ref, sum};
+    if (sum != 0.f) store_part(w, a.part_o + (r.at + r.first + col) * 128, half);
+}
+
 // The parts of four waves (threads tid of them) over the same 32 rows R, through 16 KB of LDS each.
 __device__ __forceinline__ void join_waves(Wave& w, int tid, char* lds, f32x2a (*ml)[kTile], float* part_o, f32x2a* part_ml, const Rows& r) {
     const int wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
@@ -302,8 +312,9 @@ template <int LEFT>
 __device__ __forceinline__ void dma_wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LEFT) : "memory"); }      // all but the last LEFT
 __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// A tail's 32 rows R, by four waves (threads tid of them), each over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values
+// A tail's 32 rows R, by WAVES waves, four or one (threads tid of them), each over tiles of 32 keys of its own, of which the next one's keys are on their way while the weights are made, and its values
 // while they are.  Row R's token stands at p, the first row's at p_low.
+template <int WAVES>
 __device__ __forceinline__ void tail_rows(const SharedArgs& a, int tid, char* lds, uint32_t lds_at, f32x2a (*ml)[kTile], const char* K, const char* V, int end, int p, int p_low,
                                           const char* row, const Rows& r) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5, l16 = lane & 15;
@@ -322,15 +333,15 @@ __device__ __forceinline__ void tail_rows(const SharedArgs& a, int tid, char* ld
     w.begin(row, half);
 #pragma unroll
     for (int i = 0; i < 8; ++i) loaded(w.q[i]);
-    for (int tile = wave; tile < tiles; tile += 4) {
+    for (int tile = wave; tile < tiles; tile += WAVES) {
         const int j0 = tile * 32, count = count_of(tile);
-        const bool more = tile + 4 < tiles, hidden = count < 32 || j0 + 31 > p_low;
+        const bool more = tile + WAVES < tiles, hidden = count < 32 || j0 + 31 > p_low;
         dma_wait_but<8>();
         f32x16a s[1];
         uint32_t pb[8];
         w.scores<1, 2048>(Kt, col, half, s);
         lds_wait();
-        if (more) ask_k(tile + 4);
+        if (more) ask_k(tile + WAVES);
         if (hidden) hide<1>(s, last - j0 - half * 4);
         w.raise(w.top_of<1>(s, a.scale_log2));
 #pragma unroll
@@ -341,9 +352,10 @@ __device__ __forceinline__ void tail_rows(const SharedArgs& a, int tid, char* ld
         if (hidden) hidden_values(w, Vt, v_at, pb, last - j0 - half * 4, half, lane);
         else w.values<1, 2048, true>(Vt, v_at, pb);
         lds_wait();
-        if (more) ask_v(tile + 4);
+        if (more) ask_v(tile + WAVES);
     }
-    join_waves(w, tid, lds, ml, a.part_o, a.part_ml, r);
+    if constexpr (WAVES == 4) join_waves(w, tid, lds, ml, a.part_o, a.part_ml, r);
+    else store_wave(a, w, r, col, half);
 }
 
 // 32 SETS rows R, 32 a wave, tiles of 64 keys for all.  The next tile's products go with this one's exponentials between them,
@@ -561,7 +573,7 @@ __device__ __forceinline__ void each_item(const SharedArgs& a, int share, const 
     }
 }
 // Where the partial results of share s and (head g, row tile) begin.
-__device__ __forceinline__ int64_t part_of(const SharedArgs& a, int share, int g, int tile) { return ((int64_t)share + (int64_t)g * a.tiles + tile) * a.tile_rows; }
+__device__ __forceinline__ int64_t part_of(const SharedArgs& a, int share, int g, int tile) { return ((int64_t)share + (int64_t)g * a.tiles + tile) * a.slot_rows; }
 
 template <bool MX, int SETS>
 __global__ __launch_bounds__(SETS * 64, 2) void attend_shared_kernel(SharedArgs a) {
@@ -572,15 +584,17 @@ __global__ __launch_bounds__(SETS * 64, 2) void attend_shared_kernel(SharedArgs 
     const int tid = threadIdx.x, col = tid & 31;
     int token;
     if (blockIdx.x < a.tail_blocks) {
-        const int of = SETS > 4 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;       // (a tail takes four waves; the second of the last two may be none, and writes nothing)
-        const int64_t i = (int64_t)blockIdx.x * (SETS / 4) + of;
+        const int waves = a.tail_waves, of = __builtin_amdgcn_readfirstlane(tid >> 6) / waves;        // (the last tails may be none, and write nothing)
+        const int64_t i = (int64_t)blockIdx.x * (SETS / waves) + of;
         const Tail t = tail_of(a, (int)min(i, a.tails - 1));
         Rows r = rows_of_tail(a, t);
         if (i >= a.tails) r.end = r.first;
         const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 256;
         const int64_t from = (t.sequence * c.kv + t.head) * c.stride * 256;
-        tail_rows(a, tid & 255, lds + of * 65536, lds_at + of * 65536, ml + of * 4, (const char*)c.K + from, (const char*)c.V + from, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
-                  r);
+        const char *K = (const char*)c.K + from, *V = (const char*)c.V + from;
+        const int end = max(0, t.p_high + 1), p = t.length - c.m + token, at = of * waves * 16384;
+        if (waves == 4) tail_rows<4>(a, tid & 255, lds + at, lds_at + at, ml + of * 4, K, V, end, p, t.p_low, row, r);
+        else tail_rows<1>(a, tid & 63, lds + at, lds_at + at, nullptr, K, V, end, p, t.p_low, row, r);
         return;
     }
     // (neighbours in the list are neighbours in an XCD)
@@ -653,10 +667,10 @@ template <> struct Operands32<true> {
     }
 };
 
-template <bool MX, bool TAIL>
-__device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a (*ml)[kTile], const char* K, const char* V, const uint8_t* K_scales, const uint8_t* V_scales, int begin, int end,
+template <bool MX, bool TAIL, int WAVES>
+__device__ __forceinline__ void rows_f32(const SharedArgs& a, int tid, char* lds, f32x2a (*ml)[kTile], const char* K, const char* V, const uint8_t* K_scales, const uint8_t* V_scales, int begin, int end,
                                          int p, int p_low, const char* row, const Rows& r) {
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     typedef Operands32<MX> Operands;
     Operands from;
     f32x4a q[16];
@@ -668,7 +682,7 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
 #pragma unroll
     for (int s = 0; s < 16; ++s) q[s] = ((const f32x4a*)row)[Operands::kStep * s + Operands::kHalf * half];
 #pragma unroll 1
-    for (int tile = wave; tile < tiles; tile += 4) {
+    for (int tile = wave; tile < tiles; tile += WAVES) {
         const int j0 = begin + tile * 32, count = min(32, end - j0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) from.ask_values(V, V_scales, j0 + min(i / 4 * 8 + i % 4 + half * 4, count - 1), i, col);
@@ -683,7 +697,7 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
             for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[s][e], x, 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (tile + 4 < tiles) ask_keys(tile + 4);
+        if (tile + WAVES < tiles) ask_keys(tile + WAVES);
         const bool hidden = count < 32 || (TAIL && j0 + 31 > p_low);
         const int last = TAIL ? min(p, end - 1) : end - 1;
         if (hidden)
@@ -736,7 +750,8 @@ __device__ __forceinline__ void rows_f32(const SharedArgs& a, char* lds, f32x2a 
                             if (j0 + key <= last && odd(y[e])) w.o[db][n + e] += y[e];
                     }
     }
-    join_waves(w, tid, lds, ml, a.part_o, a.part_ml, r);
+    if constexpr (WAVES == 4) join_waves(w, tid, lds, ml, a.part_o, a.part_ml, r);
+    else store_wave(a, w, r, col, half);
 }
 
 template <bool MX>
@@ -747,18 +762,24 @@ __global__ __launch_bounds__(256) void attend_shared_f32_kernel(SharedArgs a) {
     const int col = threadIdx.x & 31;
     int token;
     if (blockIdx.x < a.tail_blocks) {
-        const Tail t = tail_of(a, blockIdx.x);
+        const int waves = a.tail_waves, of = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
+        const int64_t i = (int64_t)blockIdx.x * (4 / waves) + of;
+        const Tail t = tail_of(a, (int)min(i, a.tails - 1));
+        Rows r = rows_of_tail(a, t);
+        if (i >= a.tails) r.end = r.first;
         const char* row = (const char*)c.Q + query_row(a, t.bi, t.head, min(t.R0 + col, t.R1 - 1), &token) * 512;
         const int64_t at = (t.sequence * c.kv + t.head) * c.stride * 512;
-        rows_f32<false, true>(a, lds, ml, (const char*)c.K + at, (const char*)c.V + at, nullptr, nullptr, 0, max(0, t.p_high + 1), t.length - c.m + token, t.p_low, row,
-                              rows_of_tail(a, t));
+        const char *K = (const char*)c.K + at, *V = (const char*)c.V + at;
+        const int end = max(0, t.p_high + 1), p = t.length - c.m + token;
+        if (waves == 4) rows_f32<false, true, 4>(a, threadIdx.x, lds, ml, K, V, nullptr, nullptr, 0, end, p, t.p_low, row, r);
+        else rows_f32<false, true, 1>(a, threadIdx.x & 63, lds, ml, K, V, nullptr, nullptr, 0, end, p, t.p_low, row, r);
         return;
     }
     const int block = (int)(blockIdx.x - a.tail_blocks), eighth = a.shares >> 3, share = block < eighth * 8 ? (block & 7) * eighth + (block >> 3) : block;
     each_item(a, share, [&](int g, int tile, const Kept& k, int begin, int end) ALWAYS_INLINE {
         const char* row = (const char*)c.Q + query_row(a, a.by_kv.of(g), a.by_kv.rest(g, a.by_kv.of(g)), min(tile * kTile + col, a.rows - 1), &token) * 512;
         const int width = MX ? 64 : 512;
-        rows_f32<MX, false>(a, lds, ml, (const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row,
+        rows_f32<MX, false, 4>(a, threadIdx.x, lds, ml, (const char*)c.K_kept + k.at * width, (const char*)c.V_kept + k.at * width, c.K_scales + k.at * 4, c.V_scales + k.at * 4, begin, end, 0, 0, row,
                             {part_of(a, share, g, tile) - tile * kTile, tile * kTile, min(a.rows, (tile + 1) * kTile)});
     });
 }
@@ -779,14 +800,14 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(SharedArgs a) {
     float ref = last.y == 0.f ? kNoScore : last.x;
     const auto rows_of = [&](f32x2a (&x)[16], int base, int many) ALWAYS_INLINE {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = *(const f32x2a*)(a.part_o + (at + (int64_t)(base + min(e, many - 1)) * a.tile_rows) * 128 + lane * 2);
+        for (int e = 0; e < 16; ++e) x[e] = *(const f32x2a*)(a.part_o + (at + (int64_t)(base + min(e, many - 1)) * a.slot_rows) * 128 + lane * 2);
     };
     f32x2a x[16];
     if (any) rows_of(x, from, min(16, to - from + 1));
     f32x2a ml = {0, 0};
-    if (from + lane <= to) ml = a.part_ml[at + (int64_t)(from + lane) * a.tile_rows];
+    if (from + lane <= to) ml = a.part_ml[at + (int64_t)(from + lane) * a.slot_rows];
     if (ml.y != 0.f) ref = fmaxf(ref, ml.x);
-    for (int s = from + 64 + lane; s <= to; s += 64) ref = fmaxf(ref, a.part_ml[at + (int64_t)s * a.tile_rows].x);
+    for (int s = from + 64 + lane; s <= to; s += 64) ref = fmaxf(ref, a.part_ml[at + (int64_t)s * a.slot_rows].x);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
     float sum = 0.f;
@@ -795,7 +816,7 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(SharedArgs a) {
         const int s = base + lane;
         if (base > from) {
             ml = (f32x2a){0, 0};
-            if (s <= to) ml = a.part_ml[at + (int64_t)s * a.tile_rows];
+            if (s <= to) ml = a.part_ml[at + (int64_t)s * a.slot_rows];
         }
         const float weight = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
         sum += weight * ml.y;
@@ -844,16 +865,17 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
     // A slice's partial results, of its kept rows and its tails, have to lie in scratch: whole prefixes, else sequences of one, else tokens of one.  Rows R of a head fill tiles of
     // 32 to 256, and a share is a tile more.
     const int64_t room = (call.scratch_bytes - kScratchCounters) / (int64_t)(128 * sizeof(float) + sizeof(f32x2a));
-    const int64_t most = room - 1024;
+    // Half of it is for the shares' parts, as far as one token's rows leave that much (11 prompts of 2393 rows, 27 answers of 5 tokens each: 707 us in one slice of 118 shares, 141 in three).
+    const int64_t half = (room - 1024) / 2;
     const auto padded = [&](int64_t prefixes, int64_t sequences, int64_t tokens) {       // partial results of one share, and of the tails
         const int64_t rows = sequences * tokens * call.group, tile = !bf16 ? 32 : rows <= 128 ? 128 : 256;
-        return prefixes * call.kv * ((rows + tile - 1) / tile * tile + rows);
+        return prefixes * call.kv * ((rows <= tile ? rows : (rows + tile - 1) / tile * tile) + rows);
     };
     const auto fitting = [&](int64_t of, const auto& size) {       // the most of them that fit
         int64_t x = 1, y = of;                                     // x fits (cache_api.hip sees to one token of one sequence)
         while (x < y) {
             const int64_t z = (x + y + 1) / 2;
-            if (size(z) <= most) x = z;
+            if (size(z) <= half) x = z;
             else y = z - 1;
         }
         return x;
@@ -876,18 +898,22 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 const int sets = !bf16 ? 1 : a.rows <= 128 || tiles_a_head * heads * ((a.rows + 255) / 256) < 12 * (int64_t)ctx->num_cu ? 4 : 8;
                 a.tile_rows = sets * kTile;
                 a.tiles = (a.rows + a.tile_rows - 1) / a.tile_rows;
+                a.slot_rows = std::min(a.tile_rows, a.rows);
                 a.tail_tiles = (a.nt * call.group + kTile - 1) / kTile;
                 a.by_tail_tiles = Divisor(a.tail_tiles), a.by_ns = Divisor(a.ns), a.by_quads = Divisor((a.rows + 3) / 4);
                 a.tails = (int64_t)a.nb * a.ns * call.kv * a.tail_tiles;
-                a.tail_blocks = sets > 4 ? (a.tails + 1) / 2 : a.tails;
-                // Shares of the kept rows: four tiles of 64 keys each (two, up to 64 shares), up to a workgroup a unit; eight, up to two a unit (256 rows, and fp32, whose registers fill it: one),
+                // One wave a tail: where there is no more than a tile of it, or where tails keep all waves busy (7 prompts' 45 answers of up to 8 tokens 50 us by four waves, 31 by one; 16
+                // prompts' 16 of up to 130 86 and 76; 8 prompts' 16 of 500, half as many, 81 and 88).
+                a.tail_waves = call.n <= 32 || a.tails >= (call.n <= 256 ? 4 : 8) * (int64_t)ctx->num_cu ? 1 : 4;
+                a.tail_blocks = (a.tails * a.tail_waves + std::max(sets, 4) - 1) / std::max(sets, 4);
+                // Shares of the kept rows, by their cost: four tiles of 64 keys each (two, up to 64 shares), up to a workgroup a unit; eight, up to two a unit (256 rows, and fp32, whose registers fill it: one),
                 // as far as there is scratch.  (16 answers over 13107 rows: 28.3 us with four tiles up to two workgroups, 24.0 so; over 300 rows 18.6 with four tiles, 13.8 so; fp32, 13107
                 // rows: 66 with two workgroups, 53 so.)
-                const int64_t items = heads * a.tiles, tail_rows = heads * a.rows, tiles = tiles_a_head * items;
+                const int64_t items = heads * a.tiles, tail_rows = heads * a.rows, tiles = (tiles_a_head + kItemCost) * items;
                 const int64_t useful = std::max({std::min<int64_t>(64, tiles / 2), std::min<int64_t>(ctx->num_cu, tiles / 4), tiles / 8});
                 const int64_t units = (sets == 4 ? 2 : 1) * (int64_t)ctx->num_cu;
-                a.shares = (int)std::max<int64_t>(1, std::min({useful, units, (room - 1024 - tail_rows) / a.tile_rows - items}));
-                a.tail_at = (a.shares + items) * a.tile_rows;
+                a.shares = (int)std::max<int64_t>(1, std::min({useful, units, (room - 1024 - tail_rows) / a.slot_rows - items}));
+                a.tail_at = (a.shares + items) * a.slot_rows;
                 a.part_o = (float*)((char*)call.scratch + kScratchCounters);
                 a.part_ml = (f32x2a*)(a.part_o + (a.tail_at + tail_rows) * 128);
                 a.part_of_item = (int32_t*)(a.part_ml + a.tail_at + tail_rows);

@@ -18,7 +18,7 @@ int run_shared(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V
                               scale, out, lse, scratch, scratch_bytes);
     if (rc != CURDKV_OK) return rc;
     if (!scratch || scratch_bytes < CURDKV_ATTEND_SCRATCH_BYTES) return CURDKV_ERR_INVALID_ARG;
-    // (the partial results of one token of all heads lie in scratch together, those of a head's kept rows in tiles of 32 rows at least)
+    // (the partial results of one token of all heads lie in scratch together, those of a head's kept rows in tiles that are less than half empty: 3 * 2^14 rows of the 73728 that there are)
     if (c.kv > 1 << 10 || (int64_t)c.kv * c.group > 1 << 14) return CURDKV_ERR_UNSUPPORTED;
     return launch_attend_shared(ctx, c, (int)share, (hipStream_t)stream) == hipSuccess ? CURDKV_OK : CURDKV_ERR_HIP;
 }

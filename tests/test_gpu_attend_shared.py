@@ -341,3 +341,46 @@ def test_many_rows_over_long_prefixes(mx, share, kv, keep, m):
     # (tiles of 256 rows, two tails a workgroup, an odd number of them)
     rng = np.random.default_rng(share)
     check("bf16", mx, 1, share, kv, 4, m, keep - rng.integers(0, 70, kv), 40, rng.integers(0, 41, share), heads=2, seed=share)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMS)
+@pytest.mark.parametrize("count,share,kv,m,tail", [(3, 60, 4, 2, 9), (5, 60, 4, 1, 130), (2, 130, 8, 1, 33), (9, 33, 7, 1, 20)])
+def test_many_tails(dtype, mx, count, share, kv, m, tail):
+    # (a wave a tail, and of the last workgroup's waves some that have none)
+    rng = np.random.default_rng(share)
+    check(dtype, mx, count, share, kv, 4, m, rng.integers(0, 90, count * kv), tail, rng.integers(0, tail + 1, count * share), heads=2)
+
+
+@pytest.mark.parametrize("dtype,mx", FORMS)
+@pytest.mark.parametrize("kv,group,share,m", [(1024, 16, 2, 1), (1024, 1, 3, 2), (500, 17, 2, 2), (128, 128, 1, 1), (126, 129, 2, 1), (1, 16384, 1, 2)])
+def test_as_many_heads_as_there_may_be(dtype, mx, kv, group, share, m):
+    # (parts of rows fill what scratch there is: nothing beside the outputs is written, and the last heads' are right)
+    rng = np.random.default_rng(kv)
+    scratch = Guarded((B.ATTEND_SCRATCH_BYTES // 4,), torch.int32, 0)
+    dt, budgets = U.dtype_of(dtype), rng.integers(0, 70, kv)
+    off = np.concatenate([[0], np.cumsum(budgets)]).astype(np.int64)
+    total = int(off[-1])
+    Kk, Vk = U.randn(1, (total, D), dt), U.randn(2, (total, D), dt)
+    Kt, Vt = (U.randn(i, (share, kv, 6, D), dt) for i in (3, 4))
+    Q = U.randn(5, (share, m, kv * group, D), dt)
+    out = Guarded((share * m * kv * group, D), dt, float("nan"))
+    lse = Guarded((share * kv * group, m), torch.float32, float("nan"))
+    since = dict(K_tail=Kt, V_tail=Vt, tail_n=6, tail_stride=6, lse=lse.t, scratch=scratch.t)
+    with U.context(kv, group, dtype, 64) as ctx:
+        if mx:
+            Kc, Ks, Kk = pack(dtype, Kk)
+            Vc, Vs, Vk = pack(dtype, Vk)
+            ctx.attend_shared_mx(Q, Kc, Ks, Vc, Vs, torch.from_numpy(off).cuda(), 1, share, m, total, out.t, **since)
+        else:
+            ctx.attend_shared(Q, Kk, Vk, torch.from_numpy(off).cuda(), 1, share, m, total, out.t, **since)
+        torch.cuda.synchronize()
+    for x in (scratch, out, lse):
+        x.check()
+    got, got_lse = out.t.view(share, m, kv * group, D), lse.t.view(share, kv * group, m)
+    assert not bool(got.isnan().any()) and not bool(got_lse.isnan().any())
+    for h in sorted({0, 1, kv * group // 2, kv * group - 2, kv * group - 1} & set(range(kv * group))):
+        k = torch.cat([Kk[off[h // group]:off[h // group + 1]].double(), Kt[share - 1, h // group].double()])
+        v = torch.cat([Vk[off[h // group]:off[h // group + 1]].double(), Vt[share - 1, h // group].double()])
+        seen = torch.cat([torch.ones((m, k.shape[0] - 6), dtype=torch.bool, device="cuda"), U.causal(m, 6, 6, 0, 0)], 1)
+        want = U.attention(Q[share - 1, :, h], k, v, seen, D ** -0.5)
+        U.check_attention(got[share - 1, :, h], got_lse[share - 1, h], want, dtype, k.shape[0] + 64, f"head {h}")

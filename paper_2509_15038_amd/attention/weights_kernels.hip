@@ -697,10 +697,10 @@ hipError_t launch_weights(const curdkv_ctx* ctx, const WeightsCall& call, hipStr
     a.key_tiles = (call.n + keys - 1) / keys;
     a.most = (int)(((int64_t)1 << 31) / (call.kv * (bf16 ? 256 : 512)) / stage);
     // Two workgroups a unit, each with an equal share of a head's products, where tiles of keys would leave units idle at the end; their sums lie in scratch, as far as there is any.
-    // (1021 tokens over 1021: 22 us so, 85 by tiles; 2000 over 2000: 45 and 146.  Up to two stages of rows there is little to share.)
+    // (1021 tokens over 1021: 22 us so, 85 by tiles; 2000 over 2000: 45 and 146.  Up to four stages of rows there is little to share: 100 tokens over 8000 24.7 so, 17.3 by tiles.)
     const int64_t tiles = (int64_t)a.groups * a.key_tiles, room = call.scratch ? (call.scratch_bytes - kScratchCounters) / (a.groups * (int64_t)keys * 4) - a.key_tiles : 0;
     const int64_t shares = std::min(std::min<int64_t>(2 * (int64_t)ctx->num_cu / a.groups, room), std::max<int64_t>(1, (int64_t)((a.rows + stage - 1) / stage) * a.key_tiles));
-    a.shares = tiles < 2 * (int64_t)ctx->num_cu && a.rows > 2 * stage && shares > 1 ? (int)shares : 0;
+    a.shares = tiles < 2 * (int64_t)ctx->num_cu && a.rows > 4 * stage && shares > 1 ? (int)shares : 0;
     a.part = (float*)((char*)call.scratch + kScratchCounters);
     const auto launch = [&](auto kernel, int64_t n) { kernel<<<(unsigned)n, 256, 0, stream>>>(a); };
     const int64_t blocks = a.shares ? (int64_t)a.groups * a.shares : tiles;

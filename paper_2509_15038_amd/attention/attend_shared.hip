@@ -185,9 +185,6 @@ __device__ __forceinline__ void hide(f32x16a (&s)[KB], int far) {
 __device__ __forceinline__ int permuted(int piece, int row, int column, bool keys, int keys_of_tile) {
     return piece ^ (keys_of_tile == 64 ? column : 0) ^ (keys ? (row >> 1) & 3 : 0);
 }
-__device__ __forceinline__ uint32_t piece_at(int row, int column, int piece, bool keys, int keys_of_tile) {
-    return column * (keys_of_tile * 64) + row * 64 + (permuted(piece, row, column, keys, keys_of_tile) << 4);
-}
 // 1 KB blocks of 16 rows' columns, block first .. first + COUNT - 1 of a tile, straight into LDS.
 template <int KEYS, int COUNT>
 __device__ __forceinline__ void fetch_bf16(uint32_t lds, const char* rows, int count, bool keys, int first, int lane) {
@@ -199,23 +196,17 @@ __device__ __forceinline__ void fetch_bf16(uint32_t lds, const char* rows, int c
         dma16(lds + block * 1024, rows, min(row, count - 1) * 256 + column * 64 + (permuted(lane & 3, row, column, keys, KEYS) << 4));
     }
 }
-// Rows in 4 bits: a lane's share of a tile, 16 or 32 bytes of codes of one row, and its scales.
-template <int BLOCKS>
+// Rows in 4 bits: a lane's share of a tile of 64 keys, a column of one row in 16 bytes of codes, and its scale.
 struct Codes {
-    u32x4a codes[BLOCKS];
-    uint32_t scales[BLOCKS];
-    __device__ __forceinline__ void load(const uint8_t* rows, const uint8_t* scale, int64_t row, int column) {
-#pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) {
-            codes[i] = *(const u32x4a*)(rows + row * 64 + (column + i) * 16);
-            scales[i] = scale[row * 4 + column + i];
-        }
+    u32x4a codes;
+    uint32_t scale;
+    __device__ __forceinline__ void load(const uint8_t* rows, const uint8_t* scales, int64_t row, int column) {
+        codes = *(const u32x4a*)(rows + row * 64 + column * 16);
+        scale = scales[row * 4 + column];
     }
-    __device__ __forceinline__ void store(char* tile, int row, int column, bool keys, int keys_of_tile) const {
+    __device__ __forceinline__ void store(char* tile, int row, int column, bool keys) const {
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i)
-#pragma unroll
-            for (int p = 0; p < 4; ++p) *(u32x4a*)(tile + piece_at(row, column + i, p, keys, keys_of_tile)) = eight_bf16(codes[i][p], unit_of(scales[i]));
+        for (int p = 0; p < 4; ++p) *(u32x4a*)(tile + (uint32_t)(column * 4096 + row * 64 + (permuted(p, row, column, keys, 64) << 4))) = eight_bf16(codes[p], unit_of(scale));
     }
 };
 
@@ -377,15 +368,15 @@ __device__ __forceinline__ void kept_rows_of(const SharedArgs& a, char* lds, uin
                                    wave * (16 / W), lane);
     };
     // 4 bits: a thread's 32 channels of a row of K, and of V (of eight waves, four take K and four V), into registers and from there into LDS
-    Codes<1> codes[W == 8 ? 1 : 2];
+    Codes codes[W == 8 ? 1 : 2];
     const int my_row = (tid & 255) >> 2, column = tid & 3;
-    const auto load = [&](Codes<1>& x, bool keys, int tile) ALWAYS_INLINE {
+    const auto load = [&](Codes& x, bool keys, int tile) ALWAYS_INLINE {
         const int t = min(tile, tiles - 1);
         const int64_t at = begin + t * 64 + min(my_row, count_of(t) - 1);
         x.load((const uint8_t*)(keys ? K : V), keys ? K_scales : V_scales, at, column);
     };
-    const auto store = [&](const Codes<1>& x, bool keys, int tile) ALWAYS_INLINE {
-        if (tile < tiles) x.store(lds + (tile & 1) * 16384 + (keys ? 0 : 32768), my_row, column, keys, 64);
+    const auto store = [&](const Codes& x, bool keys, int tile) ALWAYS_INLINE {
+        if (tile < tiles) x.store(lds + (tile & 1) * 16384 + (keys ? 0 : 32768), my_row, column, keys);
     };
     const auto ask_both = [&](int tile) ALWAYS_INLINE {            // K of tile + 1, V of tile
         if constexpr (MX && W == 8) {
@@ -420,7 +411,7 @@ __device__ __forceinline__ void kept_rows_of(const SharedArgs& a, char* lds, uin
     // (begin < end)
     {
         if constexpr (MX) {
-            Codes<1> k;
+            Codes k;
             if (W == 4 || wave < 4) load(k, true, 0);
             ask_both(0);
             if (W == 4 || wave < 4) store(k, true, 0);
@@ -612,7 +603,7 @@ __global__ __launch_bounds__(SETS * 64, 2) void attend_shared_kernel(SharedArgs 
 // ---- fp32: a wave's 32 rows R, 32 keys at a time, operands straight from memory; the four waves take tiles in turn and are joined.  A wave has a unit to itself and 512 registers: a tile's
 // values are on their way while its scores are made, and the next one's keys while the values are used.
 
-// 32 keys' operands: of QK the channels that `key` has at steps 0 .. 15 in either half, `channel` being the first of step 0; of PV channel 32 db + lane % 32 of key i / 4 * 8 + i % 4 + 4 half.
+// 32 keys' operands: of QK, at steps 0 .. 15, the channels of four number kStep step + kHalf half; of PV channel 32 db + lane % 32 of key i / 4 * 8 + i % 4 + 4 half.
 template <bool MX> struct Operands32;
 template <> struct Operands32<false> {
     static constexpr int kHalf = 1, kStep = 2;                     // fours of channels from half to half, and from step to step
@@ -863,7 +854,7 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
     a.share = share;
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16, mx = call.K_scales != nullptr;
     // A slice's partial results, of its kept rows and its tails, have to lie in scratch: whole prefixes, else sequences of one, else tokens of one.  Rows R of a head fill tiles of
-    // 32 to 256, and a share is a tile more.
+    // 128 or 256 (fp32: 32), and a share is a tile more.
     const int64_t room = (call.scratch_bytes - kScratchCounters) / (int64_t)(128 * sizeof(float) + sizeof(f32x2a));
     // Half of it is for the shares' parts, as far as one token's rows leave that much (11 prompts of 2393 rows, 27 answers of 5 tokens each: 707 us in one slice of 118 shares, 141 in three).
     const int64_t half = (room - 1024) / 2;
@@ -906,9 +897,9 @@ hipError_t launch_attend_shared(const curdkv_ctx* ctx, const AttendCall& call, i
                 // prompts' 16 of up to 130 86 and 76; 8 prompts' 16 of 500, half as many, 81 and 88).
                 a.tail_waves = call.n <= 32 || a.tails >= (call.n <= 256 ? 4 : 8) * (int64_t)ctx->num_cu ? 1 : 4;
                 a.tail_blocks = (a.tails * a.tail_waves + std::max(sets, 4) - 1) / std::max(sets, 4);
-                // Shares of the kept rows, by their cost: four tiles of 64 keys each (two, up to 64 shares), up to a workgroup a unit; eight, up to two a unit (256 rows, and fp32, whose registers fill it: one),
-                // as far as there is scratch.  (16 answers over 13107 rows: 28.3 us with four tiles up to two workgroups, 24.0 so; over 300 rows 18.6 with four tiles, 13.8 so; fp32, 13107
-                // rows: 66 with two workgroups, 53 so.)
+                // Shares of the kept rows, by their cost: four tiles of 64 keys each (two, up to 64 shares), up to a workgroup a unit; eight, up to two a unit (256 rows, and fp32, whose registers
+                // fill it: one), as far as there is scratch.  (16 answers over 13107 rows: 28.3 us with four tiles up to two workgroups, 24.0 so; over 300 rows 18.6 with four tiles, 13.8 so;
+                // fp32, 13107 rows: 66 with two workgroups, 53 so.)
                 const int64_t items = heads * a.tiles, tail_rows = heads * a.rows, tiles = (tiles_a_head + kItemCost) * items;
                 const int64_t useful = std::max({std::min<int64_t>(64, tiles / 2), std::min<int64_t>(ctx->num_cu, tiles / 4), tiles / 8});
                 const int64_t units = (sets == 4 ? 2 : 1) * (int64_t)ctx->num_cu;

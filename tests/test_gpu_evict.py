@@ -233,3 +233,29 @@ def test_another_stream():
 
 def test_many_heads():
     check("bf16", 300, 4, 70, 64, 2, 8, lengths=np.arange(300) % 71)
+
+
+@pytest.mark.parametrize("n,keep", [(900, 100), (5000, 4998), (40000, 4000), (220000, 50000)])
+def test_recorded_calls_of_all_sizes(n, keep):
+    # (short heads, few that leave, a long head, one whose bitmaps need more LDS than a launch has by itself), weights changed between the replays
+    K, V = (U.randn(i, (1, 2, n, D), torch.bfloat16) for i in (1, 2))
+    mass = torch.empty((1, 2, n), device="cuda")
+    outs = [[torch.zeros((1, 2, keep, D), dtype=torch.bfloat16, device="cuda") for _ in "KV"] + [torch.zeros((1, 2, keep), device="cuda"),
+                                                                                                   torch.zeros((1, 2, keep), dtype=torch.int32, device="cuda"),
+                                                                                                   torch.zeros((1, 2, keep), dtype=torch.int32, device="cuda")] for _ in range(2)]
+    with U.context(2, 1, "bf16", n) as ctx:
+        def call(out):
+            ctx.evict(K, V, mass, 1, n, n, keep, out[4], n_sink=4, recent=16, K_out=out[0], V_out=out[1], mass_out=out[2], positions_out=out[3], out_stride=keep)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(outs[0])
+        for turn in range(3):
+            mass.copy_(U.randn(10 + turn, (1, 2, n), torch.float32).exp())
+            call(outs[1])
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(*outs):
+                assert torch.equal(a, b)
+            rows = want_rows(mass[0, 1].cpu().numpy(), np.arange(n), n, keep, 4, 16)
+            assert np.array_equal(outs[0][4][0, 1].cpu().numpy(), rows)

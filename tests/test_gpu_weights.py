@@ -223,3 +223,24 @@ def test_another_stream():
 def test_which_kernel_takes_few_rows_of_long_caches(m, n, kv, group, count, window, sinks):
     # (few rows over few keys, over many, past the caches; up to 128 rows)
     check("bf16", count=count, kv=kv, group=group, m=m, n=n, window=window, sinks=sinks, decay=0.5, seed=m + n)
+
+
+@pytest.mark.parametrize("dtype,m,n", [("bf16", 1, 500), ("bf16", 1, 70000), ("bf16", 8, 3000), ("bf16", 300, 300), ("bf16", 200, 5000), ("fp32", 3, 900), ("fp32", 150, 700)])
+def test_recorded_calls_of_all_kernels(dtype, m, n):
+    kv, group, dt = 4, 4, U.dtype_of(dtype)
+    K, Q = U.randn(1, (1, kv, n, D), dt), U.randn(2, (1, m, kv * group, D), dt)
+    lse = torch.full((1, kv * group, m), 6.0, device="cuda")
+    recorded, eager = torch.zeros((2, 1, kv, n), device="cuda")
+    with U.context(kv, group, dtype, n) as ctx:
+        ctx.attend_weights(Q, K, lse, 1, m, n, n, eager, decay=0.0)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.attend_weights(Q, K, lse, 1, m, n, n, recorded, decay=0.5)
+        for turn in range(3):
+            Q.copy_(U.randn(20 + turn, Q.shape, dt))
+            eager.copy_(recorded)
+            ctx.attend_weights(Q, K, lse, 1, m, n, n, eager, decay=0.5)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(recorded, eager) and bool((recorded[..., 0] > 0).all())

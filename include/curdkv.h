@@ -380,9 +380,9 @@ int curdkv_rotate_axes(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t 
  * A whole prompt's weights are m = n; those that its last tokens give it (an observation window) fewer; a
  * generated token's m = 1.
  * Q, K, count, m, n, stride, lengths, window, n_sink, scale: as curdkv_attend takes them; lse: float [count,
- *   kv_heads*group_size, m], what curdkv_attend wrote for them.  A token of lse -infinity (it sees nothing) gives
- *   nothing, but to keys of score NaN or +infinity; one of lse NaN makes the weight of the keys that it sees NaN, and no
- *   other's.
+ *   kv_heads*group_size, m], what curdkv_attend wrote for them.  A token of lse -infinity (it sees nothing,
+ *   or is left out, as padding) gives nothing to any key, whatever its queries and the keys hold; one of lse NaN makes the
+ *   weight of the keys that it sees NaN, and no other's.
  * decay: not negative, finite; 0: the old weights are not read.
  * kv_heads <= 16384, kv_heads*group_size <= 2^20.
  * mass: float [count, kv_heads, mass_stride], rows below a sequence's length written; those behind it stay as they

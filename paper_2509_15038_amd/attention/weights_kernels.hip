@@ -296,7 +296,7 @@ __device__ __forceinline__ void spread(float (&x)[N], int lane) {
 
 // Stages from .. to - 1 of a tile of keys; `more`: the same workgroup has written this tile's sums before.
 template <bool BF16>
-__device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[32768], float (*Ls)[Many<BF16>::kTiles * 32], int* odd, int g, int b, int head, int length, int key_tile, int begin,
+__device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[32768], float (*Ls)[Many<BF16>::kTiles * 32], int (*odd)[2], int g, int b, int head, int length, int key_tile, int begin,
                                             int stages, float* part, bool more) {
     typedef Many<BF16> M;
     constexpr int kKeys = M::kBlocks * 32, kTiles = M::kTiles, kStage = kTiles * 32;
@@ -344,7 +344,7 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
     };
     const auto arrive = [&](int stage) ALWAYS_INLINE {
         if constexpr (!BF16) {
-            if (tid == 0) odd[stage & 1] = 0;
+            if (tid == 0) odd[stage & 1][0] = 0;
             __syncthreads();                                       // (nobody reads the stage before any more)
             bool mine = false;
             char* to = Qs[0] + (my_row >> 5) * 8192 + (tid & 3) * 2048 + (my_row & 31) * 64;
@@ -356,9 +356,12 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
                 *(u32x4a*)(to + 16384 + of) = p.m;
                 *(u32x4a*)(to + 32768 + of) = p.l;
             }
-            if (mine) odd[stage & 1] = 1;
+            if (mine) odd[stage & 1][0] = 1;
         }
-        if (tid < kStage) Ls[stage & 1][tid] = next_less == -INFINITY ? -INFINITY : -next_less * (1.f / kLn2);     // (a row that sees nothing weighs nothing)
+        if (tid < kStage) {
+            Ls[stage & 1][tid] = next_less == -INFINITY ? -INFINITY : -next_less * (1.f / kLn2);
+            if constexpr (BF16) odd[stage & 1][wave] = __any(next_less == -INFINITY);
+        }
         if constexpr (BF16) dma_wait();
         __syncthreads();
     };
@@ -418,7 +421,7 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
                         q[i & 1] = {*(const u32x4a*)from, *(const u32x4a*)(from + 16384), *(const u32x4a*)(from + 32768)};
                     };
                     read(0);
-                    if (!keys[0].odd && odd[stage & 1] == 0) {
+                    if (!keys[0].odd && odd[stage & 1][0] == 0) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             if (i < 7) read(i + 1);
@@ -455,17 +458,19 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
         for (int kb = 0; kb < M::kBlocks; ++kb)
 #pragma unroll
             for (int i = 0; i < 8; ++i) loaded(keys[kb].x[i]);
+    // A row that gives nothing (lse -infinity) does so whatever its scores are, NaN and infinities among them: a stage that has one goes with masks (to look costs 3 us of a prompt of 8192
+    // tokens' 290; with the next stage asked for between the look and the branch 2, but 31 us become 40 in fp32, by spills).
+    const auto all_give = [&](int stage) ALWAYS_INLINE { return !BF16 || __builtin_amdgcn_readfirstlane(odd[stage & 1][0] | odd[stage & 1][1]) == 0; };
     int stage = 0;
 #pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {                         // stages with masks, whole ones, some with masks again
-        const int until = turn == 0 ? min(whole_from, stages) : stages;
+    while (stage < stages) {                                       // stages with masks, whole ones, some with masks again
 #pragma unroll 1
-        for (; stage < until; ++stage) {
+        for (; stage < stages && (stage < whole_from || stage >= whole_to || !all_give(stage)); ++stage) {
             if (stage + 1 < stages) ask(stage + 1);
             if (stage >= seen_from && stage < seen_to) masked_stage(stage);
             if (stage + 1 < stages) arrive(stage + 1);
         }
-        if (turn == 1 || stage >= whole_to) continue;
+        if (stage >= stages) break;
         if constexpr (BF16) {
             // The scores of one tile wait for the next one's products, between which their exponentials go: two products, of either 32 keys, then two scores' of each.
             f32x16a s[2][2];
@@ -492,7 +497,7 @@ __device__ __forceinline__ void tile_stages(const WeightsArgs& a, char (*Qs)[327
                 }
             };
 #pragma unroll 1
-            for (; stage < whole_to; ++stage) {
+            for (; stage < whole_to && all_give(stage); ++stage) {
                 if (stage + 1 < stages) ask(stage + 1);
                 const char* Qt = Qs[stage & 1];
                 read(Qt, 0);
@@ -536,7 +541,7 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsArgs a) {
     constexpr int kKeys = Many<BF16>::kBlocks * 128, kStage = Many<BF16>::kTiles * 32;
     __shared__ __attribute__((aligned(16))) char Qs[2][32768];
     __shared__ float Ls[2][kStage];                                // -lse of a stage's rows, in units of log 2
-    __shared__ int odd[2];                                         // (fp32) whether a stage's rows hold an infinity or NaN
+    __shared__ int odd[2][2];                                      // of a stage: whether its rows hold an infinity or NaN (fp32), whether some of its halves' rows give nothing (bf16)
     const WeightsCall& c = a.c;
     // Neighbours in a head are neighbours in an XCD, whose caches then hold one head's queries.
     const int at = a.by_groups.of(blockIdx.x), g = a.by_groups.rest(blockIdx.x, at), b = a.by_kv.of(g), head = a.by_kv.rest(g, b), length = length_of(c, b);

@@ -34,8 +34,8 @@ int check_kept(const curdkv_ctx* ctx, AttendCall* to, const void* Q, const void*
                const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail, const void* V_tail, int64_t tail_n, int64_t tail_stride,
                const int32_t* tail_lengths, int64_t count, int64_t share, int64_t m, float scale, void* out, float* lse, void* scratch, int64_t scratch_bytes) {
     if (count < 1 || share < 1) return CURDKV_ERR_INVALID_ARG;
-    if (share > ((1LL << 31) - 1) / count) return CURDKV_ERR_UNSUPPORTED;
-    const int rc = check_attend(ctx, Q, out, count * share, m, tail_n, tail_stride, scale, scratch, scratch_bytes);
+    const int64_t most = 1LL << 31, sequences = share <= most / count ? count * share : most;      // (as many are too many, which is said once all else is right)
+    const int rc = check_attend(ctx, Q, out, sequences, m, tail_n, tail_stride, scale, scratch, scratch_bytes);
     if (rc != CURDKV_OK) return rc;
     if (!offsets || total < 0 || rows < 0 || rows > total || (total > 0 && (!K_kept || !V_kept)) || (tail_n > 0 && (!K_tail || !V_tail))) return CURDKV_ERR_INVALID_ARG;
     if (!aligned16({K_kept, V_kept, K_tail, V_tail})) return CURDKV_ERR_INVALID_ARG;

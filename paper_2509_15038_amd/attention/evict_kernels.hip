@@ -25,6 +25,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 4096, kFineBins = 1024;      // 12 bits of a key, then 10, then 10
 constexpr int kListed = 2048;                      // keys of one bin that are kept apart
 constexpr int kMostMoved = 128;                    // rows that the selection moves itself, in place (24 of 3300 of 256 heads 14.7 us, 53.6 by another kernel; 100 of 1001 of 64 heads 11.9, 15.3)
+constexpr size_t kOwnLds = 24 * 1024;              // what the selection's arrays of fixed size take at most
 constexpr int kFewLeave = 8;                       // rows that are found one by one (of 256 heads of some 3280: one 8.5 us, 13.6 by digits; four 10.3, 14.1; eight 11.0, 12.1)
 
 // Larger is better: 0 for what is none, weights in order, -0 as 0, NaN above all, and above that the protected.
@@ -491,7 +492,8 @@ hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_
     EvictCall select = call;
     select.moves = call.K_out == call.K && call.n - call.keep <= kMostMoved;       // (in place; no more rows move than leave)
     const auto launch = [&](auto kernel) {
-        const hipError_t e = lds <= 48 * 1024 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kEvictMostRows / 64 * 16));
+        // (with the kernel's own arrays, 17.7 KB, a launch of up to 64 KB needs no leave for more: heads of up to 163840 rows)
+        const hipError_t e = lds + kOwnLds <= 64 * 1024 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(kEvictMostRows / 64 * 16));
         if (e == hipSuccess) kernel<<<heads, kThreads, lds, stream>>>(select);
         return e;
     };
@@ -503,7 +505,7 @@ hipError_t launch_evict(const curdkv_ctx* ctx, const EvictCall& call, hipStream_
     const int keep = call.keep < call.n ? call.keep : call.n;
     const bool bf16 = call.dtype == CURDKV_DTYPE_BF16;
     const int blocks = bf16 ? (keep + 15) / 16 : (keep + 7) / 8;
-    // (at most 2^20 heads of 2^15 workgroups: whole heads a launch)
+    // (at most 2^20 heads of 2^15 workgroups, in fp32 2^16: whole heads a launch)
     for (unsigned h = 0; h < heads;) {
         const unsigned some = (unsigned)((kMostBlocks / blocks) < heads - h ? kMostBlocks / blocks : heads - h);
         EvictCall part = call;

@@ -384,10 +384,11 @@ int curdkv_rotate_axes(curdkv_ctx* ctx, const void* qkv, int64_t count, int64_t 
  *   or is left out, as padding) gives nothing to any key, whatever its queries and the keys hold; one of lse NaN makes the
  *   weight of the keys that it sees NaN, and no other's.
  * decay: not negative, finite; 0: the old weights are not read.
- * kv_heads <= 16384, kv_heads*group_size <= 2^20.
+ * kv_heads <= 16384, kv_heads*group_size <= 2^20, ceil(n/64)*count*kv_heads < 2^24.
  * mass: float [count, kv_heads, mass_stride], rows below a sequence's length written; those behind it stay as they
  *   are.  n <= mass_stride.
- * Scores and sums in 32 bits, summed in an order that depends on the sizes alone.  scratch as in curdkv_attend. */
+ * Scores and sums in 32 bits, summed in an order that the sizes, lengths, window, scratch_bytes and the device's number of
+ * compute units give, and nothing else: the same call gives the same bits.  scratch as in curdkv_attend. */
 int curdkv_attend_weights(curdkv_ctx* ctx, const void* Q, const void* K, const float* lse, int64_t count,
                           int64_t m, int64_t n, int64_t stride, const int32_t* lengths, int64_t window, int32_t n_sink,
                           float scale, float decay, float* mass, int64_t mass_stride, void* scratch,
@@ -400,7 +401,8 @@ int curdkv_attend_weights(curdkv_ctx* ctx, const void* Q, const void* K, const f
  * A row below `keep` that stays keeps its place; the places of the others are taken, in ascending order, by the rows that
  * stay from beyond, ascending: rows are no longer in the order of their tokens, and `positions` says which is which.
  * K, V: [count, kv_heads, stride, head_dim]; mass: float, positions: int32 [count, kv_heads, stride]; positions NULL: the
- *   row's number.  lengths: int32 [count], clamped to [0, n]; NULL = n.  1 <= keep <= 2^30, n <= stride, n <= 524288.
+ *   row's number.  lengths: int32 [count], clamped to [0, n]; NULL = n.  1 <= keep <= 2^30, n <= stride, n <= 524288,
+ *   count*kv_heads <= 2^20.
  * K_out, V_out: [count, kv_heads, out_stride, head_dim]; mass_out, positions_out: [count, kv_heads, out_stride], NULL: not
  *   written.  Only rows below min(length, keep) are written.  keep <= out_stride or n <= out_stride.
  *   K_out = K with V_out = V: in place, and mass_out may be mass, positions_out positions; wherever an array is its own
@@ -419,7 +421,10 @@ int curdkv_evict(curdkv_ctx* ctx, const void* K, const void* V, const float* mas
  * K_tail, V_tail: [count*share, kv_heads, tail_stride, head_dim]; tail_lengths: int32 [count*share].
  * count*share*m*kv_heads*group_size < 2^31, kv_heads*group_size <= 16384, kv_heads <= 1024.  scratch: not NULL here,
  * CURDKV_ATTEND_SCRATCH_BYTES at least, cleared once as for curdkv_attend; the partial results of prefixes and tails meet
- * there. */
+ * there.
+ * The kept rows are shared out over the device, a tail is not: one workgroup reads all of a sequence's KV head.  It is made
+ * for tails that are short beside the prefix; where a few sequences have thousands of tokens of their own,
+ * curdkv_attend_kept, which shares tails out too, is the faster call (and needs the kept rows once for every sequence). */
 int curdkv_attend_shared(curdkv_ctx* ctx, const void* Q, const void* K_kept, const void* V_kept,
                          const int64_t* offsets, int64_t total, int64_t rows, const void* K_tail,
                          const void* V_tail, int64_t tail_n, int64_t tail_stride, const int32_t* tail_lengths,

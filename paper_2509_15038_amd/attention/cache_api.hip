@@ -46,7 +46,7 @@ int curdkv_attend_weights(curdkv_ctx* ctx, const void* Q, const void* K, const f
     if (rc != CURDKV_OK) return rc;
     if (!K || !lse || !mass || n < 1 || m > ctx->cfg.max_tokens || window < 0 || n_sink < 0 || mass_stride < n || !aligned16({K})) return CURDKV_ERR_INVALID_ARG;
     if (!(decay >= 0.f) || !std::isfinite(decay)) return CURDKV_ERR_INVALID_ARG;
-    if ((n + 63) / 64 > kMostBlocks / (count * ctx->cfg.kv_heads)) return CURDKV_ERR_UNSUPPORTED;      // (more rows than the memory holds)
+    if ((n + 63) / 64 > kMostBlocks / (count * ctx->cfg.kv_heads)) return CURDKV_ERR_UNSUPPORTED;      // (workgroups of a launch)
     if (ctx->cfg.kv_heads > 1 << 14 || (int64_t)ctx->cfg.kv_heads * ctx->cfg.group_size > 1 << 20) return CURDKV_ERR_UNSUPPORTED;      // (offsets among a few tokens' queries have 32 bits)
     WeightsCall c{};
     c.Q = Q, c.K = K, c.lse = lse, c.count = count, c.stride = stride;

@@ -427,7 +427,10 @@ class Context:
         """positions: int32 [axes, count*m] on the device; axis_of: a host array, uint8 [head_dim/2]; all else as for rotate."""
         assert isinstance(axis_of, np.ndarray) and axis_of.dtype == np.uint8 and axis_of.size == self.cfg.head_dim // 2 and axis_of.flags.c_contiguous, \
             f"expected a contiguous array of {self.cfg.head_dim // 2} uint8"
-        rc = _attend.rotate_axes(self._address, qkv, count, m, self._row if row_stride is None else row_stride, starts, positions, positions.shape[0],
+        axes = positions.shape[0] if len(positions.shape) else 0
+        each = positions.numel() // axes if axes else 0             # (of one axis, those behind the tokens' are not looked at)
+        assert each == count * m or (axes == 1 and each > count * m), f"expected positions of [axes, {count * m}], not {list(positions.shape)}"
+        rc = _attend.rotate_axes(self._address, qkv, count, m, self._row if row_stride is None else row_stride, starts, positions, axes,
                                  _host_ptr(axis_of), table, table.shape[0], q_weight, k_weight, float(eps), 1 if pairs else 0, Q, K, V, stride, stream)
         if rc != OK:
             raise CurdkvError(rc, "curdkv_rotate_axes")

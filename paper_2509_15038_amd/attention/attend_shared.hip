@@ -7,11 +7,15 @@
 // all heads' tiles evenly, whatever the heads' lengths.  S^T = K Q^T and O^T = V^T P^T by mfma_f32_32x32x16_bf16, operands and layout of the tiles in LDS as in attend_prompt.hip: columns of 64 bytes a
 // row, V read transposed, P from the registers that S^T leaves it in.  Four (eight) waves have 32 of 128 (256) rows each and all of a tile's 64 keys.  Rows in 4 bits are expanded on their way
 // into LDS, exactly.  fp32: mfma_f32_32x32x2, operands straight from memory.
-// Weights are rounded to bf16 for their product with V (half a step of 2^-8, as the values themselves have been); sums are of what was not rounded.
+// Weights are rounded to bf16 for their product with V (by up to 2^-8 of themselves, as the values have been and the result will be: 0.0021 to 0.0023 of the result in all, root mean square, 0.0016
+// to 0.0017 without); sums are of what was not rounded.
 //
-// Bound by: over long prefixes the products, whose power lowers the clock (64 sequences over 131072 kept rows of 8 heads, 137 GFLOP, 177 us: 780 TFLOP/s; 557 MB); in 4 bits the expansion,
-// which every 128 rows take anew (4 prompts of 13107 kept rows, 16 answers to each with up to 513 tokens, 124 MB, 59 us, of which the tails' 83 MB 13); over short ones the chain of two
-// launches, a few tiles and the join (16 answers over 3276 rows, 21 MB, 18.4 us).  fp32: 16 answers over 13107 rows 53 us, of which the products of 32 bits 25.
+// Bound by: over long prefixes the products, for 42 % of the clocks, which wait for tiles and exponentials, and, for a fifth, the power that lowers the clock to 1.9 to 2.1 GHz (64 sequences
+// over 131072 kept rows of 8 heads, 137 GFLOP, 557 MB, 177 us: 780 TFLOP/s; with zeros for numbers 148); in 4 bits the expansion, which every 128 rows take anew, by the waves that have the
+// products too (4 prompts of 13107 kept rows, 16 answers to each with up to 513 tokens, 124 MB, 59 us, of which the tails' 83 MB 13); over short ones the chain of two
+// launches, a few tiles that each wait for all copies asked for, and the join (16 answers over 3276 rows, 21 MB, 18.4 us).  fp32: 16 answers over 13107 rows 53 to 60 us, of which the products of
+// 32 bits 25, and 39 of one answer, whose tiles of 32 rows are filled to an eighth.
+// Tails are not cut into parts: one of 2048 tokens takes the whole 22 us, of 32768 213 (curdkv_attend_kept 14 and 34), in fp32 81 and 1125 (21 and 64).
 #include <algorithm>
 
 #include "attend_device.h"
@@ -181,7 +185,7 @@ __device__ __forceinline__ void hide(f32x16a (&s)[KB], int far) {
 }
 
 // Tiles of 32 or 64 keys in LDS: four columns of 64 bytes a row, K's pieces of 16 bytes permuted by (row / 2) % 4, and in tiles of 64 keys all by the column: four lanes that store a row
-// in 4 bits have a column each, and would meet the same banks (16 answers over 131072 rows: 78 us without, 68 with).
+// in 4 bits have a column each, and would meet the same banks (16 answers over 131072 rows: 86 us without, 79 with; bf16, which DMA writes in whole lines, 113 either way).
 __device__ __forceinline__ int permuted(int piece, int row, int column, bool keys, int keys_of_tile) {
     return piece ^ (keys_of_tile == 64 ? column : 0) ^ (keys ? (row >> 1) & 3 : 0);
 }

@@ -9,8 +9,9 @@
 // (the first of the tied, ranks of holes and of those that fill them) are counts of bits.  evict_move_kernel copies rows, 16 bytes a lane.
 //
 // Bound by: of many heads, the copy (128 heads of up to 16384 rows, 4096 of which stay and move: 495 MB, 107 us, of which the copy 90 at 5 TB/s); of few heads, one unit's vector
-// instructions, of which one for every row takes 0.25 us at 32768 rows (8 heads, 10 % stay: 28 us, selection 21 and copy 6; 131072 rows 132); of a generated token, a chain of latencies
-// and the launch (32 sequences of 8 heads, one of 3277 rows leaves each: 8.5 us).
+// instructions, of which one for every row takes 0.25 us at 32768 rows (8 heads, 10 % stay: 28 us, selection 21 and copy 6; 131072 rows 125 to 132); of a generated token, a chain of latencies
+// and the launch (32 sequences of 8 heads, one of 3277 rows leaves each: 8.5 us).  That a head is one workgroup's is a choice: the call takes no scratch in which several could meet.  Heads of 16385
+// to 32768 rows hold 32 rows a thread in the 128 registers that 1024 threads leave each, of which 5 spill (24 bytes a lane).
 
 #include <algorithm>
 #include <type_traits>

@@ -12,9 +12,12 @@
 // Which of them: one token over 4097 keys of 8 heads 5.2 us by the first and 5.7 by the second, over 32768 16.5 and 13.8; 8 tokens' 32 rows 17.9 and 13.1 (by the third 20.3); over 131072 keys,
 // past the caches, 46 and 56; 32 tokens over 32768 19 by the second, 23 by the third.  Keys that a window hides from all rows are not read (a token over 131072 with a window of 4096: 13 us).
 // Bound by: few rows, HBM (a token of 32 sequences over up to 4096 rows, 137 MB, 31 us, 4.4 TB/s; one over 131072, 268 MB, 46 us, 5.8); up to 128, HBM at 4.4 TB/s after 3 us of start (32
-// tokens over 32768 keys, 67 MB, 19 us); many rows, the exponentials and sums between the products (2900 clocks a 128 by 64 block, of products 2048) and the power that lowers the clock: a
-// prompt of 8192 tokens, 32 heads, 275 GFLOP, 277 us, 1000 TFLOP/s; fp32 (three ragged prompts of up to 1021 tokens, window 257) 31.5 us, a chain of latencies: a tile's keys, a few stages,
-// the join.
+// tokens over 32768 keys, 67 MB, 19 us); many rows, products and exponentials that wait for each other (a 128 by 64 block has 2048 clocks of products and some 2900 of exponentials and
+// sums, of which little is at the same time: the matrix units are busy for 46 % of the clocks) and, for a seventh, the power that lowers the clock to 2.0 to 2.1 GHz: a prompt of 8192 tokens,
+// 32 heads, 275 GFLOP, 280 to 290 us, 950 to 980 TFLOP/s (with zeros for numbers 244).  128 tokens over 32768 keys, 34 GFLOP, 49 us: a workgroup a tile of keys, 1024 of them two at a time
+// on a unit, each of which loads its keys and goes over four stages, with nothing on its way for the next.  fp32 (three ragged prompts of up to 1021 tokens, window 257) 31.5 us: a workgroup's
+// few stages each wait for their rows, are taken apart and meet two barriers, there being room for one stage.  Generated tokens in fp32: 32 sequences over up to 4096 rows, 270 MB, 61 us, 4.4
+// TB/s; one over 131072, 545 MB, 105 us, 5.2.
 // Each weight is rounded nowhere: scores, exponentials and sums are of 32 bits.
 
 #include <algorithm>
